@@ -16,6 +16,9 @@
  *   sq_count_diff      byte-level audit of two buffers (Sec. 5)
  *   sq_grouped_*       the contractions, projection, merge and adapters over the experts of
  *                      an MoE linear, one launch each (Sec. 3)
+ *   sq_route, sq_sort_tokens, sq_dispatch, sq_combine and their gradients
+ *                      tokens to the experts of an MoE layer and back
+ *   sq_head_loss, sq_head_loss_grad  cross entropy against the vocabulary projection
  *   sq_fit_scale_delta, sq_group_reduce, sq_project_group_delta, sq_control_*,
  *   sq_lowrank_product scale-family variants of the ablation appendix
  * with W[n,k] = code[n,k] * s[n, k / B] decoded on the fly, where (Sec. 2)
@@ -447,6 +450,92 @@ sq_status sq_grouped_project_scales(sq_handle h, const sq_grouped_weight *w, con
  * over all planes). No code byte is read or written. */
 sq_status sq_grouped_merge(sq_handle h, const sq_grouped_weight *w, const float *latent, uint8_t *scales_inout,
                            float *ongrid_delta, int64_t *changed_bytes, void *stream);
+
+/* ---------------------------------------------------------------- routing
+ * What surrounds the grouped calls in an MoE layer: T tokens choose k experts each, the
+ * n = T * k slots t * k + j are sorted by expert, rows travel to their experts and back.
+ * All of it stays on the device and can be captured into a graph; the grouped calls take
+ * their offsets from the host, so a program copies sq_sort_tokens' E + 1 values there.
+ * 1 <= E <= 1024, 1 <= k <= 32, T * k < 2^31; T == 0 is an empty batch. Sums are fp32 in a
+ * fixed order: results do not differ from run to run. */
+
+/* The k largest of each token's router logits, in descending order, equal ones by ascending
+ * expert (k <= E):
+ *   weights[t,j] = exp(z_j) / sum over all experts exp(z)          normalize == 0
+ *   weights[t,j] = exp(z_j) / sum over the chosen experts exp(z)   normalize != 0
+ * logits device [T, E], fp32 or (logits_bf16 != 0) bf16; valid device u8 [T] or NULL: a token
+ * with 0 is not routed (its logits are not read). experts device int32 [T, k], weights device
+ * fp32 [T, k] (both overwritten). A NaN or -inf logit is never chosen and adds nothing to a sum,
+ * +inf counts as the largest finite fp32; a slot without an expert (token not routed, fewer
+ * than k eligible logits) holds expert -1 and weight 0. */
+sq_status sq_route(sq_handle h, int64_t T, int32_t E, int32_t k, int32_t logits_bf16, const void *logits,
+                   const uint8_t *valid, int32_t normalize, int32_t *experts, float *weights, void *stream);
+
+/* Gradient of the logits from that of the weights (normalize and logits as in sq_route, experts
+ * its output): with q the softmax over all experts, or over the chosen ones,
+ *   dlogits[t,e] = q_e ([e chosen] dweights - sum over the chosen q_j dweights_j)
+ * dlogits device [T, E] in the logits' type (overwritten; zero for slots without an expert,
+ * tokens without any, and, with normalize, experts not chosen). dweights of a slot without an
+ * expert is not read into any sum. */
+sq_status sq_route_grad(sq_handle h, int64_t T, int32_t E, int32_t k, int32_t logits_bf16, const void *logits,
+                        const int32_t *experts, const float *dweights, int32_t normalize, void *dlogits,
+                        void *stream);
+
+/* Stable sort of n slots by expert. experts device int32 [n]; a value outside [0, E) is a slot
+ * without an expert. Outputs (device, overwritten): offsets int64 [E + 1], expert e's rows being
+ * offsets[e] .. offsets[e+1]-1 (the grouped calls' layout); row_of int32 [n], the row of each
+ * slot, -1 without an expert; slot_of int32 [n], the slot of each row, -1 for rows >= offsets[E].
+ * n == 0 writes zero offsets. */
+sq_status sq_sort_tokens(sq_handle h, int64_t n, int32_t E, const int32_t *experts, int64_t *offsets, int32_t *row_of,
+                         int32_t *slot_of, void *stream);
+
+/* Rows to the experts: Xs[row_of[t,j]] = X[t]. X device bf16 [T, D] (D % 8 == 0), Xs device bf16
+ * [R, D] with R <= T * k, normally T * k or offsets[E]; row_of [T, k] and slot_of [T * k] as
+ * sq_sort_tokens wrote them. Rows of Xs without a slot (slot_of < 0) are zeroed; indices outside
+ * [0, R) are skipped. In all four calls below a row index outside [0, R) is a slot without an
+ * expert: its rows are neither read nor written, whatever its weight. */
+sq_status sq_dispatch(sq_handle h, int64_t T, int32_t k, int64_t D, int64_t R, const uint16_t *X,
+                      const int32_t *row_of, const int32_t *slot_of, uint16_t *Xs, void *stream);
+
+/* Gradient of sq_dispatch: dX[t] = sum_j dXs[row_of[t,j]], fp32 in the order of j, rounded once.
+ * dXs device bf16 [R, D]; dX device bf16 [T, D] (zero for a token without experts). */
+sq_status sq_dispatch_grad(sq_handle h, int64_t T, int32_t k, int64_t D, int64_t R, const uint16_t *dXs,
+                           const int32_t *row_of, uint16_t *dX, void *stream);
+
+/* Rows back from the experts: Y[t] = sum_j weights[t,j] Ys[row_of[t,j]], fp32 in the order of j,
+ * rounded once. Ys device bf16 [R, D]; weights device fp32 [T, k]; Y device bf16 [T, D]. */
+sq_status sq_combine(sq_handle h, int64_t T, int32_t k, int64_t D, int64_t R, const uint16_t *Ys,
+                     const int32_t *row_of, const float *weights, uint16_t *Y, void *stream);
+
+/* Gradients of sq_combine: dYs[row_of[t,j]] = weights[t,j] dY[t] (bf16; rows without a slot
+ * zeroed) and dweights[t,j] = <dY[t], Ys[row_of[t,j]]> (fp32; 0 without an expert).
+ * dY device bf16 [T, D]; dYs device bf16 [R, D]; dweights device fp32 [T, k]. */
+sq_status sq_combine_grad(sq_handle h, int64_t T, int32_t k, int64_t D, int64_t R, const uint16_t *dY,
+                          const uint16_t *Ys, const int32_t *row_of, const int32_t *slot_of, const float *weights,
+                          uint16_t *dYs, float *dweights, void *stream);
+
+/* ---------------------------------------------------------------- head loss
+ * Softmax cross entropy of hidden rows against the vocabulary projection W, the logits
+ * z[t,v] = sum_d X[t,d] W[v,d] formed tile by tile (fp32 accumulation) and never stored:
+ *   lse[t] = log sum_v exp z[t,v],  loss[t] = lse[t] - z[t, labels[t]]
+ * X device bf16 [T, D]; W device bf16 [V, D], frozen like every weight of this method, so it has
+ * no gradient; D % 8 == 0, D <= 65536, 1 <= V <= 2^24. labels device int64 [T]; a label outside
+ * [0, V) (such as -100) marks a token that is not a target: its row is not read into any result,
+ * its loss and lse are 0 and its dX row is zero. loss, lse device fp32 [T] or NULL (overwritten).
+ * Results do not differ from run to run. Uses scratch of the handle, its size bounded for any T:
+ * the packed rows of up to 16,384 tokens, and with the gradient up to 512 MiB of bf16 exponentials
+ * and the fp32 partial planes of that chunk. */
+sq_status sq_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint16_t *X, const uint16_t *W,
+                       const int64_t *labels, float *loss, float *lse, void *stream);
+
+/* The loss and its gradient in one call: with dloss[t] the gradient of the final loss by loss[t]
+ * (device fp32; 1 / (number of targets) for their mean),
+ *   dX[t] = dloss[t] (sum_v softmax(z[t])_v W[v] - W[labels[t]])
+ * dX device bf16 [T, D] (overwritten; not X). The exponentials are rounded to bf16 as operands of
+ * that product; sums, the label's own term and the final scaling are fp32. */
+sq_status sq_head_loss_grad(sq_handle h, int64_t T, int64_t D, int64_t V, const uint16_t *X, const uint16_t *W,
+                            const int64_t *labels, const float *dloss, float *loss, float *lse, uint16_t *dX,
+                            void *stream);
 
 #ifdef __cplusplus
 }

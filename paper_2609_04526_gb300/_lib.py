@@ -31,7 +31,9 @@ EXPORTS = ("sq_create", "sq_destroy", "sq_status_string", "sq_last_error", "sq_s
            "sq_grouped_bwd_dx", "sq_grouped_scale_grad", "sq_grouped_project_scales", "sq_grouped_merge",
            "sq_grouped_project_lowrank", "sq_grouped_lowrank_grad", "sq_fit_scale_delta", "sq_group_reduce",
            "sq_project_group_delta", "sq_control_fwd", "sq_control_bwd_dx", "sq_control_grad", "sq_lowrank_product",
-           "sq_selftest_wait_timeout", "sq_scale_grad_workspace", "sq_project_planes", "sq_merge_planes")
+           "sq_selftest_wait_timeout", "sq_scale_grad_workspace", "sq_project_planes", "sq_merge_planes",
+           "sq_route", "sq_route_grad", "sq_sort_tokens", "sq_dispatch", "sq_dispatch_grad", "sq_combine",
+           "sq_combine_grad", "sq_head_loss", "sq_head_loss_grad")
 
 
 class SQError(RuntimeError):
@@ -106,6 +108,15 @@ def load() -> ctypes.CDLL:
     L.sq_control_bwd_dx.argtypes = [vp, CW, vp, i64, vp, vp]
     L.sq_control_grad.argtypes = [vp, CW, vp, vp, i64, vp, vp]
     L.sq_lowrank_product.argtypes = [vp, i64, i64, i32, f32, vp, vp, vp, vp]
+    L.sq_route.argtypes = [vp, i64, i32, i32, i32, vp, vp, i32, vp, vp, vp]
+    L.sq_route_grad.argtypes = [vp, i64, i32, i32, i32, vp, vp, vp, i32, vp, vp]
+    L.sq_sort_tokens.argtypes = [vp, i64, i32, vp, vp, vp, vp, vp]
+    L.sq_dispatch.argtypes = [vp, i64, i32, i64, i64, vp, vp, vp, vp, vp]
+    L.sq_dispatch_grad.argtypes = [vp, i64, i32, i64, i64, vp, vp, vp, vp]
+    L.sq_combine.argtypes = [vp, i64, i32, i64, i64, vp, vp, vp, vp, vp]
+    L.sq_combine_grad.argtypes = [vp, i64, i32, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.sq_head_loss.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, vp, vp]
+    L.sq_head_loss_grad.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp]
     for name in EXPORTS:
         if name not in ("sq_status_string", "sq_last_error"):
             getattr(L, name).restype = ctypes.c_int
@@ -169,6 +180,16 @@ def _offsets(offsets, E: int):
 def _ptr(t: Optional[torch.Tensor]):
     if t is None:
         return None
+    return t.data_ptr()
+
+
+def _arg(t: torch.Tensor, name: str, dtype, shape, device=None):
+    """Pointer of a tensor argument that has to be dense, of one type and shape (and device)."""
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, not "
+                         f"{t.dtype} {tuple(t.shape)} with strides {t.stride()}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the other arguments on {device}")
     return t.data_ptr()
 
 
@@ -518,3 +539,154 @@ class Handle:
         self._check(self._L.sq_lowrank_product(self._h, N, G, r, alpha_over_r, _ptr(B), _ptr(A), _ptr(out),
                                                _stream(stream)))
         return out
+
+    # routing -------------------------------------------------------------------
+    def sq_route(self, logits: torch.Tensor, k: int, normalize: bool = True, valid: Optional[torch.Tensor] = None,
+                 experts: Optional[torch.Tensor] = None, weights: Optional[torch.Tensor] = None, stream=None):
+        """Top-k experts (int32 [T, k], -1: none) and weights (fp32 [T, k]) of router logits [T, E]
+        (fp32 or bf16). valid: u8 or bool [T], 0 for tokens that are not routed."""
+        T, E = logits.shape
+        dev = logits.device
+        if experts is None:
+            experts = torch.empty(T, k, dtype=torch.int32, device=dev)
+        if weights is None:
+            weights = torch.empty(T, k, dtype=torch.float32, device=dev)
+        bf16 = logits.dtype == torch.bfloat16
+        if valid is not None:
+            valid = _arg(valid, "valid", torch.bool if valid.dtype == torch.bool else torch.uint8, (T,), dev)
+        self._check(self._L.sq_route(
+            self._h, T, E, k, bf16, _arg(logits, "logits", torch.bfloat16 if bf16 else torch.float32, (T, E)), valid,
+            bool(normalize), _arg(experts, "experts", torch.int32, (T, k), dev),
+            _arg(weights, "weights", torch.float32, (T, k), dev), _stream(stream)))
+        return experts, weights
+
+    def sq_route_grad(self, logits: torch.Tensor, experts: torch.Tensor, dweights: torch.Tensor,
+                      normalize: bool = True, dlogits: Optional[torch.Tensor] = None, stream=None):
+        """Gradient of the router logits, in their type, from that of the weights."""
+        T, E = logits.shape
+        k = experts.shape[1]
+        dev = logits.device
+        if dlogits is None:
+            dlogits = torch.empty_like(logits)
+        bf16 = logits.dtype == torch.bfloat16
+        z = torch.bfloat16 if bf16 else torch.float32
+        self._check(self._L.sq_route_grad(
+            self._h, T, E, k, bf16, _arg(logits, "logits", z, (T, E)), _arg(experts, "experts", torch.int32, (T, k), dev),
+            _arg(dweights, "dweights", torch.float32, (T, k), dev), bool(normalize),
+            _arg(dlogits, "dlogits", z, (T, E), dev), _stream(stream)))
+        return dlogits
+
+    def sq_sort_tokens(self, experts: torch.Tensor, E: int, offsets: Optional[torch.Tensor] = None,
+                       row_of: Optional[torch.Tensor] = None, slot_of: Optional[torch.Tensor] = None, stream=None):
+        """Slots of experts [T, k] sorted by expert: offsets int64 [E + 1] (the grouped calls' offsets,
+        on the device), row_of int32 [T, k] (-1: none) and slot_of int32 [T * k] (-1: no slot)."""
+        dev, n = experts.device, experts.numel()
+        if offsets is None:
+            offsets = torch.empty(E + 1, dtype=torch.int64, device=dev)
+        if row_of is None:
+            row_of = torch.empty(experts.shape, dtype=torch.int32, device=dev)
+        if slot_of is None:
+            slot_of = torch.empty(n, dtype=torch.int32, device=dev)
+        self._check(self._L.sq_sort_tokens(
+            self._h, n, E, _arg(experts, "experts", torch.int32, experts.shape),
+            _arg(offsets, "offsets", torch.int64, (E + 1,), dev), _arg(row_of, "row_of", torch.int32, experts.shape, dev),
+            _arg(slot_of, "slot_of", torch.int32, (n,), dev), _stream(stream)))
+        return offsets, row_of, slot_of
+
+    def sq_dispatch(self, X: torch.Tensor, row_of: torch.Tensor, slot_of: torch.Tensor,
+                    Xs: Optional[torch.Tensor] = None, stream=None):
+        """Xs[row_of[t, j]] = X[t] (bf16 [T, D] -> [R, D], R = T * k unless Xs is given); rows without a
+        slot are zero."""
+        T, D = X.shape
+        k = row_of.shape[1]
+        dev, bf16 = X.device, torch.bfloat16
+        if Xs is None:
+            Xs = torch.empty(T * k, D, dtype=bf16, device=dev)
+        R = Xs.shape[0]
+        self._check(self._L.sq_dispatch(
+            self._h, T, k, D, R, _arg(X, "X", bf16, (T, D)), _arg(row_of, "row_of", torch.int32, (T, k), dev),
+            _arg(slot_of, "slot_of", torch.int32, (T * k,), dev), _arg(Xs, "Xs", bf16, (R, D), dev), _stream(stream)))
+        return Xs
+
+    def sq_dispatch_grad(self, dXs: torch.Tensor, row_of: torch.Tensor, dX: Optional[torch.Tensor] = None,
+                         stream=None):
+        """dX[t] = sum over j of dXs[row_of[t, j]] (bf16 [R, D] -> [T, D])."""
+        R, D = dXs.shape
+        T, k = row_of.shape
+        dev, bf16 = dXs.device, torch.bfloat16
+        if dX is None:
+            dX = torch.empty(T, D, dtype=bf16, device=dev)
+        self._check(self._L.sq_dispatch_grad(
+            self._h, T, k, D, R, _arg(dXs, "dXs", bf16, (R, D)), _arg(row_of, "row_of", torch.int32, (T, k), dev),
+            _arg(dX, "dX", bf16, (T, D), dev), _stream(stream)))
+        return dX
+
+    def sq_combine(self, Ys: torch.Tensor, row_of: torch.Tensor, weights: torch.Tensor,
+                   Y: Optional[torch.Tensor] = None, stream=None):
+        """Y[t] = sum over j of weights[t, j] Ys[row_of[t, j]] (bf16 [R, D] -> [T, D])."""
+        R, D = Ys.shape
+        T, k = row_of.shape
+        dev, bf16 = Ys.device, torch.bfloat16
+        if Y is None:
+            Y = torch.empty(T, D, dtype=bf16, device=dev)
+        self._check(self._L.sq_combine(
+            self._h, T, k, D, R, _arg(Ys, "Ys", bf16, (R, D)), _arg(row_of, "row_of", torch.int32, (T, k), dev),
+            _arg(weights, "weights", torch.float32, (T, k), dev), _arg(Y, "Y", bf16, (T, D), dev), _stream(stream)))
+        return Y
+
+    def sq_combine_grad(self, dY: torch.Tensor, Ys: torch.Tensor, row_of: torch.Tensor, slot_of: torch.Tensor,
+                        weights: torch.Tensor, dYs: Optional[torch.Tensor] = None,
+                        dweights: Optional[torch.Tensor] = None, stream=None):
+        """Gradients of sq_combine from dY [T, D]: dYs bf16 [R, D] and dweights fp32 [T, k]."""
+        R, D = Ys.shape
+        T, k = row_of.shape
+        dev, bf16 = Ys.device, torch.bfloat16
+        if dYs is None:
+            dYs = torch.empty(R, D, dtype=bf16, device=dev)
+        if dweights is None:
+            dweights = torch.empty(T, k, dtype=torch.float32, device=dev)
+        self._check(self._L.sq_combine_grad(
+            self._h, T, k, D, R, _arg(dY, "dY", bf16, (T, D), dev), _arg(Ys, "Ys", bf16, (R, D)),
+            _arg(row_of, "row_of", torch.int32, (T, k), dev), _arg(slot_of, "slot_of", torch.int32, (T * k,), dev),
+            _arg(weights, "weights", torch.float32, (T, k), dev), _arg(dYs, "dYs", bf16, (R, D), dev),
+            _arg(dweights, "dweights", torch.float32, (T, k), dev), _stream(stream)))
+        return dYs, dweights
+
+    # head loss -----------------------------------------------------------------
+    def sq_head_loss(self, X: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, loss: Optional[torch.Tensor] = None,
+                     lse: Optional[torch.Tensor] = None, stream=None):
+        """Cross entropy and log-sum-exp (fp32 [T]) of hidden rows X [T, D] against the vocabulary
+        projection W [V, D] (bf16). labels int64 [T]; outside [0, V): not a target."""
+        T, D = X.shape
+        V = W.shape[0]
+        dev = X.device
+        if loss is None:
+            loss = torch.empty(T, dtype=torch.float32, device=dev)
+        if lse is None:
+            lse = torch.empty(T, dtype=torch.float32, device=dev)
+        self._check(self._L.sq_head_loss(
+            self._h, T, D, V, _arg(X, "X", torch.bfloat16, (T, D)), _arg(W, "W", torch.bfloat16, (V, D), dev),
+            _arg(labels, "labels", torch.int64, (T,), dev), _arg(loss, "loss", torch.float32, (T,), dev),
+            _arg(lse, "lse", torch.float32, (T,), dev), _stream(stream)))
+        return loss, lse
+
+    def sq_head_loss_grad(self, X: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, dloss: torch.Tensor,
+                          loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                          dX: Optional[torch.Tensor] = None, stream=None):
+        """sq_head_loss together with dX (bf16 [T, D]), the gradient of sum(dloss * loss) by X; dloss
+        fp32 [T]. Returns (loss, lse, dX)."""
+        T, D = X.shape
+        V = W.shape[0]
+        dev = X.device
+        if loss is None:
+            loss = torch.empty(T, dtype=torch.float32, device=dev)
+        if lse is None:
+            lse = torch.empty(T, dtype=torch.float32, device=dev)
+        if dX is None:
+            dX = torch.empty(T, D, dtype=torch.bfloat16, device=dev)
+        self._check(self._L.sq_head_loss_grad(
+            self._h, T, D, V, _arg(X, "X", torch.bfloat16, (T, D)), _arg(W, "W", torch.bfloat16, (V, D), dev),
+            _arg(labels, "labels", torch.int64, (T,), dev), _arg(dloss, "dloss", torch.float32, (T,), dev),
+            _arg(loss, "loss", torch.float32, (T,), dev), _arg(lse, "lse", torch.float32, (T,), dev),
+            _arg(dX, "dX", torch.bfloat16, (T, D), dev), _stream(stream)))
+        return loss, lse, dX

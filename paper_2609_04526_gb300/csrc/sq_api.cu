@@ -51,9 +51,11 @@ struct DeviceState {
   int next_table;
   Scratch partial;       // token-split partial planes of the dense scale gradient
   int64_t *plane_acc;    // counter accumulators of the multi-plane calls (zero between calls)
+  Scratch head;          // packed rows, exponentials and partial planes of the head loss
 };
 
 constexpr int64_t kMaxDim = int64_t(1) << 24;       // N, K limit
+constexpr int64_t kMaxHeadDim = 1 << 16;            // hidden width of the head loss
 constexpr int64_t kMaxTokens = (int64_t(1) << 31) - 1;  // TMA coordinates are int32
 
 }  // namespace
@@ -131,9 +133,10 @@ sq_status ensure_device(sq_handle h, DeviceState **out) {
 // box_inner x box_outer tiles; out-of-range elements read as zero and are
 // not written.
 sq_status make_map(sq_handle h, CUtensorMap *map, const void *ptr, CUtensorMapDataType dtype, int elem_bytes,
-                   int64_t inner, int64_t outer, uint32_t box_inner, uint32_t box_outer, CUtensorMapSwizzle swz) {
+                   int64_t inner, int64_t outer, uint32_t box_inner, uint32_t box_outer, CUtensorMapSwizzle swz,
+                   int64_t pitch = 0) {  // elements from row to row (0: inner)
   const cuuint64_t dims[2] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(outer)};
-  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(inner) * elem_bytes};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(pitch ? pitch : inner) * elem_bytes};
   const cuuint32_t box[2] = {box_inner, box_outer};
   const cuuint32_t estr[2] = {1, 1};
   CUresult r = h->encode(map, dtype, 2, const_cast<void *>(ptr), dims, strides, box, estr,
@@ -398,6 +401,109 @@ sq_status run_control(sq_handle h, int mode, const sq_control_weight *w, const v
   a.err = dev->err_word;
   cudaError_t e = sqi::launch_control(a, tmA, tmB, mode == sqi::MODE_SGRAD ? nullptr : &tmOut, dev->sm_count, stream);
   if (e != cudaSuccess) return cuda_fail(h, e, "control kernel launch");
+  return SQ_OK;
+}
+
+// ------------------------------------------------------------------ routing and head loss
+
+sq_status check_route(sq_handle h, int64_t T, int32_t E, int32_t k) {
+  if (E < 1 || E > sqi::kRouteMaxExperts) return fail(h, SQ_ERR_INVALID_ARG, "E=%d must be in [1, 1024]", E);
+  if (k < 1 || k > sqi::kRouteMaxK || k > E) return fail(h, SQ_ERR_INVALID_ARG, "k=%d must be in [1, 32] and <= E=%d", k, E);
+  if (T < 0 || T > kMaxTokens / k) return fail(h, SQ_ERR_INVALID_ARG, "T=%lld: T * k must be in [0, 2^31)", (long long)T);
+  return SQ_OK;
+}
+
+sq_status check_move(sq_handle h, int64_t T, int32_t k, int64_t D, int64_t R) {
+  if (k < 1 || k > sqi::kRouteMaxK) return fail(h, SQ_ERR_INVALID_ARG, "k=%d must be in [1, 32]", k);
+  if (T < 0 || T > kMaxTokens / k) return fail(h, SQ_ERR_INVALID_ARG, "T=%lld: T * k must be in [0, 2^31)", (long long)T);
+  if (D <= 0 || D % 8 != 0 || D > kMaxDim)
+    return fail(h, SQ_ERR_INVALID_ARG, "D=%lld must be positive, a multiple of 8 and <= 2^24", (long long)D);
+  if (T * ((D + 255) / 256) > sqi::kMaxMoveUnits)
+    return fail(h, SQ_ERR_INVALID_ARG, "T=%lld rows of D=%lld are too many for one launch", (long long)T, (long long)D);
+  if (R < 0 || R > T * k)
+    return fail(h, SQ_ERR_INVALID_ARG, "R=%lld expert rows must be in [0, T * k]", (long long)R);
+  return SQ_OK;
+}
+
+// Cross entropy of X against W, and with dX its gradient (see sq_loss.cu).
+sq_status run_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint16_t *X, const uint16_t *W,
+                        const int64_t *labels, const float *dloss, float *loss, float *lse, uint16_t *dX,
+                        cudaStream_t stream) {
+  DeviceState *dev = nullptr;
+  SQ_TRY(ensure_device(h, &dev));
+  if (T == 0) return SQ_OK;
+  auto up = [](int64_t n, int64_t to) { return (n + to - 1) / to * to; };
+  const int64_t piece = std::min<int64_t>(T, sqi::kHeadPiece), whole = up(piece, sqi::kHeadTile);
+  sqi::HeadArgs a = {};
+  a.D = D;
+  a.V = V;
+  a.W = W;
+  a.clusters = dev->sm_count / 2;
+  a.pitch = up(V, 8);  // rows of e start on 16 bytes
+  a.err = dev->err_word;
+  int64_t chunk = whole;
+  if (dX) {
+    const int64_t fit = sqi::kHeadPieceBytes / (2 * a.pitch) / sqi::kHeadTile * sqi::kHeadTile;
+    chunk = std::min(whole, std::max<int64_t>(fit, sqi::kHeadTile));
+  }
+  a.chunk = static_cast<int>(chunk);
+  const int64_t halves = 2 * ((V + sqi::kHeadTile - 1) / sqi::kHeadTile);
+  const int64_t partial_rows = dX ? sqi::head_partial_rows(chunk, D, V, a.clusters) : 0;
+  size_t used = 0;
+  auto take = [&](int64_t bytes) {
+    const size_t at = used;
+    used += static_cast<size_t>(up(bytes, 1024));
+    return at;
+  };
+  const size_t o_count = take(4), o_token = take(4 * piece), o_label = take(4 * piece), o_z = take(4 * piece),
+               o_factors = take(8 * piece), o_rows = take(2 * D * whole), o_sums = take(8 * halves * chunk),
+               o_e = take(dX ? 2 * a.pitch * chunk : 0), o_partial = take(4 * D * partial_rows);
+  SQ_TRY(ensure_scratch(h, dev->head, used, stream, "the head loss"));
+  uint8_t *base = static_cast<uint8_t *>(dev->head.ptr);
+  a.count = reinterpret_cast<int *>(base + o_count);
+  a.token = reinterpret_cast<int *>(base + o_token);
+  a.label = reinterpret_cast<int *>(base + o_label);
+  a.label_z = reinterpret_cast<float *>(base + o_z);
+  a.factors = reinterpret_cast<float2 *>(base + o_factors);
+  a.rows = reinterpret_cast<uint16_t *>(base + o_rows);
+  a.sums = reinterpret_cast<float2 *>(base + o_sums);
+  if (dX) {
+    a.e = reinterpret_cast<uint16_t *>(base + o_e);
+    a.partial = reinterpret_cast<float *>(base + o_partial);
+  }
+  sqi::HeadMaps m;
+  SQ_TRY(make_act_map(h, &m.rows, a.rows, D, whole, 64, 128));
+  SQ_TRY(make_act_map(h, &m.weights, W, D, V, 64, 128));
+  m.e_store = m.e_load = m.partial = m.rows;
+  if (dX) {
+    SQ_TRY(make_map(h, &m.e_store, a.e, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, V, chunk, 32, 32,
+                    CU_TENSOR_MAP_SWIZZLE_64B, a.pitch));
+    SQ_TRY(make_map(h, &m.e_load, a.e, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, V, chunk, 64, 128,
+                    CU_TENSOR_MAP_SWIZZLE_128B, a.pitch));
+    SQ_TRY(make_map(h, &m.partial, a.partial, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, D, partial_rows, 32, 32,
+                    CU_TENSOR_MAP_SWIZZLE_128B));
+  }
+  for (int64_t t = 0; t < T; t += piece) {
+    a.T = static_cast<int>(std::min(piece, T - t));
+    a.X = X + t * D;
+    a.labels = labels + t;
+    a.dloss = dloss ? dloss + t : nullptr;
+    a.loss = loss ? loss + t : nullptr;
+    a.lse = lse ? lse + t : nullptr;
+    a.dX = dX ? dX + t * D : nullptr;
+    cudaError_t e = sqi::launch_head_gather(a, stream);
+    for (int first = 0; first < a.T && e == cudaSuccess; first += a.chunk)
+      e = sqi::launch_head_chunk(a, m, first, dev->sm_count, stream);
+    if (e != cudaSuccess) return cuda_fail(h, e, "head loss launch");
+  }
+  return SQ_OK;
+}
+
+sq_status check_head(sq_handle h, int64_t T, int64_t D, int64_t V) {
+  SQ_TRY(check_tokens(h, T));
+  if (D <= 0 || D % 8 != 0 || D > kMaxHeadDim)
+    return fail(h, SQ_ERR_INVALID_ARG, "D=%lld must be positive, a multiple of 8 and <= 65536", (long long)D);
+  if (V <= 0 || V > kMaxDim) return fail(h, SQ_ERR_INVALID_ARG, "V=%lld must be in [1, 2^24]", (long long)V);
   return SQ_OK;
 }
 
@@ -689,6 +795,7 @@ sq_status sq_destroy(sq_handle h) {
       if (d.plane_acc) cudaFree(d.plane_acc);
       free_scratch(d.workspace);
       free_scratch(d.partial);
+      free_scratch(d.head);
       for (auto &t : d.tables) {
         if (t.done) {
           cudaEventSynchronize(t.done);
@@ -1350,6 +1457,192 @@ sq_status sq_grouped_scale_grad(sq_handle h, const sq_grouped_weight *w, const i
   SQ_TRY(check_buf(h, X, "X"));
   SQ_TRY(check_buf(h, dY, "dY"));
   return run_grouped(h, sqi::MODE_SGRAD, w, rows, offsets, dY, X, g, mask, st);
+  SQ_GUARD_END
+}
+
+sq_status sq_route(sq_handle h, int64_t T, int32_t E, int32_t k, int32_t logits_bf16, const void *logits,
+                   const uint8_t *valid, int32_t normalize, int32_t *experts, float *weights, void *stream) {
+  if (!h) return SQ_ERR_INVALID_ARG;
+  SQ_GUARD_BEGIN
+  SQ_TRY(check_route(h, T, E, k));
+  if (T > 0) {
+    SQ_TRY(check_buf(h, logits, "logits"));
+    SQ_TRY(check_buf(h, experts, "experts"));
+    SQ_TRY(check_buf(h, weights, "weights"));
+    if (!aligned16(valid)) return fail(h, SQ_ERR_INVALID_ARG, "valid must be 16-byte aligned");
+  }
+  DeviceState *dev = nullptr;
+  SQ_TRY(ensure_device(h, &dev));
+  if (T == 0) return SQ_OK;
+  cudaError_t e = sqi::launch_route(T, E, k, logits_bf16 != 0, logits, valid, normalize != 0, experts, weights,
+                                    static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(h, e, "router launch");
+  return SQ_OK;
+  SQ_GUARD_END
+}
+
+sq_status sq_route_grad(sq_handle h, int64_t T, int32_t E, int32_t k, int32_t logits_bf16, const void *logits,
+                        const int32_t *experts, const float *dweights, int32_t normalize, void *dlogits,
+                        void *stream) {
+  if (!h) return SQ_ERR_INVALID_ARG;
+  SQ_GUARD_BEGIN
+  SQ_TRY(check_route(h, T, E, k));
+  if (T > 0) {
+    SQ_TRY(check_buf(h, logits, "logits"));
+    SQ_TRY(check_buf(h, experts, "experts"));
+    SQ_TRY(check_buf(h, dweights, "dweights"));
+    SQ_TRY(check_buf(h, dlogits, "dlogits"));
+  }
+  DeviceState *dev = nullptr;
+  SQ_TRY(ensure_device(h, &dev));
+  if (T == 0) return SQ_OK;
+  cudaError_t e = sqi::launch_route_grad(T, E, k, logits_bf16 != 0, logits, experts, dweights, normalize != 0, dlogits,
+                                         static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(h, e, "router gradient launch");
+  return SQ_OK;
+  SQ_GUARD_END
+}
+
+sq_status sq_sort_tokens(sq_handle h, int64_t n, int32_t E, const int32_t *experts, int64_t *offsets, int32_t *row_of,
+                         int32_t *slot_of, void *stream) {
+  if (!h) return SQ_ERR_INVALID_ARG;
+  SQ_GUARD_BEGIN
+  if (E < 1 || E > sqi::kRouteMaxExperts) return fail(h, SQ_ERR_INVALID_ARG, "E=%d must be in [1, 1024]", E);
+  if (n < 0 || n > kMaxTokens) return fail(h, SQ_ERR_INVALID_ARG, "n=%lld slots out of range [0, 2^31)", (long long)n);
+  SQ_TRY(check_buf(h, offsets, "offsets"));
+  if (n > 0) {
+    SQ_TRY(check_buf(h, experts, "experts"));
+    SQ_TRY(check_buf(h, row_of, "row_of"));
+    SQ_TRY(check_buf(h, slot_of, "slot_of"));
+  }
+  DeviceState *dev = nullptr;
+  SQ_TRY(ensure_device(h, &dev));
+  cudaError_t e = sqi::launch_sort(n, E, experts, offsets, row_of, slot_of, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(h, e, "sort launch");
+  return SQ_OK;
+  SQ_GUARD_END
+}
+
+sq_status sq_dispatch(sq_handle h, int64_t T, int32_t k, int64_t D, int64_t R, const uint16_t *X,
+                      const int32_t *row_of, const int32_t *slot_of, uint16_t *Xs, void *stream) {
+  if (!h) return SQ_ERR_INVALID_ARG;
+  SQ_GUARD_BEGIN
+  SQ_TRY(check_move(h, T, k, D, R));
+  if (R > 0) {
+    SQ_TRY(check_buf(h, X, "X"));
+    SQ_TRY(check_buf(h, row_of, "row_of"));
+    SQ_TRY(check_buf(h, slot_of, "slot_of"));
+    SQ_TRY(check_buf(h, Xs, "Xs"));
+  }
+  DeviceState *dev = nullptr;
+  SQ_TRY(ensure_device(h, &dev));
+  if (R == 0) return SQ_OK;
+  cudaError_t e = sqi::launch_dispatch(T, k, D, R, X, row_of, slot_of, Xs, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(h, e, "dispatch launch");
+  return SQ_OK;
+  SQ_GUARD_END
+}
+
+sq_status sq_combine(sq_handle h, int64_t T, int32_t k, int64_t D, int64_t R, const uint16_t *Ys,
+                     const int32_t *row_of, const float *weights, uint16_t *Y, void *stream) {
+  if (!h) return SQ_ERR_INVALID_ARG;
+  SQ_GUARD_BEGIN
+  SQ_TRY(check_move(h, T, k, D, R));
+  if (T > 0) {
+    if (R > 0) SQ_TRY(check_buf(h, Ys, "Ys"));
+    SQ_TRY(check_buf(h, row_of, "row_of"));
+    SQ_TRY(check_buf(h, weights, "weights"));
+    SQ_TRY(check_buf(h, Y, "Y"));
+  }
+  DeviceState *dev = nullptr;
+  SQ_TRY(ensure_device(h, &dev));
+  if (T == 0) return SQ_OK;
+  cudaError_t e = sqi::launch_combine(T, k, D, R, Ys, row_of, weights, Y, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(h, e, "combine launch");
+  return SQ_OK;
+  SQ_GUARD_END
+}
+
+sq_status sq_dispatch_grad(sq_handle h, int64_t T, int32_t k, int64_t D, int64_t R, const uint16_t *dXs,
+                           const int32_t *row_of, uint16_t *dX, void *stream) {
+  if (!h) return SQ_ERR_INVALID_ARG;
+  SQ_GUARD_BEGIN
+  SQ_TRY(check_move(h, T, k, D, R));
+  if (T > 0) {
+    if (R > 0) SQ_TRY(check_buf(h, dXs, "dXs"));
+    SQ_TRY(check_buf(h, row_of, "row_of"));
+    SQ_TRY(check_buf(h, dX, "dX"));
+  }
+  DeviceState *dev = nullptr;
+  SQ_TRY(ensure_device(h, &dev));
+  if (T == 0) return SQ_OK;
+  cudaError_t e = sqi::launch_combine(T, k, D, R, dXs, row_of, nullptr, dX, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(h, e, "dispatch gradient launch");
+  return SQ_OK;
+  SQ_GUARD_END
+}
+
+sq_status sq_combine_grad(sq_handle h, int64_t T, int32_t k, int64_t D, int64_t R, const uint16_t *dY,
+                          const uint16_t *Ys, const int32_t *row_of, const int32_t *slot_of, const float *weights,
+                          uint16_t *dYs, float *dweights, void *stream) {
+  if (!h) return SQ_ERR_INVALID_ARG;
+  SQ_GUARD_BEGIN
+  SQ_TRY(check_move(h, T, k, D, R));
+  if (T > 0) {
+    SQ_TRY(check_buf(h, dY, "dY"));
+    if (R > 0) {
+      SQ_TRY(check_buf(h, Ys, "Ys"));
+      SQ_TRY(check_buf(h, dYs, "dYs"));
+    }
+    SQ_TRY(check_buf(h, row_of, "row_of"));
+    SQ_TRY(check_buf(h, slot_of, "slot_of"));
+    SQ_TRY(check_buf(h, weights, "weights"));
+    SQ_TRY(check_buf(h, dweights, "dweights"));
+  }
+  DeviceState *dev = nullptr;
+  SQ_TRY(ensure_device(h, &dev));
+  if (T == 0) return SQ_OK;
+  cudaError_t e = sqi::launch_combine_grad(T, k, D, R, dY, Ys, row_of, slot_of, weights, dYs, dweights, dev->sm_count,
+                                           static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(h, e, "combine gradient launch");
+  return SQ_OK;
+  SQ_GUARD_END
+}
+
+sq_status sq_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint16_t *X, const uint16_t *W,
+                       const int64_t *labels, float *loss, float *lse, void *stream) {
+  if (!h) return SQ_ERR_INVALID_ARG;
+  SQ_GUARD_BEGIN
+  SQ_TRY(check_head(h, T, D, V));
+  if (!loss && !lse) return fail(h, SQ_ERR_INVALID_ARG, "loss and lse are both NULL");
+  if (T > 0) {
+    SQ_TRY(check_buf(h, X, "X"));
+    SQ_TRY(check_buf(h, W, "W"));
+    SQ_TRY(check_buf(h, labels, "labels"));
+  }
+  if (!aligned16(loss)) return fail(h, SQ_ERR_INVALID_ARG, "loss must be 16-byte aligned");
+  if (!aligned16(lse)) return fail(h, SQ_ERR_INVALID_ARG, "lse must be 16-byte aligned");
+  return run_head_loss(h, T, D, V, X, W, labels, nullptr, loss, lse, nullptr, static_cast<cudaStream_t>(stream));
+  SQ_GUARD_END
+}
+
+sq_status sq_head_loss_grad(sq_handle h, int64_t T, int64_t D, int64_t V, const uint16_t *X, const uint16_t *W,
+                            const int64_t *labels, const float *dloss, float *loss, float *lse, uint16_t *dX,
+                            void *stream) {
+  if (!h) return SQ_ERR_INVALID_ARG;
+  SQ_GUARD_BEGIN
+  SQ_TRY(check_head(h, T, D, V));
+  if (T > 0) {
+    SQ_TRY(check_buf(h, X, "X"));
+    SQ_TRY(check_buf(h, W, "W"));
+    SQ_TRY(check_buf(h, labels, "labels"));
+    SQ_TRY(check_buf(h, dloss, "dloss"));
+    SQ_TRY(check_buf(h, dX, "dX"));
+    if (X == dX) return fail(h, SQ_ERR_INVALID_ARG, "dX must not be X");
+  }
+  if (!aligned16(loss)) return fail(h, SQ_ERR_INVALID_ARG, "loss must be 16-byte aligned");
+  if (!aligned16(lse)) return fail(h, SQ_ERR_INVALID_ARG, "lse must be 16-byte aligned");
+  return run_head_loss(h, T, D, V, X, W, labels, dloss, loss, lse, dX, static_cast<cudaStream_t>(stream));
   SQ_GUARD_END
 }
 

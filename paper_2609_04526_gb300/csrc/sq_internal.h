@@ -359,6 +359,96 @@ cudaError_t launch_project_group_delta(int fmt, int64_t N, int64_t G, int64_t gd
                                        const float *delta, uint8_t *bytes_out, uint8_t *mask_out, int32_t *nonfinite,
                                        float *latent_out, int sm_count, cudaStream_t stream);
 
+// Token routing (sq_route.cu): router logits [T, E] (fp32 or bf16) to the top-k experts and
+// weights, and their gradient; the n = T * k slots sorted by expert; rows to the experts and back.
+constexpr int kRouteMaxExperts = 1024;  // 32 logits a lane; the sort's histograms fit shared memory
+constexpr int kRouteMaxK = 32;          // a token's slots are the lanes of a warp
+constexpr int64_t kMaxMoveUnits = (int64_t(1) << 31) - 8;  // 256-column pieces of all tokens
+cudaError_t launch_route(int64_t T, int E, int k, bool bf16, const void *logits, const uint8_t *valid, bool normalize,
+                         int *experts, float *weights, cudaStream_t stream);
+cudaError_t launch_route_grad(int64_t T, int E, int k, bool bf16, const void *logits, const int *experts,
+                              const float *dweights, bool normalize, void *dlogits, cudaStream_t stream);
+cudaError_t launch_sort(int64_t n, int E, const int *experts, int64_t *offsets, int *row_of, int *slot_of,
+                        cudaStream_t stream);
+cudaError_t launch_dispatch(int64_t T, int k, int64_t D, int64_t rows, const uint16_t *X, const int *row_of,
+                            const int *slot_of, uint16_t *Xs, cudaStream_t stream);
+cudaError_t launch_combine(int64_t T, int k, int64_t D, int64_t rows, const uint16_t *Ys, const int *row_of,
+                           const float *weights, uint16_t *Y, cudaStream_t stream);
+cudaError_t launch_combine_grad(int64_t T, int k, int64_t D, int64_t rows, const uint16_t *dY, const uint16_t *Ys,
+                                const int *row_of, const int *slot_of, const float *weights, uint16_t *dYs,
+                                float *dweights, int sm_count, cudaStream_t stream);
+
+// Cross entropy against a vocabulary projection W [V, D] (sq_loss.cu). A call runs over pieces of
+// kHeadPiece tokens, a piece's labelled tokens over chunks whose exponentials fit
+// kHeadPieceBytes of scratch.
+constexpr int kHeadTile = 256;
+constexpr int kHeadPiece = 16384;
+constexpr int64_t kHeadPieceBytes = int64_t(512) << 20;
+constexpr int kMaxHeadParts = 32;
+constexpr int kMinHeadPartStages = 8;  // a part of the vocabulary is at least 8 x 128 entries long
+
+// Vocabulary parts of a gradient launch of `tiles` tiles: with w(s) = ceil(tiles s / clusters) / s
+// the launch's length in whole tiles per cluster, the smallest s within 3 % of the smallest w (each
+// part writes and reads back an fp32 plane of the tile).
+__host__ __device__ inline int head_parts(int64_t tiles, int stages, int clusters) {
+  if (tiles <= 0 || clusters <= 0) return 1;
+  int most = stages / kMinHeadPartStages;
+  most = most < 1 ? 1 : (most > kMaxHeadParts ? kMaxHeadParts : most);
+  // w(s) / w(1) compared as fractions: ceil(tiles s / clusters) / s
+  int64_t best_n = 1, best_d = 0;  // infinite
+  for (int s = 1; s <= most; ++s) {
+    const int64_t n = (tiles * s + clusters - 1) / clusters;
+    if (best_d == 0 || n * best_d < best_n * s) best_n = n, best_d = s;
+  }
+  for (int s = 1; s < most; ++s) {
+    const int64_t n = (tiles * s + clusters - 1) / clusters;
+    if (100 * n * best_d <= 103 * best_n * s) return s;
+  }
+  return most;
+}
+// Rows of 4 * D bytes that the parts of at most `chunk` rows take.
+inline int64_t head_partial_rows(int64_t chunk, int64_t D, int64_t V, int clusters) {
+  int64_t most = 0;
+  for (int64_t m = 1; m <= chunk / kHeadTile; ++m) {
+    const int64_t rows =
+        m * kHeadTile * head_parts(m * ((D + kHeadTile - 1) / kHeadTile), static_cast<int>((V + 127) / 128), clusters);
+    most = rows > most ? rows : most;
+  }
+  return most;
+}
+
+struct HeadArgs {
+  int T;                  // tokens of the piece
+  int64_t D, V;
+  const uint16_t *X;      // [T, D] bf16
+  const uint16_t *W;      // [V, D] bf16
+  const int64_t *labels;  // [T]; outside [0, V): no label
+  const float *dloss;     // [T] (gradient)
+  float *loss, *lse;      // [T] or null
+  uint16_t *dX;           // [T, D] bf16, or null: no gradient
+  int chunk;              // rows of a chunk, a multiple of kHeadTile
+  int clusters;           // for head_parts
+  int64_t pitch;          // elements of a row of e
+  // scratch, by compact row of the piece
+  int *count;             // labelled tokens of the piece
+  int *token, *label;
+  float *label_z;
+  float2 *factors;
+  uint16_t *rows;         // [T, D] the labelled tokens' rows of X
+  // scratch, by row of the chunk
+  float2 *sums;           // [chunk, 2 * column tiles] sum and reference of each half tile
+  uint16_t *e;            // [chunk, pitch] bf16 exponentials (gradient)
+  float *partial;         // [parts, rows, D] fp32 (gradient)
+  int *err;
+};
+// rows and weights: 64 x 128 boxes, 128-byte swizzle; e_store 32 x 32, 64-byte swizzle; partial
+// 32 x 32 fp32, 128-byte swizzle.
+struct HeadMaps {
+  CUtensorMap rows, weights, e_store, e_load, partial;
+};
+cudaError_t launch_head_gather(const HeadArgs &a, cudaStream_t stream);
+cudaError_t launch_head_chunk(const HeadArgs &a, const HeadMaps &m, int first, int sm_count, cudaStream_t stream);
+
 // Device-side error codes written to the error word.
 constexpr int kErrWaitTimeout = 1;
 

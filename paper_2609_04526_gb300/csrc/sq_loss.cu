@@ -1,0 +1,545 @@
+// Softmax cross entropy of hidden rows against a frozen vocabulary projection, with the gradient
+// of the rows (sm_103a):
+//
+//   z = X W^T,  loss = log sum_v exp z_v - z_label,  dX = g (softmax(z) - onehot(label)) W
+//
+// The logits exist only as accumulator tiles in tensor memory. Per piece of labelled tokens:
+//
+//   gather    the labelled tokens' rows, packed, and each row's label logit z_l (CUDA cores)
+//   logits    z tile by tile; the epilogue forms e = 2^(z log2(e) - r), adds e over 128 columns
+//             and, for the gradient, writes bf16 e of the piece
+//   finalize  sums -> loss, log-sum-exp and the row's two gradient factors
+//   gradient  (e W) over the vocabulary, cut into parts where few tiles would leave SMs idle
+//   rows      dX = g / S (e W) - g (S - e_l) / S W[label]
+//
+// The reference r of a row is ceil(z_l log2(e)), known before the product: e then needs no
+// maximum first, and e W no second pass over the logits once S is known. Where a tile holds a
+// logit more than 2^100 above it (a label of probability below 2^-100), that half tile alone
+// takes its own maximum as reference, and finalize rescales the row's e. References are whole
+// powers of two, so such a change of reference is exact. Terms more than 2^126 below the label's
+// own vanish.
+//
+// The label's own term is left out of e and of the sums and carried in fp32: p_label - 1 is
+// -(S - e_l) / S without cancellation, so confident tokens keep an accurate loss and gradient.
+// e is rounded to bf16 once, as an operand of the tensor cores (relative 2^-9 per term, far
+// below the rounding of the bf16 gradient once summed); the sums S take the unrounded values.
+#include "sq_gemm_kernels.cuh"
+
+namespace sqi {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kRefSlack = 100.f;  // a logit this far above the reference (in powers of two) moves it
+
+struct HeadCfg {
+  static constexpr int kEpiWarps = 8;  // warp w: TMEM lanes 32 (w % 4) .. + 31, columns 128 (w / 4) .. + 127
+  static constexpr int kTmaWarp = kEpiWarps;
+  static constexpr int kMmaWarp = kTmaWarp + 1;
+  static constexpr int kThreads = 32 * (kMmaWarp + 1);
+  static constexpr int kBK = 128;  // contraction indices of a stage
+  static constexpr int kStages = 3;
+  static constexpr int kA = 128 * kBK * 2;  // this CTA's 128 rows
+  static constexpr int kB = 128 * kBK * 2;  // this CTA's 128 columns
+  static constexpr int kStageBytes = kA + kB;
+  static constexpr uint32_t kTx = 2 * kStageBytes;  // both CTAs' tiles, on the leader's barrier
+  static constexpr int kTile = kHeadTile;
+  static constexpr int kOffBox = kStages * kStageBytes;
+  static constexpr int kBoxBytes = 4096;  // 32 rows x 32 fp32 (or bf16) columns of a warp
+  static constexpr int kOffBar = kOffBox + kEpiWarps * kBoxBytes;
+  static constexpr int kSmemBytes = kOffBar + 512 + 1024;
+};
+static_assert(HeadCfg::kSmemBytes <= 232448, "head kernel exceeds the opt-in shared memory of one CTA");
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// 2^d of a whole d <= 0, exactly; 0 where it is not a normal number.
+__device__ __forceinline__ float whole_exp2(float d) {
+  return d < -126.f ? 0.f : __int_as_float((127 + static_cast<int>(d)) << 23);
+}
+
+__device__ __forceinline__ float warp_total(float v) {
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+  return v;
+}
+
+// Reference exponent of a row from its label logit in powers of two; never -inf, and a NaN logit
+// leaves a number here (the row's NaN reaches its results through the label's own term).
+__device__ __forceinline__ float row_reference(float label_z) { return fmaxf(ceilf(label_z * kLog2e), -1e30f); }
+
+// Rows of the piece's chunk that starts at compact row `first`.
+__device__ __forceinline__ int chunk_rows(const HeadArgs &a, int first) {
+  const int left = *a.count - first;
+  return left < 0 ? 0 : (left < a.chunk ? left : a.chunk);
+}
+
+// ---------------------------------------------------------------- gather
+
+// Eight tokens per CTA, one warp each. The labelled ones are packed in order (each CTA counts
+// the labels before its own), so rows without a label cost nothing later and what they hold
+// reaches no product.
+__global__ void __launch_bounds__(256) sq_head_gather_kernel(const HeadArgs a) {
+  __shared__ int before[8];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int t0 = blockIdx.x * 8, t = t0 + warp;
+  auto labelled = [&](int i) {
+    const int64_t y = a.labels[i];
+    return y >= 0 && y < a.V;
+  };
+  int seen = 0;
+  for (int i = threadIdx.x; i < t0; i += 256) seen += labelled(i);
+  const bool own = lane < 8 && t0 + lane < a.T && labelled(t0 + lane);
+  const uint32_t here = __ballot_sync(0xFFFFFFFFu, own);  // the same in every warp
+  seen = __reduce_add_sync(0xFFFFFFFFu, seen);
+  if (lane == 0) before[warp] = seen;
+  __syncthreads();
+  int row = __popc(here & ((1u << warp) - 1));
+#pragma unroll
+  for (int w = 0; w < 8; ++w) row += before[w];
+  if (t == a.T - 1 && lane == 0) *a.count = row + ((here >> warp) & 1);
+  if (t >= a.T) return;
+  const int pieces = static_cast<int>(a.D / 8);
+  if (!((here >> warp) & 1)) {
+    if (a.dX) {
+      uint4 *out = reinterpret_cast<uint4 *>(a.dX + static_cast<int64_t>(t) * a.D);
+      for (int i = lane; i < pieces; i += 32) out[i] = make_uint4(0, 0, 0, 0);
+    }
+    if (lane == 0) {
+      if (a.loss) a.loss[t] = 0.f;
+      if (a.lse) a.lse[t] = 0.f;
+    }
+    return;
+  }
+  const int64_t y = a.labels[t];
+  const uint4 *x = reinterpret_cast<const uint4 *>(a.X + static_cast<int64_t>(t) * a.D);
+  const uint4 *w = reinterpret_cast<const uint4 *>(a.W + y * a.D);
+  uint4 *out = reinterpret_cast<uint4 *>(a.rows + static_cast<int64_t>(row) * a.D);
+  float dot = 0.f;
+#pragma unroll 4
+  for (int i = lane; i < pieces; i += 32) {
+    const uint4 p = __ldg(x + i), q = __ldg(w + i);
+    out[i] = p;
+    const uint32_t pw[4] = {p.x, p.y, p.z, p.w}, qw[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      dot = fmaf(__uint_as_float(pw[c] << 16), __uint_as_float(qw[c] << 16), dot);
+      dot = fmaf(__uint_as_float(pw[c] & 0xFFFF0000u), __uint_as_float(qw[c] & 0xFFFF0000u), dot);
+    }
+  }
+  dot = warp_total(dot);
+  if (lane == 0) {
+    a.token[row] = t;
+    a.label[row] = static_cast<int>(y);
+    a.label_z[row] = dot;
+  }
+}
+
+// ---------------------------------------------------------------- contractions
+//
+// Both contractions run as CTA pairs (tcgen05.mma.cta_group::2, 256 x 256 tiles, two fp32
+// accumulators in tensor memory, so a tile's epilogue runs under the next tile's MMAs).
+//   logits:   D[t, v] = sum_d X[t, d] W[v, d]   both operands K-major
+//   gradient: D[t, d] = sum_v e[t, v] W[v, d]   e K-major, W MN-major; a unit is a tile over a
+//             part of the vocabulary and writes its own fp32 plane, added in order later
+
+struct HeadTile {
+  int tm, tn, part, k0, nk;  // row tile, column tile, vocabulary part, first stage and stages
+};
+
+template <bool GRAD>
+__device__ __forceinline__ HeadTile head_tile(int unit, int tiles_m, int tiles_n, int parts, int stages) {
+  HeadTile t;
+  const int per = tiles_m * tiles_n;
+  t.part = GRAD ? unit / per : 0;
+  tile_coords<8>(unit - t.part * per, tiles_m, tiles_n, t.tm, t.tn);
+  t.k0 = GRAD ? static_cast<int>(static_cast<int64_t>(stages) * t.part / parts) : 0;
+  t.nk = GRAD ? static_cast<int>(static_cast<int64_t>(stages) * (t.part + 1) / parts) - t.k0 : stages;
+  return t;
+}
+
+template <bool GRAD>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg::kThreads, 1)
+    sq_head_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                   const __grid_constant__ CUtensorMap tmO, const HeadArgs a, const int first) {
+  using C = HeadCfg;
+  constexpr int S = C::kStages;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t *full = reinterpret_cast<uint64_t *>(smem + C::kOffBar);  // [S] leader: both CTAs' tiles landed
+  uint64_t *empty = full + S;    // [S] the pair's MMAs have read the stage        (multicast commit)
+  uint64_t *tfull = empty + S;   // [2] accumulator complete                       (multicast commit)
+  uint64_t *tempty = tfull + 2;  // [2] leader: both epilogues drained it (kEpiWarps arrivals + the peer's st.async)
+  uint64_t *drain = tempty + 2;
+  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(drain + 1);
+  volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
+  uint32_t *sink = reinterpret_cast<uint32_t *>(drain + 2);  // [kEpiWarps] leader: st.async targets
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const int cluster = blockIdx.x >> 1, nclusters = gridDim.x >> 1;
+  const int tiles_m = (chunk_rows(a, first) + C::kTile - 1) / C::kTile;
+  const int tiles_n = static_cast<int>(((GRAD ? a.D : a.V) + C::kTile - 1) / C::kTile);
+  const int stages = static_cast<int>(((GRAD ? a.V : a.D) + C::kBK - 1) / C::kBK);
+  const int parts = GRAD ? head_parts(static_cast<int64_t>(tiles_m) * tiles_n, stages, a.clusters) : 1;
+  const int total = tiles_m * tiles_n * parts;
+
+  auto stage_a = [&](int s) { return smem + s * C::kStageBytes; };
+  auto stage_b = [&](int s) { return smem + s * C::kStageBytes + C::kA; };
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&tfull[b], 1);
+      mbar_init(&tempty[b], C::kEpiWarps);
+    }
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    fence_barrier_init();
+  }
+  if (warp == C::kMmaWarp) tmem_alloc_pair(tmem_slot, 2 * kTmemCols);
+  if (warp == C::kTmaWarp && lane == 0) {
+    tma_prefetch_desc(&tmA);
+    tma_prefetch_desc(&tmB);
+    tma_prefetch_desc(&tmO);
+  }
+  tc_fence_before();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+
+  if (warp == C::kTmaWarp) {
+    // ------------------------------------------------------ TMA producer (both CTAs)
+    if (lane == 0) {
+      int it = 0;
+      bool ok = true;
+      for (int unit = cluster; unit < total && ok; unit += nclusters) {
+        const HeadTile t = head_tile<GRAD>(unit, tiles_m, tiles_n, parts, stages);
+        const int32_t row0 = (GRAD ? 0 : first) + t.tm * C::kTile + 128 * static_cast<int32_t>(rank);
+        const int32_t col0 = t.tn * C::kTile + 128 * static_cast<int32_t>(rank);
+        for (int kb = t.k0; kb < t.k0 + t.nk; ++kb, ++it) {
+          const int s = it % S;
+          const uint32_t use = static_cast<uint32_t>(it / S);
+          if (it >= S && !(ok = mbar_wait(&empty[s], (use & 1u) ^ 1u, abort_flag, a.err))) break;
+          if (rank == 0) mbar_arrive_expect_tx(&full[s], C::kTx);
+          const uint32_t bar = mapa_shared(smem_u32(&full[s]), 0);
+          for (int j = 0; j < 2; ++j)
+            tma_load_2d_pair(smem_u32(stage_a(s)) + j * 16384, &tmA, bar, kb * C::kBK + 64 * j, row0);
+          for (int j = 0; j < 2; ++j) {
+            if (GRAD)  // 64 columns of D x 128 vocabulary rows
+              tma_load_2d_pair(smem_u32(stage_b(s)) + j * 16384, &tmB, bar, col0 + 64 * j, kb * C::kBK);
+            else  // 128 vocabulary rows x 64 columns of D
+              tma_load_2d_pair(smem_u32(stage_b(s)) + j * 16384, &tmB, bar, kb * C::kBK + 64 * j, col0);
+          }
+        }
+      }
+      if (*abort_flag && rank == 0) {
+        for (int i = (it > S ? it - S : 0); i < it; ++i) mbar_drain(&full[i % S], static_cast<uint32_t>(i / S) & 1u);
+      }
+    }
+  } else if (warp == C::kMmaWarp) {
+    // ------------------------------------------------------ MMA issuer (leader CTA)
+    if (lane == 0 && rank == 0) {
+      constexpr uint32_t idesc = idesc_bf16(2 * 128, C::kTile, 0, GRAD ? 1 : 0);
+      // K-major: K step kk in 64-wide chunk kk / 4 (16 KiB apart), byte 32 (kk % 4) of each row;
+      // MN-major: 16 contraction rows (2 KiB) per step, 64-column atoms 16 KiB apart
+      const uint64_t ad_base = smem_desc_sw128(smem_u32(stage_a(0)), 16, 1024);
+      const uint64_t bd_base = smem_desc_sw128(smem_u32(stage_b(0)), GRAD ? 16384 : 16, 1024);
+      int s = 0, tc = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      for (int unit = cluster; unit < total && ok; unit += nclusters, ++tc) {
+        const HeadTile t = head_tile<GRAD>(unit, tiles_m, tiles_n, parts, stages);
+        const int ab = tc & 1;
+        const uint32_t au = static_cast<uint32_t>(tc >> 1);
+        if (tc >= 2 && !(ok = mbar_spin_cluster(&tempty[ab], (au & 1u) ^ 1u, abort_flag, a.err))) break;
+        tc_fence_after();
+        const uint32_t d_tmem = tmem_base + ab * kTmemCols;
+        for (int kb = 0; kb < t.nk; ++kb) {
+          if (!(ok = mbar_spin(&full[s], ph, abort_flag, a.err))) break;
+          const uint64_t so = static_cast<uint64_t>(s * (C::kStageBytes >> 4));
+          const uint64_t a0 = ad_base + so, b0 = bd_base + so;
+#pragma unroll
+          for (int kk = 0; kk < C::kBK / 16; ++kk) {
+            const uint32_t ka = ((kk >> 2) * 16384 + (kk & 3) * 32) >> 4;
+            const uint32_t kb_ = GRAD ? (kk * 2048) >> 4 : ka;
+            umma_bf16_pair(d_tmem, a0 + ka, b0 + kb_, idesc, (kb > 0 || kk > 0) ? 1u : 0u);
+          }
+          umma_commit_pair_mc(&empty[s]);
+          if (++s == S) {
+            s = 0;
+            ph ^= 1u;
+          }
+        }
+        if (ok) umma_commit_pair_mc(&tfull[ab]);
+      }
+      umma_commit_pair(drain);
+      mbar_drain(drain, 0);
+    }
+  } else {
+    // ------------------------------------------------------ epilogue (warps 0-7, both CTAs)
+    const int quad = warp & 3, half = warp >> 2;
+    const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + half * 128;
+    const uint32_t box = smem_u32(smem + C::kOffBox + warp * C::kBoxBytes);
+    int tc = 0;
+    for (int unit = cluster; unit < total; unit += nclusters, ++tc) {
+      const HeadTile t = head_tile<GRAD>(unit, tiles_m, tiles_n, parts, stages);
+      const int ab = tc & 1;
+      const int row32 = t.tm * C::kTile + 128 * static_cast<int>(rank) + 32 * quad;  // of the chunk
+      const int col0 = t.tn * C::kTile + 128 * half;
+      const int row = first + row32 + lane;
+      int label = -1;
+      float ref = 0.f;
+      if (!GRAD && row < *a.count) {
+        label = a.label[row];
+        ref = row_reference(a.label_z[row]);
+      }
+      if (!mbar_wait(&tfull[ab], static_cast<uint32_t>(tc >> 1) & 1u, abort_flag, a.err)) break;
+      tc_fence_after();
+      const uint32_t t_buf = t_row + ab * kTmemCols;
+      if constexpr (GRAD) {
+        const int32_t out_row = t.part * tiles_m * C::kTile + row32;
+#pragma unroll 1
+        for (int g = 0; g < 4; ++g) {
+          uint32_t v[32];
+          tmem_ld32(t_buf + 32 * g, v);
+          tmem_ld_wait();
+          if (lane == 0) bulk_wait_read<0>();  // the previous box's store has read the buffer
+          __syncwarp();
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+            st_shared_v4(box + lane * 128 + ((q ^ (lane & 7)) << 4), v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+          fence_proxy_async_smem();  // the box -> async proxy (the TMA store)
+          __syncwarp();
+          if (lane == 0) {
+            if (col0 + 32 * g < a.D) tma_store_2d(&tmO, box, col0 + 32 * g, out_row);
+            bulk_commit_group();
+          }
+        }
+      } else {
+        const bool ragged = col0 + 128 > a.V;
+        float sum = 0.f;
+        // the second pass runs only where a logit lies far above a row's reference
+#pragma unroll 1
+        for (int pass = 0; pass < 2; ++pass) {
+          float most = -INFINITY;
+          sum = 0.f;
+#pragma unroll 1
+          for (int g = 0; g < 4; ++g) {
+            const int c = col0 + 32 * g;
+            if (c >= a.V) break;
+            uint32_t v[32];
+            tmem_ld32(t_buf + 32 * g, v);
+            tmem_ld_wait();
+            const int at = label - c;  // the label's own column is left out
+            if (__any_sync(0xFFFFFFFFu, at >= 0 && at < 32)) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (i == at) v[i] = 0xFF800000u;  // -inf
+            }
+            if (ragged) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (c + i >= a.V) v[i] = 0xFF800000u;
+            }
+            uint32_t packed[16];
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+              const float x0 = fmaf(__uint_as_float(v[2 * q]), kLog2e, -ref);
+              const float x1 = fmaf(__uint_as_float(v[2 * q + 1]), kLog2e, -ref);
+              most = fmaxf(most, fmaxf(x0, x1));
+              const float e0 = exp2_fast(x0), e1 = exp2_fast(x1);
+              sum += e0 + e1;
+              const __nv_bfloat162 h2 = __floats2bfloat162_rn(e0, e1);
+              packed[q] = *reinterpret_cast<const uint32_t *>(&h2);
+            }
+            if (a.e) {
+              if (lane == 0) bulk_wait_read<0>();
+              __syncwarp();
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                st_shared_v4(box + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4), packed[4 * q], packed[4 * q + 1],
+                             packed[4 * q + 2], packed[4 * q + 3]);
+              fence_proxy_async_smem();
+              __syncwarp();
+              if (lane == 0) {
+                tma_store_2d(&tmO, box, c, row32);
+                bulk_commit_group();
+              }
+            }
+          }
+          const bool far = most > kRefSlack && row < *a.count;
+          if (pass == 1 || !__any_sync(0xFFFFFFFFu, far)) break;
+          // the largest logit of the half tile becomes the reference of the rows that need it
+          float high = -INFINITY;
+#pragma unroll 1
+          for (int g = 0; g < 4; ++g) {
+            const int c = col0 + 32 * g;
+            if (c >= a.V) break;
+            uint32_t v[32];
+            tmem_ld32(t_buf + 32 * g, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (c + i < a.V && c + i != label) high = fmaxf(high, __uint_as_float(v[i]));
+          }
+          if (far) ref = ceilf(high * kLog2e);
+          if (lane == 0) bulk_wait_all();  // the first pass's boxes are written before the second's
+          __syncwarp();
+        }
+        if (row < *a.count)
+          a.sums[static_cast<int64_t>(row32 + lane) * (2 * tiles_n) + 2 * t.tn + half] = make_float2(sum, ref);
+      }
+      // accumulator drained: the leader's warps arrive (warp 0 arming the peer's bytes), the
+      // peer's signal with a non-blocking async store
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if (rank == 0) {
+          if (warp == 0)
+            mbar_arrive_expect_tx(&tempty[ab], 4 * C::kEpiWarps);
+          else
+            mbar_arrive(&tempty[ab]);
+        } else {
+          st_async_signal(mapa_shared(smem_u32(&sink[warp]), 0), mapa_shared(smem_u32(&tempty[ab]), 0));
+        }
+      }
+    }
+    if (lane == 0) bulk_wait_all();
+  }
+
+  __syncwarp();
+  tc_fence_before();
+  cluster_sync_all();
+  if (warp == C::kMmaWarp) {
+    tc_fence_after();
+    tmem_dealloc_pair(tmem_base, 2 * kTmemCols);
+  }
+}
+
+// ---------------------------------------------------------------- finalize and rows
+
+// One warp per row: the half tiles' sums brought to one reference R and added in a fixed order.
+__global__ void __launch_bounds__(256) sq_head_finalize_kernel(const HeadArgs a, const int first) {
+  const int lane = threadIdx.x & 31;
+  const int r = blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (r >= chunk_rows(a, first)) return;
+  const int row = first + r;
+  const int n = 2 * static_cast<int>((a.V + kHeadTile - 1) / kHeadTile);
+  const int filled = static_cast<int>((a.V + 127) / 128);  // half tiles that hold columns
+  const float2 *sums = a.sums + static_cast<int64_t>(r) * n;
+  const float z = a.label_z[row], z2 = z * kLog2e, ref0 = row_reference(z);
+  float ref = ref0, sum = 0.f;
+  bool moved = false;
+  for (int i = lane; i < filled; i += 32) {
+    const float2 q = sums[i];
+    moved |= q.y != ref0;
+    const float top = fmaxf(ref, q.y);
+    sum = sum * whole_exp2(ref - top) + q.x * whole_exp2(q.y - top);
+    ref = top;
+  }
+  float top = ref;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+  const float others = warp_total(sum * whole_exp2(ref - top));
+  const float own = exp2_fast(z2 - top), total = others + own;
+  if (lane == 0) {
+    const int t = a.token[row];
+    // log(total / own): where own underflows against a far larger logit, from the exponents
+    const bool near = top - z2 < 60.f;
+    const float loss = near ? log1pf(others / own) : (top - z2) * kLn2 + logf(total);
+    if (a.loss) a.loss[t] = loss;
+    if (a.lse) a.lse[t] = near ? z + loss : top * kLn2 + logf(total);
+    if (a.dX) {
+      const float g = a.dloss[t];
+      a.factors[row] = make_float2(g / total, -g * (others / total));
+    }
+  }
+  if (a.e && __any_sync(0xFFFFFFFFu, moved)) {
+    for (int i = 0; i < filled; ++i) {
+      const float by = whole_exp2(sums[i].y - top);
+      if (by == 1.f) continue;
+      __nv_bfloat16 *e = reinterpret_cast<__nv_bfloat16 *>(a.e) + static_cast<int64_t>(r) * a.pitch;
+      for (int64_t c = i * 128 + lane; c < a.V && c < (i + 1) * 128; c += 32)
+        e[c] = __float2bfloat16_rn(__bfloat162float(e[c]) * by);
+    }
+  }
+}
+
+// dX[token] = f.x sum over the parts + f.y W[label], 256 columns of a row per warp.
+__global__ void __launch_bounds__(256) sq_head_rows_kernel(const HeadArgs a, const int first) {
+  const int lane = threadIdx.x & 31;
+  const int pieces = static_cast<int>((a.D + 255) / 256);
+  const int unit = blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int r = unit / pieces;
+  const int rows = chunk_rows(a, first);
+  if (r >= rows) return;
+  const int64_t c = static_cast<int64_t>(unit % pieces) * 256 + lane * 8;
+  if (c >= a.D) return;
+  const int tiles_m = (rows + kHeadTile - 1) / kHeadTile;
+  const int tiles_n = static_cast<int>((a.D + kHeadTile - 1) / kHeadTile);
+  const int parts = head_parts(static_cast<int64_t>(tiles_m) * tiles_n,
+                               static_cast<int>((a.V + HeadCfg::kBK - 1) / HeadCfg::kBK), a.clusters);
+  const int64_t plane = static_cast<int64_t>(tiles_m) * kHeadTile * a.D;
+  const float *p = a.partial + static_cast<int64_t>(r) * a.D + c;
+  float s[8] = {};
+  for (int i = 0; i < parts; ++i, p += plane) {
+    const float4 u = __ldcs(reinterpret_cast<const float4 *>(p)), v = __ldcs(reinterpret_cast<const float4 *>(p) + 1);
+    s[0] += u.x, s[1] += u.y, s[2] += u.z, s[3] += u.w;
+    s[4] += v.x, s[5] += v.y, s[6] += v.z, s[7] += v.w;
+  }
+  const int row = first + r;
+  const float2 f = a.factors[row];
+  const uint4 w = __ldg(reinterpret_cast<const uint4 *>(a.W + static_cast<int64_t>(a.label[row]) * a.D + c));
+  const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+  uint32_t o[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const __nv_bfloat162 h2 =
+        __floats2bfloat162_rn(fmaf(f.x, s[2 * q], f.y * __uint_as_float(ww[q] << 16)),
+                              fmaf(f.x, s[2 * q + 1], f.y * __uint_as_float(ww[q] & 0xFFFF0000u)));
+    o[q] = *reinterpret_cast<const uint32_t *>(&h2);
+  }
+  *reinterpret_cast<uint4 *>(a.dX + static_cast<int64_t>(a.token[row]) * a.D + c) = make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+template <bool GRAD>
+cudaError_t launch_head_product(const CUtensorMap &tmA, const CUtensorMap &tmB, const CUtensorMap &tmO,
+                                const HeadArgs &a, int first, int64_t most, int sm_count, cudaStream_t stream) {
+  static int done_mask = 0;  // per device ordinal (first 31)
+  static int max_clusters[32] = {0};
+  return launch_persistent(sq_head_kernel<GRAD>, HeadCfg::kThreads, HeadCfg::kSmemBytes, most, sm_count, stream,
+                           max_clusters, &done_mask, tmA, tmB, tmO, a, first);
+}
+
+}  // namespace
+
+cudaError_t launch_head_gather(const HeadArgs &a, cudaStream_t stream) {
+  sq_head_gather_kernel<<<static_cast<unsigned>((a.T + 7) / 8), 256, 0, stream>>>(a);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_head_chunk(const HeadArgs &a, const HeadMaps &m, int first, int sm_count, cudaStream_t stream) {
+  const int64_t tiles_m = a.chunk / kHeadTile;
+  cudaError_t e = launch_head_product<false>(m.rows, m.weights, m.e_store, a, first,
+                                             tiles_m * ((a.V + kHeadTile - 1) / kHeadTile), sm_count, stream);
+  if (e != cudaSuccess) return e;
+  const int rows = a.T - first < a.chunk ? a.T - first : a.chunk;
+  sq_head_finalize_kernel<<<(rows + 7) / 8, 256, 0, stream>>>(a, first);
+  if ((e = cudaGetLastError()) != cudaSuccess || !a.dX) return e;
+  if ((e = launch_head_product<true>(m.e_load, m.weights, m.partial, a, first, int64_t(1) << 30, sm_count, stream)) !=
+      cudaSuccess)
+    return e;
+  const int64_t units = rows * ((a.D + 255) / 256);
+  sq_head_rows_kernel<<<static_cast<unsigned>((units + 7) / 8), 256, 0, stream>>>(a, first);
+  return cudaGetLastError();
+}
+
+}  // namespace sqi
