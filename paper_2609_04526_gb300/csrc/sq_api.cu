@@ -447,7 +447,7 @@ sq_status run_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint
     chunk = std::min(whole, std::max<int64_t>(fit, sqi::kHeadTile));
   }
   a.chunk = static_cast<int>(chunk);
-  const int64_t halves = 2 * ((V + sqi::kHeadTile - 1) / sqi::kHeadTile);
+  const int64_t quarters = 4 * ((V + sqi::kHeadTile - 1) / sqi::kHeadTile);
   const int64_t partial_rows = dX ? sqi::head_partial_rows(chunk, D, V, a.clusters) : 0;
   size_t used = 0;
   auto take = [&](int64_t bytes) {
@@ -456,7 +456,7 @@ sq_status run_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint
     return at;
   };
   const size_t o_count = take(4), o_token = take(4 * piece), o_label = take(4 * piece), o_z = take(4 * piece),
-               o_factors = take(8 * piece), o_rows = take(2 * D * whole), o_sums = take(8 * halves * chunk),
+               o_factors = take(8 * piece), o_rows = take(2 * D * whole), o_sums = take(8 * quarters * chunk),
                o_e = take(dX ? 2 * a.pitch * chunk : 0), o_partial = take(4 * D * partial_rows);
   SQ_TRY(ensure_scratch(h, dev->head, used, stream, "the head loss"));
   uint8_t *base = static_cast<uint8_t *>(dev->head.ptr);

@@ -436,7 +436,7 @@ struct HeadArgs {
   float2 *factors;
   uint16_t *rows;         // [T, D] the labelled tokens' rows of X
   // scratch, by row of the chunk
-  float2 *sums;           // [chunk, 2 * column tiles] sum and reference of each half tile
+  float2 *sums;           // [chunk, 4 * column tiles] sum and reference of each quarter tile
   uint16_t *e;            // [chunk, pitch] bf16 exponentials (gradient)
   float *partial;         // [parts, rows, D] fp32 (gradient)
   int *err;

@@ -6,7 +6,7 @@
 // The logits exist only as accumulator tiles in tensor memory. Per piece of labelled tokens:
 //
 //   gather    the labelled tokens' rows, packed, and each row's label logit z_l (CUDA cores)
-//   logits    z tile by tile; the epilogue forms e = 2^(z log2(e) - r), adds e over 128 columns
+//   logits    z tile by tile; the epilogue forms e = 2^(z log2(e) - r), adds e over 64 columns
 //             and, for the gradient, writes bf16 e of the piece
 //   finalize  sums -> loss, log-sum-exp and the row's two gradient factors
 //   gradient  (e W) over the vocabulary, cut into parts where few tiles would leave SMs idle
@@ -14,15 +14,15 @@
 //
 // The reference r of a row is ceil(z_l log2(e)), known before the product: e then needs no
 // maximum first, and e W no second pass over the logits once S is known. Where a tile holds a
-// logit more than 2^100 above it (a label of probability below 2^-100), that half tile alone
-// takes its own maximum as reference, and finalize rescales the row's e. References are whole
+// logit more than 2^100 above it (a label of probability below 2^-100), that quarter of
+// it takes its own maximum as reference, and finalize rescales the row's e. References are whole
 // powers of two, so such a change of reference is exact. Terms more than 2^126 below the label's
 // own vanish.
 //
 // The label's own term is left out of e and of the sums and carried in fp32: p_label - 1 is
 // -(S - e_l) / S without cancellation, so confident tokens keep an accurate loss and gradient.
-// e is rounded to bf16 once, as an operand of the tensor cores (relative 2^-9 per term, far
-// below the rounding of the bf16 gradient once summed); the sums S take the unrounded values.
+// e is rounded to bf16 once, as an operand of the tensor cores (at most 2^-8 of a term; errors of
+// one sign and the other, so their sum stays below the rounding of the bf16 gradient); the sums S take the unrounded values.
 #include "sq_gemm_kernels.cuh"
 
 namespace sqi {
@@ -32,8 +32,12 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRefSlack = 100.f;  // a logit this far above the reference (in powers of two) moves it
 
+// Epilogue warp w takes TMEM lanes 32 (w % 4) .. + 31 and the w / 4-th share of a tile's columns:
+// a quarter (logits, whose columns stay in registers) or a half (gradient).
+template <bool GRAD>
 struct HeadCfg {
-  static constexpr int kEpiWarps = 8;  // warp w: TMEM lanes 32 (w % 4) .. + 31, columns 128 (w / 4) .. + 127
+  static constexpr int kEpiWarps = GRAD ? 8 : 16;
+  static constexpr int kEpiCols = kHeadTile / (kEpiWarps / 4);
   static constexpr int kTmaWarp = kEpiWarps;
   static constexpr int kMmaWarp = kTmaWarp + 1;
   static constexpr int kThreads = 32 * (kMmaWarp + 1);
@@ -45,11 +49,16 @@ struct HeadCfg {
   static constexpr uint32_t kTx = 2 * kStageBytes;  // both CTAs' tiles, on the leader's barrier
   static constexpr int kTile = kHeadTile;
   static constexpr int kOffBox = kStages * kStageBytes;
-  static constexpr int kBoxBytes = 4096;  // 32 rows x 32 fp32 (or bf16) columns of a warp
+  static constexpr int kBoxBytes = 32 * 32 * (GRAD ? 4 : 2);  // 32 rows x 32 columns of a warp
+  // Stages added up in one accumulator. The tensor core truncates its running fp32 sum at every
+  // step of 16, a bias that grows with the length: a sum of 4096 products in one accumulator left
+  // the log-sum-exp 1.4e-5 too small. The logits therefore leave tensor memory every 512 products
+  // and are added in registers; the gradient, rounded to bf16 in the end, runs through.
+  static constexpr int kSegment = GRAD ? 1 << 30 : 4;
   static constexpr int kOffBar = kOffBox + kEpiWarps * kBoxBytes;
   static constexpr int kSmemBytes = kOffBar + 512 + 1024;
 };
-static_assert(HeadCfg::kSmemBytes <= 232448, "head kernel exceeds the opt-in shared memory of one CTA");
+static_assert(HeadCfg<false>::kSmemBytes <= 232448 && HeadCfg<true>::kSmemBytes <= 232448, "head kernel exceeds the opt-in shared memory of one CTA");
 
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
@@ -60,6 +69,17 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // 2^d of a whole d <= 0, exactly; 0 where it is not a normal number.
 __device__ __forceinline__ float whole_exp2(float d) {
   return d < -126.f ? 0.f : __int_as_float((127 + static_cast<int>(d)) << 23);
+}
+
+// 32 lanes x 16 consecutive fp32 columns.
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(taddr)
+      : "memory");
 }
 
 __device__ __forceinline__ float warp_total(float v) {
@@ -163,10 +183,10 @@ __device__ __forceinline__ HeadTile head_tile(int unit, int tiles_m, int tiles_n
 }
 
 template <bool GRAD>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg::kThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThreads, 1)
     sq_head_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                    const __grid_constant__ CUtensorMap tmO, const HeadArgs a, const int first) {
-  using C = HeadCfg;
+  using C = HeadCfg<GRAD>;
   constexpr int S = C::kStages;
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -252,62 +272,75 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg::kThreads, 1
       // MN-major: 16 contraction rows (2 KiB) per step, 64-column atoms 16 KiB apart
       const uint64_t ad_base = smem_desc_sw128(smem_u32(stage_a(0)), 16, 1024);
       const uint64_t bd_base = smem_desc_sw128(smem_u32(stage_b(0)), GRAD ? 16384 : 16, 1024);
-      int s = 0, tc = 0;
+      int s = 0, tc = 0;  // tc: accumulators filled
       uint32_t ph = 0;
       bool ok = true;
-      for (int unit = cluster; unit < total && ok; unit += nclusters, ++tc) {
+      for (int unit = cluster; unit < total && ok; unit += nclusters) {
         const HeadTile t = head_tile<GRAD>(unit, tiles_m, tiles_n, parts, stages);
-        const int ab = tc & 1;
-        const uint32_t au = static_cast<uint32_t>(tc >> 1);
-        if (tc >= 2 && !(ok = mbar_spin_cluster(&tempty[ab], (au & 1u) ^ 1u, abort_flag, a.err))) break;
-        tc_fence_after();
-        const uint32_t d_tmem = tmem_base + ab * kTmemCols;
-        for (int kb = 0; kb < t.nk; ++kb) {
-          if (!(ok = mbar_spin(&full[s], ph, abort_flag, a.err))) break;
-          const uint64_t so = static_cast<uint64_t>(s * (C::kStageBytes >> 4));
-          const uint64_t a0 = ad_base + so, b0 = bd_base + so;
+        for (int k0 = 0; k0 < t.nk && ok; k0 += C::kSegment, ++tc) {
+          const int ab = tc & 1;
+          const uint32_t au = static_cast<uint32_t>(tc >> 1);
+          if (tc >= 2 && !(ok = mbar_spin_cluster(&tempty[ab], (au & 1u) ^ 1u, abort_flag, a.err))) break;
+          tc_fence_after();
+          const uint32_t d_tmem = tmem_base + ab * kTmemCols;
+          const int steps = min(C::kSegment, t.nk - k0);
+          for (int kb = 0; kb < steps; ++kb) {
+            if (!(ok = mbar_spin(&full[s], ph, abort_flag, a.err))) break;
+            const uint64_t so = static_cast<uint64_t>(s * (C::kStageBytes >> 4));
+            const uint64_t a0 = ad_base + so, b0 = bd_base + so;
 #pragma unroll
-          for (int kk = 0; kk < C::kBK / 16; ++kk) {
-            const uint32_t ka = ((kk >> 2) * 16384 + (kk & 3) * 32) >> 4;
-            const uint32_t kb_ = GRAD ? (kk * 2048) >> 4 : ka;
-            umma_bf16_pair(d_tmem, a0 + ka, b0 + kb_, idesc, (kb > 0 || kk > 0) ? 1u : 0u);
+            for (int kk = 0; kk < C::kBK / 16; ++kk) {
+              const uint32_t ka = ((kk >> 2) * 16384 + (kk & 3) * 32) >> 4;
+              const uint32_t kb_ = GRAD ? (kk * 2048) >> 4 : ka;
+              umma_bf16_pair(d_tmem, a0 + ka, b0 + kb_, idesc, (kb > 0 || kk > 0) ? 1u : 0u);
+            }
+            umma_commit_pair_mc(&empty[s]);
+            if (++s == S) {
+              s = 0;
+              ph ^= 1u;
+            }
           }
-          umma_commit_pair_mc(&empty[s]);
-          if (++s == S) {
-            s = 0;
-            ph ^= 1u;
-          }
+          if (ok) umma_commit_pair_mc(&tfull[ab]);
         }
-        if (ok) umma_commit_pair_mc(&tfull[ab]);
       }
       umma_commit_pair(drain);
       mbar_drain(drain, 0);
     }
   } else {
-    // ------------------------------------------------------ epilogue (warps 0-7, both CTAs)
-    const int quad = warp & 3, half = warp >> 2;
-    const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + half * 128;
+    // ------------------------------------------------------ epilogue (both CTAs)
+    const int quad = warp & 3, share = warp >> 2;
+    const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + share * C::kEpiCols;
     const uint32_t box = smem_u32(smem + C::kOffBox + warp * C::kBoxBytes);
-    int tc = 0;
-    for (int unit = cluster; unit < total; unit += nclusters, ++tc) {
-      const HeadTile t = head_tile<GRAD>(unit, tiles_m, tiles_n, parts, stages);
-      const int ab = tc & 1;
-      const int row32 = t.tm * C::kTile + 128 * static_cast<int>(rank) + 32 * quad;  // of the chunk
-      const int col0 = t.tn * C::kTile + 128 * half;
-      const int row = first + row32 + lane;
-      int label = -1;
-      float ref = 0.f;
-      if (!GRAD && row < *a.count) {
-        label = a.label[row];
-        ref = row_reference(a.label_z[row]);
+    // accumulator drained: the leader's warps arrive (warp 0 arming the peer's bytes), the peer's
+    // signal with a non-blocking async store
+    auto release = [&](int ab) {
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if (rank == 0) {
+          if (warp == 0)
+            mbar_arrive_expect_tx(&tempty[ab], 4 * C::kEpiWarps);
+          else
+            mbar_arrive(&tempty[ab]);
+        } else {
+          st_async_signal(mapa_shared(smem_u32(&sink[warp]), 0), mapa_shared(smem_u32(&tempty[ab]), 0));
+        }
       }
-      if (!mbar_wait(&tfull[ab], static_cast<uint32_t>(tc >> 1) & 1u, abort_flag, a.err)) break;
-      tc_fence_after();
-      const uint32_t t_buf = t_row + ab * kTmemCols;
+    };
+    int tc = 0;
+    bool ok = true;
+    for (int unit = cluster; unit < total && ok; unit += nclusters) {
+      const HeadTile t = head_tile<GRAD>(unit, tiles_m, tiles_n, parts, stages);
+      const int row32 = t.tm * C::kTile + 128 * static_cast<int>(rank) + 32 * quad;  // of the chunk
+      const int col0 = t.tn * C::kTile + C::kEpiCols * share;
       if constexpr (GRAD) {
+        const int ab = tc & 1;
+        if (!(ok = mbar_wait(&tfull[ab], static_cast<uint32_t>(tc >> 1) & 1u, abort_flag, a.err))) break;
+        tc_fence_after();
+        const uint32_t t_buf = t_row + ab * kTmemCols;
         const int32_t out_row = t.part * tiles_m * C::kTile + row32;
 #pragma unroll 1
-        for (int g = 0; g < 4; ++g) {
+        for (int g = 0; g < C::kEpiCols / 32; ++g) {
           uint32_t v[32];
           tmem_ld32(t_buf + 32 * g, v);
           tmem_ld_wait();
@@ -323,93 +356,72 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg::kThreads, 1
             bulk_commit_group();
           }
         }
+        release(ab);
+        ++tc;
       } else {
-        const bool ragged = col0 + 128 > a.V;
+        const int row = first + row32 + lane;
+        const bool in = row < *a.count;
+        const int at = in ? a.label[row] - col0 : -1;  // the label's own column is left out
+        float ref = in ? row_reference(a.label_z[row]) : 0.f;
+        float z[C::kEpiCols];
+        for (int k0 = 0; k0 < stages; k0 += C::kSegment, ++tc) {
+          const int ab = tc & 1;
+          if (!(ok = mbar_wait(&tfull[ab], static_cast<uint32_t>(tc >> 1) & 1u, abort_flag, a.err))) break;
+          tc_fence_after();
+#pragma unroll
+          for (int g = 0; g < C::kEpiCols / 16; ++g) {
+            uint32_t v[16];
+            tmem_ld16(t_row + ab * kTmemCols + 16 * g, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[16 * g + i] = (k0 ? z[16 * g + i] : 0.f) + __uint_as_float(v[i]);
+          }
+          release(ab);
+        }
+        if (!ok) break;
+        if (col0 >= a.V) continue;
+        if (__any_sync(0xFFFFFFFFu, at >= 0 && at < C::kEpiCols)) {
+#pragma unroll
+          for (int i = 0; i < C::kEpiCols; ++i)
+            if (i == at) z[i] = -INFINITY;
+        }
+        if (col0 + C::kEpiCols > a.V) {
+#pragma unroll
+          for (int i = 0; i < C::kEpiCols; ++i)
+            if (col0 + i >= a.V) z[i] = -INFINITY;
+        }
+        float most = z[0];
+#pragma unroll
+        for (int i = 1; i < C::kEpiCols; ++i) most = fmaxf(most, z[i]);
+        if (fmaf(most, kLog2e, -ref) > kRefSlack) ref = ceilf(most * kLog2e);
         float sum = 0.f;
-        // the second pass runs only where a logit lies far above a row's reference
-#pragma unroll 1
-        for (int pass = 0; pass < 2; ++pass) {
-          float most = -INFINITY;
-          sum = 0.f;
-#pragma unroll 1
-          for (int g = 0; g < 4; ++g) {
-            const int c = col0 + 32 * g;
-            if (c >= a.V) break;
-            uint32_t v[32];
-            tmem_ld32(t_buf + 32 * g, v);
-            tmem_ld_wait();
-            const int at = label - c;  // the label's own column is left out
-            if (__any_sync(0xFFFFFFFFu, at >= 0 && at < 32)) {
 #pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (i == at) v[i] = 0xFF800000u;  // -inf
-            }
-            if (ragged) {
+        for (int g = 0; g < C::kEpiCols / 32; ++g) {
+          uint32_t packed[16];
 #pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (c + i >= a.V) v[i] = 0xFF800000u;
-            }
-            uint32_t packed[16];
+          for (int q = 0; q < 16; ++q) {
+            const float e0 = exp2_fast(fmaf(z[32 * g + 2 * q], kLog2e, -ref));
+            const float e1 = exp2_fast(fmaf(z[32 * g + 2 * q + 1], kLog2e, -ref));
+            sum += e0 + e1;
+            const __nv_bfloat162 h2 = __floats2bfloat162_rn(e0, e1);
+            packed[q] = *reinterpret_cast<const uint32_t *>(&h2);
+          }
+          if (a.e) {
+            if (lane == 0) bulk_wait_read<0>();  // the previous box's store has read the buffer
+            __syncwarp();
 #pragma unroll
-            for (int q = 0; q < 16; ++q) {
-              const float x0 = fmaf(__uint_as_float(v[2 * q]), kLog2e, -ref);
-              const float x1 = fmaf(__uint_as_float(v[2 * q + 1]), kLog2e, -ref);
-              most = fmaxf(most, fmaxf(x0, x1));
-              const float e0 = exp2_fast(x0), e1 = exp2_fast(x1);
-              sum += e0 + e1;
-              const __nv_bfloat162 h2 = __floats2bfloat162_rn(e0, e1);
-              packed[q] = *reinterpret_cast<const uint32_t *>(&h2);
-            }
-            if (a.e) {
-              if (lane == 0) bulk_wait_read<0>();
-              __syncwarp();
-#pragma unroll
-              for (int q = 0; q < 4; ++q)
-                st_shared_v4(box + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4), packed[4 * q], packed[4 * q + 1],
-                             packed[4 * q + 2], packed[4 * q + 3]);
-              fence_proxy_async_smem();
-              __syncwarp();
-              if (lane == 0) {
-                tma_store_2d(&tmO, box, c, row32);
-                bulk_commit_group();
-              }
+            for (int q = 0; q < 4; ++q)
+              st_shared_v4(box + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4), packed[4 * q], packed[4 * q + 1],
+                           packed[4 * q + 2], packed[4 * q + 3]);
+            fence_proxy_async_smem();  // the box -> async proxy (the TMA store)
+            __syncwarp();
+            if (lane == 0) {
+              if (col0 + 32 * g < a.V) tma_store_2d(&tmO, box, col0 + 32 * g, row32);
+              bulk_commit_group();
             }
           }
-          const bool far = most > kRefSlack && row < *a.count;
-          if (pass == 1 || !__any_sync(0xFFFFFFFFu, far)) break;
-          // the largest logit of the half tile becomes the reference of the rows that need it
-          float high = -INFINITY;
-#pragma unroll 1
-          for (int g = 0; g < 4; ++g) {
-            const int c = col0 + 32 * g;
-            if (c >= a.V) break;
-            uint32_t v[32];
-            tmem_ld32(t_buf + 32 * g, v);
-            tmem_ld_wait();
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (c + i < a.V && c + i != label) high = fmaxf(high, __uint_as_float(v[i]));
-          }
-          if (far) ref = ceilf(high * kLog2e);
-          if (lane == 0) bulk_wait_all();  // the first pass's boxes are written before the second's
-          __syncwarp();
         }
-        if (row < *a.count)
-          a.sums[static_cast<int64_t>(row32 + lane) * (2 * tiles_n) + 2 * t.tn + half] = make_float2(sum, ref);
-      }
-      // accumulator drained: the leader's warps arrive (warp 0 arming the peer's bytes), the
-      // peer's signal with a non-blocking async store
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        if (rank == 0) {
-          if (warp == 0)
-            mbar_arrive_expect_tx(&tempty[ab], 4 * C::kEpiWarps);
-          else
-            mbar_arrive(&tempty[ab]);
-        } else {
-          st_async_signal(mapa_shared(smem_u32(&sink[warp]), 0), mapa_shared(smem_u32(&tempty[ab]), 0));
-        }
+        if (in) a.sums[static_cast<int64_t>(row32 + lane) * (4 * tiles_n) + 4 * t.tn + share] = make_float2(sum, ref);
       }
     }
     if (lane == 0) bulk_wait_all();
@@ -426,14 +438,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg::kThreads, 1
 
 // ---------------------------------------------------------------- finalize and rows
 
-// One warp per row: the half tiles' sums brought to one reference R and added in a fixed order.
+// One warp per row: the quarter tiles' sums brought to one reference R and added in a fixed order.
 __global__ void __launch_bounds__(256) sq_head_finalize_kernel(const HeadArgs a, const int first) {
   const int lane = threadIdx.x & 31;
   const int r = blockIdx.x * 8 + (threadIdx.x >> 5);
   if (r >= chunk_rows(a, first)) return;
   const int row = first + r;
-  const int n = 2 * static_cast<int>((a.V + kHeadTile - 1) / kHeadTile);
-  const int filled = static_cast<int>((a.V + 127) / 128);  // half tiles that hold columns
+  constexpr int kCols = HeadCfg<false>::kEpiCols;
+  const int n = kHeadTile / kCols * static_cast<int>((a.V + kHeadTile - 1) / kHeadTile);
+  const int filled = static_cast<int>((a.V + kCols - 1) / kCols);  // quarter tiles that hold columns
   const float2 *sums = a.sums + static_cast<int64_t>(r) * n;
   const float z = a.label_z[row], z2 = z * kLog2e, ref0 = row_reference(z);
   float ref = ref0, sum = 0.f;
@@ -467,7 +480,7 @@ __global__ void __launch_bounds__(256) sq_head_finalize_kernel(const HeadArgs a,
       const float by = whole_exp2(sums[i].y - top);
       if (by == 1.f) continue;
       __nv_bfloat16 *e = reinterpret_cast<__nv_bfloat16 *>(a.e) + static_cast<int64_t>(r) * a.pitch;
-      for (int64_t c = i * 128 + lane; c < a.V && c < (i + 1) * 128; c += 32)
+      for (int64_t c = i * kCols + lane; c < a.V && c < (i + 1) * kCols; c += 32)
         e[c] = __float2bfloat16_rn(__bfloat162float(e[c]) * by);
     }
   }
@@ -486,7 +499,7 @@ __global__ void __launch_bounds__(256) sq_head_rows_kernel(const HeadArgs a, con
   const int tiles_m = (rows + kHeadTile - 1) / kHeadTile;
   const int tiles_n = static_cast<int>((a.D + kHeadTile - 1) / kHeadTile);
   const int parts = head_parts(static_cast<int64_t>(tiles_m) * tiles_n,
-                               static_cast<int>((a.V + HeadCfg::kBK - 1) / HeadCfg::kBK), a.clusters);
+                               static_cast<int>((a.V + HeadCfg<true>::kBK - 1) / HeadCfg<true>::kBK), a.clusters);
   const int64_t plane = static_cast<int64_t>(tiles_m) * kHeadTile * a.D;
   const float *p = a.partial + static_cast<int64_t>(r) * a.D + c;
   float s[8] = {};
@@ -515,7 +528,7 @@ cudaError_t launch_head_product(const CUtensorMap &tmA, const CUtensorMap &tmB, 
                                 const HeadArgs &a, int first, int64_t most, int sm_count, cudaStream_t stream) {
   static int done_mask = 0;  // per device ordinal (first 31)
   static int max_clusters[32] = {0};
-  return launch_persistent(sq_head_kernel<GRAD>, HeadCfg::kThreads, HeadCfg::kSmemBytes, most, sm_count, stream,
+  return launch_persistent(sq_head_kernel<GRAD>, HeadCfg<GRAD>::kThreads, HeadCfg<GRAD>::kSmemBytes, most, sm_count, stream,
                            max_clusters, &done_mask, tmA, tmB, tmO, a, first);
 }
 
