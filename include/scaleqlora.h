@@ -485,7 +485,8 @@ sq_status sq_route_grad(sq_handle h, int64_t T, int32_t E, int32_t k, int32_t lo
  * without an expert. Outputs (device, overwritten): offsets int64 [E + 1], expert e's rows being
  * offsets[e] .. offsets[e+1]-1 (the grouped calls' layout); row_of int32 [n], the row of each
  * slot, -1 without an expert; slot_of int32 [n], the slot of each row, -1 for rows >= offsets[E].
- * n == 0 writes zero offsets. */
+ * n == 0 writes zero offsets. More than 4096 slots use scratch of the handle (a few words per
+ * expert and SM). */
 sq_status sq_sort_tokens(sq_handle h, int64_t n, int32_t E, const int32_t *experts, int64_t *offsets, int32_t *row_of,
                          int32_t *slot_of, void *stream);
 

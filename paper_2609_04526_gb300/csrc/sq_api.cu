@@ -51,6 +51,7 @@ struct DeviceState {
   int next_table;
   Scratch partial;       // token-split partial planes of the dense scale gradient
   int64_t *plane_acc;    // counter accumulators of the multi-plane calls (zero between calls)
+  Scratch sort;          // per-CTA counts of the sort by expert
   Scratch head;          // packed rows, exponentials and partial planes of the head loss
 };
 
@@ -455,12 +456,13 @@ sq_status run_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint
     used += static_cast<size_t>(up(bytes, 1024));
     return at;
   };
-  const size_t o_count = take(4), o_token = take(4 * piece), o_label = take(4 * piece), o_z = take(4 * piece),
+  const size_t o_count = take(8), o_token = take(4 * piece), o_label = take(4 * piece), o_z = take(4 * piece),
                o_factors = take(8 * piece), o_rows = take(2 * D * whole), o_sums = take(8 * quarters * chunk),
                o_e = take(dX ? 2 * a.pitch * chunk : 0), o_partial = take(4 * D * partial_rows);
   SQ_TRY(ensure_scratch(h, dev->head, used, stream, "the head loss"));
   uint8_t *base = static_cast<uint8_t *>(dev->head.ptr);
   a.count = reinterpret_cast<int *>(base + o_count);
+  a.parts = a.count + 1;
   a.token = reinterpret_cast<int *>(base + o_token);
   a.label = reinterpret_cast<int *>(base + o_label);
   a.label_z = reinterpret_cast<float *>(base + o_z);
@@ -795,6 +797,7 @@ sq_status sq_destroy(sq_handle h) {
       if (d.plane_acc) cudaFree(d.plane_acc);
       free_scratch(d.workspace);
       free_scratch(d.partial);
+      free_scratch(d.sort);
       free_scratch(d.head);
       for (auto &t : d.tables) {
         if (t.done) {
@@ -1517,7 +1520,11 @@ sq_status sq_sort_tokens(sq_handle h, int64_t n, int32_t E, const int32_t *exper
   }
   DeviceState *dev = nullptr;
   SQ_TRY(ensure_device(h, &dev));
-  cudaError_t e = sqi::launch_sort(n, E, experts, offsets, row_of, slot_of, static_cast<cudaStream_t>(stream));
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const size_t bytes = sqi::sort_workspace(n, E, dev->sm_count);
+  if (bytes > 0) SQ_TRY(ensure_scratch(h, dev->sort, bytes, st, "the sort by expert"));
+  cudaError_t e = sqi::launch_sort(n, E, experts, offsets, row_of, slot_of, static_cast<int *>(dev->sort.ptr),
+                                   dev->sm_count, st);
   if (e != cudaSuccess) return cuda_fail(h, e, "sort launch");
   return SQ_OK;
   SQ_GUARD_END
@@ -1557,7 +1564,8 @@ sq_status sq_combine(sq_handle h, int64_t T, int32_t k, int64_t D, int64_t R, co
   DeviceState *dev = nullptr;
   SQ_TRY(ensure_device(h, &dev));
   if (T == 0) return SQ_OK;
-  cudaError_t e = sqi::launch_combine(T, k, D, R, Ys, row_of, weights, Y, static_cast<cudaStream_t>(stream));
+  cudaError_t e = sqi::launch_combine(T, k, D, R, Ys, row_of, weights, Y, dev->sm_count,
+                                      static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return cuda_fail(h, e, "combine launch");
   return SQ_OK;
   SQ_GUARD_END
@@ -1576,7 +1584,8 @@ sq_status sq_dispatch_grad(sq_handle h, int64_t T, int32_t k, int64_t D, int64_t
   DeviceState *dev = nullptr;
   SQ_TRY(ensure_device(h, &dev));
   if (T == 0) return SQ_OK;
-  cudaError_t e = sqi::launch_combine(T, k, D, R, dXs, row_of, nullptr, dX, static_cast<cudaStream_t>(stream));
+  cudaError_t e = sqi::launch_combine(T, k, D, R, dXs, row_of, nullptr, dX, dev->sm_count,
+                                      static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return cuda_fail(h, e, "dispatch gradient launch");
   return SQ_OK;
   SQ_GUARD_END

@@ -368,12 +368,13 @@ cudaError_t launch_route(int64_t T, int E, int k, bool bf16, const void *logits,
                          int *experts, float *weights, cudaStream_t stream);
 cudaError_t launch_route_grad(int64_t T, int E, int k, bool bf16, const void *logits, const int *experts,
                               const float *dweights, bool normalize, void *dlogits, cudaStream_t stream);
+size_t sort_workspace(int64_t n, int E, int sm_count);
 cudaError_t launch_sort(int64_t n, int E, const int *experts, int64_t *offsets, int *row_of, int *slot_of,
-                        cudaStream_t stream);
+                        int *workspace, int sm_count, cudaStream_t stream);
 cudaError_t launch_dispatch(int64_t T, int k, int64_t D, int64_t rows, const uint16_t *X, const int *row_of,
                             const int *slot_of, uint16_t *Xs, cudaStream_t stream);
 cudaError_t launch_combine(int64_t T, int k, int64_t D, int64_t rows, const uint16_t *Ys, const int *row_of,
-                           const float *weights, uint16_t *Y, cudaStream_t stream);
+                           const float *weights, uint16_t *Y, int sm_count, cudaStream_t stream);
 cudaError_t launch_combine_grad(int64_t T, int k, int64_t D, int64_t rows, const uint16_t *dY, const uint16_t *Ys,
                                 const int *row_of, const int *slot_of, const float *weights, uint16_t *dYs,
                                 float *dweights, int sm_count, cudaStream_t stream);
@@ -431,6 +432,7 @@ struct HeadArgs {
   int64_t pitch;          // elements of a row of e
   // scratch, by compact row of the piece
   int *count;             // labelled tokens of the piece
+  int *parts;             // vocabulary parts of the chunk's gradient launch
   int *token, *label;
   float *label_z;
   float2 *factors;

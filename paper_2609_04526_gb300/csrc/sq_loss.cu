@@ -52,9 +52,9 @@ struct HeadCfg {
   static constexpr int kBoxBytes = 32 * 32 * (GRAD ? 4 : 2);  // 32 rows x 32 columns of a warp
   // Stages added up in one accumulator. The tensor core truncates its running fp32 sum at every
   // step of 16, a bias that grows with the length: a sum of 4096 products in one accumulator left
-  // the log-sum-exp 1.4e-5 too small. The logits therefore leave tensor memory every 512 products
+  // the log-sum-exp 1.4e-5 too small. The logits therefore leave tensor memory every 1024 products
   // and are added in registers; the gradient, rounded to bf16 in the end, runs through.
-  static constexpr int kSegment = GRAD ? 1 << 30 : 4;
+  static constexpr int kSegment = GRAD ? 1 << 30 : 8;
   static constexpr int kOffBar = kOffBox + kEpiWarps * kBoxBytes;
   static constexpr int kSmemBytes = kOffBar + 512 + 1024;
 };
@@ -100,59 +100,72 @@ __device__ __forceinline__ int chunk_rows(const HeadArgs &a, int first) {
 
 // ---------------------------------------------------------------- gather
 
-// Eight tokens per CTA, one warp each. The labelled ones are packed in order (each CTA counts
-// the labels before its own), so rows without a label cost nothing later and what they hold
-// reaches no product.
+// SHARE warps per token and 8 / SHARE tokens per CTA. The labelled tokens are packed in order
+// (each CTA counts the labels before its own), so rows without a label cost nothing later and
+// what they hold reaches no product. Few tokens take a whole CTA each: one warp walked a row of
+// 4096 in 7.3 us.
+template <int SHARE>
 __global__ void __launch_bounds__(256) sq_head_gather_kernel(const HeadArgs a) {
+  constexpr int kTokens = 8 / SHARE;
   __shared__ int before[8];
+  __shared__ float dots[8];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int t0 = blockIdx.x * 8, t = t0 + warp;
+  const int t0 = blockIdx.x * kTokens, own = warp / SHARE, t = t0 + own;
   auto labelled = [&](int i) {
     const int64_t y = a.labels[i];
     return y >= 0 && y < a.V;
   };
   int seen = 0;
   for (int i = threadIdx.x; i < t0; i += 256) seen += labelled(i);
-  const bool own = lane < 8 && t0 + lane < a.T && labelled(t0 + lane);
-  const uint32_t here = __ballot_sync(0xFFFFFFFFu, own);  // the same in every warp
+  const uint32_t here =  // the same in every warp
+      __ballot_sync(0xFFFFFFFFu, lane < kTokens && t0 + lane < a.T && labelled(t0 + lane));
   seen = __reduce_add_sync(0xFFFFFFFFu, seen);
   if (lane == 0) before[warp] = seen;
   __syncthreads();
-  int row = __popc(here & ((1u << warp) - 1));
+  int row = __popc(here & ((1u << own) - 1));
 #pragma unroll
   for (int w = 0; w < 8; ++w) row += before[w];
-  if (t == a.T - 1 && lane == 0) *a.count = row + ((here >> warp) & 1);
-  if (t >= a.T) return;
+  const bool target = (here >> own) & 1;
+  const int first = (warp % SHARE) * 32 + lane;  // of this token's threads
+  if (t == a.T - 1 && first == 0) *a.count = row + target;
   const int pieces = static_cast<int>(a.D / 8);
-  if (!((here >> warp) & 1)) {
+  float dot = 0.f;
+  int64_t y = 0;
+  if (t < a.T && !target) {
     if (a.dX) {
       uint4 *out = reinterpret_cast<uint4 *>(a.dX + static_cast<int64_t>(t) * a.D);
-      for (int i = lane; i < pieces; i += 32) out[i] = make_uint4(0, 0, 0, 0);
+      for (int i = first; i < pieces; i += 32 * SHARE) out[i] = make_uint4(0, 0, 0, 0);
     }
-    if (lane == 0) {
+    if (first == 0) {
       if (a.loss) a.loss[t] = 0.f;
       if (a.lse) a.lse[t] = 0.f;
     }
-    return;
-  }
-  const int64_t y = a.labels[t];
-  const uint4 *x = reinterpret_cast<const uint4 *>(a.X + static_cast<int64_t>(t) * a.D);
-  const uint4 *w = reinterpret_cast<const uint4 *>(a.W + y * a.D);
-  uint4 *out = reinterpret_cast<uint4 *>(a.rows + static_cast<int64_t>(row) * a.D);
-  float dot = 0.f;
+  } else if (t < a.T) {
+    y = a.labels[t];
+    const uint4 *x = reinterpret_cast<const uint4 *>(a.X + static_cast<int64_t>(t) * a.D);
+    const uint4 *w = reinterpret_cast<const uint4 *>(a.W + y * a.D);
+    uint4 *out = reinterpret_cast<uint4 *>(a.rows + static_cast<int64_t>(row) * a.D);
 #pragma unroll 4
-  for (int i = lane; i < pieces; i += 32) {
-    const uint4 p = __ldg(x + i), q = __ldg(w + i);
-    out[i] = p;
-    const uint32_t pw[4] = {p.x, p.y, p.z, p.w}, qw[4] = {q.x, q.y, q.z, q.w};
+    for (int i = first; i < pieces; i += 32 * SHARE) {
+      const uint4 p = __ldg(x + i), q = __ldg(w + i);
+      out[i] = p;
+      const uint32_t pw[4] = {p.x, p.y, p.z, p.w}, qw[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      dot = fmaf(__uint_as_float(pw[c] << 16), __uint_as_float(qw[c] << 16), dot);
-      dot = fmaf(__uint_as_float(pw[c] & 0xFFFF0000u), __uint_as_float(qw[c] & 0xFFFF0000u), dot);
+      for (int c = 0; c < 4; ++c) {
+        dot = fmaf(__uint_as_float(pw[c] << 16), __uint_as_float(qw[c] << 16), dot);
+        dot = fmaf(__uint_as_float(pw[c] & 0xFFFF0000u), __uint_as_float(qw[c] & 0xFFFF0000u), dot);
+      }
     }
+    dot = warp_total(dot);
   }
-  dot = warp_total(dot);
-  if (lane == 0) {
+  if (SHARE > 1) {
+    if (lane == 0) dots[warp] = dot;
+    __syncthreads();
+    dot = 0.f;
+#pragma unroll
+    for (int w = 0; w < SHARE; ++w) dot += dots[own * SHARE + w];
+  }
+  if (t < a.T && target && first == 0) {
     a.token[row] = t;
     a.label[row] = static_cast<int>(y);
     a.label_z[row] = dot;
@@ -205,7 +218,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThre
   const int tiles_m = (chunk_rows(a, first) + C::kTile - 1) / C::kTile;
   const int tiles_n = static_cast<int>(((GRAD ? a.D : a.V) + C::kTile - 1) / C::kTile);
   const int stages = static_cast<int>(((GRAD ? a.V : a.D) + C::kBK - 1) / C::kBK);
-  const int parts = GRAD ? head_parts(static_cast<int64_t>(tiles_m) * tiles_n, stages, a.clusters) : 1;
+  const int parts = GRAD ? *a.parts : 1;
   const int total = tiles_m * tiles_n * parts;
 
   auto stage_a = [&](int s) { return smem + s * C::kStageBytes; };
@@ -438,20 +451,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThre
 
 // ---------------------------------------------------------------- finalize and rows
 
-// One warp per row: the quarter tiles' sums brought to one reference R and added in a fixed order.
+// SHARE warps per row: the quarter tiles' sums brought to one reference and added in a fixed
+// order. A large vocabulary takes a CTA per row (2004 sums: one warp needed 13.4 us).
+template <int SHARE>
 __global__ void __launch_bounds__(256) sq_head_finalize_kernel(const HeadArgs a, const int first) {
-  const int lane = threadIdx.x & 31;
-  const int r = blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (r >= chunk_rows(a, first)) return;
-  const int row = first + r;
+  __shared__ float tops[8], parts[8];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int rows = chunk_rows(a, first);
+  if (blockIdx.x == 0 && threadIdx.x == 0 && a.dX)  // the gradient launch's split of the vocabulary
+    *a.parts = head_parts(static_cast<int64_t>((rows + kHeadTile - 1) / kHeadTile) * ((a.D + kHeadTile - 1) / kHeadTile),
+                          static_cast<int>((a.V + HeadCfg<true>::kBK - 1) / HeadCfg<true>::kBK), a.clusters);
+  const int r = blockIdx.x * (8 / SHARE) + warp / SHARE;
+  if (SHARE == 8 ? r >= rows : blockIdx.x * 8 >= rows) return;  // whole CTAs
+  const bool in = r < rows;
+  const int row = first + (in ? r : 0);
   constexpr int kCols = HeadCfg<false>::kEpiCols;
   const int n = kHeadTile / kCols * static_cast<int>((a.V + kHeadTile - 1) / kHeadTile);
-  const int filled = static_cast<int>((a.V + kCols - 1) / kCols);  // quarter tiles that hold columns
+  const int filled = in ? static_cast<int>((a.V + kCols - 1) / kCols) : 0;  // quarter tiles that hold columns
   const float2 *sums = a.sums + static_cast<int64_t>(r) * n;
   const float z = a.label_z[row], z2 = z * kLog2e, ref0 = row_reference(z);
+  const int own = (warp % SHARE) * 32 + lane;
   float ref = ref0, sum = 0.f;
   bool moved = false;
-  for (int i = lane; i < filled; i += 32) {
+#pragma unroll 8
+  for (int i = own; i < filled; i += 32 * SHARE) {
     const float2 q = sums[i];
     moved |= q.y != ref0;
     const float top = fmaxf(ref, q.y);
@@ -461,13 +484,26 @@ __global__ void __launch_bounds__(256) sq_head_finalize_kernel(const HeadArgs a,
   float top = ref;
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-  const float others = warp_total(sum * whole_exp2(ref - top));
-  const float own = exp2_fast(z2 - top), total = others + own;
-  if (lane == 0) {
+  if (SHARE > 1) {
+    if (lane == 0) tops[warp] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < SHARE; ++w) top = fmaxf(top, tops[w]);
+  }
+  float others = warp_total(sum * whole_exp2(ref - top));
+  if (SHARE > 1) {
+    if (lane == 0) parts[warp] = others;
+    __syncthreads();
+    others = 0.f;
+#pragma unroll
+    for (int w = 0; w < SHARE; ++w) others += parts[w];
+  }
+  const float label = exp2_fast(z2 - top), total = others + label;
+  if (in && own == 0) {
     const int t = a.token[row];
-    // log(total / own): where own underflows against a far larger logit, from the exponents
+    // log(total / label): where label underflows against a far larger logit, from the exponents
     const bool near = top - z2 < 60.f;
-    const float loss = near ? log1pf(others / own) : (top - z2) * kLn2 + logf(total);
+    const float loss = near ? log1pf(others / label) : (top - z2) * kLn2 + logf(total);
     if (a.loss) a.loss[t] = loss;
     if (a.lse) a.lse[t] = near ? z + loss : top * kLn2 + logf(total);
     if (a.dX) {
@@ -475,8 +511,9 @@ __global__ void __launch_bounds__(256) sq_head_finalize_kernel(const HeadArgs a,
       a.factors[row] = make_float2(g / total, -g * (others / total));
     }
   }
-  if (a.e && __any_sync(0xFFFFFFFFu, moved)) {
-    for (int i = 0; i < filled; ++i) {
+  const bool rescale = SHARE > 1 ? __syncthreads_or(moved) : __any_sync(0xFFFFFFFFu, moved);
+  if (a.e && rescale) {
+    for (int i = warp % SHARE; i < filled; i += SHARE) {
       const float by = whole_exp2(sums[i].y - top);
       if (by == 1.f) continue;
       __nv_bfloat16 *e = reinterpret_cast<__nv_bfloat16 *>(a.e) + static_cast<int64_t>(r) * a.pitch;
@@ -497,12 +534,11 @@ __global__ void __launch_bounds__(256) sq_head_rows_kernel(const HeadArgs a, con
   const int64_t c = static_cast<int64_t>(unit % pieces) * 256 + lane * 8;
   if (c >= a.D) return;
   const int tiles_m = (rows + kHeadTile - 1) / kHeadTile;
-  const int tiles_n = static_cast<int>((a.D + kHeadTile - 1) / kHeadTile);
-  const int parts = head_parts(static_cast<int64_t>(tiles_m) * tiles_n,
-                               static_cast<int>((a.V + HeadCfg<true>::kBK - 1) / HeadCfg<true>::kBK), a.clusters);
+  const int parts = *a.parts;
   const int64_t plane = static_cast<int64_t>(tiles_m) * kHeadTile * a.D;
   const float *p = a.partial + static_cast<int64_t>(r) * a.D + c;
   float s[8] = {};
+#pragma unroll 4
   for (int i = 0; i < parts; ++i, p += plane) {
     const float4 u = __ldcs(reinterpret_cast<const float4 *>(p)), v = __ldcs(reinterpret_cast<const float4 *>(p) + 1);
     s[0] += u.x, s[1] += u.y, s[2] += u.z, s[3] += u.w;
@@ -535,7 +571,10 @@ cudaError_t launch_head_product(const CUtensorMap &tmA, const CUtensorMap &tmB, 
 }  // namespace
 
 cudaError_t launch_head_gather(const HeadArgs &a, cudaStream_t stream) {
-  sq_head_gather_kernel<<<static_cast<unsigned>((a.T + 7) / 8), 256, 0, stream>>>(a);
+  if (a.T <= 1024)
+    sq_head_gather_kernel<8><<<static_cast<unsigned>(a.T), 256, 0, stream>>>(a);
+  else
+    sq_head_gather_kernel<1><<<static_cast<unsigned>((a.T + 7) / 8), 256, 0, stream>>>(a);
   return cudaGetLastError();
 }
 
@@ -545,7 +584,10 @@ cudaError_t launch_head_chunk(const HeadArgs &a, const HeadMaps &m, int first, i
                                              tiles_m * ((a.V + kHeadTile - 1) / kHeadTile), sm_count, stream);
   if (e != cudaSuccess) return e;
   const int rows = a.T - first < a.chunk ? a.T - first : a.chunk;
-  sq_head_finalize_kernel<<<(rows + 7) / 8, 256, 0, stream>>>(a, first);
+  if (a.V > 16384)
+    sq_head_finalize_kernel<8><<<rows, 256, 0, stream>>>(a, first);
+  else
+    sq_head_finalize_kernel<1><<<(rows + 7) / 8, 256, 0, stream>>>(a, first);
   if ((e = cudaGetLastError()) != cudaSuccess || !a.dX) return e;
   if ((e = launch_head_product<true>(m.e_load, m.weights, m.partial, a, first, int64_t(1) << 30, sm_count, stream)) !=
       cudaSuccess)

@@ -2,6 +2,7 @@
 // gradient, the tokens sorted by expert, and the rows that travel to the experts and back.
 #include <cuda_bf16.h>
 #include <float.h>
+#include <limits.h>
 
 #include <algorithm>
 
@@ -38,6 +39,14 @@ __device__ __forceinline__ void load_logits4(const __nv_bfloat16 *p, float (&v)[
   v[0] = __uint_as_float(q.x << 16), v[1] = __uint_as_float(q.x & 0xFFFF0000u);
   v[2] = __uint_as_float(q.y << 16), v[3] = __uint_as_float(q.y & 0xFFFF0000u);
 }
+__device__ __forceinline__ void store_logits4(float *p, const float *v) {
+  *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ void store_logits4(__nv_bfloat16 *p, const float *v) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]), b = __floats2bfloat162_rn(v[2], v[3]);
+  *reinterpret_cast<uint2 *>(p) =
+      make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+}
 __device__ __forceinline__ void store_logit(float *p, float v) { *p = v; }
 __device__ __forceinline__ void store_logit(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 
@@ -69,6 +78,68 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
+// The winners of a lane in descending order: up to 8 logits are sorted first (stably, so equal
+// ones stay in the order of their experts) and a winner is shifted out; more are searched again
+// after each. 32768 tokens of 128 logits, top-8: 22.3 us with the search.
+template <int VEC, int PER>
+struct LaneTop {
+  static constexpr bool kSorted = PER <= 8;
+  uint32_t key[PER];
+  int expert[PER];
+  __device__ __forceinline__ LaneTop(const float (&z)[PER], int lane) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      key[i] = order_key(z[i]);
+      expert[i] = expert_of<VEC>(i, lane);
+    }
+    if (kSorted) {
+#pragma unroll
+      for (int n = PER - 1; n > 0; --n)
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+          const bool swap = key[i + 1] > key[i];
+          const uint32_t k = swap ? key[i + 1] : key[i];
+          const int e = swap ? expert[i + 1] : expert[i];
+          key[i + 1] = swap ? key[i] : key[i + 1];
+          expert[i + 1] = swap ? expert[i] : expert[i + 1];
+          key[i] = k;
+          expert[i] = e;
+        }
+    } else {
+      search();
+    }
+  }
+  uint32_t best_key;
+  int best_expert;
+  __device__ __forceinline__ uint32_t top() const { return kSorted ? key[0] : best_key; }
+  __device__ __forceinline__ int top_expert() const { return kSorted ? expert[0] : best_expert; }
+  __device__ __forceinline__ void pop() {
+    if (kSorted) {
+#pragma unroll
+      for (int i = 0; i + 1 < PER; ++i) {
+        key[i] = key[i + 1];
+        expert[i] = expert[i + 1];
+      }
+      key[PER - 1] = 0;
+    } else {
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (expert[i] == best_expert) key[i] = 0;
+      search();
+    }
+  }
+  __device__ __forceinline__ void search() {
+    best_key = 0;
+    best_expert = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (key[i] > best_key) {
+        best_key = key[i];
+        best_expert = expert[i];
+      }
+  }
+};
+
 template <int VEC, int PER, typename T>
 __global__ void __launch_bounds__(256)
     sq_route_kernel(int64_t tokens, int E, int k, const T *__restrict__ logits, const uint8_t *__restrict__ valid,
@@ -82,41 +153,29 @@ __global__ void __launch_bounds__(256)
   if (on) {
     float z[PER];
     load_row<VEC, PER>(logits + t * E, E, lane, z);
-    uint32_t key[PER], best = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      key[i] = order_key(z[i]);
-      best = max(best, key[i]);
-    }
+    LaneTop<VEC, PER> own(z, lane);
     for (int j = 0; j < k; ++j) {
-      const uint32_t won = __reduce_max_sync(kAll, best);
+      const uint32_t won = __reduce_max_sync(kAll, own.top());
       if (won == 0) break;
       if (j == 0) {
         top = key_value(won);
         if (!normalize) {
 #pragma unroll
           for (int i = 0; i < PER; ++i)
-            if (key[i]) total += expf(key_value(key[i]) - top);
+            if (z[i] > -INFINITY) total += expf(fminf(z[i], FLT_MAX) - top);
           total = warp_sum(total);
         }
       }
-      uint32_t mine = 0xFFFFFFFFu;  // the lowest expert of this lane with the winning logit
-      if (best == won) {
-#pragma unroll
-        for (int i = PER - 1; i >= 0; --i)
-          if (key[i] == won) mine = expert_of<VEC>(i, lane);
+      const uint32_t same = __ballot_sync(kAll, own.top() == won);
+      int winner = __ffs(same) - 1;
+      int e = __shfl_sync(kAll, own.top_expert(), winner);
+      if (same & (same - 1)) {  // equal logits in several lanes: the lowest expert
+        e = __reduce_min_sync(kAll, own.top() == won ? own.top_expert() : INT_MAX);
+        winner = __ffs(__ballot_sync(kAll, own.top() == won && own.top_expert() == e)) - 1;
       }
-      const uint32_t e = __reduce_min_sync(kAll, mine);
-      if (mine == e) {
-        best = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          if (expert_of<VEC>(i, lane) == static_cast<int>(e)) key[i] = 0;
-          best = max(best, key[i]);
-        }
-      }
+      if (lane == winner) own.pop();
       if (lane == j) {
-        my_expert = static_cast<int>(e);
+        my_expert = e;
         my_value = key_value(won);
       }
     }
@@ -177,9 +236,13 @@ __global__ void __launch_bounds__(256)
 #pragma unroll
   for (int i = 0; i < PER; ++i) dense[i] = any && !normalize ? -(dense[i] / total) * inner : 0.f;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
+  for (int i = 0; i < PER; i += VEC) {
     const int at = expert_of<VEC>(i, lane);
-    if (at < E) store_logit(out + at, dense[i]);
+    if (at >= E) continue;
+    if (VEC == 4)
+      store_logits4(out + at, dense + i);
+    else
+      store_logit(out + at, dense[i]);
   }
   __syncwarp();  // the chosen experts' values go over the row's
   if (key) store_logit(out + e, share * (dw - inner));
@@ -187,89 +250,94 @@ __global__ void __launch_bounds__(256)
 
 // ---------------------------------------------------------------- tokens by expert
 //
-// Stable counting sort of the n slots t * k + j by expert. One cluster of CTAs: each warp owns a
-// run of neighbouring slots and a histogram row, the prefix over warps, CTAs (through
-// distributed shared memory) and experts gives each its first row, and a second pass hands the
-// rows out in slot order, so the order never depends on timing.
+// Stable counting sort of the n slots t * k + j by expert. Each warp owns a run of neighbouring
+// slots and a histogram row; the prefix over warps, CTAs and experts gives each its first row, and
+// rows are handed out in slot order, so the order never depends on timing. Up to kSortOne slots
+// take one CTA; more take a launch that counts per CTA and one that adds up the counts and places
+// the slots (each CTA reads all CTAs' counts: G x E words from the L2).
 
-constexpr int kSortStep = 8;  // loads of 32 slots in flight
+constexpr int kSortStep = 4;  // loads of 32 slots in flight
+constexpr int64_t kSortOne = 4096;
+constexpr int64_t kSortMany = 2048;  // slots of a CTA at least, of several
+constexpr int kSortThreads = 512;    // of a CTA, of several
 
-__device__ __forceinline__ uint32_t sort_cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ uint32_t sort_cluster_size() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void sort_cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ int remote_int(const int *p, uint32_t rank) {
-  uint32_t a = static_cast<uint32_t>(__cvta_generic_to_shared(p)), r;
-  int v;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
-  asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(r) : "memory");
-  return v;
+__device__ __forceinline__ void load_slots(const int *experts, int64_t at, int64_t end, int E, int lane,
+                                           int (&e)[kSortStep]) {
+#pragma unroll
+  for (int s = 0; s < kSortStep; ++s) {
+    const int64_t i = at + 32 * s + lane;
+    e[s] = i < end ? __ldg(experts + i) : -1;
+    if (e[s] >= E) e[s] = -1;
+  }
 }
 
+__global__ void __launch_bounds__(kSortThreads)
+    sq_sort_count_kernel(int64_t n, int E, int64_t per, const int *__restrict__ experts, int *__restrict__ counts) {
+  extern __shared__ int sort_smem[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = kSortThreads / 32;
+  for (int i = threadIdx.x; i < E; i += kSortThreads) sort_smem[i] = 0;
+  __syncthreads();
+  const int64_t begin = blockIdx.x * per, end = min(n, begin + per);
+  for (int64_t at = begin + warp * 32 * kSortStep; at < end; at += warps * 32 * kSortStep) {
+    int e[kSortStep];
+    load_slots(experts, at, end, E, lane, e);
+#pragma unroll
+    for (int s = 0; s < kSortStep; ++s)
+      if (e[s] >= 0) atomicAdd(sort_smem + e[s], 1);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < E; i += kSortThreads) counts[static_cast<int64_t>(blockIdx.x) * E + i] = sort_smem[i];
+}
+
+// counts: [gridDim.x, E] of the launch before, or null for the one CTA that takes all slots.
 __global__ void __launch_bounds__(1024)
-    sq_sort_kernel(int64_t n, int E, const int *__restrict__ experts, int64_t *__restrict__ offsets,
-                   int *__restrict__ row_of, int *__restrict__ slot_of) {
+    sq_sort_kernel(int64_t n, int E, int64_t per, const int *__restrict__ experts, const int *__restrict__ counts,
+                   int64_t *__restrict__ offsets, int *__restrict__ row_of, int *__restrict__ slot_of) {
   extern __shared__ int sort_smem[];
   const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  int *hist = sort_smem;             // [warps][E]
-  int *counts = hist + warps * E;    // [E] slots of this CTA
-  int *first = counts + E;           // [E] first row of this CTA's slots of an expert
+  int *hist = sort_smem;           // [warps][E]
+  int *all = hist + warps * E;     // [E] slots of an expert
+  int *first = all + E;            // [E] those of earlier CTAs, then the first row of this one's
   __shared__ int scan[32];
-  __shared__ int routed;
-  const uint32_t rank = sort_cluster_rank(), ctas = sort_cluster_size();
-  const int64_t per_warp = ((n + ctas * warps - 1) / (ctas * warps) + 31) / 32 * 32;
-  const int64_t begin = min(n, (static_cast<int64_t>(rank) * warps + warp) * per_warp);
-  const int64_t end = min(n, begin + per_warp);
-  for (int i = threadIdx.x; i < warps * E; i += blockDim.x) hist[i] = 0;
+  const int64_t cta_end = min(n, (blockIdx.x + 1) * per);
+  const int64_t per_warp = (per + warps * 32 - 1) / (warps * 32) * 32;
+  const int64_t begin = min(cta_end, blockIdx.x * per + warp * per_warp);
+  const int64_t end = min(cta_end, begin + per_warp);
+  for (int i = threadIdx.x; i < (warps + 2) * E; i += blockDim.x) hist[i] = 0;
   __syncthreads();
   int *mine = hist + warp * E;
-  auto load = [&](int64_t at, int (&e)[kSortStep]) {
-#pragma unroll
-    for (int s = 0; s < kSortStep; ++s) {
-      const int64_t i = at + 32 * s + lane;
-      e[s] = i < end ? __ldg(experts + i) : -1;
-      if (e[s] >= E) e[s] = -1;
-    }
-  };
   for (int64_t at = begin; at < end; at += 32 * kSortStep) {
     int e[kSortStep];
-    load(at, e);
+    load_slots(experts, at, end, E, lane, e);
 #pragma unroll
     for (int s = 0; s < kSortStep; ++s)
       if (e[s] >= 0) atomicAdd(mine + e[s], 1);
   }
-  __syncthreads();
-  for (int e = threadIdx.x; e < E; e += blockDim.x) {
-    int sum = 0;
-    for (int w = 0; w < warps; ++w) {
-      const int c = hist[w * E + e];
-      hist[w * E + e] = sum;
-      sum += c;
+  if (counts) {
+    const int cells = gridDim.x * E, before = blockIdx.x * E;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < cells; i += blockDim.x) {
+      const int c = counts[i];
+      if (c == 0) continue;
+      const int e = i % E;
+      atomicAdd(all + e, c);
+      if (i < before) atomicAdd(first + e, c);
     }
-    counts[e] = sum;
   }
-  sort_cluster_sync();
-  // rows of all CTAs per expert, scanned over the experts a block width at a time
+  __syncthreads();
   int carry = 0;
-  for (int e0 = 0; e0 < E; e0 += blockDim.x) {
+  for (int e0 = 0; e0 < E; e0 += blockDim.x) {  // the experts' prefix, a block width at a time
     const int e = e0 + threadIdx.x;
-    int before = 0, all = 0;
-    if (e < E)
-      for (uint32_t r = 0; r < ctas; ++r) {
-        const int c = remote_int(counts + e, r);
-        before += r < rank ? c : 0;
-        all += c;
+    int here = 0;
+    if (e < E) {
+      for (int w = 0; w < warps; ++w) {
+        const int c = hist[w * E + e];
+        hist[w * E + e] = here;
+        here += c;
       }
-    int incl = all;
+      if (counts) here = all[e];
+    }
+    int incl = here;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
       const int v = __shfl_up_sync(kAll, incl, d);
@@ -287,22 +355,18 @@ __global__ void __launch_bounds__(1024)
       scan[lane] = v;
     }
     __syncthreads();
-    const int start = carry + incl - all + (warp > 0 ? scan[warp - 1] : 0);
+    const int start = carry + incl - here + (warp > 0 ? scan[warp - 1] : 0);
     carry += scan[31];
     if (e < E) {
-      first[e] = start + before;
-      if (rank == 0) offsets[e] = start;
+      first[e] += start;
+      if (blockIdx.x == 0) offsets[e] = start;
     }
     __syncthreads();
   }
-  if (threadIdx.x == 0) {
-    routed = carry;
-    if (rank == 0) offsets[E] = carry;
-  }
-  sort_cluster_sync();  // every CTA has read the others' counts; first and routed are visible
+  if (blockIdx.x == 0 && threadIdx.x == 0) offsets[E] = carry;
   for (int64_t at = begin; at < end; at += 32 * kSortStep) {
     int e[kSortStep];
-    load(at, e);
+    load_slots(experts, at, end, E, lane, e);
 #pragma unroll
     for (int s = 0; s < kSortStep; ++s) {
       const int64_t i = at + 32 * s + lane;
@@ -318,8 +382,8 @@ __global__ void __launch_bounds__(1024)
       }
     }
   }
-  for (int64_t r = routed + static_cast<int64_t>(rank) * blockDim.x + threadIdx.x; r < n;
-       r += static_cast<int64_t>(ctas) * blockDim.x)
+  for (int64_t r = carry + static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; r < n;
+       r += static_cast<int64_t>(gridDim.x) * blockDim.x)
     slot_of[r] = -1;
 }
 
@@ -392,16 +456,15 @@ __global__ void __launch_bounds__(256)
 }
 
 // Y[t] = sum_j w[t, j] Ys[row_of[t, j]] in fp32 in the order of j, rounded once (without
-// weights: the plain sum, the gradient of the dispatch). A warp takes 256 columns of one token.
+// weights: the plain sum, the gradient of the dispatch). `share` warps per token, which take its
+// 256-column pieces in turn.
 constexpr int kCombineFlight = 8;  // rows in flight
 __global__ void __launch_bounds__(256)
-    sq_combine_kernel(uint32_t units, uint32_t pieces, int k, int64_t D, int64_t rows, const uint16_t *__restrict__ Ys,
+    sq_combine_kernel(int64_t tokens, int k, int64_t D, int64_t rows, int share, const uint16_t *__restrict__ Ys,
                       const int *__restrict__ row_of, const float *__restrict__ weights, uint16_t *__restrict__ Y) {
-  const int lane = threadIdx.x & 31;
-  const uint32_t unit = blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (unit >= units) return;
-  const int64_t t = unit / pieces;
-  const int64_t c = static_cast<int64_t>(unit % pieces) * 256 + lane * 8;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * (8 / share) + warp / share;
+  if (t >= tokens) return;
   int64_t row = -1;
   float w = 1.f;
   if (lane < k) {
@@ -409,27 +472,37 @@ __global__ void __launch_bounds__(256)
     if (row >= rows) row = -1;
     if (weights) w = weights[t * k + lane];
   }
-  float sum[8] = {};
-  for (int j0 = 0; j0 < k; j0 += kCombineFlight) {
-    uint4 v[kCombineFlight];
-    int64_t from[kCombineFlight];
+  int64_t at[kCombineFlight];
+  float wj[kCombineFlight];
+  auto batch = [&](int j0) {
 #pragma unroll
     for (int i = 0; i < kCombineFlight; ++i) {
-      from[i] = __shfl_sync(kAll, row, j0 + i);
-      if (j0 + i >= k || c >= D) from[i] = -1;
-      if (from[i] >= 0) v[i] = load_row16(Ys + from[i] * D + c);
+      at[i] = __shfl_sync(kAll, row, j0 + i);
+      wj[i] = __shfl_sync(kAll, w, j0 + i);
+      if (j0 + i >= k) at[i] = -1;
     }
+  };
+  batch(0);
+  for (int64_t c0 = (warp % share) * 256; c0 < D; c0 += share * 256) {
+    const int64_t c = c0 + lane * 8;
+    float sum[8] = {};
+    for (int j0 = 0; j0 < k; j0 += kCombineFlight) {
+      if (k > kCombineFlight) batch(j0);
+      uint4 v[kCombineFlight];
 #pragma unroll
-    for (int i = 0; i < kCombineFlight; ++i) {
-      const float wi = __shfl_sync(kAll, w, j0 + i);
-      if (from[i] < 0) continue;
-      float x[8];
-      unpack8(v[i], x);
+      for (int i = 0; i < kCombineFlight; ++i)
+        if (at[i] >= 0 && c < D) v[i] = load_row16(Ys + at[i] * D + c);
 #pragma unroll
-      for (int q = 0; q < 8; ++q) sum[q] = fmaf(wi, x[q], sum[q]);
+      for (int i = 0; i < kCombineFlight; ++i) {
+        if (at[i] < 0) continue;
+        float x[8];
+        unpack8(v[i], x);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) sum[q] = fmaf(wj[i], x[q], sum[q]);
+      }
     }
+    if (c < D) store_row16(Y + t * D + c, pack8(sum));
   }
-  if (c < D) store_row16(Y + t * D + c, pack8(sum));
 }
 
 // dYs[row_of[t, j]] = w[t, j] dY[t] and dw[t, j] = sum_d dY[t, d] Ys[row_of[t, j], d]. One token
@@ -565,28 +638,46 @@ cudaError_t launch_route_grad(int64_t T, int E, int k, bool bf16, const void *lo
   return cudaGetLastError();
 }
 
+static int64_t sort_per_cta(int64_t n, int sm_count) {
+  if (n <= kSortOne) return n;
+  const int64_t even = (n + sm_count - 1) / sm_count;
+  return std::max(kSortMany, (even + kSortThreads - 1) / kSortThreads * kSortThreads);
+}
+
+size_t sort_workspace(int64_t n, int E, int sm_count) {
+  if (n <= kSortOne) return 0;
+  const int64_t per = sort_per_cta(n, sm_count);
+  return static_cast<size_t>((n + per - 1) / per) * E * sizeof(int);
+}
+
 cudaError_t launch_sort(int64_t n, int E, const int *experts, int64_t *offsets, int *row_of, int *slot_of,
-                        cudaStream_t stream) {
-  // few slots: one CTA of eight warps, whose prefix over the warps is short
-  const int ctas = n <= 8192 ? 1 : 8, threads = n <= 2048 ? 256 : 1024;
+                        int *workspace, int sm_count, cudaStream_t stream) {
+  const bool one = n <= kSortOne;
+  const int64_t per = sort_per_cta(n, sm_count);
+  const unsigned ctas = one ? 1 : static_cast<unsigned>((n + per - 1) / per);
+  // few slots: eight warps, whose prefix is short
+  const int threads = one ? (n <= 1024 ? 256 : 1024) : kSortThreads;
+  if (!one) {
+    sq_sort_count_kernel<<<ctas, kSortThreads, E * sizeof(int), stream>>>(n, E, per, experts, workspace);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+  }
   const size_t smem = (static_cast<size_t>(threads / 32) + 2) * E * sizeof(int);
   if (smem > 48 * 1024) {
     const cudaError_t e = cudaFuncSetAttribute(sq_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                34 * kRouteMaxExperts * static_cast<int>(sizeof(int)));
     if (e != cudaSuccess) return e;
   }
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(ctas, 1, 1);
-  cfg.blockDim = dim3(threads, 1, 1);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = ctas;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, sq_sort_kernel, n, E, experts, offsets, row_of, slot_of);
+  sq_sort_kernel<<<ctas, threads, smem, stream>>>(n, E, per, experts, one ? nullptr : workspace, offsets, row_of,
+                                                  slot_of);
+  return cudaGetLastError();
+}
+
+// Warps of a token: as many as it takes for `warps` in all, at most one per 256 columns.
+static int warps_of_token(int64_t T, int64_t D, int64_t warps) {
+  int share = 1;
+  while (share < 8 && T * share < warps && share * 256 < D) share *= 2;
+  return share;
 }
 
 cudaError_t launch_dispatch(int64_t T, int k, int64_t D, int64_t rows, const uint16_t *X, const int *row_of,
@@ -598,18 +689,18 @@ cudaError_t launch_dispatch(int64_t T, int k, int64_t D, int64_t rows, const uin
 }
 
 cudaError_t launch_combine(int64_t T, int k, int64_t D, int64_t rows, const uint16_t *Ys, const int *row_of,
-                           const float *weights, uint16_t *Y, cudaStream_t stream) {
-  const uint32_t pieces = static_cast<uint32_t>((D + 255) / 256), units = static_cast<uint32_t>(T) * pieces;
-  sq_combine_kernel<<<(units + 7) / 8, 256, 0, stream>>>(units, pieces, k, D, rows, Ys, row_of, weights, Y);
+                           const float *weights, uint16_t *Y, int sm_count, cudaStream_t stream) {
+  const int share = warps_of_token(T, D, 32 * static_cast<int64_t>(sm_count));
+  const int64_t per = 8 / share;
+  sq_combine_kernel<<<static_cast<unsigned>((T + per - 1) / per), 256, 0, stream>>>(T, k, D, rows, share, Ys, row_of,
+                                                                                   weights, Y);
   return cudaGetLastError();
 }
 
 cudaError_t launch_combine_grad(int64_t T, int k, int64_t D, int64_t rows, const uint16_t *dY, const uint16_t *Ys,
                                 const int *row_of, const int *slot_of, const float *weights, uint16_t *dYs,
                                 float *dweights, int sm_count, cudaStream_t stream) {
-  // warps of a token: as many as keep the SMs busy, at most one per 256 columns
-  int share = 1;
-  while (share < 8 && T * share < 16 * static_cast<int64_t>(sm_count) && share * 256 < D) share *= 2;
+  const int share = warps_of_token(T, D, 16 * static_cast<int64_t>(sm_count));
   const int64_t per = 8 / share;
   sq_combine_grad_kernel<<<static_cast<unsigned>((T + per - 1) / per), 256, 0, stream>>>(
       T, k, D, rows, share, dY, Ys, row_of, slot_of, weights, dYs, dweights);
