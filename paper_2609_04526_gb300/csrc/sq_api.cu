@@ -439,7 +439,6 @@ sq_status run_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint
   a.D = D;
   a.V = V;
   a.W = W;
-  a.clusters = dev->sm_count / 2;
   a.pitch = up(V, 8);  // rows of e start on 16 bytes
   a.err = dev->err_word;
   int64_t chunk = whole;
@@ -448,39 +447,48 @@ sq_status run_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint
     chunk = std::min(whole, std::max<int64_t>(fit, sqi::kHeadTile));
   }
   a.chunk = static_cast<int>(chunk);
+  a.box_rows = T <= 32 ? 32 : T <= 64 ? 64 : 128;
   const int64_t quarters = 4 * ((V + sqi::kHeadTile - 1) / sqi::kHeadTile);
-  const int64_t partial_rows = dX ? sqi::head_partial_rows(chunk, D, V, a.clusters) : 0;
+  int64_t partial_rows = 0;  // of 4 * D bytes: the most that any number of labelled rows takes
+  for (int64_t m = 1; dX && m <= chunk / sqi::kHeadTile; ++m) {
+    const int parts = sqi::head_parts(m * ((D + sqi::kHeadTile - 1) / sqi::kHeadTile), static_cast<int>((V + 127) / 128),
+                                      dev->sm_count / 2);
+    a.parts[m - 1] = static_cast<uint8_t>(parts - 1);
+    partial_rows = std::max(partial_rows, m * sqi::kHeadTile * parts);
+  }
   size_t used = 0;
   auto take = [&](int64_t bytes) {
     const size_t at = used;
     used += static_cast<size_t>(up(bytes, 1024));
     return at;
   };
-  const size_t o_count = take(8), o_token = take(4 * piece), o_label = take(4 * piece), o_z = take(4 * piece),
-               o_factors = take(8 * piece), o_rows = take(2 * D * whole), o_sums = take(8 * quarters * chunk),
+  const size_t o_count = take(4), o_token = take(4 * piece), o_label = take(4 * piece), o_z = take(4 * piece),
+               o_factors = take(8 * piece), o_rows = take(2 * D * whole), o_sums = take(4 * quarters * chunk), o_refs = take(4 * quarters * chunk),
+               o_moved = take(4 * chunk),
                o_e = take(dX ? 2 * a.pitch * chunk : 0), o_partial = take(4 * D * partial_rows);
   SQ_TRY(ensure_scratch(h, dev->head, used, stream, "the head loss"));
   uint8_t *base = static_cast<uint8_t *>(dev->head.ptr);
   a.count = reinterpret_cast<int *>(base + o_count);
-  a.parts = a.count + 1;
   a.token = reinterpret_cast<int *>(base + o_token);
   a.label = reinterpret_cast<int *>(base + o_label);
   a.label_z = reinterpret_cast<float *>(base + o_z);
   a.factors = reinterpret_cast<float2 *>(base + o_factors);
   a.rows = reinterpret_cast<uint16_t *>(base + o_rows);
-  a.sums = reinterpret_cast<float2 *>(base + o_sums);
+  a.sums = reinterpret_cast<float *>(base + o_sums);
+  a.refs = reinterpret_cast<float *>(base + o_refs);
+  a.moved = reinterpret_cast<int *>(base + o_moved);
   if (dX) {
     a.e = reinterpret_cast<uint16_t *>(base + o_e);
     a.partial = reinterpret_cast<float *>(base + o_partial);
   }
   sqi::HeadMaps m;
-  SQ_TRY(make_act_map(h, &m.rows, a.rows, D, whole, 64, 128));
+  SQ_TRY(make_act_map(h, &m.rows, a.rows, D, whole, 64, a.box_rows));
   SQ_TRY(make_act_map(h, &m.weights, W, D, V, 64, 128));
   m.e_store = m.e_load = m.partial = m.rows;
   if (dX) {
     SQ_TRY(make_map(h, &m.e_store, a.e, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, V, chunk, 32, 32,
                     CU_TENSOR_MAP_SWIZZLE_64B, a.pitch));
-    SQ_TRY(make_map(h, &m.e_load, a.e, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, V, chunk, 64, 128,
+    SQ_TRY(make_map(h, &m.e_load, a.e, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, V, chunk, 64, a.box_rows,
                     CU_TENSOR_MAP_SWIZZLE_128B, a.pitch));
     SQ_TRY(make_map(h, &m.partial, a.partial, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, D, partial_rows, 32, 32,
                     CU_TENSOR_MAP_SWIZZLE_128B));

@@ -6,6 +6,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 namespace sqi {
 
 enum GemmMode : int {
@@ -385,36 +387,19 @@ cudaError_t launch_combine_grad(int64_t T, int k, int64_t D, int64_t rows, const
 constexpr int kHeadTile = 256;
 constexpr int kHeadPiece = 16384;
 constexpr int64_t kHeadPieceBytes = int64_t(512) << 20;
-constexpr int kMaxHeadParts = 32;
-constexpr int kMinHeadPartStages = 8;  // a part of the vocabulary is at least 8 x 128 entries long
+constexpr int kMaxHeadParts = 64;
+constexpr int kMinHeadPartStages = 2;  // a part of the vocabulary is at least 2 x 128 entries long
 
 // Vocabulary parts of a gradient launch of `tiles` tiles: with w(s) = ceil(tiles s / clusters) / s
 // the launch's length in whole tiles per cluster, the smallest s within 3 % of the smallest w (each
 // part writes and reads back an fp32 plane of the tile).
-__host__ __device__ inline int head_parts(int64_t tiles, int stages, int clusters) {
-  if (tiles <= 0 || clusters <= 0) return 1;
-  int most = stages / kMinHeadPartStages;
-  most = most < 1 ? 1 : (most > kMaxHeadParts ? kMaxHeadParts : most);
-  // w(s) / w(1) compared as fractions: ceil(tiles s / clusters) / s
-  int64_t best_n = 1, best_d = 0;  // infinite
-  for (int s = 1; s <= most; ++s) {
-    const int64_t n = (tiles * s + clusters - 1) / clusters;
-    if (best_d == 0 || n * best_d < best_n * s) best_n = n, best_d = s;
-  }
-  for (int s = 1; s < most; ++s) {
-    const int64_t n = (tiles * s + clusters - 1) / clusters;
-    if (100 * n * best_d <= 103 * best_n * s) return s;
-  }
-  return most;
-}
-// Rows of 4 * D bytes that the parts of at most `chunk` rows take.
-inline int64_t head_partial_rows(int64_t chunk, int64_t D, int64_t V, int clusters) {
-  int64_t most = 0;
-  for (int64_t m = 1; m <= chunk / kHeadTile; ++m) {
-    const int64_t rows =
-        m * kHeadTile * head_parts(m * ((D + kHeadTile - 1) / kHeadTile), static_cast<int>((V + 127) / 128), clusters);
-    most = rows > most ? rows : most;
-  }
+inline int head_parts(int64_t tiles, int stages, int clusters) {
+  const int most = std::max(1, std::min(stages / kMinHeadPartStages, kMaxHeadParts));
+  auto waves = [&](int s) { return static_cast<double>((tiles * s + clusters - 1) / clusters) / s; };
+  double best = waves(1);
+  for (int s = 2; s <= most; ++s) best = std::min(best, waves(s));
+  for (int s = 1; s < most; ++s)
+    if (waves(s) <= 1.03 * best) return s;
   return most;
 }
 
@@ -427,23 +412,24 @@ struct HeadArgs {
   const float *dloss;     // [T] (gradient)
   float *loss, *lse;      // [T] or null
   uint16_t *dX;           // [T, D] bf16, or null: no gradient
+  int box_rows;           // rows of A in a shared-memory stage: 32, 64 or 128, all that few tokens have
   int chunk;              // rows of a chunk, a multiple of kHeadTile
-  int clusters;           // for head_parts
+  uint8_t parts[kHeadPiece / kHeadTile];  // vocabulary parts of the gradient by row tiles of the chunk, less 1
   int64_t pitch;          // elements of a row of e
   // scratch, by compact row of the piece
   int *count;             // labelled tokens of the piece
-  int *parts;             // vocabulary parts of the chunk's gradient launch
   int *token, *label;
   float *label_z;
   float2 *factors;
   uint16_t *rows;         // [T, D] the labelled tokens' rows of X
   // scratch, by row of the chunk
-  float2 *sums;           // [chunk, 4 * column tiles] sum and reference of each quarter tile
+  float *sums, *refs;     // [chunk, 4 * column tiles] sum and reference of each quarter tile
+  int *moved;             // [chunk] a row whose references differ (refs are read only there)
   uint16_t *e;            // [chunk, pitch] bf16 exponentials (gradient)
   float *partial;         // [parts, rows, D] fp32 (gradient)
   int *err;
 };
-// rows and weights: 64 x 128 boxes, 128-byte swizzle; e_store 32 x 32, 64-byte swizzle; partial
+// weights: 64 x 128 boxes, rows and e_load 64 x box_rows, 128-byte swizzle; e_store 32 x 32, 64-byte swizzle; partial
 // 32 x 32 fp32, 128-byte swizzle.
 struct HeadMaps {
   CUtensorMap rows, weights, e_store, e_load, partial;

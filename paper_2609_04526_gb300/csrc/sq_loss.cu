@@ -42,13 +42,11 @@ struct HeadCfg {
   static constexpr int kMmaWarp = kTmaWarp + 1;
   static constexpr int kThreads = 32 * (kMmaWarp + 1);
   static constexpr int kBK = 128;  // contraction indices of a stage
-  static constexpr int kStages = 3;
-  static constexpr int kA = 128 * kBK * 2;  // this CTA's 128 rows
-  static constexpr int kB = 128 * kBK * 2;  // this CTA's 128 columns
-  static constexpr int kStageBytes = kA + kB;
-  static constexpr uint32_t kTx = 2 * kStageBytes;  // both CTAs' tiles, on the leader's barrier
+  static constexpr int kB = 128 * kBK * 2;  // bytes of this CTA's 128 columns of a stage
+  static constexpr int kRing = 3 * 2 * kB;  // three stages of 128 rows and 128 columns
+  static constexpr int kMaxStages = 4;
   static constexpr int kTile = kHeadTile;
-  static constexpr int kOffBox = kStages * kStageBytes;
+  static constexpr int kOffBox = kRing;
   static constexpr int kBoxBytes = 32 * 32 * (GRAD ? 4 : 2);  // 32 rows x 32 columns of a warp
   // Stages added up in one accumulator. The tensor core truncates its running fp32 sum at every
   // step of 16, a bias that grows with the length: a sum of 4096 products in one accumulator left
@@ -88,6 +86,10 @@ __device__ __forceinline__ float warp_total(float v) {
   return v;
 }
 
+// Programmatic dependents of this launch may start; wait for the launch before this one to end.
+__device__ __forceinline__ void dependency_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // Reference exponent of a row from its label logit in powers of two; never -inf, and a NaN logit
 // leaves a number here (the row's NaN reaches its results through the label's own term).
 __device__ __forceinline__ float row_reference(float label_z) { return fmaxf(ceilf(label_z * kLog2e), -1e30f); }
@@ -109,12 +111,14 @@ __global__ void __launch_bounds__(256) sq_head_gather_kernel(const HeadArgs a) {
   constexpr int kTokens = 8 / SHARE;
   __shared__ int before[8];
   __shared__ float dots[8];
+  dependency_start();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int t0 = blockIdx.x * kTokens, own = warp / SHARE, t = t0 + own;
   auto labelled = [&](int i) {
     const int64_t y = a.labels[i];
     return y >= 0 && y < a.V;
   };
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < a.chunk; i += gridDim.x * 256) a.moved[i] = 0;
   int seen = 0;
   for (int i = threadIdx.x; i < t0; i += 256) seen += labelled(i);
   const uint32_t here =  // the same in every warp
@@ -200,12 +204,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThre
     sq_head_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                    const __grid_constant__ CUtensorMap tmO, const HeadArgs a, const int first) {
   using C = HeadCfg<GRAD>;
-  constexpr int S = C::kStages;
+  // A stage holds box_rows rows of A; the MMAs read 128 all the same, the rest of them whatever
+  // lies behind in the ring, and nothing reads those rows of the product. Few tokens so leave the
+  // ring to the columns: 4 stages of 64 rows and fewer, 3 of 128.
+  constexpr int kMax = C::kMaxStages;
+  const int a_bytes = a.box_rows * C::kBK * 2, stage_bytes = a_bytes + C::kB;
+  const int S = min(kMax, C::kRing / stage_bytes);
+  const bool both = a.T > 128;  // else the peer's rows of A are past the last token
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t *full = reinterpret_cast<uint64_t *>(smem + C::kOffBar);  // [S] leader: both CTAs' tiles landed
-  uint64_t *empty = full + S;    // [S] the pair's MMAs have read the stage        (multicast commit)
-  uint64_t *tfull = empty + S;   // [2] accumulator complete                       (multicast commit)
+  uint64_t *empty = full + kMax;    // [S] the pair's MMAs have read the stage        (multicast commit)
+  uint64_t *tfull = empty + kMax;   // [2] accumulator complete                       (multicast commit)
   uint64_t *tempty = tfull + 2;  // [2] leader: both epilogues drained it (kEpiWarps arrivals + the peer's st.async)
   uint64_t *drain = tempty + 2;
   uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(drain + 1);
@@ -215,14 +225,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThre
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const int cluster = blockIdx.x >> 1, nclusters = gridDim.x >> 1;
-  const int tiles_m = (chunk_rows(a, first) + C::kTile - 1) / C::kTile;
-  const int tiles_n = static_cast<int>(((GRAD ? a.D : a.V) + C::kTile - 1) / C::kTile);
-  const int stages = static_cast<int>(((GRAD ? a.V : a.D) + C::kBK - 1) / C::kBK);
-  const int parts = GRAD ? *a.parts : 1;
-  const int total = tiles_m * tiles_n * parts;
+  dependency_start();
 
-  auto stage_a = [&](int s) { return smem + s * C::kStageBytes; };
-  auto stage_b = [&](int s) { return smem + s * C::kStageBytes + C::kA; };
+  auto stage_a = [&](int s) { return smem + s * stage_bytes; };
+  auto stage_b = [&](int s) { return smem + s * stage_bytes + a_bytes; };
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) {
@@ -248,6 +254,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThre
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
 
+  dependency_wait();
+  const int rows = chunk_rows(a, first);
+  const int tiles_m = (rows + C::kTile - 1) / C::kTile;
+  const int tiles_n = static_cast<int>(((GRAD ? a.D : a.V) + C::kTile - 1) / C::kTile);
+  const int stages = static_cast<int>(((GRAD ? a.V : a.D) + C::kBK - 1) / C::kBK);
+  const int parts = GRAD && tiles_m > 0 ? a.parts[tiles_m - 1] + 1 : 1;
+  const int total = tiles_m * tiles_n * parts;
+
   if (warp == C::kTmaWarp) {
     // ------------------------------------------------------ TMA producer (both CTAs)
     if (lane == 0) {
@@ -261,10 +275,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThre
           const int s = it % S;
           const uint32_t use = static_cast<uint32_t>(it / S);
           if (it >= S && !(ok = mbar_wait(&empty[s], (use & 1u) ^ 1u, abort_flag, a.err))) break;
-          if (rank == 0) mbar_arrive_expect_tx(&full[s], C::kTx);
+          if (rank == 0) mbar_arrive_expect_tx(&full[s], 2 * C::kB + (both ? 2 : 1) * a_bytes);
           const uint32_t bar = mapa_shared(smem_u32(&full[s]), 0);
-          for (int j = 0; j < 2; ++j)
-            tma_load_2d_pair(smem_u32(stage_a(s)) + j * 16384, &tmA, bar, kb * C::kBK + 64 * j, row0);
+          if (rank == 0 || both)
+            for (int j = 0; j < 2; ++j)
+              tma_load_2d_pair(smem_u32(stage_a(s)) + j * (a_bytes / 2), &tmA, bar, kb * C::kBK + 64 * j, row0);
           for (int j = 0; j < 2; ++j) {
             if (GRAD)  // 64 columns of D x 128 vocabulary rows
               tma_load_2d_pair(smem_u32(stage_b(s)) + j * 16384, &tmB, bar, col0 + 64 * j, kb * C::kBK);
@@ -281,7 +296,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThre
     // ------------------------------------------------------ MMA issuer (leader CTA)
     if (lane == 0 && rank == 0) {
       constexpr uint32_t idesc = idesc_bf16(2 * 128, C::kTile, 0, GRAD ? 1 : 0);
-      // K-major: K step kk in 64-wide chunk kk / 4 (16 KiB apart), byte 32 (kk % 4) of each row;
+      // K-major: K step kk in 64-wide chunk kk / 4 (half the operand apart), byte 32 (kk % 4) of each row;
       // MN-major: 16 contraction rows (2 KiB) per step, 64-column atoms 16 KiB apart
       const uint64_t ad_base = smem_desc_sw128(smem_u32(stage_a(0)), 16, 1024);
       const uint64_t bd_base = smem_desc_sw128(smem_u32(stage_b(0)), GRAD ? 16384 : 16, 1024);
@@ -299,12 +314,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThre
           const int steps = min(C::kSegment, t.nk - k0);
           for (int kb = 0; kb < steps; ++kb) {
             if (!(ok = mbar_spin(&full[s], ph, abort_flag, a.err))) break;
-            const uint64_t so = static_cast<uint64_t>(s * (C::kStageBytes >> 4));
+            const uint64_t so = static_cast<uint64_t>(s * (stage_bytes >> 4));
             const uint64_t a0 = ad_base + so, b0 = bd_base + so;
 #pragma unroll
             for (int kk = 0; kk < C::kBK / 16; ++kk) {
-              const uint32_t ka = ((kk >> 2) * 16384 + (kk & 3) * 32) >> 4;
-              const uint32_t kb_ = GRAD ? (kk * 2048) >> 4 : ka;
+              const uint32_t ka = (kk >> 2) * (a_bytes >> 5) + (kk & 3) * 2;
+              const uint32_t kb_ = GRAD ? (kk * 2048) >> 4 : ((kk >> 2) * 16384 + (kk & 3) * 32) >> 4;
               umma_bf16_pair(d_tmem, a0 + ka, b0 + kb_, idesc, (kb > 0 || kk > 0) ? 1u : 0u);
             }
             umma_commit_pair_mc(&empty[s]);
@@ -365,7 +380,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThre
           fence_proxy_async_smem();  // the box -> async proxy (the TMA store)
           __syncwarp();
           if (lane == 0) {
-            if (col0 + 32 * g < a.D) tma_store_2d(&tmO, box, col0 + 32 * g, out_row);
+            if (col0 + 32 * g < a.D && row32 < rows) tma_store_2d(&tmO, box, col0 + 32 * g, out_row);
             bulk_commit_group();
           }
         }
@@ -373,7 +388,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThre
         ++tc;
       } else {
         const int row = first + row32 + lane;
-        const bool in = row < *a.count;
+        const bool in = row32 + lane < rows;
         const int at = in ? a.label[row] - col0 : -1;  // the label's own column is left out
         float ref = in ? row_reference(a.label_z[row]) : 0.f;
         float z[C::kEpiCols];
@@ -406,7 +421,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThre
         float most = z[0];
 #pragma unroll
         for (int i = 1; i < C::kEpiCols; ++i) most = fmaxf(most, z[i]);
-        if (fmaf(most, kLog2e, -ref) > kRefSlack) ref = ceilf(most * kLog2e);
+        const int64_t at_sum = static_cast<int64_t>(row32 + lane) * (4 * tiles_n) + 4 * t.tn + share;
+        if (fmaf(most, kLog2e, -ref) > kRefSlack) {
+          ref = ceilf(most * kLog2e);
+          if (in) a.moved[row32 + lane] = 1;
+        }
         float sum = 0.f;
 #pragma unroll
         for (int g = 0; g < C::kEpiCols / 32; ++g) {
@@ -429,12 +448,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThre
             fence_proxy_async_smem();  // the box -> async proxy (the TMA store)
             __syncwarp();
             if (lane == 0) {
-              if (col0 + 32 * g < a.V) tma_store_2d(&tmO, box, col0 + 32 * g, row32);
+              if (col0 + 32 * g < a.V && row32 < rows) tma_store_2d(&tmO, box, col0 + 32 * g, row32);
               bulk_commit_group();
             }
           }
         }
-        if (in) a.sums[static_cast<int64_t>(row32 + lane) * (4 * tiles_n) + 4 * t.tn + share] = make_float2(sum, ref);
+        if (in) {
+          a.sums[at_sum] = sum;
+          a.refs[at_sum] = ref;
+        }
       }
     }
     if (lane == 0) bulk_wait_all();
@@ -456,11 +478,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThre
 template <int SHARE>
 __global__ void __launch_bounds__(256) sq_head_finalize_kernel(const HeadArgs a, const int first) {
   __shared__ float tops[8], parts[8];
+  dependency_start();
+  dependency_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int rows = chunk_rows(a, first);
-  if (blockIdx.x == 0 && threadIdx.x == 0 && a.dX)  // the gradient launch's split of the vocabulary
-    *a.parts = head_parts(static_cast<int64_t>((rows + kHeadTile - 1) / kHeadTile) * ((a.D + kHeadTile - 1) / kHeadTile),
-                          static_cast<int>((a.V + HeadCfg<true>::kBK - 1) / HeadCfg<true>::kBK), a.clusters);
   const int r = blockIdx.x * (8 / SHARE) + warp / SHARE;
   if (SHARE == 8 ? r >= rows : blockIdx.x * 8 >= rows) return;  // whole CTAs
   const bool in = r < rows;
@@ -468,29 +489,27 @@ __global__ void __launch_bounds__(256) sq_head_finalize_kernel(const HeadArgs a,
   constexpr int kCols = HeadCfg<false>::kEpiCols;
   const int n = kHeadTile / kCols * static_cast<int>((a.V + kHeadTile - 1) / kHeadTile);
   const int filled = in ? static_cast<int>((a.V + kCols - 1) / kCols) : 0;  // quarter tiles that hold columns
-  const float2 *sums = a.sums + static_cast<int64_t>(r) * n;
-  const float z = a.label_z[row], z2 = z * kLog2e, ref0 = row_reference(z);
+  const float *sums = a.sums + static_cast<int64_t>(r) * n, *refs = a.refs + static_cast<int64_t>(r) * n;
+  const float z = a.label_z[row], z2 = z * kLog2e;
   const int own = (warp % SHARE) * 32 + lane;
-  float ref = ref0, sum = 0.f;
-  bool moved = false;
+  float top = row_reference(z), sum = 0.f;
+  const bool moved = in && a.moved[r];  // the same in all warps of a row
+  if (moved) {
+    for (int i = own; i < filled; i += 32 * SHARE) top = fmaxf(top, refs[i]);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+    if (SHARE > 1) {
+      if (lane == 0) tops[warp] = top;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < SHARE; ++w) top = fmaxf(top, tops[w]);
+    }
+    for (int i = own; i < filled; i += 32 * SHARE) sum += sums[i] * whole_exp2(refs[i] - top);
+  } else {
 #pragma unroll 8
-  for (int i = own; i < filled; i += 32 * SHARE) {
-    const float2 q = sums[i];
-    moved |= q.y != ref0;
-    const float top = fmaxf(ref, q.y);
-    sum = sum * whole_exp2(ref - top) + q.x * whole_exp2(q.y - top);
-    ref = top;
+    for (int i = own; i < filled; i += 32 * SHARE) sum += sums[i];
   }
-  float top = ref;
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-  if (SHARE > 1) {
-    if (lane == 0) tops[warp] = top;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < SHARE; ++w) top = fmaxf(top, tops[w]);
-  }
-  float others = warp_total(sum * whole_exp2(ref - top));
+  float others = warp_total(sum);
   if (SHARE > 1) {
     if (lane == 0) parts[warp] = others;
     __syncthreads();
@@ -500,6 +519,7 @@ __global__ void __launch_bounds__(256) sq_head_finalize_kernel(const HeadArgs a,
   }
   const float label = exp2_fast(z2 - top), total = others + label;
   if (in && own == 0) {
+    a.moved[r] = 0;  // for the next chunk
     const int t = a.token[row];
     // log(total / label): where label underflows against a far larger logit, from the exponents
     const bool near = top - z2 < 60.f;
@@ -511,10 +531,9 @@ __global__ void __launch_bounds__(256) sq_head_finalize_kernel(const HeadArgs a,
       a.factors[row] = make_float2(g / total, -g * (others / total));
     }
   }
-  const bool rescale = SHARE > 1 ? __syncthreads_or(moved) : __any_sync(0xFFFFFFFFu, moved);
-  if (a.e && rescale) {
+  if (moved && a.e) {
     for (int i = warp % SHARE; i < filled; i += SHARE) {
-      const float by = whole_exp2(sums[i].y - top);
+      const float by = whole_exp2(refs[i] - top);
       if (by == 1.f) continue;
       __nv_bfloat16 *e = reinterpret_cast<__nv_bfloat16 *>(a.e) + static_cast<int64_t>(r) * a.pitch;
       for (int64_t c = i * kCols + lane; c < a.V && c < (i + 1) * kCols; c += 32)
@@ -523,30 +542,51 @@ __global__ void __launch_bounds__(256) sq_head_finalize_kernel(const HeadArgs a,
   }
 }
 
-// dX[token] = f.x sum over the parts + f.y W[label], 256 columns of a row per warp.
+// dX[token] = f.x sum over the parts + f.y W[label]. A warp per 256 columns of a row, or, where
+// there are many parts (SHARE = 8), a CTA whose warps add up every eighth part each.
+template <int SHARE>
 __global__ void __launch_bounds__(256) sq_head_rows_kernel(const HeadArgs a, const int first) {
-  const int lane = threadIdx.x & 31;
-  const int pieces = static_cast<int>((a.D + 255) / 256);
-  const int unit = blockIdx.x * 8 + (threadIdx.x >> 5);
+  __shared__ float sums[SHARE > 1 ? 7 : 1][256];
+  dependency_start();
+  dependency_wait();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t pieces = static_cast<uint32_t>((a.D + 255) / 256);
+  const uint32_t unit = SHARE > 1 ? blockIdx.x : blockIdx.x * 8 + warp;
   const int r = unit / pieces;
   const int rows = chunk_rows(a, first);
   if (r >= rows) return;
   const int64_t c = static_cast<int64_t>(unit % pieces) * 256 + lane * 8;
-  if (c >= a.D) return;
+  if (SHARE == 1 && c >= a.D) return;
   const int tiles_m = (rows + kHeadTile - 1) / kHeadTile;
-  const int parts = *a.parts;
+  const int parts = a.parts[tiles_m - 1] + 1;
   const int64_t plane = static_cast<int64_t>(tiles_m) * kHeadTile * a.D;
-  const float *p = a.partial + static_cast<int64_t>(r) * a.D + c;
-  float s[8] = {};
-#pragma unroll 4
-  for (int i = 0; i < parts; ++i, p += plane) {
-    const float4 u = __ldcs(reinterpret_cast<const float4 *>(p)), v = __ldcs(reinterpret_cast<const float4 *>(p) + 1);
-    s[0] += u.x, s[1] += u.y, s[2] += u.z, s[3] += u.w;
-    s[4] += v.x, s[5] += v.y, s[6] += v.z, s[7] += v.w;
-  }
   const int row = first + r;
   const float2 f = a.factors[row];
-  const uint4 w = __ldg(reinterpret_cast<const uint4 *>(a.W + static_cast<int64_t>(a.label[row]) * a.D + c));
+  const int64_t label = a.label[row], token = a.token[row];
+  uint4 w = make_uint4(0, 0, 0, 0);
+  if (c < a.D && warp % SHARE == 0) w = __ldg(reinterpret_cast<const uint4 *>(a.W + label * a.D + c));
+  float s[8] = {};
+  if (c < a.D) {
+    const float *p = a.partial + static_cast<int64_t>(r) * a.D + c + warp % SHARE * plane;
+#pragma unroll 4
+    for (int i = warp % SHARE; i < parts; i += SHARE, p += SHARE * plane) {
+      const float4 u = __ldcs(reinterpret_cast<const float4 *>(p)), v = __ldcs(reinterpret_cast<const float4 *>(p) + 1);
+      s[0] += u.x, s[1] += u.y, s[2] += u.z, s[3] += u.w;
+      s[4] += v.x, s[5] += v.y, s[6] += v.z, s[7] += v.w;
+    }
+  }
+  if (SHARE > 1) {
+    if (warp > 0)
+#pragma unroll
+      for (int q = 0; q < 8; ++q) sums[warp - 1][q * 32 + lane] = s[q];
+    __syncthreads();
+    if (warp > 0) return;
+#pragma unroll
+    for (int i = 0; i < SHARE - 1; ++i)
+#pragma unroll
+      for (int q = 0; q < 8; ++q) s[q] += sums[i][q * 32 + lane];
+    if (c >= a.D) return;
+  }
   const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
   uint32_t o[4];
 #pragma unroll
@@ -556,16 +596,57 @@ __global__ void __launch_bounds__(256) sq_head_rows_kernel(const HeadArgs a, con
                               fmaf(f.x, s[2 * q + 1], f.y * __uint_as_float(ww[q] & 0xFFFF0000u)));
     o[q] = *reinterpret_cast<const uint32_t *>(&h2);
   }
-  *reinterpret_cast<uint4 *>(a.dX + static_cast<int64_t>(a.token[row]) * a.D + c) = make_uint4(o[0], o[1], o[2], o[3]);
+  *reinterpret_cast<uint4 *>(a.dX + token * a.D + c) = make_uint4(o[0], o[1], o[2], o[3]);
 }
 
+// The launches of a call follow each other on the stream as programmatic dependents: a kernel may
+// start, set up its barriers and tensor memory and then wait (dependency_wait, the first thing
+// each does before it reads or writes memory) while the one before it ends.
+template <typename... Params, typename... Args>
+cudaError_t launch_after(void (*kernel)(Params...), unsigned grid, int threads, int smem, cudaStream_t stream,
+                         Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid, 1, 1);
+  cfg.blockDim = dim3(threads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+}
+
+// As many two-CTA clusters as fit on the GPU at once, or one per tile (most: no number of tiles
+// that the host knows).
 template <bool GRAD>
 cudaError_t launch_head_product(const CUtensorMap &tmA, const CUtensorMap &tmB, const CUtensorMap &tmO,
                                 const HeadArgs &a, int first, int64_t most, int sm_count, cudaStream_t stream) {
+  using C = HeadCfg<GRAD>;
   static int done_mask = 0;  // per device ordinal (first 31)
   static int max_clusters[32] = {0};
-  return launch_persistent(sq_head_kernel<GRAD>, HeadCfg<GRAD>::kThreads, HeadCfg<GRAD>::kSmemBytes, most, sm_count, stream,
-                           max_clusters, &done_mask, tmA, tmB, tmO, a, first);
+  int dev = 0;
+  cudaGetDevice(&dev);
+  if (!(done_mask & (1 << (dev & 31)))) {
+    cudaError_t e =
+        cudaFuncSetAttribute(sq_head_kernel<GRAD>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2 * (sm_count / 2), 1, 1);
+    cfg.blockDim = dim3(C::kThreads, 1, 1);
+    cfg.dynamicSmemBytes = C::kSmemBytes;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, sq_head_kernel<GRAD>, &cfg) != cudaSuccess || n <= 0) {
+      cudaGetLastError();
+      n = sm_count / 2;
+    }
+    max_clusters[dev & 31] = n;
+    done_mask |= 1 << (dev & 31);
+  }
+  const int64_t clusters = std::min<int64_t>(most, max_clusters[dev & 31]);
+  return launch_after(sq_head_kernel<GRAD>, static_cast<unsigned>(2 * clusters), C::kThreads, C::kSmemBytes, stream, tmA,
+                      tmB, tmO, a, first);
 }
 
 }  // namespace
@@ -579,22 +660,29 @@ cudaError_t launch_head_gather(const HeadArgs &a, cudaStream_t stream) {
 }
 
 cudaError_t launch_head_chunk(const HeadArgs &a, const HeadMaps &m, int first, int sm_count, cudaStream_t stream) {
-  const int64_t tiles_m = a.chunk / kHeadTile;
+  const int rows = a.T - first < a.chunk ? a.T - first : a.chunk;
+  const int64_t tiles_m = (rows + kHeadTile - 1) / kHeadTile;
   cudaError_t e = launch_head_product<false>(m.rows, m.weights, m.e_store, a, first,
                                              tiles_m * ((a.V + kHeadTile - 1) / kHeadTile), sm_count, stream);
   if (e != cudaSuccess) return e;
-  const int rows = a.T - first < a.chunk ? a.T - first : a.chunk;
+  // a CTA per row pays from some 250 quarter tiles on
   if (a.V > 16384)
-    sq_head_finalize_kernel<8><<<rows, 256, 0, stream>>>(a, first);
+    e = launch_after(sq_head_finalize_kernel<8>, rows, 256, 0, stream, a, first);
   else
-    sq_head_finalize_kernel<1><<<(rows + 7) / 8, 256, 0, stream>>>(a, first);
-  if ((e = cudaGetLastError()) != cudaSuccess || !a.dX) return e;
-  if ((e = launch_head_product<true>(m.e_load, m.weights, m.partial, a, first, int64_t(1) << 30, sm_count, stream)) !=
-      cudaSuccess)
+    e = launch_after(sq_head_finalize_kernel<1>, (rows + 7) / 8, 256, 0, stream, a, first);
+  if (e != cudaSuccess || !a.dX) return e;
+  const int64_t tiles_d = (a.D + kHeadTile - 1) / kHeadTile;
+  int64_t units = 0, parts = 0;  // the most of any number of labelled rows
+  for (int64_t t = 1; t <= tiles_m; ++t) {
+    units = std::max(units, t * tiles_d * (a.parts[t - 1] + 1));
+    parts = std::max<int64_t>(parts, a.parts[t - 1] + 1);
+  }
+  if ((e = launch_head_product<true>(m.e_load, m.weights, m.partial, a, first, units, sm_count, stream)) != cudaSuccess)
     return e;
-  const int64_t units = rows * ((a.D + 255) / 256);
-  sq_head_rows_kernel<<<static_cast<unsigned>((units + 7) / 8), 256, 0, stream>>>(a, first);
-  return cudaGetLastError();
+  const int64_t pieces = rows * ((a.D + 255) / 256);
+  if (parts >= 16)
+    return launch_after(sq_head_rows_kernel<8>, static_cast<unsigned>(pieces), 256, 0, stream, a, first);
+  return launch_after(sq_head_rows_kernel<1>, static_cast<unsigned>((pieces + 7) / 8), 256, 0, stream, a, first);
 }
 
 }  // namespace sqi

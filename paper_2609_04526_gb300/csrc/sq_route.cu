@@ -16,25 +16,24 @@ constexpr uint32_t kAll = 0xFFFFFFFFu;
 // ---------------------------------------------------------------- router
 //
 // z[T, E] -> the k largest logits of each token, ties to the lowest expert. A NaN or -inf logit
-// is never chosen; +inf counts as the largest finite number. One warp per token.
+// is never chosen; +inf counts as the largest finite number.
+//
+// LANES lanes of a warp take a token, PER logits each, in groups of four that every lane sorts
+// (stably, so equal logits stay in the order of their experts). Each of k rounds takes the
+// largest of the lanes' largest and shifts it out of its group. Bound by instructions: with a
+// warp per token and the logits as ordered integers, 522 of them a token (32768 tokens, top-8
+// of 128: 19 us); eight lanes share them among four tokens.
 
-// A logit as an unsigned key with the order of the numbers; 0 for one that is never chosen.
-__device__ __forceinline__ uint32_t order_key(float z) {
-  if (!(z > -INFINITY)) return 0u;
-  const uint32_t u = __float_as_uint(fminf(z, FLT_MAX) + 0.0f);  // -0 becomes +0
-  return u ^ (static_cast<uint32_t>(static_cast<int32_t>(u) >> 31) | 0x80000000u);
-}
-__device__ __forceinline__ float key_value(uint32_t key) {
-  return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
-}
+// A logit as it is ranked; -inf is never chosen.
+__device__ __forceinline__ float rank_value(float z) { return z > -INFINITY ? fminf(z, FLT_MAX) : -INFINITY; }
 
 __device__ __forceinline__ float load_logit(const float *p) { return __ldg(p); }
 __device__ __forceinline__ float load_logit(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
-__device__ __forceinline__ void load_logits4(const float *p, float (&v)[4]) {
+__device__ __forceinline__ void load_logits4(const float *p, float *v) {
   const float4 q = __ldg(reinterpret_cast<const float4 *>(p));
   v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
 }
-__device__ __forceinline__ void load_logits4(const __nv_bfloat16 *p, float (&v)[4]) {
+__device__ __forceinline__ void load_logits4(const __nv_bfloat16 *p, float *v) {
   const uint2 q = __ldg(reinterpret_cast<const uint2 *>(p));
   v[0] = __uint_as_float(q.x << 16), v[1] = __uint_as_float(q.x & 0xFFFF0000u);
   v[2] = __uint_as_float(q.y << 16), v[3] = __uint_as_float(q.y & 0xFFFF0000u);
@@ -50,26 +49,11 @@ __device__ __forceinline__ void store_logits4(__nv_bfloat16 *p, const float *v) 
 __device__ __forceinline__ void store_logit(float *p, float v) { *p = v; }
 __device__ __forceinline__ void store_logit(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 
-// Expert of element i of a lane: lanes take VEC neighbours at a time.
-template <int VEC>
-__device__ __forceinline__ int expert_of(int i, int lane) {
-  return (i / VEC) * 32 * VEC + lane * VEC + i % VEC;
-}
-// The logits of one token, PER per lane; absent experts as NaN.
-template <int VEC, int PER, typename T>
-__device__ __forceinline__ void load_row(const T *row, int E, int lane, float (&z)[PER]) {
-#pragma unroll
-  for (int i = 0; i < PER; i += VEC) {
-    const int e = expert_of<VEC>(i, lane);
-    if (VEC == 4) {
-      float v[4] = {NAN, NAN, NAN, NAN};
-      if (e < E) load_logits4(row + e, v);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) z[i + c] = v[c];
-    } else {
-      z[i] = e < E ? load_logit(row + e) : NAN;
-    }
-  }
+// e^d for d <= 0. The product's rounding adds |d| 2^-24 of the value: less than 1e-6 where it counts.
+__device__ __forceinline__ float exp_of(float d) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(d * 1.4426950408889634f));
+  return y;
 }
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -77,112 +61,125 @@ __device__ __forceinline__ float warp_sum(float v) {
   for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(kAll, v, d);
   return v;
 }
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v) {
+#pragma unroll
+  for (int d = LANES / 2; d > 0; d >>= 1) v += __shfl_xor_sync(kAll, v, d);
+  return v;
+}
+template <int LANES>
+__device__ __forceinline__ float lanes_max(float v) {
+#pragma unroll
+  for (int d = LANES / 2; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor_sync(kAll, v, d));
+  return v;
+}
 
-// The winners of a lane in descending order: up to 8 logits are sorted first (stably, so equal
-// ones stay in the order of their experts) and a winner is shifted out; more are searched again
-// after each. 32768 tokens of 128 logits, top-8: 22.3 us with the search.
-template <int VEC, int PER>
-struct LaneTop {
-  static constexpr bool kSorted = PER <= 8;
-  uint32_t key[PER];
-  int expert[PER];
-  __device__ __forceinline__ LaneTop(const float (&z)[PER], int lane) {
+// Expert of a lane's element i: four neighbours at a time (WIDE, where E % 4 == 0), or one.
+template <int LANES, bool WIDE>
+__device__ __forceinline__ int expert_of(int i, int lane) {
+  return WIDE ? (i / 4) * 4 * LANES + lane * 4 + i % 4 : i * LANES + lane;
+}
+// The ranked logits of one token; -inf past the last expert.
+template <int LANES, bool WIDE, int PER, typename T>
+__device__ __forceinline__ void load_row(const T *row, int E, int lane, bool on, float (&z)[PER]) {
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      key[i] = order_key(z[i]);
-      expert[i] = expert_of<VEC>(i, lane);
-    }
-    if (kSorted) {
+  for (int i = 0; i < PER; i += WIDE ? 4 : 1) {
+    const int e = expert_of<LANES, WIDE>(i, lane);
+    if (WIDE) {
+      float v[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      if (on && e < E) load_logits4(row + e, v);
 #pragma unroll
-      for (int n = PER - 1; n > 0; --n)
-#pragma unroll
-        for (int i = 0; i < n; ++i) {
-          const bool swap = key[i + 1] > key[i];
-          const uint32_t k = swap ? key[i + 1] : key[i];
-          const int e = swap ? expert[i + 1] : expert[i];
-          key[i + 1] = swap ? key[i] : key[i + 1];
-          expert[i + 1] = swap ? expert[i] : expert[i + 1];
-          key[i] = k;
-          expert[i] = e;
-        }
+      for (int c = 0; c < 4; ++c) z[i + c] = rank_value(v[c]);
     } else {
-      search();
+      z[i] = on && e < E ? rank_value(load_logit(row + e)) : -INFINITY;
     }
   }
-  uint32_t best_key;
-  int best_expert;
-  __device__ __forceinline__ uint32_t top() const { return kSorted ? key[0] : best_key; }
-  __device__ __forceinline__ int top_expert() const { return kSorted ? expert[0] : best_expert; }
-  __device__ __forceinline__ void pop() {
-    if (kSorted) {
-#pragma unroll
-      for (int i = 0; i + 1 < PER; ++i) {
-        key[i] = key[i + 1];
-        expert[i] = expert[i + 1];
-      }
-      key[PER - 1] = 0;
-    } else {
-#pragma unroll
-      for (int i = 0; i < PER; ++i)
-        if (expert[i] == best_expert) key[i] = 0;
-      search();
-    }
-  }
-  __device__ __forceinline__ void search() {
-    best_key = 0;
-    best_expert = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-      if (key[i] > best_key) {
-        best_key = key[i];
-        best_expert = expert[i];
-      }
-  }
-};
+}
 
-template <int VEC, int PER, typename T>
+// k <= LANES: lane j of a token keeps its slot j.
+template <int LANES, bool WIDE, int PER, typename T>
 __global__ void __launch_bounds__(256)
     sq_route_kernel(int64_t tokens, int E, int k, const T *__restrict__ logits, const uint8_t *__restrict__ valid,
                     bool normalize, int *__restrict__ experts, float *__restrict__ weights) {
-  const int lane = threadIdx.x & 31;
-  const int64_t t = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
-  if (t >= tokens) return;
-  const bool on = !valid || valid[t];
-  int my_expert = -1;
-  float my_value = 0.f, top = 0.f, total = 0.f;
-  if (on) {
-    float z[PER];
-    load_row<VEC, PER>(logits + t * E, E, lane, z);
-    LaneTop<VEC, PER> own(z, lane);
-    for (int j = 0; j < k; ++j) {
-      const uint32_t won = __reduce_max_sync(kAll, own.top());
-      if (won == 0) break;
-      if (j == 0) {
-        top = key_value(won);
-        if (!normalize) {
+  constexpr int kGroups = PER / 4;
+  const int lane = threadIdx.x % LANES, base = threadIdx.x & 31 & ~(LANES - 1);
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * (256 / LANES) + threadIdx.x / LANES;
+  const bool on = t < tokens && (!valid || valid[t]);
+  float z[PER];
+  load_row<LANES, WIDE, PER>(logits + (on ? t * E : 0), E, lane, on, z);
+  float top = z[0];
 #pragma unroll
-          for (int i = 0; i < PER; ++i)
-            if (z[i] > -INFINITY) total += expf(fminf(z[i], FLT_MAX) - top);
-          total = warp_sum(total);
-        }
+  for (int i = 1; i < PER; ++i) top = fmaxf(top, z[i]);
+  top = lanes_max<LANES>(top);
+  float total = 0.f;
+  if (!normalize) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) total += z[i] > -INFINITY ? exp_of(z[i] - top) : 0.f;
+    total = lanes_sum<LANES>(total);
+  }
+  uint32_t order[kGroups];  // places within the group of its sorted logits, two bits each
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g) {
+    uint32_t at[4] = {0, 1, 2, 3};
+    float *v = z + 4 * g;
+#pragma unroll
+    for (int n = 3; n > 0; --n)
+#pragma unroll
+      for (int i = 0; i < n; ++i) {
+        const bool swap = v[i + 1] > v[i];
+        const float x = swap ? v[i + 1] : v[i];
+        const uint32_t p = swap ? at[i + 1] : at[i];
+        v[i + 1] = swap ? v[i] : v[i + 1];
+        at[i + 1] = swap ? at[i] : at[i + 1];
+        v[i] = x;
+        at[i] = p;
       }
-      const uint32_t same = __ballot_sync(kAll, own.top() == won);
-      int winner = __ffs(same) - 1;
-      int e = __shfl_sync(kAll, own.top_expert(), winner);
-      if (same & (same - 1)) {  // equal logits in several lanes: the lowest expert
-        e = __reduce_min_sync(kAll, own.top() == won ? own.top_expert() : INT_MAX);
-        winner = __ffs(__ballot_sync(kAll, own.top() == won && own.top_expert() == e)) - 1;
-      }
-      if (lane == winner) own.pop();
-      if (lane == j) {
-        my_expert = e;
-        my_value = key_value(won);
-      }
+    order[g] = at[0] | at[1] << 2 | at[2] << 4 | at[3] << 6;
+  }
+  int my_expert = -1;
+  float my_value = -INFINITY;
+  for (int j = 0; j < k; ++j) {
+    float best = z[0];
+    uint32_t places = order[0];
+    int group = 0;
+#pragma unroll
+    for (int g = 1; g < kGroups; ++g) {
+      const bool more = z[4 * g] > best;
+      best = more ? z[4 * g] : best;
+      places = more ? order[g] : places;
+      group = more ? g : group;
+    }
+    const float won = lanes_max<LANES>(best);
+    if (!__any_sync(kAll, won > -INFINITY)) break;
+    int e = expert_of<LANES, WIDE>(4 * group + static_cast<int>(places & 3u), lane);
+    bool mine = best == won;
+    const uint32_t same = (__ballot_sync(kAll, mine) >> base) & (LANES == 32 ? kAll : (1u << LANES % 32) - 1u);
+    if (__any_sync(kAll, (same & (same - 1)) != 0)) {  // equal logits in several lanes: the lowest expert
+      int lowest = mine ? e : INT_MAX;
+#pragma unroll
+      for (int d = LANES / 2; d > 0; d >>= 1) lowest = min(lowest, __shfl_xor_sync(kAll, lowest, d));
+      mine = mine && e == lowest;
+      e = lowest;
+    } else {
+      e = __shfl_sync(kAll, e, base + __ffs(same) - 1);
+    }
+    if (lane == j && won > -INFINITY) {
+      my_expert = e;
+      my_value = won;
+    }
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const bool pop = mine && group == g;
+      z[4 * g] = pop ? z[4 * g + 1] : z[4 * g];
+      z[4 * g + 1] = pop ? z[4 * g + 2] : z[4 * g + 1];
+      z[4 * g + 2] = pop ? z[4 * g + 3] : z[4 * g + 2];
+      z[4 * g + 3] = pop ? -INFINITY : z[4 * g + 3];
+      order[g] = pop ? order[g] >> 2 : order[g];
     }
   }
-  float w = my_expert >= 0 ? expf(my_value - top) : 0.f;
-  if (normalize) total = warp_sum(w);
-  if (lane < k) {
+  const float w = my_expert >= 0 ? exp_of(my_value - top) : 0.f;
+  if (normalize) total = lanes_sum<LANES>(w);
+  if (t < tokens && lane < k) {
     experts[t * k + lane] = my_expert;
     weights[t * k + lane] = my_expert >= 0 ? w / total : 0.f;
   }
@@ -191,61 +188,59 @@ __global__ void __launch_bounds__(256)
 // dz_e = q_e (dw_e - sum_j q_j dw_j), q the weights over the chosen experts (normalize) or the
 // softmax over all; dw_e is 0 for an expert that was not chosen. The softmax is formed again
 // from the logits: keeping it would cost a write and the same read.
-template <int VEC, int PER, typename T>
+template <int LANES, bool WIDE, int PER, typename T>
 __global__ void __launch_bounds__(256)
     sq_route_grad_kernel(int64_t tokens, int E, int k, const T *__restrict__ logits, const int *__restrict__ experts,
                          const float *__restrict__ dweights, bool normalize, T *__restrict__ dlogits) {
-  const int lane = threadIdx.x & 31;
-  const int64_t t = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
-  if (t >= tokens) return;
-  const T *row = logits + t * E;
-  T *out = dlogits + t * E;
-  int e = lane < k ? experts[t * k + lane] : -1;
+  const int lane = threadIdx.x % LANES;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * (256 / LANES) + threadIdx.x / LANES;
+  const bool slot = t < tokens && lane < k;
+  const int64_t row = t < tokens ? t * E : 0;
+  int e = slot ? experts[t * k + lane] : -1;
   if (e >= E) e = -1;
   const float dw = e >= 0 ? dweights[t * k + lane] : 0.f;
-  const float z = e >= 0 ? load_logit(row + e) : NAN;
-  const uint32_t key = e >= 0 ? order_key(z) : 0u;
-  const bool any = __any_sync(kAll, key != 0);
-  float share = 0.f, inner = 0.f, top = 0.f, total = 1.f;
-  float dense[PER];
-  if (any) {
-    if (normalize) {
-      top = key_value(__reduce_max_sync(kAll, key));
-      share = key ? expf(key_value(key) - top) : 0.f;
-      total = warp_sum(share);
-    } else {
-      float zs[PER];
-      load_row<VEC, PER>(row, E, lane, zs);
-      uint32_t best = 0;
+  const float z = e >= 0 ? rank_value(load_logit(logits + row + e)) : -INFINITY;
+  const bool any = lanes_max<LANES>(z) > -INFINITY;  // the token has an expert
+  float dense[PER], top = lanes_max<LANES>(z);
+  if (!normalize) {
+    load_row<LANES, WIDE, PER>(logits + row, E, lane, any, dense);
+    top = dense[0];
 #pragma unroll
-      for (int i = 0; i < PER; ++i) best = max(best, order_key(zs[i]));
-      top = key_value(__reduce_max_sync(kAll, best));
-      total = 0.f;
-#pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const uint32_t q = order_key(zs[i]);
-        dense[i] = q ? expf(key_value(q) - top) : 0.f;
-        total += dense[i];
-      }
-      total = warp_sum(total);
-      share = key ? expf(key_value(key) - top) : 0.f;
-    }
-    share /= total;
-    inner = warp_sum(share * dw);
+    for (int i = 1; i < PER; ++i) top = fmaxf(top, dense[i]);
+    top = lanes_max<LANES>(top);
   }
+  const float mine = z > -INFINITY ? exp_of(z - top) : 0.f;
+  float total = 0.f;
+  if (normalize) {
+    total = mine;
+  } else {
 #pragma unroll
-  for (int i = 0; i < PER; ++i) dense[i] = any && !normalize ? -(dense[i] / total) * inner : 0.f;
+    for (int i = 0; i < PER; ++i) {
+      dense[i] = dense[i] > -INFINITY ? exp_of(dense[i] - top) : 0.f;
+      total += dense[i];
+    }
+  }
+  total = lanes_sum<LANES>(total);
+  const float by = any ? 1.f / total : 0.f;
+  const float share = mine * by;
+  const float inner = lanes_sum<LANES>(share > 0.f ? share * dw : 0.f);
+  const float scale = -by * inner;
+  if (t < tokens) {
 #pragma unroll
-  for (int i = 0; i < PER; i += VEC) {
-    const int at = expert_of<VEC>(i, lane);
-    if (at >= E) continue;
-    if (VEC == 4)
-      store_logits4(out + at, dense + i);
-    else
-      store_logit(out + at, dense[i]);
+    for (int i = 0; i < PER; i += WIDE ? 4 : 1) {
+      const int at = expert_of<LANES, WIDE>(i, lane);
+      if (at >= E) continue;
+      float v[4];
+#pragma unroll
+      for (int c = 0; c < (WIDE ? 4 : 1); ++c) v[c] = normalize || !any ? 0.f : dense[i + c] * scale;
+      if (WIDE)
+        store_logits4(dlogits + row + at, v);
+      else
+        store_logit(dlogits + row + at, v[0]);
+    }
   }
   __syncwarp();  // the chosen experts' values go over the row's
-  if (key) store_logit(out + e, share * (dw - inner));
+  if (z > -INFINITY) store_logit(dlogits + row + e, share * (dw - inner));
 }
 
 // ---------------------------------------------------------------- tokens by expert
@@ -259,7 +254,7 @@ __global__ void __launch_bounds__(256)
 constexpr int kSortStep = 4;  // loads of 32 slots in flight
 constexpr int64_t kSortOne = 4096;
 constexpr int64_t kSortMany = 2048;  // slots of a CTA at least, of several
-constexpr int kSortThreads = 512;    // of a CTA, of several
+constexpr int kSortThreads = 1024;   // of a CTA, of several
 
 __device__ __forceinline__ void load_slots(const int *experts, int64_t at, int64_t end, int E, int lane,
                                            int (&e)[kSortStep]) {
@@ -314,14 +309,26 @@ __global__ void __launch_bounds__(1024)
       if (e[s] >= 0) atomicAdd(mine + e[s], 1);
   }
   if (counts) {
-    const int cells = gridDim.x * E, before = blockIdx.x * E;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < cells; i += blockDim.x) {
-      const int c = counts[i];
-      if (c == 0) continue;
-      const int e = i % E;
-      atomicAdd(all + e, c);
-      if (i < before) atomicAdd(first + e, c);
+    // a group of threads takes every groups-th CTA's counts, a thread one expert of them
+    const int width = min(static_cast<int>(blockDim.x), (E + 31) / 32 * 32);
+    const int groups = blockDim.x / width, group = threadIdx.x / width;
+    for (int e = threadIdx.x % width; e < E && group < groups; e += width) {
+      int sum = 0, before = 0;
+      for (int b0 = group; b0 < gridDim.x; b0 += groups * 8) {
+        int c[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int b = b0 + i * groups;
+          c[i] = b < gridDim.x ? __ldg(counts + b * E + e) : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          sum += c[i];
+          before += b0 + i * groups < blockIdx.x ? c[i] : 0;
+        }
+      }
+      atomicAdd(all + e, sum);
+      atomicAdd(first + e, before);
     }
   }
   __syncthreads();
@@ -458,47 +465,39 @@ __global__ void __launch_bounds__(256)
 // Y[t] = sum_j w[t, j] Ys[row_of[t, j]] in fp32 in the order of j, rounded once (without
 // weights: the plain sum, the gradient of the dispatch). `share` warps per token, which take its
 // 256-column pieces in turn.
-constexpr int kCombineFlight = 8;  // rows in flight
-__global__ void __launch_bounds__(256)
-    sq_combine_kernel(int64_t tokens, int k, int64_t D, int64_t rows, int share, const uint16_t *__restrict__ Ys,
+// FLIGHT rows are in flight at a time: 4 where k <= 4, else 8, in at most 64 registers a thread (32
+// warps per SM; with 97 registers and 16 warps a 2880-wide batch of 1999 tokens took twice as long).
+template <int FLIGHT>
+__global__ void __launch_bounds__(256, 4)
+    sq_combine_kernel(int64_t tokens, int k, int64_t D, int rows, int share, const uint16_t *__restrict__ Ys,
                       const int *__restrict__ row_of, const float *__restrict__ weights, uint16_t *__restrict__ Y) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t t = static_cast<int64_t>(blockIdx.x) * (8 / share) + warp / share;
   if (t >= tokens) return;
-  int64_t row = -1;
-  float w = 1.f;
+  int row = -1;  // lanes past k hold none
+  float w = 0.f;
   if (lane < k) {
     row = row_of[t * k + lane];
     if (row >= rows) row = -1;
-    if (weights) w = weights[t * k + lane];
+    if (row >= 0) w = weights ? weights[t * k + lane] : 1.f;  // a slot without a row adds 0 * 0
   }
-  int64_t at[kCombineFlight];
-  float wj[kCombineFlight];
-  auto batch = [&](int j0) {
-#pragma unroll
-    for (int i = 0; i < kCombineFlight; ++i) {
-      at[i] = __shfl_sync(kAll, row, j0 + i);
-      wj[i] = __shfl_sync(kAll, w, j0 + i);
-      if (j0 + i >= k) at[i] = -1;
-    }
-  };
-  batch(0);
-  for (int64_t c0 = (warp % share) * 256; c0 < D; c0 += share * 256) {
-    const int64_t c = c0 + lane * 8;
+  for (int64_t c = (warp % share) * 256 + lane * 8; c - lane * 8 < D; c += share * 256) {
     float sum[8] = {};
-    for (int j0 = 0; j0 < k; j0 += kCombineFlight) {
-      if (k > kCombineFlight) batch(j0);
-      uint4 v[kCombineFlight];
+    for (int j0 = 0; j0 < k; j0 += FLIGHT) {
+      uint4 v[FLIGHT];
 #pragma unroll
-      for (int i = 0; i < kCombineFlight; ++i)
-        if (at[i] >= 0 && c < D) v[i] = load_row16(Ys + at[i] * D + c);
+      for (int i = 0; i < FLIGHT; ++i) {
+        const int at = __shfl_sync(kAll, row, j0 + i);
+        v[i] = make_uint4(0, 0, 0, 0);
+        if (at >= 0 && c < D) v[i] = load_row16(Ys + at * D + c);
+      }
 #pragma unroll
-      for (int i = 0; i < kCombineFlight; ++i) {
-        if (at[i] < 0) continue;
+      for (int i = 0; i < FLIGHT; ++i) {
+        const float wi = __shfl_sync(kAll, w, j0 + i);
         float x[8];
         unpack8(v[i], x);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) sum[q] = fmaf(wj[i], x[q], sum[q]);
+        for (int q = 0; q < 8; ++q) sum[q] = fmaf(wi, x[q], sum[q]);
       }
     }
     if (c < D) store_row16(Y + t * D + c, pack8(sum));
@@ -581,60 +580,67 @@ __global__ void __launch_bounds__(256)
   if (part == 0 && t < tokens && lane < k) dweights[t * k + lane] = dw;
 }
 
-template <typename T, typename F>
-void with_row_shape(int E, F f) {
-  auto per = [&](auto vec) {
-    constexpr int V = decltype(vec)::value;
-    if (E <= 32 * V)
-      f(vec, std::integral_constant<int, V>{});
-    else if (E <= 128)
-      f(vec, std::integral_constant<int, 4>{});
-    else if (E <= 256)
-      f(vec, std::integral_constant<int, 8>{});
-    else if (E <= 512)
-      f(vec, std::integral_constant<int, 16>{});
-    else
-      f(vec, std::integral_constant<int, 32>{});
-  };
-  if (E % 4 == 0)
-    per(std::integral_constant<int, 4>{});
+// Lanes of a token and logits of a lane: as few lanes as hold the slots and at most 16 logits
+// each (16 lanes were no faster than 32 for more than 128 experts).
+template <bool WIDE, typename F>
+void with_row_shape(int E, int k, F f) {
+  auto go = [&](auto lanes, auto per) { f(lanes, std::integral_constant<bool, WIDE>{}, per); };
+  using std::integral_constant;
+  if (k <= 8 && E <= 32)
+    go(integral_constant<int, 8>{}, integral_constant<int, 4>{});
+  else if (k <= 8 && E <= 64)
+    go(integral_constant<int, 8>{}, integral_constant<int, 8>{});
+  else if (k <= 8 && E <= 128)
+    go(integral_constant<int, 8>{}, integral_constant<int, 16>{});
+  else if (E <= 128)
+    go(integral_constant<int, 32>{}, integral_constant<int, 4>{});
+  else if (E <= 256)
+    go(integral_constant<int, 32>{}, integral_constant<int, 8>{});
+  else if (E <= 512)
+    go(integral_constant<int, 32>{}, integral_constant<int, 16>{});
   else
-    per(std::integral_constant<int, 1>{});
+    go(integral_constant<int, 32>{}, integral_constant<int, 32>{});
+}
+
+// f(logits pointer of their type, lanes, wide, per) for this launch.
+template <typename F>
+void with_route(bool bf16, const void *logits, int E, int k, F f) {
+  auto typed = [&](auto *z) {
+    auto shaped = [&](auto lanes, auto wide, auto per) { f(z, lanes, wide, per); };
+    if (E % 4 == 0)
+      with_row_shape<true>(E, k, shaped);
+    else
+      with_row_shape<false>(E, k, shaped);
+  };
+  if (bf16)
+    typed(static_cast<const __nv_bfloat16 *>(logits));
+  else
+    typed(static_cast<const float *>(logits));
 }
 
 }  // namespace
 
 cudaError_t launch_route(int64_t T, int E, int k, bool bf16, const void *logits, const uint8_t *valid, bool normalize,
                          int *experts, float *weights, cudaStream_t stream) {
-  const unsigned grid = static_cast<unsigned>((T + 7) / 8);
-  auto go = [&](auto *z) {
+  with_route(bf16, logits, E, k, [&](auto *z, auto lanes, auto wide, auto per) {
     using L = std::remove_const_t<std::remove_pointer_t<decltype(z)>>;
-    with_row_shape<L>(E, [&](auto vec, auto per) {
-      sq_route_kernel<decltype(vec)::value, decltype(per)::value, L>
-          <<<grid, 256, 0, stream>>>(T, E, k, z, valid, normalize, experts, weights);
-    });
-  };
-  if (bf16)
-    go(static_cast<const __nv_bfloat16 *>(logits));
-  else
-    go(static_cast<const float *>(logits));
+    constexpr int kTokens = 256 / lanes.value;
+    sq_route_kernel<lanes.value, wide.value, per.value, L>
+        <<<static_cast<unsigned>((T + kTokens - 1) / kTokens), 256, 0, stream>>>(T, E, k, z, valid, normalize, experts,
+                                                                               weights);
+  });
   return cudaGetLastError();
 }
 
 cudaError_t launch_route_grad(int64_t T, int E, int k, bool bf16, const void *logits, const int *experts,
                               const float *dweights, bool normalize, void *dlogits, cudaStream_t stream) {
-  const unsigned grid = static_cast<unsigned>((T + 7) / 8);
-  auto go = [&](auto *z) {
+  with_route(bf16, logits, E, k, [&](auto *z, auto lanes, auto wide, auto per) {
     using L = std::remove_const_t<std::remove_pointer_t<decltype(z)>>;
-    with_row_shape<L>(E, [&](auto vec, auto per) {
-      sq_route_grad_kernel<decltype(vec)::value, decltype(per)::value, L>
-          <<<grid, 256, 0, stream>>>(T, E, k, z, experts, dweights, normalize, static_cast<L *>(dlogits));
-    });
-  };
-  if (bf16)
-    go(static_cast<const __nv_bfloat16 *>(logits));
-  else
-    go(static_cast<const float *>(logits));
+    constexpr int kTokens = 256 / lanes.value;
+    sq_route_grad_kernel<lanes.value, wide.value, per.value, L>
+        <<<static_cast<unsigned>((T + kTokens - 1) / kTokens), 256, 0, stream>>>(T, E, k, z, experts, dweights, normalize,
+                                                                               static_cast<L *>(dlogits));
+  });
   return cudaGetLastError();
 }
 
@@ -692,8 +698,11 @@ cudaError_t launch_combine(int64_t T, int k, int64_t D, int64_t rows, const uint
                            const float *weights, uint16_t *Y, int sm_count, cudaStream_t stream) {
   const int share = warps_of_token(T, D, 32 * static_cast<int64_t>(sm_count));
   const int64_t per = 8 / share;
-  sq_combine_kernel<<<static_cast<unsigned>((T + per - 1) / per), 256, 0, stream>>>(T, k, D, rows, share, Ys, row_of,
-                                                                                   weights, Y);
+  const unsigned grid = static_cast<unsigned>((T + per - 1) / per);
+  if (k <= 4)
+    sq_combine_kernel<4><<<grid, 256, 0, stream>>>(T, k, D, static_cast<int>(rows), share, Ys, row_of, weights, Y);
+  else
+    sq_combine_kernel<8><<<grid, 256, 0, stream>>>(T, k, D, static_cast<int>(rows), share, Ys, row_of, weights, Y);
   return cudaGetLastError();
 }
 
