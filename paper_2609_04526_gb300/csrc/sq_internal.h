@@ -412,7 +412,7 @@ struct HeadArgs {
   const float *dloss;     // [T] (gradient)
   float *loss, *lse;      // [T] or null
   uint16_t *dX;           // [T, D] bf16, or null: no gradient
-  int box_rows;           // rows of A in a shared-memory stage: 32, 64 or 128, all that few tokens have
+  int box_rows;           // rows of A in a shared-memory stage: 16, 32, 64 or 128, all that few tokens have
   int chunk;              // rows of a chunk, a multiple of kHeadTile
   uint8_t parts[kHeadPiece / kHeadTile];  // vocabulary parts of the gradient by row tiles of the chunk, less 1
   int64_t pitch;          // elements of a row of e

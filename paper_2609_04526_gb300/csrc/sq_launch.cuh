@@ -1,0 +1,37 @@
+// Launches that follow each other on a stream as programmatic dependents: a kernel may start
+// before the one ahead of it has ended, sets up what needs no memory and then waits for that
+// end (and, through it, for everything before).
+//
+// Every kernel launched with launch_after calls dependency_wait in all its threads before it
+// reads or writes global memory, and dependency_start, which lets the next launch start, only
+// after that. A kernel so starts when the last but one before it has ended, and at most one
+// kernel runs beside the ones that wait. (The one exception reads early what is older still: the
+// second launch of the sort by expert counts its slots before its wait; its count launch, having
+// passed its own wait, shows that the slots are complete.)
+#pragma once
+#include <cuda_runtime.h>
+
+namespace sqi {
+namespace {
+
+__device__ __forceinline__ void dependency_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+template <typename... Params, typename... Args>
+cudaError_t launch_after(void (*kernel)(Params...), unsigned grid, int threads, size_t smem, cudaStream_t stream,
+                         Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid, 1, 1);
+  cfg.blockDim = dim3(threads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+}
+
+}  // namespace
+}  // namespace sqi

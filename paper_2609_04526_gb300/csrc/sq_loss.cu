@@ -24,6 +24,7 @@
 // e is rounded to bf16 once, as an operand of the tensor cores (at most 2^-8 of a term; errors of
 // one sign and the other, so their sum stays below the rounding of the bf16 gradient); the sums S take the unrounded values.
 #include "sq_gemm_kernels.cuh"
+#include "sq_launch.cuh"
 
 namespace sqi {
 namespace {
@@ -44,7 +45,7 @@ struct HeadCfg {
   static constexpr int kBK = 128;  // contraction indices of a stage
   static constexpr int kB = 128 * kBK * 2;  // bytes of this CTA's 128 columns of a stage
   static constexpr int kRing = 3 * 2 * kB;  // three stages of 128 rows and 128 columns
-  static constexpr int kMaxStages = 4;
+  static constexpr int kMaxStages = 6;
   static constexpr int kTile = kHeadTile;
   static constexpr int kOffBox = kRing;
   static constexpr int kBoxBytes = 32 * 32 * (GRAD ? 4 : 2);  // 32 rows x 32 columns of a warp
@@ -86,10 +87,6 @@ __device__ __forceinline__ float warp_total(float v) {
   return v;
 }
 
-// Programmatic dependents of this launch may start; wait for the launch before this one to end.
-__device__ __forceinline__ void dependency_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ __forceinline__ void dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-
 // Reference exponent of a row from its label logit in powers of two; never -inf, and a NaN logit
 // leaves a number here (the row's NaN reaches its results through the label's own term).
 __device__ __forceinline__ float row_reference(float label_z) { return fmaxf(ceilf(label_z * kLog2e), -1e30f); }
@@ -111,6 +108,7 @@ __global__ void __launch_bounds__(256) sq_head_gather_kernel(const HeadArgs a) {
   constexpr int kTokens = 8 / SHARE;
   __shared__ int before[8];
   __shared__ float dots[8];
+  dependency_wait();
   dependency_start();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int t0 = blockIdx.x * kTokens, own = warp / SHARE, t = t0 + own;
@@ -206,10 +204,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThre
   using C = HeadCfg<GRAD>;
   // A stage holds box_rows rows of A; the MMAs read 128 all the same, the rest of them whatever
   // lies behind in the ring, and nothing reads those rows of the product. Few tokens so leave the
-  // ring to the columns: 4 stages of 64 rows and fewer, 3 of 128.
+  // ring to the columns, which are all their traffic: 3 stages of 128 rows, 4 of 64 and 32, 5 of
+  // 16 (one token against 128256 x 4096: 181 us with 3 stages, 170 with 4). Without a gradient
+  // the store boxes' room is part of the ring.
   constexpr int kMax = C::kMaxStages;
   const int a_bytes = a.box_rows * C::kBK * 2, stage_bytes = a_bytes + C::kB;
-  const int S = min(kMax, C::kRing / stage_bytes);
+  const int S = min(kMax, (GRAD || a.e ? C::kRing : C::kOffBar) / stage_bytes);
   const bool both = a.T > 128;  // else the peer's rows of A are past the last token
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -225,8 +225,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThre
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const int cluster = blockIdx.x >> 1, nclusters = gridDim.x >> 1;
-  dependency_start();
-
   auto stage_a = [&](int s) { return smem + s * stage_bytes; };
   auto stage_b = [&](int s) { return smem + s * stage_bytes + a_bytes; };
 
@@ -255,6 +253,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThre
   const uint32_t tmem_base = *tmem_slot;
 
   dependency_wait();
+  dependency_start();
   const int rows = chunk_rows(a, first);
   const int tiles_m = (rows + C::kTile - 1) / C::kTile;
   const int tiles_n = static_cast<int>(((GRAD ? a.D : a.V) + C::kTile - 1) / C::kTile);
@@ -478,8 +477,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThre
 template <int SHARE>
 __global__ void __launch_bounds__(256) sq_head_finalize_kernel(const HeadArgs a, const int first) {
   __shared__ float tops[8], parts[8];
-  dependency_start();
   dependency_wait();
+  dependency_start();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int rows = chunk_rows(a, first);
   const int r = blockIdx.x * (8 / SHARE) + warp / SHARE;
@@ -547,8 +546,8 @@ __global__ void __launch_bounds__(256) sq_head_finalize_kernel(const HeadArgs a,
 template <int SHARE>
 __global__ void __launch_bounds__(256) sq_head_rows_kernel(const HeadArgs a, const int first) {
   __shared__ float sums[SHARE > 1 ? 7 : 1][256];
-  dependency_start();
   dependency_wait();
+  dependency_start();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t pieces = static_cast<uint32_t>((a.D + 255) / 256);
   const uint32_t unit = SHARE > 1 ? blockIdx.x : blockIdx.x * 8 + warp;
@@ -599,25 +598,6 @@ __global__ void __launch_bounds__(256) sq_head_rows_kernel(const HeadArgs a, con
   *reinterpret_cast<uint4 *>(a.dX + token * a.D + c) = make_uint4(o[0], o[1], o[2], o[3]);
 }
 
-// The launches of a call follow each other on the stream as programmatic dependents: a kernel may
-// start, set up its barriers and tensor memory and then wait (dependency_wait, the first thing
-// each does before it reads or writes memory) while the one before it ends.
-template <typename... Params, typename... Args>
-cudaError_t launch_after(void (*kernel)(Params...), unsigned grid, int threads, int smem, cudaStream_t stream,
-                         Args... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid, 1, 1);
-  cfg.blockDim = dim3(threads, 1, 1);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
-}
-
 // As many two-CTA clusters as fit on the GPU at once, or one per tile (most: no number of tiles
 // that the host knows).
 template <bool GRAD>
@@ -652,11 +632,8 @@ cudaError_t launch_head_product(const CUtensorMap &tmA, const CUtensorMap &tmB, 
 }  // namespace
 
 cudaError_t launch_head_gather(const HeadArgs &a, cudaStream_t stream) {
-  if (a.T <= 1024)
-    sq_head_gather_kernel<8><<<static_cast<unsigned>(a.T), 256, 0, stream>>>(a);
-  else
-    sq_head_gather_kernel<1><<<static_cast<unsigned>((a.T + 7) / 8), 256, 0, stream>>>(a);
-  return cudaGetLastError();
+  if (a.T <= 1024) return launch_after(sq_head_gather_kernel<8>, static_cast<unsigned>(a.T), 256, 0, stream, a);
+  return launch_after(sq_head_gather_kernel<1>, static_cast<unsigned>((a.T + 7) / 8), 256, 0, stream, a);
 }
 
 cudaError_t launch_head_chunk(const HeadArgs &a, const HeadMaps &m, int first, int sm_count, cudaStream_t stream) {

@@ -7,6 +7,7 @@
 #include <algorithm>
 
 #include "sq_internal.h"
+#include "sq_launch.cuh"
 
 namespace sqi {
 namespace {
@@ -102,6 +103,8 @@ __global__ void __launch_bounds__(256)
     sq_route_kernel(int64_t tokens, int E, int k, const T *__restrict__ logits, const uint8_t *__restrict__ valid,
                     bool normalize, int *__restrict__ experts, float *__restrict__ weights) {
   constexpr int kGroups = PER / 4;
+  dependency_wait();
+  dependency_start();
   const int lane = threadIdx.x % LANES, base = threadIdx.x & 31 & ~(LANES - 1);
   const int64_t t = static_cast<int64_t>(blockIdx.x) * (256 / LANES) + threadIdx.x / LANES;
   const bool on = t < tokens && (!valid || valid[t]);
@@ -192,6 +195,8 @@ template <int LANES, bool WIDE, int PER, typename T>
 __global__ void __launch_bounds__(256)
     sq_route_grad_kernel(int64_t tokens, int E, int k, const T *__restrict__ logits, const int *__restrict__ experts,
                          const float *__restrict__ dweights, bool normalize, T *__restrict__ dlogits) {
+  dependency_wait();
+  dependency_start();
   const int lane = threadIdx.x % LANES;
   const int64_t t = static_cast<int64_t>(blockIdx.x) * (256 / LANES) + threadIdx.x / LANES;
   const bool slot = t < tokens && lane < k;
@@ -269,6 +274,8 @@ __device__ __forceinline__ void load_slots(const int *experts, int64_t at, int64
 __global__ void __launch_bounds__(kSortThreads)
     sq_sort_count_kernel(int64_t n, int E, int64_t per, const int *__restrict__ experts, int *__restrict__ counts) {
   extern __shared__ int sort_smem[];
+  dependency_wait();
+  dependency_start();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = kSortThreads / 32;
   for (int i = threadIdx.x; i < E; i += kSortThreads) sort_smem[i] = 0;
   __syncthreads();
@@ -299,6 +306,11 @@ __global__ void __launch_bounds__(1024)
   const int64_t begin = min(cta_end, blockIdx.x * per + warp * per_warp);
   const int64_t end = min(cta_end, begin + per_warp);
   for (int i = threadIdx.x; i < (warps + 2) * E; i += blockDim.x) hist[i] = 0;
+  // behind a count launch `experts` is complete already; each CTA counts its own slots meanwhile
+  if (!counts) {
+    dependency_wait();
+    dependency_start();
+  }
   __syncthreads();
   int *mine = hist + warp * E;
   for (int64_t at = begin; at < end; at += 32 * kSortStep) {
@@ -309,6 +321,8 @@ __global__ void __launch_bounds__(1024)
       if (e[s] >= 0) atomicAdd(mine + e[s], 1);
   }
   if (counts) {
+    dependency_wait();  // the counts are complete
+    dependency_start();
     // a group of threads takes every groups-th CTA's counts, a thread one expert of them
     const int width = min(static_cast<int>(blockDim.x), (E + 31) / 32 * 32);
     const int groups = blockDim.x / width, group = threadIdx.x / width;
@@ -319,7 +333,7 @@ __global__ void __launch_bounds__(1024)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int b = b0 + i * groups;
-          c[i] = b < gridDim.x ? __ldg(counts + b * E + e) : 0;
+          c[i] = b < gridDim.x ? __ldcg(counts + b * E + e) : 0;
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -431,6 +445,8 @@ __global__ void __launch_bounds__(256)
                        const int *__restrict__ row_of, const int *__restrict__ slot_of, uint16_t *__restrict__ Xs) {
   const int lane = threadIdx.x & 31;
   const uint32_t unit = blockIdx.x * 8 + (threadIdx.x >> 5);
+  dependency_wait();
+  dependency_start();
   if (unit >= units) return;
   const int64_t t = unit / pieces;
   const int64_t c0 = static_cast<int64_t>(unit % pieces) * kMoveCols + lane * 8;
@@ -471,6 +487,8 @@ template <int FLIGHT>
 __global__ void __launch_bounds__(256, 4)
     sq_combine_kernel(int64_t tokens, int k, int64_t D, int rows, int share, const uint16_t *__restrict__ Ys,
                       const int *__restrict__ row_of, const float *__restrict__ weights, uint16_t *__restrict__ Y) {
+  dependency_wait();
+  dependency_start();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t t = static_cast<int64_t>(blockIdx.x) * (8 / share) + warp / share;
   if (t >= tokens) return;
@@ -513,6 +531,8 @@ __global__ void __launch_bounds__(256)
                            const int *__restrict__ slot_of, const float *__restrict__ weights,
                            uint16_t *__restrict__ dYs, float *__restrict__ dweights) {
   __shared__ float partial[8][32];
+  dependency_wait();
+  dependency_start();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int part = warp % share;
   const int64_t t = static_cast<int64_t>(blockIdx.x) * (8 / share) + warp / share;
@@ -622,26 +642,28 @@ void with_route(bool bf16, const void *logits, int E, int k, F f) {
 
 cudaError_t launch_route(int64_t T, int E, int k, bool bf16, const void *logits, const uint8_t *valid, bool normalize,
                          int *experts, float *weights, cudaStream_t stream) {
+  cudaError_t status = cudaSuccess;
   with_route(bf16, logits, E, k, [&](auto *z, auto lanes, auto wide, auto per) {
     using L = std::remove_const_t<std::remove_pointer_t<decltype(z)>>;
     constexpr int kTokens = 256 / lanes.value;
-    sq_route_kernel<lanes.value, wide.value, per.value, L>
-        <<<static_cast<unsigned>((T + kTokens - 1) / kTokens), 256, 0, stream>>>(T, E, k, z, valid, normalize, experts,
-                                                                               weights);
+    status = launch_after(sq_route_kernel<lanes.value, wide.value, per.value, L>,
+                          static_cast<unsigned>((T + kTokens - 1) / kTokens), 256, 0, stream, T, E, k, z, valid,
+                          normalize, experts, weights);
   });
-  return cudaGetLastError();
+  return status;
 }
 
 cudaError_t launch_route_grad(int64_t T, int E, int k, bool bf16, const void *logits, const int *experts,
                               const float *dweights, bool normalize, void *dlogits, cudaStream_t stream) {
+  cudaError_t status = cudaSuccess;
   with_route(bf16, logits, E, k, [&](auto *z, auto lanes, auto wide, auto per) {
     using L = std::remove_const_t<std::remove_pointer_t<decltype(z)>>;
     constexpr int kTokens = 256 / lanes.value;
-    sq_route_grad_kernel<lanes.value, wide.value, per.value, L>
-        <<<static_cast<unsigned>((T + kTokens - 1) / kTokens), 256, 0, stream>>>(T, E, k, z, experts, dweights, normalize,
-                                                                               static_cast<L *>(dlogits));
+    status = launch_after(sq_route_grad_kernel<lanes.value, wide.value, per.value, L>,
+                          static_cast<unsigned>((T + kTokens - 1) / kTokens), 256, 0, stream, T, E, k, z, experts,
+                          dweights, normalize, static_cast<L *>(dlogits));
   });
-  return cudaGetLastError();
+  return status;
 }
 
 static int64_t sort_per_cta(int64_t n, int sm_count) {
@@ -664,8 +686,8 @@ cudaError_t launch_sort(int64_t n, int E, const int *experts, int64_t *offsets, 
   // few slots: eight warps, whose prefix is short
   const int threads = one ? (n <= 1024 ? 256 : 1024) : kSortThreads;
   if (!one) {
-    sq_sort_count_kernel<<<ctas, kSortThreads, E * sizeof(int), stream>>>(n, E, per, experts, workspace);
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e =
+        launch_after(sq_sort_count_kernel, ctas, kSortThreads, E * sizeof(int), stream, n, E, per, experts, workspace);
     if (e != cudaSuccess) return e;
   }
   const size_t smem = (static_cast<size_t>(threads / 32) + 2) * E * sizeof(int);
@@ -674,9 +696,8 @@ cudaError_t launch_sort(int64_t n, int E, const int *experts, int64_t *offsets, 
                                                34 * kRouteMaxExperts * static_cast<int>(sizeof(int)));
     if (e != cudaSuccess) return e;
   }
-  sq_sort_kernel<<<ctas, threads, smem, stream>>>(n, E, per, experts, one ? nullptr : workspace, offsets, row_of,
-                                                  slot_of);
-  return cudaGetLastError();
+  return launch_after(sq_sort_kernel, ctas, threads, smem, stream, n, E, per, experts, one ? nullptr : workspace, offsets,
+                      row_of, slot_of);
 }
 
 // Warps of a token: as many as it takes for `warps` in all, at most one per 256 columns.
@@ -690,8 +711,8 @@ cudaError_t launch_dispatch(int64_t T, int k, int64_t D, int64_t rows, const uin
                             const int *slot_of, uint16_t *Xs, cudaStream_t stream) {
   const uint32_t pieces = static_cast<uint32_t>((D + kMoveCols - 1) / kMoveCols);
   const uint32_t units = static_cast<uint32_t>(T) * pieces;
-  sq_dispatch_kernel<<<(units + 7) / 8, 256, 0, stream>>>(units, pieces, k, D, rows, X, row_of, slot_of, Xs);
-  return cudaGetLastError();
+  return launch_after(sq_dispatch_kernel, (units + 7) / 8, 256, 0, stream, units, pieces, k, D, rows, X, row_of, slot_of,
+                      Xs);
 }
 
 cudaError_t launch_combine(int64_t T, int k, int64_t D, int64_t rows, const uint16_t *Ys, const int *row_of,
@@ -699,11 +720,8 @@ cudaError_t launch_combine(int64_t T, int k, int64_t D, int64_t rows, const uint
   const int share = warps_of_token(T, D, 32 * static_cast<int64_t>(sm_count));
   const int64_t per = 8 / share;
   const unsigned grid = static_cast<unsigned>((T + per - 1) / per);
-  if (k <= 4)
-    sq_combine_kernel<4><<<grid, 256, 0, stream>>>(T, k, D, static_cast<int>(rows), share, Ys, row_of, weights, Y);
-  else
-    sq_combine_kernel<8><<<grid, 256, 0, stream>>>(T, k, D, static_cast<int>(rows), share, Ys, row_of, weights, Y);
-  return cudaGetLastError();
+  return launch_after(k <= 4 ? sq_combine_kernel<4> : sq_combine_kernel<8>, grid, 256, 0, stream, T, k, D, rows, share, Ys,
+                      row_of, weights, Y);
 }
 
 cudaError_t launch_combine_grad(int64_t T, int k, int64_t D, int64_t rows, const uint16_t *dY, const uint16_t *Ys,
@@ -711,9 +729,8 @@ cudaError_t launch_combine_grad(int64_t T, int k, int64_t D, int64_t rows, const
                                 float *dweights, int sm_count, cudaStream_t stream) {
   const int share = warps_of_token(T, D, 16 * static_cast<int64_t>(sm_count));
   const int64_t per = 8 / share;
-  sq_combine_grad_kernel<<<static_cast<unsigned>((T + per - 1) / per), 256, 0, stream>>>(
-      T, k, D, rows, share, dY, Ys, row_of, slot_of, weights, dYs, dweights);
-  return cudaGetLastError();
+  return launch_after(sq_combine_grad_kernel, static_cast<unsigned>((T + per - 1) / per), 256, 0, stream, T, k, D, rows,
+                      share, dY, Ys, row_of, slot_of, weights, dYs, dweights);
 }
 
 }  // namespace sqi
