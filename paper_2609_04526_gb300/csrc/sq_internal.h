@@ -423,16 +423,16 @@ struct HeadArgs {
   float2 *factors;
   uint16_t *rows;         // [T, D] the labelled tokens' rows of X
   // scratch, by row of the chunk
-  float *sums, *refs;     // [chunk, 4 * column tiles] sum and reference of each quarter tile
+  float *sums, *refs;     // [4 * column tiles, chunk] sum and reference of each quarter tile
   int *moved;             // [chunk] a row whose references differ (refs are read only there)
   uint16_t *e;            // [chunk, pitch] bf16 exponentials (gradient)
   float *partial;         // [parts, rows, D] fp32 (gradient)
   int *err;
 };
-// weights: 64 x 128 boxes, rows and e_load 64 x box_rows, 128-byte swizzle; e_store 32 x 32, 64-byte swizzle; partial
-// 32 x 32 fp32, 128-byte swizzle.
+// weights: 64 x 128 boxes, weights_short 64 x 64, rows and e_load 64 x box_rows, partial 32 x 32 fp32,
+// all with the 128-byte swizzle; e_store 32 x 32, 64-byte swizzle.
 struct HeadMaps {
-  CUtensorMap rows, weights, e_store, e_load, partial;
+  CUtensorMap rows, weights, weights_short, e_store, e_load, partial;
 };
 cudaError_t launch_head_gather(const HeadArgs &a, cudaStream_t stream);
 cudaError_t launch_head_chunk(const HeadArgs &a, const HeadMaps &m, int first, int sm_count, cudaStream_t stream);

@@ -30,22 +30,27 @@ namespace sqi {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr uint32_t kMinusInfinity = 0xFF800000u;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRefSlack = 100.f;  // a logit this far above the reference (in powers of two) moves it
+constexpr float kFarSum = 0x1p100f;  // the sum of a quarter tile that may hold one
 
 // Epilogue warp w takes TMEM lanes 32 (w % 4) .. + 31 and the w / 4-th share of a tile's columns:
-// a quarter (logits, whose columns stay in registers) or a half (gradient).
-template <bool GRAD>
+// a quarter (logits, whose columns stay in registers) or a half (gradient). Stages are BK deep: 64
+// keeps more of the ring in flight, 128 reads rows of W in longer runs (few tokens, see
+// launch_head_chunk).
+template <bool GRAD, int BK>
 struct HeadCfg {
   static constexpr int kEpiWarps = GRAD ? 8 : 16;
   static constexpr int kEpiCols = kHeadTile / (kEpiWarps / 4);
   static constexpr int kTmaWarp = kEpiWarps;
   static constexpr int kMmaWarp = kTmaWarp + 1;
   static constexpr int kThreads = 32 * (kMmaWarp + 1);
-  static constexpr int kBK = 128;  // contraction indices of a stage
-  static constexpr int kB = 128 * kBK * 2;  // bytes of this CTA's 128 columns of a stage
-  static constexpr int kRing = 3 * 2 * kB;  // three stages of 128 rows and 128 columns
-  static constexpr int kMaxStages = 6;
+  static constexpr int kBK = BK;
+  static constexpr int kB = 128 * kBK * 2;    // bytes of this CTA's 128 columns of a stage
+  static constexpr int kRing = 192 * 1024;    // 6 stages of 128 rows and 128 columns, 64 deep
+  static constexpr int kMaxStages = 12;
+  static constexpr int kUnit = GRAD ? 128 / kBK : 1;  // stages of a unit of the walk's contraction
   static constexpr int kTile = kHeadTile;
   static constexpr int kOffBox = kRing;
   static constexpr int kBoxBytes = 32 * 32 * (GRAD ? 4 : 2);  // 32 rows x 32 columns of a warp
@@ -53,11 +58,11 @@ struct HeadCfg {
   // step of 16, a bias that grows with the length: a sum of 4096 products in one accumulator left
   // the log-sum-exp 1.4e-5 too small. The logits therefore leave tensor memory every 1024 products
   // and are added in registers; the gradient, rounded to bf16 in the end, runs through.
-  static constexpr int kSegment = GRAD ? 1 << 30 : 8;
+  static constexpr int kSegment = GRAD ? 1 << 30 : 1024 / kBK;
   static constexpr int kOffBar = kOffBox + kEpiWarps * kBoxBytes;
   static constexpr int kSmemBytes = kOffBar + 512 + 1024;
 };
-static_assert(HeadCfg<false>::kSmemBytes <= 232448 && HeadCfg<true>::kSmemBytes <= 232448, "head kernel exceeds the opt-in shared memory of one CTA");
+static_assert(HeadCfg<false, 64>::kSmemBytes <= 232448 && HeadCfg<true, 64>::kSmemBytes <= 232448, "head kernel exceeds the opt-in shared memory of one CTA");
 
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
@@ -68,6 +73,36 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // 2^d of a whole d <= 0, exactly; 0 where it is not a normal number.
 __device__ __forceinline__ float whole_exp2(float d) {
   return d < -126.f ? 0.f : __int_as_float((127 + static_cast<int>(d)) << 23);
+}
+
+// The pair's MMA and its commits from one elected lane of a converged warp (the same lane at every
+// election): the descriptors stay in uniform registers. A single lane's are moved there for every
+// MMA, which beside four epilogue warps on its scheduler takes longer than the MMA itself.
+__device__ __forceinline__ void umma_pair_elect(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
+                                                uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t"
+      "elect.sync _|e, 0xFFFFFFFF;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "@e tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void umma_commit_pair_mc_elect(uint64_t *bar) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t"
+      "elect.sync _|e, 0xFFFFFFFF;\n\t"
+      "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}" ::"r"(
+          smem_u32(bar)),
+      "h"(static_cast<unsigned short>(3))
+      : "memory");
+}
+__device__ __forceinline__ void umma_commit_pair_elect(uint64_t *bar) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t"
+      "elect.sync _|e, 0xFFFFFFFF;\n\t"
+      "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar))
+      : "memory");
 }
 
 // 32 lanes x 16 consecutive fp32 columns.
@@ -182,31 +217,68 @@ __global__ void __launch_bounds__(256) sq_head_gather_kernel(const HeadArgs a) {
 //   gradient: D[t, d] = sum_v e[t, v] W[v, d]   e K-major, W MN-major; a unit is a tile over a
 //             part of the vocabulary and writes its own fp32 plane, added in order later
 
-struct HeadTile {
-  int tm, tn, part, k0, nk;  // row tile, column tile, vocabulary part, first stage and stages
+// The tiles of one cluster in order: every step-th of a list that goes part by part, in panels of
+// up to 8 row tiles, a panel column by column (so the CTAs resident at any moment share a few row
+// and column tiles in the L2). Stepped without divisions: they took a thread 1,000 cycles a tile,
+// in which the ring of loads ran dry and sixteen epilogue warps spent 600 issue slots each.
+template <bool GRAD>
+struct HeadWalk {
+  int tm, tn, part;  // row tile, column tile, part of the vocabulary
+  int k0, nk;        // its first stage and stages
+  int step, tiles_m, tiles_n, parts, stages;
+  int panel, height, at;  // first row tile of the panel, its row tiles, place in it
+  uint32_t by_height, by_parts;  // 2^32 / height and parts, rounded up: exact quotients below 2^26
+  __device__ __forceinline__ HeadWalk(int first, int step_, int tiles_m_, int tiles_n_, int parts_, int stages_)
+      : step(step_), tiles_m(tiles_m_), tiles_n(tiles_n_), parts(parts_), stages(stages_) {
+    part = tiles_m > 0 ? 0 : parts;
+    at = first;
+    by_parts = inverse(parts);
+    open(0);
+    place();
+  }
+  __device__ __forceinline__ bool more() const { return part < parts; }
+  __device__ __forceinline__ void advance() {
+    at += step;
+    place();
+  }
+
+ private:
+  static __device__ __forceinline__ uint32_t inverse(int n) { return n > 1 ? 0xFFFFFFFFu / n + 1 : 0; }
+  static __device__ __forceinline__ int quotient(int x, int n, uint32_t by) {
+    return n > 1 ? static_cast<int>(__umulhi(static_cast<uint32_t>(x), by)) : x;
+  }
+  __device__ __forceinline__ void open(int first) {
+    panel = first;
+    height = min(8, tiles_m - first);
+    by_height = inverse(height);
+  }
+  __device__ __forceinline__ void place() {
+    while (part < parts && at >= height * tiles_n) {
+      at -= height * tiles_n;
+      if (panel + height < tiles_m) {
+        open(panel + height);
+      } else {
+        ++part;
+        if (panel > 0) open(0);
+      }
+    }
+    tn = quotient(at, height, by_height);
+    tm = panel + at - tn * height;
+    k0 = GRAD ? quotient(stages * part, parts, by_parts) : 0;
+    nk = GRAD ? quotient(stages * (part + 1), parts, by_parts) - k0 : stages;
+  }
 };
 
-template <bool GRAD>
-__device__ __forceinline__ HeadTile head_tile(int unit, int tiles_m, int tiles_n, int parts, int stages) {
-  HeadTile t;
-  const int per = tiles_m * tiles_n;
-  t.part = GRAD ? unit / per : 0;
-  tile_coords<8>(unit - t.part * per, tiles_m, tiles_n, t.tm, t.tn);
-  t.k0 = GRAD ? static_cast<int>(static_cast<int64_t>(stages) * t.part / parts) : 0;
-  t.nk = GRAD ? static_cast<int>(static_cast<int64_t>(stages) * (t.part + 1) / parts) - t.k0 : stages;
-  return t;
-}
-
-template <bool GRAD>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThreads, 1)
+template <bool GRAD, int BK>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK>::kThreads, 1)
     sq_head_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                    const __grid_constant__ CUtensorMap tmO, const HeadArgs a, const int first) {
-  using C = HeadCfg<GRAD>;
+  using C = HeadCfg<GRAD, BK>;
   // A stage holds box_rows rows of A; the MMAs read 128 all the same, the rest of them whatever
   // lies behind in the ring, and nothing reads those rows of the product. Few tokens so leave the
-  // ring to the columns, which are all their traffic: 3 stages of 128 rows, 4 of 64 and 32, 5 of
-  // 16 (one token against 128256 x 4096: 181 us with 3 stages, 170 with 4). Without a gradient
-  // the store boxes' room is part of the ring.
+  // ring to the columns, which are all their traffic (one token against 128256 x 4096: 181 us with
+  // 96 KiB of columns in flight, 170 with 128). Without a gradient the store boxes' room is part of
+  // the ring.
   constexpr int kMax = C::kMaxStages;
   const int a_bytes = a.box_rows * C::kBK * 2, stage_bytes = a_bytes + C::kB;
   const int S = min(kMax, (GRAD || a.e ? C::kRing : C::kOffBar) / stage_bytes);
@@ -224,7 +296,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThre
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
-  const int cluster = blockIdx.x >> 1, nclusters = gridDim.x >> 1;
   auto stage_a = [&](int s) { return smem + s * stage_bytes; };
   auto stage_b = [&](int s) { return smem + s * stage_bytes + a_bytes; };
 
@@ -257,33 +328,38 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThre
   const int rows = chunk_rows(a, first);
   const int tiles_m = (rows + C::kTile - 1) / C::kTile;
   const int tiles_n = static_cast<int>(((GRAD ? a.D : a.V) + C::kTile - 1) / C::kTile);
-  const int stages = static_cast<int>(((GRAD ? a.V : a.D) + C::kBK - 1) / C::kBK);
+  constexpr int kDepth = C::kBK * C::kUnit;
+  const int stages = static_cast<int>(((GRAD ? a.V : a.D) + kDepth - 1) / kDepth);
   const int parts = GRAD && tiles_m > 0 ? a.parts[tiles_m - 1] + 1 : 1;
-  const int total = tiles_m * tiles_n * parts;
+  HeadWalk<GRAD> t(blockIdx.x >> 1, gridDim.x >> 1, tiles_m, tiles_n, parts, stages);
 
   if (warp == C::kTmaWarp) {
     // ------------------------------------------------------ TMA producer (both CTAs)
     if (lane == 0) {
       int it = 0;
       bool ok = true;
-      for (int unit = cluster; unit < total && ok; unit += nclusters) {
-        const HeadTile t = head_tile<GRAD>(unit, tiles_m, tiles_n, parts, stages);
+      int s = 0;
+      uint32_t ph = 1;  // parity of the phase that frees slot s: its first use finds it free
+      for (; t.more() && ok; t.advance()) {
         const int32_t row0 = (GRAD ? 0 : first) + t.tm * C::kTile + 128 * static_cast<int32_t>(rank);
         const int32_t col0 = t.tn * C::kTile + 128 * static_cast<int32_t>(rank);
-        for (int kb = t.k0; kb < t.k0 + t.nk; ++kb, ++it) {
-          const int s = it % S;
-          const uint32_t use = static_cast<uint32_t>(it / S);
-          if (it >= S && !(ok = mbar_wait(&empty[s], (use & 1u) ^ 1u, abort_flag, a.err))) break;
+        for (int kb = t.k0 * C::kUnit; kb < (t.k0 + t.nk) * C::kUnit; ++kb, ++it) {
+          if (it >= S && !(ok = mbar_wait(&empty[s], ph, abort_flag, a.err))) break;
           if (rank == 0) mbar_arrive_expect_tx(&full[s], 2 * C::kB + (both ? 2 : 1) * a_bytes);
           const uint32_t bar = mapa_shared(smem_u32(&full[s]), 0);
           if (rank == 0 || both)
+            for (int j = 0; j < C::kBK / 64; ++j)
+              tma_load_2d_pair(smem_u32(stage_a(s)) + j * (a.box_rows * 128), &tmA, bar, kb * C::kBK + 64 * j, row0);
+          if (GRAD) {  // 64 columns of D x kBK vocabulary rows
             for (int j = 0; j < 2; ++j)
-              tma_load_2d_pair(smem_u32(stage_a(s)) + j * (a_bytes / 2), &tmA, bar, kb * C::kBK + 64 * j, row0);
-          for (int j = 0; j < 2; ++j) {
-            if (GRAD)  // 64 columns of D x 128 vocabulary rows
-              tma_load_2d_pair(smem_u32(stage_b(s)) + j * 16384, &tmB, bar, col0 + 64 * j, kb * C::kBK);
-            else  // 128 vocabulary rows x 64 columns of D
+              tma_load_2d_pair(smem_u32(stage_b(s)) + j * (C::kB / 2), &tmB, bar, col0 + 64 * j, kb * C::kBK);
+          } else {  // 128 vocabulary rows x 64 columns of D
+            for (int j = 0; j < C::kBK / 64; ++j)
               tma_load_2d_pair(smem_u32(stage_b(s)) + j * 16384, &tmB, bar, kb * C::kBK + 64 * j, col0);
+          }
+          if (++s == S) {
+            s = 0;
+            ph ^= 1u;
           }
         }
       }
@@ -293,44 +369,45 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThre
     }
   } else if (warp == C::kMmaWarp) {
     // ------------------------------------------------------ MMA issuer (leader CTA)
-    if (lane == 0 && rank == 0) {
+    // The whole warp walks the stages, so a wait that runs out for some lanes ends all of them.
+    if (rank == 0) {
       constexpr uint32_t idesc = idesc_bf16(2 * 128, C::kTile, 0, GRAD ? 1 : 0);
-      // K-major: K step kk in 64-wide chunk kk / 4 (half the operand apart), byte 32 (kk % 4) of each row;
-      // MN-major: 16 contraction rows (2 KiB) per step, 64-column atoms 16 KiB apart
+      // K-major: K step kk in 64-wide chunk kk / 4 (a box apart), byte 32 (kk % 4) of each row;
+      // MN-major: 16 contraction rows (2 KiB) per step, 64-column atoms half the operand apart
       const uint64_t ad_base = smem_desc_sw128(smem_u32(stage_a(0)), 16, 1024);
-      const uint64_t bd_base = smem_desc_sw128(smem_u32(stage_b(0)), GRAD ? 16384 : 16, 1024);
+      const uint64_t bd_base = smem_desc_sw128(smem_u32(stage_b(0)), GRAD ? C::kB / 2 : 16, 1024);
       int s = 0, tc = 0;  // tc: accumulators filled
       uint32_t ph = 0;
       bool ok = true;
-      for (int unit = cluster; unit < total && ok; unit += nclusters) {
-        const HeadTile t = head_tile<GRAD>(unit, tiles_m, tiles_n, parts, stages);
-        for (int k0 = 0; k0 < t.nk && ok; k0 += C::kSegment, ++tc) {
+      for (; t.more() && ok; t.advance()) {
+        const int steps_all = t.nk * C::kUnit;
+        for (int k0 = 0; k0 < steps_all && ok; k0 += C::kSegment, ++tc) {
           const int ab = tc & 1;
           const uint32_t au = static_cast<uint32_t>(tc >> 1);
-          if (tc >= 2 && !(ok = mbar_spin_cluster(&tempty[ab], (au & 1u) ^ 1u, abort_flag, a.err))) break;
+          if (tc >= 2 && !(ok = __all_sync(0xFFFFFFFFu, mbar_spin_cluster(&tempty[ab], (au & 1u) ^ 1u, abort_flag, a.err)))) break;
           tc_fence_after();
           const uint32_t d_tmem = tmem_base + ab * kTmemCols;
-          const int steps = min(C::kSegment, t.nk - k0);
+          const int steps = min(C::kSegment, steps_all - k0);
           for (int kb = 0; kb < steps; ++kb) {
-            if (!(ok = mbar_spin(&full[s], ph, abort_flag, a.err))) break;
+            if (!(ok = __all_sync(0xFFFFFFFFu, mbar_spin(&full[s], ph, abort_flag, a.err)))) break;
             const uint64_t so = static_cast<uint64_t>(s * (stage_bytes >> 4));
             const uint64_t a0 = ad_base + so, b0 = bd_base + so;
 #pragma unroll
             for (int kk = 0; kk < C::kBK / 16; ++kk) {
-              const uint32_t ka = (kk >> 2) * (a_bytes >> 5) + (kk & 3) * 2;
+              const uint32_t ka = (kk >> 2) * (a.box_rows * 8) + (kk & 3) * 2;
               const uint32_t kb_ = GRAD ? (kk * 2048) >> 4 : ((kk >> 2) * 16384 + (kk & 3) * 32) >> 4;
-              umma_bf16_pair(d_tmem, a0 + ka, b0 + kb_, idesc, (kb > 0 || kk > 0) ? 1u : 0u);
+              umma_pair_elect(d_tmem, a0 + ka, b0 + kb_, idesc, (kb > 0 || kk > 0) ? 1u : 0u);
             }
-            umma_commit_pair_mc(&empty[s]);
+            umma_commit_pair_mc_elect(&empty[s]);
             if (++s == S) {
               s = 0;
               ph ^= 1u;
             }
           }
-          if (ok) umma_commit_pair_mc(&tfull[ab]);
+          if (ok) umma_commit_pair_mc_elect(&tfull[ab]);
         }
       }
-      umma_commit_pair(drain);
+      umma_commit_pair_elect(drain);
       mbar_drain(drain, 0);
     }
   } else {
@@ -356,8 +433,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThre
     };
     int tc = 0;
     bool ok = true;
-    for (int unit = cluster; unit < total && ok; unit += nclusters) {
-      const HeadTile t = head_tile<GRAD>(unit, tiles_m, tiles_n, parts, stages);
+    int label = -1;  // of this lane's row in the next tile, and its logit
+    float label_z = 0.f;
+    auto labels = [&] {
+      const int r = t.tm * C::kTile + 128 * static_cast<int>(rank) + 32 * quad + lane;
+      label = -1;
+      label_z = 0.f;
+      if (!GRAD && r < rows) {
+        label = a.label[first + r];
+        label_z = a.label_z[first + r];
+      }
+    };
+    if (t.more()) labels();
+    while (t.more() && ok) {
       const int row32 = t.tm * C::kTile + 128 * static_cast<int>(rank) + 32 * quad;  // of the chunk
       const int col0 = t.tn * C::kTile + C::kEpiCols * share;
       if constexpr (GRAD) {
@@ -385,72 +473,96 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThre
         }
         release(ab);
         ++tc;
+        t.advance();
       } else {
-        const int row = first + row32 + lane;
         const bool in = row32 + lane < rows;
-        const int at = in ? a.label[row] - col0 : -1;  // the label's own column is left out
-        float ref = in ? row_reference(a.label_z[row]) : 0.f;
-        float z[C::kEpiCols];
+        const int at = label - col0;  // the label's own column is left out
+        float ref = row_reference(label_z);
+        uint32_t z[2][32];  // the row's logits
+        static_assert(C::kEpiCols == 64, "two 32-column loads");
         for (int k0 = 0; k0 < stages; k0 += C::kSegment, ++tc) {
           const int ab = tc & 1;
           if (!(ok = mbar_wait(&tfull[ab], static_cast<uint32_t>(tc >> 1) & 1u, abort_flag, a.err))) break;
           tc_fence_after();
+          if (k0 == 0) {
+            tmem_ld32(t_row + ab * kTmemCols, z[0]);
+            tmem_ld32(t_row + ab * kTmemCols + 32, z[1]);
+            tmem_ld_wait_for(z[0]);
+            tmem_ld_wait_for(z[1]);
+          } else {
 #pragma unroll
-          for (int g = 0; g < C::kEpiCols / 16; ++g) {
-            uint32_t v[16];
-            tmem_ld16(t_row + ab * kTmemCols + 16 * g, v);
-            tmem_ld_wait();
+            for (int g = 0; g < 4; ++g) {
+              uint32_t v[16];
+              tmem_ld16(t_row + ab * kTmemCols + 16 * g, v);
+              tmem_ld_wait();
 #pragma unroll
-            for (int i = 0; i < 16; ++i) z[16 * g + i] = (k0 ? z[16 * g + i] : 0.f) + __uint_as_float(v[i]);
+              for (int i = 0; i < 16; ++i) {
+                uint32_t &q = z[g / 2][16 * (g % 2) + i];
+                q = __float_as_uint(__uint_as_float(q) + __uint_as_float(v[i]));
+              }
+            }
           }
           release(ab);
         }
         if (!ok) break;
+        // the next tile's labels are on their way while this one's exponentials are formed
+        const int64_t at_sum = static_cast<int64_t>(4 * t.tn + share) * a.chunk + row32 + lane;
+        t.advance();
+        if (t.more()) labels();
         if (col0 >= a.V) continue;
         if (__any_sync(0xFFFFFFFFu, at >= 0 && at < C::kEpiCols)) {
 #pragma unroll
           for (int i = 0; i < C::kEpiCols; ++i)
-            if (i == at) z[i] = -INFINITY;
+            if (i == at) z[i / 32][i % 32] = kMinusInfinity;
         }
         if (col0 + C::kEpiCols > a.V) {
 #pragma unroll
           for (int i = 0; i < C::kEpiCols; ++i)
-            if (col0 + i >= a.V) z[i] = -INFINITY;
+            if (col0 + i >= a.V) z[i / 32][i % 32] = kMinusInfinity;
         }
-        float most = z[0];
-#pragma unroll
-        for (int i = 1; i < C::kEpiCols; ++i) most = fmaxf(most, z[i]);
-        const int64_t at_sum = static_cast<int64_t>(row32 + lane) * (4 * tiles_n) + 4 * t.tn + share;
-        if (fmaf(most, kLog2e, -ref) > kRefSlack) {
-          ref = ceilf(most * kLog2e);
-          if (in) a.moved[row32 + lane] = 1;
-        }
+        // A logit far above the reference shows in the sum; the largest one then becomes the
+        // reference and the exponentials are formed again.
         float sum = 0.f;
+#pragma unroll 1
+        for (bool again = false;; again = true) {
+          float part[4] = {};
 #pragma unroll
-        for (int g = 0; g < C::kEpiCols / 32; ++g) {
-          uint32_t packed[16];
+          for (int g = 0; g < C::kEpiCols / 32; ++g) {
+            uint32_t packed[16];
 #pragma unroll
-          for (int q = 0; q < 16; ++q) {
-            const float e0 = exp2_fast(fmaf(z[32 * g + 2 * q], kLog2e, -ref));
-            const float e1 = exp2_fast(fmaf(z[32 * g + 2 * q + 1], kLog2e, -ref));
-            sum += e0 + e1;
-            const __nv_bfloat162 h2 = __floats2bfloat162_rn(e0, e1);
-            packed[q] = *reinterpret_cast<const uint32_t *>(&h2);
-          }
-          if (a.e) {
-            if (lane == 0) bulk_wait_read<0>();  // the previous box's store has read the buffer
-            __syncwarp();
+            for (int q = 0; q < 16; ++q) {
+              const float e0 = exp2_fast(fmaf(__uint_as_float(z[g][2 * q]), kLog2e, -ref));
+              const float e1 = exp2_fast(fmaf(__uint_as_float(z[g][2 * q + 1]), kLog2e, -ref));
+              part[q % 4] += e0 + e1;
+              const __nv_bfloat162 h2 = __floats2bfloat162_rn(e0, e1);
+              packed[q] = *reinterpret_cast<const uint32_t *>(&h2);
+            }
+            if (a.e) {
+              if (lane == 0) bulk_wait_read<0>();  // the box's last store, half a tile ago, has read it
+              __syncwarp();
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-              st_shared_v4(box + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4), packed[4 * q], packed[4 * q + 1],
-                           packed[4 * q + 2], packed[4 * q + 3]);
-            fence_proxy_async_smem();  // the box -> async proxy (the TMA store)
-            __syncwarp();
-            if (lane == 0) {
-              if (col0 + 32 * g < a.V && row32 < rows) tma_store_2d(&tmO, box, col0 + 32 * g, row32);
-              bulk_commit_group();
+              for (int q = 0; q < 4; ++q)
+                st_shared_v4(box + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4), packed[4 * q], packed[4 * q + 1],
+                             packed[4 * q + 2], packed[4 * q + 3]);
+              fence_proxy_async_smem();  // the box -> async proxy (the TMA store)
+              __syncwarp();
+              if (lane == 0) {
+                if (col0 + 32 * g < a.V && row32 < rows) tma_store_2d(&tmO, box, col0 + 32 * g, row32);
+                bulk_commit_group();
+              }
             }
           }
+          sum = (part[0] + part[1]) + (part[2] + part[3]);
+          if (again || !__any_sync(0xFFFFFFFFu, in && !(sum < kFarSum))) break;
+          float most = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < C::kEpiCols; ++i) most = fmaxf(most, __uint_as_float(z[i / 32][i % 32]));
+          if (fmaf(most, kLog2e, -ref) > kRefSlack) {
+            ref = ceilf(most * kLog2e);
+            if (in) a.moved[row32 + lane] = 1;
+          }
+          if (lane == 0) bulk_wait_all();  // the first box is written before the second one
+          __syncwarp();
         }
         if (in) {
           a.sums[at_sum] = sum;
@@ -472,73 +584,63 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD>::kThre
 
 // ---------------------------------------------------------------- finalize and rows
 
-// SHARE warps per row: the quarter tiles' sums brought to one reference and added in a fixed
-// order. A large vocabulary takes a CTA per row (2004 sums: one warp needed 13.4 us).
-template <int SHARE>
-__global__ void __launch_bounds__(256) sq_head_finalize_kernel(const HeadArgs a, const int first) {
-  __shared__ float tops[8], parts[8];
+// 32 rows per CTA, one per lane; the warps take the quarter tiles in turn (coalesced: a column of
+// quarter tiles lies row by row), and the rows' 32 partial sums are added in order.
+__global__ void __launch_bounds__(1024) sq_head_finalize_kernel(const HeadArgs a, const int first) {
+  __shared__ float parts[32][33];
   dependency_wait();
   dependency_start();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int rows = chunk_rows(a, first);
-  const int r = blockIdx.x * (8 / SHARE) + warp / SHARE;
-  if (SHARE == 8 ? r >= rows : blockIdx.x * 8 >= rows) return;  // whole CTAs
-  const bool in = r < rows;
-  const int row = first + (in ? r : 0);
-  constexpr int kCols = HeadCfg<false>::kEpiCols;
-  const int n = kHeadTile / kCols * static_cast<int>((a.V + kHeadTile - 1) / kHeadTile);
-  const int filled = in ? static_cast<int>((a.V + kCols - 1) / kCols) : 0;  // quarter tiles that hold columns
-  const float *sums = a.sums + static_cast<int64_t>(r) * n, *refs = a.refs + static_cast<int64_t>(r) * n;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const int rows = chunk_rows(a, first), r0 = blockIdx.x * 32;
+  if (r0 >= rows) return;
+  const int r = min(r0 + lane, rows - 1), row = first + r;  // lanes past the last row repeat it
+  constexpr int kCols = HeadCfg<false, 64>::kEpiCols;
+  const int filled = static_cast<int>((a.V + kCols - 1) / kCols);  // quarter tiles that hold columns
+  const float *sums = a.sums + r, *refs = a.refs + r;
   const float z = a.label_z[row], z2 = z * kLog2e;
-  const int own = (warp % SHARE) * 32 + lane;
+  const int t = a.token[row];
+  const float g = a.dX ? a.dloss[t] : 0.f;
   float top = row_reference(z), sum = 0.f;
-  const bool moved = in && a.moved[r];  // the same in all warps of a row
-  if (moved) {
-    for (int i = own; i < filled; i += 32 * SHARE) top = fmaxf(top, refs[i]);
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-    if (SHARE > 1) {
-      if (lane == 0) tops[warp] = top;
-      __syncthreads();
-#pragma unroll
-      for (int w = 0; w < SHARE; ++w) top = fmaxf(top, tops[w]);
+  const bool moved = a.moved[r];
+  const bool any = __any_sync(0xFFFFFFFFu, moved);  // the same rows in every warp
+  if (any) {  // references differ: the largest of them first
+    for (int i = warp; i < filled; i += warps) top = fmaxf(top, refs[static_cast<int64_t>(i) * a.chunk]);
+    parts[warp][lane] = top;
+    __syncthreads();
+    for (int w = 0; w < warps; ++w) top = fmaxf(top, parts[w][lane]);
+    __syncthreads();
+    for (int i = warp; i < filled; i += warps) {
+      const int64_t at = static_cast<int64_t>(i) * a.chunk;
+      sum += sums[at] * whole_exp2(refs[at] - top);
     }
-    for (int i = own; i < filled; i += 32 * SHARE) sum += sums[i] * whole_exp2(refs[i] - top);
   } else {
 #pragma unroll 8
-    for (int i = own; i < filled; i += 32 * SHARE) sum += sums[i];
+    for (int i = warp; i < filled; i += warps) sum += sums[static_cast<int64_t>(i) * a.chunk];
   }
-  float others = warp_total(sum);
-  if (SHARE > 1) {
-    if (lane == 0) parts[warp] = others;
-    __syncthreads();
-    others = 0.f;
-#pragma unroll
-    for (int w = 0; w < SHARE; ++w) others += parts[w];
+  parts[warp][lane] = sum;
+  __syncthreads();
+  if (any && a.e) {  // the exponentials of moved rows follow their reference
+    for (int i = warp; i < filled; i += warps)
+      for (int l = 0; l < 32 && r0 + l < rows; ++l) {
+        if (!__shfl_sync(0xFFFFFFFFu, moved, l)) continue;
+        const float by = whole_exp2(a.refs[static_cast<int64_t>(i) * a.chunk + r0 + l] - __shfl_sync(0xFFFFFFFFu, top, l));
+        if (by == 1.f) continue;
+        __nv_bfloat16 *e = reinterpret_cast<__nv_bfloat16 *>(a.e) + static_cast<int64_t>(r0 + l) * a.pitch;
+        for (int64_t c = i * kCols + lane; c < a.V && c < (i + 1) * kCols; c += 32)
+          e[c] = __float2bfloat16_rn(__bfloat162float(e[c]) * by);
+      }
   }
+  if (warp > 0 || r0 + lane >= rows) return;
+  float others = 0.f;
+  for (int w = 0; w < warps; ++w) others += parts[w][lane];
+  a.moved[r] = 0;  // for the next chunk
   const float label = exp2_fast(z2 - top), total = others + label;
-  if (in && own == 0) {
-    a.moved[r] = 0;  // for the next chunk
-    const int t = a.token[row];
-    // log(total / label): where label underflows against a far larger logit, from the exponents
-    const bool near = top - z2 < 60.f;
-    const float loss = near ? log1pf(others / label) : (top - z2) * kLn2 + logf(total);
-    if (a.loss) a.loss[t] = loss;
-    if (a.lse) a.lse[t] = near ? z + loss : top * kLn2 + logf(total);
-    if (a.dX) {
-      const float g = a.dloss[t];
-      a.factors[row] = make_float2(g / total, -g * (others / total));
-    }
-  }
-  if (moved && a.e) {
-    for (int i = warp % SHARE; i < filled; i += SHARE) {
-      const float by = whole_exp2(refs[i] - top);
-      if (by == 1.f) continue;
-      __nv_bfloat16 *e = reinterpret_cast<__nv_bfloat16 *>(a.e) + static_cast<int64_t>(r) * a.pitch;
-      for (int64_t c = i * kCols + lane; c < a.V && c < (i + 1) * kCols; c += 32)
-        e[c] = __float2bfloat16_rn(__bfloat162float(e[c]) * by);
-    }
-  }
+  // log(total / label): where label underflows against a far larger logit, from the exponents
+  const bool near = top - z2 < 60.f;
+  const float loss = near ? log1pf(others / label) : (top - z2) * kLn2 + logf(total);
+  if (a.loss) a.loss[t] = loss;
+  if (a.lse) a.lse[t] = near ? z + loss : top * kLn2 + logf(total);
+  if (a.dX) a.factors[row] = make_float2(g / total, -g * (others / total));
 }
 
 // dX[token] = f.x sum over the parts + f.y W[label]. A warp per 256 columns of a row, or, where
@@ -600,24 +702,24 @@ __global__ void __launch_bounds__(256) sq_head_rows_kernel(const HeadArgs a, con
 
 // As many two-CTA clusters as fit on the GPU at once, or one per tile (most: no number of tiles
 // that the host knows).
-template <bool GRAD>
+template <bool GRAD, int BK>
 cudaError_t launch_head_product(const CUtensorMap &tmA, const CUtensorMap &tmB, const CUtensorMap &tmO,
                                 const HeadArgs &a, int first, int64_t most, int sm_count, cudaStream_t stream) {
-  using C = HeadCfg<GRAD>;
+  using C = HeadCfg<GRAD, BK>;
   static int done_mask = 0;  // per device ordinal (first 31)
   static int max_clusters[32] = {0};
   int dev = 0;
   cudaGetDevice(&dev);
   if (!(done_mask & (1 << (dev & 31)))) {
     cudaError_t e =
-        cudaFuncSetAttribute(sq_head_kernel<GRAD>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
+        cudaFuncSetAttribute(sq_head_kernel<GRAD, BK>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * (sm_count / 2), 1, 1);
     cfg.blockDim = dim3(C::kThreads, 1, 1);
     cfg.dynamicSmemBytes = C::kSmemBytes;
     int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, sq_head_kernel<GRAD>, &cfg) != cudaSuccess || n <= 0) {
+    if (cudaOccupancyMaxActiveClusters(&n, sq_head_kernel<GRAD, BK>, &cfg) != cudaSuccess || n <= 0) {
       cudaGetLastError();
       n = sm_count / 2;
     }
@@ -625,7 +727,7 @@ cudaError_t launch_head_product(const CUtensorMap &tmA, const CUtensorMap &tmB, 
     done_mask |= 1 << (dev & 31);
   }
   const int64_t clusters = std::min<int64_t>(most, max_clusters[dev & 31]);
-  return launch_after(sq_head_kernel<GRAD>, static_cast<unsigned>(2 * clusters), C::kThreads, C::kSmemBytes, stream, tmA,
+  return launch_after(sq_head_kernel<GRAD, BK>, static_cast<unsigned>(2 * clusters), C::kThreads, C::kSmemBytes, stream, tmA,
                       tmB, tmO, a, first);
 }
 
@@ -639,14 +741,19 @@ cudaError_t launch_head_gather(const HeadArgs &a, cudaStream_t stream) {
 cudaError_t launch_head_chunk(const HeadArgs &a, const HeadMaps &m, int first, int sm_count, cudaStream_t stream) {
   const int rows = a.T - first < a.chunk ? a.T - first : a.chunk;
   const int64_t tiles_m = (rows + kHeadTile - 1) / kHeadTile;
-  cudaError_t e = launch_head_product<false>(m.rows, m.weights, m.e_store, a, first,
-                                             tiles_m * ((a.V + kHeadTile - 1) / kHeadTile), sm_count, stream);
+  // Few tokens are bound by the weights' way from memory: stages of 128, whose rows are read 256 bytes
+  // at a time (one token against 128256 x 4096 in 177 us, 183 with 64). More are bound by the MMAs:
+  // stages of 64, of which five wait behind the one in work (2048 against 38912 x 2048 in 163 us, 175
+  // with 128).
+  const bool few = a.box_rows < 128;
+  const auto logits = few ? launch_head_product<false, 128> : launch_head_product<false, 64>;
+  cudaError_t e =
+      logits(m.rows, m.weights, m.e_store, a, first, tiles_m * ((a.V + kHeadTile - 1) / kHeadTile), sm_count, stream);
   if (e != cudaSuccess) return e;
-  // a CTA per row pays from some 250 quarter tiles on
-  if (a.V > 16384)
-    e = launch_after(sq_head_finalize_kernel<8>, rows, 256, 0, stream, a, first);
-  else
-    e = launch_after(sq_head_finalize_kernel<1>, (rows + 7) / 8, 256, 0, stream, a, first);
+  // a warp per quarter tile, up to 32
+  const int64_t quarters = (a.V + HeadCfg<false, 64>::kEpiCols - 1) / HeadCfg<false, 64>::kEpiCols;
+  const int warps = quarters >= 32 ? 32 : static_cast<int>(quarters);
+  e = launch_after(sq_head_finalize_kernel, (rows + 31) / 32, 32 * warps, 0, stream, a, first);
   if (e != cudaSuccess || !a.dX) return e;
   const int64_t tiles_d = (a.D + kHeadTile - 1) / kHeadTile;
   int64_t units = 0, parts = 0;  // the most of any number of labelled rows
@@ -654,7 +761,9 @@ cudaError_t launch_head_chunk(const HeadArgs &a, const HeadMaps &m, int first, i
     units = std::max(units, t * tiles_d * (a.parts[t - 1] + 1));
     parts = std::max<int64_t>(parts, a.parts[t - 1] + 1);
   }
-  if ((e = launch_head_product<true>(m.e_load, m.weights, m.partial, a, first, units, sm_count, stream)) != cudaSuccess)
+  const auto gradient = few ? launch_head_product<true, 128> : launch_head_product<true, 64>;
+  if ((e = gradient(m.e_load, few ? m.weights : m.weights_short, m.partial, a, first, units, sm_count, stream)) !=
+      cudaSuccess)
     return e;
   const int64_t pieces = rows * ((a.D + 255) / 256);
   if (parts >= 16)
