@@ -447,6 +447,7 @@ sq_status run_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint
     chunk = std::min(whole, std::max<int64_t>(fit, sqi::kHeadTile));
   }
   a.chunk = static_cast<int>(chunk);
+  a.sum_rows = static_cast<int>(up(std::min(piece, chunk), 4));
   a.box_rows = T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128;
   const int64_t quarters = 4 * ((V + sqi::kHeadTile - 1) / sqi::kHeadTile);
   int64_t partial_rows = 0;  // of 4 * D bytes: the most that any number of labelled rows takes

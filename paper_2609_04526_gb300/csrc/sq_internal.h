@@ -423,7 +423,8 @@ struct HeadArgs {
   float2 *factors;
   uint16_t *rows;         // [T, D] the labelled tokens' rows of X
   // scratch, by row of the chunk
-  float *sums, *refs;     // [4 * column tiles, chunk] sum and reference of each quarter tile
+  int sum_rows;           // a chunk's rows, up to a multiple of 4
+  float *sums, *refs;     // [4 * column tiles, sum_rows] sum and reference of each quarter tile
   int *moved;             // [chunk] a row whose references differ (refs are read only there)
   uint16_t *e;            // [chunk, pitch] bf16 exponentials (gradient)
   float *partial;         // [parts, rows, D] fp32 (gradient)

@@ -506,7 +506,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK>::k
         }
         if (!ok) break;
         // the next tile's labels are on their way while this one's exponentials are formed
-        const int64_t at_sum = static_cast<int64_t>(4 * t.tn + share) * a.chunk + row32 + lane;
+        const int64_t at_sum = static_cast<int64_t>(4 * t.tn + share) * a.sum_rows + row32 + lane;
         t.advance();
         if (t.more()) labels();
         if (col0 >= a.V) continue;
@@ -584,16 +584,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK>::k
 
 // ---------------------------------------------------------------- finalize and rows
 
-// 32 rows per CTA, one per lane; the warps take the quarter tiles in turn (coalesced: a column of
-// quarter tiles lies row by row), and the rows' 32 partial sums are added in order.
+// ROWS rows per CTA: each takes 32 / ROWS lanes of every warp, which take the quarter tiles in turn
+// (neighbouring rows of one quarter tile lie side by side). 32 rows read whole lines; 4 give few
+// tokens eight times the threads. The order of a row's sum is the same in both, so it depends on
+// nothing but the row: 256 sums of every 256th quarter tile, eight to a warp, then the warps'.
+template <int ROWS>
 __global__ void __launch_bounds__(1024) sq_head_finalize_kernel(const HeadArgs a, const int first) {
-  __shared__ float parts[32][33];
+  constexpr int kShare = 32 / ROWS;
+  __shared__ float parts[32][ROWS + 1];
   dependency_wait();
   dependency_start();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  const int rows = chunk_rows(a, first), r0 = blockIdx.x * 32;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int rows = chunk_rows(a, first), r0 = blockIdx.x * ROWS;
   if (r0 >= rows) return;
-  const int r = min(r0 + lane, rows - 1), row = first + r;  // lanes past the last row repeat it
+  const int own = lane % ROWS;  // of the CTA's rows
+  const int r = min(r0 + own, rows - 1), row = first + r;  // lanes past the last row repeat it
   constexpr int kCols = HeadCfg<false, 64>::kEpiCols;
   const int filled = static_cast<int>((a.V + kCols - 1) / kCols);  // quarter tiles that hold columns
   const float *sums = a.sums + r, *refs = a.refs + r;
@@ -603,36 +608,56 @@ __global__ void __launch_bounds__(1024) sq_head_finalize_kernel(const HeadArgs a
   float top = row_reference(z), sum = 0.f;
   const bool moved = a.moved[r];
   const bool any = __any_sync(0xFFFFFFFFu, moved);  // the same rows in every warp
-  if (any) {  // references differ: the largest of them first
-    for (int i = warp; i < filled; i += warps) top = fmaxf(top, refs[static_cast<int64_t>(i) * a.chunk]);
-    parts[warp][lane] = top;
-    __syncthreads();
-    for (int w = 0; w < warps; ++w) top = fmaxf(top, parts[w][lane]);
-    __syncthreads();
-    for (int i = warp; i < filled; i += warps) {
-      const int64_t at = static_cast<int64_t>(i) * a.chunk;
-      sum += sums[at] * whole_exp2(refs[at] - top);
+  // f over the row's quarter tiles of this warp
+  constexpr int kOwn = 8 / kShare;  // of the warp's eight sums, those of this lane
+  auto over_tiles = [&](float start, auto value, auto f) {
+    float v[kOwn];
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j) v[j] = start;
+#pragma unroll kShare
+    for (int i0 = 8 * warp + lane / ROWS; i0 < filled; i0 += 256) {
+#pragma unroll
+      for (int j = 0; j < kOwn; ++j)
+        if (i0 + j < filled) v[j] = f(v[j], value(static_cast<int64_t>(i0 + j) * a.sum_rows));
     }
+#pragma unroll
+    for (int d = 4; d > 0; d >>= 1) {
+      if (d < kOwn) {
+#pragma unroll
+        for (int j = 0; j < d; ++j) v[j] = f(v[j], v[j + d]);
+      } else if (kShare > 1) {
+        v[0] = f(v[0], __shfl_xor_sync(0xFFFFFFFFu, v[0], d * ROWS));
+      }
+    }
+    return v[0];
+  };
+  auto larger = [](float x, float y) { return fmaxf(x, y); };
+  auto plus = [](float x, float y) { return x + y; };
+  if (any) {  // references differ: the largest of them first
+    parts[warp][own] = over_tiles(top, [&](int64_t at) { return refs[at]; }, larger);
+    __syncthreads();
+    for (int w = 0; w < 32; ++w) top = fmaxf(top, parts[w][own]);
+    __syncthreads();
+    sum = over_tiles(0.f, [&](int64_t at) { return sums[at] * whole_exp2(refs[at] - top); }, plus);
   } else {
-#pragma unroll 8
-    for (int i = warp; i < filled; i += warps) sum += sums[static_cast<int64_t>(i) * a.chunk];
+    sum = over_tiles(0.f, [&](int64_t at) { return sums[at]; }, plus);
   }
-  parts[warp][lane] = sum;
+  parts[warp][own] = sum;
   __syncthreads();
   if (any && a.e) {  // the exponentials of moved rows follow their reference
-    for (int i = warp; i < filled; i += warps)
-      for (int l = 0; l < 32 && r0 + l < rows; ++l) {
+    for (int i = warp; i < filled; i += 32)
+      for (int l = 0; l < ROWS && r0 + l < rows; ++l) {
         if (!__shfl_sync(0xFFFFFFFFu, moved, l)) continue;
-        const float by = whole_exp2(a.refs[static_cast<int64_t>(i) * a.chunk + r0 + l] - __shfl_sync(0xFFFFFFFFu, top, l));
+        const float by = whole_exp2(a.refs[static_cast<int64_t>(i) * a.sum_rows + r0 + l] - __shfl_sync(0xFFFFFFFFu, top, l));
         if (by == 1.f) continue;
         __nv_bfloat16 *e = reinterpret_cast<__nv_bfloat16 *>(a.e) + static_cast<int64_t>(r0 + l) * a.pitch;
         for (int64_t c = i * kCols + lane; c < a.V && c < (i + 1) * kCols; c += 32)
           e[c] = __float2bfloat16_rn(__bfloat162float(e[c]) * by);
       }
   }
-  if (warp > 0 || r0 + lane >= rows) return;
+  if (warp > 0 || lane >= ROWS || r0 + lane >= rows) return;
   float others = 0.f;
-  for (int w = 0; w < warps; ++w) others += parts[w][lane];
+  for (int w = 0; w < 32; ++w) others += parts[w][own];
   a.moved[r] = 0;  // for the next chunk
   const float label = exp2_fast(z2 - top), total = others + label;
   // log(total / label): where label underflows against a far larger logit, from the exponents
@@ -750,10 +775,10 @@ cudaError_t launch_head_chunk(const HeadArgs &a, const HeadMaps &m, int first, i
   cudaError_t e =
       logits(m.rows, m.weights, m.e_store, a, first, tiles_m * ((a.V + kHeadTile - 1) / kHeadTile), sm_count, stream);
   if (e != cudaSuccess) return e;
-  // a warp per quarter tile, up to 32
-  const int64_t quarters = (a.V + HeadCfg<false, 64>::kEpiCols - 1) / HeadCfg<false, 64>::kEpiCols;
-  const int warps = quarters >= 32 ? 32 : static_cast<int>(quarters);
-  e = launch_after(sq_head_finalize_kernel, (rows + 31) / 32, 32 * warps, 0, stream, a, first);
+  if (rows <= 1024)
+    e = launch_after(sq_head_finalize_kernel<4>, (rows + 3) / 4, 1024, 0, stream, a, first);
+  else
+    e = launch_after(sq_head_finalize_kernel<32>, (rows + 31) / 32, 1024, 0, stream, a, first);
   if (e != cudaSuccess || !a.dX) return e;
   const int64_t tiles_d = (a.D + kHeadTile - 1) / kHeadTile;
   int64_t units = 0, parts = 0;  // the most of any number of labelled rows
