@@ -485,6 +485,7 @@ sq_status run_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint
   sqi::HeadMaps m;
   SQ_TRY(make_act_map(h, &m.rows, a.rows, D, whole, 64, a.box_rows));
   SQ_TRY(make_act_map(h, &m.weights, W, D, V, 64, 128));
+  SQ_TRY(make_act_map(h, &m.weights_narrow, W, D, V, 64, 32));
   m.weights_short = m.e_store = m.e_load = m.partial = m.rows;
   if (dX) {
     SQ_TRY(make_act_map(h, &m.weights_short, W, D, V, 64, 64));

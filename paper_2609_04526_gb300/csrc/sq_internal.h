@@ -430,10 +430,10 @@ struct HeadArgs {
   float *partial;         // [parts, rows, D] fp32 (gradient)
   int *err;
 };
-// weights: 64 x 128 boxes, weights_short 64 x 64, rows and e_load 64 x box_rows, partial 32 x 32 fp32,
+// weights: 64 x 128 boxes, weights_short 64 x 64, weights_narrow 64 x 32, rows and e_load 64 x box_rows, partial 32 x 32 fp32,
 // all with the 128-byte swizzle; e_store 32 x 32, 64-byte swizzle.
 struct HeadMaps {
-  CUtensorMap rows, weights, weights_short, e_store, e_load, partial;
+  CUtensorMap rows, weights, weights_short, weights_narrow, e_store, e_load, partial;
 };
 cudaError_t launch_head_gather(const HeadArgs &a, cudaStream_t stream);
 cudaError_t launch_head_chunk(const HeadArgs &a, const HeadMaps &m, int first, int sm_count, cudaStream_t stream);

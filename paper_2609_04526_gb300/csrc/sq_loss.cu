@@ -35,23 +35,22 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRefSlack = 100.f;  // a logit this far above the reference (in powers of two) moves it
 constexpr float kFarSum = 0x1p100f;  // the sum of a quarter tile that may hold one
 
-// Epilogue warp w takes TMEM lanes 32 (w % 4) .. + 31 and the w / 4-th share of a tile's columns:
-// a quarter (logits, whose columns stay in registers) or a half (gradient). Stages are BK deep: 64
-// keeps more of the ring in flight, 128 reads rows of W in longer runs (few tokens, see
-// launch_head_chunk).
-template <bool GRAD, int BK>
+// A pair's tile has 256 rows and NT columns, its stages are BK deep. Epilogue warp w takes TMEM lanes
+// 32 (w % 4) .. + 31 and the w / 4-th 64 columns (logits, which stay in registers) or 128 (gradient).
+template <bool GRAD, int BK, int NT>
 struct HeadCfg {
-  static constexpr int kEpiWarps = GRAD ? 8 : 16;
-  static constexpr int kEpiCols = kHeadTile / (kEpiWarps / 4);
+  static constexpr int kEpiCols = GRAD ? 128 : 64;
+  static constexpr int kEpiWarps = NT / kEpiCols * 4;
   static constexpr int kTmaWarp = kEpiWarps;
   static constexpr int kMmaWarp = kTmaWarp + 1;
   static constexpr int kThreads = 32 * (kMmaWarp + 1);
   static constexpr int kBK = BK;
-  static constexpr int kB = 128 * kBK * 2;    // bytes of this CTA's 128 columns of a stage
-  static constexpr int kRing = 192 * 1024;    // 6 stages of 128 rows and 128 columns, 64 deep
+  static constexpr int kCols = NT / 2;             // columns of a CTA
+  static constexpr int kB = kCols * kBK * 2;       // bytes of them in a stage
+  static constexpr int kRing = 192 * 1024;         // 6 stages of 128 rows and 128 columns, 64 deep
   static constexpr int kMaxStages = 12;
   static constexpr int kUnit = GRAD ? 128 / kBK : 1;  // stages of a unit of the walk's contraction
-  static constexpr int kTile = kHeadTile;
+  static constexpr int kRows = kHeadTile;
   static constexpr int kOffBox = kRing;
   static constexpr int kBoxBytes = 32 * 32 * (GRAD ? 4 : 2);  // 32 rows x 32 columns of a warp
   // Stages added up in one accumulator. The tensor core truncates its running fp32 sum at every
@@ -62,7 +61,8 @@ struct HeadCfg {
   static constexpr int kOffBar = kOffBox + kEpiWarps * kBoxBytes;
   static constexpr int kSmemBytes = kOffBar + 512 + 1024;
 };
-static_assert(HeadCfg<false, 64>::kSmemBytes <= 232448 && HeadCfg<true, 64>::kSmemBytes <= 232448, "head kernel exceeds the opt-in shared memory of one CTA");
+static_assert(HeadCfg<false, 64, 256>::kSmemBytes <= 232448 && HeadCfg<true, 64, 256>::kSmemBytes <= 232448,
+              "head kernel exceeds the opt-in shared memory of one CTA");
 
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
@@ -269,11 +269,11 @@ struct HeadWalk {
   }
 };
 
-template <bool GRAD, int BK>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK>::kThreads, 1)
+template <bool GRAD, int BK, int NT>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK, NT>::kThreads, 1)
     sq_head_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                    const __grid_constant__ CUtensorMap tmO, const HeadArgs a, const int first) {
-  using C = HeadCfg<GRAD, BK>;
+  using C = HeadCfg<GRAD, BK, NT>;
   // A stage holds box_rows rows of A; the MMAs read 128 all the same, the rest of them whatever
   // lies behind in the ring, and nothing reads those rows of the product. Few tokens so leave the
   // ring to the columns, which are all their traffic (one token against 128256 x 4096: 181 us with
@@ -326,8 +326,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK>::k
   dependency_wait();
   dependency_start();
   const int rows = chunk_rows(a, first);
-  const int tiles_m = (rows + C::kTile - 1) / C::kTile;
-  const int tiles_n = static_cast<int>(((GRAD ? a.D : a.V) + C::kTile - 1) / C::kTile);
+  const int tiles_m = (rows + C::kRows - 1) / C::kRows;
+  const int tiles_n = static_cast<int>(((GRAD ? a.D : a.V) + NT - 1) / NT);
   constexpr int kDepth = C::kBK * C::kUnit;
   const int stages = static_cast<int>(((GRAD ? a.V : a.D) + kDepth - 1) / kDepth);
   const int parts = GRAD && tiles_m > 0 ? a.parts[tiles_m - 1] + 1 : 1;
@@ -341,8 +341,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK>::k
       int s = 0;
       uint32_t ph = 1;  // parity of the phase that frees slot s: its first use finds it free
       for (; t.more() && ok; t.advance()) {
-        const int32_t row0 = (GRAD ? 0 : first) + t.tm * C::kTile + 128 * static_cast<int32_t>(rank);
-        const int32_t col0 = t.tn * C::kTile + 128 * static_cast<int32_t>(rank);
+        const int32_t row0 = (GRAD ? 0 : first) + t.tm * C::kRows + 128 * static_cast<int32_t>(rank);
+        const int32_t col0 = t.tn * NT + C::kCols * static_cast<int32_t>(rank);
         for (int kb = t.k0 * C::kUnit; kb < (t.k0 + t.nk) * C::kUnit; ++kb, ++it) {
           if (it >= S && !(ok = mbar_wait(&empty[s], ph, abort_flag, a.err))) break;
           if (rank == 0) mbar_arrive_expect_tx(&full[s], 2 * C::kB + (both ? 2 : 1) * a_bytes);
@@ -353,9 +353,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK>::k
           if (GRAD) {  // 64 columns of D x kBK vocabulary rows
             for (int j = 0; j < 2; ++j)
               tma_load_2d_pair(smem_u32(stage_b(s)) + j * (C::kB / 2), &tmB, bar, col0 + 64 * j, kb * C::kBK);
-          } else {  // 128 vocabulary rows x 64 columns of D
+          } else {  // kCols vocabulary rows x 64 columns of D
             for (int j = 0; j < C::kBK / 64; ++j)
-              tma_load_2d_pair(smem_u32(stage_b(s)) + j * 16384, &tmB, bar, kb * C::kBK + 64 * j, col0);
+              tma_load_2d_pair(smem_u32(stage_b(s)) + j * (C::kCols * 128), &tmB, bar, kb * C::kBK + 64 * j, col0);
           }
           if (++s == S) {
             s = 0;
@@ -371,7 +371,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK>::k
     // ------------------------------------------------------ MMA issuer (leader CTA)
     // The whole warp walks the stages, so a wait that runs out for some lanes ends all of them.
     if (rank == 0) {
-      constexpr uint32_t idesc = idesc_bf16(2 * 128, C::kTile, 0, GRAD ? 1 : 0);
+      constexpr uint32_t idesc = idesc_bf16(2 * 128, NT, 0, GRAD ? 1 : 0);
       // K-major: K step kk in 64-wide chunk kk / 4 (a box apart), byte 32 (kk % 4) of each row;
       // MN-major: 16 contraction rows (2 KiB) per step, 64-column atoms half the operand apart
       const uint64_t ad_base = smem_desc_sw128(smem_u32(stage_a(0)), 16, 1024);
@@ -395,7 +395,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK>::k
 #pragma unroll
             for (int kk = 0; kk < C::kBK / 16; ++kk) {
               const uint32_t ka = (kk >> 2) * (a.box_rows * 8) + (kk & 3) * 2;
-              const uint32_t kb_ = GRAD ? (kk * 2048) >> 4 : ((kk >> 2) * 16384 + (kk & 3) * 32) >> 4;
+              const uint32_t kb_ = GRAD ? (kk * 2048) >> 4 : ((kk >> 2) * (C::kCols * 128) + (kk & 3) * 32) >> 4;
               umma_pair_elect(d_tmem, a0 + ka, b0 + kb_, idesc, (kb > 0 || kk > 0) ? 1u : 0u);
             }
             umma_commit_pair_mc_elect(&empty[s]);
@@ -436,7 +436,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK>::k
     int label = -1;  // of this lane's row in the next tile, and its logit
     float label_z = 0.f;
     auto labels = [&] {
-      const int r = t.tm * C::kTile + 128 * static_cast<int>(rank) + 32 * quad + lane;
+      const int r = t.tm * C::kRows + 128 * static_cast<int>(rank) + 32 * quad + lane;
       label = -1;
       label_z = 0.f;
       if (!GRAD && r < rows) {
@@ -446,14 +446,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK>::k
     };
     if (t.more()) labels();
     while (t.more() && ok) {
-      const int row32 = t.tm * C::kTile + 128 * static_cast<int>(rank) + 32 * quad;  // of the chunk
-      const int col0 = t.tn * C::kTile + C::kEpiCols * share;
+      const int row32 = t.tm * C::kRows + 128 * static_cast<int>(rank) + 32 * quad;  // of the chunk
+      const int col0 = t.tn * NT + C::kEpiCols * share;
       if constexpr (GRAD) {
         const int ab = tc & 1;
         if (!(ok = mbar_wait(&tfull[ab], static_cast<uint32_t>(tc >> 1) & 1u, abort_flag, a.err))) break;
         tc_fence_after();
         const uint32_t t_buf = t_row + ab * kTmemCols;
-        const int32_t out_row = t.part * tiles_m * C::kTile + row32;
+        const int32_t out_row = t.part * tiles_m * C::kRows + row32;
 #pragma unroll 1
         for (int g = 0; g < C::kEpiCols / 32; ++g) {
           uint32_t v[32];
@@ -506,7 +506,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK>::k
         }
         if (!ok) break;
         // the next tile's labels are on their way while this one's exponentials are formed
-        const int64_t at_sum = static_cast<int64_t>(4 * t.tn + share) * a.sum_rows + row32 + lane;
+        const int64_t at_sum = static_cast<int64_t>(col0 / C::kEpiCols) * a.sum_rows + row32 + lane;
         t.advance();
         if (t.more()) labels();
         if (col0 >= a.V) continue;
@@ -599,7 +599,7 @@ __global__ void __launch_bounds__(1024) sq_head_finalize_kernel(const HeadArgs a
   if (r0 >= rows) return;
   const int own = lane % ROWS;  // of the CTA's rows
   const int r = min(r0 + own, rows - 1), row = first + r;  // lanes past the last row repeat it
-  constexpr int kCols = HeadCfg<false, 64>::kEpiCols;
+  constexpr int kCols = HeadCfg<false, 64, 256>::kEpiCols;
   const int filled = static_cast<int>((a.V + kCols - 1) / kCols);  // quarter tiles that hold columns
   const float *sums = a.sums + r, *refs = a.refs + r;
   const float z = a.label_z[row], z2 = z * kLog2e;
@@ -727,24 +727,24 @@ __global__ void __launch_bounds__(256) sq_head_rows_kernel(const HeadArgs a, con
 
 // As many two-CTA clusters as fit on the GPU at once, or one per tile (most: no number of tiles
 // that the host knows).
-template <bool GRAD, int BK>
+template <bool GRAD, int BK, int NT>
 cudaError_t launch_head_product(const CUtensorMap &tmA, const CUtensorMap &tmB, const CUtensorMap &tmO,
                                 const HeadArgs &a, int first, int64_t most, int sm_count, cudaStream_t stream) {
-  using C = HeadCfg<GRAD, BK>;
+  using C = HeadCfg<GRAD, BK, NT>;
   static int done_mask = 0;  // per device ordinal (first 31)
   static int max_clusters[32] = {0};
   int dev = 0;
   cudaGetDevice(&dev);
   if (!(done_mask & (1 << (dev & 31)))) {
     cudaError_t e =
-        cudaFuncSetAttribute(sq_head_kernel<GRAD, BK>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
+        cudaFuncSetAttribute(sq_head_kernel<GRAD, BK, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * (sm_count / 2), 1, 1);
     cfg.blockDim = dim3(C::kThreads, 1, 1);
     cfg.dynamicSmemBytes = C::kSmemBytes;
     int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, sq_head_kernel<GRAD, BK>, &cfg) != cudaSuccess || n <= 0) {
+    if (cudaOccupancyMaxActiveClusters(&n, sq_head_kernel<GRAD, BK, NT>, &cfg) != cudaSuccess || n <= 0) {
       cudaGetLastError();
       n = sm_count / 2;
     }
@@ -752,7 +752,7 @@ cudaError_t launch_head_product(const CUtensorMap &tmA, const CUtensorMap &tmB, 
     done_mask |= 1 << (dev & 31);
   }
   const int64_t clusters = std::min<int64_t>(most, max_clusters[dev & 31]);
-  return launch_after(sq_head_kernel<GRAD, BK>, static_cast<unsigned>(2 * clusters), C::kThreads, C::kSmemBytes, stream, tmA,
+  return launch_after(sq_head_kernel<GRAD, BK, NT>, static_cast<unsigned>(2 * clusters), C::kThreads, C::kSmemBytes, stream, tmA,
                       tmB, tmO, a, first);
 }
 
@@ -767,13 +767,20 @@ cudaError_t launch_head_chunk(const HeadArgs &a, const HeadMaps &m, int first, i
   const int rows = a.T - first < a.chunk ? a.T - first : a.chunk;
   const int64_t tiles_m = (rows + kHeadTile - 1) / kHeadTile;
   // Few tokens are bound by the weights' way from memory: stages of 128, whose rows are read 256 bytes
-  // at a time (one token against 128256 x 4096 in 177 us, 183 with 64). More are bound by the MMAs:
-  // stages of 64, of which five wait behind the one in work (2048 against 38912 x 2048 in 163 us, 175
-  // with 128).
+  // at a time. More are bound by the MMAs: stages of 64, of which five wait behind the one in work
+  // (2048 against 38912 x 2048 in 163 us, 175 with 128). Up to 256 tokens whose tiles of 256 columns
+  // would reach every other cluster at most take tiles of 64 (8 tokens against 3211 x 2312, loss and
+  // gradient: 26.6 us, 32.7 with 256; 1000 tokens against 2000 x 4096 were 2 % slower).
   const bool few = a.box_rows < 128;
-  const auto logits = few ? launch_head_product<false, 128> : launch_head_product<false, 64>;
-  cudaError_t e =
-      logits(m.rows, m.weights, m.e_store, a, first, tiles_m * ((a.V + kHeadTile - 1) / kHeadTile), sm_count, stream);
+  const int64_t wide = tiles_m * ((a.V + 255) / 256);
+  cudaError_t e;
+  if (tiles_m == 1 && 4 * wide <= sm_count)
+    e = launch_head_product<false, 128, 64>(m.rows, m.weights_narrow, m.e_store, a, first, tiles_m * ((a.V + 63) / 64),
+                                            sm_count, stream);
+  else if (few)
+    e = launch_head_product<false, 128, 256>(m.rows, m.weights, m.e_store, a, first, wide, sm_count, stream);
+  else
+    e = launch_head_product<false, 64, 256>(m.rows, m.weights, m.e_store, a, first, wide, sm_count, stream);
   if (e != cudaSuccess) return e;
   if (rows <= 1024)
     e = launch_after(sq_head_finalize_kernel<4>, (rows + 3) / 4, 1024, 0, stream, a, first);
@@ -786,7 +793,7 @@ cudaError_t launch_head_chunk(const HeadArgs &a, const HeadMaps &m, int first, i
     units = std::max(units, t * tiles_d * (a.parts[t - 1] + 1));
     parts = std::max<int64_t>(parts, a.parts[t - 1] + 1);
   }
-  const auto gradient = few ? launch_head_product<true, 128> : launch_head_product<true, 64>;
+  const auto gradient = few ? launch_head_product<true, 128, 256> : launch_head_product<true, 64, 256>;
   if ((e = gradient(m.e_load, few ? m.weights : m.weights_short, m.partial, a, first, units, sm_count, stream)) !=
       cudaSuccess)
     return e;
