@@ -140,6 +140,7 @@ __device__ __forceinline__ int chunk_rows(const HeadArgs &a, int first) {
 // 4096 in 7.3 us.
 template <int SHARE>
 __global__ void __launch_bounds__(256) sq_head_gather_kernel(const HeadArgs a) {
+  static_assert(SHARE == 1 || SHARE == 8, "a token's 256 lanes, or 32 that take their eight sums");
   constexpr int kTokens = 8 / SHARE;
   __shared__ int before[8];
   __shared__ float dots[8];
@@ -182,18 +183,25 @@ __global__ void __launch_bounds__(256) sq_head_gather_kernel(const HeadArgs a) {
     const uint4 *x = reinterpret_cast<const uint4 *>(a.X + static_cast<int64_t>(t) * a.D);
     const uint4 *w = reinterpret_cast<const uint4 *>(a.W + y * a.D);
     uint4 *out = reinterpret_cast<uint4 *>(a.rows + static_cast<int64_t>(row) * a.D);
-#pragma unroll 4
-    for (int i = first; i < pieces; i += 32 * SHARE) {
-      const uint4 p = __ldg(x + i), q = __ldg(w + i);
-      out[i] = p;
-      const uint32_t pw[4] = {p.x, p.y, p.z, p.w}, qw[4] = {q.x, q.y, q.z, q.w};
+    // eight sums of every 256th 16 bytes, a warp's or, of one warp, each lane's own: one order for both
+    float sums[kTokens] = {};
+    for (int i0 = first; i0 < pieces; i0 += 256) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        dot = fmaf(__uint_as_float(pw[c] << 16), __uint_as_float(qw[c] << 16), dot);
-        dot = fmaf(__uint_as_float(pw[c] & 0xFFFF0000u), __uint_as_float(qw[c] & 0xFFFF0000u), dot);
+      for (int c = 0; c < kTokens; ++c) {
+        const int i = i0 + 32 * c;
+        if (i >= pieces) break;
+        const uint4 p = __ldg(x + i), q = __ldg(w + i);
+        out[i] = p;
+        const uint32_t pw[4] = {p.x, p.y, p.z, p.w}, qw[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          sums[c] = fmaf(__uint_as_float(pw[e] << 16), __uint_as_float(qw[e] << 16), sums[c]);
+          sums[c] = fmaf(__uint_as_float(pw[e] & 0xFFFF0000u), __uint_as_float(qw[e] & 0xFFFF0000u), sums[c]);
+        }
       }
     }
-    dot = warp_total(dot);
+#pragma unroll
+    for (int c = 0; c < kTokens; ++c) dot += warp_total(sums[c]);
   }
   if (SHARE > 1) {
     if (lane == 0) dots[warp] = dot;

@@ -210,3 +210,12 @@ def test_refusals(h):
         h.sq_head_loss(X[:, :12].contiguous(), W[:, :12].contiguous(), labels)
     with pytest.raises(pkg.SQError, match="dX must not be X"):
         h.sq_head_loss_grad(X, W, labels, dloss, dX=X)
+
+
+def test_loss_of_a_row_is_its_own(h):
+    """Loss and log-sum-exp of a token have the same bits alone, among few and among many."""
+    X, W, labels, _ = _case(1500, 264, 3001, 12, ignored=0.0)
+    loss, lse = h.sq_head_loss(X, W, labels)
+    for first, n in ((0, 1), (700, 7), (1000, 100), (3, 300)):
+        for got, want in zip(h.sq_head_loss(X[first:first + n].contiguous(), W, labels[first:first + n].clone()), (loss, lse)):
+            assert torch.equal(got, want[first:first + n])
