@@ -452,8 +452,8 @@ sq_status run_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint
   const int64_t quarters = 4 * ((V + sqi::kHeadTile - 1) / sqi::kHeadTile);
   int64_t partial_rows = 0;  // of 4 * D bytes: the most that any number of labelled rows takes
   for (int64_t m = 1; dX && m <= chunk / sqi::kHeadTile; ++m) {
-    const int parts = sqi::head_parts(m * ((D + sqi::kHeadTile - 1) / sqi::kHeadTile), static_cast<int>((V + 127) / 128),
-                                      dev->sm_count / 2);
+    const int parts = sqi::head_parts(std::min(m * sqi::kHeadTile, piece), D, static_cast<int>((V + 127) / 128),
+                                      std::max(1, dev->sm_count / 2));
     a.parts[m - 1] = static_cast<uint8_t>(parts - 1);
     partial_rows = std::max(partial_rows, m * sqi::kHeadTile * parts);
   }

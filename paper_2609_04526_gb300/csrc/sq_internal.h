@@ -390,17 +390,22 @@ constexpr int64_t kHeadPieceBytes = int64_t(512) << 20;
 constexpr int kMaxHeadParts = 64;
 constexpr int kMinHeadPartStages = 2;  // a part of the vocabulary is at least 2 x 128 entries long
 
-// Vocabulary parts of a gradient launch of `tiles` tiles: with w(s) = ceil(tiles s / clusters) / s
-// the launch's length in whole tiles per cluster, the smallest s within 3 % of the smallest w (each
-// part writes and reads back an fp32 plane of the tile).
-inline int head_parts(int64_t tiles, int stages, int clusters) {
+// Vocabulary parts of a gradient launch over `rows` rows of D columns, `stages` 128 deep: the s with
+// the least estimate of the launch, ceil(tiles s / clusters) / s tiles per cluster at 0.56 us a
+// stage, and of the s fp32 planes it writes and the row kernel reads back, at 5 TB/s. (The longest
+// waves alone as the rule gave 2048 rows against 38912 x 2048 19 parts: product and rows 184 + 38
+// us; unsplit 170 + 9.)
+inline int head_parts(int64_t rows, int64_t D, int stages, int clusters) {
   const int most = std::max(1, std::min(stages / kMinHeadPartStages, kMaxHeadParts));
-  auto waves = [&](int s) { return static_cast<double>((tiles * s + clusters - 1) / clusters) / s; };
-  double best = waves(1);
-  for (int s = 2; s <= most; ++s) best = std::min(best, waves(s));
-  for (int s = 1; s < most; ++s)
-    if (waves(s) <= 1.03 * best) return s;
-  return most;
+  const int64_t tiles = (rows + kHeadTile - 1) / kHeadTile * ((D + kHeadTile - 1) / kHeadTile);
+  const double plane_us = static_cast<double>(rows) * static_cast<double>(D) * 8 / 5e6;
+  auto us = [&](int s) {
+    return static_cast<double>((tiles * s + clusters - 1) / clusters) / s * stages * 0.56 + s * plane_us;
+  };
+  int best = 1;
+  for (int s = 2; s <= most; ++s)
+    if (us(s) < us(best)) best = s;
+  return best;
 }
 
 struct HeadArgs {

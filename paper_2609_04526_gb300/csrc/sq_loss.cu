@@ -806,7 +806,7 @@ cudaError_t launch_head_chunk(const HeadArgs &a, const HeadMaps &m, int first, i
       cudaSuccess)
     return e;
   const int64_t pieces = rows * ((a.D + 255) / 256);
-  if (parts >= 16)
+  if (parts >= 8 && pieces <= 16 * static_cast<int64_t>(sm_count))  // too few warps for loads one after the other
     return launch_after(sq_head_rows_kernel<8>, static_cast<unsigned>(pieces), 256, 0, stream, a, first);
   return launch_after(sq_head_rows_kernel<1>, static_cast<unsigned>((pieces + 7) / 8), 256, 0, stream, a, first);
 }
