@@ -25,8 +25,8 @@ constexpr uint32_t kAll = 0xFFFFFFFFu;
 // warp per token and the logits as ordered integers, 522 of them a token (32768 tokens, top-8
 // of 128: 19 us); eight lanes share them among four tokens.
 
-// A logit as it is ranked; -inf is never chosen.
-__device__ __forceinline__ float rank_value(float z) { return z > -INFINITY ? fminf(z, FLT_MAX) : -INFINITY; }
+// A logit as it is ranked; -inf, and so NaN, is never chosen.
+__device__ __forceinline__ float rank_value(float z) { return fminf(fmaxf(z, -INFINITY), FLT_MAX); }
 
 __device__ __forceinline__ float load_logit(const float *p) { return __ldg(p); }
 __device__ __forceinline__ float load_logit(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(256)
   float total = 0.f;
   if (!normalize) {
 #pragma unroll
-    for (int i = 0; i < PER; ++i) total += z[i] > -INFINITY ? exp_of(z[i] - top) : 0.f;
+    for (int i = 0; i < PER; ++i) total += exp_of(z[i] - top);  // not a number without any logit, and unused
     total = lanes_sum<LANES>(total);
   }
   uint32_t order[kGroups];  // places within the group of its sorted logits, two bits each
@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(256)
   } else {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      dense[i] = dense[i] > -INFINITY ? exp_of(dense[i] - top) : 0.f;
+      dense[i] = exp_of(dense[i] - top);
       total += dense[i];
     }
   }
@@ -256,7 +256,7 @@ __global__ void __launch_bounds__(256)
 // take one CTA; more take a launch that counts per CTA and one that adds up the counts and places
 // the slots (each CTA reads all CTAs' counts: G x E words from the L2).
 
-constexpr int kSortStep = 4;  // loads of 32 slots in flight
+constexpr int kSortStep = 2;  // loads of 32 slots in flight
 constexpr int64_t kSortOne = 4096;
 constexpr int64_t kSortMany = 2048;  // slots of a CTA at least, of several
 constexpr int kSortThreads = 1024;   // of a CTA, of several
@@ -269,6 +269,17 @@ __device__ __forceinline__ void load_slots(const int *experts, int64_t at, int64
     e[s] = i < end ? __ldg(experts + i) : -1;
     if (e[s] >= E) e[s] = -1;
   }
+}
+
+// The lanes with the same expert (of `bits` bits) as this one, among those that have one: a vote per
+// bit (0.5 us less than __match_any_sync over 262144 slots of 128 experts).
+__device__ __forceinline__ uint32_t same_expert(int e, int bits) {
+  uint32_t same = __ballot_sync(kAll, e >= 0);
+  for (int b = 0; b < bits; ++b) {
+    const uint32_t set = __ballot_sync(kAll, (e >> b) & 1);
+    same &= (e >> b) & 1 ? set : ~set;
+  }
+  return same;
 }
 
 __global__ void __launch_bounds__(kSortThreads)
@@ -385,13 +396,14 @@ __global__ void __launch_bounds__(1024)
     __syncthreads();
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) offsets[E] = carry;
+  const int bits = 32 - __clz(E - 1);  // of the largest expert (none for one expert)
   for (int64_t at = begin; at < end; at += 32 * kSortStep) {
     int e[kSortStep];
     load_slots(experts, at, end, E, lane, e);
 #pragma unroll
     for (int s = 0; s < kSortStep; ++s) {
       const int64_t i = at + 32 * s + lane;
-      const uint32_t same = __match_any_sync(kAll, e[s]);
+      const uint32_t same = same_expert(e[s], bits);
       int row = -1;
       if (e[s] >= 0) row = first[e[s]] + mine[e[s]] + __popc(same & ((1u << lane) - 1));
       __syncwarp();
