@@ -441,15 +441,14 @@ sq_status run_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint
   a.W = W;
   a.pitch = up(V, 8);  // rows of e start on 16 bytes
   a.err = dev->err_word;
-  int64_t chunk = whole;
-  if (dX) {
-    const int64_t fit = sqi::kHeadPieceBytes / (2 * a.pitch) / sqi::kHeadTile * sqi::kHeadTile;
-    chunk = std::min(whole, std::max<int64_t>(fit, sqi::kHeadTile));
-  }
+  const int64_t quarters = 4 * ((V + sqi::kHeadTile - 1) / sqi::kHeadTile);
+  // rows whose exponentials or, without a gradient, sums and references fit the bound
+  const int64_t row_bytes = dX ? 2 * a.pitch : 8 * quarters;
+  const int64_t fit = sqi::kHeadPieceBytes / row_bytes / sqi::kHeadTile * sqi::kHeadTile;
+  const int64_t chunk = std::min(whole, std::max<int64_t>(fit, sqi::kHeadTile));
   a.chunk = static_cast<int>(chunk);
   a.sum_rows = static_cast<int>(up(std::min(piece, chunk), 4));
   a.box_rows = T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128;
-  const int64_t quarters = 4 * ((V + sqi::kHeadTile - 1) / sqi::kHeadTile);
   int64_t partial_rows = 0;  // of 4 * D bytes: the most that any number of labelled rows takes
   for (int64_t m = 1; dX && m <= chunk / sqi::kHeadTile; ++m) {
     const int parts = sqi::head_parts(std::min(m * sqi::kHeadTile, piece), D, static_cast<int>((V + 127) / 128),

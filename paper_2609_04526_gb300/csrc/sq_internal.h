@@ -382,8 +382,8 @@ cudaError_t launch_combine_grad(int64_t T, int k, int64_t D, int64_t rows, const
                                 float *dweights, int sm_count, cudaStream_t stream);
 
 // Cross entropy against a vocabulary projection W [V, D] (sq_loss.cu). A call runs over pieces of
-// kHeadPiece tokens, a piece's labelled tokens over chunks whose exponentials fit
-// kHeadPieceBytes of scratch.
+// kHeadPiece tokens, a piece's labelled tokens over chunks whose exponentials (or, without a
+// gradient, sums) fit kHeadPieceBytes of scratch.
 constexpr int kHeadTile = 256;
 constexpr int kHeadPiece = 16384;
 constexpr int64_t kHeadPieceBytes = int64_t(512) << 20;

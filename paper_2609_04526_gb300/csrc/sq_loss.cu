@@ -420,6 +420,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK, NT
     }
   } else {
     // ------------------------------------------------------ epilogue (both CTAs)
+    // (a wait that runs out for some lanes ends the warp's tiles as a whole)
     const int quad = warp & 3, share = warp >> 2;
     const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + share * C::kEpiCols;
     const uint32_t box = smem_u32(smem + C::kOffBox + warp * C::kBoxBytes);
@@ -458,7 +459,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK, NT
       const int col0 = t.tn * NT + C::kEpiCols * share;
       if constexpr (GRAD) {
         const int ab = tc & 1;
-        if (!(ok = mbar_wait(&tfull[ab], static_cast<uint32_t>(tc >> 1) & 1u, abort_flag, a.err))) break;
+        if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&tfull[ab], static_cast<uint32_t>(tc >> 1) & 1u, abort_flag, a.err)))) break;
         tc_fence_after();
         const uint32_t t_buf = t_row + ab * kTmemCols;
         const int32_t out_row = t.part * tiles_m * C::kRows + row32;
@@ -490,7 +491,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK, NT
         static_assert(C::kEpiCols == 64, "two 32-column loads");
         for (int k0 = 0; k0 < stages; k0 += C::kSegment, ++tc) {
           const int ab = tc & 1;
-          if (!(ok = mbar_wait(&tfull[ab], static_cast<uint32_t>(tc >> 1) & 1u, abort_flag, a.err))) break;
+          if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&tfull[ab], static_cast<uint32_t>(tc >> 1) & 1u, abort_flag, a.err)))) break;
           tc_fence_after();
           if (k0 == 0) {
             tmem_ld32(t_row + ab * kTmemCols, z[0]);

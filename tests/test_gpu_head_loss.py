@@ -219,3 +219,20 @@ def test_loss_of_a_row_is_its_own(h):
     for first, n in ((0, 1), (700, 7), (1000, 100), (3, 300)):
         for got, want in zip(h.sq_head_loss(X[first:first + n].contiguous(), W, labels[first:first + n].clone()), (loss, lse)):
             assert torch.equal(got, want[first:first + n])
+
+
+def test_sums_of_a_large_vocabulary_in_chunks(h):
+    """A vocabulary whose sums alone pass the scratch's bound: the rows go in several chunks."""
+    T, D, V = 700, 8, 9_000_003
+    X, W, labels, _ = _case(T, D, V, 13, ignored=0.1)
+    loss, lse = h.sq_head_loss(X, W, labels)
+    for t in (0, 255, 256, 399, 511, 512, 699):
+        z = (X[t].double() @ W.double().t())
+        want = torch.logsumexp(z, 0)
+        if not 0 <= int(labels[t]) < V:
+            assert lse[t] == 0 and loss[t] == 0
+            continue
+        # fp32 logits of 8 products, 64-term and 562,501-term sums of positive terms (256 + 35,157 roundings a path)
+        tol = 1e-3
+        assert abs(float(lse[t]) - float(want)) < tol
+        assert abs(float(loss[t]) - float(want - z[labels[t]])) < tol
