@@ -185,18 +185,31 @@ __global__ void __launch_bounds__(256) sq_head_gather_kernel(const HeadArgs a) {
     uint4 *out = reinterpret_cast<uint4 *>(a.rows + static_cast<int64_t>(row) * a.D);
     // eight sums of every 256th 16 bytes, a warp's or, of one warp, each lane's own: one order for both
     float sums[kTokens] = {};
+    constexpr int kFlight = kTokens < 4 ? kTokens : 4;  // 16-byte loads of each row in flight
     for (int i0 = first; i0 < pieces; i0 += 256) {
 #pragma unroll
-      for (int c = 0; c < kTokens; ++c) {
-        const int i = i0 + 32 * c;
-        if (i >= pieces) break;
-        const uint4 p = __ldg(x + i), q = __ldg(w + i);
-        out[i] = p;
-        const uint32_t pw[4] = {p.x, p.y, p.z, p.w}, qw[4] = {q.x, q.y, q.z, q.w};
+      for (int c0 = 0; c0 < kTokens; c0 += kFlight) {
+        uint4 p[kFlight], q[kFlight];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          sums[c] = fmaf(__uint_as_float(pw[e] << 16), __uint_as_float(qw[e] << 16), sums[c]);
-          sums[c] = fmaf(__uint_as_float(pw[e] & 0xFFFF0000u), __uint_as_float(qw[e] & 0xFFFF0000u), sums[c]);
+        for (int c = 0; c < kFlight; ++c) {
+          const int i = i0 + 32 * (c0 + c);
+          p[c] = q[c] = make_uint4(0, 0, 0, 0);
+          if (i < pieces) {
+            p[c] = __ldg(x + i);
+            q[c] = __ldg(w + i);
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < kFlight; ++c) {
+          const int i = i0 + 32 * (c0 + c);
+          if (i < pieces) out[i] = p[c];
+          const uint32_t pw[4] = {p[c].x, p[c].y, p[c].z, p[c].w}, qw[4] = {q[c].x, q[c].y, q[c].z, q[c].w};
+          float &sum = sums[c0 + c];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            sum = fmaf(__uint_as_float(pw[e] << 16), __uint_as_float(qw[e] << 16), sum);
+            sum = fmaf(__uint_as_float(pw[e] & 0xFFFF0000u), __uint_as_float(qw[e] & 0xFFFF0000u), sum);
+          }
         }
       }
     }
@@ -594,9 +607,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK, NT
 // ---------------------------------------------------------------- finalize and rows
 
 // ROWS rows per CTA: each takes 32 / ROWS lanes of every warp, which take the quarter tiles in turn
-// (neighbouring rows of one quarter tile lie side by side). 32 rows read whole lines; 4 give few
-// tokens eight times the threads. The order of a row's sum is the same in both, so it depends on
-// nothing but the row: 256 sums of every 256th quarter tile, eight to a warp, then the warps'.
+// (neighbouring rows of one quarter tile lie side by side): 8 read whole sectors, 4 give few tokens
+// twice the CTAs (32, whole lines, left most SMs without rows: 14 us for 2048). The order of a row's
+// sum is the same in all, so it depends on nothing but the row: 256 sums of every 256th quarter
+// tile, eight to a warp, then the warps'.
 template <int ROWS>
 __global__ void __launch_bounds__(1024) sq_head_finalize_kernel(const HeadArgs a, const int first) {
   constexpr int kShare = 32 / ROWS;
@@ -624,18 +638,19 @@ __global__ void __launch_bounds__(1024) sq_head_finalize_kernel(const HeadArgs a
 #pragma unroll
     for (int j = 0; j < kOwn; ++j) v[j] = start;
 #pragma unroll kShare
-    for (int i0 = 8 * warp + lane / ROWS; i0 < filled; i0 += 256) {
+    for (int i0 = 8 * warp + lane / ROWS * kOwn; i0 < filled; i0 += 256) {
 #pragma unroll
       for (int j = 0; j < kOwn; ++j)
         if (i0 + j < filled) v[j] = f(v[j], value(static_cast<int64_t>(i0 + j) * a.sum_rows));
     }
 #pragma unroll
-    for (int d = 4; d > 0; d >>= 1) {
-      if (d < kOwn) {
+    for (int d = 4; d > 0; d >>= 1) {  // the eight sums in one order, over lanes or in the lane
+      if (d >= kOwn) {
+#pragma unroll
+        for (int j = 0; j < kOwn; ++j) v[j] = f(v[j], __shfl_xor_sync(0xFFFFFFFFu, v[j], d / kOwn * ROWS));
+      } else {
 #pragma unroll
         for (int j = 0; j < d; ++j) v[j] = f(v[j], v[j + d]);
-      } else if (kShare > 1) {
-        v[0] = f(v[0], __shfl_xor_sync(0xFFFFFFFFu, v[0], d * ROWS));
       }
     }
     return v[0];
@@ -791,10 +806,10 @@ cudaError_t launch_head_chunk(const HeadArgs &a, const HeadMaps &m, int first, i
   else
     e = launch_head_product<false, 64, 256>(m.rows, m.weights, m.e_store, a, first, wide, sm_count, stream);
   if (e != cudaSuccess) return e;
-  if (rows <= 1024)
+  if (rows <= 4 * sm_count)
     e = launch_after(sq_head_finalize_kernel<4>, (rows + 3) / 4, 1024, 0, stream, a, first);
   else
-    e = launch_after(sq_head_finalize_kernel<32>, (rows + 31) / 32, 1024, 0, stream, a, first);
+    e = launch_after(sq_head_finalize_kernel<8>, (rows + 7) / 8, 1024, 0, stream, a, first);
   if (e != cudaSuccess || !a.dX) return e;
   const int64_t tiles_d = (a.D + kHeadTile - 1) / kHeadTile;
   int64_t units = 0, parts = 0;  // the most of any number of labelled rows
