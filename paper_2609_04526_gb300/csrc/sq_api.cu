@@ -485,9 +485,9 @@ sq_status run_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint
   SQ_TRY(make_act_map(h, &m.rows, a.rows, D, whole, 64, a.box_rows));
   SQ_TRY(make_act_map(h, &m.weights, W, D, V, 64, 128));
   SQ_TRY(make_act_map(h, &m.weights_narrow, W, D, V, 64, 32));
-  m.weights_short = m.e_store = m.e_load = m.partial = m.rows;
+  SQ_TRY(make_act_map(h, &m.weights_short, W, D, V, 64, 64));
+  m.e_store = m.e_load = m.partial = m.rows;
   if (dX) {
-    SQ_TRY(make_act_map(h, &m.weights_short, W, D, V, 64, 64));
     SQ_TRY(make_map(h, &m.e_store, a.e, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, V, chunk, 32, 32,
                     CU_TENSOR_MAP_SWIZZLE_64B, a.pitch));
     SQ_TRY(make_map(h, &m.e_load, a.e, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, V, chunk, 64, a.box_rows,

@@ -792,19 +792,30 @@ cudaError_t launch_head_chunk(const HeadArgs &a, const HeadMaps &m, int first, i
   const int64_t tiles_m = (rows + kHeadTile - 1) / kHeadTile;
   // Few tokens are bound by the weights' way from memory: stages of 128, whose rows are read 256 bytes
   // at a time. More are bound by the MMAs: stages of 64, of which five wait behind the one in work
-  // (2048 against 38912 x 2048 in 163 us, 175 with 128). Up to 256 tokens whose tiles of 256 columns
-  // would reach every other cluster at most take tiles of 64 (8 tokens against 3211 x 2312, loss and
-  // gradient: 26.6 us, 32.7 with 256; 1000 tokens against 2000 x 4096 were 2 % slower).
+  // (2048 against 38912 x 2048 in 163 us, 175 with 128).
   const bool few = a.box_rows < 128;
-  const int64_t wide = tiles_m * ((a.V + 255) / 256);
+  const int64_t clusters = sm_count / 2;
+  auto tiles = [&](int64_t columns) { return tiles_m * ((a.V + columns - 1) / columns); };
+  // Narrower tiles where one row of them leaves clusters idle: by the waves, a tile of 128 columns
+  // lasting 0.54 and one of 64 lasting 0.4 of one of 256 (8 tokens against 3211 x 2312, loss and
+  // gradient: 32.7 us with 256, 26.6 with 64; 32 against 64000 x 2048: 57.7, 51.3 with 128). Where
+  // the MMAs bound the launch, only if it is one wave (200 tokens against 64000 x 2048: 61.3, 64.7).
+  auto waves = [&](int64_t columns) { return static_cast<double>((tiles(columns) + clusters - 1) / clusters); };
+  int narrow = 256;
+  if (tiles_m == 1 && (few || waves(256) == 1)) {
+    double best = waves(256);
+    if (0.54 * waves(128) < best) best = 0.54 * waves(128), narrow = 128;
+    if (0.4 * waves(64) < best) narrow = 64;
+  }
   cudaError_t e;
-  if (tiles_m == 1 && 4 * wide <= sm_count)
-    e = launch_head_product<false, 128, 64>(m.rows, m.weights_narrow, m.e_store, a, first, tiles_m * ((a.V + 63) / 64),
-                                            sm_count, stream);
+  if (narrow == 64)
+    e = launch_head_product<false, 128, 64>(m.rows, m.weights_narrow, m.e_store, a, first, tiles(64), sm_count, stream);
+  else if (narrow == 128)
+    e = launch_head_product<false, 128, 128>(m.rows, m.weights_short, m.e_store, a, first, tiles(128), sm_count, stream);
   else if (few)
-    e = launch_head_product<false, 128, 256>(m.rows, m.weights, m.e_store, a, first, wide, sm_count, stream);
+    e = launch_head_product<false, 128, 256>(m.rows, m.weights, m.e_store, a, first, tiles(256), sm_count, stream);
   else
-    e = launch_head_product<false, 64, 256>(m.rows, m.weights, m.e_store, a, first, wide, sm_count, stream);
+    e = launch_head_product<false, 64, 256>(m.rows, m.weights, m.e_store, a, first, tiles(256), sm_count, stream);
   if (e != cudaSuccess) return e;
   if (rows <= 4 * sm_count)
     e = launch_after(sq_head_finalize_kernel<4>, (rows + 3) / 4, 1024, 0, stream, a, first);
