@@ -55,9 +55,9 @@ struct HeadCfg {
   static constexpr int kBoxBytes = 32 * 32 * (GRAD ? 4 : 2);  // 32 rows x 32 columns of a warp
   // Stages added up in one accumulator. The tensor core truncates its running fp32 sum at every
   // step of 16, a bias that grows with the length: a sum of 4096 products in one accumulator left
-  // the log-sum-exp 1.4e-5 too small. The logits therefore leave tensor memory every 1024 products
+  // the log-sum-exp 1.4e-5 too small. The logits therefore leave tensor memory every 512 products
   // and are added in registers; the gradient, rounded to bf16 in the end, runs through.
-  static constexpr int kSegment = GRAD ? 1 << 30 : 1024 / kBK;
+  static constexpr int kSegment = GRAD ? 1 << 30 : 512 / kBK;
   static constexpr int kOffBar = kOffBox + kEpiWarps * kBoxBytes;
   static constexpr int kSmemBytes = kOffBar + 512 + 1024;
 };
