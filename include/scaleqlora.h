@@ -523,9 +523,10 @@ sq_status sq_combine_grad(sq_handle h, int64_t T, int32_t k, int64_t D, int64_t 
  * no gradient; D % 8 == 0, D <= 65536, 1 <= V <= 2^24. labels device int64 [T]; a label outside
  * [0, V) (such as -100) marks a token that is not a target: its row is not read into any result,
  * its loss and lse are 0 and its dX row is zero. loss, lse device fp32 [T] or NULL (overwritten).
- * Results do not differ from run to run. Uses scratch of the handle, its size bounded for any T:
- * the packed rows of up to 16,384 tokens, and with the gradient up to 512 MiB of bf16 exponentials
- * and the fp32 partial planes of that chunk. */
+ * Results do not differ from run to run, and the loss and lse of a token not with the tokens beside
+ * it. Uses scratch of the handle, its size bounded for any T: the packed rows of up to 16,384 tokens
+ * and up to 512 MiB of sums, or, with the gradient, of bf16 exponentials, and the fp32 partial planes
+ * of that chunk. */
 sq_status sq_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint16_t *X, const uint16_t *W,
                        const int64_t *labels, float *loss, float *lse, void *stream);
 

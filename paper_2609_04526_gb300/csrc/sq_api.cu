@@ -449,10 +449,13 @@ sq_status run_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint
   a.chunk = static_cast<int>(chunk);
   a.sum_rows = static_cast<int>(up(std::min(piece, chunk), 4));
   a.box_rows = T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128;
+  a.few = a.box_rows < 128;
+  const int clusters = std::max(1, dev->sm_count / 2);
+  a.columns = sqi::head_columns(T, V, a.few, clusters);
   int64_t partial_rows = 0;  // of 4 * D bytes: the most that any number of labelled rows takes
   for (int64_t m = 1; dX && m <= chunk / sqi::kHeadTile; ++m) {
     const int parts = sqi::head_parts(std::min(m * sqi::kHeadTile, piece), D, static_cast<int>((V + 127) / 128),
-                                      std::max(1, dev->sm_count / 2));
+                                      clusters);
     a.parts[m - 1] = static_cast<uint8_t>(parts - 1);
     partial_rows = std::max(partial_rows, m * sqi::kHeadTile * parts);
   }
@@ -463,8 +466,8 @@ sq_status run_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint
     return at;
   };
   const size_t o_count = take(4), o_token = take(4 * piece), o_label = take(4 * piece), o_z = take(4 * piece),
-               o_factors = take(8 * piece), o_rows = take(2 * D * whole), o_sums = take(4 * quarters * chunk), o_refs = take(4 * quarters * chunk),
-               o_moved = take(4 * chunk),
+               o_factors = take(8 * piece), o_rows = take(2 * D * whole), o_sums = take(4 * quarters * chunk),
+               o_refs = take(4 * quarters * chunk), o_moved = take(4 * chunk),
                o_e = take(dX ? 2 * a.pitch * chunk : 0), o_partial = take(4 * D * partial_rows);
   SQ_TRY(ensure_scratch(h, dev->head, used, stream, "the head loss"));
   uint8_t *base = static_cast<uint8_t *>(dev->head.ptr);
@@ -483,11 +486,10 @@ sq_status run_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint
   }
   sqi::HeadMaps m;
   SQ_TRY(make_act_map(h, &m.rows, a.rows, D, whole, 64, a.box_rows));
-  SQ_TRY(make_act_map(h, &m.weights, W, D, V, 64, 128));
-  SQ_TRY(make_act_map(h, &m.weights_narrow, W, D, V, 64, 32));
-  SQ_TRY(make_act_map(h, &m.weights_short, W, D, V, 64, 64));
-  m.e_store = m.e_load = m.partial = m.rows;
+  SQ_TRY(make_act_map(h, &m.weights, W, D, V, 64, a.columns / 2));
+  m.weights_grad = m.e_store = m.e_load = m.partial = m.rows;
   if (dX) {
+    SQ_TRY(make_act_map(h, &m.weights_grad, W, D, V, 64, a.few ? 128 : 64));
     SQ_TRY(make_map(h, &m.e_store, a.e, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, V, chunk, 32, 32,
                     CU_TENSOR_MAP_SWIZZLE_64B, a.pitch));
     SQ_TRY(make_map(h, &m.e_load, a.e, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, V, chunk, 64, a.box_rows,

@@ -408,6 +408,21 @@ inline int head_parts(int64_t rows, int64_t D, int stages, int clusters) {
   return best;
 }
 
+// Columns of a tile of the logits: 256, or fewer where the call is one row of tiles and they would
+// leave clusters idle, by the waves of the launch, a tile of 128 columns lasting 0.54 and one of 64
+// lasting 0.4 of one of 256 (8 tokens against 3211 x 2312, loss and gradient: 32.7 us with 256, 26.6
+// with 64; 32 against 64000 x 2048: 57.7, 51.3 with 128). Where the MMAs bound the launch, only if
+// it is one wave (200 tokens against 64000 x 2048: 61.3, 64.7).
+inline int head_columns(int64_t T, int64_t V, bool few, int clusters) {
+  auto waves = [&](int64_t columns) {
+    return static_cast<double>(((V + columns - 1) / columns + clusters - 1) / clusters);
+  };
+  if (T > kHeadTile || (!few && waves(256) > 1)) return 256;
+  const double wide = waves(256), half = 0.54 * waves(128), quarter = 0.4 * waves(64);
+  if (quarter < wide && quarter < half) return 64;
+  return half < wide ? 128 : 256;
+}
+
 struct HeadArgs {
   int T;                  // tokens of the piece
   int64_t D, V;
@@ -418,6 +433,8 @@ struct HeadArgs {
   float *loss, *lse;      // [T] or null
   uint16_t *dX;           // [T, D] bf16, or null: no gradient
   int box_rows;           // rows of A in a shared-memory stage: 16, 32, 64 or 128, all that few tokens have
+  bool few;               // box_rows < 128: stages of 128 instead of 64
+  int columns;            // of a tile of the logits
   int chunk;              // rows of a chunk, a multiple of kHeadTile
   uint8_t parts[kHeadPiece / kHeadTile];  // vocabulary parts of the gradient by row tiles of the chunk, less 1
   int64_t pitch;          // elements of a row of e
@@ -435,10 +452,10 @@ struct HeadArgs {
   float *partial;         // [parts, rows, D] fp32 (gradient)
   int *err;
 };
-// weights: 64 x 128 boxes, weights_short 64 x 64, weights_narrow 64 x 32, rows and e_load 64 x box_rows, partial 32 x 32 fp32,
-// all with the 128-byte swizzle; e_store 32 x 32, 64-byte swizzle.
+// rows and e_load: 64 x box_rows boxes, weights 64 x columns / 2, weights_grad 64 x 128 (few) or 64 x
+// 64, partial 32 x 32 fp32, all with the 128-byte swizzle; e_store 32 x 32, 64-byte swizzle.
 struct HeadMaps {
-  CUtensorMap rows, weights, weights_short, weights_narrow, e_store, e_load, partial;
+  CUtensorMap rows, weights, weights_grad, e_store, e_load, partial;
 };
 cudaError_t launch_head_gather(const HeadArgs &a, cudaStream_t stream);
 cudaError_t launch_head_chunk(const HeadArgs &a, const HeadMaps &m, int first, int sm_count, cudaStream_t stream);

@@ -22,7 +22,8 @@
 // The label's own term is left out of e and of the sums and carried in fp32: p_label - 1 is
 // -(S - e_l) / S without cancellation, so confident tokens keep an accurate loss and gradient.
 // e is rounded to bf16 once, as an operand of the tensor cores (at most 2^-8 of a term; errors of
-// one sign and the other, so their sum stays below the rounding of the bf16 gradient); the sums S take the unrounded values.
+// one sign and the other, so their sum stays below the rounding of the bf16 gradient); the sums S
+// take the unrounded values.
 #include "sq_gemm_kernels.cuh"
 #include "sq_launch.cuh"
 
@@ -61,6 +62,9 @@ struct HeadCfg {
   static constexpr int kOffBar = kOffBox + kEpiWarps * kBoxBytes;
   static constexpr int kSmemBytes = kOffBar + 512 + 1024;
 };
+// The last stage's A, read to 128 rows of its second 64-wide chunk, ends within the shared memory (the
+// smallest tiles: 12 stages of 16 KiB).
+static_assert(11 * 16384 + 4096 + 16384 <= HeadCfg<false, 128, 64>::kOffBar, "operand rows past the shared memory");
 static_assert(HeadCfg<false, 64, 256>::kSmemBytes <= 232448 && HeadCfg<true, 64, 256>::kSmemBytes <= 232448,
               "head kernel exceeds the opt-in shared memory of one CTA");
 
@@ -296,7 +300,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK, NT
                    const __grid_constant__ CUtensorMap tmO, const HeadArgs a, const int first) {
   using C = HeadCfg<GRAD, BK, NT>;
   // A stage holds box_rows rows of A; the MMAs read 128 all the same, the rest of them whatever
-  // lies behind in the ring, and nothing reads those rows of the product. Few tokens so leave the
+  // lies behind in the ring and the store boxes, and nothing reads those rows of the product. Few tokens so leave the
   // ring to the columns, which are all their traffic (one token against 128256 x 4096: 181 us with
   // 96 KiB of columns in flight, 170 with 128). Without a gradient the store boxes' room is part of
   // the ring.
@@ -405,7 +409,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK, NT
         for (int k0 = 0; k0 < steps_all && ok; k0 += C::kSegment, ++tc) {
           const int ab = tc & 1;
           const uint32_t au = static_cast<uint32_t>(tc >> 1);
-          if (tc >= 2 && !(ok = __all_sync(0xFFFFFFFFu, mbar_spin_cluster(&tempty[ab], (au & 1u) ^ 1u, abort_flag, a.err)))) break;
+          if (tc >= 2 &&
+              !(ok = __all_sync(0xFFFFFFFFu, mbar_spin_cluster(&tempty[ab], (au & 1u) ^ 1u, abort_flag, a.err))))
+            break;
           tc_fence_after();
           const uint32_t d_tmem = tmem_base + ab * kTmemCols;
           const int steps = min(C::kSegment, steps_all - k0);
@@ -472,7 +478,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK, NT
       const int col0 = t.tn * NT + C::kEpiCols * share;
       if constexpr (GRAD) {
         const int ab = tc & 1;
-        if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&tfull[ab], static_cast<uint32_t>(tc >> 1) & 1u, abort_flag, a.err)))) break;
+        ok = __all_sync(0xFFFFFFFFu, mbar_wait(&tfull[ab], static_cast<uint32_t>(tc >> 1) & 1u, abort_flag, a.err));
+        if (!ok) break;
         tc_fence_after();
         const uint32_t t_buf = t_row + ab * kTmemCols;
         const int32_t out_row = t.part * tiles_m * C::kRows + row32;
@@ -504,7 +511,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK, NT
         static_assert(C::kEpiCols == 64, "two 32-column loads");
         for (int k0 = 0; k0 < stages; k0 += C::kSegment, ++tc) {
           const int ab = tc & 1;
-          if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&tfull[ab], static_cast<uint32_t>(tc >> 1) & 1u, abort_flag, a.err)))) break;
+          ok = __all_sync(0xFFFFFFFFu, mbar_wait(&tfull[ab], static_cast<uint32_t>(tc >> 1) & 1u, abort_flag, a.err));
+          if (!ok) break;
           tc_fence_after();
           if (k0 == 0) {
             tmem_ld32(t_row + ab * kTmemCols, z[0]);
@@ -793,29 +801,12 @@ cudaError_t launch_head_chunk(const HeadArgs &a, const HeadMaps &m, int first, i
   // Few tokens are bound by the weights' way from memory: stages of 128, whose rows are read 256 bytes
   // at a time. More are bound by the MMAs: stages of 64, of which five wait behind the one in work
   // (2048 against 38912 x 2048 in 163 us, 175 with 128).
-  const bool few = a.box_rows < 128;
-  const int64_t clusters = sm_count / 2;
-  auto tiles = [&](int64_t columns) { return tiles_m * ((a.V + columns - 1) / columns); };
-  // Narrower tiles where one row of them leaves clusters idle: by the waves, a tile of 128 columns
-  // lasting 0.54 and one of 64 lasting 0.4 of one of 256 (8 tokens against 3211 x 2312, loss and
-  // gradient: 32.7 us with 256, 26.6 with 64; 32 against 64000 x 2048: 57.7, 51.3 with 128). Where
-  // the MMAs bound the launch, only if it is one wave (200 tokens against 64000 x 2048: 61.3, 64.7).
-  auto waves = [&](int64_t columns) { return static_cast<double>((tiles(columns) + clusters - 1) / clusters); };
-  int narrow = 256;
-  if (tiles_m == 1 && (few || waves(256) == 1)) {
-    double best = waves(256);
-    if (0.54 * waves(128) < best) best = 0.54 * waves(128), narrow = 128;
-    if (0.4 * waves(64) < best) narrow = 64;
-  }
-  cudaError_t e;
-  if (narrow == 64)
-    e = launch_head_product<false, 128, 64>(m.rows, m.weights_narrow, m.e_store, a, first, tiles(64), sm_count, stream);
-  else if (narrow == 128)
-    e = launch_head_product<false, 128, 128>(m.rows, m.weights_short, m.e_store, a, first, tiles(128), sm_count, stream);
-  else if (few)
-    e = launch_head_product<false, 128, 256>(m.rows, m.weights, m.e_store, a, first, tiles(256), sm_count, stream);
-  else
-    e = launch_head_product<false, 64, 256>(m.rows, m.weights, m.e_store, a, first, tiles(256), sm_count, stream);
+  const auto logits = a.columns == 64    ? launch_head_product<false, 128, 64>
+                      : a.columns == 128 ? launch_head_product<false, 128, 128>
+                      : a.few            ? launch_head_product<false, 128, 256>
+                                         : launch_head_product<false, 64, 256>;
+  cudaError_t e = logits(m.rows, m.weights, m.e_store, a, first, tiles_m * ((a.V + a.columns - 1) / a.columns), sm_count,
+                         stream);
   if (e != cudaSuccess) return e;
   if (rows <= 4 * sm_count)
     e = launch_after(sq_head_finalize_kernel<4>, (rows + 3) / 4, 1024, 0, stream, a, first);
@@ -828,10 +819,8 @@ cudaError_t launch_head_chunk(const HeadArgs &a, const HeadMaps &m, int first, i
     units = std::max(units, t * tiles_d * (a.parts[t - 1] + 1));
     parts = std::max<int64_t>(parts, a.parts[t - 1] + 1);
   }
-  const auto gradient = few ? launch_head_product<true, 128, 256> : launch_head_product<true, 64, 256>;
-  if ((e = gradient(m.e_load, few ? m.weights : m.weights_short, m.partial, a, first, units, sm_count, stream)) !=
-      cudaSuccess)
-    return e;
+  const auto gradient = a.few ? launch_head_product<true, 128, 256> : launch_head_product<true, 64, 256>;
+  if ((e = gradient(m.e_load, m.weights_grad, m.partial, a, first, units, sm_count, stream)) != cudaSuccess) return e;
   const int64_t pieces = rows * ((a.D + 255) / 256);
   if (parts >= 8 && pieces <= 16 * static_cast<int64_t>(sm_count))  // too few warps for loads one after the other
     return launch_after(sq_head_rows_kernel<8>, static_cast<unsigned>(pieces), 256, 0, stream, a, first);
