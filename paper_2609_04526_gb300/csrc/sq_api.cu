@@ -439,7 +439,9 @@ sq_status run_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint
   a.D = D;
   a.V = V;
   a.W = W;
-  a.pitch = up(V, 8);  // rows of e start on 16 bytes
+  // rows of scratch start on 128-byte lines: half the requests of boxes that start between them
+  a.pitch = up(V, 64);
+  a.width = up(D, 64);
   a.err = dev->err_word;
   const int64_t quarters = 4 * ((V + sqi::kHeadTile - 1) / sqi::kHeadTile);
   // rows whose exponentials or, without a gradient, sums and references fit the bound
@@ -466,9 +468,9 @@ sq_status run_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint
     return at;
   };
   const size_t o_count = take(4), o_token = take(4 * piece), o_label = take(4 * piece), o_z = take(4 * piece),
-               o_factors = take(8 * piece), o_rows = take(2 * D * whole), o_sums = take(4 * quarters * chunk),
+               o_factors = take(8 * piece), o_rows = take(2 * a.width * whole), o_sums = take(4 * quarters * chunk),
                o_refs = take(4 * quarters * chunk), o_moved = take(4 * chunk),
-               o_e = take(dX ? 2 * a.pitch * chunk : 0), o_partial = take(4 * D * partial_rows);
+               o_e = take(dX ? 2 * a.pitch * chunk : 0), o_partial = take(4 * a.width * partial_rows);
   SQ_TRY(ensure_scratch(h, dev->head, used, stream, "the head loss"));
   uint8_t *base = static_cast<uint8_t *>(dev->head.ptr);
   a.count = reinterpret_cast<int *>(base + o_count);
@@ -485,7 +487,8 @@ sq_status run_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint
     a.partial = reinterpret_cast<float *>(base + o_partial);
   }
   sqi::HeadMaps m;
-  SQ_TRY(make_act_map(h, &m.rows, a.rows, D, whole, 64, a.box_rows));
+  SQ_TRY(make_map(h, &m.rows, a.rows, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, D, whole, 64, a.box_rows,
+                  CU_TENSOR_MAP_SWIZZLE_128B, a.width));
   SQ_TRY(make_act_map(h, &m.weights, W, D, V, 64, a.columns / 2));
   m.weights_grad = m.e_store = m.e_load = m.partial = m.rows;
   if (dX) {
@@ -495,7 +498,7 @@ sq_status run_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint
     SQ_TRY(make_map(h, &m.e_load, a.e, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, V, chunk, 64, a.box_rows,
                     CU_TENSOR_MAP_SWIZZLE_128B, a.pitch));
     SQ_TRY(make_map(h, &m.partial, a.partial, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, D, partial_rows, 32, 32,
-                    CU_TENSOR_MAP_SWIZZLE_128B));
+                    CU_TENSOR_MAP_SWIZZLE_128B, a.width));
   }
   for (int64_t t = 0; t < T; t += piece) {
     a.T = static_cast<int>(std::min(piece, T - t));

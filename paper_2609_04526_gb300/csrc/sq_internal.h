@@ -437,7 +437,8 @@ struct HeadArgs {
   int columns;            // of a tile of the logits
   int chunk;              // rows of a chunk, a multiple of kHeadTile
   uint8_t parts[kHeadPiece / kHeadTile];  // vocabulary parts of the gradient by row tiles of the chunk, less 1
-  int64_t pitch;          // elements of a row of e
+  int64_t pitch;          // elements from row to row of e
+  int64_t width;          // and of the packed rows and partial planes
   // scratch, by compact row of the piece
   int *count;             // labelled tokens of the piece
   int *token, *label;

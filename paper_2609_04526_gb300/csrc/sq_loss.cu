@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(256) sq_head_gather_kernel(const HeadArgs a) {
     y = a.labels[t];
     const uint4 *x = reinterpret_cast<const uint4 *>(a.X + static_cast<int64_t>(t) * a.D);
     const uint4 *w = reinterpret_cast<const uint4 *>(a.W + y * a.D);
-    uint4 *out = reinterpret_cast<uint4 *>(a.rows + static_cast<int64_t>(row) * a.D);
+    uint4 *out = reinterpret_cast<uint4 *>(a.rows + static_cast<int64_t>(row) * a.width);
     // eight sums of every 256th 16 bytes, a warp's or, of one warp, each lane's own: one order for both
     float sums[kTokens] = {};
     constexpr int kFlight = kTokens < 4 ? kTokens : 4;  // 16-byte loads of each row in flight
@@ -717,7 +717,7 @@ __global__ void __launch_bounds__(256) sq_head_rows_kernel(const HeadArgs a, con
   if (SHARE == 1 && c >= a.D) return;
   const int tiles_m = (rows + kHeadTile - 1) / kHeadTile;
   const int parts = a.parts[tiles_m - 1] + 1;
-  const int64_t plane = static_cast<int64_t>(tiles_m) * kHeadTile * a.D;
+  const int64_t plane = static_cast<int64_t>(tiles_m) * kHeadTile * a.width;
   const int row = first + r;
   const float2 f = a.factors[row];
   const int64_t label = a.label[row], token = a.token[row];
@@ -725,7 +725,7 @@ __global__ void __launch_bounds__(256) sq_head_rows_kernel(const HeadArgs a, con
   if (c < a.D && warp % SHARE == 0) w = __ldg(reinterpret_cast<const uint4 *>(a.W + label * a.D + c));
   float s[8] = {};
   if (c < a.D) {
-    const float *p = a.partial + static_cast<int64_t>(r) * a.D + c + warp % SHARE * plane;
+    const float *p = a.partial + static_cast<int64_t>(r) * a.width + c + warp % SHARE * plane;
 #pragma unroll 4
     for (int i = warp % SHARE; i < parts; i += SHARE, p += SHARE * plane) {
       const float4 u = __ldcs(reinterpret_cast<const float4 *>(p)), v = __ldcs(reinterpret_cast<const float4 *>(p) + 1);
