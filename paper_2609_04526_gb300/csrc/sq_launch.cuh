@@ -8,6 +8,10 @@
 // kernel runs beside the ones that wait. (The one exception reads early what is older still: the
 // second launch of the sort by expert counts its slots before its wait; its count launch, having
 // passed its own wait, shows that the slots are complete.)
+//
+// Such a kernel reads memory with ordinary loads alone: the non-coherent ones (__ldg, or a const
+// __restrict__ pointer) are for what nobody writes while the kernel runs, and may be moved ahead of
+// the wait.
 #pragma once
 #include <cuda_runtime.h>
 

@@ -199,8 +199,8 @@ __global__ void __launch_bounds__(256) sq_head_gather_kernel(const HeadArgs a) {
           const int i = i0 + 32 * (c0 + c);
           p[c] = q[c] = make_uint4(0, 0, 0, 0);
           if (i < pieces) {
-            p[c] = __ldg(x + i);
-            q[c] = __ldg(w + i);
+            p[c] = x[i];
+            q[c] = w[i];
           }
         }
 #pragma unroll
@@ -727,13 +727,13 @@ __global__ void __launch_bounds__(256) sq_head_rows_kernel(const HeadArgs a, con
   const float2 f = a.factors[row];
   const int64_t label = a.label[row], token = a.token[row];
   uint4 w = make_uint4(0, 0, 0, 0);
-  if (c < a.D && warp % SHARE == 0) w = __ldg(reinterpret_cast<const uint4 *>(a.W + label * a.D + c));
+  if (c < a.D && warp % SHARE == 0) w = *reinterpret_cast<const uint4 *>(a.W + label * a.D + c);
   float s[8] = {};
   if (c < a.D) {
     const float *p = a.partial + static_cast<int64_t>(r) * a.width + c + warp % SHARE * plane;
 #pragma unroll 4
     for (int i = warp % SHARE; i < parts; i += SHARE, p += SHARE * plane) {
-      const float4 u = __ldcs(reinterpret_cast<const float4 *>(p)), v = __ldcs(reinterpret_cast<const float4 *>(p) + 1);
+      const float4 u = reinterpret_cast<const float4 *>(p)[0], v = reinterpret_cast<const float4 *>(p)[1];
       s[0] += u.x, s[1] += u.y, s[2] += u.z, s[3] += u.w;
       s[4] += v.x, s[5] += v.y, s[6] += v.z, s[7] += v.w;
     }

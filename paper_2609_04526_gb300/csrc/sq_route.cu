@@ -29,14 +29,14 @@ constexpr uint32_t kAll = 0xFFFFFFFFu;
 // A logit as it is ranked; -inf, and so NaN, is never chosen.
 __device__ __forceinline__ float rank_value(float z) { return fminf(fmaxf(z, -INFINITY), FLT_MAX); }
 
-__device__ __forceinline__ float load_logit(const float *p) { return __ldg(p); }
+__device__ __forceinline__ float load_logit(const float *p) { return *p; }
 __device__ __forceinline__ float load_logit(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
 __device__ __forceinline__ void load_logits4(const float *p, float *v) {
-  const float4 q = __ldg(reinterpret_cast<const float4 *>(p));
+  const float4 q = *reinterpret_cast<const float4 *>(p);
   v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
 }
 __device__ __forceinline__ void load_logits4(const __nv_bfloat16 *p, float *v) {
-  const uint2 q = __ldg(reinterpret_cast<const uint2 *>(p));
+  const uint2 q = *reinterpret_cast<const uint2 *>(p);
   v[0] = __uint_as_float(q.x << 16), v[1] = __uint_as_float(q.x & 0xFFFF0000u);
   v[2] = __uint_as_float(q.y << 16), v[3] = __uint_as_float(q.y & 0xFFFF0000u);
 }
@@ -101,7 +101,7 @@ __device__ __forceinline__ void load_row(const T *row, int E, int lane, bool on,
 // k <= LANES: lane j of a token keeps its slot j.
 template <int LANES, bool WIDE, int PER, typename T>
 __global__ void __launch_bounds__(256)
-    sq_route_kernel(int64_t tokens, int E, int k, const T *__restrict__ logits, const uint8_t *__restrict__ valid,
+    sq_route_kernel(int64_t tokens, int E, int k, const T *logits, const uint8_t *valid,
                     bool normalize, int *__restrict__ experts, float *__restrict__ weights) {
   constexpr int kGroups = PER / 4;
   dependency_wait();
@@ -194,8 +194,8 @@ __global__ void __launch_bounds__(256)
 // from the logits: keeping it would cost a write and the same read.
 template <int LANES, bool WIDE, int PER, typename T>
 __global__ void __launch_bounds__(256)
-    sq_route_grad_kernel(int64_t tokens, int E, int k, const T *__restrict__ logits, const int *__restrict__ experts,
-                         const float *__restrict__ dweights, bool normalize, T *__restrict__ dlogits) {
+    sq_route_grad_kernel(int64_t tokens, int E, int k, const T *logits, const int *experts,
+                         const float *dweights, bool normalize, T *__restrict__ dlogits) {
   dependency_wait();
   dependency_start();
   const int lane = threadIdx.x % LANES;
@@ -267,7 +267,7 @@ __device__ __forceinline__ void load_slots(const int *experts, int64_t at, int64
 #pragma unroll
   for (int s = 0; s < kSortStep; ++s) {
     const int64_t i = at + 32 * s + lane;
-    e[s] = i < end ? __ldg(experts + i) : -1;
+    e[s] = i < end ? experts[i] : -1;
     if (e[s] >= E) e[s] = -1;
   }
 }
@@ -284,7 +284,7 @@ __device__ __forceinline__ uint32_t same_expert(int e, int bits) {
 }
 
 __global__ void __launch_bounds__(kSortThreads)
-    sq_sort_count_kernel(int64_t n, int E, int64_t per, const int *__restrict__ experts, int *__restrict__ counts) {
+    sq_sort_count_kernel(int64_t n, int E, int64_t per, const int *experts, int *__restrict__ counts) {
   extern __shared__ int sort_smem[];
   dependency_wait();
   dependency_start();
@@ -305,7 +305,7 @@ __global__ void __launch_bounds__(kSortThreads)
 
 // counts: [gridDim.x, E] of the launch before, or null for the one CTA that takes all slots.
 __global__ void __launch_bounds__(1024)
-    sq_sort_kernel(int64_t n, int E, int64_t per, const int *__restrict__ experts, const int *__restrict__ counts,
+    sq_sort_kernel(int64_t n, int E, int64_t per, const int *experts, const int *counts,
                    int64_t *__restrict__ offsets, int *__restrict__ row_of, int *__restrict__ slot_of) {
   extern __shared__ int sort_smem[];
   const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -345,7 +345,7 @@ __global__ void __launch_bounds__(1024)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int b = b0 + i * groups;
-          c[i] = b < gridDim.x ? __ldcg(counts + b * E + e) : 0;
+          c[i] = b < gridDim.x ? counts[b * E + e] : 0;
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -426,8 +426,26 @@ __global__ void __launch_bounds__(1024)
 // bf16 rows of D elements, moved 8 (16 bytes) per lane. A row index outside [0, rows) marks a
 // slot that no expert serves.
 
-__device__ __forceinline__ uint4 load_row16(const uint16_t *p) {
-  return __ldg(reinterpret_cast<const uint4 *>(p));
+// 16 bytes, or zeros where not `on`. Loads of several rows are issued one after the other in both
+// forms; with a branch around each the backward pass of 2677 tokens of width 1496 from 4 experts
+// took 29.1 us, 24.7 without. load_or_first reads the tensor's first elements instead, in fewer
+// registers: the sum of eight rows stays below 64 (2048 tokens of width 2048: 15.2 us, 16.4 with
+// predicates; of one row, 32768 of width 4096, 82.3 and 80.7).
+__device__ __forceinline__ uint4 load_row16(const uint16_t *p, bool on) {
+  uint4 v;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "mov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
+      "@p ld.global.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
+      : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w)
+      : "l"(p), "r"(static_cast<int>(on))
+      : "memory");
+  return v;
+}
+__device__ __forceinline__ uint4 load_or_first(const uint16_t *p, int64_t at, bool on) {
+  const uint4 v = *reinterpret_cast<const uint4 *>(p + (on ? at : 0));
+  return make_uint4(on ? v.x : 0, on ? v.y : 0, on ? v.z : 0, on ? v.w : 0);
 }
 __device__ __forceinline__ void store_row16(uint16_t *p, const uint4 &v) { *reinterpret_cast<uint4 *>(p) = v; }
 __device__ __forceinline__ void unpack8(const uint4 &q, float (&v)[8]) {
@@ -454,8 +472,8 @@ constexpr int kMoveCols = 32 * 8 * kMoveVecs;
 // Xs[row_of[t, j]] = X[t]; rows whose slot_of is negative are zero. A warp takes kMoveCols
 // columns of one token, read once and written k times.
 __global__ void __launch_bounds__(256)
-    sq_dispatch_kernel(uint32_t units, uint32_t pieces, int k, int64_t D, int64_t rows, const uint16_t *__restrict__ X,
-                       const int *__restrict__ row_of, const int *__restrict__ slot_of, uint16_t *__restrict__ Xs) {
+    sq_dispatch_kernel(uint32_t units, uint32_t pieces, int k, int64_t D, int64_t rows, const uint16_t *X,
+                       const int *row_of, const int *slot_of, uint16_t *__restrict__ Xs) {
   const int lane = threadIdx.x & 31;
   const uint32_t unit = blockIdx.x * 8 + (threadIdx.x >> 5);
   dependency_wait();
@@ -475,7 +493,7 @@ __global__ void __launch_bounds__(256)
   const bool read = __any_sync(kAll, row >= 0);
 #pragma unroll
   for (int i = 0; i < kMoveVecs; ++i)
-    if (read && c0 + 256 * i < D) v[i] = load_row16(X + t * D + c0 + 256 * i);
+    v[i] = load_row16(X + t * D + c0 + 256 * i, read && c0 + 256 * i < D);
   for (int j = 0; j < k; ++j) {
     const int64_t to = __shfl_sync(kAll, row, j);
     if (to < 0) continue;
@@ -492,14 +510,16 @@ __global__ void __launch_bounds__(256)
 }
 
 // Rows that a warp has in flight (ROWS of the token's k) and 256-column pieces of each (COLS): 8
-// loads of 16 bytes a lane where k > 4, 4 or 8 below. With the rows of one piece alone, k = 1 left
-// one load in flight (17182 tokens of width 1544, backward: 92 us).
-template <typename F>
+// loads of 16 bytes a lane where k > 4, 4 below. With the rows of one piece alone, k = 1 left one
+// load in flight (17182 tokens of width 1544, backward: 92 us instead of 47). The gradient, whose
+// stores keep the next piece's loads back, takes two pieces of four rows (8192 tokens of width 2880:
+// 68 us, 73 with one).
+template <bool GRAD, typename F>
 cudaError_t with_flight(int k, F f) {
   using std::integral_constant;
   if (k == 1) return f(integral_constant<int, 1>{}, integral_constant<int, 4>{});
   if (k == 2) return f(integral_constant<int, 2>{}, integral_constant<int, 2>{});
-  if (k <= 4) return f(integral_constant<int, 4>{}, integral_constant<int, 1>{});
+  if (k <= 4) return f(integral_constant<int, 4>{}, integral_constant<int, GRAD ? 2 : 1>{});
   return f(integral_constant<int, 8>{}, integral_constant<int, 1>{});
 }
 
@@ -509,8 +529,8 @@ cudaError_t with_flight(int k, F f) {
 // registers and 16 warps a 2880-wide batch of 1999 tokens took 19 us instead of 12).
 template <int ROWS, int COLS>
 __global__ void __launch_bounds__(256, 4)
-    sq_combine_kernel(int64_t tokens, int k, int D, int rows, int share, const uint16_t *__restrict__ Ys,
-                      const int *__restrict__ row_of, const float *__restrict__ weights, uint16_t *__restrict__ Y) {
+    sq_combine_kernel(int64_t tokens, int k, int D, int rows, int share, const uint16_t *Ys,
+                      const int *row_of, const float *weights, uint16_t *__restrict__ Y) {
   dependency_wait();
   dependency_start();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -533,8 +553,9 @@ __global__ void __launch_bounds__(256, 4)
         const int at = __shfl_sync(kAll, row, j0 + i);
 #pragma unroll
         for (int q = 0; q < COLS; ++q) {
-          v[i][q] = make_uint4(0, 0, 0, 0);
-          if (at >= 0 && c + 256 * q < D) v[i][q] = load_row16(Ys + static_cast<int64_t>(at) * D + (c + 256 * q));
+          const int64_t from = static_cast<int64_t>(at) * D + (c + 256 * q);
+          const bool on = at >= 0 && c + 256 * q < D;
+          v[i][q] = ROWS > 1 ? load_or_first(Ys, from, on) : load_row16(Ys + from, on);
         }
       }
 #pragma unroll
@@ -560,9 +581,9 @@ __global__ void __launch_bounds__(256, 4)
 // Bound by memory: 32768 tokens of width 2048 to 8 experts move 2.2 GB in 328 us.
 template <int ROWS, int COLS>
 __global__ void __launch_bounds__(256)
-    sq_combine_grad_kernel(int64_t tokens, int k, int D, int rows, int share, const uint16_t *__restrict__ dY,
-                           const uint16_t *__restrict__ Ys, const int *__restrict__ row_of,
-                           const int *__restrict__ slot_of, const float *__restrict__ weights,
+    sq_combine_grad_kernel(int64_t tokens, int k, int D, int rows, int share, const uint16_t *dY,
+                           const uint16_t *Ys, const int *row_of,
+                           const int *slot_of, const float *weights,
                            uint16_t *__restrict__ dYs, float *__restrict__ dweights) {
   __shared__ float partial[8][32];
   dependency_wait();
@@ -596,11 +617,11 @@ __global__ void __launch_bounds__(256)
         uint4 g[COLS], v[ROWS][COLS];
 #pragma unroll
         for (int q = 0; q < COLS; ++q) {
-          if (c + 256 * q >= D) break;
+          const bool in = c + 256 * q < D;
 #pragma unroll
           for (int i = 0; i < ROWS; ++i)
-            if (at[i] >= 0) v[i][q] = load_row16(Ys + static_cast<int64_t>(at[i]) * D + (c + 256 * q));
-          g[q] = load_row16(dY + t * D + c + 256 * q);
+            v[i][q] = load_row16(Ys + static_cast<int64_t>(at[i]) * D + (c + 256 * q), in && at[i] >= 0);
+          g[q] = load_row16(dY + t * D + c + 256 * q, in);
         }
 #pragma unroll
         for (int q = 0; q < COLS; ++q) {
@@ -767,7 +788,7 @@ cudaError_t launch_combine(int64_t T, int k, int64_t D, int64_t rows, const uint
                            const float *weights, uint16_t *Y, int sm_count, cudaStream_t stream) {
   const int share = warps_of_token(T, D, 32 * static_cast<int64_t>(sm_count));
   const int64_t per = 8 / share;
-  return with_flight(k, [&](auto r, auto c) {
+  return with_flight<false>(k, [&](auto r, auto c) {
     return launch_after(sq_combine_kernel<r.value, c.value>, static_cast<unsigned>((T + per - 1) / per), 256, 0, stream, T,
                         k, D, rows, share, Ys, row_of, weights, Y);
   });
@@ -778,7 +799,7 @@ cudaError_t launch_combine_grad(int64_t T, int k, int64_t D, int64_t rows, const
                                 float *dweights, int sm_count, cudaStream_t stream) {
   const int share = warps_of_token(T, D, 16 * static_cast<int64_t>(sm_count));
   const int64_t per = 8 / share;
-  return with_flight(k, [&](auto r, auto c) {
+  return with_flight<true>(k, [&](auto r, auto c) {
     return launch_after(sq_combine_grad_kernel<r.value, c.value>, static_cast<unsigned>((T + per - 1) / per), 256, 0,
                         stream, T, k, D, rows, share, dY, Ys, row_of, slot_of, weights, dYs, dweights);
   });
