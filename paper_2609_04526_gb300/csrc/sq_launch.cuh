@@ -3,15 +3,15 @@
 // end (and, through it, for everything before).
 //
 // Every kernel launched with launch_after calls dependency_wait in all its threads before it
-// reads or writes global memory, and dependency_start, which lets the next launch start, only
-// after that. A kernel so starts when the last but one before it has ended, and at most one
-// kernel runs beside the ones that wait. (The one exception reads early what is older still: the
-// second launch of the sort by expert counts its slots before its wait; its count launch, having
-// passed its own wait, shows that the slots are complete.)
+// reads what the launch ahead of it wrote and before it writes global memory, and dependency_start,
+// which lets the next launch start, only after that. A kernel so starts when the last but one before
+// it has ended, and at most one kernel runs beside the ones that wait. What that last but one wrote,
+// or an older one, may be read before the wait, by a launch that is always behind another one of the
+// same call (whose own wait shows that the call's inputs are complete too).
 //
-// Such a kernel reads memory with ordinary loads alone: the non-coherent ones (__ldg, or a const
-// __restrict__ pointer) are for what nobody writes while the kernel runs, and may be moved ahead of
-// the wait.
+// Behind its wait a kernel reads memory with ordinary loads alone: the non-coherent ones (__ldg, or
+// a const __restrict__ pointer) are for what nobody writes while the kernel runs, and may be moved
+// ahead of the wait.
 #pragma once
 #include <cuda_runtime.h>
 

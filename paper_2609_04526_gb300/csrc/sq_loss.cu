@@ -130,9 +130,12 @@ __device__ __forceinline__ float warp_total(float v) {
 // leaves a number here (the row's NaN reaches its results through the label's own term).
 __device__ __forceinline__ float row_reference(float label_z) { return fmaxf(ceilf(label_z * kLog2e), -1e30f); }
 
-// Rows of the piece's chunk that starts at compact row `first`.
+// Rows of the piece's chunk that starts at compact row `first`. The launches behind the logits read
+// what gather wrote before their wait, from the L2: the launch ahead of them, having passed its own
+// wait, shows that it is complete (64 rows of width 512 against 8000, loss and gradient: 22.2 us, 21.2
+// so; 8 of 2312 against 3211: 26.6, 25.2).
 __device__ __forceinline__ int chunk_rows(const HeadArgs &a, int first) {
-  const int left = *a.count - first;
+  const int left = __ldcg(a.count) - first;
   return left < 0 ? 0 : (left < a.chunk ? left : a.chunk);
 }
 
@@ -350,9 +353,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK, NT
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
 
+  int rows = GRAD ? chunk_rows(a, first) : 0;
   dependency_wait();
   dependency_start();
-  const int rows = chunk_rows(a, first);
+  if (!GRAD) rows = chunk_rows(a, first);
   const int tiles_m = (rows + C::kRows - 1) / C::kRows;
   const int tiles_n = static_cast<int>(((GRAD ? a.D : a.V) + NT - 1) / NT);
   constexpr int kDepth = C::kBK * C::kUnit;
@@ -628,19 +632,20 @@ template <int ROWS>
 __global__ void __launch_bounds__(1024) sq_head_finalize_kernel(const HeadArgs a, const int first) {
   constexpr int kShare = 32 / ROWS;
   __shared__ float parts[32][ROWS + 1];
-  dependency_wait();
-  dependency_start();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int rows = chunk_rows(a, first), r0 = blockIdx.x * ROWS;
-  if (r0 >= rows) return;
   const int own = lane % ROWS;  // of the CTA's rows
   const int r = min(r0 + own, rows - 1), row = first + r;  // lanes past the last row repeat it
+  const bool on = r0 < rows;
+  const float z = on ? __ldcg(a.label_z + row) : 0.f, z2 = z * kLog2e;
+  const int t = on ? __ldcg(a.token + row) : 0;
+  const float g = on && a.dX ? __ldcg(a.dloss + t) : 0.f;
+  dependency_wait();
+  dependency_start();
+  if (!on) return;
   constexpr int kCols = HeadCfg<false, 64, 256>::kEpiCols;
   const int filled = static_cast<int>((a.V + kCols - 1) / kCols);  // quarter tiles that hold columns
   const float *sums = a.sums + r, *refs = a.refs + r;
-  const float z = a.label_z[row], z2 = z * kLog2e;
-  const int t = a.token[row];
-  const float g = a.dX ? a.dloss[t] : 0.f;
   float top = row_reference(z), sum = 0.f;
   const bool moved = a.moved[r];
   const bool any = __any_sync(0xFFFFFFFFu, moved);  // the same rows in every warp
@@ -710,24 +715,27 @@ __global__ void __launch_bounds__(1024) sq_head_finalize_kernel(const HeadArgs a
 template <int SHARE>
 __global__ void __launch_bounds__(256) sq_head_rows_kernel(const HeadArgs a, const int first) {
   __shared__ float sums[SHARE > 1 ? 7 : 1][256];
-  dependency_wait();
-  dependency_start();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t pieces = static_cast<uint32_t>((a.D + 255) / 256);
   const uint32_t unit = SHARE > 1 ? blockIdx.x : blockIdx.x * 8 + warp;
-  const int r = unit / pieces;
+  const int r = unit / pieces, row = first + r;
   const int rows = chunk_rows(a, first);
-  if (r >= rows) return;
   const int64_t c = static_cast<int64_t>(unit % pieces) * 256 + lane * 8;
-  if (SHARE == 1 && c >= a.D) return;
   const int tiles_m = (rows + kHeadTile - 1) / kHeadTile;
-  const int parts = a.parts[tiles_m - 1] + 1;
+  const int parts = tiles_m > 0 ? a.parts[tiles_m - 1] + 1 : 0;
   const int64_t plane = static_cast<int64_t>(tiles_m) * kHeadTile * a.width;
-  const int row = first + r;
-  const float2 f = a.factors[row];
-  const int64_t label = a.label[row], token = a.token[row];
+  float2 f = make_float2(0.f, 0.f);
+  int64_t token = 0;
   uint4 w = make_uint4(0, 0, 0, 0);
-  if (c < a.D && warp % SHARE == 0) w = *reinterpret_cast<const uint4 *>(a.W + label * a.D + c);
+  if (r < rows) {  // what the launch before the one ahead wrote, and the weights
+    f = __ldcg(a.factors + row);
+    token = __ldcg(a.token + row);
+    if (c < a.D && warp % SHARE == 0)
+      w = __ldcg(reinterpret_cast<const uint4 *>(a.W + static_cast<int64_t>(__ldcg(a.label + row)) * a.D + c));
+  }
+  dependency_wait();
+  dependency_start();
+  if (r >= rows || (SHARE == 1 && c >= a.D)) return;
   float s[8] = {};
   if (c < a.D) {
     const float *p = a.partial + static_cast<int64_t>(r) * a.width + c + warp % SHARE * plane;
