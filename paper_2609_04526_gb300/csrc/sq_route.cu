@@ -788,6 +788,7 @@ cudaError_t launch_combine(int64_t T, int k, int64_t D, int64_t rows, const uint
                            const float *weights, uint16_t *Y, int sm_count, cudaStream_t stream) {
   const int share = warps_of_token(T, D, 32 * static_cast<int64_t>(sm_count));
   const int64_t per = 8 / share;
+  if (rows == 0) Ys = Y;  // no rows and perhaps no tensor: load_or_first still needs one to read
   return with_flight<false>(k, [&](auto r, auto c) {
     return launch_after(sq_combine_kernel<r.value, c.value>, static_cast<unsigned>((T + per - 1) / per), 256, 0, stream, T,
                         k, D, rows, share, Ys, row_of, weights, Y);

@@ -169,6 +169,21 @@ def test_rows_out_and_back(h, T, D, k, E, whole):
     assert np.all(np.abs(_np(dw) - want_dw) <= (D + 16) * ref.U32 * size)
 
 
+@pytest.mark.parametrize("k", [1, 2, 4, 8, 9])
+def test_no_expert_rows_at_all(h, k):
+    """Tokens that no expert serves, with an expert tensor of no rows: zeros, and nothing is read."""
+    T, D = 37, 264
+    _, row_of, slot_of = h.sq_sort_tokens(torch.full((T, k), -1, dtype=torch.int32, device="cuda"), 8)
+    none = torch.empty(0, D, dtype=torch.bfloat16, device="cuda")
+    w = torch.rand(T, k, generator=_gen(k), device="cuda")
+    X = torch.full((T, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+    assert h.sq_dispatch(X, row_of, slot_of, Xs=none.clone()).numel() == 0
+    assert not h.sq_combine(none, row_of, w, Y=X.clone()).any()
+    assert not h.sq_dispatch_grad(none, row_of, dX=X.clone()).any()
+    dYs, dw = h.sq_combine_grad(X, none, row_of, slot_of, w)
+    assert dYs.numel() == 0 and not dw.any()
+
+
 def test_combine_gradient_against_differences(h):
     """sum(dY Y) is linear in the weights and in Ys, so differences give the gradients exactly, up to
     the bf16 rounding of Y (2^-8 of each element)."""
