@@ -236,3 +236,24 @@ def test_sums_of_a_large_vocabulary_in_chunks(h):
         tol = 1e-3
         assert abs(float(lse[t]) - float(want)) < tol
         assert abs(float(loss[t]) - float(want - z[labels[t]])) < tol
+
+
+def test_inputs_written_just_before_the_call(h):
+    """Calls of changing sizes back to back, every input written by a kernel right ahead of its call, give
+    the bits of the same calls one by one."""
+    cases = [_case(T, 520, 2003, 50 + i, ignored=0.3) for i, T in enumerate((300, 7, 64, 1, 700, 33, 256, 130))]
+    want = []
+    for case in cases:
+        want.append([r.clone() for r in h.sq_head_loss_grad(*case)])
+        torch.cuda.synchronize()
+    X, W = torch.empty(700, 520, dtype=torch.bfloat16, device="cuda"), torch.empty_like(cases[0][1])
+    labels, dloss = torch.empty(700, dtype=torch.int64, device="cuda"), torch.empty(700, device="cuda")
+    got = []
+    for _ in range(6):
+        for x, w, y, d in cases:
+            T = len(x)
+            W.copy_(w), labels[:T].copy_(y), dloss[:T].copy_(d), X[:T].copy_(x)
+            got.append([r.clone() for r in h.sq_head_loss_grad(X[:T], W, labels[:T], dloss[:T])])
+    for i, results in enumerate(got):
+        for r, first in zip(results, want[i % len(cases)]):
+            assert torch.equal(r, first), i

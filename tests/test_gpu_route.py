@@ -68,6 +68,12 @@ def test_route(h, E, k, kind, bf16):
         assert np.all(err <= tol * size + (1.01 * ref.U16 * np.abs(want) if bf16 else 0) + 1e-37), err.max()
 
 
+@pytest.mark.parametrize("E, k", [(9, 9), (100, 16), (128, 12), (131, 9), (256, 16)])
+@pytest.mark.parametrize("kind, bf16", [("gauss", False), ("ties", True), ("masked", True)])
+def test_route_of_more_choices(h, E, k, kind, bf16):
+    test_route(h, E, k, kind, bf16)
+
+
 def test_route_infinite_logit(h):
     z = torch.zeros(2, 8, device="cuda")
     z[0, 3] = float("inf")
@@ -288,3 +294,34 @@ def test_refusals(h):
         h.sq_combine(torch.zeros(9, 64, dtype=torch.bfloat16, device="cuda"), row_of, weights)
     with pytest.raises(pkg.SQError, match="16-byte"):
         h.sq_dispatch(torch.zeros(4 * 64 + 4, dtype=torch.bfloat16, device="cuda")[4:].view(4, 64), row_of, slot_of)
+
+
+def test_inputs_written_just_before_the_call(h):
+    """Steps of changing sizes back to back, logits and rows written by kernels right ahead of them, give
+    the bits of the same steps one by one."""
+    E, k, D = 60, 4, 264
+    sizes = (2000, 1, 37, 500, 1999, 8)
+    zs = [torch.randn(T, E, generator=_gen(T), device="cuda") for T in sizes]
+    xs = [torch.randn(T, D, generator=_gen(T + 1), device="cuda").bfloat16() for T in sizes]
+
+    def step(z, x):
+        experts, weights = h.sq_route(z, k)
+        offsets, row_of, slot_of = h.sq_sort_tokens(experts, E)
+        Xs = h.sq_dispatch(x, row_of, slot_of)
+        Y = h.sq_combine(Xs, row_of, weights)
+        dYs, dw = h.sq_combine_grad(x, Xs, row_of, slot_of, weights)
+        return experts, weights, offsets, row_of, slot_of, Y, dYs, dw, h.sq_dispatch_grad(dYs, row_of), h.sq_route_grad(z, experts, dw)
+
+    want = []
+    for z, x in zip(zs, xs):
+        want.append([r.clone() for r in step(z, x)])
+        torch.cuda.synchronize()
+    z, x = torch.empty(2000, E, device="cuda"), torch.empty(2000, D, dtype=torch.bfloat16, device="cuda")
+    got = []
+    for _ in range(8):
+        for T, zi, xi in zip(sizes, zs, xs):
+            x[:T].copy_(xi), z[:T].copy_(zi)
+            got.append([r.clone() for r in step(z[:T], x[:T])])
+    for i, results in enumerate(got):
+        for j, (r, first) in enumerate(zip(results, want[i % len(sizes)])):
+            assert torch.equal(r, first), (i, j)
