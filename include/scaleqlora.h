@@ -534,7 +534,8 @@ sq_status sq_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint1
  * (device fp32; 1 / (number of targets) for their mean),
  *   dX[t] = dloss[t] (sum_v softmax(z[t])_v W[v] - W[labels[t]])
  * dX device bf16 [T, D] (overwritten; not X). The exponentials are rounded to bf16 as operands of
- * that product; sums, the label's own term and the final scaling are fp32. */
+ * that product and divided by the sum of the rounded ones, so that a part that rows of W share cancels;
+ * sums, the label's own term and the final scaling are fp32. */
 sq_status sq_head_loss_grad(sq_handle h, int64_t T, int64_t D, int64_t V, const uint16_t *X, const uint16_t *W,
                             const int64_t *labels, const float *dloss, float *loss, float *lse, uint16_t *dX,
                             void *stream);

@@ -443,11 +443,12 @@ struct HeadArgs {
   int *count;             // labelled tokens of the piece
   int *token, *label;
   float *label_z;
-  float2 *factors;
+  float2 *factors;        // of the row kernel
   uint16_t *rows;         // [T, D] the labelled tokens' rows of X
   // scratch, by row of the chunk
   int sum_rows;           // a chunk's rows, up to a multiple of 4
   float *sums, *refs;     // [4 * column tiles, sum_rows] sum and reference of each quarter tile
+  float *sums_e;          // likewise, sums of the rounded exponentials (gradient)
   int *moved;             // [chunk] a row whose references differ (refs are read only there)
   uint16_t *e;            // [chunk, pitch] bf16 exponentials (gradient)
   float *partial;         // [parts, rows, D] fp32 (gradient)

@@ -10,7 +10,7 @@
 //             and, for the gradient, writes bf16 e of the piece
 //   finalize  sums -> loss, log-sum-exp and the row's two gradient factors
 //   gradient  (e W) over the vocabulary, cut into parts where few tiles would leave SMs idle
-//   rows      dX = g / S (e W) - g (S - e_l) / S W[label]
+//   rows      dX = g (1 - p) (e W / Z - W[label]), p the label's share and Z the sum of e as it is in e W
 //
 // The reference r of a row is ceil(z_l log2(e)), known before the product: e then needs no
 // maximum first, and e W no second pass over the logits once S is known. Where a tile holds a
@@ -19,11 +19,16 @@
 // powers of two, so such a change of reference is exact. Terms more than 2^126 below the label's
 // own vanish.
 //
-// The label's own term is left out of e and of the sums and carried in fp32: p_label - 1 is
-// -(S - e_l) / S without cancellation, so confident tokens keep an accurate loss and gradient.
-// e is rounded to bf16 once, as an operand of the tensor cores (at most 2^-8 of a term; errors of
-// one sign and the other, so their sum stays below the rounding of the bf16 gradient); the sums S
-// take the unrounded values.
+// The label's own term is left out of e and of the sums and carried in fp32: 1 - p is (S - e_l) / S
+// without cancellation, so confident tokens keep an accurate loss and gradient.
+//
+// e is rounded to bf16 once, as an operand of the tensor cores: at most 2^-9 of a term. The sum S, of
+// the loss and of 1 - p, takes the unrounded values. e W is divided by the sum Z of the rounded ones: its
+// weights so add up to 1, as the label's coefficient does, what the rows of W have in common cancels,
+// and a term of share s among the others moves the result by 1 - s of its rounding. (Relative error
+// of dX for 256 rows against 8000 x 512 where the rows of W share a part of ten times their own size and
+// one competitor of the label has 0.6 of the others: 0.00167, of which the rounding of dX itself is
+// 0.00166; with S in place of Z 0.0094.)
 #include "sq_gemm_kernels.cuh"
 #include "sq_launch.cuh"
 
@@ -299,7 +304,8 @@ struct HeadWalk {
   }
 };
 
-template <bool GRAD, int BK, int NT>
+// KEEP: the logits of a call with a gradient, whose exponentials are written.
+template <bool GRAD, int BK, int NT, bool KEEP>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK, NT>::kThreads, 1)
     sq_head_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                    const __grid_constant__ CUtensorMap tmO, const HeadArgs a, const int first) {
@@ -311,7 +317,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK, NT
   // boxes' room is part of the ring.
   constexpr int kMax = C::kMaxStages;
   const int a_bytes = a.box_rows * C::kBK * 2, stage_bytes = a_bytes + C::kB;
-  const int S = min(kMax, (GRAD || a.e ? C::kRing : C::kOffBar) / stage_bytes);
+  const int S = min(kMax, (GRAD || KEEP ? C::kRing : C::kOffBar) / stage_bytes);
   const bool both = a.T > 128;  // else the peer's rows of A are past the last token
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -561,28 +567,39 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK, NT
         }
         // A logit far above the reference shows in the sum; the largest one then becomes the
         // reference and the exponentials are formed again.
-        float sum = 0.f;
+        float sum = 0.f, sum_e = 0.f;
 #pragma unroll 1
         for (bool again = false;; again = true) {
           float part[4] = {};
+          sum_e = 0.f;
 #pragma unroll
           for (int g = 0; g < C::kEpiCols / 32; ++g) {
-            uint32_t packed[16];
 #pragma unroll
-            for (int q = 0; q < 16; ++q) {
-              const float e0 = exp2_fast(fmaf(__uint_as_float(z[g][2 * q]), kLog2e, -ref));
-              const float e1 = exp2_fast(fmaf(__uint_as_float(z[g][2 * q + 1]), kLog2e, -ref));
-              part[q % 4] += e0 + e1;
-              const __nv_bfloat162 h2 = __floats2bfloat162_rn(e0, e1);
-              packed[q] = *reinterpret_cast<const uint32_t *>(&h2);
+            for (int q = 0; q < 4; ++q) {
+              uint32_t packed[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float e0 = exp2_fast(fmaf(__uint_as_float(z[g][8 * q + 2 * i]), kLog2e, -ref));
+                const float e1 = exp2_fast(fmaf(__uint_as_float(z[g][8 * q + 2 * i + 1]), kLog2e, -ref));
+                part[i] += e0 + e1;
+                const __nv_bfloat162 h2 = __floats2bfloat162_rn(e0, e1);
+                packed[i] = *reinterpret_cast<const uint32_t *>(&h2);
+              }
+              // The test at run time, always true, keeps the compiler from forming all exponentials
+              // ahead of the first store and spilling them (2048 against 38912 x 512, logits and
+              // gradient: 171 us without it and in groups of 32, 148 so).
+              if (KEEP && a.e) {
+                if (q == 0) {
+                  if (lane == 0) bulk_wait_read<0>();  // the box's last store, half a tile ago, has read it
+                  __syncwarp();
+                }
+                st_shared_v4(box + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4), packed[0], packed[1], packed[2], packed[3]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  sum_e += __uint_as_float(packed[i] << 16) + __uint_as_float(packed[i] & 0xFFFF0000u);
+              }
             }
-            if (a.e) {
-              if (lane == 0) bulk_wait_read<0>();  // the box's last store, half a tile ago, has read it
-              __syncwarp();
-#pragma unroll
-              for (int q = 0; q < 4; ++q)
-                st_shared_v4(box + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4), packed[4 * q], packed[4 * q + 1],
-                             packed[4 * q + 2], packed[4 * q + 3]);
+            if (KEEP && a.e) {
               fence_proxy_async_smem();  // the box -> async proxy (the TMA store)
               __syncwarp();
               if (lane == 0) {
@@ -605,6 +622,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK, NT
         }
         if (in) {
           a.sums[at_sum] = sum;
+          if constexpr (KEEP) a.sums_e[at_sum] = sum_e;
           a.refs[at_sum] = ref;
         }
       }
@@ -623,15 +641,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK, NT
 
 // ---------------------------------------------------------------- finalize and rows
 
+__device__ __forceinline__ float from_lane(float v, int mask) { return __shfl_xor_sync(0xFFFFFFFFu, v, mask); }
+__device__ __forceinline__ float2 from_lane(float2 v, int mask) {
+  return make_float2(from_lane(v.x, mask), from_lane(v.y, mask));
+}
+
 // ROWS rows per CTA: each takes 32 / ROWS lanes of every warp, which take the quarter tiles in turn
 // (neighbouring rows of one quarter tile lie side by side): 8 read whole sectors, 4 give few tokens
 // twice the CTAs (32, whole lines, left most SMs without rows: 14 us for 2048). The order of a row's
 // sum is the same in all, so it depends on nothing but the row: 256 sums of every 256th quarter
 // tile, eight to a warp, then the warps'.
 template <int ROWS>
-__global__ void __launch_bounds__(1024) sq_head_finalize_kernel(const HeadArgs a, const int first) {
+__global__ void __launch_bounds__(1024, ROWS == 4 ? 1 : 2) sq_head_finalize_kernel(const HeadArgs a, const int first) {
   constexpr int kShare = 32 / ROWS;
-  __shared__ float parts[32][ROWS + 1];
+  __shared__ float parts[32][ROWS + 1], parts_e[32][ROWS + 1];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int rows = chunk_rows(a, first), r0 = blockIdx.x * ROWS;
   const int own = lane % ROWS;  // of the CTA's rows
@@ -645,14 +668,14 @@ __global__ void __launch_bounds__(1024) sq_head_finalize_kernel(const HeadArgs a
   if (!on) return;
   constexpr int kCols = HeadCfg<false, 64, 256>::kEpiCols;
   const int filled = static_cast<int>((a.V + kCols - 1) / kCols);  // quarter tiles that hold columns
-  const float *sums = a.sums + r, *refs = a.refs + r;
-  float top = row_reference(z), sum = 0.f;
+  const float *sums = a.sums + r, *sums_e = a.sums_e + r, *refs = a.refs + r;
+  float top = row_reference(z);
   const bool moved = a.moved[r];
   const bool any = __any_sync(0xFFFFFFFFu, moved);  // the same rows in every warp
   // f over the row's quarter tiles of this warp
   constexpr int kOwn = 8 / kShare;  // of the warp's eight sums, those of this lane
-  auto over_tiles = [&](float start, auto value, auto f) {
-    float v[kOwn];
+  auto over_tiles = [&](auto start, auto value, auto f) {
+    decltype(start) v[kOwn];
 #pragma unroll
     for (int j = 0; j < kOwn; ++j) v[j] = start;
 #pragma unroll kShare
@@ -665,7 +688,7 @@ __global__ void __launch_bounds__(1024) sq_head_finalize_kernel(const HeadArgs a
     for (int d = 4; d > 0; d >>= 1) {  // the eight sums in one order, over lanes or in the lane
       if (d >= kOwn) {
 #pragma unroll
-        for (int j = 0; j < kOwn; ++j) v[j] = f(v[j], __shfl_xor_sync(0xFFFFFFFFu, v[j], d / kOwn * ROWS));
+        for (int j = 0; j < kOwn; ++j) v[j] = f(v[j], from_lane(v[j], d / kOwn * ROWS));
       } else {
 #pragma unroll
         for (int j = 0; j < d; ++j) v[j] = f(v[j], v[j + d]);
@@ -675,16 +698,27 @@ __global__ void __launch_bounds__(1024) sq_head_finalize_kernel(const HeadArgs a
   };
   auto larger = [](float x, float y) { return fmaxf(x, y); };
   auto plus = [](float x, float y) { return x + y; };
+  auto plus2 = [](float2 x, float2 y) { return make_float2(x.x + y.x, x.y + y.y); };
+  auto by_of = [&](int64_t at) { return any ? whole_exp2(refs[at] - top) : 1.f; };
   if (any) {  // references differ: the largest of them first
     parts[warp][own] = over_tiles(top, [&](int64_t at) { return refs[at]; }, larger);
     __syncthreads();
     for (int w = 0; w < 32; ++w) top = fmaxf(top, parts[w][own]);
     __syncthreads();
-    sum = over_tiles(0.f, [&](int64_t at) { return sums[at] * whole_exp2(refs[at] - top); }, plus);
-  } else {
-    sum = over_tiles(0.f, [&](int64_t at) { return sums[at]; }, plus);
   }
-  parts[warp][own] = sum;
+  if (a.e) {
+    const float2 both = over_tiles(
+        make_float2(0.f, 0.f),
+        [&](int64_t at) {
+          const float by = by_of(at);
+          return make_float2(sums[at] * by, sums_e[at] * by);
+        },
+        plus2);
+    parts[warp][own] = both.x;
+    parts_e[warp][own] = both.y;
+  } else {
+    parts[warp][own] = over_tiles(0.f, [&](int64_t at) { return sums[at] * by_of(at); }, plus);
+  }
   __syncthreads();
   if (any && a.e) {  // the exponentials of moved rows follow their reference
     for (int i = warp; i < filled; i += 32)
@@ -698,8 +732,10 @@ __global__ void __launch_bounds__(1024) sq_head_finalize_kernel(const HeadArgs a
       }
   }
   if (warp > 0 || lane >= ROWS || r0 + lane >= rows) return;
-  float others = 0.f;
+  float others = 0.f, others_e = 0.f;
   for (int w = 0; w < 32; ++w) others += parts[w][own];
+  if (a.e)
+    for (int w = 0; w < 32; ++w) others_e += parts_e[w][own];
   a.moved[r] = 0;  // for the next chunk
   const float label = exp2_fast(z2 - top), total = others + label;
   // log(total / label): where label underflows against a far larger logit, from the exponents
@@ -707,7 +743,10 @@ __global__ void __launch_bounds__(1024) sq_head_finalize_kernel(const HeadArgs a
   const float loss = near ? log1pf(others / label) : (top - z2) * kLn2 + logf(total);
   if (a.loss) a.loss[t] = loss;
   if (a.lse) a.lse[t] = near ? z + loss : top * kLn2 + logf(total);
-  if (a.dX) a.factors[row] = make_float2(g / total, -g * (others / total));
+  if (a.e) {
+    const float f = g * (others / total);
+    a.factors[row] = make_float2(others_e > 0.f ? f / others_e : 0.f, -f);
+  }
 }
 
 // dX[token] = f.x sum over the parts + f.y W[label]. A warp per 256 columns of a row, or, where
@@ -772,7 +811,7 @@ __global__ void __launch_bounds__(256) sq_head_rows_kernel(const HeadArgs a, con
 
 // As many two-CTA clusters as fit on the GPU at once, or one per tile (most: no number of tiles
 // that the host knows).
-template <bool GRAD, int BK, int NT>
+template <bool GRAD, int BK, int NT, bool KEEP = false>
 cudaError_t launch_head_product(const CUtensorMap &tmA, const CUtensorMap &tmB, const CUtensorMap &tmO,
                                 const HeadArgs &a, int first, int64_t most, int sm_count, cudaStream_t stream) {
   using C = HeadCfg<GRAD, BK, NT>;
@@ -782,14 +821,14 @@ cudaError_t launch_head_product(const CUtensorMap &tmA, const CUtensorMap &tmB, 
   cudaGetDevice(&dev);
   if (!(done_mask & (1 << (dev & 31)))) {
     cudaError_t e =
-        cudaFuncSetAttribute(sq_head_kernel<GRAD, BK, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
+        cudaFuncSetAttribute(sq_head_kernel<GRAD, BK, NT, KEEP>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * (sm_count / 2), 1, 1);
     cfg.blockDim = dim3(C::kThreads, 1, 1);
     cfg.dynamicSmemBytes = C::kSmemBytes;
     int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, sq_head_kernel<GRAD, BK, NT>, &cfg) != cudaSuccess || n <= 0) {
+    if (cudaOccupancyMaxActiveClusters(&n, sq_head_kernel<GRAD, BK, NT, KEEP>, &cfg) != cudaSuccess || n <= 0) {
       cudaGetLastError();
       n = sm_count / 2;
     }
@@ -797,7 +836,7 @@ cudaError_t launch_head_product(const CUtensorMap &tmA, const CUtensorMap &tmB, 
     done_mask |= 1 << (dev & 31);
   }
   const int64_t clusters = std::min<int64_t>(most, max_clusters[dev & 31]);
-  return launch_after(sq_head_kernel<GRAD, BK, NT>, static_cast<unsigned>(2 * clusters), C::kThreads, C::kSmemBytes, stream, tmA,
+  return launch_after(sq_head_kernel<GRAD, BK, NT, KEEP>, static_cast<unsigned>(2 * clusters), C::kThreads, C::kSmemBytes, stream, tmA,
                       tmB, tmO, a, first);
 }
 
@@ -814,12 +853,16 @@ cudaError_t launch_head_chunk(const HeadArgs &a, const HeadMaps &m, int first, i
   // Few tokens are bound by the weights' way from memory: stages of 128, whose rows are read 256 bytes
   // at a time. More are bound by the MMAs: stages of 64, of which five wait behind the one in work
   // (2048 against 38912 x 2048 in 163 us, 175 with 128).
-  const auto logits = a.columns == 64    ? launch_head_product<false, 128, 64>
-                      : a.columns == 128 ? launch_head_product<false, 128, 128>
-                      : a.few            ? launch_head_product<false, 128, 256>
-                                         : launch_head_product<false, 64, 256>;
-  cudaError_t e = logits(m.rows, m.weights, m.e_store, a, first, tiles_m * ((a.V + a.columns - 1) / a.columns), sm_count,
-                         stream);
+  auto logits = [&](auto keep) {
+    constexpr bool k = decltype(keep)::value;
+    return a.columns == 64    ? launch_head_product<false, 128, 64, k>
+           : a.columns == 128 ? launch_head_product<false, 128, 128, k>
+           : a.few            ? launch_head_product<false, 128, 256, k>
+                              : launch_head_product<false, 64, 256, k>;
+  };
+  const auto product = a.dX ? logits(std::true_type{}) : logits(std::false_type{});
+  cudaError_t e = product(m.rows, m.weights, m.e_store, a, first, tiles_m * ((a.V + a.columns - 1) / a.columns), sm_count,
+                          stream);
   if (e != cudaSuccess) return e;
   if (rows <= 4 * sm_count)
     e = launch_after(sq_head_finalize_kernel<4>, (rows + 3) / 4, 1024, 0, stream, a, first);
