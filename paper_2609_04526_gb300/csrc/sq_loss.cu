@@ -743,13 +743,10 @@ __global__ void __launch_bounds__(1024, ROWS == 4 ? 1 : 2) sq_head_finalize_kern
   const float loss = near ? log1pf(others / label) : (top - z2) * kLn2 + logf(total);
   if (a.loss) a.loss[t] = loss;
   if (a.lse) a.lse[t] = near ? z + loss : top * kLn2 + logf(total);
-  if (a.e) {
-    const float f = g * (others / total);
-    a.factors[row] = make_float2(others_e > 0.f ? f / others_e : 0.f, -f);
-  }
+  if (a.e) a.factors[row] = make_float2(g * (others / total), others_e > 0.f ? 1.f / others_e : 0.f);
 }
 
-// dX[token] = f.x sum over the parts + f.y W[label]. A warp per 256 columns of a row, or, where
+// dX[token] = f.x (f.y sum over the parts - W[label]). A warp per 256 columns of a row, or, where
 // there are many parts (SHARE = 8), a CTA whose warps add up every eighth part each.
 template <int SHARE>
 __global__ void __launch_bounds__(256) sq_head_rows_kernel(const HeadArgs a, const int first) {
@@ -802,8 +799,8 @@ __global__ void __launch_bounds__(256) sq_head_rows_kernel(const HeadArgs a, con
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const __nv_bfloat162 h2 =
-        __floats2bfloat162_rn(fmaf(f.x, s[2 * q], f.y * __uint_as_float(ww[q] << 16)),
-                              fmaf(f.x, s[2 * q + 1], f.y * __uint_as_float(ww[q] & 0xFFFF0000u)));
+        __floats2bfloat162_rn(f.x * fmaf(f.y, s[2 * q], -__uint_as_float(ww[q] << 16)),
+                              f.x * fmaf(f.y, s[2 * q + 1], -__uint_as_float(ww[q] & 0xFFFF0000u)));
     o[q] = *reinterpret_cast<const uint32_t *>(&h2);
   }
   *reinterpret_cast<uint4 *>(a.dX + token * a.D + c) = make_uint4(o[0], o[1], o[2], o[3]);

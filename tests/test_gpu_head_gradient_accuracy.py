@@ -58,3 +58,18 @@ def _check(h, X, W, labels):
 def test_rounded_exponentials_cancel(h, T, common, rival, lean):
     """What the weights share leaves the gradient exactly, however the exponentials are rounded."""
     _check(h, *_case(T, 512, 8000, common, rival, lean, seed=int(common) + T))
+
+
+def test_small_factor_of_an_unlikely_label(h):
+    """Gradients far below 1 of labels whose competitors are 2^95 as likely: no factor leaves fp32's normal range."""
+    T, D, V = 70, 64, 700
+    X, W, labels = _case(T, D, V, 0.0, 0.0, 0.0, seed=3)
+    X[:, 0], W[:, 0] = 8.0, 0.0
+    W[333, 0] = 95 * math.log(2) / 8
+    labels = torch.where(labels == 333, 334, labels)
+    dloss = torch.full((T,), 2.0 ** -50, device="cuda")
+    dX = h.sq_head_loss_grad(X, W, labels, dloss)[2]
+    h.sq_sync()
+    want = _gradient(X, W, labels, dloss)
+    err = (dX.double() - want).norm(dim=1) / want.norm(dim=1)
+    assert float(err.max()) <= 1.25 * 2.0 ** -8, float(err.max())
