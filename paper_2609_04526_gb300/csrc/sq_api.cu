@@ -456,8 +456,9 @@ sq_status run_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint
   a.columns = sqi::head_columns(T, V, a.few, clusters);
   int64_t partial_rows = 0;  // of 4 * D bytes: the most that any number of labelled rows takes
   for (int64_t m = 1; dX && m <= chunk / sqi::kHeadTile; ++m) {
-    const int parts = sqi::head_parts(std::min(m * sqi::kHeadTile, piece), D, static_cast<int>((V + 127) / 128),
-                                      clusters);
+    const int stages = static_cast<int>((V + 127) / 128);  // the gradient's, of 128 vocabulary entries
+    const int parts = sqi::head_parts(std::min(m * sqi::kHeadTile, piece), D, stages, clusters);
+    if ((stages + parts - 1) / parts > sqi::kHeadSegment / 128) a.long_sums = true;
     a.parts[m - 1] = static_cast<uint8_t>(parts - 1);
     partial_rows = std::max(partial_rows, m * sqi::kHeadTile * parts);
   }
@@ -499,8 +500,8 @@ sq_status run_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint
                     CU_TENSOR_MAP_SWIZZLE_64B, a.pitch));
     SQ_TRY(make_map(h, &m.e_load, a.e, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, V, chunk, 64, a.box_rows,
                     CU_TENSOR_MAP_SWIZZLE_128B, a.pitch));
-    SQ_TRY(make_map(h, &m.partial, a.partial, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, D, partial_rows, 32, 32,
-                    CU_TENSOR_MAP_SWIZZLE_128B, a.width));
+    SQ_TRY(make_map(h, &m.partial, a.partial, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, D, partial_rows, a.long_sums ? 16 : 32, 32,
+                    a.long_sums ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, a.width));
   }
   for (int64_t t = 0; t < T; t += piece) {
     a.T = static_cast<int>(std::min(piece, T - t));

@@ -41,11 +41,21 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRefSlack = 100.f;  // a logit this far above the reference (in powers of two) moves it
 constexpr float kFarSum = 0x1p100f;  // the sum of a quarter tile that may hold one
 
+// What a product launch does.
+enum HeadStep {
+  HEAD_LOSS,       // logits, of a call without a gradient
+  HEAD_KEEP,       // logits, whose exponentials are written for the gradient
+  HEAD_GRAD,       // gradient, each sum in one accumulator
+  HEAD_GRAD_LONG,  // gradient, sums longer than kHeadSegment products
+};
+
 // A pair's tile has 256 rows and NT columns, its stages are BK deep. Epilogue warp w takes TMEM lanes
-// 32 (w % 4) .. + 31 and the w / 4-th 64 columns (logits, which stay in registers) or 128 (gradient).
-template <bool GRAD, int BK, int NT>
+// 32 (w % 4) .. + 31 and the w / 4-th 64 columns (which stay in registers) or, where a sum leaves tensor
+// memory once, 128.
+template <int STEP, int BK, int NT>
 struct HeadCfg {
-  static constexpr int kEpiCols = GRAD ? 128 : 64;
+  static constexpr bool GRAD = STEP >= HEAD_GRAD;
+  static constexpr int kEpiCols = STEP == HEAD_GRAD ? 128 : 64;
   static constexpr int kEpiWarps = NT / kEpiCols * 4;
   static constexpr int kTmaWarp = kEpiWarps;
   static constexpr int kMmaWarp = kTmaWarp + 1;
@@ -58,19 +68,22 @@ struct HeadCfg {
   static constexpr int kUnit = GRAD ? 128 / kBK : 1;  // stages of a unit of the walk's contraction
   static constexpr int kRows = kHeadTile;
   static constexpr int kOffBox = kRing;
-  static constexpr int kBoxBytes = 32 * 32 * (GRAD ? 4 : 2);  // 32 rows x 32 columns of a warp
+  static constexpr int kBoxCols = STEP == HEAD_GRAD_LONG ? 16 : 32;
+  static constexpr int kBoxBytes = 32 * kBoxCols * (GRAD ? 4 : 2);  // 32 rows x kBoxCols columns of a warp
   // Stages added up in one accumulator. The tensor core truncates its running fp32 sum at every
   // step of 16, a bias that grows with the length: a sum of 4096 products in one accumulator left
   // the log-sum-exp 1.4e-5 too small. The logits therefore leave tensor memory every 512 products
-  // and are added in registers; the gradient, rounded to bf16 in the end, runs through.
-  static constexpr int kSegment = GRAD ? 1 << 30 : 512 / kBK;
+  // and are added in registers, and so does the gradient, rounded to bf16 in the end, every
+  // kHeadSegment.
+  static constexpr int kSegment = STEP == HEAD_GRAD ? 1 << 30 : (GRAD ? kHeadSegment : 512) / kBK;
   static constexpr int kOffBar = kOffBox + kEpiWarps * kBoxBytes;
   static constexpr int kSmemBytes = kOffBar + 512 + 1024;
 };
 // The last stage's A, read to 128 rows of its second 64-wide chunk, ends within the shared memory (the
 // smallest tiles: 12 stages of 16 KiB).
-static_assert(11 * 16384 + 4096 + 16384 <= HeadCfg<false, 128, 64>::kOffBar, "operand rows past the shared memory");
-static_assert(HeadCfg<false, 64, 256>::kSmemBytes <= 232448 && HeadCfg<true, 64, 256>::kSmemBytes <= 232448,
+static_assert(11 * 16384 + 4096 + 16384 <= HeadCfg<HEAD_LOSS, 128, 64>::kOffBar, "operand rows past the shared memory");
+static_assert(HeadCfg<HEAD_KEEP, 64, 256>::kSmemBytes <= 232448 && HeadCfg<HEAD_GRAD, 64, 256>::kSmemBytes <= 232448 &&
+                  HeadCfg<HEAD_GRAD_LONG, 64, 256>::kSmemBytes <= 232448,
               "head kernel exceeds the opt-in shared memory of one CTA");
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -112,6 +125,23 @@ __device__ __forceinline__ void umma_commit_pair_elect(uint64_t *bar) {
       "elect.sync _|e, 0xFFFFFFFF;\n\t"
       "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar))
       : "memory");
+}
+
+// mbar_wait without a call, for a thread that holds many registers.
+__device__ __forceinline__ bool mbar_wait_inline(uint64_t *bar, uint32_t parity, volatile int *abort_flag, int *err) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const unsigned long long t0 = globaltimer();
+  while (true) {
+#pragma unroll 1
+    for (int i = 0; i < 32; ++i)
+      if (mbar_try_wait(bar, parity)) return true;
+    if (*abort_flag) return false;
+    if (globaltimer() - t0 > kWaitLimitNs) {
+      *abort_flag = 1;
+      atomicOr(err, kErrWaitTimeout);
+      return false;
+    }
+  }
 }
 
 // 32 lanes x 16 consecutive fp32 columns.
@@ -304,12 +334,12 @@ struct HeadWalk {
   }
 };
 
-// KEEP: the logits of a call with a gradient, whose exponentials are written.
-template <bool GRAD, int BK, int NT, bool KEEP>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK, NT>::kThreads, 1)
+template <int STEP, int BK, int NT>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<STEP, BK, NT>::kThreads, 1)
     sq_head_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                    const __grid_constant__ CUtensorMap tmO, const HeadArgs a, const int first) {
-  using C = HeadCfg<GRAD, BK, NT>;
+  using C = HeadCfg<STEP, BK, NT>;
+  constexpr bool GRAD = C::GRAD, KEEP = STEP == HEAD_KEEP;
   // A stage holds box_rows rows of A; the MMAs read 128 all the same, the rest of them whatever
   // lies behind in the ring and the store boxes, and nothing reads those rows of the product. Few
   // tokens so leave the ring to the columns, which are all their traffic (one token against 128256
@@ -491,7 +521,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK, NT
     while (t.more() && ok) {
       const int row32 = t.tm * C::kRows + 128 * static_cast<int>(rank) + 32 * quad;  // of the chunk
       const int col0 = t.tn * NT + C::kEpiCols * share;
-      if constexpr (GRAD) {
+      if constexpr (STEP == HEAD_GRAD) {
         const int ab = tc & 1;
         ok = __all_sync(0xFFFFFFFFu, mbar_wait(&tfull[ab], static_cast<uint32_t>(tc >> 1) & 1u, abort_flag, a.err));
         if (!ok) break;
@@ -517,6 +547,48 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<GRAD, BK, NT
         }
         release(ab);
         ++tc;
+        t.advance();
+      } else if constexpr (GRAD) {
+        const int32_t out_row = t.part * tiles_m * C::kRows + row32;
+        const int steps = t.nk * C::kUnit;
+        float v[C::kEpiCols] = {};  // the row's sums
+#pragma unroll 1
+        for (int k0 = 0; k0 < steps; k0 += C::kSegment, ++tc) {
+          const int ab = tc & 1;
+          ok = __all_sync(0xFFFFFFFFu, mbar_wait_inline(&tfull[ab], static_cast<uint32_t>(tc >> 1) & 1u, abort_flag, a.err));
+          if (!ok) break;
+          tc_fence_after();
+          // Added to zeros the first time too: with loads in place, as of the logits, or a call in the wait
+          // 50 registers were saved in memory at every turn (2048 against 38912 x 2048, loss and gradient:
+          // 394 us, 381 so).
+#pragma unroll
+          for (int g = 0; g < C::kEpiCols / 16; ++g) {
+            uint32_t x[16];
+            tmem_ld16(t_row + ab * kTmemCols + 16 * g, x);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[16 * g + i] += __uint_as_float(x[i]);
+          }
+          release(ab);
+        }
+        if (!ok) break;
+#pragma unroll
+        for (int g = 0; g < C::kEpiCols / 16; ++g) {
+          if (lane == 0) bulk_wait_read<0>();  // the previous box's store has read the buffer
+          __syncwarp();
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const float *x = v + 16 * g + 4 * q;
+            st_shared_v4(box + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4), __float_as_uint(x[0]), __float_as_uint(x[1]),
+                         __float_as_uint(x[2]), __float_as_uint(x[3]));
+          }
+          fence_proxy_async_smem();  // the box -> async proxy (the TMA store)
+          __syncwarp();
+          if (lane == 0) {
+            if (col0 + 16 * g < a.D && row32 < rows) tma_store_2d(&tmO, box, col0 + 16 * g, out_row);
+            bulk_commit_group();
+          }
+        }
         t.advance();
       } else {
         const bool in = row32 + lane < rows;
@@ -666,7 +738,7 @@ __global__ void __launch_bounds__(1024, ROWS == 4 ? 1 : 2) sq_head_finalize_kern
   dependency_wait();
   dependency_start();
   if (!on) return;
-  constexpr int kCols = HeadCfg<false, 64, 256>::kEpiCols;
+  constexpr int kCols = HeadCfg<HEAD_LOSS, 64, 256>::kEpiCols;
   const int filled = static_cast<int>((a.V + kCols - 1) / kCols);  // quarter tiles that hold columns
   const float *sums = a.sums + r, *sums_e = a.sums_e + r, *refs = a.refs + r;
   float top = row_reference(z);
@@ -808,24 +880,24 @@ __global__ void __launch_bounds__(256) sq_head_rows_kernel(const HeadArgs a, con
 
 // As many two-CTA clusters as fit on the GPU at once, or one per tile (most: no number of tiles
 // that the host knows).
-template <bool GRAD, int BK, int NT, bool KEEP = false>
+template <int STEP, int BK, int NT>
 cudaError_t launch_head_product(const CUtensorMap &tmA, const CUtensorMap &tmB, const CUtensorMap &tmO,
                                 const HeadArgs &a, int first, int64_t most, int sm_count, cudaStream_t stream) {
-  using C = HeadCfg<GRAD, BK, NT>;
+  using C = HeadCfg<STEP, BK, NT>;
   static int done_mask = 0;  // per device ordinal (first 31)
   static int max_clusters[32] = {0};
   int dev = 0;
   cudaGetDevice(&dev);
   if (!(done_mask & (1 << (dev & 31)))) {
     cudaError_t e =
-        cudaFuncSetAttribute(sq_head_kernel<GRAD, BK, NT, KEEP>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
+        cudaFuncSetAttribute(sq_head_kernel<STEP, BK, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * (sm_count / 2), 1, 1);
     cfg.blockDim = dim3(C::kThreads, 1, 1);
     cfg.dynamicSmemBytes = C::kSmemBytes;
     int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, sq_head_kernel<GRAD, BK, NT, KEEP>, &cfg) != cudaSuccess || n <= 0) {
+    if (cudaOccupancyMaxActiveClusters(&n, sq_head_kernel<STEP, BK, NT>, &cfg) != cudaSuccess || n <= 0) {
       cudaGetLastError();
       n = sm_count / 2;
     }
@@ -833,7 +905,7 @@ cudaError_t launch_head_product(const CUtensorMap &tmA, const CUtensorMap &tmB, 
     done_mask |= 1 << (dev & 31);
   }
   const int64_t clusters = std::min<int64_t>(most, max_clusters[dev & 31]);
-  return launch_after(sq_head_kernel<GRAD, BK, NT, KEEP>, static_cast<unsigned>(2 * clusters), C::kThreads, C::kSmemBytes, stream, tmA,
+  return launch_after(sq_head_kernel<STEP, BK, NT>, static_cast<unsigned>(2 * clusters), C::kThreads, C::kSmemBytes, stream, tmA,
                       tmB, tmO, a, first);
 }
 
@@ -850,14 +922,14 @@ cudaError_t launch_head_chunk(const HeadArgs &a, const HeadMaps &m, int first, i
   // Few tokens are bound by the weights' way from memory: stages of 128, whose rows are read 256 bytes
   // at a time. More are bound by the MMAs: stages of 64, of which five wait behind the one in work
   // (2048 against 38912 x 2048 in 163 us, 175 with 128).
-  auto logits = [&](auto keep) {
-    constexpr bool k = decltype(keep)::value;
-    return a.columns == 64    ? launch_head_product<false, 128, 64, k>
-           : a.columns == 128 ? launch_head_product<false, 128, 128, k>
-           : a.few            ? launch_head_product<false, 128, 256, k>
-                              : launch_head_product<false, 64, 256, k>;
+  auto logits = [&](auto step) {
+    constexpr int k = decltype(step)::value;
+    return a.columns == 64    ? launch_head_product<k, 128, 64>
+           : a.columns == 128 ? launch_head_product<k, 128, 128>
+           : a.few            ? launch_head_product<k, 128, 256>
+                              : launch_head_product<k, 64, 256>;
   };
-  const auto product = a.dX ? logits(std::true_type{}) : logits(std::false_type{});
+  const auto product = a.dX ? logits(std::integral_constant<int, HEAD_KEEP>{}) : logits(std::integral_constant<int, HEAD_LOSS>{});
   cudaError_t e = product(m.rows, m.weights, m.e_store, a, first, tiles_m * ((a.V + a.columns - 1) / a.columns), sm_count,
                           stream);
   if (e != cudaSuccess) return e;
@@ -872,7 +944,10 @@ cudaError_t launch_head_chunk(const HeadArgs &a, const HeadMaps &m, int first, i
     units = std::max(units, t * tiles_d * (a.parts[t - 1] + 1));
     parts = std::max<int64_t>(parts, a.parts[t - 1] + 1);
   }
-  const auto gradient = a.few ? launch_head_product<true, 128, 256> : launch_head_product<true, 64, 256>;
+  const auto gradient = a.few ? a.long_sums ? launch_head_product<HEAD_GRAD_LONG, 128, 256>
+                                            : launch_head_product<HEAD_GRAD, 128, 256>
+                        : a.long_sums ? launch_head_product<HEAD_GRAD_LONG, 64, 256>
+                                      : launch_head_product<HEAD_GRAD, 64, 256>;
   if ((e = gradient(m.e_load, m.weights_grad, m.partial, a, first, units, sm_count, stream)) != cudaSuccess) return e;
   const int64_t pieces = rows * ((a.D + 255) / 256);
   if (parts >= 8 && pieces <= 16 * static_cast<int64_t>(sm_count))  // too few warps for loads one after the other

@@ -73,3 +73,11 @@ def test_small_factor_of_an_unlikely_label(h):
     want = _gradient(X, W, labels, dloss)
     err = (dX.double() - want).norm(dim=1) / want.norm(dim=1)
     assert float(err.max()) <= 1.25 * 2.0 ** -8, float(err.max())
+
+
+@pytest.mark.parametrize("T, D, V", [(2048, 1024, 50257), (64, 32768, 8300)])
+def test_long_sums_cancel(h, T, D, V):
+    """Tens of thousands of products that add up to a part which the label's row takes away again: a sum
+    truncated at every sixteenth product would be off by 2^-25 of itself for each, here 60 times the rows' own
+    part and thousands of steps."""
+    _check(h, *_case(T, D, V, 60.0, 0.0, 0.0, seed=T))
