@@ -732,7 +732,7 @@ __global__ void __launch_bounds__(1024, ROWS == 4 ? 1 : 2) sq_head_finalize_kern
   const int own = lane % ROWS;  // of the CTA's rows
   const int r = min(r0 + own, rows - 1), row = first + r;  // lanes past the last row repeat it
   const bool on = r0 < rows;
-  const float z = on ? __ldcg(a.label_z + row) : 0.f, z2 = z * kLog2e;
+  const float z = on ? __ldcg(a.label_z + row) : 0.f;
   const int t = on ? __ldcg(a.token + row) : 0;
   const float g = on && a.dX ? __ldcg(a.dloss + t) : 0.f;
   dependency_wait();
@@ -809,10 +809,11 @@ __global__ void __launch_bounds__(1024, ROWS == 4 ? 1 : 2) sq_head_finalize_kern
   if (a.e)
     for (int w = 0; w < 32; ++w) others_e += parts_e[w][own];
   a.moved[r] = 0;  // for the next chunk
-  const float label = exp2_fast(z2 - top), total = others + label;
+  const float above = fmaf(z, kLog2e, -top);  // once rounded, as the others' exponents are
+  const float label = exp2_fast(above), total = others + label;
   // log(total / label): where label underflows against a far larger logit, from the exponents
-  const bool near = top - z2 < 60.f;
-  const float loss = near ? log1pf(others / label) : (top - z2) * kLn2 + logf(total);
+  const bool near = above > -60.f;
+  const float loss = near ? log1pf(others / label) : logf(total) - above * kLn2;
   if (a.loss) a.loss[t] = loss;
   if (a.lse) a.lse[t] = near ? z + loss : top * kLn2 + logf(total);
   if (a.e) a.factors[row] = make_float2(g * (others / total), others_e > 0.f ? 1.f / others_e : 0.f);
