@@ -58,6 +58,16 @@ __device__ __forceinline__ float exp_of(float d) {
   return y;
 }
 
+// The same to 2^-22 for any d, of the weights themselves: what the product and the constant round off
+// comes back to first order.
+__device__ __forceinline__ float exp_close(float d) {
+  constexpr float kLog2e = 1.44269504f, kRest = 1.92596299e-8f;  // log2(e) = kLog2e + kRest
+  d = fmaxf(d, -200.f);  // 0 from there on
+  const float t = d * kLog2e, rest = fmaf(d, kRest, fmaf(d, kLog2e, -t));
+  const float y = exp_of(d);
+  return fmaf(y, rest * 0.6931471805599453f, y);
+}
+
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(kAll, v, d);
@@ -181,7 +191,7 @@ __global__ void __launch_bounds__(256)
       order[g] = pop ? order[g] >> 2 : order[g];
     }
   }
-  const float w = my_expert >= 0 ? exp_of(my_value - top) : 0.f;
+  const float w = my_expert >= 0 ? exp_close(my_value - top) : 0.f;
   if (normalize) total = lanes_sum<LANES>(w);
   if (t < tokens && lane < k) {
     experts[t * k + lane] = my_expert;
@@ -215,7 +225,7 @@ __global__ void __launch_bounds__(256)
     for (int i = 1; i < PER; ++i) top = fmaxf(top, dense[i]);
     top = lanes_max<LANES>(top);
   }
-  const float mine = z > -INFINITY ? exp_of(z - top) : 0.f;
+  const float mine = z > -INFINITY ? exp_close(z - top) : 0.f;
   float total = 0.f;
   if (normalize) {
     total = mine;
