@@ -34,7 +34,9 @@
  *  - codes [N, K/2] u8: element k of row n is nibble (k & 1) of byte k/2, the even
  *    k in the low nibble. scales [N, K/B] u8.
  *  - Shape rules: N > 0 with N % 8 == 0; K > 0 with K % 32 == 0; M >= 0 (M == 0
- *    is an empty batch). Every device pointer must be 16-byte aligned.
+ *    is an empty batch). Every device pointer must be 16-byte aligned, but for what
+ *    routing and the head loss take one element at a time: labels, dloss, experts,
+ *    weights, dweights and row_of need the alignment of their type.
  *  - Argument errors return SQ_ERR_INVALID_ARG before anything is launched; the
  *    text is in sq_last_error(h). No exception or abort crosses the ABI.
  *  - A handle is not thread-safe; use one handle per host thread. The scratch a

@@ -203,6 +203,15 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _staged(t: torch.Tensor, stream) -> torch.Tensor:
+    """A copy of t made on the call's stream, from memory that is used again only behind that stream's work."""
+    raw = _stream(stream)
+    if raw == _stream(None):
+        return t.clone()
+    with torch.cuda.stream(torch.cuda.ExternalStream(raw)):
+        return t.clone()
+
+
 class Handle:
     """Owns one sq_handle (not thread-safe: one per host thread)."""
 
@@ -553,10 +562,14 @@ class Handle:
             weights = torch.empty(T, k, dtype=torch.float32, device=dev)
         bf16 = logits.dtype == torch.bfloat16
         if valid is not None:
-            valid = _arg(valid, "valid", torch.bool if valid.dtype == torch.bool else torch.uint8, (T,), dev)
+            mask = torch.bool if valid.dtype == torch.bool else torch.uint8
+            ptr = _arg(valid, "valid", mask, (T,), dev)
+            if ptr % 16:  # one sequence's row of a batch's mask
+                valid = _staged(valid, stream)
+                ptr = valid.data_ptr()
         self._check(self._L.sq_route(
-            self._h, T, E, k, bf16, _arg(logits, "logits", torch.bfloat16 if bf16 else torch.float32, (T, E)), valid,
-            bool(normalize), _arg(experts, "experts", torch.int32, (T, k), dev),
+            self._h, T, E, k, bf16, _arg(logits, "logits", torch.bfloat16 if bf16 else torch.float32, (T, E)),
+            None if valid is None else ptr, bool(normalize), _arg(experts, "experts", torch.int32, (T, k), dev),
             _arg(weights, "weights", torch.float32, (T, k), dev), _stream(stream)))
         return experts, weights
 

@@ -197,6 +197,15 @@ sq_status check_buf(sq_handle h, const void *p, const char *name) {
   return SQ_OK;
 }
 
+// Tensors that are read and written by single elements: slices of a user's own (the labels from the second
+// token on, one sequence's of a batch) start on an element, no more.
+template <typename T>
+sq_status check_elements(sq_handle h, const T *p, const char *name) {
+  if (!p || reinterpret_cast<uintptr_t>(p) % sizeof(T) != 0)
+    return fail(h, SQ_ERR_INVALID_ARG, "%s must be non-NULL and %d-byte aligned", name, static_cast<int>(sizeof(T)));
+  return SQ_OK;
+}
+
 #define SQ_TRY(expr)                    \
   do {                                  \
     sq_status _s = (expr);              \
@@ -1488,8 +1497,8 @@ sq_status sq_route(sq_handle h, int64_t T, int32_t E, int32_t k, int32_t logits_
   SQ_TRY(check_route(h, T, E, k));
   if (T > 0) {
     SQ_TRY(check_buf(h, logits, "logits"));
-    SQ_TRY(check_buf(h, experts, "experts"));
-    SQ_TRY(check_buf(h, weights, "weights"));
+    SQ_TRY(check_elements(h, experts, "experts"));
+    SQ_TRY(check_elements(h, weights, "weights"));
     if (!aligned16(valid)) return fail(h, SQ_ERR_INVALID_ARG, "valid must be 16-byte aligned");
   }
   DeviceState *dev = nullptr;
@@ -1510,8 +1519,8 @@ sq_status sq_route_grad(sq_handle h, int64_t T, int32_t E, int32_t k, int32_t lo
   SQ_TRY(check_route(h, T, E, k));
   if (T > 0) {
     SQ_TRY(check_buf(h, logits, "logits"));
-    SQ_TRY(check_buf(h, experts, "experts"));
-    SQ_TRY(check_buf(h, dweights, "dweights"));
+    SQ_TRY(check_elements(h, experts, "experts"));
+    SQ_TRY(check_elements(h, dweights, "dweights"));
     SQ_TRY(check_buf(h, dlogits, "dlogits"));
   }
   DeviceState *dev = nullptr;
@@ -1532,8 +1541,8 @@ sq_status sq_sort_tokens(sq_handle h, int64_t n, int32_t E, const int32_t *exper
   if (n < 0 || n > kMaxTokens) return fail(h, SQ_ERR_INVALID_ARG, "n=%lld slots out of range [0, 2^31)", (long long)n);
   SQ_TRY(check_buf(h, offsets, "offsets"));
   if (n > 0) {
-    SQ_TRY(check_buf(h, experts, "experts"));
-    SQ_TRY(check_buf(h, row_of, "row_of"));
+    SQ_TRY(check_elements(h, experts, "experts"));
+    SQ_TRY(check_elements(h, row_of, "row_of"));
     SQ_TRY(check_buf(h, slot_of, "slot_of"));
   }
   DeviceState *dev = nullptr;
@@ -1555,7 +1564,7 @@ sq_status sq_dispatch(sq_handle h, int64_t T, int32_t k, int64_t D, int64_t R, c
   SQ_TRY(check_move(h, T, k, D, R));
   if (R > 0) {
     SQ_TRY(check_buf(h, X, "X"));
-    SQ_TRY(check_buf(h, row_of, "row_of"));
+    SQ_TRY(check_elements(h, row_of, "row_of"));
     SQ_TRY(check_buf(h, slot_of, "slot_of"));
     SQ_TRY(check_buf(h, Xs, "Xs"));
   }
@@ -1575,8 +1584,8 @@ sq_status sq_combine(sq_handle h, int64_t T, int32_t k, int64_t D, int64_t R, co
   SQ_TRY(check_move(h, T, k, D, R));
   if (T > 0) {
     if (R > 0) SQ_TRY(check_buf(h, Ys, "Ys"));
-    SQ_TRY(check_buf(h, row_of, "row_of"));
-    SQ_TRY(check_buf(h, weights, "weights"));
+    SQ_TRY(check_elements(h, row_of, "row_of"));
+    SQ_TRY(check_elements(h, weights, "weights"));
     SQ_TRY(check_buf(h, Y, "Y"));
   }
   DeviceState *dev = nullptr;
@@ -1596,7 +1605,7 @@ sq_status sq_dispatch_grad(sq_handle h, int64_t T, int32_t k, int64_t D, int64_t
   SQ_TRY(check_move(h, T, k, D, R));
   if (T > 0) {
     if (R > 0) SQ_TRY(check_buf(h, dXs, "dXs"));
-    SQ_TRY(check_buf(h, row_of, "row_of"));
+    SQ_TRY(check_elements(h, row_of, "row_of"));
     SQ_TRY(check_buf(h, dX, "dX"));
   }
   DeviceState *dev = nullptr;
@@ -1621,10 +1630,10 @@ sq_status sq_combine_grad(sq_handle h, int64_t T, int32_t k, int64_t D, int64_t 
       SQ_TRY(check_buf(h, Ys, "Ys"));
       SQ_TRY(check_buf(h, dYs, "dYs"));
     }
-    SQ_TRY(check_buf(h, row_of, "row_of"));
+    SQ_TRY(check_elements(h, row_of, "row_of"));
     SQ_TRY(check_buf(h, slot_of, "slot_of"));
-    SQ_TRY(check_buf(h, weights, "weights"));
-    SQ_TRY(check_buf(h, dweights, "dweights"));
+    SQ_TRY(check_elements(h, weights, "weights"));
+    SQ_TRY(check_elements(h, dweights, "dweights"));
   }
   DeviceState *dev = nullptr;
   SQ_TRY(ensure_device(h, &dev));
@@ -1645,7 +1654,7 @@ sq_status sq_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint1
   if (T > 0) {
     SQ_TRY(check_buf(h, X, "X"));
     SQ_TRY(check_buf(h, W, "W"));
-    SQ_TRY(check_buf(h, labels, "labels"));
+    SQ_TRY(check_elements(h, labels, "labels"));
   }
   if (!aligned16(loss)) return fail(h, SQ_ERR_INVALID_ARG, "loss must be 16-byte aligned");
   if (!aligned16(lse)) return fail(h, SQ_ERR_INVALID_ARG, "lse must be 16-byte aligned");
@@ -1662,8 +1671,8 @@ sq_status sq_head_loss_grad(sq_handle h, int64_t T, int64_t D, int64_t V, const 
   if (T > 0) {
     SQ_TRY(check_buf(h, X, "X"));
     SQ_TRY(check_buf(h, W, "W"));
-    SQ_TRY(check_buf(h, labels, "labels"));
-    SQ_TRY(check_buf(h, dloss, "dloss"));
+    SQ_TRY(check_elements(h, labels, "labels"));
+    SQ_TRY(check_elements(h, dloss, "dloss"));
     SQ_TRY(check_buf(h, dX, "dX"));
     if (X == dX) return fail(h, SQ_ERR_INVALID_ARG, "dX must not be X");
   }
