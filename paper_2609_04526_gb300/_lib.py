@@ -184,11 +184,15 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 def _arg(t: torch.Tensor, name: str, dtype, shape, device=None):
-    """Pointer of a tensor argument that has to be dense, of one type and shape (and device)."""
+    """Pointer of a tensor argument that has to be dense, of one type and shape, and on the others' device:
+    without one, on the current CUDA device, where the call is launched."""
     if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, not "
                          f"{t.dtype} {tuple(t.shape)} with strides {t.stride()}")
-    if device is not None and t.device != device:
+    if device is None:
+        if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
+            raise ValueError(f"{name} is on {t.device}, not on the current CUDA device")
+    elif t.device != device:
         raise ValueError(f"{name} is on {t.device}, the other arguments on {device}")
     return t.data_ptr()
 
@@ -561,6 +565,7 @@ class Handle:
         if weights is None:
             weights = torch.empty(T, k, dtype=torch.float32, device=dev)
         bf16 = logits.dtype == torch.bfloat16
+        z = _arg(logits, "logits", torch.bfloat16 if bf16 else torch.float32, (T, E))
         if valid is not None:
             mask = torch.bool if valid.dtype == torch.bool else torch.uint8
             ptr = _arg(valid, "valid", mask, (T,), dev)
@@ -568,9 +573,9 @@ class Handle:
                 valid = _staged(valid, stream)
                 ptr = valid.data_ptr()
         self._check(self._L.sq_route(
-            self._h, T, E, k, bf16, _arg(logits, "logits", torch.bfloat16 if bf16 else torch.float32, (T, E)),
-            None if valid is None else ptr, bool(normalize), _arg(experts, "experts", torch.int32, (T, k), dev),
-            _arg(weights, "weights", torch.float32, (T, k), dev), _stream(stream)))
+            self._h, T, E, k, bf16, z, None if valid is None else ptr, bool(normalize),
+            _arg(experts, "experts", torch.int32, (T, k), dev), _arg(weights, "weights", torch.float32, (T, k), dev),
+            _stream(stream)))
         return experts, weights
 
     def sq_route_grad(self, logits: torch.Tensor, experts: torch.Tensor, dweights: torch.Tensor,
