@@ -207,6 +207,17 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _empty(stream, *shape, dtype, device) -> torch.Tensor:
+    """An output of a call on `stream`. Its memory is that stream's: nothing queued on another one still reads it.
+    It is not used again before what the current stream, where the caller goes on, has queued by then."""
+    if stream is None or device.type != "cuda" or _stream(stream) == _stream(None):
+        return torch.empty(*shape, dtype=dtype, device=device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream))):
+        t = torch.empty(*shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream())
+    return t
+
+
 def _staged(t: torch.Tensor, stream) -> torch.Tensor:
     """A copy of t made on the call's stream, from memory that is used again only behind that stream's work."""
     raw = _stream(stream)
@@ -261,7 +272,7 @@ class Handle:
     def sq_fwd(self, w: QuantWeight, X: torch.Tensor, Y: Optional[torch.Tensor] = None, stream=None):
         M = X.shape[0]
         if Y is None:
-            Y = torch.empty(M, w.N, dtype=torch.bfloat16, device=X.device)
+            Y = _empty(stream, M, w.N, dtype=torch.bfloat16, device=X.device)
         wc = w._c()
         self._check(self._L.sq_fwd(self._h, ctypes.byref(wc), _ptr(X), M, _ptr(Y), _stream(stream)))
         return Y
@@ -269,7 +280,7 @@ class Handle:
     def sq_bwd_dx(self, w: QuantWeight, dY: torch.Tensor, dX: Optional[torch.Tensor] = None, stream=None):
         M = dY.shape[0]
         if dX is None:
-            dX = torch.empty(M, w.K, dtype=torch.bfloat16, device=dY.device)
+            dX = _empty(stream, M, w.K, dtype=torch.bfloat16, device=dY.device)
         wc = w._c()
         self._check(self._L.sq_bwd_dx(self._h, ctypes.byref(wc), _ptr(dY), M, _ptr(dX), _stream(stream)))
         return dX
@@ -287,7 +298,7 @@ class Handle:
                       g: Optional[torch.Tensor] = None, stream=None):
         M = X.shape[0]
         if g is None:
-            g = torch.empty(w.N, w.K // BLOCK[w.fmt], dtype=torch.float32, device=X.device)
+            g = _empty(stream, w.N, w.K // BLOCK[w.fmt], dtype=torch.float32, device=X.device)
         wc = w._c()
         self._check(self._L.sq_scale_grad(self._h, ctypes.byref(wc), _ptr(X), _ptr(dY), M, _ptr(mask), _ptr(g),
                                           _stream(stream)))
@@ -298,9 +309,9 @@ class Handle:
                           want_mask: bool = True, stream=None):
         N, G = latent.shape
         if bytes_out is None:
-            bytes_out = torch.empty(N, G, dtype=torch.uint8, device=latent.device)
+            bytes_out = _empty(stream, N, G, dtype=torch.uint8, device=latent.device)
         if mask_out is None and want_mask:
-            mask_out = torch.empty(N, G, dtype=torch.uint8, device=latent.device)
+            mask_out = _empty(stream, N, G, dtype=torch.uint8, device=latent.device)
         self._check(self._L.sq_project_scales(self._h, fmt, N, G, ws2, _ptr(latent), _ptr(bytes_out), _ptr(mask_out),
                                               _ptr(nonfinite), _stream(stream)))
         return bytes_out, mask_out
@@ -314,7 +325,7 @@ class Handle:
         N, G = base_scales.shape
         r = B.shape[1]
         if bytes_out is None:
-            bytes_out = torch.empty(N, G, dtype=torch.uint8, device=base_scales.device)
+            bytes_out = _empty(stream, N, G, dtype=torch.uint8, device=base_scales.device)
         self._check(self._L.sq_project_lowrank(self._h, fmt, N, G, r, ws2, alpha_over_r, _ptr(base_scales), _ptr(B),
                                                _ptr(A), _ptr(bytes_out), _ptr(mask_out), _ptr(nonfinite),
                                                _ptr(latent_out), _stream(stream)))
@@ -328,9 +339,9 @@ class Handle:
         N, G = g.shape
         r = B.shape[1]
         if dB is None and want_dB:
-            dB = torch.empty(N, r, dtype=torch.float32, device=g.device)
+            dB = _empty(stream, N, r, dtype=torch.float32, device=g.device)
         if dA is None and want_dA:
-            dA = torch.empty(r, G, dtype=torch.float32, device=g.device)
+            dA = _empty(stream, r, G, dtype=torch.float32, device=g.device)
         self._check(self._L.sq_lowrank_grad(self._h, N, G, r, alpha_over_r, _ptr(g), _ptr(B), _ptr(A), _ptr(dB),
                                             _ptr(dA), _stream(stream)))
         return dB, dA
@@ -354,7 +365,7 @@ class Handle:
     def sq_count_diff(self, a: torch.Tensor, b: torch.Tensor, count: Optional[torch.Tensor] = None, stream=None):
         """Device int64 tensor holding the number of differing bytes of a and b."""
         if count is None:
-            count = torch.empty(1, dtype=torch.int64, device=a.device)
+            count = _empty(stream, 1, dtype=torch.int64, device=a.device)
         nbytes = a.numel() * a.element_size()
         assert b.numel() * b.element_size() == nbytes
         self._check(self._L.sq_count_diff(self._h, _ptr(a), _ptr(b), nbytes, _ptr(count), _stream(stream)))
@@ -394,7 +405,7 @@ class Handle:
         """Y rows offsets[e]..offsets[e+1]-1 = X rows of expert e times W_e^T (offsets: E + 1 host ints)."""
         off, vals = _offsets(offsets, w.E)
         if Y is None:
-            Y = torch.empty(vals[-1], w.N, dtype=torch.bfloat16, device=X.device)
+            Y = _empty(stream, vals[-1], w.N, dtype=torch.bfloat16, device=X.device)
         wc, keep = w._c()
         self._check(self._L.sq_grouped_fwd(self._h, ctypes.byref(wc), off, _ptr(X), _ptr(Y), _stream(stream)))
         return Y
@@ -403,7 +414,7 @@ class Handle:
                           stream=None):
         off, vals = _offsets(offsets, w.E)
         if dX is None:
-            dX = torch.empty(vals[-1], w.K, dtype=torch.bfloat16, device=dY.device)
+            dX = _empty(stream, vals[-1], w.K, dtype=torch.bfloat16, device=dY.device)
         wc, keep = w._c()
         self._check(self._L.sq_grouped_bwd_dx(self._h, ctypes.byref(wc), off, _ptr(dY), _ptr(dX), _stream(stream)))
         return dX
@@ -413,7 +424,7 @@ class Handle:
         """g [E, N, K/B] fp32: every expert's block-reduced scale gradient over its own rows."""
         off, _ = _offsets(offsets, w.E)
         if g is None:
-            g = torch.empty(w.E, w.N, w.K // BLOCK[w.fmt], dtype=torch.float32, device=X.device)
+            g = _empty(stream, w.E, w.N, w.K // BLOCK[w.fmt], dtype=torch.float32, device=X.device)
         wc, keep = w._c()
         self._check(self._L.sq_grouped_scale_grad(self._h, ctypes.byref(wc), off, _ptr(X), _ptr(dY), _ptr(mask),
                                                   _ptr(g), _stream(stream)))
@@ -424,9 +435,9 @@ class Handle:
                                   want_mask: bool = True, stream=None):
         """Project every expert's latent plane [E, N, G] with its own ws2. Returns (bytes, mask)."""
         if bytes_out is None:
-            bytes_out = torch.empty(latent.shape, dtype=torch.uint8, device=latent.device)
+            bytes_out = _empty(stream, latent.shape, dtype=torch.uint8, device=latent.device)
         if mask_out is None and want_mask:
-            mask_out = torch.empty(latent.shape, dtype=torch.uint8, device=latent.device)
+            mask_out = _empty(stream, latent.shape, dtype=torch.uint8, device=latent.device)
         wc, keep = w._c()
         self._check(self._L.sq_grouped_project_scales(self._h, ctypes.byref(wc), _ptr(latent), _ptr(bytes_out),
                                                       _ptr(mask_out), _ptr(nonfinite), _stream(stream)))
@@ -449,7 +460,7 @@ class Handle:
         projected with its ws2. B [E, N, r], A [E, r, G] bf16. Returns (bytes, mask, latent)."""
         r = B.shape[2]
         if bytes_out is None:
-            bytes_out = torch.empty(w.scales.shape, dtype=torch.uint8, device=w.scales.device)
+            bytes_out = _empty(stream, w.scales.shape, dtype=torch.uint8, device=w.scales.device)
         wc, keep = w._c()
         self._check(self._L.sq_grouped_project_lowrank(self._h, ctypes.byref(wc), r, alpha_over_r, _ptr(B), _ptr(A),
                                                        _ptr(bytes_out), _ptr(mask_out), _ptr(nonfinite),
@@ -463,9 +474,9 @@ class Handle:
         E, N, G = g.shape
         r = B.shape[2]
         if dB is None and want_dB:
-            dB = torch.empty(E, N, r, dtype=torch.float32, device=g.device)
+            dB = _empty(stream, E, N, r, dtype=torch.float32, device=g.device)
         if dA is None and want_dA:
-            dA = torch.empty(E, r, G, dtype=torch.float32, device=g.device)
+            dA = _empty(stream, E, r, G, dtype=torch.float32, device=g.device)
         self._check(self._L.sq_grouped_lowrank_grad(self._h, E, N, G, r, alpha_over_r, _ptr(g), _ptr(B), _ptr(A),
                                                     _ptr(dB), _ptr(dA), _stream(stream)))
         return dB, dA
@@ -479,10 +490,10 @@ class Handle:
         unless asked for (energies with want_energy, the latent when scales are given)."""
         N, K = dW.shape
         G = K // BLOCK[fmt]
-        delta = torch.empty(N, G, dtype=torch.float32, device=dW.device)
-        cap = torch.empty_like(delta) if want_energy else None
-        tot = torch.empty_like(delta) if want_energy else None
-        lat = torch.empty_like(delta) if scales is not None else None
+        delta = _empty(stream, N, G, dtype=torch.float32, device=dW.device)
+        cap = _empty(stream, N, G, dtype=torch.float32, device=dW.device) if want_energy else None
+        tot = _empty(stream, N, G, dtype=torch.float32, device=dW.device) if want_energy else None
+        lat = _empty(stream, N, G, dtype=torch.float32, device=dW.device) if scales is not None else None
         self._check(self._L.sq_fit_scale_delta(self._h, fmt, N, K, ws2, _ptr(codes), _ptr(scales), _ptr(dW),
                                                _ptr(delta), _ptr(cap), _ptr(tot), _ptr(lat), _stream(stream)))
         return delta, cap, tot, lat
@@ -491,7 +502,7 @@ class Handle:
         """Gradient of per-group scale deltas: sums of each group's G / gd block gradients, [N, gd]."""
         N, G = g.shape
         if out is None:
-            out = torch.empty(N, gd, dtype=torch.float32, device=g.device)
+            out = _empty(stream, N, gd, dtype=torch.float32, device=g.device)
         self._check(self._L.sq_group_reduce(self._h, N, G, gd, _ptr(g), _ptr(out), _stream(stream)))
         return out
 
@@ -503,7 +514,7 @@ class Handle:
         N, G = base_scales.shape
         gd = delta.shape[1]
         if bytes_out is None:
-            bytes_out = torch.empty(N, G, dtype=torch.uint8, device=base_scales.device)
+            bytes_out = _empty(stream, N, G, dtype=torch.uint8, device=base_scales.device)
         self._check(self._L.sq_project_group_delta(self._h, fmt, N, G, gd, ws2, _ptr(base_scales), _ptr(delta),
                                                    _ptr(bytes_out), _ptr(mask_out), _ptr(nonfinite), _ptr(latent_out),
                                                    _stream(stream)))
@@ -516,7 +527,7 @@ class Handle:
         N, K = W.shape
         M = X.shape[0]
         if Y is None:
-            Y = torch.empty(M, N, dtype=torch.bfloat16, device=X.device)
+            Y = _empty(stream, M, N, dtype=torch.bfloat16, device=X.device)
         cw = _SqControlWeight(N, K, _ptr(W), _ptr(dS))
         self._check(self._L.sq_control_fwd(self._h, ctypes.byref(cw), _ptr(X), M, _ptr(Y), _stream(stream)))
         return Y
@@ -526,7 +537,7 @@ class Handle:
         N, K = W.shape
         M = dY.shape[0]
         if dX is None:
-            dX = torch.empty(M, K, dtype=torch.bfloat16, device=dY.device)
+            dX = _empty(stream, M, K, dtype=torch.bfloat16, device=dY.device)
         cw = _SqControlWeight(N, K, _ptr(W), _ptr(dS))
         self._check(self._L.sq_control_bwd_dx(self._h, ctypes.byref(cw), _ptr(dY), M, _ptr(dX), _stream(stream)))
         return dX
@@ -537,7 +548,7 @@ class Handle:
         N, K = W.shape
         M = X.shape[0]
         if g is None:
-            g = torch.empty(N, K // 16, dtype=torch.float32, device=X.device)
+            g = _empty(stream, N, K // 16, dtype=torch.float32, device=X.device)
         cw = _SqControlWeight(N, K, _ptr(W), None)
         self._check(self._L.sq_control_grad(self._h, ctypes.byref(cw), _ptr(X), _ptr(dY), M, _ptr(g), _stream(stream)))
         return g
@@ -548,7 +559,7 @@ class Handle:
         N, r = B.shape
         G = A.shape[1]
         if out is None:
-            out = torch.empty(N, G, dtype=torch.float32, device=B.device)
+            out = _empty(stream, N, G, dtype=torch.float32, device=B.device)
         self._check(self._L.sq_lowrank_product(self._h, N, G, r, alpha_over_r, _ptr(B), _ptr(A), _ptr(out),
                                                _stream(stream)))
         return out
@@ -561,9 +572,9 @@ class Handle:
         T, E = logits.shape
         dev = logits.device
         if experts is None:
-            experts = torch.empty(T, k, dtype=torch.int32, device=dev)
+            experts = _empty(stream, T, k, dtype=torch.int32, device=dev)
         if weights is None:
-            weights = torch.empty(T, k, dtype=torch.float32, device=dev)
+            weights = _empty(stream, T, k, dtype=torch.float32, device=dev)
         bf16 = logits.dtype == torch.bfloat16
         z = _arg(logits, "logits", torch.bfloat16 if bf16 else torch.float32, (T, E))
         if valid is not None:
@@ -585,7 +596,7 @@ class Handle:
         k = experts.shape[1]
         dev = logits.device
         if dlogits is None:
-            dlogits = torch.empty_like(logits)
+            dlogits = _empty(stream, logits.shape, dtype=logits.dtype, device=dev)
         bf16 = logits.dtype == torch.bfloat16
         z = torch.bfloat16 if bf16 else torch.float32
         self._check(self._L.sq_route_grad(
@@ -600,11 +611,11 @@ class Handle:
         on the device), row_of int32 [T, k] (-1: none) and slot_of int32 [T * k] (-1: no slot)."""
         dev, n = experts.device, experts.numel()
         if offsets is None:
-            offsets = torch.empty(E + 1, dtype=torch.int64, device=dev)
+            offsets = _empty(stream, E + 1, dtype=torch.int64, device=dev)
         if row_of is None:
-            row_of = torch.empty(experts.shape, dtype=torch.int32, device=dev)
+            row_of = _empty(stream, experts.shape, dtype=torch.int32, device=dev)
         if slot_of is None:
-            slot_of = torch.empty(n, dtype=torch.int32, device=dev)
+            slot_of = _empty(stream, n, dtype=torch.int32, device=dev)
         self._check(self._L.sq_sort_tokens(
             self._h, n, E, _arg(experts, "experts", torch.int32, experts.shape),
             _arg(offsets, "offsets", torch.int64, (E + 1,), dev), _arg(row_of, "row_of", torch.int32, experts.shape, dev),
@@ -619,7 +630,7 @@ class Handle:
         k = row_of.shape[1]
         dev, bf16 = X.device, torch.bfloat16
         if Xs is None:
-            Xs = torch.empty(T * k, D, dtype=bf16, device=dev)
+            Xs = _empty(stream, T * k, D, dtype=bf16, device=dev)
         R = Xs.shape[0]
         self._check(self._L.sq_dispatch(
             self._h, T, k, D, R, _arg(X, "X", bf16, (T, D)), _arg(row_of, "row_of", torch.int32, (T, k), dev),
@@ -633,7 +644,7 @@ class Handle:
         T, k = row_of.shape
         dev, bf16 = dXs.device, torch.bfloat16
         if dX is None:
-            dX = torch.empty(T, D, dtype=bf16, device=dev)
+            dX = _empty(stream, T, D, dtype=bf16, device=dev)
         self._check(self._L.sq_dispatch_grad(
             self._h, T, k, D, R, _arg(dXs, "dXs", bf16, (R, D)), _arg(row_of, "row_of", torch.int32, (T, k), dev),
             _arg(dX, "dX", bf16, (T, D), dev), _stream(stream)))
@@ -646,7 +657,7 @@ class Handle:
         T, k = row_of.shape
         dev, bf16 = Ys.device, torch.bfloat16
         if Y is None:
-            Y = torch.empty(T, D, dtype=bf16, device=dev)
+            Y = _empty(stream, T, D, dtype=bf16, device=dev)
         self._check(self._L.sq_combine(
             self._h, T, k, D, R, _arg(Ys, "Ys", bf16, (R, D)), _arg(row_of, "row_of", torch.int32, (T, k), dev),
             _arg(weights, "weights", torch.float32, (T, k), dev), _arg(Y, "Y", bf16, (T, D), dev), _stream(stream)))
@@ -660,9 +671,9 @@ class Handle:
         T, k = row_of.shape
         dev, bf16 = Ys.device, torch.bfloat16
         if dYs is None:
-            dYs = torch.empty(R, D, dtype=bf16, device=dev)
+            dYs = _empty(stream, R, D, dtype=bf16, device=dev)
         if dweights is None:
-            dweights = torch.empty(T, k, dtype=torch.float32, device=dev)
+            dweights = _empty(stream, T, k, dtype=torch.float32, device=dev)
         self._check(self._L.sq_combine_grad(
             self._h, T, k, D, R, _arg(dY, "dY", bf16, (T, D), dev), _arg(Ys, "Ys", bf16, (R, D)),
             _arg(row_of, "row_of", torch.int32, (T, k), dev), _arg(slot_of, "slot_of", torch.int32, (T * k,), dev),
@@ -679,9 +690,9 @@ class Handle:
         V = W.shape[0]
         dev = X.device
         if loss is None:
-            loss = torch.empty(T, dtype=torch.float32, device=dev)
+            loss = _empty(stream, T, dtype=torch.float32, device=dev)
         if lse is None:
-            lse = torch.empty(T, dtype=torch.float32, device=dev)
+            lse = _empty(stream, T, dtype=torch.float32, device=dev)
         self._check(self._L.sq_head_loss(
             self._h, T, D, V, _arg(X, "X", torch.bfloat16, (T, D)), _arg(W, "W", torch.bfloat16, (V, D), dev),
             _arg(labels, "labels", torch.int64, (T,), dev), _arg(loss, "loss", torch.float32, (T,), dev),
@@ -697,11 +708,11 @@ class Handle:
         V = W.shape[0]
         dev = X.device
         if loss is None:
-            loss = torch.empty(T, dtype=torch.float32, device=dev)
+            loss = _empty(stream, T, dtype=torch.float32, device=dev)
         if lse is None:
-            lse = torch.empty(T, dtype=torch.float32, device=dev)
+            lse = _empty(stream, T, dtype=torch.float32, device=dev)
         if dX is None:
-            dX = torch.empty(T, D, dtype=torch.bfloat16, device=dev)
+            dX = _empty(stream, T, D, dtype=torch.bfloat16, device=dev)
         self._check(self._L.sq_head_loss_grad(
             self._h, T, D, V, _arg(X, "X", torch.bfloat16, (T, D)), _arg(W, "W", torch.bfloat16, (V, D), dev),
             _arg(labels, "labels", torch.int64, (T,), dev), _arg(dloss, "dloss", torch.float32, (T,), dev),
