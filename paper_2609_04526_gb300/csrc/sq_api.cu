@@ -1650,8 +1650,8 @@ sq_status sq_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint1
   if (!h) return SQ_ERR_INVALID_ARG;
   SQ_GUARD_BEGIN
   SQ_TRY(check_head(h, T, D, V));
-  if (!loss && !lse) return fail(h, SQ_ERR_INVALID_ARG, "loss and lse are both NULL");
   if (T > 0) {
+    if (!loss && !lse) return fail(h, SQ_ERR_INVALID_ARG, "loss and lse are both NULL");
     SQ_TRY(check_buf(h, X, "X"));
     SQ_TRY(check_buf(h, W, "W"));
     SQ_TRY(check_elements(h, labels, "labels"));
