@@ -526,9 +526,12 @@ sq_status sq_combine_grad(sq_handle h, int64_t T, int32_t k, int64_t D, int64_t 
  * [0, V) (such as -100) marks a token that is not a target: its row is not read into any result,
  * its loss and lse are 0 and its dX row is zero. loss, lse device fp32 [T] or NULL (overwritten).
  * Results do not differ from run to run, and the loss and lse of a token not with the tokens beside
- * it. Uses scratch of the handle, its size bounded for any T: the packed rows of up to 16,384 tokens
- * and up to 512 MiB of sums, or, with the gradient, of bf16 exponentials, and the fp32 partial planes
- * of that chunk. */
+ * it. Uses scratch of the handle, its size bounded for any T:
+ *   the packed rows of up to 16,384 tokens, 2 D bytes each;
+ *   without the gradient up to 512 MiB of sums;
+ *   with it the bf16 exponentials of a chunk of tokens, 512 MiB or, where 256 tokens have more (V above
+ *   2^20), 2 V bytes for each of up to 256; a tenth of that of sums; up to 512 MiB of fp32 partial planes.
+ * A call takes no more of these than its own tokens need. */
 sq_status sq_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint16_t *X, const uint16_t *W,
                        const int64_t *labels, float *loss, float *lse, void *stream);
 

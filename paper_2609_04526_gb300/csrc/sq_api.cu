@@ -453,10 +453,15 @@ sq_status run_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint
   a.width = up(D, 64);
   a.err = dev->err_word;
   const int64_t quarters = 4 * ((V + sqi::kHeadTile - 1) / sqi::kHeadTile);
-  // rows whose exponentials or, without a gradient, sums and references fit the bound
-  const int64_t row_bytes = dX ? 2 * a.pitch : 8 * quarters;
-  const int64_t fit = sqi::kHeadPieceBytes / row_bytes / sqi::kHeadTile * sqi::kHeadTile;
-  const int64_t chunk = std::min(whole, std::max<int64_t>(fit, sqi::kHeadTile));
+  // Rows of a chunk: as many as have exponentials or, without a gradient, sums and references within the
+  // bound, but a whole tile (of a vocabulary above 2^20 less would read W again for a few rows each),
+  // and as have a partial plane within it. Never more than the call has, in steps of a TMA box of few rows.
+  auto tiles_within = [](int64_t row_bytes) {
+    return sqi::kHeadPieceBytes / row_bytes / sqi::kHeadTile * sqi::kHeadTile;
+  };
+  int64_t chunk = std::max<int64_t>(tiles_within(dX ? 2 * a.pitch : 8 * quarters), sqi::kHeadTile);
+  if (dX) chunk = std::min(chunk, tiles_within(4 * a.width));  // at least 2048: D is bounded
+  chunk = std::min(chunk, up(piece, 16));
   a.chunk = static_cast<int>(chunk);
   a.sum_rows = static_cast<int>(up(std::min(piece, chunk), 4));
   a.box_rows = T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128;
@@ -464,9 +469,11 @@ sq_status run_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint
   const int clusters = std::max(1, dev->sm_count / 2);
   a.columns = sqi::head_columns(T, V, a.few, clusters);
   int64_t partial_rows = 0;  // of 4 * D bytes: the most that any number of labelled rows takes
-  for (int64_t m = 1; dX && m <= chunk / sqi::kHeadTile; ++m) {
+  for (int64_t m = 1; dX && m <= (chunk + sqi::kHeadTile - 1) / sqi::kHeadTile; ++m) {
     const int stages = static_cast<int>((V + 127) / 128);  // the gradient's, of 128 vocabulary entries
-    const int parts = sqi::head_parts(std::min(m * sqi::kHeadTile, piece), D, stages, clusters);
+    const int64_t planes = sqi::kHeadPieceBytes / (4 * a.width * m * sqi::kHeadTile);  // within the bound
+    const int parts = static_cast<int>(
+        std::min<int64_t>(sqi::head_parts(std::min(m * sqi::kHeadTile, piece), D, stages, clusters), planes));
     if ((stages + parts - 1) / parts > sqi::kHeadSegment / 128) a.long_sums = true;
     a.parts[m - 1] = static_cast<uint8_t>(parts - 1);
     partial_rows = std::max(partial_rows, m * sqi::kHeadTile * parts);

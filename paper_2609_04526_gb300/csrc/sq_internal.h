@@ -382,8 +382,8 @@ cudaError_t launch_combine_grad(int64_t T, int k, int64_t D, int64_t rows, const
                                 float *dweights, int sm_count, cudaStream_t stream);
 
 // Cross entropy against a vocabulary projection W [V, D] (sq_loss.cu). A call runs over pieces of
-// kHeadPiece tokens, a piece's labelled tokens over chunks whose exponentials (or, without a
-// gradient, sums) fit kHeadPieceBytes of scratch.
+// kHeadPiece tokens, a piece's labelled tokens over chunks of whole tiles whose exponentials (or, without
+// a gradient, sums) fit kHeadPieceBytes of scratch, or of one tile; their partial planes fit it too.
 constexpr int kHeadTile = 256;
 constexpr int kHeadPiece = 16384;
 constexpr int64_t kHeadPieceBytes = int64_t(512) << 20;
@@ -440,7 +440,7 @@ struct HeadArgs {
   bool few;               // box_rows < 128: stages of 128 instead of 64
   int columns;            // of a tile of the logits
   bool long_sums;         // the gradient's parts are longer than kHeadSegment
-  int chunk;              // rows of a chunk, a multiple of kHeadTile
+  int chunk;              // rows of a chunk: a multiple of kHeadTile, or all of a shorter call, up to one of 16
   uint8_t parts[kHeadPiece / kHeadTile];  // vocabulary parts of the gradient by row tiles of the chunk, less 1
   int64_t pitch;          // elements from row to row of e
   int64_t width;          // and of the packed rows and partial planes
