@@ -41,8 +41,10 @@
  *    text is in sq_last_error(h). No exception or abort crosses the ABI.
  *  - A handle is not thread-safe; use one handle per host thread. The scratch a
  *    handle owns (a split scale gradient's partial planes; the adapter kernels'
- *    partial sums) is one buffer per kind and device: calls of one handle that
- *    use it must run on one stream or be ordered by the caller. It is allocated,
+ *    partial sums; the counts of a sort of more than 4096 slots; the head loss's
+ *    rows, sums, exponentials and planes) is one buffer per kind and device:
+ *    calls of one handle that use the same kind must run on one stream or be
+ *    ordered by the caller. It is allocated,
  *    or grown, by the first call that needs it; a call that would grow it while
  *    its stream is being captured into a CUDA graph returns SQ_ERR_UNSUPPORTED,
  *    so make one call outside the capture first. A buffer that a capture has
