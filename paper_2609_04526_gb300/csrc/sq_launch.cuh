@@ -6,8 +6,9 @@
 // reads what the launch ahead of it wrote and before it writes global memory, and dependency_start,
 // which lets the next launch start, only after that. A kernel so starts when the last but one before
 // it has ended, and at most one kernel runs beside the ones that wait. What that last but one wrote,
-// or an older one, may be read before the wait, by a launch that is always behind another one of the
-// same call (whose own wait shows that the call's inputs are complete too).
+// or an older one, may be read before the wait, from the L2 (__ldcg: nothing but the wait says that an
+// SM's own cache holds no older copy), by a launch that is always behind another one of the same call
+// (whose own wait shows that the call's inputs are complete too).
 //
 // Behind its wait a kernel reads memory with ordinary loads alone: the non-coherent ones (__ldg, or
 // a const __restrict__ pointer) are for what nobody writes while the kernel runs, and may be moved

@@ -272,12 +272,14 @@ constexpr int64_t kSortOne = 4096;
 constexpr int64_t kSortMany = 2048;  // slots of a CTA at least, of several
 constexpr int kSortThreads = 1024;   // of a CTA, of several
 
+// EARLY: ahead of the launch's wait, from the L2, where older launches' results are.
+template <bool EARLY = false>
 __device__ __forceinline__ void load_slots(const int *experts, int64_t at, int64_t end, int E, int lane,
                                            int (&e)[kSortStep]) {
 #pragma unroll
   for (int s = 0; s < kSortStep; ++s) {
     const int64_t i = at + 32 * s + lane;
-    e[s] = i < end ? experts[i] : -1;
+    e[s] = i < end ? (EARLY ? __ldcg(experts + i) : experts[i]) : -1;
     if (e[s] >= E) e[s] = -1;
   }
 }
@@ -337,7 +339,7 @@ __global__ void __launch_bounds__(1024)
   int *mine = hist + warp * E;
   for (int64_t at = begin; at < end; at += 32 * kSortStep) {
     int e[kSortStep];
-    load_slots(experts, at, end, E, lane, e);
+    load_slots<true>(experts, at, end, E, lane, e);
 #pragma unroll
     for (int s = 0; s < kSortStep; ++s)
       if (e[s] >= 0) atomicAdd(mine + e[s], 1);
