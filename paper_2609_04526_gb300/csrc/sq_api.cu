@@ -485,9 +485,8 @@ sq_status run_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint
     return at;
   };
   const size_t o_count = take(4), o_token = take(4 * piece), o_label = take(4 * piece), o_z = take(4 * piece),
-               o_factors = take(8 * piece), o_rows = take(2 * a.width * whole), o_sums = take(4 * quarters * chunk),
-               o_refs = take(4 * quarters * chunk), o_sums_e = take(dX ? 4 * quarters * chunk : 0),
-               o_moved = take(4 * chunk),
+               o_factors = take(8 * piece), o_rows = take(2 * a.width * whole), o_sums = take((dX ? 8 : 4) * quarters * chunk),
+               o_refs = take(4 * quarters * chunk), o_moved = take(4 * chunk),
                o_e = take(dX ? 2 * a.pitch * chunk : 0), o_partial = take(4 * a.width * partial_rows);
   SQ_TRY(ensure_scratch(h, dev->head, used, stream, "the head loss"));
   uint8_t *base = static_cast<uint8_t *>(dev->head.ptr);
@@ -502,7 +501,6 @@ sq_status run_head_loss(sq_handle h, int64_t T, int64_t D, int64_t V, const uint
   a.moved = reinterpret_cast<int *>(base + o_moved);
   if (dX) {
     a.e = reinterpret_cast<uint16_t *>(base + o_e);
-    a.sums_e = reinterpret_cast<float *>(base + o_sums_e);
     a.partial = reinterpret_cast<float *>(base + o_partial);
   }
   sqi::HeadMaps m;

@@ -452,8 +452,9 @@ struct HeadArgs {
   uint16_t *rows;         // [T, D] the labelled tokens' rows of X
   // scratch, by row of the chunk
   int sum_rows;           // a chunk's rows, up to a multiple of 4
-  float *sums, *refs;     // [4 * column tiles, sum_rows] sum and reference of each quarter tile
-  float *sums_e;          // likewise, sums of the rounded exponentials (gradient)
+  // [4 * column tiles, sum_rows] of each quarter tile: its sum (with a gradient, float2: and that of its rounded
+  // exponentials) and its reference
+  float *sums, *refs;
   int *moved;             // [chunk] a row whose references differ (refs are read only there)
   uint16_t *e;            // [chunk, pitch] bf16 exponentials (gradient)
   float *partial;         // [parts, rows, D] fp32 (gradient)

@@ -693,8 +693,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HeadCfg<STEP, BK, NT
           __syncwarp();
         }
         if (in) {
-          a.sums[at_sum] = sum;
-          if constexpr (KEEP) a.sums_e[at_sum] = sum_e;
+          if constexpr (KEEP)
+            reinterpret_cast<float2 *>(a.sums)[at_sum] = make_float2(sum, sum_e);
+          else
+            a.sums[at_sum] = sum;
           a.refs[at_sum] = ref;
         }
       }
@@ -723,7 +725,7 @@ __device__ __forceinline__ float2 from_lane(float2 v, int mask) {
 // twice the CTAs (32, whole lines, left most SMs without rows: 14 us for 2048). The order of a row's
 // sum is the same in all, so it depends on nothing but the row: 256 sums of every 256th quarter
 // tile, eight to a warp, then the warps'.
-template <int ROWS>
+template <int ROWS, bool KEEP>
 __global__ void __launch_bounds__(1024, ROWS == 4 ? 1 : 2) sq_head_finalize_kernel(const HeadArgs a, const int first) {
   constexpr int kShare = 32 / ROWS;
   __shared__ float parts[32][ROWS + 1], parts_e[32][ROWS + 1];
@@ -734,13 +736,13 @@ __global__ void __launch_bounds__(1024, ROWS == 4 ? 1 : 2) sq_head_finalize_kern
   const bool on = r0 < rows;
   const float z = on ? __ldcg(a.label_z + row) : 0.f;
   const int t = on ? __ldcg(a.token + row) : 0;
-  const float g = on && a.dX ? __ldcg(a.dloss + t) : 0.f;
+  const float g = on && KEEP ? __ldcg(a.dloss + t) : 0.f;
   dependency_wait();
   dependency_start();
   if (!on) return;
   constexpr int kCols = HeadCfg<HEAD_LOSS, 64, 256>::kEpiCols;
   const int filled = static_cast<int>((a.V + kCols - 1) / kCols);  // quarter tiles that hold columns
-  const float *sums = a.sums + r, *sums_e = a.sums_e + r, *refs = a.refs + r;
+  const float *refs = a.refs + r;
   float top = row_reference(z);
   const bool moved = a.moved[r];
   const bool any = __any_sync(0xFFFFFFFFu, moved);  // the same rows in every warp
@@ -771,28 +773,36 @@ __global__ void __launch_bounds__(1024, ROWS == 4 ? 1 : 2) sq_head_finalize_kern
   auto larger = [](float x, float y) { return fmaxf(x, y); };
   auto plus = [](float x, float y) { return x + y; };
   auto plus2 = [](float2 x, float2 y) { return make_float2(x.x + y.x, x.y + y.y); };
-  auto by_of = [&](int64_t at) { return any ? whole_exp2(refs[at] - top) : 1.f; };
+  // the sums, or with a gradient both kinds, each times `by` of its place
+  auto add_up = [&](auto by) {
+    if constexpr (KEEP) {
+      const float2 *sums = reinterpret_cast<const float2 *>(a.sums) + r;
+      const float2 both = over_tiles(
+          make_float2(0.f, 0.f),
+          [&](int64_t at) {
+            const float2 v = sums[at];
+            const float f = by(at);
+            return make_float2(v.x * f, v.y * f);
+          },
+          plus2);
+      parts[warp][own] = both.x;
+      parts_e[warp][own] = both.y;
+    } else {
+      const float *sums = a.sums + r;
+      parts[warp][own] = over_tiles(0.f, [&](int64_t at) { return sums[at] * by(at); }, plus);
+    }
+  };
   if (any) {  // references differ: the largest of them first
     parts[warp][own] = over_tiles(top, [&](int64_t at) { return refs[at]; }, larger);
     __syncthreads();
     for (int w = 0; w < 32; ++w) top = fmaxf(top, parts[w][own]);
     __syncthreads();
-  }
-  if (a.e) {
-    const float2 both = over_tiles(
-        make_float2(0.f, 0.f),
-        [&](int64_t at) {
-          const float by = by_of(at);
-          return make_float2(sums[at] * by, sums_e[at] * by);
-        },
-        plus2);
-    parts[warp][own] = both.x;
-    parts_e[warp][own] = both.y;
+    add_up([&](int64_t at) { return whole_exp2(refs[at] - top); });
   } else {
-    parts[warp][own] = over_tiles(0.f, [&](int64_t at) { return sums[at] * by_of(at); }, plus);
+    add_up([](int64_t) { return 1.f; });
   }
   __syncthreads();
-  if (any && a.e) {  // the exponentials of moved rows follow their reference
+  if (KEEP && any) {  // the exponentials of moved rows follow their reference
     for (int i = warp; i < filled; i += 32)
       for (int l = 0; l < ROWS && r0 + l < rows; ++l) {
         if (!__shfl_sync(0xFFFFFFFFu, moved, l)) continue;
@@ -806,7 +816,7 @@ __global__ void __launch_bounds__(1024, ROWS == 4 ? 1 : 2) sq_head_finalize_kern
   if (warp > 0 || lane >= ROWS || r0 + lane >= rows) return;
   float others = 0.f, others_e = 0.f;
   for (int w = 0; w < 32; ++w) others += parts[w][own];
-  if (a.e)
+  if constexpr (KEEP)
     for (int w = 0; w < 32; ++w) others_e += parts_e[w][own];
   a.moved[r] = 0;  // for the next chunk
   const float above = fmaf(z, kLog2e, -top);  // once rounded, as the others' exponents are
@@ -816,7 +826,7 @@ __global__ void __launch_bounds__(1024, ROWS == 4 ? 1 : 2) sq_head_finalize_kern
   const float loss = near ? log1pf(others / label) : logf(total) - above * kLn2;
   if (a.loss) a.loss[t] = loss;
   if (a.lse) a.lse[t] = near ? z + loss : top * kLn2 + logf(total);
-  if (a.e) a.factors[row] = make_float2(g * (others / total), others_e > 0.f ? 1.f / others_e : 0.f);
+  if constexpr (KEEP) a.factors[row] = make_float2(g * (others / total), others_e > 0.f ? 1.f / others_e : 0.f);
 }
 
 // dX[token] = f.x (f.y sum over the parts - W[label]). A warp per 256 columns of a row, or, where
@@ -934,10 +944,13 @@ cudaError_t launch_head_chunk(const HeadArgs &a, const HeadMaps &m, int first, i
   cudaError_t e = product(m.rows, m.weights, m.e_store, a, first, tiles_m * ((a.V + a.columns - 1) / a.columns), sm_count,
                           stream);
   if (e != cudaSuccess) return e;
-  if (rows <= 4 * sm_count)
-    e = launch_after(sq_head_finalize_kernel<4>, (rows + 3) / 4, 1024, 0, stream, a, first);
-  else
-    e = launch_after(sq_head_finalize_kernel<8>, (rows + 7) / 8, 1024, 0, stream, a, first);
+  auto finalize = [&](auto keep) {
+    constexpr bool k = decltype(keep)::value;
+    return rows <= 4 * sm_count
+               ? launch_after(sq_head_finalize_kernel<4, k>, (rows + 3) / 4, 1024, 0, stream, a, first)
+               : launch_after(sq_head_finalize_kernel<8, k>, (rows + 7) / 8, 1024, 0, stream, a, first);
+  };
+  e = a.dX ? finalize(std::true_type{}) : finalize(std::false_type{});
   if (e != cudaSuccess || !a.dX) return e;
   const int64_t tiles_d = (a.D + kHeadTile - 1) / kHeadTile;
   int64_t units = 0, parts = 0;  // the most of any number of labelled rows
