@@ -72,7 +72,7 @@ struct HeadCfg {
   static constexpr int kBoxBytes = 32 * kBoxCols * (GRAD ? 4 : 2);  // 32 rows x kBoxCols columns of a warp
   // Stages added up in one accumulator. The tensor core truncates its running fp32 sum at every
   // step of 16, a bias that grows with the length: a sum of 4096 products in one accumulator left
-  // the log-sum-exp 1.4e-5 too small. The logits therefore leave tensor memory every 512 products
+  // the log-sum-exp, of 11 to 14, 1.6e-5 too small (1.6e-6 now). The logits therefore leave tensor memory every 512 products
   // and are added in registers, and so does the gradient, rounded to bf16 in the end, every
   // kHeadSegment.
   static constexpr int kSegment = STEP == HEAD_GRAD ? 1 << 30 : (GRAD ? kHeadSegment : 512) / kBK;
