@@ -189,11 +189,11 @@ def _run_own(s):
     if s["kind"] == "linear":
         h.sq_quantize(fmt, s["X"], ws2=s["xs2"], out=q)
         w = pkg.QuantWeight(fmt, s["N"], K, s["wcodes"][0], s["wscales"][0], s["ws2"][0])
-        h.sq_fp4_fwd(w, q, Y=s["Y"])
+        h.sq_quant_fwd(w, q, Y=s["Y"])
         return {"Y": s["Y"]}
     h.sq_quantize(fmt, s["X"], ws2=s["xs2"], slot_of=s["slot_of"], k=s["k"], out=q)
     w = pkg.GroupedWeight(fmt, s["E"], s["N"], K, s["wcodes"], s["wscales"], s["wws2"])
-    h.sq_grouped_fp4_fwd(w, s["offsets"], q, Y=s["Y"])
+    h.sq_grouped_quant_fwd(w, s["offsets"], q, Y=s["Y"])
     return {"Y": s["Y"]}
 
 
