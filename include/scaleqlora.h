@@ -18,6 +18,8 @@
  *                      an MoE linear, one launch each (Sec. 3)
  *   sq_route, sq_sort_tokens, sq_dispatch, sq_combine and their gradients
  *                      tokens to the experts of an MoE layer and back
+ *   sq_quantize, sq_dequantize  activations to the weights' 4-bit formats and back
+ *   sq_quant_fwd, sq_grouped_quant_fwd  forward with both operands in 4 bits
  *   sq_head_loss, sq_head_loss_grad  cross entropy against the vocabulary projection
  *   sq_fit_scale_delta, sq_group_reduce, sq_project_group_delta, sq_control_*,
  *   sq_lowrank_product scale-family variants of the ablation appendix
@@ -35,8 +37,9 @@
  *    k in the low nibble. scales [N, K/B] u8.
  *  - Shape rules: N > 0 with N % 8 == 0; K > 0 with K % 32 == 0; M >= 0 (M == 0
  *    is an empty batch). Every device pointer must be 16-byte aligned, but for what
- *    routing and the head loss take one element at a time: labels, dloss, experts,
- *    weights, dweights and row_of need the alignment of their type.
+ *    routing, 4-bit rows and the head loss take one element at a time: labels, dloss,
+ *    experts, weights, dweights, row_of and, of 4-bit rows, slot_of, offsets, ws2 and
+ *    row_ws2 need the alignment of their type.
  *  - Argument errors return SQ_ERR_INVALID_ARG before anything is launched; the
  *    text is in sq_last_error(h). No exception or abort crosses the ABI.
  *  - A handle is not thread-safe; use one handle per host thread. The scratch a
@@ -518,6 +521,59 @@ sq_status sq_combine(sq_handle h, int64_t T, int32_t k, int64_t D, int64_t R, co
 sq_status sq_combine_grad(sq_handle h, int64_t T, int32_t k, int64_t D, int64_t R, const uint16_t *dY,
                           const uint16_t *Ys, const int32_t *row_of, const int32_t *slot_of, const float *weights,
                           uint16_t *dYs, float *dweights, void *stream);
+
+/* ---------------------------------------------------------------- 4-bit rows
+ * Activations in the weights' own formats, and products with both operands in 4 bits. A row of K
+ * values is K/2 bytes of E2M1 codes and K/B scale bytes, laid out as a weight's:
+ *   x[r,i] ~ code[r,i] * s[r, i / B] * row[r]
+ * with row[r] = row_ws2[r] (NVFP4: each row's own scale) or, where row_ws2 is NULL, ws2 for all rows
+ * (NVFP4: finite and > 0; MXFP4: exactly 1.0). */
+typedef struct {
+  int32_t fmt;      /* sq_format                                                  */
+  int32_t K;        /* values of a row, K % 32 == 0                               */
+  int64_t R;        /* rows, 0 <= R < 2^31                                        */
+  uint8_t *codes;   /* device [R, K/2]                                            */
+  uint8_t *scales;  /* device [R, K/B]                                            */
+  float ws2;        /* scale of all rows (1.0 with row_ws2)                       */
+  float *row_ws2;   /* device fp32 [R] or NULL; NULL for MXFP4                    */
+} sq_rows;
+
+/* bf16 rows to 4 bits: q's buffers are overwritten. Every rounding is to nearest, ties to even.
+ *  NVFP4: u = x / row, s = max(2^-9, E4M3(max of the block's |u| / 6)), code = E2M1(u / s). With
+ *   q->row_ws2 (overwritten) a row's own scale is the smallest power of two 2^e >= 2^-116 with
+ *   max |x| <= 6 * 448 * 2^e: nothing saturates, and decoded values are normal bf16 numbers (above
+ *   1.29 * 2^127 a block's largest may decode to infinity). Without, u = fl32(x * fl32(1 / ws2)), 2^-126 <=
+ *   ws2 <= 2^126, and s and codes saturate at 448 and 6.
+ *  MXFP4: s = 2^(floor(log2 of the block's largest |x|) - 2), byte clamped to [0, 254]; code =
+ *   E2M1(x / s), saturating at 6.
+ * A block that holds an infinity or NaN gets scale byte 0x7F (NVFP4) or 0xFF, NaN, whatever its codes,
+ * and has no part in its row's own scale.
+ * X device bf16 [T, K]. slot_of device int32 [R] or NULL: NULL, R == T and row r is X[r]; else row r
+ * is X[slot_of[r] / k] (1 <= k <= 32, T * k < 2^31), the row that sq_dispatch would copy there, and a row whose slot
+ * is outside [0, T * k) is a row of zeros. Results of a row do not depend on the rows beside it. */
+sq_status sq_quantize(sq_handle h, const sq_rows *q, int64_t T, int32_t k, const uint16_t *X, const int32_t *slot_of,
+                      void *stream);
+
+/* 4-bit rows back to bf16, X device bf16 [R, K] (overwritten): code * s exactly, times row[r] in fp32,
+ * rounded to bf16. Exact for the rows that sq_quantize writes with their own scales or as MXFP4. In a training
+ * step these are the rows that sq_scale_grad takes where only their 4 bits were kept. */
+sq_status sq_dequantize(sq_handle h, const sq_rows *q, uint16_t *X, void *stream);
+
+/* Forward with both operands in 4 bits, on the tensor cores' block-scaled products:
+ *   Y[m,n] = ws2 row[m] sum_b s_x[m,b] s_w[n,b] sum over k in block b of code_x[m,k] code_w[n,k]
+ * summed in fp32 (a launch of few tiles cuts K into parts and adds them in order), scaled in fp32 and rounded to
+ * bf16. Formats and K of w and x are the same; scale bytes may be negative (NVFP4). Products of scales outside
+ * fp32's range are not kept apart (MXFP4: bytes whose sum is far from 254). w device weight as in sq_fwd;
+ * Y device bf16 [x->R, N] (overwritten). The gradients are sq_bwd_dx and, of the scales, sq_scale_grad
+ * with sq_dequantize's rows: the roundings of x pass them straight through. */
+sq_status sq_quant_fwd(sq_handle h, const sq_weight *w, const sq_rows *x, uint16_t *Y, void *stream);
+
+/* sq_quant_fwd of every expert over its own rows, in one launch that a graph can capture: offsets is a
+ * DEVICE int64 array [E + 1] (sq_sort_tokens'), read when the launch runs and kept within [0, x->R];
+ * E <= 1024. ws2 DEVICE fp32 [E] for NVFP4, NULL for MXFP4 (w->ws2 is not read).
+ * Y device bf16 [x->R, N]: rows of no expert are left as they are. */
+sq_status sq_grouped_quant_fwd(sq_handle h, const sq_grouped_weight *w, const float *ws2, const int64_t *offsets,
+                             const sq_rows *x, uint16_t *Y, void *stream);
 
 /* ---------------------------------------------------------------- head loss
  * Softmax cross entropy of hidden rows against the vocabulary projection W, the logits

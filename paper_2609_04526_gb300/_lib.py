@@ -33,7 +33,8 @@ EXPORTS = ("sq_create", "sq_destroy", "sq_status_string", "sq_last_error", "sq_s
            "sq_project_group_delta", "sq_control_fwd", "sq_control_bwd_dx", "sq_control_grad", "sq_lowrank_product",
            "sq_selftest_wait_timeout", "sq_scale_grad_workspace", "sq_project_planes", "sq_merge_planes",
            "sq_route", "sq_route_grad", "sq_sort_tokens", "sq_dispatch", "sq_dispatch_grad", "sq_combine",
-           "sq_combine_grad", "sq_head_loss", "sq_head_loss_grad")
+           "sq_combine_grad", "sq_quantize", "sq_dequantize", "sq_quant_fwd", "sq_grouped_quant_fwd", "sq_head_loss",
+           "sq_head_loss_grad")
 
 
 class SQError(RuntimeError):
@@ -54,6 +55,11 @@ class _SqGroupedWeight(ctypes.Structure):
 
 class _SqControlWeight(ctypes.Structure):
     _fields_ = [("N", ctypes.c_int32), ("K", ctypes.c_int32), ("W", ctypes.c_void_p), ("dS", ctypes.c_void_p)]
+
+
+class _SqRows(ctypes.Structure):
+    _fields_ = [("fmt", ctypes.c_int32), ("K", ctypes.c_int32), ("R", ctypes.c_int64), ("codes", ctypes.c_void_p),
+                ("scales", ctypes.c_void_p), ("ws2", ctypes.c_float), ("row_ws2", ctypes.c_void_p)]
 
 
 _lib = None
@@ -115,6 +121,11 @@ def load() -> ctypes.CDLL:
     L.sq_dispatch_grad.argtypes = [vp, i64, i32, i64, i64, vp, vp, vp, vp]
     L.sq_combine.argtypes = [vp, i64, i32, i64, i64, vp, vp, vp, vp, vp]
     L.sq_combine_grad.argtypes = [vp, i64, i32, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp]
+    Q = ctypes.POINTER(_SqRows)
+    L.sq_quantize.argtypes = [vp, Q, i64, i32, vp, vp, vp]
+    L.sq_dequantize.argtypes = [vp, Q, vp, vp]
+    L.sq_quant_fwd.argtypes = [vp, W, Q, vp, vp]
+    L.sq_grouped_quant_fwd.argtypes = [vp, GW, vp, vp, Q, vp, vp]
     L.sq_head_loss.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, vp, vp]
     L.sq_head_loss_grad.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp]
     for name in EXPORTS:
@@ -147,7 +158,8 @@ class QuantWeight:
 @dataclasses.dataclass
 class GroupedWeight:
     """The E experts of one MoE linear, each [N, K]: codes [E, N, K/2] u8, scales
-    [E, N, K/B] u8 (device), ws2 one tensor scale per expert (host floats)."""
+    [E, N, K/B] u8 (device), ws2 one tensor scale per expert (host floats; for
+    sq_grouped_quant_fwd a device fp32 tensor [E], MXFP4 any)."""
     fmt: int
     E: int
     N: int
@@ -166,6 +178,27 @@ class GroupedWeight:
         """Expert e as a dense weight (views into the grouped planes)."""
         return QuantWeight(self.fmt, self.N, self.K, self.codes[e],
                            None if self.scales is None else self.scales[e], float(self.ws2[e]))
+
+
+@dataclasses.dataclass
+class QuantRows:
+    """R rows of K activations in 4 bits, laid out as a weight: codes [R, K/2] u8, scales [R, K/B] u8, and
+    above those ws2 for all rows or, NVFP4, a scale of each row's own, row_ws2 fp32 [R]."""
+    fmt: int
+    R: int
+    K: int
+    codes: torch.Tensor
+    scales: torch.Tensor
+    ws2: float = 1.0
+    row_ws2: Optional[torch.Tensor] = None
+
+    def _c(self, device=None) -> _SqRows:
+        """The C struct of rows whose tensors are dense and on `device` (the current one)."""
+        u8, scales = torch.uint8, (self.R, self.K // BLOCK[self.fmt])
+        codes = _arg(self.codes, "codes", u8, (self.R, self.K // 2), device)
+        dev = self.codes.device
+        return _SqRows(self.fmt, self.K, self.R, codes, _arg(self.scales, "scales", u8, scales, dev), float(self.ws2),
+                       None if self.row_ws2 is None else _arg(self.row_ws2, "row_ws2", torch.float32, (self.R,), dev))
 
 
 def _offsets(offsets, E: int):
@@ -680,6 +713,71 @@ class Handle:
             _arg(weights, "weights", torch.float32, (T, k), dev), _arg(dYs, "dYs", bf16, (R, D), dev),
             _arg(dweights, "dweights", torch.float32, (T, k), dev), _stream(stream)))
         return dYs, dweights
+
+    # 4-bit rows ----------------------------------------------------------------
+    def sq_quantize(self, fmt: int, X: torch.Tensor, ws2: Optional[float] = None, slot_of: Optional[torch.Tensor] = None,
+                    k: int = 1, out: Optional[QuantRows] = None, stream=None) -> QuantRows:
+        """bf16 rows X [T, K] to 4 bits. NVFP4: under the scale ws2 or, without it, a power of two of each
+        row's own. slot_of int32 [R]: row r is X[slot_of[r] // k] (sq_dispatch's rows; zeros where there is
+        none). out: rows whose buffers are overwritten."""
+        T, K = X.shape
+        dev, R = X.device, T if slot_of is None else slot_of.shape[0]
+        own = fmt == NVFP4 and ws2 is None
+        if out is None:
+            row = _empty(stream, R, dtype=torch.float32, device=dev) if own else None
+            out = QuantRows(fmt, R, K, _empty(stream, R, K // 2, dtype=torch.uint8, device=dev),
+                            _empty(stream, R, K // BLOCK[fmt], dtype=torch.uint8, device=dev), 1.0, row)
+        elif (out.fmt, out.R, out.K, out.row_ws2 is not None) != (fmt, R, K, own):
+            raise ValueError(f"out holds {out.R} rows of {out.K} in format {out.fmt} with"
+                             f"{'' if out.row_ws2 is not None else 'out'} row_ws2; {R} of {K} in format {fmt} "
+                             f"with{'' if own else 'out'} it are written")
+        out.ws2 = 1.0 if ws2 is None else float(ws2)
+        x = _arg(X, "X", torch.bfloat16, (T, K))
+        c = out._c(dev)
+        self._check(self._L.sq_quantize(
+            self._h, ctypes.byref(c), T, int(k), x,
+            None if slot_of is None else _arg(slot_of, "slot_of", torch.int32, (R,), dev), _stream(stream)))
+        return out
+
+    def sq_dequantize(self, q: QuantRows, X: Optional[torch.Tensor] = None, stream=None):
+        """4-bit rows back to bf16 [R, K]."""
+        if X is None:
+            X = _empty(stream, q.R, q.K, dtype=torch.bfloat16, device=q.codes.device)
+        c = q._c()
+        self._check(self._L.sq_dequantize(self._h, ctypes.byref(c), _arg(X, "X", torch.bfloat16, (q.R, q.K), q.codes.device),
+                                          _stream(stream)))
+        return X
+
+    def sq_quant_fwd(self, w: QuantWeight, q: QuantRows, Y: Optional[torch.Tensor] = None, stream=None):
+        """Y = X W^T with both operands in 4 bits (bf16 [R, N])."""
+        if Y is None:
+            Y = _empty(stream, q.R, w.N, dtype=torch.bfloat16, device=q.codes.device)
+        c, wc = q._c(), w._c()
+        self._check(self._L.sq_quant_fwd(self._h, ctypes.byref(wc), ctypes.byref(c),
+                                       _arg(Y, "Y", torch.bfloat16, (q.R, w.N), q.codes.device), _stream(stream)))
+        return Y
+
+    def sq_grouped_quant_fwd(self, w: GroupedWeight, offsets: torch.Tensor, q: QuantRows, Y: Optional[torch.Tensor] = None,
+                           stream=None):
+        """Y rows offsets[e]..offsets[e+1]-1 = X rows of expert e times W_e^T, both in 4 bits; the other rows of
+        Y are left as they are (zeros of a new one). offsets int64 [E + 1] and, NVFP4, w.ws2 fp32 [E] are on the
+        device: nothing comes back to the host, and a graph can capture the call."""
+        dev = q.codes.device
+        if Y is None:
+            Y = _empty(stream, q.R, w.N, dtype=torch.bfloat16, device=dev)
+            with torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream))):
+                Y.zero_()
+        c = q._c()
+        ws2 = None
+        if w.fmt == NVFP4:
+            if not isinstance(w.ws2, torch.Tensor):
+                raise ValueError("sq_grouped_quant_fwd reads w.ws2 on the device: a fp32 tensor [E]")
+            ws2 = _arg(w.ws2, "w.ws2", torch.float32, (w.E,), dev)
+        wc = _SqGroupedWeight(w.fmt, w.E, w.N, w.K, _ptr(w.codes), _ptr(w.scales), None)
+        self._check(self._L.sq_grouped_quant_fwd(
+            self._h, ctypes.byref(wc), ws2, _arg(offsets, "offsets", torch.int64, (w.E + 1,), dev), ctypes.byref(c),
+            _arg(Y, "Y", torch.bfloat16, (q.R, w.N), dev), _stream(stream)))
+        return Y
 
     # head loss -----------------------------------------------------------------
     def sq_head_loss(self, X: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, loss: Optional[torch.Tensor] = None,

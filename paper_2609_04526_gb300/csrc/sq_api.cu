@@ -541,6 +541,81 @@ sq_status check_head(sq_handle h, int64_t T, int64_t D, int64_t V) {
   return SQ_OK;
 }
 
+// ------------------------------------------------------------------ 4-bit rows
+
+sq_status check_rows(sq_handle h, const sq_rows *q) {
+  if (!q) return fail(h, SQ_ERR_INVALID_ARG, "rows are NULL");
+  SQ_TRY(check_ws2(h, q->fmt, q->ws2));
+  if (q->R < 0 || q->R > kMaxTokens) return fail(h, SQ_ERR_INVALID_ARG, "R=%lld out of range [0, 2^31)", (long long)q->R);
+  if (q->K <= 0 || q->K % 32 != 0 || q->K > kMaxDim)
+    return fail(h, SQ_ERR_INVALID_ARG, "K=%d must be positive, a multiple of 32 and <= 2^24", q->K);
+  if (q->row_ws2 && (q->fmt != SQ_NVFP4 || q->ws2 != 1.0f))
+    return fail(h, SQ_ERR_INVALID_ARG, "row_ws2 goes with NVFP4 and ws2 = 1.0");
+  if (q->R > 0) {
+    SQ_TRY(check_buf(h, q->codes, "codes of the rows"));
+    SQ_TRY(check_buf(h, q->scales, "scales of the rows"));
+    if (q->row_ws2) SQ_TRY(check_elements(h, q->row_ws2, "row_ws2"));
+  }
+  return SQ_OK;
+}
+
+sqi::QuantArgs quant_args(const sq_rows *q) {
+  sqi::QuantArgs a = {};
+  a.R = q->R;
+  a.K = q->K;
+  a.codes = q->codes;
+  a.scales = q->scales;
+  a.row_ws2 = q->row_ws2;
+  a.ws2 = q->ws2;
+  a.inv = 1.0f / q->ws2;
+  return a;
+}
+
+// A product of x with one weight, or with E of them over the rows between device offsets.
+sq_status run_fp4(sq_handle h, int fmt, int E, int64_t N, int64_t K, const uint8_t *codes, const uint8_t *scales, float ws2,
+                  const float *dev_ws2, const int64_t *offsets, const sq_rows *x, uint16_t *Y, cudaStream_t stream) {
+  DeviceState *dev = nullptr;
+  SQ_TRY(ensure_device(h, &dev));
+  if (x->R == 0) return SQ_OK;
+  sqi::Fp4Args p = {};
+  p.R = x->R;
+  p.E = E;
+  p.N = static_cast<int>(N);
+  p.K = static_cast<int>(K);
+  p.G = static_cast<int>(K / block_of(fmt));
+  p.w_scales = scales;
+  p.x_scales = x->scales;
+  p.w_ws2 = dev_ws2;
+  p.ws2 = ws2;
+  p.row_ws2 = x->row_ws2;
+  p.x_ws2 = x->ws2;
+  p.offsets = offsets;
+  p.out = Y;
+  p.err = dev->err_word;
+  sqi::fp4_plan(fmt, dev->sm_count, p);
+  sqi::Fp4Maps m;
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(K / 2), static_cast<cuuint64_t>(N), static_cast<cuuint64_t>(E)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(K / 2), static_cast<cuuint64_t>(N * (K / 2))};
+  const cuuint32_t box[3] = {128, 128, 1}, estr[3] = {1, 1, 1};
+  const CUresult r = h->encode(&m.w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<uint8_t *>(codes), dims, strides, box, estr,
+                               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(h, SQ_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
+  for (int i = 0; i < sqi::kFp4FewBoxes; ++i)
+    SQ_TRY(make_map(h, &m.x[i], x->codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, K / 2, x->R, 128, 8u << i,
+                    CU_TENSOR_MAP_SWIZZLE_128B));
+  const cudaError_t e = sqi::launch_fp4_few(fmt, m, p, stream);
+  if (e != cudaSuccess) return cuda_fail(h, e, "4-bit product launch");
+  return SQ_OK;
+}
+
+sq_status check_operands(sq_handle h, int fmt, int K, const sq_rows *x) {
+  SQ_TRY(check_rows(h, x));
+  if (x->fmt != fmt || x->K != K)
+    return fail(h, SQ_ERR_INVALID_ARG, "rows of format %d and K=%d against a weight of format %d and K=%d", x->fmt, x->K, fmt, K);
+  return SQ_OK;
+}
+
 // ------------------------------------------------------------------ grouped (experts)
 
 constexpr int kMaxExperts = 1 << 16;
@@ -1647,6 +1722,83 @@ sq_status sq_combine_grad(sq_handle h, int64_t T, int32_t k, int64_t D, int64_t 
                                            static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return cuda_fail(h, e, "combine gradient launch");
   return SQ_OK;
+  SQ_GUARD_END
+}
+
+sq_status sq_quantize(sq_handle h, const sq_rows *q, int64_t T, int32_t k, const uint16_t *X, const int32_t *slot_of,
+                      void *stream) {
+  if (!h) return SQ_ERR_INVALID_ARG;
+  SQ_GUARD_BEGIN
+  SQ_TRY(check_rows(h, q));
+  SQ_TRY(check_tokens(h, T));
+  if (slot_of) {
+    if (k < 1 || k > sqi::kRouteMaxK) return fail(h, SQ_ERR_INVALID_ARG, "k=%d must be in [1, 32]", k);
+    if (T > kMaxTokens / k) return fail(h, SQ_ERR_INVALID_ARG, "T=%lld: T * k must be in [0, 2^31)", (long long)T);
+    SQ_TRY(check_elements(h, slot_of, "slot_of"));
+  } else if (q->R != T) {
+    return fail(h, SQ_ERR_INVALID_ARG, "R=%lld rows of T=%lld tokens without slot_of", (long long)q->R, (long long)T);
+  }
+  if (!q->row_ws2 && !(q->ws2 >= 0x1p-126f && q->ws2 <= 0x1p126f))
+    return fail(h, SQ_ERR_INVALID_ARG, "ws2=%g: a scale to quantise with is in [2^-126, 2^126]", q->ws2);
+  if (q->R > 0 && T > 0) SQ_TRY(check_buf(h, X, "X"));
+  DeviceState *dev = nullptr;
+  SQ_TRY(ensure_device(h, &dev));
+  if (q->R == 0) return SQ_OK;
+  sqi::QuantArgs a = quant_args(q);
+  a.X = X;
+  a.slot_of = slot_of;
+  a.k = slot_of ? k : 1;
+  a.slots = T * a.k;
+  a.wide = reinterpret_cast<uintptr_t>(X) % 32 == 0;
+  cudaError_t e = sqi::launch_quantize(q->fmt, a, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(h, e, "quantisation launch");
+  return SQ_OK;
+  SQ_GUARD_END
+}
+
+sq_status sq_dequantize(sq_handle h, const sq_rows *q, uint16_t *X, void *stream) {
+  if (!h) return SQ_ERR_INVALID_ARG;
+  SQ_GUARD_BEGIN
+  SQ_TRY(check_rows(h, q));
+  if (q->R > 0) SQ_TRY(check_buf(h, X, "X"));
+  DeviceState *dev = nullptr;
+  SQ_TRY(ensure_device(h, &dev));
+  if (q->R == 0) return SQ_OK;
+  cudaError_t e = sqi::launch_dequantize(q->fmt, quant_args(q), X, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(h, e, "dequantisation launch");
+  return SQ_OK;
+  SQ_GUARD_END
+}
+
+sq_status sq_quant_fwd(sq_handle h, const sq_weight *w, const sq_rows *x, uint16_t *Y, void *stream) {
+  if (!h) return SQ_ERR_INVALID_ARG;
+  SQ_GUARD_BEGIN
+  SQ_TRY(check_weight(h, w, true));
+  SQ_TRY(check_operands(h, w->fmt, w->K, x));
+  if (x->R > 0) SQ_TRY(check_buf(h, Y, "Y"));
+  return run_fp4(h, w->fmt, 1, w->N, w->K, w->codes, w->scales, w->ws2, nullptr, nullptr, x, Y,
+                 static_cast<cudaStream_t>(stream));
+  SQ_GUARD_END
+}
+
+sq_status sq_grouped_quant_fwd(sq_handle h, const sq_grouped_weight *w, const float *ws2, const int64_t *offsets,
+                             const sq_rows *x, uint16_t *Y, void *stream) {
+  if (!h) return SQ_ERR_INVALID_ARG;
+  SQ_GUARD_BEGIN
+  if (!w) return fail(h, SQ_ERR_INVALID_ARG, "grouped weight is NULL");
+  if (w->E < 1 || w->E > sqi::kRouteMaxExperts) return fail(h, SQ_ERR_INVALID_ARG, "E=%d must be in [1, 1024]", w->E);
+  // an expert's weight is checked as a dense one, its tensor scale being on the device
+  const sq_weight one = {w->fmt, w->N, w->K, w->codes, w->scales, 1.0f};
+  SQ_TRY(check_weight(h, &one, true));
+  if (w->fmt == SQ_NVFP4)
+    SQ_TRY(check_elements(h, ws2, "ws2 on the device"));
+  else if (ws2)
+    return fail(h, SQ_ERR_INVALID_ARG, "MXFP4 experts have no ws2");
+  SQ_TRY(check_elements(h, offsets, "offsets on the device"));
+  SQ_TRY(check_operands(h, w->fmt, w->K, x));
+  if (x->R > 0) SQ_TRY(check_buf(h, Y, "Y"));
+  return run_fp4(h, w->fmt, w->E, w->N, w->K, w->codes, w->scales, 1.0f, ws2, offsets, x, Y,
+                 static_cast<cudaStream_t>(stream));
   SQ_GUARD_END
 }
 

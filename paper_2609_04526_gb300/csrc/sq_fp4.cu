@@ -1,0 +1,549 @@
+// Products of FP4 rows with FP4 weights (sm_103a), dense and grouped by expert:
+//
+//   Y[m, n] = ws2 row[m] sum_b sx[m, b] sw[n, b] sum_{k in b} cx[m, k] cw[n, k]
+//
+// on tcgen05.mma with block scales: codes go from memory to the tensor cores as they are, packed two
+// to a byte, and the tensor cores apply the scale bytes of both operands to each block's products
+// before they add them up in fp32. What is left to the SM is to bring the scale bytes, row-major
+// planes in memory, into the order that the tensor cores read: atoms of 128 rows x 4 bytes, the words
+// of rows l, l + 32, l + 64 and l + 96 side by side in line l.
+//
+// The tensor cores take E4M3 scales without a sign. A negative scale byte (training may drive one below
+// zero) goes in as its magnitude, and the codes of its block, in shared memory by then, change their
+// signs.
+//
+// A stage is 256 deep: 128 bytes of codes and 16 (NVFP4) or 8 (MXFP4) scale bytes of each row.
+#include "sq_gemm_kernels.cuh"
+#include "sq_launch.cuh"
+
+namespace sqi {
+namespace {
+
+constexpr int kDeep = 256;                 // contraction of a stage
+constexpr int kAtom = 512;                 // bytes of a scale atom
+template <int FMT>
+struct Fp4 {
+  static constexpr int kBlock = FMT == 0 ? 16 : 32;
+  static constexpr int kBytes = kDeep / kBlock;  // scale bytes of a row and stage
+  static constexpr int kWords = kBytes / 4;      // atoms of 128 rows and a stage: one per 64 (NVFP4) or 128 of its depth
+};
+
+// Instruction descriptor of block-scaled FP4 products: E2M1 operands (bits 7-9 and 10-12 = 1), N >> 3 in
+// bits 17-22, scales E8M0 (bit 23) or E4M3, M >> 4 in bits 24-28, and which of a word's scale bytes an
+// MMA of depth 64 begins with, of B in bits 4-5 and of A in 29-30 (MXFP4: two of four).
+template <int FMT>
+__host__ __device__ constexpr uint32_t idesc_fp4(int M, int N, int byte) {
+  return (static_cast<uint32_t>(byte) << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(N >> 3) << 17) |
+         (FMT == 1 ? 1u << 23 : 0u) | (static_cast<uint32_t>(M >> 4) << 24) | (static_cast<uint32_t>(byte) << 29);
+}
+
+// An atom in shared memory for tcgen05.cp: 8-row groups of 16-byte lines, 128 bytes apart, no swizzle.
+__device__ __forceinline__ uint64_t atom_desc(uint32_t saddr) {
+  return static_cast<uint64_t>((saddr >> 4) & 0x3FFFu) | (static_cast<uint64_t>(1) << 16) |
+         (static_cast<uint64_t>(128 >> 4) << 32) | (static_cast<uint64_t>(1) << 46);
+}
+
+// One atom to 4 columns of tensor memory, the same in all four lane quadrants, and a product of depth 64,
+// by an elected lane of a converged warp.
+__device__ __forceinline__ void atom_to_tmem_elect(uint32_t taddr, uint64_t desc) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t"
+      "elect.sync _|e, 0xFFFFFFFF;\n\t"
+      "@e tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(taddr),
+      "l"(desc)
+      : "memory");
+}
+template <int FMT>
+__device__ __forceinline__ void umma_fp4_elect(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa,
+                                               uint32_t sb, uint32_t accumulate) {
+  if (FMT == 0)
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t"
+        "elect.sync _|e, 0xFFFFFFFF;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t"
+        "elect.sync _|e, 0xFFFFFFFF;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
+        : "memory");
+}
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, uint64_t *bar, int32_t x, int32_t y,
+                                            int32_t z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
+          dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
+
+// The scale bytes of 128 rows, stage by stage, for one warp: lane l takes rows l, l + 32, l + 64 and
+// l + 96. A row's bytes start anywhere (rows of K / 16 bytes), so a stage's are cut out of the one
+// or, not ALIGNED, two aligned pieces of kBytes that hold them; all four rows of a lane lie alike
+// to those, being 32 rows apart (32 K / 16 is a multiple of 64, 32 K / 32 of 32). Pieces are read
+// kAhead of the warp's stages early.
+template <int FMT, bool ALIGNED>
+struct ScaleRows {
+  static constexpr int kBytes = Fp4<FMT>::kBytes, kWords = Fp4<FMT>::kWords;
+  static constexpr int kAhead = ALIGNED ? 4 : 2;
+  static constexpr int kPieces = ALIGNED ? 1 : 2;
+  const uint8_t *at;        // aligned piece of the lane's first row and stage 0
+  const uint8_t *end;       // of the plane
+  int64_t apart;            // bytes of 32 rows
+  int G, shift, rows;       // scale bytes of a row; bytes from `at` to the row's; the lane's rows that exist
+  uint32_t v[kAhead][4][kPieces * kWords];
+
+  __device__ __forceinline__ void open(const uint8_t *plane, int64_t plane_rows, int64_t row0, int rows_left, int G_, int lane) {
+    G = G_;
+    const uint8_t *first = plane + (row0 + lane) * G;
+    shift = ALIGNED ? 0 : static_cast<int>(reinterpret_cast<uintptr_t>(first) % kBytes);
+    at = first - shift;
+    end = plane + plane_rows * G;
+    apart = 32 * static_cast<int64_t>(G);
+    rows = rows_left > lane ? (rows_left - lane + 31) / 32 : 0;  // of the lane's
+  }
+  __device__ __forceinline__ void piece(const uint8_t *p, uint32_t *w) const {
+    if (ALIGNED || p + kBytes <= end) {
+      if constexpr (kWords == 4) {
+        const uint4 x = *reinterpret_cast<const uint4 *>(p);
+        w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+      } else {
+        const uint2 x = *reinterpret_cast<const uint2 *>(p);
+        w[0] = x.x, w[1] = x.y;
+      }
+    } else {  // the plane ends inside
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) {
+        w[i] = 0;
+#pragma unroll 1
+        for (int b = 0; b < 4; ++b)
+          if (p + 4 * i + b < end) w[i] |= static_cast<uint32_t>(p[4 * i + b]) << (8 * b);
+      }
+    }
+  }
+  // Stage `it` into slot d; past the last one (cnt) nothing is read.
+  __device__ __forceinline__ void load(int d, int it, int cnt) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+#pragma unroll
+      for (int i = 0; i < kPieces * kWords; ++i) v[d][r][i] = 0;
+      if (r < rows && it < cnt) {
+        const uint8_t *p = at + r * apart + static_cast<int64_t>(it) * kBytes;
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j)
+          if (j == 0 || it * kBytes + j * kBytes - shift < G) piece(p + j * kBytes, &v[d][r][j * kWords]);
+      }
+    }
+  }
+  // The scale bytes of row r (0 .. 3) in slot d, stage `it`; those behind the row's end are zero.
+  __device__ __forceinline__ void take(int d, int r, int it, uint32_t (&w)[kWords]) const {
+    const uint32_t *x = v[d][r];
+    if constexpr (ALIGNED) {
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) w[i] = x[i];
+    } else {
+      uint32_t y[2 * kWords];
+#pragma unroll
+      for (int i = 0; i < 2 * kWords; ++i) y[i] = x[i];
+      if constexpr (kWords == 4) {
+        if (shift & 8) {
+#pragma unroll
+          for (int i = 0; i < 6; ++i) y[i] = y[i + 2];
+        }
+      }
+      if (shift & 4) {
+#pragma unroll
+        for (int i = 0; i < kWords + 1; ++i) y[i] = y[i + 1 < 2 * kWords ? i + 1 : i];
+      }
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) w[i] = __funnelshift_r(y[i], y[i + 1], 8 * (shift & 3));
+      const int valid = G - it * kBytes;
+      if (valid < kBytes) {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+          const int b = valid - 4 * i;
+          w[i] = b <= 0 ? 0u : (b < 4 ? w[i] & ((1u << (8 * b)) - 1) : w[i]);
+        }
+      }
+    }
+  }
+};
+
+// Changes the signs of the codes under the negative scale bytes of a row's stage: word p covers 64 of
+// the stage's depth, 32 bytes of the row's 128 in the swizzled tile, byte j of it 8 of those.
+__device__ __noinline__ void flip_codes(uint32_t tile, int row, int p, uint32_t word) {
+  for (int j = 0; j < 4; ++j)
+    if (word & (0x80u << (8 * j))) {
+      const uint32_t a = tile + row * 128 + (((2 * p + (j >> 1)) ^ (row & 7)) << 4) + (j & 1) * 8;
+      uint32_t lo, hi;
+      asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(lo), "=r"(hi) : "r"(a));
+      asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(a), "r"(lo ^ 0x88888888u), "r"(hi ^ 0x88888888u) : "memory");
+    }
+}
+
+// Puts a stage's scale bytes of 128 rows (slot d of s) into its atoms, and mends the codes of blocks
+// with a negative scale once they have landed (`landed`). Returns false if that wait ran out.
+template <int FMT, bool ALIGNED>
+__device__ __forceinline__ bool store_scales(const ScaleRows<FMT, ALIGNED> &s, int d, int it, uint32_t atoms,
+                                             uint32_t tile, uint64_t *landed, uint32_t parity,
+                                             volatile int *abort_flag, int *err) {
+  constexpr int W = Fp4<FMT>::kWords;
+  const int lane = threadIdx.x & 31;
+  uint32_t w[4][W], sign = 0;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    s.take(d, r, it, w[r]);
+    if (FMT == 0) {
+#pragma unroll
+      for (int i = 0; i < W; ++i) sign |= w[r][i];
+    }
+  }
+  bool ok = true;
+  if (FMT == 0 && __any_sync(0xFFFFFFFFu, sign & 0x80808080u)) {
+    ok = __all_sync(0xFFFFFFFFu, mbar_wait(landed, parity, abort_flag, err));
+    if (ok) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+          if (w[r][i] & 0x80808080u) flip_codes(tile, lane + 32 * r, i, w[r][i]);
+          w[r][i] &= 0x7F7F7F7Fu;
+        }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < W; ++i) st_shared_v4(atoms + i * kAtom + lane * 16, w[0][i], w[1][i], w[2][i], w[3][i]);
+  return ok;
+}
+
+// ---------------------------------------------------------------- tiles of ragged experts
+//
+// The rows of expert e are offsets[e] .. offsets[e + 1] - 1, read on the device and kept within the R
+// rows that there are, whatever they hold.
+__device__ __forceinline__ void expert_rows(const Fp4Args &p, int e, int &lo, int &hi) {
+  const int64_t a = p.offsets[e], b = p.offsets[e + 1];
+  lo = static_cast<int>(max(int64_t(0), min(a, p.R)));
+  hi = static_cast<int>(min(p.R, max(b, static_cast<int64_t>(lo))));
+}
+
+// Token tile tt of the experts' tiles of `height` rows, expert by expert: its expert, first row and
+// rows (0 past the last tile). One warp; each lane counts the tiles of its share of the experts.
+__device__ __forceinline__ void find_tile(const Fp4Args &p, int tt, int height, int &e, int &row0, int &rows) {
+  const int lane = threadIdx.x & 31;
+  const int per = (p.E + 31) / 32, first = lane * per, last = min(p.E, first + per);
+  int mine = 0;
+  for (int x = first; x < last; ++x) {
+    int lo, hi;
+    expert_rows(p, x, lo, hi);
+    mine += (hi - lo + height - 1) / height;
+  }
+  int upto = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const int v = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+    if (lane >= d) upto += v;
+  }
+  const bool here = tt >= upto - mine && tt < upto;
+  const uint32_t who = __ballot_sync(0xFFFFFFFFu, here);
+  e = row0 = rows = 0;
+  if (who == 0) return;
+  if (here) {
+    int left = tt - (upto - mine);
+    for (int x = first; x < last; ++x) {
+      int lo, hi;
+      expert_rows(p, x, lo, hi);
+      const int tiles = (hi - lo + height - 1) / height;
+      if (left < tiles) {
+        e = x;
+        row0 = lo + left * height;
+        rows = min(height, hi - row0);
+        break;
+      }
+      left -= tiles;
+    }
+  }
+  const int from = __ffs(who) - 1;
+  e = __shfl_sync(0xFFFFFFFFu, e, from);
+  row0 = __shfl_sync(0xFFFFFFFFu, row0, from);
+  rows = __shfl_sync(0xFFFFFFFFu, rows, from);
+}
+
+// ---------------------------------------------------------------- few tokens
+//
+// The weights are the MMA's A operand (128 output features), up to 128 tokens its N, so tensor work
+// and traffic follow the token count. A cluster of up to 8 CTAs cuts the contraction of a tile where
+// few tiles would leave SMs idle; its CTAs add their parts up through distributed shared memory, in
+// the order of the parts.
+
+struct Fp4FewCfg {
+  static constexpr int kF = 128;
+  static constexpr int kThreads = 192;  // warps 0-1: scales of the weights, 2-3: of the tokens (each every other stage); TMA; MMA
+  static constexpr int kTmaWarp = 4, kMmaWarp = 5;
+  static constexpr int kMaxStages = 8;
+  static constexpr int kTmemCols = 256;  // 128 of the accumulator; scales: two stages of 16 + 16
+  static constexpr int kScaleCols = 32;
+};
+
+template <int FMT, bool ALIGNED>
+__global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
+    sq_fp4_few_kernel(const __grid_constant__ Fp4Maps maps, const Fp4Args p) {
+  using C = Fp4FewCfg;
+  constexpr int W = Fp4<FMT>::kWords;
+  extern __shared__ uint8_t fp4_smem_raw[];
+  uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(fp4_smem_raw) + 1023) & ~uintptr_t(1023));
+  __shared__ uint64_t bars[3 * C::kMaxStages + 1];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_word;
+  __shared__ int tile_info[3];  // expert, first row, rows
+  volatile int *abort_flag = &abort_word;
+  uint64_t *full = bars;                     // [S] codes of both operands landed          (1 arrival + tx)
+  uint64_t *sfull = full + C::kMaxStages;    // [S] their scales are in place              (2 warps)
+  uint64_t *empty = sfull + C::kMaxStages;   // [S] the MMAs reading the stage are done    (commit)
+  uint64_t *done = empty + C::kMaxStages;    // every MMA of the tile is done              (commit)
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int S = p.stages, splits = p.splits;
+  const int part = splits > 1 ? static_cast<int>(cluster_ctarank()) : 0;
+  const int unit = static_cast<int>(blockIdx.x) / splits;
+  const int tt = unit / p.ftiles, ft = unit - tt * p.ftiles;
+  const int f0 = ft * C::kF;
+
+  if (warp == C::kTmaWarp && lane == 0) {
+    for (int s = 0; s < S; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&sfull[s], 2);
+      mbar_init(&empty[s], 1);
+    }
+    mbar_init(done, 1);
+    abort_word = 0;
+    fence_barrier_init();
+    fence_proxy_async_smem();
+  }
+  if (warp == C::kMmaWarp) tmem_alloc(&tmem_slot, C::kTmemCols);
+  dependency_wait();
+  dependency_start();
+  if (warp == 0) {
+    int e = 0, row0 = tt * p.tile_tokens, rows = static_cast<int>(min(p.R - row0, static_cast<int64_t>(p.tile_tokens)));
+    if (p.offsets) find_tile(p, tt, p.tile_tokens, e, row0, rows);
+    if (lane == 0) {
+      tile_info[0] = e;
+      tile_info[1] = row0;
+      tile_info[2] = rows;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const int expert = tile_info[0], row0 = tile_info[1], rows = tile_info[2];
+  const uint32_t tmem = tmem_slot;
+  const int cnt_all = (p.K + kDeep - 1) / kDeep;
+  const int it0 = cnt_all * part / splits, cnt = rows > 0 ? cnt_all * (part + 1) / splits - it0 : 0;
+  const int n8 = (rows + 7) & ~7;
+  const uint32_t ring = smem_u32(smem);
+  const int x_off = C::kF * 128, sf_off = x_off + p.tile_tokens * 128, stage = sf_off + 2 * W * kAtom;
+
+  if (warp == C::kTmaWarp) {
+    // ------------------------------------------------------ codes
+    int box = 0;
+    while ((8 << box) < rows) ++box;
+    int it = 0, s = 0;
+    uint32_t ph = 0;
+    for (; it < cnt; ++it) {
+      if (it >= S && !__all_sync(0xFFFFFFFFu, mbar_wait(&empty[s], ph ^ 1u, abort_flag, p.err))) break;
+      if (lane == 0) {
+        mbar_arrive_expect_tx(&full[s], C::kF * 128 + (8u << box) * 128);
+        const int x = (it0 + it) * (kDeep / 2);
+        tma_load_3d(ring + s * stage, &maps.w, &full[s], x, f0, expert);
+        tma_load_2d(ring + s * stage + x_off, &maps.x[box], &full[s], x, row0);
+      }
+      __syncwarp();
+      if (++s == S) {
+        s = 0;
+        ph ^= 1u;
+      }
+    }
+    if (*abort_flag)
+      for (int i = (it > S ? it - S : 0); i < it; ++i) mbar_drain(&full[i % S], static_cast<uint32_t>(i / S) & 1u);
+  } else if (warp == C::kMmaWarp) {
+    // ------------------------------------------------------ MMA issuer (one elected lane of the converged warp)
+    const uint64_t ad0 = smem_desc_sw128(ring, 16, 1024), bd0 = smem_desc_sw128(ring + x_off, 16, 1024);
+    const uint64_t sd0 = atom_desc(ring + sf_off);
+    int s = 0;
+    uint32_t ph = 0;
+    bool ok = true;
+    for (int it = 0; it < cnt && ok; ++it) {
+      if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&sfull[s], ph, abort_flag, p.err) &&
+                                             mbar_wait(&full[s], ph, abort_flag, p.err))))
+        break;
+      tc_fence_after();
+      const uint32_t so = static_cast<uint32_t>(s * stage) >> 4;
+      const uint32_t sa = tmem + 128 + (it & 1) * C::kScaleCols, sb = sa + 4 * W;
+#pragma unroll
+      for (int i = 0; i < 2 * W; ++i) atom_to_tmem_elect(sa + 4 * i, sd0 + so + i * (kAtom >> 4));
+      const int steps = min(4, (p.K - (it0 + it) * kDeep + 63) / 64);
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+        const int word = FMT == 0 ? kk : kk / 2;
+        const uint32_t idesc = idesc_fp4<FMT>(C::kF, 0, FMT == 0 ? 0 : 2 * (kk & 1)) | (static_cast<uint32_t>(n8 >> 3) << 17);
+        if (kk < steps)
+          umma_fp4_elect<FMT>(tmem, ad0 + so + 2 * kk, bd0 + so + 2 * kk, idesc, sa + 4 * word, sb + 4 * word,
+                              (it > 0 || kk > 0) ? 1u : 0u);
+      }
+      umma_commit_elect(&empty[s]);
+      if (++s == S) {
+        s = 0;
+        ph ^= 1u;
+      }
+    }
+    umma_commit_elect(done);
+    mbar_drain(done, 0);
+  } else {
+    // ------------------------------------------------------ scales, every other stage of one operand
+    using Rows = ScaleRows<FMT, ALIGNED>;
+    const bool tokens = warp >= 2;
+    Rows sc;
+    if (tokens)
+      sc.open(p.x_scales, p.R, row0, rows, p.G, lane);
+    else
+      sc.open(p.w_scales, static_cast<int64_t>(p.E) * p.N, static_cast<int64_t>(expert) * p.N + f0, p.N - f0, p.G, lane);
+    const int last = it0 + cnt;
+    int it = warp & 1;
+#pragma unroll
+    for (int d = 0; d < Rows::kAhead; ++d) sc.load(d, it0 + it + 2 * d, last);
+    int s = it % S;
+    uint32_t ph = static_cast<uint32_t>(it / S) & 1u;
+    bool ok = true;
+    while (it < cnt && ok) {
+#pragma unroll
+      for (int d = 0; d < Rows::kAhead; ++d) {
+        if (it >= cnt) break;
+        if (it >= S && !(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&empty[s], ph ^ 1u, abort_flag, p.err)))) break;
+        const uint32_t base = ring + s * stage;
+        ok = store_scales(sc, d, it0 + it, base + sf_off + (tokens ? W * kAtom : 0), base + (tokens ? x_off : 0), &full[s],
+                          ph, abort_flag, p.err);
+        if (!ok) break;
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sfull[s]);
+        sc.load(d, it0 + it + 2 * Rows::kAhead, last);
+        it += 2;
+        if ((s += 2) >= S) {
+          s -= S;
+          ph ^= 1u;
+        }
+      }
+    }
+    // ------------------------------------------------------ accumulator to shared memory, [token][feature] in fp32
+    __syncwarp();
+    if (cnt > 0) mbar_wait(done, 0, abort_flag, p.err);
+    __syncwarp();
+    tc_fence_after();
+    const uint32_t t_row = tmem + (static_cast<uint32_t>(warp * 32) << 16);
+    float *sums = reinterpret_cast<float *>(smem) + warp * 32 + lane;
+#pragma unroll 1
+    for (int c = 0; c < rows; c += 32) {
+      uint32_t v[32];
+      if (cnt > 0) {
+        tmem_ld32(t_row + c, v);
+        tmem_ld_wait();
+      }
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (c + i < rows) sums[(c + i) * C::kF] = cnt > 0 ? __uint_as_float(v[i]) : 0.f;
+    }
+  }
+  // ------------------------------------------------------ parts added up, scaled, rounded, stored
+  __syncwarp();
+  tc_fence_before();
+  if (splits > 1)
+    cluster_sync_all();
+  else
+    __syncthreads();
+  if (warp == C::kMmaWarp) {
+    tc_fence_after();
+    tmem_dealloc(tmem, C::kTmemCols);
+  }
+  const float ws2 = p.w_ws2 ? p.w_ws2[expert] : p.ws2;
+  const int j = threadIdx.x & 15, f = f0 + 8 * j;
+  if (f < p.N) {
+    for (int t = part * (C::kThreads / 16) + (threadIdx.x >> 4); t < rows; t += splits * (C::kThreads / 16)) {
+      float y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = 0.f;
+      const uint32_t mine = ring + (t * C::kF + 8 * j) * 4;
+      for (int q = 0; q < splits; ++q) {
+        const uint32_t at = splits > 1 ? mapa_shared(mine, q) : mine;
+#pragma unroll
+        for (int i = 0; i < 8; i += 4) {
+          float4 v;
+          asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                       : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                       : "r"(at + 4 * i));
+          y[i] += v.x, y[i + 1] += v.y, y[i + 2] += v.z, y[i + 3] += v.w;
+        }
+      }
+      const float row = p.row_ws2 ? p.row_ws2[row0 + t] : p.x_ws2;
+      uint32_t o[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(y[2 * i] * ws2 * row, y[2 * i + 1] * ws2 * row);
+        o[i] = *reinterpret_cast<const uint32_t *>(&h);
+      }
+      *reinterpret_cast<uint4 *>(p.out + (static_cast<int64_t>(row0) + t) * p.N + f) = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+  }
+  if (splits > 1) cluster_sync_all();  // the others have read this CTA's sums
+}
+
+template <typename Kernel>
+cudaError_t launch_fp4(Kernel kernel, int &done_mask, int most_smem, unsigned grid, int threads, size_t smem, int cluster,
+                       cudaStream_t stream, const Fp4Maps &maps, const Fp4Args &p) {
+  int dev = 0;
+  cudaGetDevice(&dev);
+  if (!(done_mask & (1 << (dev & 31)))) {
+    cudaError_t e;
+    if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most_smem)) != cudaSuccess ||
+        (e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout,
+                                  cudaSharedmemCarveoutMaxShared)) != cudaSuccess)
+      return e;
+    done_mask |= 1 << (dev & 31);
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid, 1, 1);
+  cfg.blockDim = dim3(threads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, maps, p);
+}
+
+template <int FMT, bool ALIGNED>
+cudaError_t launch_few_fp4(const Fp4Maps &maps, const Fp4Args &p, cudaStream_t stream) {
+  static int done_mask = 0;
+  const size_t smem = static_cast<size_t>(p.stages) * fp4_few_stage(FMT, p.tile_tokens) + 1024;
+  return launch_fp4(sq_fp4_few_kernel<FMT, ALIGNED>, done_mask, kFp4SmemAlone,
+                    static_cast<unsigned>(p.units * p.splits), Fp4FewCfg::kThreads, smem, p.splits, stream, maps, p);
+}
+
+}  // namespace
+
+cudaError_t launch_fp4_few(int fmt, const Fp4Maps &maps, const Fp4Args &p, cudaStream_t stream) {
+  const bool aligned = p.K % kDeep == 0;
+  if (fmt == 0) return aligned ? launch_few_fp4<0, true>(maps, p, stream) : launch_few_fp4<0, false>(maps, p, stream);
+  return aligned ? launch_few_fp4<1, true>(maps, p, stream) : launch_few_fp4<1, false>(maps, p, stream);
+}
+
+}  // namespace sqi

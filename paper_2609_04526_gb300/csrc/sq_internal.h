@@ -469,6 +469,65 @@ struct HeadMaps {
 cudaError_t launch_head_gather(const HeadArgs &a, cudaStream_t stream);
 cudaError_t launch_head_chunk(const HeadArgs &a, const HeadMaps &m, int first, int sm_count, cudaStream_t stream);
 
+// Rows of FP4 (sq_rows.cu, sq_fp4.cu).
+struct QuantArgs {
+  int64_t R;           // rows of codes
+  int K;
+  uint8_t *codes, *scales;
+  float *row_ws2;      // each row's own scale, or null: ws2 for all
+  float ws2, inv;      // inv: fl32(1 / ws2)
+  // quantisation
+  const uint16_t *X;
+  const int32_t *slot_of;  // [R] slot of a row, its source row slot / k; null: row r is X[r]
+  int k;
+  int64_t slots;           // T * k
+  bool wide;               // X starts on 32 bytes
+};
+cudaError_t launch_quantize(int fmt, const QuantArgs &a, cudaStream_t stream);
+cudaError_t launch_dequantize(int fmt, const QuantArgs &a, uint16_t *X, cudaStream_t stream);
+
+// Products of FP4 rows with FP4 weights (sq_fp4.cu).
+constexpr int kFp4FewTokens = 128;           // of a tile of the few-token kernel, at most
+constexpr int kFp4FewBoxes = 5;              // boxes of 8 .. 128 token rows
+constexpr int kFp4SmemAlone = 224 * 1024;    // of a CTA alone on its SM
+constexpr int kFp4SmemShared = 112 * 1024;   // ... of two
+struct Fp4Maps {
+  CUtensorMap w;                // codes [E][N][K / 2], boxes of 128 bytes x 128 rows
+  CUtensorMap x[kFp4FewBoxes];  // codes [R][K / 2], boxes of 128 bytes x (8 << i) rows
+};
+struct Fp4Args {
+  int64_t R;                 // rows
+  int E, N, K, G;            // experts (1: dense), out features, in features, scale bytes of a row
+  const uint8_t *w_scales, *x_scales;
+  const float *w_ws2;        // device [E], or null: ws2
+  float ws2;
+  const float *row_ws2;      // device [R], or null: x_ws2
+  float x_ws2;
+  const int64_t *offsets;    // device [E + 1] of a grouped call, or null
+  uint16_t *out;
+  int *err;
+  int ftiles;                // feature tiles
+  int tile_tokens;           // few: tokens of a tile (8 .. 128, a power of two)
+  int64_t units;             // few: tiles, at most
+  int splits, stages;        // few: parts of the contraction (CTAs of a cluster), stages of the ring
+};
+// A few-token stage: codes of 128 features and a tile's tokens, scale atoms of both.
+constexpr int fp4_few_stage(int fmt, int tile_tokens) { return 128 * 128 + tile_tokens * 128 + 2 * (fmt == 0 ? 4 : 2) * 512; }
+// Tiles and parts of a product on sm_count SMs: fills the last fields of p.
+inline void fp4_plan(int fmt, int sm_count, Fp4Args &p) {
+  p.ftiles = (p.N + 127) / 128;
+  const int64_t groups = p.offsets ? std::min<int64_t>(p.E, p.R) : 1;
+  p.tile_tokens = 8;
+  while (p.tile_tokens < kFp4FewTokens && p.tile_tokens * groups < p.R) p.tile_tokens *= 2;
+  p.units = ((p.R + (p.tile_tokens - 1) * groups) / p.tile_tokens) * p.ftiles;
+  const int cnt = (p.K + 255) / 256;
+  p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({8, cnt, sm_count / p.units})));
+  const int stage = fp4_few_stage(fmt, p.tile_tokens);
+  const bool alone = p.units * p.splits <= sm_count;
+  p.stages = std::min(8, ((alone ? kFp4SmemAlone : kFp4SmemShared) - 1024) / stage);
+}
+cudaError_t launch_fp4_few(int fmt, const Fp4Maps &maps, const Fp4Args &p, cudaStream_t stream);
+
 // Device-side error codes written to the error word.
 constexpr int kErrWaitTimeout = 1;
 

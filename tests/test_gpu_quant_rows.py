@@ -1,0 +1,98 @@
+"""Activations to microscaled 4 bits and back, against the definition in 64 bits.
+
+Every rounding of the definition is decided in exact arithmetic here (comparisons in 64 bits of
+numbers that 64 bits hold exactly), so codes, scale bytes and row scales have to be equal."""
+import pytest
+import torch
+
+import quant_ref as ref
+
+pkg = pytest.importorskip("paper_2609_04526_gb300")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def h():
+    return pkg.Handle()
+
+
+def check(h, fmt, X, ws2=None, slot_of=None, k=1):
+    q = h.sq_quantize(fmt, X, ws2=ws2, slot_of=slot_of, k=k)
+    back = h.sq_dequantize(q)
+    h.sq_sync()
+    src = X if slot_of is None else ref.gathered(X, slot_of, k)
+    codes, scales, row = ref.quantize(fmt, src.cpu(), ws2)
+    assert torch.equal(q.scales.cpu(), scales)
+    if q.row_ws2 is not None:
+        assert torch.equal(q.row_ws2.cpu().double(), row)
+    finite = ref.block_finite(fmt, src.cpu())
+    same = ref.unpack(q.codes.cpu()) == codes
+    assert (same | ~finite).all(), f"{int((~same & finite).sum())} codes differ"
+    values = ref.values(fmt, q.codes.cpu(), q.scales.cpu())
+    want = (values.float() * (row.float() if q.row_ws2 is not None else torch.tensor(1.0 if ws2 is None else ws2))[..., None]
+            if q.row_ws2 is not None else values.float() * (1.0 if ws2 is None else ws2)).bfloat16()
+    assert torch.equal(back.cpu().view(torch.int16)[finite], want.view(torch.int16)[finite])
+    assert torch.isnan(back.cpu().float()[~finite]).all()
+    return q
+
+
+SHAPES = [(1, 32), (1, 4096), (3, 64), (5, 544), (187, 2720), (33, 1056), (2, 14336), (7, 16416), (1, 70016)]
+
+
+@pytest.mark.parametrize("T, K", SHAPES)
+@pytest.mark.parametrize("fmt, ws2", [(pkg.NVFP4, None), (pkg.NVFP4, 0.00317), (pkg.MXFP4, None)])
+def test_rows_of_all_widths(h, fmt, ws2, T, K):
+    g = torch.Generator(device="cuda").manual_seed(T * 7 + K)
+    X = torch.randn(T, K, generator=g, device="cuda") * torch.exp(torch.randn(T, K, generator=g, device="cuda"))
+    check(h, fmt, X.bfloat16(), ws2)
+
+
+@pytest.mark.parametrize("fmt, ws2", [(pkg.NVFP4, None), (pkg.NVFP4, 1.0), (pkg.NVFP4, 0.25), (pkg.MXFP4, None)])
+def test_values_on_the_borders(h, fmt, ws2):
+    """Rows whose values lie on borders between codes: m * s with every midpoint m and E4M3 significand s."""
+    check(h, fmt, ref.border_rows().cuda(), ws2)
+
+
+@pytest.mark.parametrize("fmt, ws2", [(pkg.NVFP4, None), (pkg.NVFP4, 1.7), (pkg.MXFP4, None)])
+def test_every_bf16_value(h, fmt, ws2):
+    bits = torch.arange(65536, dtype=torch.int32)
+    X = bits.to(torch.int16).view(torch.bfloat16).view(-1, 128)  # neighbours share a binade, some rows are not finite
+    check(h, fmt, X.cuda(), ws2)
+
+
+@pytest.mark.parametrize("ws2", [2.0 ** -126, 1e-30, 3.3e-9, 1e-3, 7.0, 1e30, 2.0 ** 126])
+def test_fixed_scales_far_from_the_values(h, ws2):
+    g = torch.Generator(device="cuda").manual_seed(3)
+    X = torch.randn(40, 256, generator=g, device="cuda") * 10.0 ** torch.randint(-30, 30, (40, 1), generator=g, device="cuda")
+    check(h, pkg.NVFP4, X.bfloat16(), ws2)
+
+
+@pytest.mark.parametrize("fmt", [pkg.NVFP4, pkg.MXFP4])
+def test_rows_not_finite_and_empty(h, fmt):
+    g = torch.Generator(device="cuda").manual_seed(4)
+    X = torch.randn(16, 320, generator=g, device="cuda").bfloat16()
+    X[0] = 0
+    X[1] = float("nan")
+    X[2, 5], X[3, 64], X[4, 319] = float("inf"), float("-inf"), float("nan")
+    X[5, 16:32] = 3.38e38
+    X[6] = 1e-38
+    X[7] = -0.0
+    check(h, fmt, X)
+
+
+@pytest.mark.parametrize("fmt", [pkg.NVFP4, pkg.MXFP4])
+@pytest.mark.parametrize("k", [1, 4])
+def test_rows_by_slot(h, fmt, k):
+    g = torch.Generator(device="cuda").manual_seed(5)
+    T, K = 50, 416
+    X = torch.randn(T, K, generator=g, device="cuda").bfloat16()
+    slots = torch.randperm(T * k, generator=g, device="cuda").int()
+    slots[7], slots[20], slots[31] = -1, T * k, -(1 << 31)
+    q = check(h, fmt, X, slot_of=slots, k=k)
+    # the rows that sq_dispatch copies, quantised
+    row_of = torch.full((T * k,), -1, dtype=torch.int32, device="cuda")
+    on = (slots >= 0) & (slots < T * k)
+    row_of[slots[on].long()] = torch.arange(T * k, device="cuda", dtype=torch.int32)[on]
+    slot_of = torch.where(on, slots, -1)
+    other = h.sq_quantize(fmt, h.sq_dispatch(X, row_of.view(T, k), slot_of))
+    assert torch.equal(other.codes, q.codes) and torch.equal(other.scales, q.scales)
