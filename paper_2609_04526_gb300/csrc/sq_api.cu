@@ -596,15 +596,18 @@ sq_status run_fp4(sq_handle h, int fmt, int E, int64_t N, int64_t K, const uint8
   sqi::Fp4Maps m;
   const cuuint64_t dims[3] = {static_cast<cuuint64_t>(K / 2), static_cast<cuuint64_t>(N), static_cast<cuuint64_t>(E)};
   const cuuint64_t strides[2] = {static_cast<cuuint64_t>(K / 2), static_cast<cuuint64_t>(N * (K / 2))};
-  const cuuint32_t box[3] = {128, 128, 1}, estr[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {128, p.pair ? sqi::kFp4PairFeatures / 2u : 128u, 1}, estr[3] = {1, 1, 1};
   const CUresult r = h->encode(&m.w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<uint8_t *>(codes), dims, strides, box, estr,
                                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return fail(h, SQ_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
-  for (int i = 0; i < sqi::kFp4FewBoxes; ++i)
+  for (int i = sqi::kFp4FewBoxes - 1; i >= 0; --i) {
+    // the pair kernel's 128 rows; a tile's of the few-token kernel, and with ragged experts every smaller one
+    if (p.pair ? i < sqi::kFp4FewBoxes - 1 : offsets ? (8 << i) > p.tile_tokens : (8 << i) != p.tile_tokens) continue;
     SQ_TRY(make_map(h, &m.x[i], x->codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, K / 2, x->R, 128, 8u << i,
                     CU_TENSOR_MAP_SWIZZLE_128B));
-  const cudaError_t e = sqi::launch_fp4_few(fmt, m, p, stream);
+  }
+  const cudaError_t e = sqi::launch_fp4(fmt, m, p, dev->sm_count, stream);
   if (e != cudaSuccess) return cuda_fail(h, e, "4-bit product launch");
   return SQ_OK;
 }

@@ -13,6 +13,8 @@
 // signs.
 //
 // A stage is 256 deep: 128 bytes of codes and 16 (NVFP4) or 8 (MXFP4) scale bytes of each row.
+#include <type_traits>
+
 #include "sq_gemm_kernels.cuh"
 #include "sq_launch.cuh"
 
@@ -187,12 +189,14 @@ __device__ __noinline__ void flip_codes(uint32_t tile, int row, int p, uint32_t 
     }
 }
 
-// Puts a stage's scale bytes of 128 rows (slot d of s) into its atoms, and mends the codes of blocks
-// with a negative scale once they have landed (`landed`). Returns false if that wait ran out.
+// Puts a stage's scale bytes of 128 rows (slot d of s) into its atoms (`apart` bytes from one to the
+// next), and mends the codes of blocks with a negative scale once they have landed (`landed`): row r of
+// the atom is row r + lift of the `rows` rows of codes at `tile`, where it is one. Returns false if that
+// wait ran out.
 template <int FMT, bool ALIGNED>
 __device__ __forceinline__ bool store_scales(const ScaleRows<FMT, ALIGNED> &s, int d, int it, uint32_t atoms,
-                                             uint32_t tile, uint64_t *landed, uint32_t parity,
-                                             volatile int *abort_flag, int *err) {
+                                             int apart, uint32_t tile, int lift, int rows, uint64_t *landed,
+                                             uint32_t parity, volatile int *abort_flag, int *err) {
   constexpr int W = Fp4<FMT>::kWords;
   const int lane = threadIdx.x & 31;
   uint32_t w[4][W], sign = 0;
@@ -212,13 +216,14 @@ __device__ __forceinline__ bool store_scales(const ScaleRows<FMT, ALIGNED> &s, i
       for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int i = 0; i < W; ++i) {
-          if (w[r][i] & 0x80808080u) flip_codes(tile, lane + 32 * r, i, w[r][i]);
+          const int row = lane + 32 * r + lift;
+          if ((w[r][i] & 0x80808080u) && row >= 0 && row < rows) flip_codes(tile, row, i, w[r][i]);
           w[r][i] &= 0x7F7F7F7Fu;
         }
     }
   }
 #pragma unroll
-  for (int i = 0; i < W; ++i) st_shared_v4(atoms + i * kAtom + lane * 16, w[0][i], w[1][i], w[2][i], w[3][i]);
+  for (int i = 0; i < W; ++i) st_shared_v4(atoms + i * apart + lane * 16, w[0][i], w[1][i], w[2][i], w[3][i]);
   return ok;
 }
 
@@ -350,8 +355,8 @@ __global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
 
   if (warp == C::kTmaWarp) {
     // ------------------------------------------------------ codes
-    int box = 0;
-    while ((8 << box) < rows) ++box;
+    int box = 0;  // the smallest that holds the tile's rows; of a dense product all tiles have one
+    while ((8 << box) < (p.offsets ? rows : p.tile_tokens)) ++box;
     int it = 0, s = 0;
     uint32_t ph = 0;
     for (; it < cnt; ++it) {
@@ -425,8 +430,8 @@ __global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
         if (it >= cnt) break;
         if (it >= S && !(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&empty[s], ph ^ 1u, abort_flag, p.err)))) break;
         const uint32_t base = ring + s * stage;
-        ok = store_scales(sc, d, it0 + it, base + sf_off + (tokens ? W * kAtom : 0), base + (tokens ? x_off : 0), &full[s],
-                          ph, abort_flag, p.err);
+        ok = store_scales(sc, d, it0 + it, base + sf_off + (tokens ? W * kAtom : 0), kAtom, base + (tokens ? x_off : 0), 0,
+                          tokens ? p.tile_tokens : C::kF, &full[s], ph, abort_flag, p.err);
         if (!ok) break;
         fence_proxy_async_smem();
         __syncwarp();
@@ -501,8 +506,350 @@ __global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
   if (splits > 1) cluster_sync_all();  // the others have read this CTA's sums
 }
 
+// ---------------------------------------------------------------- many tokens
+//
+// A cluster of two CTAs per tile of 256 tokens x kNT features (tcgen05.mma.cta_group::2): each CTA
+// holds 128 of the tokens and half of the features' codes, the scales of its tokens and those of all
+// the features. Persistent, with two accumulators, so a tile's epilogue runs under the next one's MMAs.
+
+struct Fp4PairCfg {
+  static constexpr int kTokens = kFp4PairTokens, kNT = kFp4PairFeatures;
+  static constexpr int kEpiWarps = 8;  // lane quadrant w % 4, half of the columns w / 4
+  static constexpr int kScaleWarp = kEpiWarps, kScaleWarps = 6;  // two sets of three: an atom each of every other stage
+  static constexpr int kTmaWarp = kScaleWarp + kScaleWarps, kMmaWarp = kTmaWarp + 1;
+  static constexpr int kThreads = 32 * (kMmaWarp + 1);
+  static constexpr int kA = 128 * 128, kB = kNT / 2 * 128;
+  static constexpr int kMaxStages = 8;
+  static constexpr int kBox = 32 * 64;  // 32 rows x 32 columns of an epilogue warp
+  static constexpr int kMostTable = (kRouteMaxExperts + 1) * 4;
+};
+static_assert(Fp4PairCfg::kNT <= 256 && Fp4PairCfg::kNT % 32 == 0 && 2 * Fp4PairCfg::kNT + 48 <= 512,
+              "two accumulators and a stage's scales in tensor memory");
+
+__device__ __forceinline__ void atom_to_tmem_pair_elect(uint32_t taddr, uint64_t desc) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t"
+      "elect.sync _|e, 0xFFFFFFFF;\n\t"
+      "@e tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(taddr),
+      "l"(desc)
+      : "memory");
+}
+template <int FMT>
+__device__ __forceinline__ void umma_fp4_pair_elect(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa,
+                                                    uint32_t sb, uint32_t accumulate) {
+  if (FMT == 0)
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t"
+        "elect.sync _|e, 0xFFFFFFFF;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "@e tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t"
+        "elect.sync _|e, 0xFFFFFFFF;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "@e tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void commit_pair_mc_elect(uint64_t *bar) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t"
+      "elect.sync _|e, 0xFFFFFFFF;\n\t"
+      "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}" ::"r"(
+          smem_u32(bar)),
+      "h"(static_cast<unsigned short>(3))
+      : "memory");
+}
+__device__ __forceinline__ void commit_pair_elect(uint64_t *bar) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t"
+      "elect.sync _|e, 0xFFFFFFFF;\n\t"
+      "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar))
+      : "memory");
+}
+__device__ __forceinline__ void arrive_cluster(uint32_t cluster_bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+
+// Tile of a launch: expert, first row and rows of its 256, first feature. Every role walks the tiles in
+// increasing order, so the expert only moves forward.
+struct Fp4Tile {
+  int e = 0, row0, rows, f0;
+  __device__ __forceinline__ bool at(const Fp4Args &p, const int *starts, int tile) {
+    int tm, tn;
+    if (p.offsets) {
+      if (tile >= starts[p.E]) return false;
+      while (starts[e + 1] <= tile) ++e;
+      int lo, hi;
+      expert_rows(p, e, lo, hi);
+      tile_coords(tile - starts[e], (starts[e + 1] - starts[e]) / p.ftiles, p.ftiles, tm, tn);
+      row0 = lo + tm * kFp4PairTokens;
+      rows = min(kFp4PairTokens, hi - row0);
+    } else {
+      if (tile >= p.units) return false;
+      tile_coords(tile, static_cast<int>(p.units) / p.ftiles, p.ftiles, tm, tn);
+      row0 = tm * kFp4PairTokens;
+      rows = static_cast<int>(min(static_cast<int64_t>(kFp4PairTokens), p.R - row0));
+    }
+    f0 = tn * kFp4PairFeatures;
+    return true;
+  }
+};
+
+template <int FMT, bool ALIGNED>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads, 1)
+    sq_fp4_pair_kernel(const __grid_constant__ Fp4Maps maps, const Fp4Args p) {
+  using C = Fp4PairCfg;
+  constexpr int W = Fp4<FMT>::kWords;
+  constexpr int kSf = C::kA + C::kB, kStage = kSf + 3 * W * kAtom;
+  constexpr int kScaleCols = 12 * W, kScaleAt = 2 * C::kNT, kScaleBufs = (512 - kScaleAt) / kScaleCols >= 2 ? 2 : 1;
+  extern __shared__ uint8_t fp4_smem_raw[];
+  uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(fp4_smem_raw) + 1023) & ~uintptr_t(1023));
+  __shared__ uint64_t bars[3 * C::kMaxStages + 5];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_word;
+  volatile int *abort_flag = &abort_word;
+  const int S = p.stages;
+  uint64_t *full = bars;                    // [S] this CTA's codes landed                          (1 arrival + tx)
+  uint64_t *sfull = full + C::kMaxStages;   // [S] leader: codes and scales of both CTAs are there  (3 warps of each)
+  uint64_t *empty = sfull + C::kMaxStages;  // [S] the pair's MMAs have read the stage              (multicast commit)
+  uint64_t *tfull = empty + C::kMaxStages;  // [2] accumulator complete                             (multicast commit)
+  uint64_t *tempty = tfull + 2;             // [2] leader: both epilogues have read it              (8 warps of each)
+  uint64_t *drain = tempty + 2;
+  int *starts = reinterpret_cast<int *>(smem + S * kStage + C::kEpiWarps * C::kBox);  // grouped: [E + 1] first tile of an expert
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&sfull[s], 6);
+      mbar_init(&empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&tfull[b], 1);
+      mbar_init(&tempty[b], 2 * C::kEpiWarps);
+    }
+    mbar_init(drain, 1);
+    abort_word = 0;
+    fence_barrier_init();
+    fence_proxy_async_smem();
+  }
+  if (warp == C::kMmaWarp) tmem_alloc_pair(&tmem_slot, 512);
+  dependency_wait();
+  dependency_start();
+  if (p.offsets) {
+    for (int e = threadIdx.x; e < p.E; e += C::kThreads) {
+      int lo, hi;
+      expert_rows(p, e, lo, hi);
+      starts[e + 1] = (hi - lo + C::kTokens - 1) / C::kTokens * p.ftiles;
+    }
+    __syncthreads();
+    if (warp == 0) {
+      int before = 0;
+      for (int e0 = 0; e0 < p.E; e0 += 32) {
+        int v = e0 + lane < p.E ? starts[e0 + lane + 1] : 0;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+          const int u = __shfl_up_sync(0xFFFFFFFFu, v, d);
+          if (lane >= d) v += u;
+        }
+        if (e0 + lane < p.E) starts[e0 + lane + 1] = before + v;
+        before += __shfl_sync(0xFFFFFFFFu, v, 31);
+      }
+      if (lane == 0) starts[0] = 0;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot, ring = smem_u32(smem);
+  const int cnt = (p.K + kDeep - 1) / kDeep;
+  const int first = static_cast<int>(blockIdx.x >> 1), step = static_cast<int>(gridDim.x >> 1);
+  Fp4Tile t;
+
+  if (warp == C::kTmaWarp) {
+    // ------------------------------------------------------ codes
+    int it = 0, s = 0;
+    uint32_t ph = 1;
+    bool ok = true;
+    for (int tile = first; ok && t.at(p, starts, tile); tile += step) {
+      const int row = t.row0 + 128 * static_cast<int>(rank), f = t.f0 + C::kNT / 2 * static_cast<int>(rank);
+      for (int kb = 0; kb < cnt; ++kb, ++it) {
+        if (it >= S && !(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&empty[s], ph, abort_flag, p.err)))) break;
+        if (lane == 0) {
+          mbar_arrive_expect_tx(&full[s], C::kA + C::kB);
+          tma_load_2d(ring + s * kStage, &maps.x[kFp4FewBoxes - 1], &full[s], kb * (kDeep / 2), row);
+          tma_load_3d(ring + s * kStage + C::kA, &maps.w, &full[s], kb * (kDeep / 2), f, t.e);
+        }
+        __syncwarp();
+        if (++s == S) {
+          s = 0;
+          ph ^= 1u;
+        }
+      }
+    }
+    if (*abort_flag)
+      for (int i = (it > S ? it - S : 0); i < it; ++i) mbar_drain(&full[i % S], static_cast<uint32_t>(i / S) & 1u);
+  } else if (warp == C::kMmaWarp) {
+    // ------------------------------------------------------ MMA issuer (leader; one elected lane)
+    if (rank == 0) {
+      const uint64_t ad0 = smem_desc_sw128(ring, 16, 1024), bd0 = smem_desc_sw128(ring + C::kA, 16, 1024);
+      const uint64_t sd0 = atom_desc(ring + kSf);
+      int s = 0, tc = 0, it = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      for (int tile = first; ok && t.at(p, starts, tile); tile += step, ++tc) {
+        const int ab = tc & 1;
+        if (tc >= 2 &&
+            !(ok = __all_sync(0xFFFFFFFFu, mbar_spin_cluster(&tempty[ab], (static_cast<uint32_t>(tc >> 1) & 1u) ^ 1u, abort_flag, p.err))))
+          break;
+        tc_fence_after();
+        const uint32_t d = tmem + ab * C::kNT;
+        for (int kb = 0; kb < cnt; ++kb, ++it) {
+          if (!(ok = __all_sync(0xFFFFFFFFu, mbar_spin_cluster(&sfull[s], ph, abort_flag, p.err)))) break;
+          tc_fence_after();
+          const uint32_t so = static_cast<uint32_t>(s * kStage) >> 4;
+          const uint32_t sa = tmem + kScaleAt + (it & (kScaleBufs - 1)) * kScaleCols, sb = sa + 4 * W;
+#pragma unroll
+          for (int i = 0; i < 3 * W; ++i) atom_to_tmem_pair_elect(sa + 4 * i, sd0 + so + i * (kAtom >> 4));
+          const int steps = min(4, (p.K - kb * kDeep + 63) / 64);
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) {
+            const int word = FMT == 0 ? kk : kk / 2;
+            constexpr uint32_t kDesc[2] = {idesc_fp4<FMT>(2 * 128, C::kNT, 0), idesc_fp4<FMT>(2 * 128, C::kNT, FMT == 0 ? 0 : 2)};
+            if (kk < steps)
+              umma_fp4_pair_elect<FMT>(d, ad0 + so + 2 * kk, bd0 + so + 2 * kk, kDesc[kk & 1], sa + 4 * word, sb + 8 * word,
+                                       (kb > 0 || kk > 0) ? 1u : 0u);
+          }
+          commit_pair_mc_elect(&empty[s]);
+          if (++s == S) {
+            s = 0;
+            ph ^= 1u;
+          }
+        }
+        if (ok) commit_pair_mc_elect(&tfull[ab]);
+      }
+      commit_pair_elect(drain);
+      mbar_drain(drain, 0);
+    }
+  } else if (warp >= C::kScaleWarp) {
+    // ------------------------------------------------------ scales
+    // Warp 0 of a set also sees this CTA's codes land before it reports the stage.
+    using Rows = ScaleRows<FMT, ALIGNED>;
+    const int set = (warp - C::kScaleWarp) / 3, atom = (warp - C::kScaleWarp) % 3;
+    const uint32_t atoms = kSf + (atom == 0 ? 0 : (W + atom - 1) * kAtom);
+    const int apart = atom == 0 ? kAtom : 2 * kAtom;
+    const int lift = atom == 0 ? 0 : 128 * (atom - 1) - C::kNT / 2 * static_cast<int>(rank);  // atom row 0 in the tile of codes
+    Rows sc;
+    int g = 0, s = 0;  // stages of the ring so far; the set takes every other one
+    uint32_t ph = 0;
+    bool ok = true;
+    for (int tile = first; ok && t.at(p, starts, tile); tile += step) {
+      if (atom == 0)
+        sc.open(p.x_scales, p.R, static_cast<int64_t>(t.row0) + 128 * rank, t.rows - 128 * static_cast<int>(rank), p.G, lane);
+      else
+        sc.open(p.w_scales, static_cast<int64_t>(p.E) * p.N, static_cast<int64_t>(t.e) * p.N + t.f0 + 128 * (atom - 1),
+                min(p.N - t.f0, C::kNT) - 128 * (atom - 1), p.G, lane);
+      int kb = (g ^ set) & 1;  // the tile's first stage of this set
+#pragma unroll
+      for (int d = 0; d < Rows::kAhead; ++d) sc.load(d, kb + 2 * d, cnt);
+      int at = s + kb;
+      uint32_t par = ph;
+      if (at >= S) {
+        at -= S;
+        par ^= 1u;
+      }
+      while (kb < cnt && ok) {
+#pragma unroll
+        for (int d = 0; d < Rows::kAhead; ++d) {
+          if (kb >= cnt) break;
+          if (g + kb >= S && !(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&empty[at], par ^ 1u, abort_flag, p.err)))) break;
+          const uint32_t base = ring + at * kStage;
+          ok = store_scales(sc, d, kb, base + atoms, apart, base + (atom == 0 ? 0 : C::kA), lift, atom == 0 ? 128 : C::kNT / 2,
+                            &full[at], par, abort_flag, p.err);
+          if (!ok) break;
+          fence_proxy_async_smem();
+          if (atom == 0 && !(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&full[at], par, abort_flag, p.err)))) break;
+          __syncwarp();
+          if (lane == 0) arrive_cluster(mapa_shared(smem_u32(&sfull[at]), 0));
+          sc.load(d, kb + 2 * Rows::kAhead, cnt);
+          kb += 2;
+          if ((at += 2) >= S) {
+            at -= S;
+            par ^= 1u;
+          }
+        }
+      }
+      g += cnt;
+      s += cnt;
+      while (s >= S) {
+        s -= S;
+        ph ^= 1u;
+      }
+    }
+  } else {
+    // ------------------------------------------------------ epilogue
+    const int quad = warp & 3, share = warp >> 2;
+    const uint32_t t_row = tmem + (static_cast<uint32_t>(quad * 32) << 16) + share * (C::kNT / 2);
+    const uint32_t box = ring + S * kStage + warp * C::kBox;
+    int tc = 0;
+    bool ok = true;
+    for (int tile = first; ok && t.at(p, starts, tile); tile += step, ++tc) {
+      const int ab = tc & 1;
+      const int r0 = 128 * static_cast<int>(rank) + 32 * quad;  // of the tile's rows
+      const float ws2 = p.w_ws2 ? p.w_ws2[t.e] : p.ws2;
+      const float row = r0 + lane < t.rows ? (p.row_ws2 ? p.row_ws2[static_cast<int64_t>(t.row0) + r0 + lane] : p.x_ws2) : 0.f;
+      ok = __all_sync(0xFFFFFFFFu, mbar_wait(&tfull[ab], static_cast<uint32_t>(tc >> 1) & 1u, abort_flag, p.err));
+      if (!ok) break;
+      tc_fence_after();
+#pragma unroll 1
+      for (int g = 0; g < C::kNT / 64; ++g) {
+        uint32_t v[32];
+        tmem_ld32(t_row + ab * C::kNT + 32 * g, v);
+        tmem_ld_wait();
+        if (g == C::kNT / 64 - 1) {  // the accumulator is read
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) arrive_cluster(mapa_shared(smem_u32(&tempty[ab]), 0));
+        }
+        uint32_t o[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(v[2 * i]) * ws2 * row, __uint_as_float(v[2 * i + 1]) * ws2 * row);
+          o[i] = *reinterpret_cast<const uint32_t *>(&h);
+        }
+        __syncwarp();  // the box is read
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          st_shared_v4(box + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4), o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
+        __syncwarp();
+        const int f = t.f0 + share * (C::kNT / 2) + 32 * g + 8 * (lane & 3);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int r = 8 * q + (lane >> 2);
+          const uint4 y = lds128(box + r * 64 + (((lane & 3) ^ ((r >> 1) & 3)) << 4));
+          if (r0 + r < t.rows && f < p.N)
+            *reinterpret_cast<uint4 *>(p.out + (static_cast<int64_t>(t.row0) + r0 + r) * p.N + f) = y;
+        }
+      }
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  cluster_sync_all();
+  if (warp == C::kMmaWarp) {
+    tc_fence_after();
+    tmem_dealloc_pair(tmem, 512);
+  }
+}
+
 template <typename Kernel>
-cudaError_t launch_fp4(Kernel kernel, int &done_mask, int most_smem, unsigned grid, int threads, size_t smem, int cluster,
+cudaError_t launch_kernel(Kernel kernel, int &done_mask, int most_smem, unsigned grid, int threads, size_t smem, int cluster,
                        cudaStream_t stream, const Fp4Maps &maps, const Fp4Args &p) {
   int dev = 0;
   cudaGetDevice(&dev);
@@ -534,16 +881,29 @@ template <int FMT, bool ALIGNED>
 cudaError_t launch_few_fp4(const Fp4Maps &maps, const Fp4Args &p, cudaStream_t stream) {
   static int done_mask = 0;
   const size_t smem = static_cast<size_t>(p.stages) * fp4_few_stage(FMT, p.tile_tokens) + 1024;
-  return launch_fp4(sq_fp4_few_kernel<FMT, ALIGNED>, done_mask, kFp4SmemAlone,
+  return launch_kernel(sq_fp4_few_kernel<FMT, ALIGNED>, done_mask, kFp4SmemAlone,
                     static_cast<unsigned>(p.units * p.splits), Fp4FewCfg::kThreads, smem, p.splits, stream, maps, p);
 }
 
 }  // namespace
 
-cudaError_t launch_fp4_few(int fmt, const Fp4Maps &maps, const Fp4Args &p, cudaStream_t stream) {
+cudaError_t launch_fp4(int fmt, const Fp4Maps &maps, const Fp4Args &p, int sm_count, cudaStream_t stream) {
   const bool aligned = p.K % kDeep == 0;
-  if (fmt == 0) return aligned ? launch_few_fp4<0, true>(maps, p, stream) : launch_few_fp4<0, false>(maps, p, stream);
-  return aligned ? launch_few_fp4<1, true>(maps, p, stream) : launch_few_fp4<1, false>(maps, p, stream);
+  auto launch = [&](auto f, auto al) {
+    constexpr int FMT = decltype(f)::value;
+    constexpr bool ALIGNED = decltype(al)::value;
+    if (!p.pair) return launch_few_fp4<FMT, ALIGNED>(maps, p, stream);
+    static int done_mask = 0;
+    const size_t smem = fp4_pair_smem(FMT, p.stages, p.offsets ? p.E : 0);
+    const int clusters = static_cast<int>(std::min<int64_t>(p.units, sm_count / 2));
+    return launch_kernel(sq_fp4_pair_kernel<FMT, ALIGNED>, done_mask, kFp4SmemMost, 2u * clusters, Fp4PairCfg::kThreads, smem, 1,
+                         stream, maps, p);
+  };
+  using std::bool_constant;
+  using std::integral_constant;
+  if (fmt == 0)
+    return aligned ? launch(integral_constant<int, 0>(), bool_constant<true>()) : launch(integral_constant<int, 0>(), bool_constant<false>());
+  return aligned ? launch(integral_constant<int, 1>(), bool_constant<true>()) : launch(integral_constant<int, 1>(), bool_constant<false>());
 }
 
 }  // namespace sqi

@@ -491,8 +491,10 @@ constexpr int kFp4FewTokens = 128;           // of a tile of the few-token kerne
 constexpr int kFp4FewBoxes = 5;              // boxes of 8 .. 128 token rows
 constexpr int kFp4SmemAlone = 224 * 1024;    // of a CTA alone on its SM
 constexpr int kFp4SmemShared = 112 * 1024;   // ... of two
+constexpr int kFp4SmemMost = 232448 - 512;  // ... beside its static shared memory
+constexpr int kFp4PairTokens = 256, kFp4PairFeatures = 192;  // a tile of the pair kernel
 struct Fp4Maps {
-  CUtensorMap w;                // codes [E][N][K / 2], boxes of 128 bytes x 128 rows
+  CUtensorMap w;                // codes [E][N][K / 2], boxes of 128 bytes x 128 rows (few) or half a pair's features
   CUtensorMap x[kFp4FewBoxes];  // codes [R][K / 2], boxes of 128 bytes x (8 << i) rows
 };
 struct Fp4Args {
@@ -507,16 +509,33 @@ struct Fp4Args {
   uint16_t *out;
   int *err;
   int ftiles;                // feature tiles
+  bool pair;                 // the pair kernel, else the few-token one
   int tile_tokens;           // few: tokens of a tile (8 .. 128, a power of two)
-  int64_t units;             // few: tiles, at most
-  int splits, stages;        // few: parts of the contraction (CTAs of a cluster), stages of the ring
+  int64_t units;             // tiles, at most
+  int splits;                // few: parts of the contraction (CTAs of a cluster)
+  int stages;                // of the ring
 };
 // A few-token stage: codes of 128 features and a tile's tokens, scale atoms of both.
 constexpr int fp4_few_stage(int fmt, int tile_tokens) { return 128 * 128 + tile_tokens * 128 + 2 * (fmt == 0 ? 4 : 2) * 512; }
-// Tiles and parts of a product on sm_count SMs: fills the last fields of p.
+// A pair stage: codes of 128 tokens and half the features, scale atoms of those tokens and of all features; behind
+// the ring eight 2 KiB boxes of the epilogue and the experts' first tiles.
+constexpr int fp4_pair_stage(int fmt) { return 128 * 128 + kFp4PairFeatures / 2 * 128 + 3 * (fmt == 0 ? 4 : 2) * 512; }
+constexpr size_t fp4_pair_smem(int fmt, int stages, int E) {
+  return 1024 + static_cast<size_t>(stages) * fp4_pair_stage(fmt) + 8 * 2048 + (E > 0 ? 4 * (E + 1) : 0);
+}
+// Kernel, tiles and parts of a product on sm_count SMs: fills the last fields of p.
 inline void fp4_plan(int fmt, int sm_count, Fp4Args &p) {
-  p.ftiles = (p.N + 127) / 128;
   const int64_t groups = p.offsets ? std::min<int64_t>(p.E, p.R) : 1;
+  p.pair = p.R >= 192 * groups;
+  if (p.pair) {
+    p.ftiles = (p.N + kFp4PairFeatures - 1) / kFp4PairFeatures;
+    p.units = (p.R + (kFp4PairTokens - 1) * groups) / kFp4PairTokens * p.ftiles;
+    p.splits = 1;
+    p.stages = 8;
+    while (fp4_pair_smem(fmt, p.stages, p.offsets ? p.E : 0) > static_cast<size_t>(kFp4SmemMost)) --p.stages;
+    return;
+  }
+  p.ftiles = (p.N + 127) / 128;
   p.tile_tokens = 8;
   while (p.tile_tokens < kFp4FewTokens && p.tile_tokens * groups < p.R) p.tile_tokens *= 2;
   p.units = ((p.R + (p.tile_tokens - 1) * groups) / p.tile_tokens) * p.ftiles;
@@ -526,7 +545,7 @@ inline void fp4_plan(int fmt, int sm_count, Fp4Args &p) {
   const bool alone = p.units * p.splits <= sm_count;
   p.stages = std::min(8, ((alone ? kFp4SmemAlone : kFp4SmemShared) - 1024) / stage);
 }
-cudaError_t launch_fp4_few(int fmt, const Fp4Maps &maps, const Fp4Args &p, cudaStream_t stream);
+cudaError_t launch_fp4(int fmt, const Fp4Maps &maps, const Fp4Args &p, int sm_count, cudaStream_t stream);
 
 // Device-side error codes written to the error word.
 constexpr int kErrWaitTimeout = 1;
