@@ -53,6 +53,7 @@ struct DeviceState {
   int64_t *plane_acc;    // counter accumulators of the multi-plane calls (zero between calls)
   Scratch sort;          // per-CTA counts of the sort by expert
   Scratch head;          // packed rows, exponentials and partial planes of the head loss
+  Scratch scales;        // scale planes with padded rows of the 4-bit products
 };
 
 constexpr int64_t kMaxDim = int64_t(1) << 24;       // N, K limit
@@ -571,6 +572,19 @@ sqi::QuantArgs quant_args(const sq_rows *q) {
   return a;
 }
 
+// Byte planes [E, N, inner] of the experts of one linear in boxes of box_inner x box_rows of one of them.
+sq_status make_experts_map(sq_handle h, CUtensorMap *map, const uint8_t *ptr, int64_t inner, int64_t N, int64_t E,
+                           uint32_t box_inner, uint32_t box_rows, CUtensorMapSwizzle swz) {
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(N), static_cast<cuuint64_t>(E)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(N * inner)};
+  const cuuint32_t box[3] = {box_inner, box_rows, 1}, estr[3] = {1, 1, 1};
+  CUresult r = h->encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<uint8_t *>(ptr), dims, strides, box, estr,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, swz, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(h, SQ_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
+  return SQ_OK;
+}
+
 // A product of x with one weight, or with E of them over the rows between device offsets.
 sq_status run_fp4(sq_handle h, int fmt, int E, int64_t N, int64_t K, const uint8_t *codes, const uint8_t *scales, float ws2,
                   const float *dev_ws2, const int64_t *offsets, const sq_rows *x, uint16_t *Y, cudaStream_t stream) {
@@ -592,20 +606,36 @@ sq_status run_fp4(sq_handle h, int fmt, int E, int64_t N, int64_t K, const uint8
   p.offsets = offsets;
   p.out = Y;
   p.err = dev->err_word;
-  sqi::fp4_plan(fmt, dev->sm_count, p);
+  sqi::fp4_plan(dev->sm_count, p);
+  int pitch = p.G;  // of the scale planes that TMA reads
+  const uint8_t *x_scales = x->scales;
+  if (p.pair && p.G % 16 != 0) {
+    pitch = (p.G + 15) / 16 * 16;
+    const int64_t w_rows = E * N;
+    SQ_TRY(ensure_scratch(h, dev->scales, static_cast<size_t>((w_rows + x->R) * pitch), stream, "a product of such a K"));
+    sqi::PadArgs pad = {{scales, x_scales}, {}, {w_rows, x->R}, p.G, pitch};
+    pad.dst[0] = static_cast<uint8_t *>(dev->scales.ptr);
+    pad.dst[1] = pad.dst[0] + w_rows * pitch;
+    const cudaError_t e = sqi::launch_fp4_pad(pad, dev->sm_count, stream);
+    if (e != cudaSuccess) return cuda_fail(h, e, "scale plane launch");
+    scales = pad.dst[0];
+    x_scales = pad.dst[1];
+    p.G = pitch;
+  }
+  // Rows of codes in boxes of 128 bytes and, where they are whole 16-byte pieces, of scale bytes in boxes of 16.
   sqi::Fp4Maps m;
-  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(K / 2), static_cast<cuuint64_t>(N), static_cast<cuuint64_t>(E)};
-  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(K / 2), static_cast<cuuint64_t>(N * (K / 2))};
-  const cuuint32_t box[3] = {128, p.pair ? sqi::kFp4PairFeatures / 2u : 128u, 1}, estr[3] = {1, 1, 1};
-  const CUresult r = h->encode(&m.w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<uint8_t *>(codes), dims, strides, box, estr,
-                               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) return fail(h, SQ_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
+  const uint32_t features = p.pair ? sqi::kFp4PairFeatures / 2 : 128;
+  const bool raw = pitch % 16 == 0;
+  SQ_TRY(make_experts_map(h, &m.w, codes, K / 2, N, E, 128, features, CU_TENSOR_MAP_SWIZZLE_128B));
+  if (raw) SQ_TRY(make_experts_map(h, &m.w_scales, scales, pitch, N, E, 16, features, CU_TENSOR_MAP_SWIZZLE_NONE));
   for (int i = sqi::kFp4FewBoxes - 1; i >= 0; --i) {
     // the pair kernel's 128 rows; a tile's of the few-token kernel, and with ragged experts every smaller one
     if (p.pair ? i < sqi::kFp4FewBoxes - 1 : offsets ? (8 << i) > p.tile_tokens : (8 << i) != p.tile_tokens) continue;
     SQ_TRY(make_map(h, &m.x[i], x->codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, K / 2, x->R, 128, 8u << i,
                     CU_TENSOR_MAP_SWIZZLE_128B));
+    if (raw)
+      SQ_TRY(make_map(h, &m.x_scales[i], x_scales, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, pitch, x->R, 16, 8u << i,
+                      CU_TENSOR_MAP_SWIZZLE_NONE));
   }
   const cudaError_t e = sqi::launch_fp4(fmt, m, p, dev->sm_count, stream);
   if (e != cudaSuccess) return cuda_fail(h, e, "4-bit product launch");
@@ -909,6 +939,7 @@ sq_status sq_destroy(sq_handle h) {
       free_scratch(d.partial);
       free_scratch(d.sort);
       free_scratch(d.head);
+      free_scratch(d.scales);
       for (auto &t : d.tables) {
         if (t.done) {
           cudaEventSynchronize(t.done);

@@ -6,7 +6,13 @@
 // to a byte, and the tensor cores apply the scale bytes of both operands to each block's products
 // before they add them up in fp32. What is left to the SM is to bring the scale bytes, row-major
 // planes in memory, into the order that the tensor cores read: atoms of 128 rows x 4 bytes, the words
-// of rows l, l + 32, l + 64 and l + 96 side by side in line l.
+// of rows l, l + 32, l + 64 and l + 96 side by side in line l. TMA brings 16 bytes of each row and a
+// warp turns them into atoms, in place. A plane whose rows are not whole 16-byte pieces (K / 16 or K /
+// 32 not a multiple of 16) has no TMA descriptor. For many tokens it is copied with longer rows first;
+// for few the warp loads the bytes itself. (Those loads take 37 wavefronts each, the lanes' rows being
+// different lines: in the pair kernel 441 of a stage whose MMAs take 384 cycles. And the proxy fence
+// behind the atoms waits for the loads that run ahead, so on that path it is the reader that executes
+// it, behind the barrier.)
 //
 // The tensor cores take E4M3 scales without a sign. A negative scale byte (training may drive one below
 // zero) goes in as its magnitude, and the codes of its block, in shared memory by then, change their
@@ -29,6 +35,8 @@ struct Fp4 {
   static constexpr int kBytes = kDeep / kBlock;  // scale bytes of a row and stage
   static constexpr int kWords = kBytes / 4;      // atoms of 128 rows and a stage: one per 64 (NVFP4) or 128 of its depth
 };
+constexpr int kSpan = 16;                  // scale bytes of a row that a TMA box brings (MXFP4: those of two stages)
+constexpr int kScales = 128 * kSpan;       // ... of 128 rows, and the room of their atoms
 
 // Instruction descriptor of block-scaled FP4 products: E2M1 operands (bits 7-9 and 10-12 = 1), N >> 3 in
 // bits 17-22, scales E8M0 (bit 23) or E4M3, M >> 4 in bits 24-28, and which of a word's scale bytes an
@@ -85,33 +93,31 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map
       : "memory");
 }
 
-// The scale bytes of 128 rows, stage by stage, for one warp: lane l takes rows l, l + 32, l + 64 and
-// l + 96. A row's bytes start anywhere (rows of K / 16 bytes), so a stage's are cut out of the one
-// or, not ALIGNED, two aligned pieces of kBytes that hold them; all four rows of a lane lie alike
-// to those, being 32 rows apart (32 K / 16 is a multiple of 64, 32 K / 32 of 32). Pieces are read
-// kAhead of the warp's stages early.
-template <int FMT, bool ALIGNED>
+// The scale bytes of 128 rows, stage by stage, for one warp that loads them itself: lane l takes rows l,
+// l + 32, l + 64 and l + 96. A row's bytes start anywhere, so a stage's are cut out of the two aligned
+// pieces of kBytes that hold them; all four rows of a lane lie alike to those, being 32 rows apart (32 K
+// / 16 is a multiple of 64, 32 K / 32 of 32). Pieces are read kAhead of the warp's stages early.
+template <int FMT>
 struct ScaleRows {
   static constexpr int kBytes = Fp4<FMT>::kBytes, kWords = Fp4<FMT>::kWords;
-  static constexpr int kAhead = ALIGNED ? 4 : 2;
-  static constexpr int kPieces = ALIGNED ? 1 : 2;
+  static constexpr int kAhead = 2;
   const uint8_t *at;        // aligned piece of the lane's first row and stage 0
   const uint8_t *end;       // of the plane
   int64_t apart;            // bytes of 32 rows
   int G, shift, rows;       // scale bytes of a row; bytes from `at` to the row's; the lane's rows that exist
-  uint32_t v[kAhead][4][kPieces * kWords];
+  uint32_t v[kAhead][4][2 * kWords];
 
   __device__ __forceinline__ void open(const uint8_t *plane, int64_t plane_rows, int64_t row0, int rows_left, int G_, int lane) {
     G = G_;
     const uint8_t *first = plane + (row0 + lane) * G;
-    shift = ALIGNED ? 0 : static_cast<int>(reinterpret_cast<uintptr_t>(first) % kBytes);
+    shift = static_cast<int>(reinterpret_cast<uintptr_t>(first) % kBytes);
     at = first - shift;
     end = plane + plane_rows * G;
     apart = 32 * static_cast<int64_t>(G);
     rows = rows_left > lane ? (rows_left - lane + 31) / 32 : 0;  // of the lane's
   }
   __device__ __forceinline__ void piece(const uint8_t *p, uint32_t *w) const {
-    if (ALIGNED || p + kBytes <= end) {
+    if (p + kBytes <= end) {
       if constexpr (kWords == 4) {
         const uint4 x = *reinterpret_cast<const uint4 *>(p);
         w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
@@ -134,44 +140,37 @@ struct ScaleRows {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
 #pragma unroll
-      for (int i = 0; i < kPieces * kWords; ++i) v[d][r][i] = 0;
+      for (int i = 0; i < 2 * kWords; ++i) v[d][r][i] = 0;
       if (r < rows && it < cnt) {
         const uint8_t *p = at + r * apart + static_cast<int64_t>(it) * kBytes;
-#pragma unroll
-        for (int j = 0; j < kPieces; ++j)
-          if (j == 0 || it * kBytes + j * kBytes - shift < G) piece(p + j * kBytes, &v[d][r][j * kWords]);
+        piece(p, &v[d][r][0]);
+        if ((it + 1) * kBytes - shift < G) piece(p + kBytes, &v[d][r][kWords]);
       }
     }
   }
   // The scale bytes of row r (0 .. 3) in slot d, stage `it`; those behind the row's end are zero.
   __device__ __forceinline__ void take(int d, int r, int it, uint32_t (&w)[kWords]) const {
-    const uint32_t *x = v[d][r];
-    if constexpr (ALIGNED) {
+    uint32_t y[2 * kWords];
 #pragma unroll
-      for (int i = 0; i < kWords; ++i) w[i] = x[i];
-    } else {
-      uint32_t y[2 * kWords];
+    for (int i = 0; i < 2 * kWords; ++i) y[i] = v[d][r][i];
+    if constexpr (kWords == 4) {
+      if (shift & 8) {
 #pragma unroll
-      for (int i = 0; i < 2 * kWords; ++i) y[i] = x[i];
-      if constexpr (kWords == 4) {
-        if (shift & 8) {
-#pragma unroll
-          for (int i = 0; i < 6; ++i) y[i] = y[i + 2];
-        }
+        for (int i = 0; i < 6; ++i) y[i] = y[i + 2];
       }
-      if (shift & 4) {
+    }
+    if (shift & 4) {
 #pragma unroll
-        for (int i = 0; i < kWords + 1; ++i) y[i] = y[i + 1 < 2 * kWords ? i + 1 : i];
-      }
+      for (int i = 0; i < kWords + 1; ++i) y[i] = y[i + 1 < 2 * kWords ? i + 1 : i];
+    }
 #pragma unroll
-      for (int i = 0; i < kWords; ++i) w[i] = __funnelshift_r(y[i], y[i + 1], 8 * (shift & 3));
-      const int valid = G - it * kBytes;
-      if (valid < kBytes) {
+    for (int i = 0; i < kWords; ++i) w[i] = __funnelshift_r(y[i], y[i + 1], 8 * (shift & 3));
+    const int valid = G - it * kBytes;
+    if (valid < kBytes) {
 #pragma unroll
-        for (int i = 0; i < kWords; ++i) {
-          const int b = valid - 4 * i;
-          w[i] = b <= 0 ? 0u : (b < 4 ? w[i] & ((1u << (8 * b)) - 1) : w[i]);
-        }
+      for (int i = 0; i < kWords; ++i) {
+        const int b = valid - 4 * i;
+        w[i] = b <= 0 ? 0u : (b < 4 ? w[i] & ((1u << (8 * b)) - 1) : w[i]);
       }
     }
   }
@@ -189,43 +188,86 @@ __device__ __noinline__ void flip_codes(uint32_t tile, int row, int p, uint32_t 
     }
 }
 
-// Puts a stage's scale bytes of 128 rows (slot d of s) into its atoms (`apart` bytes from one to the
-// next), and mends the codes of blocks with a negative scale once they have landed (`landed`): row r of
-// the atom is row r + lift of the `rows` rows of codes at `tile`, where it is one. Returns false if that
-// wait ran out.
-template <int FMT, bool ALIGNED>
-__device__ __forceinline__ bool store_scales(const ScaleRows<FMT, ALIGNED> &s, int d, int it, uint32_t atoms,
-                                             int apart, uint32_t tile, int lift, int rows, uint64_t *landed,
-                                             uint32_t parity, volatile int *abort_flag, int *err) {
+// Where the codes of 128 rows of scales lie: row r of the scales is row r + lift of the `rows` rows of
+// codes that a stage has `off` bytes from its start.
+struct CodeRows {
+  int off, lift, rows;
+};
+
+// A stage's scale bytes of 128 rows, lane l's rows l + 32 r, to their atoms. Codes of blocks with a
+// negative scale are mended, once they have landed (LANDED: they have; else `landed` says so). Returns
+// false if that wait ran out.
+template <int FMT, bool LANDED>
+__device__ __forceinline__ bool store_scales(uint32_t (&w)[4][Fp4<FMT>::kWords], uint32_t atoms, uint32_t stage,
+                                             const CodeRows &c, uint64_t *landed, uint32_t parity,
+                                             volatile int *abort_flag, int *err) {
   constexpr int W = Fp4<FMT>::kWords;
   const int lane = threadIdx.x & 31;
-  uint32_t w[4][W], sign = 0;
+  bool ok = true;
+  if (FMT == 0) {
+    uint32_t sign = 0;
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    s.take(d, r, it, w[r]);
-    if (FMT == 0) {
+    for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int i = 0; i < W; ++i) sign |= w[r][i];
+    if (__any_sync(0xFFFFFFFFu, sign & 0x80808080u)) {
+      if (!LANDED) ok = __all_sync(0xFFFFFFFFu, mbar_wait(landed, parity, abort_flag, err));
+      if (ok) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int i = 0; i < W; ++i) {
+            const int row = lane + 32 * r + c.lift;
+            if ((w[r][i] & 0x80808080u) && row >= 0 && row < c.rows) flip_codes(stage + c.off, row, i, w[r][i]);
+            w[r][i] &= 0x7F7F7F7Fu;
+          }
+      }
     }
   }
-  bool ok = true;
-  if (FMT == 0 && __any_sync(0xFFFFFFFFu, sign & 0x80808080u)) {
-    ok = __all_sync(0xFFFFFFFFu, mbar_wait(landed, parity, abort_flag, err));
-    if (ok) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-          const int row = lane + 32 * r + lift;
-          if ((w[r][i] & 0x80808080u) && row >= 0 && row < rows) flip_codes(tile, row, i, w[r][i]);
-          w[r][i] &= 0x7F7F7F7Fu;
-        }
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < W; ++i) st_shared_v4(atoms + i * apart + lane * 16, w[0][i], w[1][i], w[2][i], w[3][i]);
+  for (int i = 0; i < W; ++i) st_shared_v4(atoms + i * kAtom + lane * 16, w[0][i], w[1][i], w[2][i], w[3][i]);
   return ok;
 }
+
+// The bytes that TMA brought, 16 of each of up to 128 rows from `at` on (`rows` of them were asked for),
+// to atoms in their place. MXFP4: those of stage `it` are one half.
+template <int FMT>
+__device__ __forceinline__ void turn_scales(uint32_t at, int rows, int it, uint32_t stage, const CodeRows &c) {
+  constexpr int W = Fp4<FMT>::kWords;
+  const int lane = threadIdx.x & 31;
+  uint32_t w[4][W];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    uint4 x = make_uint4(0, 0, 0, 0);
+    if (lane + 32 * r < rows) x = lds128(at + (lane + 32 * r) * kSpan);
+    if constexpr (FMT == 0) {
+      w[r][0] = x.x, w[r][1] = x.y, w[r][2] = x.z, w[r][3] = x.w;
+    } else {
+      w[r][0] = it & 1 ? x.z : x.x, w[r][1] = it & 1 ? x.w : x.y;
+    }
+  }
+  __syncwarp();  // all of them are read
+  store_scales<FMT, true>(w, at, stage, c, nullptr, 0, nullptr, nullptr);
+}
+
+// The stages of one of two warps that share an operand's scales: those whose slot of the ring is even, or
+// odd. A wait by parity cannot tell a use of a slot from the one two before, and need not where every
+// use of a slot is the same warp's. (Every other stage, in a ring of an odd number of slots, ran into that.)
+struct ScaleStages {
+  int it, s;    // stage and slot
+  uint32_t ph;  // parity of the slot's use
+  __device__ __forceinline__ explicit ScaleStages(int set) : it(set), s(set), ph(0) {}
+  __device__ __forceinline__ void next(int S) {
+    if (s + 2 < S) {
+      it += 2;
+      s += 2;
+    } else {  // on to slot 0 or 1
+      it += S - s + (s & 1);
+      s &= 1;
+      ph ^= 1u;
+    }
+  }
+};
 
 // ---------------------------------------------------------------- tiles of ragged experts
 //
@@ -295,7 +337,7 @@ struct Fp4FewCfg {
   static constexpr int kScaleCols = 32;
 };
 
-template <int FMT, bool ALIGNED>
+template <int FMT, bool RAW>
 __global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
     sq_fp4_few_kernel(const __grid_constant__ Fp4Maps maps, const Fp4Args p) {
   using C = Fp4FewCfg;
@@ -348,24 +390,29 @@ __global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
   const int expert = tile_info[0], row0 = tile_info[1], rows = tile_info[2];
   const uint32_t tmem = tmem_slot;
   const int cnt_all = (p.K + kDeep - 1) / kDeep;
-  const int it0 = cnt_all * part / splits, cnt = rows > 0 ? cnt_all * (part + 1) / splits - it0 : 0;
+  const int it0 = cnt_all * part / splits, cnt = __any_sync(0xFFFFFFFFu, rows > 0) ? cnt_all * (part + 1) / splits - it0 : 0;
   const int n8 = (rows + 7) & ~7;
   const uint32_t ring = smem_u32(smem);
-  const int x_off = C::kF * 128, sf_off = x_off + p.tile_tokens * 128, stage = sf_off + 2 * W * kAtom;
+  const int x_off = C::kF * 128, sf_off = x_off + p.tile_tokens * 128, stage = sf_off + 2 * kScales;
+  int box = 0;  // the smallest that holds the tile's rows; of a dense product all tiles have one
+  while ((8 << box) < (p.offsets ? rows : p.tile_tokens)) ++box;
 
   if (warp == C::kTmaWarp) {
     // ------------------------------------------------------ codes
-    int box = 0;  // the smallest that holds the tile's rows; of a dense product all tiles have one
-    while ((8 << box) < (p.offsets ? rows : p.tile_tokens)) ++box;
     int it = 0, s = 0;
     uint32_t ph = 0;
     for (; it < cnt; ++it) {
       if (it >= S && !__all_sync(0xFFFFFFFFu, mbar_wait(&empty[s], ph ^ 1u, abort_flag, p.err))) break;
       if (lane == 0) {
-        mbar_arrive_expect_tx(&full[s], C::kF * 128 + (8u << box) * 128);
+        mbar_arrive_expect_tx(&full[s], (C::kF + (8u << box)) * (128 + (RAW ? kSpan : 0)));
         const int x = (it0 + it) * (kDeep / 2);
         tma_load_3d(ring + s * stage, &maps.w, &full[s], x, f0, expert);
         tma_load_2d(ring + s * stage + x_off, &maps.x[box], &full[s], x, row0);
+        if (RAW) {
+          const int b = (it0 + it) * Fp4<FMT>::kBytes / kSpan * kSpan;
+          tma_load_3d(ring + s * stage + sf_off, &maps.w_scales, &full[s], b, f0, expert);
+          tma_load_2d(ring + s * stage + sf_off + kScales, &maps.x_scales[box], &full[s], b, row0);
+        }
       }
       __syncwarp();
       if (++s == S) {
@@ -384,13 +431,17 @@ __global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
     bool ok = true;
     for (int it = 0; it < cnt && ok; ++it) {
       if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&sfull[s], ph, abort_flag, p.err) &&
-                                             mbar_wait(&full[s], ph, abort_flag, p.err))))
+                                             (RAW || mbar_wait(&full[s], ph, abort_flag, p.err)))))
         break;
+      if (!RAW) fence_proxy_async_smem();
       tc_fence_after();
       const uint32_t so = static_cast<uint32_t>(s * stage) >> 4;
       const uint32_t sa = tmem + 128 + (it & 1) * C::kScaleCols, sb = sa + 4 * W;
 #pragma unroll
-      for (int i = 0; i < 2 * W; ++i) atom_to_tmem_elect(sa + 4 * i, sd0 + so + i * (kAtom >> 4));
+      for (int i = 0; i < W; ++i) {
+        atom_to_tmem_elect(sa + 4 * i, sd0 + so + i * (kAtom >> 4));
+        atom_to_tmem_elect(sb + 4 * i, sd0 + so + ((kScales + i * kAtom) >> 4));
+      }
       const int steps = min(4, (p.K - (it0 + it) * kDeep + 63) / 64);
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) {
@@ -409,38 +460,50 @@ __global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
     umma_commit_elect(done);
     mbar_drain(done, 0);
   } else {
-    // ------------------------------------------------------ scales, every other stage of one operand
-    using Rows = ScaleRows<FMT, ALIGNED>;
+    // ------------------------------------------------------ scales, half of the stages of one operand
     const bool tokens = warp >= 2;
-    Rows sc;
-    if (tokens)
-      sc.open(p.x_scales, p.R, row0, rows, p.G, lane);
-    else
-      sc.open(p.w_scales, static_cast<int64_t>(p.E) * p.N, static_cast<int64_t>(expert) * p.N + f0, p.N - f0, p.G, lane);
-    const int last = it0 + cnt;
-    int it = warp & 1;
-#pragma unroll
-    for (int d = 0; d < Rows::kAhead; ++d) sc.load(d, it0 + it + 2 * d, last);
-    int s = it % S;
-    uint32_t ph = static_cast<uint32_t>(it / S) & 1u;
+    const int at = sf_off + (tokens ? kScales : 0);
+    const CodeRows codes = {tokens ? x_off : 0, 0, tokens ? 8 << box : C::kF};
+    ScaleStages c(warp & 1);
     bool ok = true;
-    while (it < cnt && ok) {
-#pragma unroll
-      for (int d = 0; d < Rows::kAhead; ++d) {
-        if (it >= cnt) break;
-        if (it >= S && !(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&empty[s], ph ^ 1u, abort_flag, p.err)))) break;
-        const uint32_t base = ring + s * stage;
-        ok = store_scales(sc, d, it0 + it, base + sf_off + (tokens ? W * kAtom : 0), kAtom, base + (tokens ? x_off : 0), 0,
-                          tokens ? p.tile_tokens : C::kF, &full[s], ph, abort_flag, p.err);
-        if (!ok) break;
+    auto next = [&] {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sfull[c.s]);
+      c.next(S);
+    };
+    if constexpr (RAW) {
+      while (c.it < cnt) {
+        if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&full[c.s], c.ph, abort_flag, p.err)))) break;
+        const uint32_t base = ring + c.s * stage;
+        turn_scales<FMT>(base + at, codes.rows, it0 + c.it, base, codes);
         fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sfull[s]);
-        sc.load(d, it0 + it + 2 * Rows::kAhead, last);
-        it += 2;
-        if ((s += 2) >= S) {
-          s -= S;
-          ph ^= 1u;
+        next();
+      }
+    } else {
+      using Rows = ScaleRows<FMT>;
+      Rows sc;
+      if (tokens)
+        sc.open(p.x_scales, p.R, row0, rows, p.G, lane);
+      else
+        sc.open(p.w_scales, static_cast<int64_t>(p.E) * p.N, static_cast<int64_t>(expert) * p.N + f0, p.N - f0, p.G, lane);
+      const int last = it0 + cnt;
+      ScaleStages ahead = c;
+#pragma unroll
+      for (int d = 0; d < Rows::kAhead; ++d, ahead.next(S)) sc.load(d, it0 + ahead.it, last);
+      while (c.it < cnt && ok) {
+#pragma unroll
+        for (int d = 0; d < Rows::kAhead; ++d) {
+          if (c.it >= cnt) break;
+          if (c.it >= S && !(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&empty[c.s], c.ph ^ 1u, abort_flag, p.err)))) break;
+          const uint32_t base = ring + c.s * stage;
+          uint32_t w[4][W];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sc.take(d, r, it0 + c.it, w[r]);
+          ok = store_scales<FMT, false>(w, base + at, base, codes, &full[c.s], c.ph, abort_flag, p.err);
+          if (!ok) break;
+          sc.load(d, it0 + ahead.it, last);
+          ahead.next(S);
+          next();
         }
       }
     }
@@ -599,22 +662,23 @@ struct Fp4Tile {
   }
 };
 
-template <int FMT, bool ALIGNED>
+template <int FMT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads, 1)
     sq_fp4_pair_kernel(const __grid_constant__ Fp4Maps maps, const Fp4Args p) {
   using C = Fp4PairCfg;
   constexpr int W = Fp4<FMT>::kWords;
-  constexpr int kSf = C::kA + C::kB, kStage = kSf + 3 * W * kAtom;
+  constexpr int kSf = C::kA + C::kB, kStage = kSf + 3 * kScales;
   constexpr int kScaleCols = 12 * W, kScaleAt = 2 * C::kNT, kScaleBufs = (512 - kScaleAt) / kScaleCols >= 2 ? 2 : 1;
   extern __shared__ uint8_t fp4_smem_raw[];
   uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(fp4_smem_raw) + 1023) & ~uintptr_t(1023));
   __shared__ uint64_t bars[3 * C::kMaxStages + 5];
+  __shared__ uint32_t sink[3 * 2];  // leader: what the peer's signals write
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_word;
   volatile int *abort_flag = &abort_word;
   const int S = p.stages;
   uint64_t *full = bars;                    // [S] this CTA's codes landed                          (1 arrival + tx)
-  uint64_t *sfull = full + C::kMaxStages;   // [S] leader: codes and scales of both CTAs are there  (3 warps of each)
+  uint64_t *sfull = full + C::kMaxStages;   // [S] leader: atoms and codes of both CTAs are there   (3 warps, the peer's bytes)
   uint64_t *empty = sfull + C::kMaxStages;  // [S] the pair's MMAs have read the stage              (multicast commit)
   uint64_t *tfull = empty + C::kMaxStages;  // [2] accumulator complete                             (multicast commit)
   uint64_t *tempty = tfull + 2;             // [2] leader: both epilogues have read it              (8 warps of each)
@@ -626,7 +690,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) {
       mbar_init(&full[s], 1);
-      mbar_init(&sfull[s], 6);
+      mbar_init(&sfull[s], 3);
       mbar_init(&empty[s], 1);
     }
     for (int b = 0; b < 2; ++b) {
@@ -682,9 +746,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
       for (int kb = 0; kb < cnt; ++kb, ++it) {
         if (it >= S && !(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&empty[s], ph, abort_flag, p.err)))) break;
         if (lane == 0) {
-          mbar_arrive_expect_tx(&full[s], C::kA + C::kB);
+          mbar_arrive_expect_tx(&full[s], C::kA + C::kB + kScales + C::kNT * kSpan);
           tma_load_2d(ring + s * kStage, &maps.x[kFp4FewBoxes - 1], &full[s], kb * (kDeep / 2), row);
           tma_load_3d(ring + s * kStage + C::kA, &maps.w, &full[s], kb * (kDeep / 2), f, t.e);
+          const int b = kb * Fp4<FMT>::kBytes / kSpan * kSpan;
+          const uint32_t sf = ring + s * kStage + kSf;
+          tma_load_2d(sf, &maps.x_scales[kFp4FewBoxes - 1], &full[s], b, row);
+          tma_load_3d(sf + kScales, &maps.w_scales, &full[s], b, t.f0, t.e);
+          tma_load_3d(sf + kScales + C::kNT / 2 * kSpan, &maps.w_scales, &full[s], b, t.f0 + C::kNT / 2, t.e);
         }
         __syncwarp();
         if (++s == S) {
@@ -703,7 +772,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
       int s = 0, tc = 0, it = 0;
       uint32_t ph = 0;
       bool ok = true;
-      for (int tile = first; ok && t.at(p, starts, tile); tile += step, ++tc) {
+      // (The votes tell the compiler that the warp walks as one: descriptors then stay in uniform registers.)
+      for (int tile = first; ok && __all_sync(0xFFFFFFFFu, t.at(p, starts, tile)); tile += step, ++tc) {
         const int ab = tc & 1;
         if (tc >= 2 &&
             !(ok = __all_sync(0xFFFFFFFFu, mbar_spin_cluster(&tempty[ab], (static_cast<uint32_t>(tc >> 1) & 1u) ^ 1u, abort_flag, p.err))))
@@ -711,12 +781,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
         tc_fence_after();
         const uint32_t d = tmem + ab * C::kNT;
         for (int kb = 0; kb < cnt; ++kb, ++it) {
-          if (!(ok = __all_sync(0xFFFFFFFFu, mbar_spin_cluster(&sfull[s], ph, abort_flag, p.err)))) break;
+          if (!(ok = __all_sync(0xFFFFFFFFu, mbar_spin(&sfull[s], ph, abort_flag, p.err)))) break;
           tc_fence_after();
           const uint32_t so = static_cast<uint32_t>(s * kStage) >> 4;
           const uint32_t sa = tmem + kScaleAt + (it & (kScaleBufs - 1)) * kScaleCols, sb = sa + 4 * W;
 #pragma unroll
-          for (int i = 0; i < 3 * W; ++i) atom_to_tmem_pair_elect(sa + 4 * i, sd0 + so + i * (kAtom >> 4));
+          for (int i = 0; i < W; ++i) {
+            atom_to_tmem_pair_elect(sa + 4 * i, sd0 + so + i * (kAtom >> 4));
+            atom_to_tmem_pair_elect(sb + 8 * i, sd0 + so + ((kScales + i * kAtom) >> 4));
+            atom_to_tmem_pair_elect(sb + 8 * i + 4, sd0 + so + ((2 * kScales + i * kAtom) >> 4));
+          }
           const int steps = min(4, (p.K - kb * kDeep + 63) / 64);
 #pragma unroll
           for (int kk = 0; kk < 4; ++kk) {
@@ -739,57 +813,32 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
     }
   } else if (warp >= C::kScaleWarp) {
     // ------------------------------------------------------ scales
-    // Warp 0 of a set also sees this CTA's codes land before it reports the stage.
-    using Rows = ScaleRows<FMT, ALIGNED>;
     const int set = (warp - C::kScaleWarp) / 3, atom = (warp - C::kScaleWarp) % 3;
-    const uint32_t atoms = kSf + (atom == 0 ? 0 : (W + atom - 1) * kAtom);
-    const int apart = atom == 0 ? kAtom : 2 * kAtom;
-    const int lift = atom == 0 ? 0 : 128 * (atom - 1) - C::kNT / 2 * static_cast<int>(rank);  // atom row 0 in the tile of codes
-    Rows sc;
-    int g = 0, s = 0;  // stages of the ring so far; the set takes every other one
-    uint32_t ph = 0;
+    const int at = kSf + atom * kScales;
+    const CodeRows codes = {atom == 0 ? 0 : C::kA, atom == 0 ? 0 : 128 * (atom - 1) - C::kNT / 2 * static_cast<int>(rank),
+                            atom == 0 ? 128 : C::kNT / 2};
+    const int rows = atom == 0 ? 128 : C::kNT - 128 * (atom - 1);
+    int g = 0;  // stages before the tile
+    ScaleStages c(set);
     bool ok = true;
-    for (int tile = first; ok && t.at(p, starts, tile); tile += step) {
-      if (atom == 0)
-        sc.open(p.x_scales, p.R, static_cast<int64_t>(t.row0) + 128 * rank, t.rows - 128 * static_cast<int>(rank), p.G, lane);
-      else
-        sc.open(p.w_scales, static_cast<int64_t>(p.E) * p.N, static_cast<int64_t>(t.e) * p.N + t.f0 + 128 * (atom - 1),
-                min(p.N - t.f0, C::kNT) - 128 * (atom - 1), p.G, lane);
-      int kb = (g ^ set) & 1;  // the tile's first stage of this set
-#pragma unroll
-      for (int d = 0; d < Rows::kAhead; ++d) sc.load(d, kb + 2 * d, cnt);
-      int at = s + kb;
-      uint32_t par = ph;
-      if (at >= S) {
-        at -= S;
-        par ^= 1u;
-      }
-      while (kb < cnt && ok) {
-#pragma unroll
-        for (int d = 0; d < Rows::kAhead; ++d) {
-          if (kb >= cnt) break;
-          if (g + kb >= S && !(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&empty[at], par ^ 1u, abort_flag, p.err)))) break;
-          const uint32_t base = ring + at * kStage;
-          ok = store_scales(sc, d, kb, base + atoms, apart, base + (atom == 0 ? 0 : C::kA), lift, atom == 0 ? 128 : C::kNT / 2,
-                            &full[at], par, abort_flag, p.err);
-          if (!ok) break;
-          fence_proxy_async_smem();
-          if (atom == 0 && !(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&full[at], par, abort_flag, p.err)))) break;
-          __syncwarp();
-          if (lane == 0) arrive_cluster(mapa_shared(smem_u32(&sfull[at]), 0));
-          sc.load(d, kb + 2 * Rows::kAhead, cnt);
-          kb += 2;
-          if ((at += 2) >= S) {
-            at -= S;
-            par ^= 1u;
-          }
+    for (int tile = first; ok && t.at(p, starts, tile); tile += step, g += cnt) {
+      while (c.it < g + cnt) {
+        if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&full[c.s], c.ph, abort_flag, p.err)))) break;
+        const uint32_t base = ring + c.s * kStage;
+        turn_scales<FMT>(base + at, rows, c.it - g, base, codes);
+        fence_proxy_async_smem();
+        __syncwarp();
+        // The peer's warps report by a store that does not wait for anything. (With an arrival, which at
+        // cluster scope waits for the writes before it, it took 1,000 cycles a stage.)
+        if (lane == 0) {
+          if (rank != 0)
+            st_async_signal(mapa_shared(smem_u32(&sink[warp - C::kScaleWarp]), 0), mapa_shared(smem_u32(&sfull[c.s]), 0));
+          else if (atom == 0)
+            mbar_arrive_expect_tx(&sfull[c.s], 3 * 4);
+          else
+            mbar_arrive(&sfull[c.s]);
         }
-      }
-      g += cnt;
-      s += cnt;
-      while (s >= S) {
-        s -= S;
-        ph ^= 1u;
+        c.next(S);
       }
     }
   } else {
@@ -848,6 +897,42 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
   }
 }
 
+// Planes of scale bytes whose rows are not whole 16-byte pieces, with rows that are: row r of G bytes to
+// row r of `pitch`, the rest zero. A thread writes a piece; it reads the units of two bytes, or one, that it
+// is made of.
+__global__ void __launch_bounds__(256) sq_fp4_pad_kernel(const PadArgs a) {
+  dependency_wait();
+  dependency_start();
+  const int pieces = a.pitch / 16;
+  const int64_t total = (a.rows[0] + a.rows[1]) * pieces;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
+    int64_t row = i / pieces;
+    const int b = static_cast<int>(i - row * pieces) * 16;
+    const bool second = row >= a.rows[0];
+    if (second) row -= a.rows[0];
+    const uint8_t *src = (second ? a.src[1] : a.src[0]) + row * a.G + b;
+    uint8_t *dst = (second ? a.dst[1] : a.dst[0]) + row * a.pitch + b;
+    uint32_t w[4];
+    if ((a.G & 1) == 0) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t lo = b + 4 * j < a.G ? *reinterpret_cast<const uint16_t *>(src + 4 * j) : 0u;
+        const uint32_t hi = b + 4 * j + 2 < a.G ? *reinterpret_cast<const uint16_t *>(src + 4 * j + 2) : 0u;
+        w[j] = lo | hi << 16;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        w[j] = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (b + 4 * j + e < a.G) w[j] |= static_cast<uint32_t>(src[4 * j + e]) << (8 * e);
+      }
+    }
+    *reinterpret_cast<uint4 *>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
 template <typename Kernel>
 cudaError_t launch_kernel(Kernel kernel, int &done_mask, int most_smem, unsigned grid, int threads, size_t smem, int cluster,
                        cudaStream_t stream, const Fp4Maps &maps, const Fp4Args &p) {
@@ -877,33 +962,39 @@ cudaError_t launch_kernel(Kernel kernel, int &done_mask, int most_smem, unsigned
   return cudaLaunchKernelEx(&cfg, kernel, maps, p);
 }
 
-template <int FMT, bool ALIGNED>
+template <int FMT, bool RAW>
 cudaError_t launch_few_fp4(const Fp4Maps &maps, const Fp4Args &p, cudaStream_t stream) {
   static int done_mask = 0;
-  const size_t smem = static_cast<size_t>(p.stages) * fp4_few_stage(FMT, p.tile_tokens) + 1024;
-  return launch_kernel(sq_fp4_few_kernel<FMT, ALIGNED>, done_mask, kFp4SmemAlone,
+  const size_t smem = static_cast<size_t>(p.stages) * fp4_few_stage(p.tile_tokens) + 1024;
+  return launch_kernel(sq_fp4_few_kernel<FMT, RAW>, done_mask, kFp4SmemAlone,
                     static_cast<unsigned>(p.units * p.splits), Fp4FewCfg::kThreads, smem, p.splits, stream, maps, p);
 }
 
 }  // namespace
 
+cudaError_t launch_fp4_pad(const PadArgs &a, int sm_count, cudaStream_t stream) {
+  const int64_t units = ((a.rows[0] + a.rows[1]) * (a.pitch / 16) + 255) / 256;
+  return launch_after(sq_fp4_pad_kernel, static_cast<unsigned>(std::min<int64_t>(units, 8 * sm_count)), 256, 0, stream, a);
+}
+
 cudaError_t launch_fp4(int fmt, const Fp4Maps &maps, const Fp4Args &p, int sm_count, cudaStream_t stream) {
-  const bool aligned = p.K % kDeep == 0;
+  const bool raw = p.G % kSpan == 0;
   auto launch = [&](auto f, auto al) {
     constexpr int FMT = decltype(f)::value;
-    constexpr bool ALIGNED = decltype(al)::value;
-    if (!p.pair) return launch_few_fp4<FMT, ALIGNED>(maps, p, stream);
+    constexpr bool RAW = decltype(al)::value;
+    if (!p.pair) return launch_few_fp4<FMT, RAW>(maps, p, stream);
+    if (!RAW) return cudaErrorInvalidValue;  // fp4_plan gives its planes whole pieces
     static int done_mask = 0;
-    const size_t smem = fp4_pair_smem(FMT, p.stages, p.offsets ? p.E : 0);
+    const size_t smem = fp4_pair_smem(p.stages, p.offsets ? p.E : 0);
     const int clusters = static_cast<int>(std::min<int64_t>(p.units, sm_count / 2));
-    return launch_kernel(sq_fp4_pair_kernel<FMT, ALIGNED>, done_mask, kFp4SmemMost, 2u * clusters, Fp4PairCfg::kThreads, smem, 1,
+    return launch_kernel(sq_fp4_pair_kernel<FMT>, done_mask, kFp4SmemMost, 2u * clusters, Fp4PairCfg::kThreads, smem, 1,
                          stream, maps, p);
   };
   using std::bool_constant;
   using std::integral_constant;
   if (fmt == 0)
-    return aligned ? launch(integral_constant<int, 0>(), bool_constant<true>()) : launch(integral_constant<int, 0>(), bool_constant<false>());
-  return aligned ? launch(integral_constant<int, 1>(), bool_constant<true>()) : launch(integral_constant<int, 1>(), bool_constant<false>());
+    return raw ? launch(integral_constant<int, 0>(), bool_constant<true>()) : launch(integral_constant<int, 0>(), bool_constant<false>());
+  return raw ? launch(integral_constant<int, 1>(), bool_constant<true>()) : launch(integral_constant<int, 1>(), bool_constant<false>());
 }
 
 }  // namespace sqi

@@ -496,6 +496,7 @@ constexpr int kFp4PairTokens = 256, kFp4PairFeatures = 192;  // a tile of the pa
 struct Fp4Maps {
   CUtensorMap w;                // codes [E][N][K / 2], boxes of 128 bytes x 128 rows (few) or half a pair's features
   CUtensorMap x[kFp4FewBoxes];  // codes [R][K / 2], boxes of 128 bytes x (8 << i) rows
+  CUtensorMap w_scales, x_scales[kFp4FewBoxes];  // scale bytes, boxes of 16 bytes x the same rows (whole 16-byte rows only)
 };
 struct Fp4Args {
   int64_t R;                 // rows
@@ -515,16 +516,16 @@ struct Fp4Args {
   int splits;                // few: parts of the contraction (CTAs of a cluster)
   int stages;                // of the ring
 };
-// A few-token stage: codes of 128 features and a tile's tokens, scale atoms of both.
-constexpr int fp4_few_stage(int fmt, int tile_tokens) { return 128 * 128 + tile_tokens * 128 + 2 * (fmt == 0 ? 4 : 2) * 512; }
-// A pair stage: codes of 128 tokens and half the features, scale atoms of those tokens and of all features; behind
-// the ring eight 2 KiB boxes of the epilogue and the experts' first tiles.
-constexpr int fp4_pair_stage(int fmt) { return 128 * 128 + kFp4PairFeatures / 2 * 128 + 3 * (fmt == 0 ? 4 : 2) * 512; }
-constexpr size_t fp4_pair_smem(int fmt, int stages, int E) {
-  return 1024 + static_cast<size_t>(stages) * fp4_pair_stage(fmt) + 8 * 2048 + (E > 0 ? 4 * (E + 1) : 0);
+// A few-token stage: codes of 128 features and a tile's tokens, scales of 128 rows of both. A pair stage: codes of 128
+// tokens and half the features, scales of those tokens and of all features; behind the ring eight 2 KiB boxes of the
+// epilogue and the experts' first tiles.
+constexpr int fp4_few_stage(int tile_tokens) { return 128 * 128 + tile_tokens * 128 + 2 * 2048; }
+constexpr int fp4_pair_stage() { return 128 * 128 + kFp4PairFeatures / 2 * 128 + 3 * 2048; }
+constexpr size_t fp4_pair_smem(int stages, int E) {
+  return 1024 + static_cast<size_t>(stages) * fp4_pair_stage() + 8 * 2048 + (E > 0 ? 4 * (E + 1) : 0);
 }
 // Kernel, tiles and parts of a product on sm_count SMs: fills the last fields of p.
-inline void fp4_plan(int fmt, int sm_count, Fp4Args &p) {
+inline void fp4_plan(int sm_count, Fp4Args &p) {
   const int64_t groups = p.offsets ? std::min<int64_t>(p.E, p.R) : 1;
   p.pair = p.R >= 192 * groups;
   if (p.pair) {
@@ -532,7 +533,7 @@ inline void fp4_plan(int fmt, int sm_count, Fp4Args &p) {
     p.units = (p.R + (kFp4PairTokens - 1) * groups) / kFp4PairTokens * p.ftiles;
     p.splits = 1;
     p.stages = 8;
-    while (fp4_pair_smem(fmt, p.stages, p.offsets ? p.E : 0) > static_cast<size_t>(kFp4SmemMost)) --p.stages;
+    while (fp4_pair_smem(p.stages, p.offsets ? p.E : 0) > static_cast<size_t>(kFp4SmemMost)) --p.stages;
     return;
   }
   p.ftiles = (p.N + 127) / 128;
@@ -541,10 +542,18 @@ inline void fp4_plan(int fmt, int sm_count, Fp4Args &p) {
   p.units = ((p.R + (p.tile_tokens - 1) * groups) / p.tile_tokens) * p.ftiles;
   const int cnt = (p.K + 255) / 256;
   p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({8, cnt, sm_count / p.units})));
-  const int stage = fp4_few_stage(fmt, p.tile_tokens);
+  const int stage = fp4_few_stage(p.tile_tokens);
   const bool alone = p.units * p.splits <= sm_count;
   p.stages = std::min(8, ((alone ? kFp4SmemAlone : kFp4SmemShared) - 1024) / stage);
 }
+// Planes of rows[i] x G scale bytes copied to rows of `pitch` bytes, a multiple of 16.
+struct PadArgs {
+  const uint8_t *src[2];
+  uint8_t *dst[2];
+  int64_t rows[2];
+  int G, pitch;
+};
+cudaError_t launch_fp4_pad(const PadArgs &a, int sm_count, cudaStream_t stream);
 cudaError_t launch_fp4(int fmt, const Fp4Maps &maps, const Fp4Args &p, int sm_count, cudaStream_t stream);
 
 // Device-side error codes written to the error word.

@@ -105,6 +105,14 @@ def test_experts_of_ragged_sizes(h, fmt, counts, N, K):
     check_grouped(h, fmt, counts, N, K, seed=len(counts) + N)
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("E, per, N, K", [(96, 120, 264, 4096), (96, 60, 392, 2560), (160, 3, 264, 4096), (96, 120, 264, 2080)])
+def test_experts_in_rings_of_an_odd_number_of_slots(h, fmt, E, per, N, K):
+    """Two CTAs share an SM and its shared memory: rings of 3 and 5 slots, gone through many times."""
+    counts = [per + (e * 5) % 9 - 4 if per > 8 else e % (per + 1) for e in range(E)]
+    check_grouped(h, fmt, counts, N, K, seed=E + K)
+
+
 def test_experts_with_negative_scales(h):
     check_grouped(h, pkg.NVFP4, [3, 0, 70, 400], 200, 544, seed=1, signs=True)
     check_grouped(h, pkg.NVFP4, [900, 0, 1300], 328, 1024, seed=2, signs=True)
