@@ -84,11 +84,53 @@ __device__ __forceinline__ void umma_fp4_elect(uint32_t d, uint64_t a, uint64_t 
         : "memory");
 }
 
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, uint64_t *bar, int32_t x, int32_t y,
-                                            int32_t z) {
+// A bounded wait of a whole warp without a call and with votes for its branches: around a call, or where
+// lanes might part, the compiler keeps the descriptors of the loop in ordinary registers and moves them to
+// the uniform ones at every use (12 atoms and 4 MMAs of a stage took 807 cycles to issue, where the
+// tensor cores take 384).
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag, int *err) {
+  if (__all_sync(0xFFFFFFFFu, mbar_test_wait(bar, parity))) return true;
+  const unsigned long long t0 = globaltimer();
+  while (true) {
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+      if (__all_sync(0xFFFFFFFFu, mbar_test_wait(bar, parity))) return true;
+    const bool late = globaltimer() - t0 > kWaitLimitNs;
+    if (__any_sync(0xFFFFFFFFu, late || *abort_flag)) {
+      if (__any_sync(0xFFFFFFFFu, late)) {
+        *abort_flag = 1;
+        atomicOr(err, kErrWaitTimeout);
+      }
+      return false;
+    }
+  }
+}
+
+// Barrier arrivals and TMA loads by an elected lane of a converged warp, for the same reason.
+__device__ __forceinline__ void expect_tx_elect(uint64_t *bar, uint32_t bytes) {
   asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
-          dst),
+      "{\n\t.reg .pred e;\n\t"
+      "elect.sync _|e, 0xFFFFFFFF;\n\t"
+      "@e mbarrier.arrive.expect_tx.release.cta.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(smem_u32(bar)),
+      "r"(bytes)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_2d_elect(uint32_t dst, const CUtensorMap *map, uint64_t *bar, int32_t x, int32_t y) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t"
+      "elect.sync _|e, 0xFFFFFFFF;\n\t"
+      "@e cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], "
+      "[%2];\n\t}" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_3d_elect(uint32_t dst, const CUtensorMap *map, uint64_t *bar, int32_t x, int32_t y,
+                                                  int32_t z) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t"
+      "elect.sync _|e, 0xFFFFFFFF;\n\t"
+      "@e cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], "
+      "[%2];\n\t}" ::"r"(dst),
       "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
       : "memory");
 }
@@ -402,19 +444,16 @@ __global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
     int it = 0, s = 0;
     uint32_t ph = 0;
     for (; it < cnt; ++it) {
-      if (it >= S && !__all_sync(0xFFFFFFFFu, mbar_wait(&empty[s], ph ^ 1u, abort_flag, p.err))) break;
-      if (lane == 0) {
-        mbar_arrive_expect_tx(&full[s], (C::kF + (8u << box)) * (128 + (RAW ? kSpan : 0)));
-        const int x = (it0 + it) * (kDeep / 2);
-        tma_load_3d(ring + s * stage, &maps.w, &full[s], x, f0, expert);
-        tma_load_2d(ring + s * stage + x_off, &maps.x[box], &full[s], x, row0);
-        if (RAW) {
-          const int b = (it0 + it) * Fp4<FMT>::kBytes / kSpan * kSpan;
-          tma_load_3d(ring + s * stage + sf_off, &maps.w_scales, &full[s], b, f0, expert);
-          tma_load_2d(ring + s * stage + sf_off + kScales, &maps.x_scales[box], &full[s], b, row0);
-        }
+      if (it >= S && !warp_wait(&empty[s], ph ^ 1u, abort_flag, p.err)) break;
+      expect_tx_elect(&full[s], (C::kF + (8u << box)) * (128 + (RAW ? kSpan : 0)));
+      const int x = (it0 + it) * (kDeep / 2);
+      tma_load_3d_elect(ring + s * stage, &maps.w, &full[s], x, f0, expert);
+      tma_load_2d_elect(ring + s * stage + x_off, &maps.x[box], &full[s], x, row0);
+      if (RAW) {
+        const int b = (it0 + it) * Fp4<FMT>::kBytes / kSpan * kSpan;
+        tma_load_3d_elect(ring + s * stage + sf_off, &maps.w_scales, &full[s], b, f0, expert);
+        tma_load_2d_elect(ring + s * stage + sf_off + kScales, &maps.x_scales[box], &full[s], b, row0);
       }
-      __syncwarp();
       if (++s == S) {
         s = 0;
         ph ^= 1u;
@@ -430,9 +469,7 @@ __global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
     uint32_t ph = 0;
     bool ok = true;
     for (int it = 0; it < cnt && ok; ++it) {
-      if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&sfull[s], ph, abort_flag, p.err) &&
-                                             (RAW || mbar_wait(&full[s], ph, abort_flag, p.err)))))
-        break;
+      if (!(ok = warp_wait(&sfull[s], ph, abort_flag, p.err) && (RAW || warp_wait(&full[s], ph, abort_flag, p.err)))) break;
       if (!RAW) fence_proxy_async_smem();
       tc_fence_after();
       const uint32_t so = static_cast<uint32_t>(s * stage) >> 4;
@@ -741,21 +778,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
     int it = 0, s = 0;
     uint32_t ph = 1;
     bool ok = true;
-    for (int tile = first; ok && t.at(p, starts, tile); tile += step) {
+    for (int tile = first; ok && __all_sync(0xFFFFFFFFu, t.at(p, starts, tile)); tile += step) {
       const int row = t.row0 + 128 * static_cast<int>(rank), f = t.f0 + C::kNT / 2 * static_cast<int>(rank);
       for (int kb = 0; kb < cnt; ++kb, ++it) {
-        if (it >= S && !(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&empty[s], ph, abort_flag, p.err)))) break;
-        if (lane == 0) {
-          mbar_arrive_expect_tx(&full[s], C::kA + C::kB + kScales + C::kNT * kSpan);
-          tma_load_2d(ring + s * kStage, &maps.x[kFp4FewBoxes - 1], &full[s], kb * (kDeep / 2), row);
-          tma_load_3d(ring + s * kStage + C::kA, &maps.w, &full[s], kb * (kDeep / 2), f, t.e);
-          const int b = kb * Fp4<FMT>::kBytes / kSpan * kSpan;
-          const uint32_t sf = ring + s * kStage + kSf;
-          tma_load_2d(sf, &maps.x_scales[kFp4FewBoxes - 1], &full[s], b, row);
-          tma_load_3d(sf + kScales, &maps.w_scales, &full[s], b, t.f0, t.e);
-          tma_load_3d(sf + kScales + C::kNT / 2 * kSpan, &maps.w_scales, &full[s], b, t.f0 + C::kNT / 2, t.e);
-        }
-        __syncwarp();
+        if (it >= S && !(ok = warp_wait(&empty[s], ph, abort_flag, p.err))) break;
+        expect_tx_elect(&full[s], C::kA + C::kB + kScales + C::kNT * kSpan);
+        tma_load_2d_elect(ring + s * kStage, &maps.x[kFp4FewBoxes - 1], &full[s], kb * (kDeep / 2), row);
+        tma_load_3d_elect(ring + s * kStage + C::kA, &maps.w, &full[s], kb * (kDeep / 2), f, t.e);
+        const int b = kb * Fp4<FMT>::kBytes / kSpan * kSpan;
+        const uint32_t sf = ring + s * kStage + kSf;
+        tma_load_2d_elect(sf, &maps.x_scales[kFp4FewBoxes - 1], &full[s], b, row);
+        tma_load_3d_elect(sf + kScales, &maps.w_scales, &full[s], b, t.f0, t.e);
+        tma_load_3d_elect(sf + kScales + C::kNT / 2 * kSpan, &maps.w_scales, &full[s], b, t.f0 + C::kNT / 2, t.e);
         if (++s == S) {
           s = 0;
           ph ^= 1u;
@@ -776,12 +810,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
       for (int tile = first; ok && __all_sync(0xFFFFFFFFu, t.at(p, starts, tile)); tile += step, ++tc) {
         const int ab = tc & 1;
         if (tc >= 2 &&
-            !(ok = __all_sync(0xFFFFFFFFu, mbar_spin_cluster(&tempty[ab], (static_cast<uint32_t>(tc >> 1) & 1u) ^ 1u, abort_flag, p.err))))
+            !(ok = warp_wait(&tempty[ab], (static_cast<uint32_t>(tc >> 1) & 1u) ^ 1u, abort_flag, p.err)))
           break;
         tc_fence_after();
         const uint32_t d = tmem + ab * C::kNT;
         for (int kb = 0; kb < cnt; ++kb, ++it) {
-          if (!(ok = __all_sync(0xFFFFFFFFu, mbar_spin(&sfull[s], ph, abort_flag, p.err)))) break;
+          if (!(ok = warp_wait(&sfull[s], ph, abort_flag, p.err))) break;
           tc_fence_after();
           const uint32_t so = static_cast<uint32_t>(s * kStage) >> 4;
           const uint32_t sa = tmem + kScaleAt + (it & (kScaleBufs - 1)) * kScaleCols, sb = sa + 4 * W;
