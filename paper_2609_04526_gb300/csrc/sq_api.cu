@@ -53,7 +53,7 @@ struct DeviceState {
   int64_t *plane_acc;    // counter accumulators of the multi-plane calls (zero between calls)
   Scratch sort;          // per-CTA counts of the sort by expert
   Scratch head;          // packed rows, exponentials and partial planes of the head loss
-  Scratch scales;        // scale planes with padded rows of the 4-bit products
+  Scratch scales;        // scale atoms of the 4-bit products
 };
 
 constexpr int64_t kMaxDim = int64_t(1) << 24;       // N, K limit
@@ -606,38 +606,43 @@ sq_status run_fp4(sq_handle h, int fmt, int E, int64_t N, int64_t K, const uint8
   p.offsets = offsets;
   p.out = Y;
   p.err = dev->err_word;
-  sqi::fp4_plan(dev->sm_count, p);
-  int pitch = p.G;  // of the scale planes that TMA reads
-  const uint8_t *x_scales = x->scales;
-  if (p.pair && p.G % 16 != 0) {
-    pitch = (p.G + 15) / 16 * 16;
-    const int64_t w_rows = E * N;
-    SQ_TRY(ensure_scratch(h, dev->scales, static_cast<size_t>((w_rows + x->R) * pitch), stream, "a product of such a K"));
-    sqi::PadArgs pad = {{scales, x_scales}, {}, {w_rows, x->R}, p.G, pitch};
-    pad.dst[0] = static_cast<uint8_t *>(dev->scales.ptr);
-    pad.dst[1] = pad.dst[0] + w_rows * pitch;
-    const cudaError_t e = sqi::launch_fp4_pad(pad, dev->sm_count, stream);
-    if (e != cudaSuccess) return cuda_fail(h, e, "scale plane launch");
-    scales = pad.dst[0];
-    x_scales = pad.dst[1];
-    p.G = pitch;
+  sqi::fp4_plan(fmt, dev->sm_count, p);
+  cudaError_t e;
+  if (p.pair) {
+    // scratch: the atoms of both operands' scales, one word of each CTA that writes them
+    const int64_t cnt = (K + 255) / 256, block = cnt * sqi::fp4_atoms(fmt);
+    const int64_t x_bytes = p.token_blocks * block, w_bytes = 2 * int64_t(E) * p.ftiles * block;
+    SQ_TRY(ensure_scratch(h, dev->scales, static_cast<size_t>(x_bytes + w_bytes + 4 * int64_t(p.atom_ctas)), stream,
+                          "a 4-bit product of this size"));
+    uint8_t *base = static_cast<uint8_t *>(dev->scales.ptr);
+    p.x_atoms = reinterpret_cast<uint4 *>(base);
+    p.w_atoms = reinterpret_cast<uint4 *>(base + x_bytes);
+    p.negative = reinterpret_cast<int *>(base + x_bytes + w_bytes);
+    sqi::Fp4PairMaps m;
+    const uint32_t atoms = sqi::fp4_atoms(fmt) / 512;
+    SQ_TRY(make_experts_map(h, &m.w, codes, K / 2, N, E, 128, sqi::kFp4PairFeatures / 2, CU_TENSOR_MAP_SWIZZLE_128B));
+    SQ_TRY(make_map(h, &m.x, x->codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, K / 2, x->R, 128, 128, CU_TENSOR_MAP_SWIZZLE_128B));
+    SQ_TRY(make_map(h, &m.x_atoms, p.x_atoms, CU_TENSOR_MAP_DATA_TYPE_UINT32, 4, 128, x_bytes / 512, 128, atoms,
+                    CU_TENSOR_MAP_SWIZZLE_NONE));
+    SQ_TRY(make_map(h, &m.w_atoms, p.w_atoms, CU_TENSOR_MAP_DATA_TYPE_UINT32, 4, 128, w_bytes / 512, 128, 2 * atoms,
+                    CU_TENSOR_MAP_SWIZZLE_NONE));
+    e = sqi::launch_fp4_pair(fmt, m, p, dev->sm_count, stream);
+  } else {
+    // rows of codes in boxes of 128 bytes and, where they are whole 16-byte pieces, of scale bytes in boxes of 16
+    sqi::Fp4Maps m;
+    const bool raw = p.G % 16 == 0;
+    SQ_TRY(make_experts_map(h, &m.w, codes, K / 2, N, E, 128, 128, CU_TENSOR_MAP_SWIZZLE_128B));
+    if (raw) SQ_TRY(make_experts_map(h, &m.w_scales, scales, p.G, N, E, 16, 128, CU_TENSOR_MAP_SWIZZLE_NONE));
+    for (int i = 0; i < sqi::kFp4FewBoxes; ++i) {
+      if (offsets ? (8 << i) > p.tile_tokens : (8 << i) != p.tile_tokens) continue;  // of ragged experts every smaller one
+      SQ_TRY(make_map(h, &m.x[i], x->codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, K / 2, x->R, 128, 8u << i,
+                      CU_TENSOR_MAP_SWIZZLE_128B));
+      if (raw)
+        SQ_TRY(make_map(h, &m.x_scales[i], x->scales, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.G, x->R, 16, 8u << i,
+                        CU_TENSOR_MAP_SWIZZLE_NONE));
+    }
+    e = sqi::launch_fp4_few(fmt, m, p, stream);
   }
-  // Rows of codes in boxes of 128 bytes and, where they are whole 16-byte pieces, of scale bytes in boxes of 16.
-  sqi::Fp4Maps m;
-  const uint32_t features = p.pair ? sqi::kFp4PairFeatures / 2 : 128;
-  const bool raw = pitch % 16 == 0;
-  SQ_TRY(make_experts_map(h, &m.w, codes, K / 2, N, E, 128, features, CU_TENSOR_MAP_SWIZZLE_128B));
-  if (raw) SQ_TRY(make_experts_map(h, &m.w_scales, scales, pitch, N, E, 16, features, CU_TENSOR_MAP_SWIZZLE_NONE));
-  for (int i = sqi::kFp4FewBoxes - 1; i >= 0; --i) {
-    // the pair kernel's 128 rows; a tile's of the few-token kernel, and with ragged experts every smaller one
-    if (p.pair ? i < sqi::kFp4FewBoxes - 1 : offsets ? (8 << i) > p.tile_tokens : (8 << i) != p.tile_tokens) continue;
-    SQ_TRY(make_map(h, &m.x[i], x->codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, K / 2, x->R, 128, 8u << i,
-                    CU_TENSOR_MAP_SWIZZLE_128B));
-    if (raw)
-      SQ_TRY(make_map(h, &m.x_scales[i], x_scales, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, pitch, x->R, 16, 8u << i,
-                      CU_TENSOR_MAP_SWIZZLE_NONE));
-  }
-  const cudaError_t e = sqi::launch_fp4(fmt, m, p, dev->sm_count, stream);
   if (e != cudaSuccess) return cuda_fail(h, e, "4-bit product launch");
   return SQ_OK;
 }

@@ -6,13 +6,14 @@
 // to a byte, and the tensor cores apply the scale bytes of both operands to each block's products
 // before they add them up in fp32. What is left to the SM is to bring the scale bytes, row-major
 // planes in memory, into the order that the tensor cores read: atoms of 128 rows x 4 bytes, the words
-// of rows l, l + 32, l + 64 and l + 96 side by side in line l. TMA brings 16 bytes of each row and a
-// warp turns them into atoms, in place. A plane whose rows are not whole 16-byte pieces (K / 16 or K /
-// 32 not a multiple of 16) has no TMA descriptor. For many tokens it is copied with longer rows first;
-// for few the warp loads the bytes itself. (Those loads take 37 wavefronts each, the lanes' rows being
-// different lines: in the pair kernel 441 of a stage whose MMAs take 384 cycles. And the proxy fence
-// behind the atoms waits for the loads that run ahead, so on that path it is the reader that executes
-// it, behind the barrier.)
+// of rows l, l + 32, l + 64 and l + 96 side by side in line l. For many tokens a launch ahead lays both
+// planes out as atoms, which TMA then brings like the codes; for few, TMA brings 16 bytes of each row
+// and a warp turns them into atoms, in place, or, where rows are not whole 16-byte pieces (K / 16 or K /
+// 32 not a multiple of 16) and have no TMA descriptor, loads them itself. (Turned in the pair kernel
+// too, a stage took 750 cycles whatever its MMAs: 390 ns with tiles of 128, 160, 192 and 224 features
+// alike. Loaded by warps 1,600: such loads take 37 wavefronts each, the lanes' rows being different
+// lines, and the proxy fence behind the atoms waits for the loads that run ahead. So where warps load
+// it is the reader that executes the fence, behind the barrier.)
 //
 // The tensor cores take E4M3 scales without a sign. A negative scale byte (training may drive one below
 // zero) goes in as its magnitude, and the codes of its block, in shared memory by then, change their
@@ -132,6 +133,28 @@ __device__ __forceinline__ void tma_load_3d_elect(uint32_t dst, const CUtensorMa
       "@e cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], "
       "[%2];\n\t}" ::"r"(dst),
       "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
+
+// The same of a CTA pair, counted on a barrier of either CTA (`bar_cluster`).
+__device__ __forceinline__ void tma_load_2d_pair_elect(uint32_t dst, const CUtensorMap *map, uint32_t bar_cluster, int32_t x,
+                                                       int32_t y) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t"
+      "elect.sync _|e, 0xFFFFFFFF;\n\t"
+      "@e cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4}], "
+      "[%2];\n\t}" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar_cluster), "r"(x), "r"(y)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_3d_pair_elect(uint32_t dst, const CUtensorMap *map, uint32_t bar_cluster, int32_t x,
+                                                       int32_t y, int32_t z) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t"
+      "elect.sync _|e, 0xFFFFFFFF;\n\t"
+      "@e cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4, %5}], "
+      "[%2];\n\t}" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar_cluster), "r"(x), "r"(y), "r"(z)
       : "memory");
 }
 
@@ -609,19 +632,21 @@ __global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
 // ---------------------------------------------------------------- many tokens
 //
 // A cluster of two CTAs per tile of 256 tokens x kNT features (tcgen05.mma.cta_group::2): each CTA
-// holds 128 of the tokens and half of the features' codes, the scales of its tokens and those of all
+// holds 128 of the tokens and half of the features' codes, the atoms of its tokens and those of all
 // the features. Persistent, with two accumulators, so a tile's epilogue runs under the next one's MMAs.
+//
+// A launch ahead (sq_fp4_atoms_kernel) writes the atoms: of each token tile two blocks of 128 rows, of
+// each feature tile two (the second of fewer rows), for every stage, and whether it met a negative scale.
+// Only then the pair kernel has a warp that mends the codes of each stage before the MMAs may read it.
 
 struct Fp4PairCfg {
   static constexpr int kTokens = kFp4PairTokens, kNT = kFp4PairFeatures;
-  static constexpr int kEpiWarps = 8;  // lane quadrant w % 4, half of the columns w / 4
-  static constexpr int kScaleWarp = kEpiWarps, kScaleWarps = 6;  // two sets of three: an atom each of every other stage
-  static constexpr int kTmaWarp = kScaleWarp + kScaleWarps, kMmaWarp = kTmaWarp + 1;
-  static constexpr int kThreads = 32 * (kMmaWarp + 1);
+  static constexpr int kEpiWarps = 8;  // lane quadrant w % 4, every other 32 columns from w / 4 on
+  static constexpr int kTmaWarp = kEpiWarps, kMmaWarp = kTmaWarp + 1, kMendWarp = kMmaWarp + 1;
+  static constexpr int kThreads = 32 * (kMendWarp + 1);
   static constexpr int kA = 128 * 128, kB = kNT / 2 * 128;
   static constexpr int kMaxStages = 8;
   static constexpr int kBox = 32 * 64;  // 32 rows x 32 columns of an epilogue warp
-  static constexpr int kMostTable = (kRouteMaxExperts + 1) * 4;
 };
 static_assert(Fp4PairCfg::kNT <= 256 && Fp4PairCfg::kNT % 32 == 0 && 2 * Fp4PairCfg::kNT + 48 <= 512,
               "two accumulators and a stage's scales in tensor memory");
@@ -678,6 +703,7 @@ __device__ __forceinline__ void arrive_cluster(uint32_t cluster_bar) {
 // increasing order, so the expert only moves forward.
 struct Fp4Tile {
   int e = 0, row0, rows, f0;
+  int token_tile, feature_tile;  // of all experts
   __device__ __forceinline__ bool at(const Fp4Args &p, const int *starts, int tile) {
     int tm, tn;
     if (p.offsets) {
@@ -688,35 +714,162 @@ struct Fp4Tile {
       tile_coords(tile - starts[e], (starts[e + 1] - starts[e]) / p.ftiles, p.ftiles, tm, tn);
       row0 = lo + tm * kFp4PairTokens;
       rows = min(kFp4PairTokens, hi - row0);
+      token_tile = starts[e] / p.ftiles + tm;
     } else {
       if (tile >= p.units) return false;
       tile_coords(tile, static_cast<int>(p.units) / p.ftiles, p.ftiles, tm, tn);
       row0 = tm * kFp4PairTokens;
       rows = static_cast<int>(min(static_cast<int64_t>(kFp4PairTokens), p.R - row0));
+      token_tile = tm;
     }
     f0 = tn * kFp4PairFeatures;
+    feature_tile = e * p.ftiles + tn;
     return true;
   }
 };
 
+// Atoms of 128 rows and 8 stages per CTA. The rows' bytes come in whole 16-byte pieces to shared memory
+// (lines apart by an odd number of pieces, free of bank conflicts) and are cut out from there.
+template <int FMT>
+struct AtomCfg {
+  static constexpr int kThreads = 256, kStages = 8;
+  static constexpr int kSpanBytes = kStages * Fp4<FMT>::kBytes;     // of a row: 128 or 64
+  static constexpr int kPieces = kSpanBytes / 16 + 1;               // that hold them
+  static_assert(kPieces % 2 == 1, "rows an odd number of 16-byte pieces apart");
+};
+
+template <int FMT>
+__global__ void __launch_bounds__(AtomCfg<FMT>::kThreads) sq_fp4_atoms_kernel(const Fp4Args p) {
+  using C = AtomCfg<FMT>;
+  constexpr int W = Fp4<FMT>::kWords;
+  __shared__ uint4 piece[128 * C::kPieces];
+  __shared__ int info[3];
+  const int cnt = (p.K + kDeep - 1) / kDeep, groups = (cnt + C::kStages - 1) / C::kStages;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  int block = static_cast<int>(blockIdx.x) / groups;
+  const int kb0 = (static_cast<int>(blockIdx.x) - block * groups) * C::kStages;
+  dependency_wait();
+  dependency_start();
+  const bool tokens = block < p.token_blocks;
+  const uint8_t *plane = p.w_scales;
+  int64_t row0, plane_rows = static_cast<int64_t>(p.E) * p.N;
+  int rows;
+  uint4 *out;
+  if (tokens) {
+    if (p.offsets) {
+      if (warp == 0) {
+        int e, r0, n;
+        find_tile(p, block >> 1, kFp4PairTokens, e, r0, n);
+        if (lane == 0) {
+          info[0] = r0;
+          info[1] = n;
+        }
+      }
+      __syncthreads();
+      row0 = info[0];
+      rows = info[1];
+    } else {
+      row0 = static_cast<int64_t>(block >> 1) * kFp4PairTokens;
+      rows = static_cast<int>(min(static_cast<int64_t>(kFp4PairTokens), p.R - row0));
+    }
+    plane = p.x_scales;
+    plane_rows = p.R;
+    row0 += 128 * (block & 1);
+    rows -= 128 * (block & 1);
+    out = p.x_atoms + static_cast<int64_t>(block) * cnt * (W * kAtom / 16);
+  } else {
+    block -= p.token_blocks;
+    const int tile = block >> 1, e = tile / p.ftiles, f0 = (tile - e * p.ftiles) * kFp4PairFeatures + 128 * (block & 1);
+    row0 = static_cast<int64_t>(e) * p.N + f0;
+    rows = min(p.N - f0, kFp4PairFeatures - 128 * (block & 1));
+    out = p.w_atoms + (static_cast<int64_t>(tile) * cnt * 2 + (block & 1)) * (W * kAtom / 16);
+  }
+  rows = min(rows, 128);
+  const uint8_t *first = plane + row0 * p.G, *end = plane + plane_rows * p.G;
+  for (int i = threadIdx.x; i < rows * C::kPieces; i += C::kThreads) {
+    const int r = i / C::kPieces, j = i - r * C::kPieces;
+    const uint8_t *at = first + static_cast<int64_t>(r) * p.G + kb0 * Fp4<FMT>::kBytes;  // of the row's bytes
+    const uint8_t *from = at - reinterpret_cast<uintptr_t>(at) % 16 + 16 * j;
+    const int64_t left = end - from;  // of the plane
+    uint4 x = make_uint4(0, 0, 0, 0);
+    if (left >= 16) {
+      x = *reinterpret_cast<const uint4 *>(from);
+    } else if (left > 0) {  // the plane ends inside
+      uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int b = 0; b < 16; ++b)
+        if (b < left) w[b / 4] |= static_cast<uint32_t>(from[b]) << (8 * (b % 4));
+      x = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    piece[i] = x;
+  }
+  __syncthreads();
+  uint32_t sign = 0;
+  const int kb = kb0 + warp;
+  if (kb < cnt) {
+    uint32_t w[4][W];
+    const int valid = p.G - kb * Fp4<FMT>::kBytes;  // scale bytes of the row from the stage's first on
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int row = lane + 32 * r;
+      uint32_t y[8] = {};
+      const uintptr_t at = reinterpret_cast<uintptr_t>(first) + static_cast<int64_t>(row) * p.G + kb0 * Fp4<FMT>::kBytes;
+      const int from = static_cast<int>(at % 16) + warp * Fp4<FMT>::kBytes;  // in the row's pieces
+      if (row < rows) {
+        const uint4 *q = piece + row * C::kPieces + from / 16;
+        const uint4 a = q[0];
+        y[0] = a.x, y[1] = a.y, y[2] = a.z, y[3] = a.w;
+        if (from % 16 + Fp4<FMT>::kBytes > 16) {
+          const uint4 b = q[1];
+          y[4] = b.x, y[5] = b.y, y[6] = b.z, y[7] = b.w;
+        }
+      }
+      const int shift = from % 16;
+      if (shift & 8) {
+#pragma unroll
+        for (int i = 0; i < 6; ++i) y[i] = y[i + 2];
+      }
+      if (shift & 4) {
+#pragma unroll
+        for (int i = 0; i < 5; ++i) y[i] = y[i + 1];
+      }
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        const int b = valid - 4 * i;
+        w[r][i] = __funnelshift_r(y[i], y[i + 1], 8 * (shift & 3));
+        if (b < 4) w[r][i] = b <= 0 ? 0u : w[r][i] & ((1u << (8 * b)) - 1);
+        sign |= w[r][i];
+      }
+    }
+    uint4 *dst = out + static_cast<int64_t>(kb) * (W * kAtom / 16) * (tokens ? 1 : 2) + lane;
+#pragma unroll
+    for (int i = 0; i < W; ++i) dst[i * (kAtom / 16)] = make_uint4(w[0][i], w[1][i], w[2][i], w[3][i]);
+  }
+  if (FMT == 0) {
+    const int any = __syncthreads_or(sign & 0x80808080u);
+    if (threadIdx.x == 0) p.negative[blockIdx.x] = any != 0;
+  }
+}
+
 template <int FMT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads, 1)
-    sq_fp4_pair_kernel(const __grid_constant__ Fp4Maps maps, const Fp4Args p) {
+    sq_fp4_pair_kernel(const __grid_constant__ Fp4PairMaps maps, const Fp4Args p) {
   using C = Fp4PairCfg;
   constexpr int W = Fp4<FMT>::kWords;
-  constexpr int kSf = C::kA + C::kB, kStage = kSf + 3 * kScales;
+  constexpr int kBlock = W * kAtom;  // the atoms of 128 rows and a stage
+  constexpr int kSf = C::kA + C::kB, kBytes = kSf + 3 * kBlock, kStage = fp4_pair_stage(FMT);
+  static_assert(kBytes <= kStage && kStage % 1024 == 0, "a stage");
   constexpr int kScaleCols = 12 * W, kScaleAt = 2 * C::kNT, kScaleBufs = (512 - kScaleAt) / kScaleCols >= 2 ? 2 : 1;
   extern __shared__ uint8_t fp4_smem_raw[];
   uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(fp4_smem_raw) + 1023) & ~uintptr_t(1023));
   __shared__ uint64_t bars[3 * C::kMaxStages + 5];
-  __shared__ uint32_t sink[3 * 2];  // leader: what the peer's signals write
-  __shared__ uint32_t tmem_slot;
+  __shared__ uint32_t tmem_slot, sink;
   __shared__ int abort_word;
   volatile int *abort_flag = &abort_word;
   const int S = p.stages;
-  uint64_t *full = bars;                    // [S] this CTA's codes landed                          (1 arrival + tx)
-  uint64_t *sfull = full + C::kMaxStages;   // [S] leader: atoms and codes of both CTAs are there   (3 warps, the peer's bytes)
-  uint64_t *empty = sfull + C::kMaxStages;  // [S] the pair's MMAs have read the stage              (multicast commit)
+  uint64_t *full = bars;                    // [S] leader: both CTAs' stages are there              (1 arrival + tx)
+  uint64_t *landed = full + C::kMaxStages;  // [S] with codes to mend: this CTA's copies have landed  (1 arrival + tx)
+  uint64_t *empty = landed + C::kMaxStages;  // [S] the pair's MMAs have read the stage             (multicast commit)
   uint64_t *tfull = empty + C::kMaxStages;  // [2] accumulator complete                             (multicast commit)
   uint64_t *tempty = tfull + 2;             // [2] leader: both epilogues have read it              (8 warps of each)
   uint64_t *drain = tempty + 2;
@@ -727,7 +880,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) {
       mbar_init(&full[s], 1);
-      mbar_init(&sfull[s], 3);
+      mbar_init(&landed[s], 1);
       mbar_init(&empty[s], 1);
     }
     for (int b = 0; b < 2; ++b) {
@@ -742,6 +895,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
   if (warp == C::kMmaWarp) tmem_alloc_pair(&tmem_slot, 512);
   dependency_wait();
   dependency_start();
+  bool mend = false;  // some scale is negative
+  if (FMT == 0)
+    for (int i = threadIdx.x; i < p.atom_ctas; i += C::kThreads) mend |= p.negative[i] != 0;
   if (p.offsets) {
     for (int e = threadIdx.x; e < p.E; e += C::kThreads) {
       int lo, hi;
@@ -765,7 +921,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
     }
   }
   tc_fence_before();
-  __syncthreads();
+  mend = __syncthreads_or(mend);
   cluster_sync_all();
   tc_fence_after();
   const uint32_t tmem = tmem_slot, ring = smem_u32(smem);
@@ -774,30 +930,40 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
   Fp4Tile t;
 
   if (warp == C::kTmaWarp) {
-    // ------------------------------------------------------ codes
+    // ------------------------------------------------------ codes and atoms
+    // Counted on the leader's barrier or, where codes have to be mended, on this CTA's own.
     int it = 0, s = 0;
     uint32_t ph = 1;
     bool ok = true;
     for (int tile = first; ok && __all_sync(0xFFFFFFFFu, t.at(p, starts, tile)); tile += step) {
       const int row = t.row0 + 128 * static_cast<int>(rank), f = t.f0 + C::kNT / 2 * static_cast<int>(rank);
+      int xa = (2 * t.token_tile + static_cast<int>(rank)) * cnt * W, wa = t.feature_tile * cnt * 2 * W;  // atoms' rows of 512 bytes
       for (int kb = 0; kb < cnt; ++kb, ++it) {
         if (it >= S && !(ok = warp_wait(&empty[s], ph, abort_flag, p.err))) break;
-        expect_tx_elect(&full[s], C::kA + C::kB + kScales + C::kNT * kSpan);
-        tma_load_2d_elect(ring + s * kStage, &maps.x[kFp4FewBoxes - 1], &full[s], kb * (kDeep / 2), row);
-        tma_load_3d_elect(ring + s * kStage + C::kA, &maps.w, &full[s], kb * (kDeep / 2), f, t.e);
-        const int b = kb * Fp4<FMT>::kBytes / kSpan * kSpan;
-        const uint32_t sf = ring + s * kStage + kSf;
-        tma_load_2d_elect(sf, &maps.x_scales[kFp4FewBoxes - 1], &full[s], b, row);
-        tma_load_3d_elect(sf + kScales, &maps.w_scales, &full[s], b, t.f0, t.e);
-        tma_load_3d_elect(sf + kScales + C::kNT / 2 * kSpan, &maps.w_scales, &full[s], b, t.f0 + C::kNT / 2, t.e);
+        const uint32_t at = ring + s * kStage;
+        uint32_t bar = smem_u32(&landed[s]);
+        if (mend) {
+          expect_tx_elect(&landed[s], kBytes);
+        } else {
+          if (rank == 0) expect_tx_elect(&full[s], 2 * kBytes);
+          bar = mapa_shared(smem_u32(&full[s]), 0);
+        }
+        tma_load_2d_pair_elect(at, &maps.x, bar, kb * (kDeep / 2), row);
+        tma_load_3d_pair_elect(at + C::kA, &maps.w, bar, kb * (kDeep / 2), f, t.e);
+        tma_load_2d_pair_elect(at + kSf, &maps.x_atoms, bar, 0, xa);
+        tma_load_2d_pair_elect(at + kSf + kBlock, &maps.w_atoms, bar, 0, wa);
+        xa += W;
+        wa += 2 * W;
         if (++s == S) {
           s = 0;
           ph ^= 1u;
         }
       }
     }
-    if (*abort_flag)
-      for (int i = (it > S ? it - S : 0); i < it; ++i) mbar_drain(&full[i % S], static_cast<uint32_t>(i / S) & 1u);
+    if (*abort_flag && (mend || rank == 0)) {
+      uint64_t *bar = mend ? landed : full;
+      for (int i = (it > S ? it - S : 0); i < it; ++i) mbar_drain(&bar[i % S], static_cast<uint32_t>(i / S) & 1u);
+    }
   } else if (warp == C::kMmaWarp) {
     // ------------------------------------------------------ MMA issuer (leader; one elected lane)
     if (rank == 0) {
@@ -806,7 +972,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
       int s = 0, tc = 0, it = 0;
       uint32_t ph = 0;
       bool ok = true;
-      // (The votes tell the compiler that the warp walks as one: descriptors then stay in uniform registers.)
+      // (The votes tell the compiler that the warp walks as one.)
       for (int tile = first; ok && __all_sync(0xFFFFFFFFu, t.at(p, starts, tile)); tile += step, ++tc) {
         const int ab = tc & 1;
         if (tc >= 2 &&
@@ -815,15 +981,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
         tc_fence_after();
         const uint32_t d = tmem + ab * C::kNT;
         for (int kb = 0; kb < cnt; ++kb, ++it) {
-          if (!(ok = warp_wait(&sfull[s], ph, abort_flag, p.err))) break;
+          if (!(ok = warp_wait(&full[s], ph, abort_flag, p.err))) break;
           tc_fence_after();
           const uint32_t so = static_cast<uint32_t>(s * kStage) >> 4;
           const uint32_t sa = tmem + kScaleAt + (it & (kScaleBufs - 1)) * kScaleCols, sb = sa + 4 * W;
 #pragma unroll
           for (int i = 0; i < W; ++i) {
             atom_to_tmem_pair_elect(sa + 4 * i, sd0 + so + i * (kAtom >> 4));
-            atom_to_tmem_pair_elect(sb + 8 * i, sd0 + so + ((kScales + i * kAtom) >> 4));
-            atom_to_tmem_pair_elect(sb + 8 * i + 4, sd0 + so + ((2 * kScales + i * kAtom) >> 4));
+            atom_to_tmem_pair_elect(sb + 8 * i, sd0 + so + ((kBlock + i * kAtom) >> 4));
+            atom_to_tmem_pair_elect(sb + 8 * i + 4, sd0 + so + ((2 * kBlock + i * kAtom) >> 4));
           }
           const int steps = min(4, (p.K - kb * kDeep + 63) / 64);
 #pragma unroll
@@ -845,40 +1011,49 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
       commit_pair_elect(drain);
       mbar_drain(drain, 0);
     }
-  } else if (warp >= C::kScaleWarp) {
-    // ------------------------------------------------------ scales
-    const int set = (warp - C::kScaleWarp) / 3, atom = (warp - C::kScaleWarp) % 3;
-    const int at = kSf + atom * kScales;
-    const CodeRows codes = {atom == 0 ? 0 : C::kA, atom == 0 ? 0 : 128 * (atom - 1) - C::kNT / 2 * static_cast<int>(rank),
-                            atom == 0 ? 128 : C::kNT / 2};
-    const int rows = atom == 0 ? 128 : C::kNT - 128 * (atom - 1);
-    int g = 0;  // stages before the tile
-    ScaleStages c(set);
-    bool ok = true;
-    for (int tile = first; ok && t.at(p, starts, tile); tile += step, g += cnt) {
-      while (c.it < g + cnt) {
-        if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&full[c.s], c.ph, abort_flag, p.err)))) break;
-        const uint32_t base = ring + c.s * kStage;
-        turn_scales<FMT>(base + at, rows, c.it - g, base, codes);
-        fence_proxy_async_smem();
-        __syncwarp();
-        // The peer's warps report by a store that does not wait for anything. (With an arrival, which at
-        // cluster scope waits for the writes before it, it took 1,000 cycles a stage.)
-        if (lane == 0) {
-          if (rank != 0)
-            st_async_signal(mapa_shared(smem_u32(&sink[warp - C::kScaleWarp]), 0), mapa_shared(smem_u32(&sfull[c.s]), 0));
-          else if (atom == 0)
-            mbar_arrive_expect_tx(&sfull[c.s], 3 * 4);
-          else
-            mbar_arrive(&sfull[c.s]);
+  } else if (warp == C::kMendWarp) {
+    // ------------------------------------------------------ codes of blocks with a negative scale
+    if (FMT == 0 && mend) {
+      int s = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      for (int tile = first; ok && t.at(p, starts, tile); tile += step)
+        for (int kb = 0; kb < cnt; ++kb) {
+          if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&landed[s], ph, abort_flag, p.err)))) break;
+          const uint32_t at = ring + s * kStage;
+          for (int i = 0; i < 3 * W; ++i) {  // atom i % W of the tokens, the first and the other features
+            const int of = i / W, word = i % W;
+            const int lift = of == 0 ? 0 : 128 * (of - 1) - C::kNT / 2 * static_cast<int>(rank), rows = of == 0 ? 128 : C::kNT / 2;
+            const uint32_t line = at + kSf + i * kAtom + lane * 16;
+            const uint4 x = lds128(line);
+            uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int row = lane + 32 * r + lift;
+              if ((w[r] & 0x80808080u) && row >= 0 && row < rows) flip_codes(at + (of == 0 ? 0 : C::kA), row, word, w[r]);
+            }
+            st_shared_v4(line, w[0] & 0x7F7F7F7Fu, w[1] & 0x7F7F7F7Fu, w[2] & 0x7F7F7F7Fu, w[3] & 0x7F7F7F7Fu);
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          // the peer reports by a store that waits for nothing (an arrival at cluster scope waits for all writes
+          // before it, 1,000 cycles)
+          if (lane == 0) {
+            if (rank == 0)
+              mbar_arrive_expect_tx(&full[s], 4);
+            else
+              st_async_signal(mapa_shared(smem_u32(&sink), 0), mapa_shared(smem_u32(&full[s]), 0));
+          }
+          if (++s == S) {
+            s = 0;
+            ph ^= 1u;
+          }
         }
-        c.next(S);
-      }
     }
   } else {
     // ------------------------------------------------------ epilogue
     const int quad = warp & 3, share = warp >> 2;
-    const uint32_t t_row = tmem + (static_cast<uint32_t>(quad * 32) << 16) + share * (C::kNT / 2);
+    const uint32_t t_row = tmem + (static_cast<uint32_t>(quad * 32) << 16);
     const uint32_t box = ring + S * kStage + warp * C::kBox;
     int tc = 0;
     bool ok = true;
@@ -891,11 +1066,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
       if (!ok) break;
       tc_fence_after();
 #pragma unroll 1
-      for (int g = 0; g < C::kNT / 64; ++g) {
+      for (int g = share; g < C::kNT / 32; g += 2) {  // 32 columns
         uint32_t v[32];
         tmem_ld32(t_row + ab * C::kNT + 32 * g, v);
         tmem_ld_wait();
-        if (g == C::kNT / 64 - 1) {  // the accumulator is read
+        if (g + 2 >= C::kNT / 32) {  // the warp's part of the accumulator is read
           tc_fence_before();
           __syncwarp();
           if (lane == 0) arrive_cluster(mapa_shared(smem_u32(&tempty[ab]), 0));
@@ -911,7 +1086,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
         for (int q = 0; q < 4; ++q)
           st_shared_v4(box + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4), o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
         __syncwarp();
-        const int f = t.f0 + share * (C::kNT / 2) + 32 * g + 8 * (lane & 3);
+        const int f = t.f0 + 32 * g + 8 * (lane & 3);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const int r = 8 * q + (lane >> 2);
@@ -931,45 +1106,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
   }
 }
 
-// Planes of scale bytes whose rows are not whole 16-byte pieces, with rows that are: row r of G bytes to
-// row r of `pitch`, the rest zero. A thread writes a piece; it reads the units of two bytes, or one, that it
-// is made of.
-__global__ void __launch_bounds__(256) sq_fp4_pad_kernel(const PadArgs a) {
-  dependency_wait();
-  dependency_start();
-  const int pieces = a.pitch / 16;
-  const int64_t total = (a.rows[0] + a.rows[1]) * pieces;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
-    int64_t row = i / pieces;
-    const int b = static_cast<int>(i - row * pieces) * 16;
-    const bool second = row >= a.rows[0];
-    if (second) row -= a.rows[0];
-    const uint8_t *src = (second ? a.src[1] : a.src[0]) + row * a.G + b;
-    uint8_t *dst = (second ? a.dst[1] : a.dst[0]) + row * a.pitch + b;
-    uint32_t w[4];
-    if ((a.G & 1) == 0) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t lo = b + 4 * j < a.G ? *reinterpret_cast<const uint16_t *>(src + 4 * j) : 0u;
-        const uint32_t hi = b + 4 * j + 2 < a.G ? *reinterpret_cast<const uint16_t *>(src + 4 * j + 2) : 0u;
-        w[j] = lo | hi << 16;
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        w[j] = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (b + 4 * j + e < a.G) w[j] |= static_cast<uint32_t>(src[4 * j + e]) << (8 * e);
-      }
-    }
-    *reinterpret_cast<uint4 *>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
-  }
-}
-
-template <typename Kernel>
-cudaError_t launch_kernel(Kernel kernel, int &done_mask, int most_smem, unsigned grid, int threads, size_t smem, int cluster,
-                       cudaStream_t stream, const Fp4Maps &maps, const Fp4Args &p) {
+template <typename Maps>
+cudaError_t launch_kernel(void (*kernel)(Maps, Fp4Args), int &done_mask, int most_smem, unsigned grid, int threads, size_t smem, int cluster,
+                       cudaStream_t stream, const Maps &maps, const Fp4Args &p) {
   int dev = 0;
   cudaGetDevice(&dev);
   if (!(done_mask & (1 << (dev & 31)))) {
@@ -1006,29 +1145,24 @@ cudaError_t launch_few_fp4(const Fp4Maps &maps, const Fp4Args &p, cudaStream_t s
 
 }  // namespace
 
-cudaError_t launch_fp4_pad(const PadArgs &a, int sm_count, cudaStream_t stream) {
-  const int64_t units = ((a.rows[0] + a.rows[1]) * (a.pitch / 16) + 255) / 256;
-  return launch_after(sq_fp4_pad_kernel, static_cast<unsigned>(std::min<int64_t>(units, 8 * sm_count)), 256, 0, stream, a);
+cudaError_t launch_fp4_few(int fmt, const Fp4Maps &maps, const Fp4Args &p, cudaStream_t stream) {
+  const bool raw = p.G % kSpan == 0;
+  if (fmt == 0) return raw ? launch_few_fp4<0, true>(maps, p, stream) : launch_few_fp4<0, false>(maps, p, stream);
+  return raw ? launch_few_fp4<1, true>(maps, p, stream) : launch_few_fp4<1, false>(maps, p, stream);
 }
 
-cudaError_t launch_fp4(int fmt, const Fp4Maps &maps, const Fp4Args &p, int sm_count, cudaStream_t stream) {
-  const bool raw = p.G % kSpan == 0;
-  auto launch = [&](auto f, auto al) {
-    constexpr int FMT = decltype(f)::value;
-    constexpr bool RAW = decltype(al)::value;
-    if (!p.pair) return launch_few_fp4<FMT, RAW>(maps, p, stream);
-    if (!RAW) return cudaErrorInvalidValue;  // fp4_plan gives its planes whole pieces
-    static int done_mask = 0;
-    const size_t smem = fp4_pair_smem(p.stages, p.offsets ? p.E : 0);
-    const int clusters = static_cast<int>(std::min<int64_t>(p.units, sm_count / 2));
-    return launch_kernel(sq_fp4_pair_kernel<FMT>, done_mask, kFp4SmemMost, 2u * clusters, Fp4PairCfg::kThreads, smem, 1,
-                         stream, maps, p);
-  };
-  using std::bool_constant;
-  using std::integral_constant;
-  if (fmt == 0)
-    return raw ? launch(integral_constant<int, 0>(), bool_constant<true>()) : launch(integral_constant<int, 0>(), bool_constant<false>());
-  return raw ? launch(integral_constant<int, 1>(), bool_constant<true>()) : launch(integral_constant<int, 1>(), bool_constant<false>());
+template <int FMT>
+static cudaError_t launch_pair(const Fp4PairMaps &maps, const Fp4Args &p, int sm_count, cudaStream_t stream) {
+  static int done_mask = 0;
+  const cudaError_t e = launch_after(sq_fp4_atoms_kernel<FMT>, static_cast<unsigned>(p.atom_ctas), AtomCfg<FMT>::kThreads, 0, stream, p);
+  if (e != cudaSuccess) return e;
+  const int clusters = static_cast<int>(std::min<int64_t>(p.units, sm_count / 2));
+  return launch_kernel<const Fp4PairMaps>(sq_fp4_pair_kernel<FMT>, done_mask, kFp4SmemMost, 2u * clusters, Fp4PairCfg::kThreads,
+                                          fp4_pair_smem(FMT, p.stages, p.offsets ? p.E : 0), 1, stream, maps, p);
+}
+
+cudaError_t launch_fp4_pair(int fmt, const Fp4PairMaps &maps, const Fp4Args &p, int sm_count, cudaStream_t stream) {
+  return fmt == 0 ? launch_pair<0>(maps, p, sm_count, stream) : launch_pair<1>(maps, p, sm_count, stream);
 }
 
 }  // namespace sqi

@@ -492,11 +492,15 @@ constexpr int kFp4FewBoxes = 5;              // boxes of 8 .. 128 token rows
 constexpr int kFp4SmemAlone = 224 * 1024;    // of a CTA alone on its SM
 constexpr int kFp4SmemShared = 112 * 1024;   // ... of two
 constexpr int kFp4SmemMost = 232448 - 512;  // ... beside its static shared memory
-constexpr int kFp4PairTokens = 256, kFp4PairFeatures = 192;  // a tile of the pair kernel
+constexpr int kFp4PairTokens = 256, kFp4PairFeatures = 224;  // a tile of the pair kernel
 struct Fp4Maps {
-  CUtensorMap w;                // codes [E][N][K / 2], boxes of 128 bytes x 128 rows (few) or half a pair's features
+  CUtensorMap w;                // codes [E][N][K / 2], boxes of 128 bytes x 128 rows
   CUtensorMap x[kFp4FewBoxes];  // codes [R][K / 2], boxes of 128 bytes x (8 << i) rows
   CUtensorMap w_scales, x_scales[kFp4FewBoxes];  // scale bytes, boxes of 16 bytes x the same rows (whole 16-byte rows only)
+};
+struct Fp4PairMaps {
+  CUtensorMap w, x;              // codes, boxes of 128 bytes x half the features and 128 rows
+  CUtensorMap w_atoms, x_atoms;  // [atoms][512 bytes], boxes of a stage's of 256 features and 128 rows
 };
 struct Fp4Args {
   int64_t R;                 // rows
@@ -515,25 +519,34 @@ struct Fp4Args {
   int64_t units;             // tiles, at most
   int splits;                // few: parts of the contraction (CTAs of a cluster)
   int stages;                // of the ring
+  // pair: atoms of the scales, [token block][stage] and [feature tile][stage][2], and per CTA that writes them whether
+  // it met a negative one
+  uint4 *x_atoms, *w_atoms;
+  int *negative;
+  int token_blocks, atom_ctas;
 };
 // A few-token stage: codes of 128 features and a tile's tokens, scales of 128 rows of both. A pair stage: codes of 128
-// tokens and half the features, scales of those tokens and of all features; behind the ring eight 2 KiB boxes of the
+// tokens and half the features, atoms of those tokens and of 256 features; behind the ring eight 2 KiB boxes of the
 // epilogue and the experts' first tiles.
 constexpr int fp4_few_stage(int tile_tokens) { return 128 * 128 + tile_tokens * 128 + 2 * 2048; }
-constexpr int fp4_pair_stage() { return 128 * 128 + kFp4PairFeatures / 2 * 128 + 3 * 2048; }
-constexpr size_t fp4_pair_smem(int stages, int E) {
-  return 1024 + static_cast<size_t>(stages) * fp4_pair_stage() + 8 * 2048 + (E > 0 ? 4 * (E + 1) : 0);
+__host__ __device__ constexpr int fp4_atoms(int fmt) { return fmt == 0 ? 2048 : 1024; }  // bytes of 128 rows and a stage
+__host__ __device__ constexpr int fp4_pair_stage(int fmt) { return 128 * 128 + kFp4PairFeatures / 2 * 128 + 3 * fp4_atoms(fmt); }
+constexpr size_t fp4_pair_smem(int fmt, int stages, int E) {
+  return 1024 + static_cast<size_t>(stages) * fp4_pair_stage(fmt) + 8 * 2048 + (E > 0 ? 4 * (E + 1) : 0);
 }
 // Kernel, tiles and parts of a product on sm_count SMs: fills the last fields of p.
-inline void fp4_plan(int sm_count, Fp4Args &p) {
+inline void fp4_plan(int fmt, int sm_count, Fp4Args &p) {
   const int64_t groups = p.offsets ? std::min<int64_t>(p.E, p.R) : 1;
   p.pair = p.R >= 192 * groups;
   if (p.pair) {
     p.ftiles = (p.N + kFp4PairFeatures - 1) / kFp4PairFeatures;
-    p.units = (p.R + (kFp4PairTokens - 1) * groups) / kFp4PairTokens * p.ftiles;
+    const int64_t token_tiles = (p.R + (kFp4PairTokens - 1) * groups) / kFp4PairTokens;
+    p.units = token_tiles * p.ftiles;
+    p.token_blocks = static_cast<int>(2 * token_tiles);
+    p.atom_ctas = static_cast<int>((p.token_blocks + 2 * int64_t(p.E) * p.ftiles) * (((p.K + 255) / 256 + 7) / 8));
     p.splits = 1;
     p.stages = 8;
-    while (fp4_pair_smem(p.stages, p.offsets ? p.E : 0) > static_cast<size_t>(kFp4SmemMost)) --p.stages;
+    while (fp4_pair_smem(fmt, p.stages, p.offsets ? p.E : 0) > static_cast<size_t>(kFp4SmemMost)) --p.stages;
     return;
   }
   p.ftiles = (p.N + 127) / 128;
@@ -546,15 +559,8 @@ inline void fp4_plan(int sm_count, Fp4Args &p) {
   const bool alone = p.units * p.splits <= sm_count;
   p.stages = std::min(8, ((alone ? kFp4SmemAlone : kFp4SmemShared) - 1024) / stage);
 }
-// Planes of rows[i] x G scale bytes copied to rows of `pitch` bytes, a multiple of 16.
-struct PadArgs {
-  const uint8_t *src[2];
-  uint8_t *dst[2];
-  int64_t rows[2];
-  int G, pitch;
-};
-cudaError_t launch_fp4_pad(const PadArgs &a, int sm_count, cudaStream_t stream);
-cudaError_t launch_fp4(int fmt, const Fp4Maps &maps, const Fp4Args &p, int sm_count, cudaStream_t stream);
+cudaError_t launch_fp4_few(int fmt, const Fp4Maps &maps, const Fp4Args &p, cudaStream_t stream);
+cudaError_t launch_fp4_pair(int fmt, const Fp4PairMaps &maps, const Fp4Args &p, int sm_count, cudaStream_t stream);
 
 // Device-side error codes written to the error word.
 constexpr int kErrWaitTimeout = 1;
