@@ -85,10 +85,11 @@ __device__ __forceinline__ void umma_fp4_elect(uint32_t d, uint64_t a, uint64_t 
         : "memory");
 }
 
-// A bounded wait of a whole warp without a call and with votes for its branches: around a call, or where
-// lanes might part, the compiler keeps the descriptors of the loop in ordinary registers and moves them to
-// the uniform ones at every use (12 atoms and 4 MMAs of a stage took 807 cycles to issue, where the
-// tensor cores take 384).
+// A bounded wait of a whole warp without a call and with votes for its branches. In a loop around a call,
+// or one that lanes might leave apart, the compiler keeps the MMAs' descriptors in ordinary registers and
+// moves them to the uniform ones at every use: an instruction then takes 30 cycles to issue, not 8. The
+// MMA warps for that reason go on after a wait that ran out: they issue what is left (on whatever the
+// shared memory holds), every later wait returns at once, and the error word is set.
 __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag, int *err) {
   if (__all_sync(0xFFFFFFFFu, mbar_test_wait(bar, parity))) return true;
   const unsigned long long t0 = globaltimer();
@@ -490,9 +491,9 @@ __global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
     const uint64_t sd0 = atom_desc(ring + sf_off);
     int s = 0;
     uint32_t ph = 0;
-    bool ok = true;
-    for (int it = 0; it < cnt && ok; ++it) {
-      if (!(ok = warp_wait(&sfull[s], ph, abort_flag, p.err) && (RAW || warp_wait(&full[s], ph, abort_flag, p.err)))) break;
+    for (int it = 0; it < cnt; ++it) {
+      warp_wait(&sfull[s], ph, abort_flag, p.err);
+      if (!RAW) warp_wait(&full[s], ph, abort_flag, p.err);
       if (!RAW) fence_proxy_async_smem();
       tc_fence_after();
       const uint32_t so = static_cast<uint32_t>(s * stage) >> 4;
@@ -969,19 +970,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
     if (rank == 0) {
       const uint64_t ad0 = smem_desc_sw128(ring, 16, 1024), bd0 = smem_desc_sw128(ring + C::kA, 16, 1024);
       const uint64_t sd0 = atom_desc(ring + kSf);
-      int s = 0, tc = 0, it = 0;
+      // Behind the MMA that they run the tensor cores hold about two more: between the last MMA of a stage and
+      // the first of the next there are 250 cycles for the barriers, the commit and the atoms.
+      const int tiles = p.offsets ? starts[p.E] : static_cast<int>(p.units);
+      const int mine = __reduce_max_sync(0xFFFFFFFFu, first < tiles ? (tiles - first + step - 1) / step : 0);
+      int s = 0, it = 0;
       uint32_t ph = 0;
-      bool ok = true;
-      // (The votes tell the compiler that the warp walks as one.)
-      for (int tile = first; ok && __all_sync(0xFFFFFFFFu, t.at(p, starts, tile)); tile += step, ++tc) {
+      for (int tc = 0; tc < mine; ++tc) {
         const int ab = tc & 1;
-        if (tc >= 2 &&
-            !(ok = warp_wait(&tempty[ab], (static_cast<uint32_t>(tc >> 1) & 1u) ^ 1u, abort_flag, p.err)))
-          break;
-        tc_fence_after();
+        if (tc >= 2) warp_wait(&tempty[ab], (static_cast<uint32_t>(tc >> 1) & 1u) ^ 1u, abort_flag, p.err);
         const uint32_t d = tmem + ab * C::kNT;
         for (int kb = 0; kb < cnt; ++kb, ++it) {
-          if (!(ok = warp_wait(&full[s], ph, abort_flag, p.err))) break;
+          warp_wait(&full[s], ph, abort_flag, p.err);
           tc_fence_after();
           const uint32_t so = static_cast<uint32_t>(s * kStage) >> 4;
           const uint32_t sa = tmem + kScaleAt + (it & (kScaleBufs - 1)) * kScaleCols, sb = sa + 4 * W;
@@ -1006,7 +1006,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
             ph ^= 1u;
           }
         }
-        if (ok) commit_pair_mc_elect(&tfull[ab]);
+        commit_pair_mc_elect(&tfull[ab]);
       }
       commit_pair_elect(drain);
       mbar_drain(drain, 0);
