@@ -1789,7 +1789,7 @@ sq_status sq_quantize(sq_handle h, const sq_rows *q, int64_t T, int32_t k, const
   a.k = slot_of ? k : 1;
   a.slots = T * a.k;
   a.wide = reinterpret_cast<uintptr_t>(X) % 32 == 0;
-  cudaError_t e = sqi::launch_quantize(q->fmt, a, static_cast<cudaStream_t>(stream));
+  cudaError_t e = sqi::launch_quantize(q->fmt, a, dev->sm_count, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return cuda_fail(h, e, "quantisation launch");
   return SQ_OK;
   SQ_GUARD_END
@@ -1803,7 +1803,7 @@ sq_status sq_dequantize(sq_handle h, const sq_rows *q, uint16_t *X, void *stream
   DeviceState *dev = nullptr;
   SQ_TRY(ensure_device(h, &dev));
   if (q->R == 0) return SQ_OK;
-  cudaError_t e = sqi::launch_dequantize(q->fmt, quant_args(q), X, static_cast<cudaStream_t>(stream));
+  cudaError_t e = sqi::launch_dequantize(q->fmt, quant_args(q), X, dev->sm_count, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return cuda_fail(h, e, "dequantisation launch");
   return SQ_OK;
   SQ_GUARD_END

@@ -182,36 +182,41 @@ struct ScaleRows {
     apart = 32 * static_cast<int64_t>(G);
     rows = rows_left > lane ? (rows_left - lane + 31) / 32 : 0;  // of the lane's
   }
-  __device__ __forceinline__ void piece(const uint8_t *p, uint32_t *w) const {
-    if (p + kBytes <= end) {
-      if constexpr (kWords == 4) {
-        const uint4 x = *reinterpret_cast<const uint4 *>(p);
-        w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
-      } else {
-        const uint2 x = *reinterpret_cast<const uint2 *>(p);
-        w[0] = x.x, w[1] = x.y;
-      }
-    } else {  // the plane ends inside
-#pragma unroll
-      for (int i = 0; i < kWords; ++i) {
-        w[i] = 0;
-#pragma unroll 1
-        for (int b = 0; b < 4; ++b)
-          if (p + 4 * i + b < end) w[i] |= static_cast<uint32_t>(p[4 * i + b]) << (8 * b);
-      }
-    }
-  }
-  // Stage `it` into slot d; past the last one (cnt) nothing is read.
+  // Stage `it` into slot d; past the last one (cnt) nothing is read. All loads first, without a branch
+  // between them: one by one they took a microsecond each.
   __device__ __forceinline__ void load(int d, int it, int cnt) {
+    bool cut = false;  // the plane ends inside a piece
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
 #pragma unroll
-      for (int i = 0; i < 2 * kWords; ++i) v[d][r][i] = 0;
-      if (r < rows && it < cnt) {
-        const uint8_t *p = at + r * apart + static_cast<int64_t>(it) * kBytes;
-        piece(p, &v[d][r][0]);
-        if ((it + 1) * kBytes - shift < G) piece(p + kBytes, &v[d][r][kWords]);
+      for (int j = 0; j < 2; ++j) {
+        uint32_t *w = &v[d][r][j * kWords];
+        const uint8_t *p = at + r * apart + static_cast<int64_t>(it + j) * kBytes;
+        const bool in = r < rows && it < cnt && (j == 0 || (it + 1) * kBytes - shift < G);
+        const bool whole = in && p + kBytes <= end;
+        cut |= in && !whole;
+        if constexpr (kWords == 4) {
+          uint4 x = make_uint4(0, 0, 0, 0);
+          if (whole) x = *reinterpret_cast<const uint4 *>(p);
+          w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+        } else {
+          uint2 x = make_uint2(0, 0);
+          if (whole) x = *reinterpret_cast<const uint2 *>(p);
+          w[0] = x.x, w[1] = x.y;
+        }
       }
+    }
+    if (cut) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint8_t *p = at + r * apart + static_cast<int64_t>(it + j) * kBytes;
+          if (r < rows && p < end && p + kBytes > end && (j == 0 || (it + 1) * kBytes - shift < G))
+#pragma unroll
+            for (int b = 0; b < kBytes; ++b)
+              if (p + b < end) v[d][r][j * kWords + b / 4] |= static_cast<uint32_t>(p[b]) << (8 * (b % 4));
+        }
     }
   }
   // The scale bytes of row r (0 .. 3) in slot d, stage `it`; those behind the row's end are zero.
@@ -346,45 +351,49 @@ __device__ __forceinline__ void expert_rows(const Fp4Args &p, int e, int &lo, in
 }
 
 // Token tile tt of the experts' tiles of `height` rows, expert by expert: its expert, first row and
-// rows (0 past the last tile). One warp; each lane counts the tiles of its share of the experts.
-__device__ __forceinline__ void find_tile(const Fp4Args &p, int tt, int height, int &e, int &row0, int &rows) {
-  const int lane = threadIdx.x & 31;
-  const int per = (p.E + 31) / 32, first = lane * per, last = min(p.E, first + per);
-  int mine = 0;
-  for (int x = first; x < last; ++x) {
+// rows (0 past the last tile). Called by a whole CTA, which reads all offsets at once, between barriers of its
+// own; each lane of warp 0 counts the tiles of its share of the experts.
+struct TileSearch {
+  int lo[kRouteMaxExperts], rows[kRouteMaxExperts];
+  int found[3];
+};
+__device__ __forceinline__ void find_tile(const Fp4Args &p, TileSearch &f, int tt, int height, int &e, int &row0, int &rows) {
+  for (int x = threadIdx.x; x < p.E; x += blockDim.x) {
     int lo, hi;
     expert_rows(p, x, lo, hi);
-    mine += (hi - lo + height - 1) / height;
+    f.lo[x] = lo;
+    f.rows[x] = hi - lo;
   }
-  int upto = mine;
+  if (threadIdx.x < 3) f.found[threadIdx.x] = 0;
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    const int lane = threadIdx.x, per = (p.E + 31) / 32, first = lane * per, last = min(p.E, first + per);
+    int mine = 0;
+    for (int x = first; x < last; ++x) mine += (f.rows[x] + height - 1) / height;
+    int upto = mine;
 #pragma unroll
-  for (int d = 1; d < 32; d *= 2) {
-    const int v = __shfl_up_sync(0xFFFFFFFFu, upto, d);
-    if (lane >= d) upto += v;
-  }
-  const bool here = tt >= upto - mine && tt < upto;
-  const uint32_t who = __ballot_sync(0xFFFFFFFFu, here);
-  e = row0 = rows = 0;
-  if (who == 0) return;
-  if (here) {
-    int left = tt - (upto - mine);
-    for (int x = first; x < last; ++x) {
-      int lo, hi;
-      expert_rows(p, x, lo, hi);
-      const int tiles = (hi - lo + height - 1) / height;
-      if (left < tiles) {
-        e = x;
-        row0 = lo + left * height;
-        rows = min(height, hi - row0);
-        break;
+    for (int d = 1; d < 32; d *= 2) {
+      const int v = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+      if (lane >= d) upto += v;
+    }
+    if (tt >= upto - mine && tt < upto) {  // one lane, or none
+      int left = tt - (upto - mine);
+      for (int x = first; x < last; ++x) {
+        const int tiles = (f.rows[x] + height - 1) / height;
+        if (left < tiles) {
+          f.found[0] = x;
+          f.found[1] = f.lo[x] + left * height;
+          f.found[2] = min(height, f.rows[x] - left * height);
+          break;
+        }
+        left -= tiles;
       }
-      left -= tiles;
     }
   }
-  const int from = __ffs(who) - 1;
-  e = __shfl_sync(0xFFFFFFFFu, e, from);
-  row0 = __shfl_sync(0xFFFFFFFFu, row0, from);
-  rows = __shfl_sync(0xFFFFFFFFu, rows, from);
+  __syncthreads();
+  e = f.found[0];
+  row0 = f.found[1];
+  rows = f.found[2];
 }
 
 // ---------------------------------------------------------------- few tokens
@@ -413,7 +422,6 @@ __global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
   __shared__ uint64_t bars[3 * C::kMaxStages + 1];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_word;
-  __shared__ int tile_info[3];  // expert, first row, rows
   volatile int *abort_flag = &abort_word;
   uint64_t *full = bars;                     // [S] codes of both operands landed          (1 arrival + tx)
   uint64_t *sfull = full + C::kMaxStages;    // [S] their scales are in place              (2 warps)
@@ -441,19 +449,14 @@ __global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
   if (warp == C::kMmaWarp) tmem_alloc(&tmem_slot, C::kTmemCols);
   dependency_wait();
   dependency_start();
-  if (warp == 0) {
-    int e = 0, row0 = tt * p.tile_tokens, rows = static_cast<int>(min(p.R - row0, static_cast<int64_t>(p.tile_tokens)));
-    if (p.offsets) find_tile(p, tt, p.tile_tokens, e, row0, rows);
-    if (lane == 0) {
-      tile_info[0] = e;
-      tile_info[1] = row0;
-      tile_info[2] = rows;
-    }
+  int expert = 0, row0 = tt * p.tile_tokens, rows = static_cast<int>(min(p.R - row0, static_cast<int64_t>(p.tile_tokens)));
+  if (p.offsets) {
+    find_tile(p, *reinterpret_cast<TileSearch *>(smem), tt, p.tile_tokens, expert, row0, rows);
+    fence_proxy_async_smem();  // the search's memory is the ring's
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const int expert = tile_info[0], row0 = tile_info[1], rows = tile_info[2];
   const uint32_t tmem = tmem_slot;
   const int cnt_all = (p.K + kDeep - 1) / kDeep;
   const int it0 = cnt_all * part / splits, cnt = __any_sync(0xFFFFFFFFu, rows > 0) ? cnt_all * (part + 1) / splits - it0 : 0;
@@ -744,7 +747,7 @@ __global__ void __launch_bounds__(AtomCfg<FMT>::kThreads) sq_fp4_atoms_kernel(co
   using C = AtomCfg<FMT>;
   constexpr int W = Fp4<FMT>::kWords;
   __shared__ uint4 piece[128 * C::kPieces];
-  __shared__ int info[3];
+  static_assert(sizeof(TileSearch) <= sizeof(piece), "the search's memory");
   const int cnt = (p.K + kDeep - 1) / kDeep, groups = (cnt + C::kStages - 1) / C::kStages;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int block = static_cast<int>(blockIdx.x) / groups;
@@ -758,17 +761,10 @@ __global__ void __launch_bounds__(AtomCfg<FMT>::kThreads) sq_fp4_atoms_kernel(co
   uint4 *out;
   if (tokens) {
     if (p.offsets) {
-      if (warp == 0) {
-        int e, r0, n;
-        find_tile(p, block >> 1, kFp4PairTokens, e, r0, n);
-        if (lane == 0) {
-          info[0] = r0;
-          info[1] = n;
-        }
-      }
-      __syncthreads();
-      row0 = info[0];
-      rows = info[1];
+      int e, r0;
+      find_tile(p, *reinterpret_cast<TileSearch *>(piece), block >> 1, kFp4PairTokens, e, r0, rows);
+      row0 = r0;
+      __syncthreads();  // the search's memory is the pieces'
     } else {
       row0 = static_cast<int64_t>(block >> 1) * kFp4PairTokens;
       rows = static_cast<int>(min(static_cast<int64_t>(kFp4PairTokens), p.R - row0));
@@ -787,22 +783,29 @@ __global__ void __launch_bounds__(AtomCfg<FMT>::kThreads) sq_fp4_atoms_kernel(co
   }
   rows = min(rows, 128);
   const uint8_t *first = plane + row0 * p.G, *end = plane + plane_rows * p.G;
-  for (int i = threadIdx.x; i < rows * C::kPieces; i += C::kThreads) {
-    const int r = i / C::kPieces, j = i - r * C::kPieces;
+  constexpr int kLoads = (128 * C::kPieces + C::kThreads - 1) / C::kThreads;
+  uint4 x[kLoads];
+#pragma unroll
+  for (int l = 0; l < kLoads; ++l) {
+    const int i = threadIdx.x + l * C::kThreads, r = i / C::kPieces, j = i - r * C::kPieces;
     const uint8_t *at = first + static_cast<int64_t>(r) * p.G + kb0 * Fp4<FMT>::kBytes;  // of the row's bytes
     const uint8_t *from = at - reinterpret_cast<uintptr_t>(at) % 16 + 16 * j;
-    const int64_t left = end - from;  // of the plane
-    uint4 x = make_uint4(0, 0, 0, 0);
-    if (left >= 16) {
-      x = *reinterpret_cast<const uint4 *>(from);
-    } else if (left > 0) {  // the plane ends inside
+    x[l] = make_uint4(0, 0, 0, 0);
+    if (r < rows && from + 16 <= end) x[l] = *reinterpret_cast<const uint4 *>(from);
+  }
+#pragma unroll
+  for (int l = 0; l < kLoads; ++l) {
+    const int i = threadIdx.x + l * C::kThreads, r = i / C::kPieces, j = i - r * C::kPieces;
+    const uint8_t *at = first + static_cast<int64_t>(r) * p.G + kb0 * Fp4<FMT>::kBytes;
+    const uint8_t *from = at - reinterpret_cast<uintptr_t>(at) % 16 + 16 * j;
+    if (r < rows && from < end && from + 16 > end) {  // the plane ends inside
       uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
       for (int b = 0; b < 16; ++b)
-        if (b < left) w[b / 4] |= static_cast<uint32_t>(from[b]) << (8 * (b % 4));
-      x = make_uint4(w[0], w[1], w[2], w[3]);
+        if (from + b < end) w[b / 4] |= static_cast<uint32_t>(from[b]) << (8 * (b % 4));
+      x[l] = make_uint4(w[0], w[1], w[2], w[3]);
     }
-    piece[i] = x;
+    if (r < rows) piece[i] = x[l];
   }
   __syncthreads();
   uint32_t sign = 0;

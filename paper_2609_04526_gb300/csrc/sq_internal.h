@@ -483,8 +483,8 @@ struct QuantArgs {
   int64_t slots;           // T * k
   bool wide;               // X starts on 32 bytes
 };
-cudaError_t launch_quantize(int fmt, const QuantArgs &a, cudaStream_t stream);
-cudaError_t launch_dequantize(int fmt, const QuantArgs &a, uint16_t *X, cudaStream_t stream);
+cudaError_t launch_quantize(int fmt, const QuantArgs &a, int sm_count, cudaStream_t stream);
+cudaError_t launch_dequantize(int fmt, const QuantArgs &a, uint16_t *X, int sm_count, cudaStream_t stream);
 
 // Products of FP4 rows with FP4 weights (sq_fp4.cu).
 constexpr int kFp4FewTokens = 128;           // of a tile of the few-token kernel, at most

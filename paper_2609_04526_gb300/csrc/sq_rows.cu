@@ -263,20 +263,23 @@ __global__ void __launch_bounds__(kRowsThreads) sq_dequantize_kernel(const Quant
   }
 }
 
+// Threads of a row. Many rows: as few as hold it in registers, each with kRowsHold chunks in flight (32768 x
+// 4096 quantised with 256 threads of one chunk 105 us, with 64 of four XX; rows back 69, XX). Few
+// rows: as many as it has chunks.
 template <typename F>
-cudaError_t by_width(int K, F f) {
-  const int chunks = K / 16;
-  if (chunks <= 32) return f(std::integral_constant<int, 32>());
-  if (chunks <= 64) return f(std::integral_constant<int, 64>());
-  if (chunks <= 128) return f(std::integral_constant<int, 128>());
+cudaError_t by_width(int64_t R, int K, int sm_count, F f) {
+  const int chunks = K / 16, want = R >= 8 * static_cast<int64_t>(sm_count) ? (chunks + kRowsHold - 1) / kRowsHold : chunks;
+  if (want <= 32) return f(std::integral_constant<int, 32>());
+  if (want <= 64) return f(std::integral_constant<int, 64>());
+  if (want <= 128) return f(std::integral_constant<int, 128>());
   return f(std::integral_constant<int, 256>());
 }
 unsigned row_ctas(int64_t R, int tpr) { return static_cast<unsigned>((R + kRowsThreads / tpr - 1) / (kRowsThreads / tpr)); }
 
 }  // namespace
 
-cudaError_t launch_quantize(int fmt, const QuantArgs &a, cudaStream_t stream) {
-  return by_width(a.K, [&](auto tpr) {
+cudaError_t launch_quantize(int fmt, const QuantArgs &a, int sm_count, cudaStream_t stream) {
+  return by_width(a.R, a.K, sm_count, [&](auto tpr) {
     constexpr int kTpr = decltype(tpr)::value;
     const auto kernel = fmt == 1       ? sq_quantize_kernel<1, false, kTpr>
                         : a.row_ws2 ? sq_quantize_kernel<0, true, kTpr>
@@ -285,9 +288,9 @@ cudaError_t launch_quantize(int fmt, const QuantArgs &a, cudaStream_t stream) {
   });
 }
 
-cudaError_t launch_dequantize(int fmt, const QuantArgs &a, uint16_t *X, cudaStream_t stream) {
+cudaError_t launch_dequantize(int fmt, const QuantArgs &a, uint16_t *X, int sm_count, cudaStream_t stream) {
   const bool wide = reinterpret_cast<uintptr_t>(X) % 32 == 0;
-  return by_width(a.K, [&](auto tpr) {
+  return by_width(a.R, a.K, sm_count, [&](auto tpr) {
     constexpr int kTpr = decltype(tpr)::value;
     const auto kernel = fmt == 1 ? sq_dequantize_kernel<1, kTpr> : sq_dequantize_kernel<0, kTpr>;
     return launch_after(kernel, row_ctas(a.R, kTpr), kRowsThreads, 0, stream, a, X, wide);
