@@ -350,14 +350,21 @@ __device__ __forceinline__ void expert_rows(const Fp4Args &p, int e, int &lo, in
   hi = static_cast<int>(min(p.R, max(b, static_cast<int64_t>(lo))));
 }
 
-// Token tile tt of the experts' tiles of `height` rows, expert by expert: its expert, first row and
+// Rows of the token tiles that `rows` rows are cut into, `most` at most: equal ones, whole steps of the MMA's N.
+__device__ __forceinline__ int tile_count(int rows, int most) { return (rows + most - 1) / most; }
+__device__ __forceinline__ int tile_height(int rows, int most, int unit) {
+  const int tiles = tile_count(rows, most);
+  return tiles > 0 ? ((rows + tiles - 1) / tiles + unit - 1) / unit * unit : unit;
+}
+
+// Token tile tt of the experts' tiles, expert by expert: its expert, first row and
 // rows (0 past the last tile). Called by a whole CTA, which reads all offsets at once, between barriers of its
 // own; each lane of warp 0 counts the tiles of its share of the experts.
 struct TileSearch {
   int lo[kRouteMaxExperts], rows[kRouteMaxExperts];
   int found[3];
 };
-__device__ __forceinline__ void find_tile(const Fp4Args &p, TileSearch &f, int tt, int height, int &e, int &row0, int &rows) {
+__device__ __forceinline__ void find_tile(const Fp4Args &p, TileSearch &f, int tt, int most, int unit, int &e, int &row0, int &rows) {
   for (int x = threadIdx.x; x < p.E; x += blockDim.x) {
     int lo, hi;
     expert_rows(p, x, lo, hi);
@@ -369,7 +376,7 @@ __device__ __forceinline__ void find_tile(const Fp4Args &p, TileSearch &f, int t
   if (threadIdx.x < 32) {
     const int lane = threadIdx.x, per = (p.E + 31) / 32, first = lane * per, last = min(p.E, first + per);
     int mine = 0;
-    for (int x = first; x < last; ++x) mine += (f.rows[x] + height - 1) / height;
+    for (int x = first; x < last; ++x) mine += tile_count(f.rows[x], most);
     int upto = mine;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
@@ -379,11 +386,11 @@ __device__ __forceinline__ void find_tile(const Fp4Args &p, TileSearch &f, int t
     if (tt >= upto - mine && tt < upto) {  // one lane, or none
       int left = tt - (upto - mine);
       for (int x = first; x < last; ++x) {
-        const int tiles = (f.rows[x] + height - 1) / height;
+        const int tiles = tile_count(f.rows[x], most), height = tile_height(f.rows[x], most, unit);
         if (left < tiles) {
           f.found[0] = x;
           f.found[1] = f.lo[x] + left * height;
-          f.found[2] = min(height, f.rows[x] - left * height);
+          f.found[2] = max(0, min(height, f.rows[x] - left * height));
           break;
         }
         left -= tiles;
@@ -451,7 +458,7 @@ __global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
   dependency_start();
   int expert = 0, row0 = tt * p.tile_tokens, rows = static_cast<int>(min(p.R - row0, static_cast<int64_t>(p.tile_tokens)));
   if (p.offsets) {
-    find_tile(p, *reinterpret_cast<TileSearch *>(smem), tt, p.tile_tokens, expert, row0, rows);
+    find_tile(p, *reinterpret_cast<TileSearch *>(smem), tt, p.tile_tokens, 8, expert, row0, rows);
     fence_proxy_async_smem();  // the search's memory is the ring's
   }
   tc_fence_before();
@@ -635,22 +642,24 @@ __global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
 
 // ---------------------------------------------------------------- many tokens
 //
-// A cluster of two CTAs per tile of 256 tokens x kNT features (tcgen05.mma.cta_group::2): each CTA
-// holds 128 of the tokens and half of the features' codes, the atoms of its tokens and those of all
-// the features. Persistent, with two accumulators, so a tile's epilogue runs under the next one's MMAs.
+// A cluster of two CTAs per tile of 256 features and up to 224 tokens (tcgen05.mma.cta_group::2): each CTA
+// holds the codes of 128 of the features and half of the tokens, the atoms of its features and those of
+// all the tokens. The tokens are the MMA's N, of any multiple of 16: an expert's rows, cut into equal
+// tiles, cost what they are. (With tokens as the 256 rows of a tile 32444 rows of 128 experts of 2880 x 2880
+// took 171 us, XX so.) Persistent, with two accumulators, so a tile's epilogue runs under the next one's MMAs.
 //
-// A launch ahead (sq_fp4_atoms_kernel) writes the atoms: of each token tile two blocks of 128 rows, of
-// each feature tile two (the second of fewer rows), for every stage, and whether it met a negative scale.
+// A launch ahead (sq_fp4_atoms_kernel) writes the atoms: of each token tile two blocks of 128 rows (the second
+// of fewer), of each feature tile two, for every stage, and whether it met a negative scale.
 // Only then the pair kernel has a warp that mends the codes of each stage before the MMAs may read it.
 
 struct Fp4PairCfg {
-  static constexpr int kTokens = kFp4PairTokens, kNT = kFp4PairFeatures;
-  static constexpr int kEpiWarps = 8;  // lane quadrant w % 4, every other 32 columns from w / 4 on
+  static constexpr int kNT = kFp4PairTokens;  // columns of an accumulator
+  static constexpr int kEpiWarps = 8;  // 32 features w % 4, every other 32 tokens from w / 4 on
   static constexpr int kTmaWarp = kEpiWarps, kMmaWarp = kTmaWarp + 1, kMendWarp = kMmaWarp + 1;
   static constexpr int kThreads = 32 * (kMendWarp + 1);
   static constexpr int kA = 128 * 128, kB = kNT / 2 * 128;
   static constexpr int kMaxStages = 8;
-  static constexpr int kBox = 32 * 64;  // 32 rows x 32 columns of an epilogue warp
+  static constexpr int kBox = 32 * 64;  // 32 tokens x 32 features of an epilogue warp
 };
 static_assert(Fp4PairCfg::kNT <= 256 && Fp4PairCfg::kNT % 32 == 0 && 2 * Fp4PairCfg::kNT + 48 <= 512,
               "two accumulators and a stage's scales in tensor memory");
@@ -703,29 +712,26 @@ __device__ __forceinline__ void arrive_cluster(uint32_t cluster_bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 
-// Tile of a launch: expert, first row and rows of its 256, first feature. Every role walks the tiles in
+// Tile of a launch: expert, first row and rows, first feature. Every role walks the tiles in
 // increasing order, so the expert only moves forward.
 struct Fp4Tile {
   int e = 0, row0, rows, f0;
   int token_tile, feature_tile;  // of all experts
   __device__ __forceinline__ bool at(const Fp4Args &p, const int *starts, int tile) {
-    int tm, tn;
+    int tm, tn, lo = 0, hi = static_cast<int>(p.R), before = 0;
     if (p.offsets) {
       if (tile >= starts[p.E]) return false;
       while (starts[e + 1] <= tile) ++e;
-      int lo, hi;
       expert_rows(p, e, lo, hi);
-      tile_coords(tile - starts[e], (starts[e + 1] - starts[e]) / p.ftiles, p.ftiles, tm, tn);
-      row0 = lo + tm * kFp4PairTokens;
-      rows = min(kFp4PairTokens, hi - row0);
-      token_tile = starts[e] / p.ftiles + tm;
-    } else {
-      if (tile >= p.units) return false;
-      tile_coords(tile, static_cast<int>(p.units) / p.ftiles, p.ftiles, tm, tn);
-      row0 = tm * kFp4PairTokens;
-      rows = static_cast<int>(min(static_cast<int64_t>(kFp4PairTokens), p.R - row0));
-      token_tile = tm;
+      before = starts[e];
+    } else if (tile >= p.units) {
+      return false;
     }
+    tile_coords(tile - before, tile_count(hi - lo, kFp4PairTokens), p.ftiles, tm, tn);
+    const int height = tile_height(hi - lo, kFp4PairTokens, 16);
+    row0 = lo + tm * height;
+    rows = max(0, min(height, hi - row0));
+    token_tile = before / p.ftiles + tm;
     f0 = tn * kFp4PairFeatures;
     feature_tile = e * p.ftiles + tn;
     return true;
@@ -762,24 +768,25 @@ __global__ void __launch_bounds__(AtomCfg<FMT>::kThreads) sq_fp4_atoms_kernel(co
   if (tokens) {
     if (p.offsets) {
       int e, r0;
-      find_tile(p, *reinterpret_cast<TileSearch *>(piece), block >> 1, kFp4PairTokens, e, r0, rows);
+      find_tile(p, *reinterpret_cast<TileSearch *>(piece), block >> 1, kFp4PairTokens, 16, e, r0, rows);
       row0 = r0;
       __syncthreads();  // the search's memory is the pieces'
     } else {
-      row0 = static_cast<int64_t>(block >> 1) * kFp4PairTokens;
-      rows = static_cast<int>(min(static_cast<int64_t>(kFp4PairTokens), p.R - row0));
+      const int height = tile_height(static_cast<int>(p.R), kFp4PairTokens, 16);
+      row0 = static_cast<int64_t>(block >> 1) * height;
+      rows = static_cast<int>(max(int64_t(0), min(static_cast<int64_t>(height), p.R - row0)));
     }
     plane = p.x_scales;
     plane_rows = p.R;
     row0 += 128 * (block & 1);
     rows -= 128 * (block & 1);
-    out = p.x_atoms + static_cast<int64_t>(block) * cnt * (W * kAtom / 16);
+    out = p.x_atoms + (static_cast<int64_t>(block >> 1) * cnt * 2 + (block & 1)) * (W * kAtom / 16);
   } else {
     block -= p.token_blocks;
     const int tile = block >> 1, e = tile / p.ftiles, f0 = (tile - e * p.ftiles) * kFp4PairFeatures + 128 * (block & 1);
     row0 = static_cast<int64_t>(e) * p.N + f0;
-    rows = min(p.N - f0, kFp4PairFeatures - 128 * (block & 1));
-    out = p.w_atoms + (static_cast<int64_t>(tile) * cnt * 2 + (block & 1)) * (W * kAtom / 16);
+    rows = p.N - f0;
+    out = p.w_atoms + static_cast<int64_t>(block) * cnt * (W * kAtom / 16);
   }
   rows = min(rows, 128);
   const uint8_t *first = plane + row0 * p.G, *end = plane + plane_rows * p.G;
@@ -845,7 +852,7 @@ __global__ void __launch_bounds__(AtomCfg<FMT>::kThreads) sq_fp4_atoms_kernel(co
         sign |= w[r][i];
       }
     }
-    uint4 *dst = out + static_cast<int64_t>(kb) * (W * kAtom / 16) * (tokens ? 1 : 2) + lane;
+    uint4 *dst = out + static_cast<int64_t>(kb) * (W * kAtom / 16) * (tokens ? 2 : 1) + lane;
 #pragma unroll
     for (int i = 0; i < W; ++i) dst[i * (kAtom / 16)] = make_uint4(w[0][i], w[1][i], w[2][i], w[3][i]);
   }
@@ -861,8 +868,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
   using C = Fp4PairCfg;
   constexpr int W = Fp4<FMT>::kWords;
   constexpr int kBlock = W * kAtom;  // the atoms of 128 rows and a stage
-  constexpr int kSf = C::kA + C::kB, kBytes = kSf + 3 * kBlock, kStage = fp4_pair_stage(FMT);
-  static_assert(kBytes <= kStage && kStage % 1024 == 0, "a stage");
+  constexpr int kSf = C::kA + C::kB, kStage = fp4_pair_stage(FMT);
+  static_assert(kSf + 3 * kBlock <= kStage && kStage % 1024 == 0, "a stage");
   constexpr int kScaleCols = 12 * W, kScaleAt = 2 * C::kNT, kScaleBufs = (512 - kScaleAt) / kScaleCols >= 2 ? 2 : 1;
   extern __shared__ uint8_t fp4_smem_raw[];
   uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(fp4_smem_raw) + 1023) & ~uintptr_t(1023));
@@ -877,6 +884,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
   uint64_t *tfull = empty + C::kMaxStages;  // [2] accumulator complete                             (multicast commit)
   uint64_t *tempty = tfull + 2;             // [2] leader: both epilogues have read it              (8 warps of each)
   uint64_t *drain = tempty + 2;
+  __shared__ __align__(16) float row_scale[C::kEpiWarps][32];
+  __shared__ volatile uint32_t tile_n[C::kMaxStages];  // tokens of the tile that a stage belongs to, in whole 16
   int *starts = reinterpret_cast<int *>(smem + S * kStage + C::kEpiWarps * C::kBox);  // grouped: [E + 1] first tile of an expert
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -906,7 +915,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
     for (int e = threadIdx.x; e < p.E; e += C::kThreads) {
       int lo, hi;
       expert_rows(p, e, lo, hi);
-      starts[e + 1] = (hi - lo + C::kTokens - 1) / C::kTokens * p.ftiles;
+      starts[e + 1] = tile_count(hi - lo, kFp4PairTokens) * p.ftiles;
     }
     __syncthreads();
     if (warp == 0) {
@@ -940,24 +949,33 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
     uint32_t ph = 1;
     bool ok = true;
     for (int tile = first; ok && __all_sync(0xFFFFFFFFu, t.at(p, starts, tile)); tile += step) {
-      const int row = t.row0 + 128 * static_cast<int>(rank), f = t.f0 + C::kNT / 2 * static_cast<int>(rank);
-      int xa = (2 * t.token_tile + static_cast<int>(rank)) * cnt * W, wa = t.feature_tile * cnt * 2 * W;  // atoms' rows of 512 bytes
+      const int half = ((t.rows + 15) & ~15) / 2;  // tokens of a CTA, in the smallest box that holds them
+      int box = 0;
+      while (box + 1 < kFp4PairBoxes && (8 << box) < half) ++box;
+      const int box_rows = box + 1 < kFp4PairBoxes ? 8 << box : C::kNT / 2;
+      const int row = t.row0 + half * static_cast<int>(rank), f = t.f0 + 128 * static_cast<int>(rank);
+      int xa = t.token_tile * cnt * 2 * W, wa = (2 * t.feature_tile + static_cast<int>(rank)) * cnt * W;  // atoms' rows of 512 bytes
       for (int kb = 0; kb < cnt; ++kb, ++it) {
         if (it >= S && !(ok = warp_wait(&empty[s], ph, abort_flag, p.err))) break;
         const uint32_t at = ring + s * kStage;
+        if (kb == 0) {
+          tile_n[s] = 2 * half;
+          __syncwarp();
+        }
+        const uint32_t bytes = C::kA + 3 * kBlock + box_rows * 128;
         uint32_t bar = smem_u32(&landed[s]);
         if (mend) {
-          expect_tx_elect(&landed[s], kBytes);
+          expect_tx_elect(&landed[s], bytes);
         } else {
-          if (rank == 0) expect_tx_elect(&full[s], 2 * kBytes);
+          if (rank == 0) expect_tx_elect(&full[s], 2 * bytes);
           bar = mapa_shared(smem_u32(&full[s]), 0);
         }
-        tma_load_2d_pair_elect(at, &maps.x, bar, kb * (kDeep / 2), row);
-        tma_load_3d_pair_elect(at + C::kA, &maps.w, bar, kb * (kDeep / 2), f, t.e);
-        tma_load_2d_pair_elect(at + kSf, &maps.x_atoms, bar, 0, xa);
-        tma_load_2d_pair_elect(at + kSf + kBlock, &maps.w_atoms, bar, 0, wa);
-        xa += W;
-        wa += 2 * W;
+        tma_load_3d_pair_elect(at, &maps.w, bar, kb * (kDeep / 2), f, t.e);
+        tma_load_2d_pair_elect(at + C::kA, &maps.x[box], bar, kb * (kDeep / 2), row);
+        tma_load_2d_pair_elect(at + kSf, &maps.w_atoms, bar, 0, wa);
+        tma_load_2d_pair_elect(at + kSf + kBlock, &maps.x_atoms, bar, 0, xa);
+        wa += W;
+        xa += 2 * W;
         if (++s == S) {
           s = 0;
           ph ^= 1u;
@@ -982,6 +1000,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
       for (int tc = 0; tc < mine; ++tc) {
         const int ab = tc & 1;
         if (tc >= 2) warp_wait(&tempty[ab], (static_cast<uint32_t>(tc >> 1) & 1u) ^ 1u, abort_flag, p.err);
+        // the tile's N comes with its first stage: looked up here it would bring its branches into the loop
+        warp_wait(&full[s], ph, abort_flag, p.err);
+        const uint32_t n16 = __reduce_max_sync(0xFFFFFFFFu, tile_n[s]);
         const uint32_t d = tmem + ab * C::kNT;
         for (int kb = 0; kb < cnt; ++kb, ++it) {
           warp_wait(&full[s], ph, abort_flag, p.err);
@@ -998,9 +1019,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
 #pragma unroll
           for (int kk = 0; kk < 4; ++kk) {
             const int word = FMT == 0 ? kk : kk / 2;
-            constexpr uint32_t kDesc[2] = {idesc_fp4<FMT>(2 * 128, C::kNT, 0), idesc_fp4<FMT>(2 * 128, C::kNT, FMT == 0 ? 0 : 2)};
+            constexpr uint32_t kDesc[2] = {idesc_fp4<FMT>(2 * 128, 0, 0), idesc_fp4<FMT>(2 * 128, 0, FMT == 0 ? 0 : 2)};
             if (kk < steps)
-              umma_fp4_pair_elect<FMT>(d, ad0 + so + 2 * kk, bd0 + so + 2 * kk, kDesc[kk & 1], sa + 4 * word, sb + 8 * word,
+              umma_fp4_pair_elect<FMT>(d, ad0 + so + 2 * kk, bd0 + so + 2 * kk, kDesc[kk & 1] | n16 << 14, sa + 4 * word, sb + 8 * word,
                                        (kb > 0 || kk > 0) ? 1u : 0u);
           }
           commit_pair_mc_elect(&empty[s]);
@@ -1024,9 +1045,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
         for (int kb = 0; kb < cnt; ++kb) {
           if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&landed[s], ph, abort_flag, p.err)))) break;
           const uint32_t at = ring + s * kStage;
-          for (int i = 0; i < 3 * W; ++i) {  // atom i % W of the tokens, the first and the other features
+          const int half = ((t.rows + 15) & ~15) / 2;
+          for (int i = 0; i < 3 * W; ++i) {  // atom i % W of the features, the first 128 and the other tokens
             const int of = i / W, word = i % W;
-            const int lift = of == 0 ? 0 : 128 * (of - 1) - C::kNT / 2 * static_cast<int>(rank), rows = of == 0 ? 128 : C::kNT / 2;
+            const int lift = of == 0 ? 0 : 128 * (of - 1) - half * static_cast<int>(rank), rows = of == 0 ? 128 : half;
             const uint32_t line = at + kSf + i * kAtom + lane * 16;
             const uint4 x = lds128(line);
             uint32_t w[4] = {x.x, x.y, x.z, x.w};
@@ -1055,47 +1077,65 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
     }
   } else {
     // ------------------------------------------------------ epilogue
+    // A lane has a feature's 32 tokens. Two neighbours exchange halves, so each has two features of 16
+    // tokens, and put them into a box whose line t holds tokens t and t + 16, 64 bytes each: written and
+    // read without bank conflicts.
     const int quad = warp & 3, share = warp >> 2;
     const uint32_t t_row = tmem + (static_cast<uint32_t>(quad * 32) << 16);
     const uint32_t box = ring + S * kStage + warp * C::kBox;
+    float *scales = row_scale[warp];
     int tc = 0;
     bool ok = true;
     for (int tile = first; ok && t.at(p, starts, tile); tile += step, ++tc) {
       const int ab = tc & 1;
-      const int r0 = 128 * static_cast<int>(rank) + 32 * quad;  // of the tile's rows
+      const int groups = (t.rows + 31) / 32;  // of 32 tokens
       const float ws2 = p.w_ws2 ? p.w_ws2[t.e] : p.ws2;
-      const float row = r0 + lane < t.rows ? (p.row_ws2 ? p.row_ws2[static_cast<int64_t>(t.row0) + r0 + lane] : p.x_ws2) : 0.f;
       ok = __all_sync(0xFFFFFFFFu, mbar_wait(&tfull[ab], static_cast<uint32_t>(tc >> 1) & 1u, abort_flag, p.err));
       if (!ok) break;
       tc_fence_after();
+      auto release = [&] {  // the warp's part of the accumulator is read
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive_cluster(mapa_shared(smem_u32(&tempty[ab]), 0));
+      };
+      if (share >= groups) release();
 #pragma unroll 1
-      for (int g = share; g < C::kNT / 32; g += 2) {  // 32 columns
+      for (int g = share; g < groups; g += 2) {
+        const int left = t.rows - 32 * g;  // tokens of the group
         uint32_t v[32];
         tmem_ld32(t_row + ab * C::kNT + 32 * g, v);
+        const float mine = lane < left ? (p.row_ws2 ? p.row_ws2[static_cast<int64_t>(t.row0) + 32 * g + lane] : p.x_ws2) : 0.f;
+        __syncwarp();  // the box and the scales are read
+        scales[lane] = mine;
         tmem_ld_wait();
-        if (g + 2 >= C::kNT / 32) {  // the warp's part of the accumulator is read
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) arrive_cluster(mapa_shared(smem_u32(&tempty[ab]), 0));
-        }
-        uint32_t o[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(v[2 * i]) * ws2 * row, __uint_as_float(v[2 * i + 1]) * ws2 * row);
-          o[i] = *reinterpret_cast<const uint32_t *>(&h);
-        }
-        __syncwarp();  // the box is read
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          st_shared_v4(box + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4), o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
+        if (g + 2 >= groups) release();
         __syncwarp();
-        const int f = t.f0 + 32 * g + 8 * (lane & 3);
+        uint32_t o[16];  // tokens 2 i and 2 i + 1
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+          const float4 r = *reinterpret_cast<const float4 *>(scales + i);
+          const __nv_bfloat162 a = __floats2bfloat162_rn(__uint_as_float(v[i]) * ws2 * r.x, __uint_as_float(v[i + 1]) * ws2 * r.y);
+          const __nv_bfloat162 b = __floats2bfloat162_rn(__uint_as_float(v[i + 2]) * ws2 * r.z, __uint_as_float(v[i + 3]) * ws2 * r.w);
+          o[i / 2] = *reinterpret_cast<const uint32_t *>(&a);
+          o[i / 2 + 1] = *reinterpret_cast<const uint32_t *>(&b);
+        }
+        const bool odd = lane & 1;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {  // even lanes keep tokens 0-15, odd ones 16-31, of both features
+          const uint32_t other = __shfl_xor_sync(0xFFFFFFFFu, odd ? o[i] : o[i + 8], 1);
+          const uint32_t even_f = odd ? other : o[i], odd_f = odd ? o[i + 8] : other;
+          const uint32_t at = box + 2 * i * 128 + (odd ? 64 : 0) + (lane >> 1) * 4;
+          asm volatile("st.shared.b32 [%0], %1;" ::"r"(at), "r"(prmt(even_f, odd_f, 0x5410u)) : "memory");
+          asm volatile("st.shared.b32 [%0], %1;" ::"r"(at + 128), "r"(prmt(even_f, odd_f, 0x7632u)) : "memory");
+        }
+        __syncwarp();
+        const int f = t.f0 + 128 * static_cast<int>(rank) + 32 * quad + 8 * (lane & 3);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const int r = 8 * q + (lane >> 2);
-          const uint4 y = lds128(box + r * 64 + (((lane & 3) ^ ((r >> 1) & 3)) << 4));
-          if (r0 + r < t.rows && f < p.N)
-            *reinterpret_cast<uint4 *>(p.out + (static_cast<int64_t>(t.row0) + r0 + r) * p.N + f) = y;
+          const int line = 4 * q + (lane >> 3), r = line + (lane & 4 ? 16 : 0);  // eight lanes a line
+          const uint4 y = lds128(box + line * 128 + (lane & 7) * 16);
+          if (r < left && f < p.N)
+            *reinterpret_cast<uint4 *>(p.out + (static_cast<int64_t>(t.row0) + 32 * g + r) * p.N + f) = y;
         }
       }
     }

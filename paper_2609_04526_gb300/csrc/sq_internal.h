@@ -491,16 +491,17 @@ constexpr int kFp4FewTokens = 128;           // of a tile of the few-token kerne
 constexpr int kFp4FewBoxes = 5;              // boxes of 8 .. 128 token rows
 constexpr int kFp4SmemAlone = 224 * 1024;    // of a CTA alone on its SM
 constexpr int kFp4SmemShared = 112 * 1024;   // ... of two
-constexpr int kFp4SmemMost = 232448 - 512;  // ... beside its static shared memory
-constexpr int kFp4PairTokens = 256, kFp4PairFeatures = 224;  // a tile of the pair kernel
+constexpr int kFp4SmemMost = 232448 - 1536;  // ... beside its static shared memory
+constexpr int kFp4PairTokens = 224, kFp4PairFeatures = 256;  // a tile of the pair kernel, at most
+constexpr int kFp4PairBoxes = 5;                             // boxes of 8 .. 64 and 112 token rows
 struct Fp4Maps {
   CUtensorMap w;                // codes [E][N][K / 2], boxes of 128 bytes x 128 rows
   CUtensorMap x[kFp4FewBoxes];  // codes [R][K / 2], boxes of 128 bytes x (8 << i) rows
   CUtensorMap w_scales, x_scales[kFp4FewBoxes];  // scale bytes, boxes of 16 bytes x the same rows (whole 16-byte rows only)
 };
 struct Fp4PairMaps {
-  CUtensorMap w, x;              // codes, boxes of 128 bytes x half the features and 128 rows
-  CUtensorMap w_atoms, x_atoms;  // [atoms][512 bytes], boxes of a stage's of 256 features and 128 rows
+  CUtensorMap w, x[kFp4PairBoxes];  // codes, boxes of 128 bytes x 128 features and of as many token rows
+  CUtensorMap w_atoms, x_atoms;     // [atoms][512 bytes], boxes of a stage's of 128 features and 256 rows
 };
 struct Fp4Args {
   int64_t R;                 // rows
@@ -519,18 +520,18 @@ struct Fp4Args {
   int64_t units;             // tiles, at most
   int splits;                // few: parts of the contraction (CTAs of a cluster)
   int stages;                // of the ring
-  // pair: atoms of the scales, [token block][stage] and [feature tile][stage][2], and per CTA that writes them whether
-  // it met a negative one
+  // pair: atoms of the scales, [token tile][stage][2] and [block of 128 features][stage], and per CTA that writes them
+  // whether it met a negative one
   uint4 *x_atoms, *w_atoms;
   int *negative;
   int token_blocks, atom_ctas;
 };
 // A few-token stage: codes of 128 features and a tile's tokens, scales of 128 rows of both. A pair stage: codes of 128
-// tokens and half the features, atoms of those tokens and of 256 features; behind the ring eight 2 KiB boxes of the
+// features and half the tokens, atoms of those features and of 256 tokens; behind the ring eight 2 KiB boxes of the
 // epilogue and the experts' first tiles.
 constexpr int fp4_few_stage(int tile_tokens) { return 128 * 128 + tile_tokens * 128 + 2 * 2048; }
 __host__ __device__ constexpr int fp4_atoms(int fmt) { return fmt == 0 ? 2048 : 1024; }  // bytes of 128 rows and a stage
-__host__ __device__ constexpr int fp4_pair_stage(int fmt) { return 128 * 128 + kFp4PairFeatures / 2 * 128 + 3 * fp4_atoms(fmt); }
+__host__ __device__ constexpr int fp4_pair_stage(int fmt) { return 128 * 128 + kFp4PairTokens / 2 * 128 + 3 * fp4_atoms(fmt); }
 constexpr size_t fp4_pair_smem(int fmt, int stages, int E) {
   return 1024 + static_cast<size_t>(stages) * fp4_pair_stage(fmt) + 8 * 2048 + (E > 0 ? 4 * (E + 1) : 0);
 }
