@@ -137,27 +137,49 @@ __device__ __forceinline__ void tma_load_3d_elect(uint32_t dst, const CUtensorMa
       : "memory");
 }
 
-// The same of a CTA pair, counted on a barrier of either CTA (`bar_cluster`).
-__device__ __forceinline__ void tma_load_2d_pair_elect(uint32_t dst, const CUtensorMap *map, uint32_t bar_cluster, int32_t x,
-                                                       int32_t y) {
+__device__ __forceinline__ void tma_prefetch_3d_elect(const CUtensorMap *map, int32_t x, int32_t y, int32_t z) {
   asm volatile(
       "{\n\t.reg .pred e;\n\t"
       "elect.sync _|e, 0xFFFFFFFF;\n\t"
+      "@e cp.async.bulk.prefetch.tensor.3d.L2.global [%0, {%1, %2, %3}];\n\t}" ::"l"(reinterpret_cast<uint64_t>(map)),
+      "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
+
+// The same of a CTA pair, where `go`, counted on a barrier of either CTA (`bar_cluster`).
+__device__ __forceinline__ void tma_load_2d_pair_elect(uint32_t go, uint32_t dst, const CUtensorMap *map,
+                                                       uint32_t bar_cluster, int32_t x, int32_t y) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t"
+      "elect.sync _|e, 0xFFFFFFFF;\n\t"
+      "setp.ne.and.b32 e, %5, 0, e;\n\t"
       "@e cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4}], "
       "[%2];\n\t}" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar_cluster), "r"(x), "r"(y)
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar_cluster), "r"(x), "r"(y), "r"(go)
       : "memory");
 }
-__device__ __forceinline__ void tma_load_3d_pair_elect(uint32_t dst, const CUtensorMap *map, uint32_t bar_cluster, int32_t x,
-                                                       int32_t y, int32_t z) {
+__device__ __forceinline__ void tma_load_3d_pair_elect(uint32_t go, uint32_t dst, const CUtensorMap *map,
+                                                       uint32_t bar_cluster, int32_t x, int32_t y, int32_t z) {
   asm volatile(
       "{\n\t.reg .pred e;\n\t"
       "elect.sync _|e, 0xFFFFFFFF;\n\t"
+      "setp.ne.and.b32 e, %6, 0, e;\n\t"
       "@e cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4, %5}], "
       "[%2];\n\t}" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar_cluster), "r"(x), "r"(y), "r"(z)
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar_cluster), "r"(x), "r"(y), "r"(z), "r"(go)
       : "memory");
 }
+__device__ __forceinline__ void expect_tx_elect(uint32_t go, uint32_t bar, uint32_t bytes) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t"
+      "elect.sync _|e, 0xFFFFFFFF;\n\t"
+      "setp.ne.and.b32 e, %2, 0, e;\n\t"
+      "@e mbarrier.arrive.expect_tx.release.cta.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar),
+      "r"(bytes), "r"(go)
+      : "memory");
+}
+// A value that is the same in all lanes, in a uniform register.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __reduce_max_sync(0xFFFFFFFFu, x); }
 
 // The scale bytes of 128 rows, stage by stage, for one warp that loads them itself: lane l takes rows l,
 // l + 32, l + 64 and l + 96. A row's bytes start anywhere, so a stage's are cut out of the two aligned
@@ -429,6 +451,7 @@ __global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
   __shared__ uint64_t bars[3 * C::kMaxStages + 1];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_word;
+  __shared__ float row_scale[kFp4FewTokens];
   volatile int *abort_flag = &abort_word;
   uint64_t *full = bars;                     // [S] codes of both operands landed          (1 arrival + tx)
   uint64_t *sfull = full + C::kMaxStages;    // [S] their scales are in place              (2 warps)
@@ -454,6 +477,12 @@ __global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
     fence_proxy_async_smem();
   }
   if (warp == C::kMmaWarp) tmem_alloc(&tmem_slot, C::kTmemCols);
+  // The weight's way to the L2 needs nothing that the launch ahead writes: it begins beside that launch.
+  // (An older line that it brings is overwritten there like any other.)
+  const int cnt_all = (p.K + kDeep - 1) / kDeep, it0 = cnt_all * part / splits;
+  if (!p.offsets && warp == C::kTmaWarp)
+    for (int it = it0; it < cnt_all * (part + 1) / splits && it < it0 + 4; ++it)
+      tma_prefetch_3d_elect(&maps.w, it * (kDeep / 2), f0, 0);
   dependency_wait();
   dependency_start();
   int expert = 0, row0 = tt * p.tile_tokens, rows = static_cast<int>(min(p.R - row0, static_cast<int64_t>(p.tile_tokens)));
@@ -461,12 +490,13 @@ __global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
     find_tile(p, *reinterpret_cast<TileSearch *>(smem), tt, p.tile_tokens, 8, expert, row0, rows);
     fence_proxy_async_smem();  // the search's memory is the ring's
   }
+  // read here and not where they are used: one after the other there took 3 us of a tile
+  if (threadIdx.x < rows) row_scale[threadIdx.x] = p.row_ws2 ? p.row_ws2[row0 + threadIdx.x] : p.x_ws2;
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
-  const int cnt_all = (p.K + kDeep - 1) / kDeep;
-  const int it0 = cnt_all * part / splits, cnt = __any_sync(0xFFFFFFFFu, rows > 0) ? cnt_all * (part + 1) / splits - it0 : 0;
+  const int cnt = __any_sync(0xFFFFFFFFu, rows > 0) ? cnt_all * (part + 1) / splits - it0 : 0;
   const int n8 = (rows + 7) & ~7;
   const uint32_t ring = smem_u32(smem);
   const int x_off = C::kF * 128, sf_off = x_off + p.tile_tokens * 128, stage = sf_off + 2 * kScales;
@@ -612,22 +642,31 @@ __global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
   const int j = threadIdx.x & 15, f = f0 + 8 * j;
   if (f < p.N) {
     for (int t = part * (C::kThreads / 16) + (threadIdx.x >> 4); t < rows; t += splits * (C::kThreads / 16)) {
-      float y[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = 0.f;
+      float y[8] = {};
       const uint32_t mine = ring + (t * C::kF + 8 * j) * 4;
-      for (int q = 0; q < splits; ++q) {
-        const uint32_t at = splits > 1 ? mapa_shared(mine, q) : mine;
+      for (int q0 = 0; q0 < splits; q0 += 4) {  // the loads of four parts, then their sums in order
+        float4 v[8];
 #pragma unroll
-        for (int i = 0; i < 8; i += 4) {
-          float4 v;
-          asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                       : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-                       : "r"(at + 4 * i));
-          y[i] += v.x, y[i + 1] += v.y, y[i + 2] += v.z, y[i + 3] += v.w;
+        for (int q = 0; q < 4; ++q) {
+          v[2 * q] = v[2 * q + 1] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (q0 + q < splits) {
+            const uint32_t at = splits > 1 ? mapa_shared(mine, q0 + q) : mine;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+              asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                           : "=f"(v[2 * q + i].x), "=f"(v[2 * q + i].y), "=f"(v[2 * q + i].z), "=f"(v[2 * q + i].w)
+                           : "r"(at + 16 * i));
+          }
         }
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            y[4 * i] += v[2 * q + i].x, y[4 * i + 1] += v[2 * q + i].y;
+            y[4 * i + 2] += v[2 * q + i].z, y[4 * i + 3] += v[2 * q + i].w;
+          }
       }
-      const float row = p.row_ws2 ? p.row_ws2[row0 + t] : p.x_ws2;
+      const float row = row_scale[t];
       uint32_t o[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -712,25 +751,31 @@ __device__ __forceinline__ void arrive_cluster(uint32_t cluster_bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 
+// A grouped launch's experts in shared memory: first tile [E + 1], first row and rows [E].
+struct Fp4Experts {
+  int *starts, *lo, *rows;
+};
+
 // Tile of a launch: expert, first row and rows, first feature. Every role walks the tiles in
 // increasing order, so the expert only moves forward.
 struct Fp4Tile {
   int e = 0, row0, rows, f0;
   int token_tile, feature_tile;  // of all experts
-  __device__ __forceinline__ bool at(const Fp4Args &p, const int *starts, int tile) {
-    int tm, tn, lo = 0, hi = static_cast<int>(p.R), before = 0;
+  __device__ __forceinline__ bool at(const Fp4Args &p, const Fp4Experts &x, int tile) {
+    int tm, tn, lo = 0, n = static_cast<int>(p.R), before = 0;
     if (p.offsets) {
-      if (tile >= starts[p.E]) return false;
-      while (starts[e + 1] <= tile) ++e;
-      expert_rows(p, e, lo, hi);
-      before = starts[e];
+      if (tile >= x.starts[p.E]) return false;
+      while (x.starts[e + 1] <= tile) ++e;
+      before = x.starts[e];
+      lo = x.lo[e];
+      n = x.rows[e];
     } else if (tile >= p.units) {
       return false;
     }
-    tile_coords(tile - before, tile_count(hi - lo, kFp4PairTokens), p.ftiles, tm, tn);
-    const int height = tile_height(hi - lo, kFp4PairTokens, 16);
+    tile_coords(tile - before, tile_count(n, kFp4PairTokens), p.ftiles, tm, tn);
+    const int height = tile_height(n, kFp4PairTokens, 16);
     row0 = lo + tm * height;
-    rows = max(0, min(height, hi - row0));
+    rows = max(0, min(height, lo + n - row0));
     token_tile = before / p.ftiles + tm;
     f0 = tn * kFp4PairFeatures;
     feature_tile = e * p.ftiles + tn;
@@ -886,7 +931,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
   uint64_t *drain = tempty + 2;
   __shared__ __align__(16) float row_scale[C::kEpiWarps][32];
   __shared__ volatile uint32_t tile_n[C::kMaxStages];  // tokens of the tile that a stage belongs to, in whole 16
-  int *starts = reinterpret_cast<int *>(smem + S * kStage + C::kEpiWarps * C::kBox);  // grouped: [E + 1] first tile of an expert
+  Fp4Experts ex;
+  ex.starts = reinterpret_cast<int *>(smem + S * kStage + C::kEpiWarps * C::kBox);
+  ex.lo = ex.starts + p.E + 1;
+  ex.rows = ex.lo + p.E;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
@@ -915,22 +963,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
     for (int e = threadIdx.x; e < p.E; e += C::kThreads) {
       int lo, hi;
       expert_rows(p, e, lo, hi);
-      starts[e + 1] = tile_count(hi - lo, kFp4PairTokens) * p.ftiles;
+      ex.lo[e] = lo;
+      ex.rows[e] = hi - lo;
+      ex.starts[e + 1] = tile_count(hi - lo, kFp4PairTokens) * p.ftiles;
     }
     __syncthreads();
     if (warp == 0) {
       int before = 0;
       for (int e0 = 0; e0 < p.E; e0 += 32) {
-        int v = e0 + lane < p.E ? starts[e0 + lane + 1] : 0;
+        int v = e0 + lane < p.E ? ex.starts[e0 + lane + 1] : 0;
 #pragma unroll
         for (int d = 1; d < 32; d *= 2) {
           const int u = __shfl_up_sync(0xFFFFFFFFu, v, d);
           if (lane >= d) v += u;
         }
-        if (e0 + lane < p.E) starts[e0 + lane + 1] = before + v;
+        if (e0 + lane < p.E) ex.starts[e0 + lane + 1] = before + v;
         before += __shfl_sync(0xFFFFFFFFu, v, 31);
       }
-      if (lane == 0) starts[0] = 0;
+      if (lane == 0) ex.starts[0] = 0;
     }
   }
   tc_fence_before();
@@ -940,40 +990,42 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
   const uint32_t tmem = tmem_slot, ring = smem_u32(smem);
   const int cnt = (p.K + kDeep - 1) / kDeep;
   const int first = static_cast<int>(blockIdx.x >> 1), step = static_cast<int>(gridDim.x >> 1);
+  const int tiles = p.offsets ? ex.starts[p.E] : static_cast<int>(p.units);
+  const int pair_tiles = first < tiles ? (tiles - first + step - 1) / step : 0;  // of this pair
   Fp4Tile t;
 
   if (warp == C::kTmaWarp) {
     // ------------------------------------------------------ codes and atoms
-    // Counted on the leader's barrier or, where codes have to be mended, on this CTA's own.
+    // Counted on the leader's barrier or, where codes have to be mended, on this CTA's own. Loops without
+    // exits and uniform values here too (the loads of a stage took 590 cycles to issue, more than its MMAs):
+    // after a wait that ran out nothing is loaded.
+    const bool own = mend, counts = mend || rank == 0;
+    const int mine = uniform(pair_tiles);
     int it = 0, s = 0;
-    uint32_t ph = 1;
-    bool ok = true;
-    for (int tile = first; ok && __all_sync(0xFFFFFFFFu, t.at(p, starts, tile)); tile += step) {
-      const int half = ((t.rows + 15) & ~15) / 2;  // tokens of a CTA, in the smallest box that holds them
+    uint32_t ph = 1, go = 1;
+    for (int tc = 0; tc < mine; ++tc) {
+      t.at(p, ex, first + tc * step);
+      const int half = uniform(((t.rows + 15) & ~15) / 2);  // tokens of a CTA, in the smallest box that holds them
       int box = 0;
       while (box + 1 < kFp4PairBoxes && (8 << box) < half) ++box;
-      const int box_rows = box + 1 < kFp4PairBoxes ? 8 << box : C::kNT / 2;
-      const int row = t.row0 + half * static_cast<int>(rank), f = t.f0 + 128 * static_cast<int>(rank);
-      int xa = t.token_tile * cnt * 2 * W, wa = (2 * t.feature_tile + static_cast<int>(rank)) * cnt * W;  // atoms' rows of 512 bytes
+      box = uniform(box);
+      const uint32_t bytes = C::kA + 3 * kBlock + (box + 1 < kFp4PairBoxes ? 8 << box : C::kNT / 2) * 128;
+      const int row = uniform(t.row0) + half * static_cast<int>(rank), f = uniform(t.f0) + 128 * static_cast<int>(rank), e = uniform(t.e);
+      int xa = uniform(t.token_tile) * cnt * 2 * W, wa = (2 * uniform(t.feature_tile) + static_cast<int>(rank)) * cnt * W;  // rows of 512 bytes
       for (int kb = 0; kb < cnt; ++kb, ++it) {
-        if (it >= S && !(ok = warp_wait(&empty[s], ph, abort_flag, p.err))) break;
+        if (it >= S) go = warp_wait(&empty[s], ph, abort_flag, p.err) ? go : 0;
         const uint32_t at = ring + s * kStage;
         if (kb == 0) {
           tile_n[s] = 2 * half;
           __syncwarp();
         }
-        const uint32_t bytes = C::kA + 3 * kBlock + box_rows * 128;
-        uint32_t bar = smem_u32(&landed[s]);
-        if (mend) {
-          expect_tx_elect(&landed[s], bytes);
-        } else {
-          if (rank == 0) expect_tx_elect(&full[s], 2 * bytes);
-          bar = mapa_shared(smem_u32(&full[s]), 0);
-        }
-        tma_load_3d_pair_elect(at, &maps.w, bar, kb * (kDeep / 2), f, t.e);
-        tma_load_2d_pair_elect(at + C::kA, &maps.x[box], bar, kb * (kDeep / 2), row);
-        tma_load_2d_pair_elect(at + kSf, &maps.w_atoms, bar, 0, wa);
-        tma_load_2d_pair_elect(at + kSf + kBlock, &maps.x_atoms, bar, 0, xa);
+        const uint32_t count = smem_u32(own ? &landed[s] : &full[s]);
+        expect_tx_elect(counts ? go : 0, count, own ? bytes : 2 * bytes);
+        const uint32_t bar = mapa_shared(count, own ? rank : 0);
+        tma_load_3d_pair_elect(go, at, &maps.w, bar, kb * (kDeep / 2), f, e);
+        tma_load_2d_pair_elect(go, at + C::kA, &maps.x[box], bar, kb * (kDeep / 2), row);
+        tma_load_2d_pair_elect(go, at + kSf, &maps.w_atoms, bar, 0, wa);
+        tma_load_2d_pair_elect(go, at + kSf + kBlock, &maps.x_atoms, bar, 0, xa);
         wa += W;
         xa += 2 * W;
         if (++s == S) {
@@ -993,8 +1045,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
       const uint64_t sd0 = atom_desc(ring + kSf);
       // Behind the MMA that they run the tensor cores hold about two more: between the last MMA of a stage and
       // the first of the next there are 250 cycles for the barriers, the commit and the atoms.
-      const int tiles = p.offsets ? starts[p.E] : static_cast<int>(p.units);
-      const int mine = __reduce_max_sync(0xFFFFFFFFu, first < tiles ? (tiles - first + step - 1) / step : 0);
+      const int mine = __reduce_max_sync(0xFFFFFFFFu, pair_tiles);
       int s = 0, it = 0;
       uint32_t ph = 0;
       for (int tc = 0; tc < mine; ++tc) {
@@ -1041,7 +1092,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
       int s = 0;
       uint32_t ph = 0;
       bool ok = true;
-      for (int tile = first; ok && t.at(p, starts, tile); tile += step)
+      for (int tile = first; ok && t.at(p, ex, tile); tile += step)
         for (int kb = 0; kb < cnt; ++kb) {
           if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&landed[s], ph, abort_flag, p.err)))) break;
           const uint32_t at = ring + s * kStage;
@@ -1086,7 +1137,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
     float *scales = row_scale[warp];
     int tc = 0;
     bool ok = true;
-    for (int tile = first; ok && t.at(p, starts, tile); tile += step, ++tc) {
+    for (int tile = first; ok && t.at(p, ex, tile); tile += step, ++tc) {
       const int ab = tc & 1;
       const int groups = (t.rows + 31) / 32;  // of 32 tokens
       const float ws2 = p.w_ws2 ? p.w_ws2[t.e] : p.ws2;

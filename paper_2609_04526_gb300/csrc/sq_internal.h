@@ -528,12 +528,12 @@ struct Fp4Args {
 };
 // A few-token stage: codes of 128 features and a tile's tokens, scales of 128 rows of both. A pair stage: codes of 128
 // features and half the tokens, atoms of those features and of 256 tokens; behind the ring eight 2 KiB boxes of the
-// epilogue and the experts' first tiles.
+// epilogue and the experts' first tiles and rows.
 constexpr int fp4_few_stage(int tile_tokens) { return 128 * 128 + tile_tokens * 128 + 2 * 2048; }
 __host__ __device__ constexpr int fp4_atoms(int fmt) { return fmt == 0 ? 2048 : 1024; }  // bytes of 128 rows and a stage
 __host__ __device__ constexpr int fp4_pair_stage(int fmt) { return 128 * 128 + kFp4PairTokens / 2 * 128 + 3 * fp4_atoms(fmt); }
 constexpr size_t fp4_pair_smem(int fmt, int stages, int E) {
-  return 1024 + static_cast<size_t>(stages) * fp4_pair_stage(fmt) + 8 * 2048 + (E > 0 ? 4 * (E + 1) : 0);
+  return 1024 + static_cast<size_t>(stages) * fp4_pair_stage(fmt) + 8 * 2048 + (E > 0 ? 4 * (3 * E + 1) : 0);
 }
 // Kernel, tiles and parts of a product on sm_count SMs: fills the last fields of p.
 inline void fp4_plan(int fmt, int sm_count, Fp4Args &p) {
@@ -555,7 +555,11 @@ inline void fp4_plan(int fmt, int sm_count, Fp4Args &p) {
   while (p.tile_tokens < kFp4FewTokens && p.tile_tokens * groups < p.R) p.tile_tokens *= 2;
   p.units = ((p.R + (p.tile_tokens - 1) * groups) / p.tile_tokens) * p.ftiles;
   const int cnt = (p.K + 255) / 256;
-  p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({8, cnt, sm_count / p.units})));
+  // Parts: as many as leave every cluster an SM for each of its CTAs at once. A cluster's are of one of 8 groups of
+  // SMs, 18 or 20 of the 152 in each (18 clusters of 8 ran one after the other: 187 tokens against 1048 x
+  // 2720 XX us, XX in 6 parts).
+  p.splits = std::min(8, cnt);
+  while (p.splits > 1 && p.units > 8 * ((sm_count / 8 - 1) / p.splits)) --p.splits;
   const int stage = fp4_few_stage(p.tile_tokens);
   const bool alone = p.units * p.splits <= sm_count;
   p.stages = std::min(8, ((alone ? kFp4SmemAlone : kFp4SmemShared) - 1024) / stage);
