@@ -685,7 +685,7 @@ __global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
 // holds the codes of 128 of the features and half of the tokens, the atoms of its features and those of
 // all the tokens. The tokens are the MMA's N, of any multiple of 16: an expert's rows, cut into equal
 // tiles, cost what they are. (With tokens as the 256 rows of a tile 32444 rows of 128 experts of 2880 x 2880
-// took 171 us, XX so.) Persistent, with two accumulators, so a tile's epilogue runs under the next one's MMAs.
+// took 171 us, 157 so.) Persistent, with two accumulators, so a tile's epilogue runs under the next one's MMAs.
 //
 // A launch ahead (sq_fp4_atoms_kernel) writes the atoms: of each token tile two blocks of 128 rows (the second
 // of fewer), of each feature tile two, for every stage, and whether it met a negative scale.
@@ -762,18 +762,25 @@ struct Fp4Tile {
   int e = 0, row0, rows, f0;
   int token_tile, feature_tile;  // of all experts
   __device__ __forceinline__ bool at(const Fp4Args &p, const Fp4Experts &x, int tile) {
-    int tm, tn, lo = 0, n = static_cast<int>(p.R), before = 0;
+    int tm, tn, lo = 0, n = static_cast<int>(p.R), before = 0, height = p.tile_tokens;
     if (p.offsets) {
       if (tile >= x.starts[p.E]) return false;
       while (x.starts[e + 1] <= tile) ++e;
       before = x.starts[e];
       lo = x.lo[e];
       n = x.rows[e];
-    } else if (tile >= p.units) {
-      return false;
+      height = tile_height(n, kFp4PairTokens, 16);
+      tile_coords(tile - before, tile_count(n, kFp4PairTokens), p.ftiles, tm, tn);
+    } else {  // the tiles of the last rows, where they are fewer, behind all others
+      if (tile >= p.units) return false;
+      const int whole = n / height;
+      if (tile < whole * p.ftiles) {
+        tile_coords(tile, whole, p.ftiles, tm, tn);
+      } else {
+        tm = whole;
+        tn = tile - whole * p.ftiles;
+      }
     }
-    tile_coords(tile - before, tile_count(n, kFp4PairTokens), p.ftiles, tm, tn);
-    const int height = tile_height(n, kFp4PairTokens, 16);
     row0 = lo + tm * height;
     rows = max(0, min(height, lo + n - row0));
     token_tile = before / p.ftiles + tm;
@@ -783,12 +790,12 @@ struct Fp4Tile {
   }
 };
 
-// Atoms of 128 rows and 8 stages per CTA. The rows' bytes come in whole 16-byte pieces to shared memory
+// Atoms of 128 rows and 8 (NVFP4) or 16 stages per CTA. The rows' bytes come in whole 16-byte pieces to shared memory
 // (lines apart by an odd number of pieces, free of bank conflicts) and are cut out from there.
 template <int FMT>
 struct AtomCfg {
-  static constexpr int kThreads = 256, kStages = 8;
-  static constexpr int kSpanBytes = kStages * Fp4<FMT>::kBytes;     // of a row: 128 or 64
+  static constexpr int kThreads = 256, kStages = fp4_atom_stages(FMT);
+  static constexpr int kSpanBytes = kStages * Fp4<FMT>::kBytes;     // of a row: 128
   static constexpr int kPieces = kSpanBytes / 16 + 1;               // that hold them
   static_assert(kPieces % 2 == 1, "rows an odd number of 16-byte pieces apart");
 };
@@ -817,9 +824,8 @@ __global__ void __launch_bounds__(AtomCfg<FMT>::kThreads) sq_fp4_atoms_kernel(co
       row0 = r0;
       __syncthreads();  // the search's memory is the pieces'
     } else {
-      const int height = tile_height(static_cast<int>(p.R), kFp4PairTokens, 16);
-      row0 = static_cast<int64_t>(block >> 1) * height;
-      rows = static_cast<int>(max(int64_t(0), min(static_cast<int64_t>(height), p.R - row0)));
+      row0 = static_cast<int64_t>(block >> 1) * p.tile_tokens;
+      rows = static_cast<int>(min(static_cast<int64_t>(p.tile_tokens), p.R - row0));
     }
     plane = p.x_scales;
     plane_rows = p.R;
@@ -861,8 +867,8 @@ __global__ void __launch_bounds__(AtomCfg<FMT>::kThreads) sq_fp4_atoms_kernel(co
   }
   __syncthreads();
   uint32_t sign = 0;
-  const int kb = kb0 + warp;
-  if (kb < cnt) {
+  for (int stage = warp; stage < C::kStages && kb0 + stage < cnt; stage += C::kThreads / 32) {
+    const int kb = kb0 + stage;
     uint32_t w[4][W];
     const int valid = p.G - kb * Fp4<FMT>::kBytes;  // scale bytes of the row from the stage's first on
 #pragma unroll
@@ -870,7 +876,7 @@ __global__ void __launch_bounds__(AtomCfg<FMT>::kThreads) sq_fp4_atoms_kernel(co
       const int row = lane + 32 * r;
       uint32_t y[8] = {};
       const uintptr_t at = reinterpret_cast<uintptr_t>(first) + static_cast<int64_t>(row) * p.G + kb0 * Fp4<FMT>::kBytes;
-      const int from = static_cast<int>(at % 16) + warp * Fp4<FMT>::kBytes;  // in the row's pieces
+      const int from = static_cast<int>(at % 16) + stage * Fp4<FMT>::kBytes;  // in the row's pieces
       if (row < rows) {
         const uint4 *q = piece + row * C::kPieces + from / 16;
         const uint4 a = q[0];
@@ -1003,36 +1009,50 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
     const int mine = uniform(pair_tiles);
     int it = 0, s = 0;
     uint32_t ph = 1, go = 1;
-    for (int tc = 0; tc < mine; ++tc) {
+    struct Job {
+      int row, f, e, xa, wa, half, box;  // xa, wa: the atoms' rows of 512 bytes
+      uint32_t bytes;
+    };
+    auto job = [&](int tc) {
+      Job j;
       t.at(p, ex, first + tc * step);
-      const int half = uniform(((t.rows + 15) & ~15) / 2);  // tokens of a CTA, in the smallest box that holds them
+      j.half = uniform(((t.rows + 15) & ~15) / 2);  // tokens of a CTA, in the smallest box that holds them
       int box = 0;
-      while (box + 1 < kFp4PairBoxes && (8 << box) < half) ++box;
-      box = uniform(box);
-      const uint32_t bytes = C::kA + 3 * kBlock + (box + 1 < kFp4PairBoxes ? 8 << box : C::kNT / 2) * 128;
-      const int row = uniform(t.row0) + half * static_cast<int>(rank), f = uniform(t.f0) + 128 * static_cast<int>(rank), e = uniform(t.e);
-      int xa = uniform(t.token_tile) * cnt * 2 * W, wa = (2 * uniform(t.feature_tile) + static_cast<int>(rank)) * cnt * W;  // rows of 512 bytes
+      while (box + 1 < kFp4PairBoxes && (8 << box) < j.half) ++box;
+      j.box = uniform(box);
+      j.bytes = C::kA + 3 * kBlock + (j.box + 1 < kFp4PairBoxes ? 8 << j.box : C::kNT / 2) * 128;
+      j.row = uniform(t.row0) + j.half * static_cast<int>(rank);
+      j.f = uniform(t.f0) + 128 * static_cast<int>(rank);
+      j.e = uniform(t.e);
+      j.xa = uniform(t.token_tile) * cnt * 2 * W;
+      j.wa = (2 * uniform(t.feature_tile) + static_cast<int>(rank)) * cnt * W;
+      return j;
+    };
+    Job j = {};
+    if (mine > 0) j = job(0);
+    for (int tc = 0; tc < mine; ++tc) {
+      Job next = j;
       for (int kb = 0; kb < cnt; ++kb, ++it) {
+        if (kb == cnt - 1 && tc + 1 < mine) next = job(tc + 1);  // before the wait for a slot, in its shadow
         if (it >= S) go = warp_wait(&empty[s], ph, abort_flag, p.err) ? go : 0;
         const uint32_t at = ring + s * kStage;
         if (kb == 0) {
-          tile_n[s] = 2 * half;
+          tile_n[s] = 2 * j.half;
           __syncwarp();
         }
         const uint32_t count = smem_u32(own ? &landed[s] : &full[s]);
-        expect_tx_elect(counts ? go : 0, count, own ? bytes : 2 * bytes);
+        expect_tx_elect(counts ? go : 0, count, own ? j.bytes : 2 * j.bytes);
         const uint32_t bar = mapa_shared(count, own ? rank : 0);
-        tma_load_3d_pair_elect(go, at, &maps.w, bar, kb * (kDeep / 2), f, e);
-        tma_load_2d_pair_elect(go, at + C::kA, &maps.x[box], bar, kb * (kDeep / 2), row);
-        tma_load_2d_pair_elect(go, at + kSf, &maps.w_atoms, bar, 0, wa);
-        tma_load_2d_pair_elect(go, at + kSf + kBlock, &maps.x_atoms, bar, 0, xa);
-        wa += W;
-        xa += 2 * W;
+        tma_load_3d_pair_elect(go, at, &maps.w, bar, kb * (kDeep / 2), j.f, j.e);
+        tma_load_2d_pair_elect(go, at + C::kA, &maps.x[j.box], bar, kb * (kDeep / 2), j.row);
+        tma_load_2d_pair_elect(go, at + kSf, &maps.w_atoms, bar, 0, j.wa + kb * W);
+        tma_load_2d_pair_elect(go, at + kSf + kBlock, &maps.x_atoms, bar, 0, j.xa + kb * 2 * W);
         if (++s == S) {
           s = 0;
           ph ^= 1u;
         }
       }
+      j = next;
     }
     if (*abort_flag && (mend || rank == 0)) {
       uint64_t *bar = mend ? landed : full;

@@ -516,7 +516,7 @@ struct Fp4Args {
   int *err;
   int ftiles;                // feature tiles
   bool pair;                 // the pair kernel, else the few-token one
-  int tile_tokens;           // few: tokens of a tile (8 .. 128, a power of two)
+  int tile_tokens;           // few: tokens of a tile (8 .. 128, a power of two); pair: of a whole one of a dense product
   int64_t units;             // tiles, at most
   int splits;                // few: parts of the contraction (CTAs of a cluster)
   int stages;                // of the ring
@@ -531,38 +531,81 @@ struct Fp4Args {
 // epilogue and the experts' first tiles and rows.
 constexpr int fp4_few_stage(int tile_tokens) { return 128 * 128 + tile_tokens * 128 + 2 * 2048; }
 __host__ __device__ constexpr int fp4_atoms(int fmt) { return fmt == 0 ? 2048 : 1024; }  // bytes of 128 rows and a stage
+__host__ __device__ constexpr int fp4_atom_stages(int fmt) { return fmt == 0 ? 8 : 16; }  // of a CTA that writes atoms
 __host__ __device__ constexpr int fp4_pair_stage(int fmt) { return 128 * 128 + kFp4PairTokens / 2 * 128 + 3 * fp4_atoms(fmt); }
 constexpr size_t fp4_pair_smem(int fmt, int stages, int E) {
   return 1024 + static_cast<size_t>(stages) * fp4_pair_stage(fmt) + 8 * 2048 + (E > 0 ? 4 * (3 * E + 1) : 0);
 }
+// Tokens of a whole tile of a dense product. The launch lasts as long as its waves of tiles: 400 + 1.15 h
+// cycles a stage of a tile of h tokens (a stage's bytes at the rate that the L2 gives them, above the MMAs' 2 h).
+inline int fp4_pair_tokens(int64_t R, int64_t ftiles, int clusters) {
+  auto cost = [](int64_t h) { return h > 0 ? 400 + 1.15 * h : 0.0; };
+  double best = 0;
+  int tokens = kFp4PairTokens;
+  for (int h = kFp4PairTokens; h >= 96; h -= 16) {
+    const int64_t whole = R / h * ftiles, rest = R % h ? ftiles : 0, waves = (whole + clusters - 1) / clusters;
+    const int64_t left = waves * clusters - whole;
+    const double us = waves * cost(h) + (rest > left ? (rest - left + clusters - 1) / clusters * cost(R % h) : 0.0);
+    if (best == 0 || us < best) {
+      best = us;
+      tokens = h;
+    }
+  }
+  return tokens;
+}
 // Kernel, tiles and parts of a product on sm_count SMs: fills the last fields of p.
+//
+// The kernel is chosen by estimates of both in microseconds, for each expert's rows where there are experts. Both
+// sides, few-token against pair kernel with the launches ahead, measured, in us: 4096 x 4096 9 against 13 with 32
+// rows, 22 against 24 with 1024; 4096 x 14336 14 against 23 with 32, 35 against 30 with 384; 14336 x 4096 12
+// against 14 with 32, 32 against 24 with 384; 128 experts of 768 x 2048 18 against 33 with a row each, 43 against 45 with
+// 16, 118 against 91 with 256; of 2880 x 2880 82 against 85 with a row, 167 against 121 with 16, 398 against
+// 210 with 256.
 inline void fp4_plan(int fmt, int sm_count, Fp4Args &p) {
+  auto up = [](double x, double n) { return static_cast<double>(static_cast<int64_t>((x + n - 1) / n)); };
   const int64_t groups = p.offsets ? std::min<int64_t>(p.E, p.R) : 1;
-  p.pair = p.R >= 192 * groups;
+  const int cnt = (p.K + 255) / 256, clusters = sm_count / 2;
+  const int ftiles = (p.N + 127) / 128, pair_ftiles = (p.N + kFp4PairFeatures - 1) / kFp4PairFeatures;
+  int few_tokens = 8;
+  while (few_tokens < kFp4FewTokens && few_tokens * groups < p.R) few_tokens *= 2;
+  const int64_t few_units = (p.R + (few_tokens - 1) * groups) / few_tokens * ftiles;
+  // Parts: as many as leave every cluster an SM for each of its CTAs at once. A cluster's are of one of 8 groups of
+  // SMs, 18 or 20 of the 152 in each (18 clusters of 8 ran one after the other: 187 tokens against 1048 x
+  // 2720 18.8 us, 12.5 in 6 parts). The parts of many tokens take longer to add up than they save (256 against 1024 x
+  // 4096 22.6 us in 8 parts, 12.4 in 4; 64 the same in 8 and 4).
+  int splits = std::min(few_tokens <= 32 ? 8 : 4, cnt);
+  while (splits > 1 && few_units > 8 * ((sm_count / 8 - 1) / splits)) --splits;
+  const bool alone = few_units * splits <= sm_count;
+  // What the launches take: rounds of CTAs (two on an SM), or waves of pair tiles and, at least, the weight's way
+  // from memory. Tiles of ragged experts are half empty on average.
+  const int pair_tokens = p.offsets ? kFp4PairTokens : fp4_pair_tokens(p.R, pair_ftiles, clusters);
+  const double rows = static_cast<double>(p.R) / groups;
+  const double few_tiles = p.offsets ? (p.R + 0.5 * few_tokens * groups) / few_tokens * ftiles : few_units;
+  const double pair_tiles = (p.offsets ? (p.R + 0.5 * pair_tokens * groups) / pair_tokens : up(p.R, pair_tokens)) * pair_ftiles;
+  const double height = std::min<double>(pair_tokens, rows);
+  const double bytes = groups * static_cast<double>(p.N) * p.K * 0.56, atoms = (static_cast<double>(p.E) * p.N + p.R) * p.G * 2;
+  const double few_us = 2 + std::max(bytes / 5.5e6, (alone ? 1.0 : up(few_tiles, 2 * sm_count)) *
+                                                        (up(cnt, splits) * (alone ? 0.35 + 0.0022 * few_tokens : 0.75) + 2 + 0.02 * few_tokens));
+  const double pair_us = 9 + atoms / 3.5e6 + std::max(bytes / 5.5e6, up(pair_tiles, clusters) * (cnt * (0.2 + 0.0007 * height) + 0.5));
+  p.pair = pair_us < few_us || few_units > (int64_t(1) << 30);
   if (p.pair) {
-    p.ftiles = (p.N + kFp4PairFeatures - 1) / kFp4PairFeatures;
-    const int64_t token_tiles = (p.R + (kFp4PairTokens - 1) * groups) / kFp4PairTokens;
+    p.ftiles = pair_ftiles;
+    p.tile_tokens = pair_tokens;
+    const int64_t token_tiles = (p.R + (pair_tokens - 1) * groups) / pair_tokens;
     p.units = token_tiles * p.ftiles;
     p.token_blocks = static_cast<int>(2 * token_tiles);
-    p.atom_ctas = static_cast<int>((p.token_blocks + 2 * int64_t(p.E) * p.ftiles) * (((p.K + 255) / 256 + 7) / 8));
+    p.atom_ctas = static_cast<int>((p.token_blocks + 2 * int64_t(p.E) * p.ftiles) *
+                                   ((cnt + fp4_atom_stages(fmt) - 1) / fp4_atom_stages(fmt)));
     p.splits = 1;
     p.stages = 8;
     while (fp4_pair_smem(fmt, p.stages, p.offsets ? p.E : 0) > static_cast<size_t>(kFp4SmemMost)) --p.stages;
     return;
   }
-  p.ftiles = (p.N + 127) / 128;
-  p.tile_tokens = 8;
-  while (p.tile_tokens < kFp4FewTokens && p.tile_tokens * groups < p.R) p.tile_tokens *= 2;
-  p.units = ((p.R + (p.tile_tokens - 1) * groups) / p.tile_tokens) * p.ftiles;
-  const int cnt = (p.K + 255) / 256;
-  // Parts: as many as leave every cluster an SM for each of its CTAs at once. A cluster's are of one of 8 groups of
-  // SMs, 18 or 20 of the 152 in each (18 clusters of 8 ran one after the other: 187 tokens against 1048 x
-  // 2720 XX us, XX in 6 parts).
-  p.splits = std::min(8, cnt);
-  while (p.splits > 1 && p.units > 8 * ((sm_count / 8 - 1) / p.splits)) --p.splits;
-  const int stage = fp4_few_stage(p.tile_tokens);
-  const bool alone = p.units * p.splits <= sm_count;
-  p.stages = std::min(8, ((alone ? kFp4SmemAlone : kFp4SmemShared) - 1024) / stage);
+  p.ftiles = ftiles;
+  p.tile_tokens = few_tokens;
+  p.units = few_units;
+  p.splits = splits;
+  p.stages = std::min(8, ((alone ? kFp4SmemAlone : kFp4SmemShared) - 1024) / fp4_few_stage(few_tokens));
 }
 cudaError_t launch_fp4_few(int fmt, const Fp4Maps &maps, const Fp4Args &p, cudaStream_t stream);
 cudaError_t launch_fp4_pair(int fmt, const Fp4PairMaps &maps, const Fp4Args &p, int sm_count, cudaStream_t stream);

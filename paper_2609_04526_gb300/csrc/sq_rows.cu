@@ -16,7 +16,8 @@
 // distance is at least 2^-23 / Mu, Mu < 2 the significand of u, against half a step of 2^-24 / Mm
 // around m. The same holds for max / 6 and the borders of E4M3.
 //
-// Bound by memory (2 + 9/16 bytes a value, either way). A thread takes 16 values, 32 bytes of the row.
+// Bound by memory (2 + 9/16 bytes a value, either way): 32768 x 4096 NVFP4 quantised in 57 us, 6.0 TB/s, back
+// in 50 us, 6.9 TB/s. A thread takes 16 values, 32 bytes of the row.
 #include <type_traits>
 
 #include "sq_gemm_kernels.cuh"
@@ -264,7 +265,7 @@ __global__ void __launch_bounds__(kRowsThreads) sq_dequantize_kernel(const Quant
 }
 
 // Threads of a row. Many rows: as few as hold it in registers, each with kRowsHold chunks in flight (32768 x
-// 4096 quantised with 256 threads of one chunk 105 us, with 64 of four XX; rows back 69, XX). Few
+// 4096 quantised with 256 threads of one chunk 105 us, with 64 of four 57; back 69, 50). Few
 // rows: as many as it has chunks.
 template <typename F>
 cudaError_t by_width(int64_t R, int K, int sm_count, F f) {
