@@ -194,11 +194,11 @@ class QuantRows:
 
     def _c(self, device=None) -> _SqRows:
         """The C struct of rows whose tensors are dense and on `device` (the current one)."""
-        u8, scales = torch.uint8, (self.R, self.K // BLOCK[self.fmt])
-        codes = _arg(self.codes, "codes", u8, (self.R, self.K // 2), device)
-        dev = self.codes.device
-        return _SqRows(self.fmt, self.K, self.R, codes, _arg(self.scales, "scales", u8, scales, dev), float(self.ws2),
-                       None if self.row_ws2 is None else _arg(self.row_ws2, "row_ws2", torch.float32, (self.R,), dev))
+        fmt, R, K, codes, row = self.fmt, self.R, self.K, self.codes, self.row_ws2
+        u8, at = torch.uint8, _arg(codes, "codes", torch.uint8, (R, K // 2), device)
+        dev = codes.device
+        return _SqRows(fmt, K, R, at, _arg(self.scales, "scales", u8, (R, K // BLOCK[fmt]), dev), self.ws2,
+                       None if row is None else _arg(row, "row_ws2", torch.float32, (R,), dev))
 
 
 def _offsets(offsets, E: int):
@@ -727,7 +727,7 @@ class Handle:
             row = _empty(stream, R, dtype=torch.float32, device=dev) if own else None
             out = QuantRows(fmt, R, K, _empty(stream, R, K // 2, dtype=torch.uint8, device=dev),
                             _empty(stream, R, K // BLOCK[fmt], dtype=torch.uint8, device=dev), 1.0, row)
-        elif (out.fmt, out.R, out.K, out.row_ws2 is not None) != (fmt, R, K, own):
+        elif out.R != R or out.K != K or out.fmt != fmt or (out.row_ws2 is None) == own:
             raise ValueError(f"out holds {out.R} rows of {out.K} in format {out.fmt} with"
                              f"{'' if out.row_ws2 is not None else 'out'} row_ws2; {R} of {K} in format {fmt} "
                              f"with{'' if own else 'out'} it are written")

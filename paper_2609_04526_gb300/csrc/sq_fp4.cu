@@ -543,14 +543,12 @@ __global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
         atom_to_tmem_elect(sa + 4 * i, sd0 + so + i * (kAtom >> 4));
         atom_to_tmem_elect(sb + 4 * i, sd0 + so + ((kScales + i * kAtom) >> 4));
       }
-      const int steps = min(4, (p.K - (it0 + it) * kDeep + 63) / 64);
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
+      for (int kk = 0; kk < 4; ++kk) {  // past the end of K: codes and scales are zeros
         const int word = FMT == 0 ? kk : kk / 2;
         const uint32_t idesc = idesc_fp4<FMT>(C::kF, 0, FMT == 0 ? 0 : 2 * (kk & 1)) | (static_cast<uint32_t>(n8 >> 3) << 17);
-        if (kk < steps)
-          umma_fp4_elect<FMT>(tmem, ad0 + so + 2 * kk, bd0 + so + 2 * kk, idesc, sa + 4 * word, sb + 4 * word,
-                              (it > 0 || kk > 0) ? 1u : 0u);
+        umma_fp4_elect<FMT>(tmem, ad0 + so + 2 * kk, bd0 + so + 2 * kk, idesc, sa + 4 * word, sb + 4 * word,
+                            (it > 0 || kk > 0) ? 1u : 0u);
       }
       umma_commit_elect(&empty[s]);
       if (++s == S) {
@@ -1068,15 +1066,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
       const int mine = __reduce_max_sync(0xFFFFFFFFu, pair_tiles);
       int s = 0, it = 0;
       uint32_t ph = 0;
+      bool there = false;  // the stage was found complete while the one before was issued
       for (int tc = 0; tc < mine; ++tc) {
         const int ab = tc & 1;
         if (tc >= 2) warp_wait(&tempty[ab], (static_cast<uint32_t>(tc >> 1) & 1u) ^ 1u, abort_flag, p.err);
         // the tile's N comes with its first stage: looked up here it would bring its branches into the loop
-        warp_wait(&full[s], ph, abort_flag, p.err);
+        if (!there) warp_wait(&full[s], ph, abort_flag, p.err);
+        there = true;
         const uint32_t n16 = __reduce_max_sync(0xFFFFFFFFu, tile_n[s]);
         const uint32_t d = tmem + ab * C::kNT;
+        const uint32_t desc0 = idesc_fp4<FMT>(2 * 128, 0, 0) | n16 << 14, desc1 = idesc_fp4<FMT>(2 * 128, 0, FMT == 0 ? 0 : 2) | n16 << 14;
         for (int kb = 0; kb < cnt; ++kb, ++it) {
-          warp_wait(&full[s], ph, abort_flag, p.err);
+          if (!there) warp_wait(&full[s], ph, abort_flag, p.err);
           tc_fence_after();
           const uint32_t so = static_cast<uint32_t>(s * kStage) >> 4;
           const uint32_t sa = tmem + kScaleAt + (it & (kScaleBufs - 1)) * kScaleCols, sb = sa + 4 * W;
@@ -1086,20 +1087,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
             atom_to_tmem_pair_elect(sb + 8 * i, sd0 + so + ((kBlock + i * kAtom) >> 4));
             atom_to_tmem_pair_elect(sb + 8 * i + 4, sd0 + so + ((2 * kBlock + i * kAtom) >> 4));
           }
-          const int steps = min(4, (p.K - kb * kDeep + 63) / 64);
+          const bool found = mbar_test_wait(&full[s + 1 == S ? 0 : s + 1], s + 1 == S ? ph ^ 1u : ph);
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk) {
+          for (int kk = 0; kk < 4; ++kk) {  // past the end of K: codes and scales are zeros
             const int word = FMT == 0 ? kk : kk / 2;
-            constexpr uint32_t kDesc[2] = {idesc_fp4<FMT>(2 * 128, 0, 0), idesc_fp4<FMT>(2 * 128, 0, FMT == 0 ? 0 : 2)};
-            if (kk < steps)
-              umma_fp4_pair_elect<FMT>(d, ad0 + so + 2 * kk, bd0 + so + 2 * kk, kDesc[kk & 1] | n16 << 14, sa + 4 * word, sb + 8 * word,
-                                       (kb > 0 || kk > 0) ? 1u : 0u);
+            umma_fp4_pair_elect<FMT>(d, ad0 + so + 2 * kk, bd0 + so + 2 * kk, kk & 1 ? desc1 : desc0, sa + 4 * word, sb + 8 * word,
+                                     (kb > 0 || kk > 0) ? 1u : 0u);
           }
           commit_pair_mc_elect(&empty[s]);
           if (++s == S) {
             s = 0;
             ph ^= 1u;
           }
+          there = __all_sync(0xFFFFFFFFu, found);
         }
         commit_pair_mc_elect(&tfull[ab]);
       }
