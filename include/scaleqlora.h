@@ -44,7 +44,8 @@
  *    text is in sq_last_error(h). No exception or abort crosses the ABI.
  *  - A handle is not thread-safe; use one handle per host thread. The scratch a
  *    handle owns (a split scale gradient's partial planes; the adapter kernels'
- *    partial sums; the counts of a sort of more than 4096 slots; the head loss's
+ *    partial sums; the counts of a sort of more than 4096 slots; the scales of a large
+ *    4-bit product, laid out for the tensor cores; the head loss's
  *    rows, sums, exponentials and planes) is one buffer per kind and device:
  *    calls of one handle that use the same kind must run on one stream or be
  *    ordered by the caller. It is allocated,
@@ -531,7 +532,7 @@ sq_status sq_combine_grad(sq_handle h, int64_t T, int32_t k, int64_t D, int64_t 
 typedef struct {
   int32_t fmt;      /* sq_format                                                  */
   int32_t K;        /* values of a row, K % 32 == 0                               */
-  int64_t R;        /* rows, 0 <= R < 2^31                                        */
+  int64_t R;        /* rows, 0 <= R < 2^31 - 1024                                 */
   uint8_t *codes;   /* device [R, K/2]                                            */
   uint8_t *scales;  /* device [R, K/B]                                            */
   float ws2;        /* scale of all rows (1.0 with row_ws2)                       */
@@ -565,10 +566,11 @@ sq_status sq_dequantize(sq_handle h, const sq_rows *q, uint16_t *X, void *stream
  * bf16. Formats and K of w and x are the same; scale bytes may be negative (NVFP4). Products of scales outside
  * fp32's range are not kept apart (MXFP4: bytes whose sum is far from 254). w device weight as in sq_fwd;
  * Y device bf16 [x->R, N] (overwritten). The gradients are sq_bwd_dx and, of the scales, sq_scale_grad
- * with sq_dequantize's rows: the roundings of x pass them straight through. */
+ * with sq_dequantize's rows: the roundings of x pass them straight through. Large products use scratch of the handle,
+ * about as much as both scale planes have bytes. */
 sq_status sq_quant_fwd(sq_handle h, const sq_weight *w, const sq_rows *x, uint16_t *Y, void *stream);
 
-/* sq_quant_fwd of every expert over its own rows, in one launch that a graph can capture: offsets is a
+/* sq_quant_fwd of every expert over its own rows. A graph can capture it: offsets is a
  * DEVICE int64 array [E + 1] (sq_sort_tokens'), read when the launch runs and kept within [0, x->R];
  * E <= 1024. ws2 DEVICE fp32 [E] for NVFP4, NULL for MXFP4 (w->ws2 is not read).
  * Y device bf16 [x->R, N]: rows of no expert are left as they are. */

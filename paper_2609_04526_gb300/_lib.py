@@ -192,13 +192,20 @@ class QuantRows:
     ws2: float = 1.0
     row_ws2: Optional[torch.Tensor] = None
 
-    def _c(self, device=None) -> _SqRows:
-        """The C struct of rows whose tensors are dense and on `device` (the current one)."""
+    def _c(self, device=None, stream=None, staged=False) -> _SqRows:
+        """The C struct of rows whose tensors are dense and on `device` (the current one). staged: scale bytes
+        of a slice, which start anywhere, are copied on the call's stream."""
         fmt, R, K, codes, row = self.fmt, self.R, self.K, self.codes, self.row_ws2
         u8, at = torch.uint8, _arg(codes, "codes", torch.uint8, (R, K // 2), device)
-        dev = codes.device
-        return _SqRows(fmt, K, R, at, _arg(self.scales, "scales", u8, (R, K // BLOCK[fmt]), dev), self.ws2,
-                       None if row is None else _arg(row, "row_ws2", torch.float32, (R,), dev))
+        dev, keep = codes.device, None
+        scales = _arg(self.scales, "scales", u8, (R, K // BLOCK[fmt]), dev)
+        if staged and scales % 16:
+            keep = _staged(self.scales, stream)
+            scales = keep.data_ptr()
+        c = _SqRows(fmt, K, R, at, scales, self.ws2, None if row is None else _arg(row, "row_ws2", torch.float32, (R,), dev))
+        if keep is not None:
+            c.keep = keep  # until the call is queued
+        return c
 
 
 def _offsets(offsets, E: int):
@@ -743,7 +750,7 @@ class Handle:
         """4-bit rows back to bf16 [R, K]."""
         if X is None:
             X = _empty(stream, q.R, q.K, dtype=torch.bfloat16, device=q.codes.device)
-        c = q._c()
+        c = q._c(None, stream, True)
         self._check(self._L.sq_dequantize(self._h, ctypes.byref(c), _arg(X, "X", torch.bfloat16, (q.R, q.K), q.codes.device),
                                           _stream(stream)))
         return X
@@ -752,9 +759,11 @@ class Handle:
         """Y = X W^T with both operands in 4 bits (bf16 [R, N])."""
         if Y is None:
             Y = _empty(stream, q.R, w.N, dtype=torch.bfloat16, device=q.codes.device)
-        c, wc = q._c(), w._c()
+        c, dev = q._c(None, stream, True), q.codes.device
+        wc = _SqWeight(w.fmt, w.N, w.K, _arg(w.codes, "w.codes", torch.uint8, (w.N, w.K // 2), dev),
+                       _arg(w.scales, "w.scales", torch.uint8, (w.N, w.K // BLOCK[w.fmt]), dev), w.ws2)
         self._check(self._L.sq_quant_fwd(self._h, ctypes.byref(wc), ctypes.byref(c),
-                                       _arg(Y, "Y", torch.bfloat16, (q.R, w.N), q.codes.device), _stream(stream)))
+                                         _arg(Y, "Y", torch.bfloat16, (q.R, w.N), dev), _stream(stream)))
         return Y
 
     def sq_grouped_quant_fwd(self, w: GroupedWeight, offsets: torch.Tensor, q: QuantRows, Y: Optional[torch.Tensor] = None,
@@ -767,13 +776,14 @@ class Handle:
             Y = _empty(stream, q.R, w.N, dtype=torch.bfloat16, device=dev)
             with torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream))):
                 Y.zero_()
-        c = q._c()
+        c = q._c(None, stream, True)
         ws2 = None
         if w.fmt == NVFP4:
             if not isinstance(w.ws2, torch.Tensor):
                 raise ValueError("sq_grouped_quant_fwd reads w.ws2 on the device: a fp32 tensor [E]")
             ws2 = _arg(w.ws2, "w.ws2", torch.float32, (w.E,), dev)
-        wc = _SqGroupedWeight(w.fmt, w.E, w.N, w.K, _ptr(w.codes), _ptr(w.scales), None)
+        wc = _SqGroupedWeight(w.fmt, w.E, w.N, w.K, _arg(w.codes, "w.codes", torch.uint8, (w.E, w.N, w.K // 2), dev),
+                              _arg(w.scales, "w.scales", torch.uint8, (w.E, w.N, w.K // BLOCK[w.fmt]), dev), None)
         self._check(self._L.sq_grouped_quant_fwd(
             self._h, ctypes.byref(wc), ws2, _arg(offsets, "offsets", torch.int64, (w.E + 1,), dev), ctypes.byref(c),
             _arg(Y, "Y", torch.bfloat16, (q.R, w.N), dev), _stream(stream)))

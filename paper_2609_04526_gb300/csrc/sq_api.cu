@@ -547,7 +547,8 @@ sq_status check_head(sq_handle h, int64_t T, int64_t D, int64_t V) {
 sq_status check_rows(sq_handle h, const sq_rows *q) {
   if (!q) return fail(h, SQ_ERR_INVALID_ARG, "rows are NULL");
   SQ_TRY(check_ws2(h, q->fmt, q->ws2));
-  if (q->R < 0 || q->R > kMaxTokens) return fail(h, SQ_ERR_INVALID_ARG, "R=%lld out of range [0, 2^31)", (long long)q->R);
+  // TMA coordinates are int32, those of a tile's overhang among them
+  if (q->R < 0 || q->R > kMaxTokens - 1024) return fail(h, SQ_ERR_INVALID_ARG, "R=%lld out of range [0, 2^31 - 1024)", (long long)q->R);
   if (q->K <= 0 || q->K % 32 != 0 || q->K > kMaxDim)
     return fail(h, SQ_ERR_INVALID_ARG, "K=%d must be positive, a multiple of 32 and <= 2^24", q->K);
   if (q->row_ws2 && (q->fmt != SQ_NVFP4 || q->ws2 != 1.0f))

@@ -33,6 +33,10 @@ def test_many_rows_of_ragged_experts(h, fmt, counts, N, K):  # noqa: F811
     check_grouped(h, fmt, counts, N, K, seed=len(counts) + N)
 
 
+def test_many_rows_of_no_expert(h):  # noqa: F811
+    check_grouped(h, pkg.NVFP4, [0] * 6, 2056, 544, seed=2, tail=6000)
+
+
 def test_ragged_experts_with_negative_scales(h):  # noqa: F811
     check_grouped(h, pkg.NVFP4, [900, 0, 1, 224, 225, 448, 3200], 1032, 544, seed=3, signs=True)
 

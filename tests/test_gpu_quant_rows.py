@@ -96,3 +96,49 @@ def test_rows_by_slot(h, fmt, k):
     slot_of = torch.where(on, slots, -1)
     other = h.sq_quantize(fmt, h.sq_dispatch(X, row_of.view(T, k), slot_of))
     assert torch.equal(other.codes, q.codes) and torch.equal(other.scales, q.scales)
+
+
+@pytest.mark.parametrize("fmt", [pkg.NVFP4, pkg.MXFP4])
+@pytest.mark.parametrize("T", [3, 2000])
+def test_tensors_that_start_on_16_bytes(h, fmt, T):
+    """Rows read and written from a 16-byte boundary that is none of 32, and scale bytes of a slice."""
+    K = 544
+    g = torch.Generator(device="cuda").manual_seed(6)
+    room = torch.randn(T * K + 8, generator=g, device="cuda").bfloat16()
+    X = room[8:].view(T, K)
+    assert X.data_ptr() % 32 == 16
+    q = check(h, fmt, X)
+    back = torch.empty(T * K + 8, dtype=torch.bfloat16, device="cuda")[8:].view(T, K)
+    assert torch.equal(h.sq_dequantize(q, X=back), h.sq_dequantize(q))
+    part = pkg.QuantRows(fmt, T - 1, K, q.codes[1:], q.scales[1:], 1.0, None if q.row_ws2 is None else q.row_ws2[1:])
+    assert part.scales.data_ptr() % 16 != 0
+    assert torch.equal(h.sq_dequantize(part), h.sq_dequantize(q)[1:])
+    codes = torch.randint(0, 256, (136, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+    scales = torch.full((136, K // ref.BLOCK[fmt]), 0x38 if fmt == pkg.NVFP4 else 120, dtype=torch.uint8, device="cuda")
+    w = pkg.QuantWeight(fmt, 136, K, codes, scales, 1.0)
+    assert torch.equal(h.sq_quant_fwd(w, part), h.sq_quant_fwd(w, pkg.QuantRows(fmt, T - 1, K, part.codes, part.scales.clone(), 1.0, part.row_ws2)))
+
+
+def test_no_tokens_but_rows_by_slot(h):
+    q = h.sq_quantize(pkg.NVFP4, torch.empty(0, 64, dtype=torch.bfloat16, device="cuda"),
+                      slot_of=torch.zeros(5, dtype=torch.int32, device="cuda"), k=2)
+    assert (h.sq_dequantize(q) == 0).all() and (q.scales == 1).all()
+
+
+def test_tensors_elsewhere_are_refused(h):
+    X = torch.zeros(4, 64, dtype=torch.bfloat16, device="cuda")
+    q = h.sq_quantize(pkg.NVFP4, X)
+    host = pkg.QuantWeight(pkg.NVFP4, 16, 64, torch.zeros(16, 32, dtype=torch.uint8), torch.zeros(16, 4, dtype=torch.uint8), 1.0)
+    with pytest.raises(ValueError, match="w.codes"):
+        h.sq_quant_fwd(host, q)
+    with pytest.raises(ValueError, match="slot_of"):
+        h.sq_quantize(pkg.NVFP4, X, slot_of=torch.zeros(4, dtype=torch.int32))
+    gw = pkg.GroupedWeight(pkg.NVFP4, 2, 16, 64, torch.zeros(2, 16, 32, dtype=torch.uint8, device="cuda"),
+                           torch.zeros(2, 16, 4, dtype=torch.uint8, device="cuda"), [1.0, 1.0])
+    with pytest.raises(ValueError, match="w.ws2"):
+        h.sq_grouped_quant_fwd(gw, torch.zeros(3, dtype=torch.int64, device="cuda"), q)
+    gw.ws2 = torch.ones(2, device="cuda")
+    with pytest.raises(ValueError, match="offsets"):
+        h.sq_grouped_quant_fwd(gw, torch.zeros(3, dtype=torch.int64), q)
+    with pytest.raises(pkg.SQError, match="format"):
+        h.sq_quant_fwd(pkg.QuantWeight(pkg.MXFP4, 16, 64, gw.codes[0], torch.zeros(16, 2, dtype=torch.uint8, device="cuda"), 1.0), q)
