@@ -525,16 +525,17 @@ struct Fp4Args {
   uint4 *x_atoms, *w_atoms;
   int *negative;
   int token_blocks, atom_ctas;
+  int whole;                 // pair, dense: whole token tiles
 };
 // A few-token stage: codes of 128 features and a tile's tokens, scales of 128 rows of both. A pair stage: codes of 128
 // features and half the tokens, atoms of those features and of 256 tokens; behind the ring eight 2 KiB boxes of the
-// epilogue and the experts' first tiles and rows.
+// epilogue and the experts' tiles and rows.
 constexpr int fp4_few_stage(int tile_tokens) { return 128 * 128 + tile_tokens * 128 + 2 * 2048; }
 __host__ __device__ constexpr int fp4_atoms(int fmt) { return fmt == 0 ? 2048 : 1024; }  // bytes of 128 rows and a stage
 __host__ __device__ constexpr int fp4_atom_stages(int fmt) { return fmt == 0 ? 8 : 16; }  // of a CTA that writes atoms
 __host__ __device__ constexpr int fp4_pair_stage(int fmt) { return 128 * 128 + kFp4PairTokens / 2 * 128 + 3 * fp4_atoms(fmt); }
 constexpr size_t fp4_pair_smem(int fmt, int stages, int E) {
-  return 1024 + static_cast<size_t>(stages) * fp4_pair_stage(fmt) + 8 * 2048 + (E > 0 ? 4 * (3 * E + 1) : 0);
+  return 1024 + static_cast<size_t>(stages) * fp4_pair_stage(fmt) + 8 * 2048 + (E > 0 ? 4 * (4 * E + 1) : 0);
 }
 // Tokens of a whole tile of a dense product. The launch lasts as long as its waves of tiles: 400 + 1.15 h
 // cycles a stage of a tile of h tokens (a stage's bytes at the rate that the L2 gives them, above the MMAs' 2 h).
@@ -593,6 +594,7 @@ inline void fp4_plan(int fmt, int sm_count, Fp4Args &p) {
     p.tile_tokens = pair_tokens;
     const int64_t token_tiles = (p.R + (pair_tokens - 1) * groups) / pair_tokens;
     p.units = token_tiles * p.ftiles;
+    p.whole = static_cast<int>(p.R / pair_tokens);
     p.token_blocks = static_cast<int>(2 * token_tiles);
     p.atom_ctas = static_cast<int>((p.token_blocks + 2 * int64_t(p.E) * p.ftiles) *
                                    ((cnt + fp4_atom_stages(fmt) - 1) / fp4_atom_stages(fmt)));
