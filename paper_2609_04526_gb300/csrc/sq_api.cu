@@ -54,6 +54,7 @@ struct DeviceState {
   Scratch sort;          // per-CTA counts of the sort by expert
   Scratch head;          // packed rows, exponentials and partial planes of the head loss
   Scratch scales;        // scale atoms of the 4-bit products
+  sqi::Fp4Clusters clusters;  // of their few-token kernel, asked for by the first call
 };
 
 constexpr int64_t kMaxDim = int64_t(1) << 24;       // N, K limit
@@ -607,8 +608,9 @@ sq_status run_fp4(sq_handle h, int fmt, int E, int64_t N, int64_t K, const uint8
   p.offsets = offsets;
   p.out = Y;
   p.err = dev->err_word;
-  sqi::fp4_plan(fmt, dev->sm_count, p);
   cudaError_t e;
+  if (dev->clusters.alone[0] == 0 && (e = sqi::fp4_clusters(dev->clusters)) != cudaSuccess) return cuda_fail(h, e, "cluster query");
+  sqi::fp4_plan(fmt, dev->sm_count, dev->clusters, p);
   if (p.pair) {
     // scratch: the atoms of both operands' scales, one word of each CTA that writes them
     const int64_t cnt = (K + 255) / 256, block = cnt * sqi::fp4_atoms(fmt);

@@ -1269,6 +1269,29 @@ cudaError_t launch_few_fp4(const Fp4Maps &maps, const Fp4Args &p, cudaStream_t s
 
 }  // namespace
 
+cudaError_t fp4_clusters(Fp4Clusters &fit) {
+  const auto kernel = sq_fp4_few_kernel<0, true>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFp4SmemAlone);
+  if (e != cudaSuccess) return e;
+  for (int c = 8; c >= 1; --c) {
+    for (int two = 0; two < 2; ++two) {
+      cudaLaunchConfig_t cfg = {};
+      cfg.gridDim = dim3(8 * c, 1, 1);
+      cfg.blockDim = dim3(Fp4FewCfg::kThreads, 1, 1);
+      cfg.dynamicSmemBytes = two ? kFp4SmemShared : kFp4SmemAlone;
+      cudaLaunchAttribute attr[1];
+      attr[0].id = cudaLaunchAttributeClusterDimension;
+      attr[0].val.clusterDim.x = c;
+      attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+      cfg.attrs = attr;
+      cfg.numAttrs = 1;
+      if ((e = cudaOccupancyMaxActiveClusters(two ? &fit.shared[c] : &fit.alone[c], kernel, &cfg)) != cudaSuccess) return e;
+    }
+  }
+  fit.alone[0] = 1;
+  return cudaSuccess;
+}
+
 cudaError_t launch_fp4_few(int fmt, const Fp4Maps &maps, const Fp4Args &p, cudaStream_t stream) {
   const bool raw = p.G % kSpan == 0;
   if (fmt == 0) return raw ? launch_few_fp4<0, true>(maps, p, stream) : launch_few_fp4<0, false>(maps, p, stream);

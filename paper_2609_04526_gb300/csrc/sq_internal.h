@@ -554,6 +554,11 @@ inline int fp4_pair_tokens(int64_t R, int64_t ftiles, int clusters) {
   }
   return tokens;
 }
+// Clusters of 1 .. 8 CTAs of the few-token kernel that a device runs at once, a CTA alone on its SM or two on one.
+struct Fp4Clusters {
+  int alone[9], shared[9];  // alone[0] == 0: not asked yet
+};
+cudaError_t fp4_clusters(Fp4Clusters &fit);
 // Kernel, tiles and parts of a product on sm_count SMs: fills the last fields of p.
 //
 // The kernel is chosen by estimates of both in microseconds, for each expert's rows where there are experts. Both
@@ -562,7 +567,7 @@ inline int fp4_pair_tokens(int64_t R, int64_t ftiles, int clusters) {
 // against 14 with 32, 32 against 24 with 384; 128 experts of 768 x 2048 18 against 33 with a row each, 43 against 45 with
 // 16, 118 against 91 with 256; of 2880 x 2880 82 against 85 with a row, 167 against 121 with 16, 398 against
 // 210 with 256.
-inline void fp4_plan(int fmt, int sm_count, Fp4Args &p) {
+inline void fp4_plan(int fmt, int sm_count, const Fp4Clusters &fit, Fp4Args &p) {
   auto up = [](double x, double n) { return static_cast<double>(static_cast<int64_t>((x + n - 1) / n)); };
   const int64_t groups = p.offsets ? std::min<int64_t>(p.E, p.R) : 1;
   const int cnt = (p.K + 255) / 256, clusters = sm_count / 2;
@@ -570,13 +575,17 @@ inline void fp4_plan(int fmt, int sm_count, Fp4Args &p) {
   int few_tokens = 8;
   while (few_tokens < kFp4FewTokens && few_tokens * groups < p.R) few_tokens *= 2;
   const int64_t few_units = (p.R + (few_tokens - 1) * groups) / few_tokens * ftiles;
-  // Parts: as many as leave every cluster an SM for each of its CTAs at once. A cluster's are of one of 8 groups of
-  // SMs, 18 or 20 of the 152 in each (18 clusters of 8 ran one after the other: 187 tokens against 1048 x
-  // 2720 18.8 us, 12.5 in 6 parts). The parts of many tokens take longer to add up than they save (256 against 1024 x
-  // 4096 22.6 us in 8 parts, 12.4 in 4; 64 the same in 8 and 4).
+  // Parts: as many as let all clusters run at once, a CTA to an SM or, where a part has few stages, two. (18 clusters of
+  // 8, of which 15 fit: 187 tokens against 1048 x 2720 18.8 us, 12.5 in 6 parts; 48 of 3, of which 46 fit: a token
+  // through 8 experts of 768 x 2048 12.7, 8.0 in 2.) The parts of many tokens take longer to add up than they save (256
+  // against 1024 x 4096 22.6 us in 8 parts, 12.4 in 4; 64 the same in 8 and 4).
+  const int stage = fp4_few_stage(few_tokens), shared_stages = std::min(8, (kFp4SmemShared - 1024) / stage);
   int splits = std::min(few_tokens <= 32 ? 8 : 4, cnt);
-  while (splits > 1 && few_units > 8 * ((sm_count / 8 - 1) / splits)) --splits;
-  const bool alone = few_units * splits <= sm_count;
+  auto fits = [&](int s) {
+    return few_units <= fit.alone[s] || ((cnt + s - 1) / s <= shared_stages && few_units <= fit.shared[s]);
+  };
+  while (splits > 1 && !fits(splits)) --splits;
+  const bool alone = few_units <= fit.alone[splits];
   // What the launches take: rounds of CTAs (two on an SM), or waves of pair tiles and, at least, the weight's way
   // from memory. Tiles of ragged experts are half empty on average.
   const int pair_tokens = p.offsets ? kFp4PairTokens : fp4_pair_tokens(p.R, pair_ftiles, clusters);
@@ -607,7 +616,7 @@ inline void fp4_plan(int fmt, int sm_count, Fp4Args &p) {
   p.tile_tokens = few_tokens;
   p.units = few_units;
   p.splits = splits;
-  p.stages = std::min(8, ((alone ? kFp4SmemAlone : kFp4SmemShared) - 1024) / fp4_few_stage(few_tokens));
+  p.stages = alone ? std::min(8, (kFp4SmemAlone - 1024) / stage) : shared_stages;
 }
 cudaError_t launch_fp4_few(int fmt, const Fp4Maps &maps, const Fp4Args &p, cudaStream_t stream);
 cudaError_t launch_fp4_pair(int fmt, const Fp4PairMaps &maps, const Fp4Args &p, int sm_count, cudaStream_t stream);
