@@ -847,68 +847,98 @@ __global__ void __launch_bounds__(AtomCfg<FMT>::kThreads) sq_fp4_atoms_kernel(co
   }
   rows = min(rows, 128);
   const uint8_t *first = plane + row0 * p.G, *end = plane + plane_rows * p.G;
+  // Row r's bytes from stage kb0 on begin off(r) behind the 16-byte boundary `base`.
+  const uint8_t *base = first + kb0 * Fp4<FMT>::kBytes;
+  const int lead = static_cast<int>(reinterpret_cast<uintptr_t>(base) % 16);
+  base -= lead;
+  auto off = [&](int r) { return static_cast<int64_t>(r) * p.G + lead; };
   constexpr int kLoads = (128 * C::kPieces + C::kThreads - 1) / C::kThreads;
   uint4 x[kLoads];
 #pragma unroll
   for (int l = 0; l < kLoads; ++l) {
     const int i = threadIdx.x + l * C::kThreads, r = i / C::kPieces, j = i - r * C::kPieces;
-    const uint8_t *at = first + static_cast<int64_t>(r) * p.G + kb0 * Fp4<FMT>::kBytes;  // of the row's bytes
-    const uint8_t *from = at - reinterpret_cast<uintptr_t>(at) % 16 + 16 * j;
+    const uint8_t *from = base + (off(r) & ~int64_t(15)) + 16 * j;
     x[l] = make_uint4(0, 0, 0, 0);
     if (r < rows && from + 16 <= end) x[l] = *reinterpret_cast<const uint4 *>(from);
   }
+  if (rows > 0 && base + off(rows - 1) + C::kPieces * 16 > end) {  // the plane's last rows: it may end inside a piece
+#pragma unroll
+    for (int l = 0; l < kLoads; ++l) {
+      const int i = threadIdx.x + l * C::kThreads, r = i / C::kPieces, j = i - r * C::kPieces;
+      const uint8_t *from = base + (off(r) & ~int64_t(15)) + 16 * j;
+      if (r < rows && from < end && from + 16 > end) {
+        uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int b = 0; b < 16; ++b)
+          if (from + b < end) w[b / 4] |= static_cast<uint32_t>(from[b]) << (8 * (b % 4));
+        x[l] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+  }
 #pragma unroll
   for (int l = 0; l < kLoads; ++l) {
-    const int i = threadIdx.x + l * C::kThreads, r = i / C::kPieces, j = i - r * C::kPieces;
-    const uint8_t *at = first + static_cast<int64_t>(r) * p.G + kb0 * Fp4<FMT>::kBytes;
-    const uint8_t *from = at - reinterpret_cast<uintptr_t>(at) % 16 + 16 * j;
-    if (r < rows && from < end && from + 16 > end) {  // the plane ends inside
-      uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-      for (int b = 0; b < 16; ++b)
-        if (from + b < end) w[b / 4] |= static_cast<uint32_t>(from[b]) << (8 * (b % 4));
-      x[l] = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-    if (r < rows) piece[i] = x[l];
+    const int i = threadIdx.x + l * C::kThreads;
+    if (i < rows * C::kPieces) piece[i] = x[l];
   }
   __syncthreads();
   uint32_t sign = 0;
+  const bool level = p.G % 16 == 0;  // every row begins on a boundary
   for (int stage = warp; stage < C::kStages && kb0 + stage < cnt; stage += C::kThreads / 32) {
     const int kb = kb0 + stage;
     uint32_t w[4][W];
-    const int valid = p.G - kb * Fp4<FMT>::kBytes;  // scale bytes of the row from the stage's first on
+    if (level) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int row = lane + 32 * r;
-      uint32_t y[8] = {};
-      const uintptr_t at = reinterpret_cast<uintptr_t>(first) + static_cast<int64_t>(row) * p.G + kb0 * Fp4<FMT>::kBytes;
-      const int from = static_cast<int>(at % 16) + stage * Fp4<FMT>::kBytes;  // in the row's pieces
-      if (row < rows) {
-        const uint4 *q = piece + row * C::kPieces + from / 16;
-        const uint4 a = q[0];
-        y[0] = a.x, y[1] = a.y, y[2] = a.z, y[3] = a.w;
-        if (from % 16 + Fp4<FMT>::kBytes > 16) {
-          const uint4 b = q[1];
-          y[4] = b.x, y[5] = b.y, y[6] = b.z, y[7] = b.w;
+      for (int r = 0; r < 4; ++r) {
+        const int row = lane + 32 * r;
+        uint4 a = make_uint4(0, 0, 0, 0);
+        if (row < rows) a = piece[row * C::kPieces + stage * Fp4<FMT>::kBytes / 16];
+        if constexpr (FMT == 0) {
+          w[r][0] = a.x, w[r][1] = a.y, w[r][2] = a.z, w[r][3] = a.w;
+        } else {
+          w[r][0] = stage & 1 ? a.z : a.x, w[r][1] = stage & 1 ? a.w : a.y;
         }
       }
-      const int shift = from % 16;
-      if (shift & 8) {
+    } else {
 #pragma unroll
-        for (int i = 0; i < 6; ++i) y[i] = y[i + 2];
-      }
-      if (shift & 4) {
+      for (int r = 0; r < 4; ++r) {
+        const int row = lane + 32 * r;
+        uint32_t y[8] = {};
+        const int from = static_cast<int>(off(row) & 15) + stage * Fp4<FMT>::kBytes, shift = from % 16;  // in the row's pieces
+        if (row < rows) {
+          const uint4 *q = piece + row * C::kPieces + from / 16;
+          const uint4 a = q[0];
+          y[0] = a.x, y[1] = a.y, y[2] = a.z, y[3] = a.w;
+          if (shift + Fp4<FMT>::kBytes > 16) {
+            const uint4 b = q[1];
+            y[4] = b.x, y[5] = b.y, y[6] = b.z, y[7] = b.w;
+          }
+        }
+        if (shift & 8) {
 #pragma unroll
-        for (int i = 0; i < 5; ++i) y[i] = y[i + 1];
+          for (int i = 0; i < 6; ++i) y[i] = y[i + 2];
+        }
+        if (shift & 4) {
+#pragma unroll
+          for (int i = 0; i < 5; ++i) y[i] = y[i + 1];
+        }
+#pragma unroll
+        for (int i = 0; i < W; ++i) w[r][i] = __funnelshift_r(y[i], y[i + 1], 8 * (shift & 3));
       }
+    }
+    const int valid = p.G - kb * Fp4<FMT>::kBytes;  // scale bytes of a row from the stage's first on
+    if (valid < Fp4<FMT>::kBytes) {
 #pragma unroll
       for (int i = 0; i < W; ++i) {
         const int b = valid - 4 * i;
-        w[r][i] = __funnelshift_r(y[i], y[i + 1], 8 * (shift & 3));
-        if (b < 4) w[r][i] = b <= 0 ? 0u : w[r][i] & ((1u << (8 * b)) - 1);
-        sign |= w[r][i];
+        const uint32_t keep = b >= 4 ? 0xFFFFFFFFu : b <= 0 ? 0u : (1u << (8 * b)) - 1;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) w[r][i] &= keep;
       }
     }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int i = 0; i < W; ++i) sign |= w[r][i];
     uint4 *dst = out + static_cast<int64_t>(kb) * (W * kAtom / 16) * (tokens ? 2 : 1) + lane;
 #pragma unroll
     for (int i = 0; i < W; ++i) dst[i * (kAtom / 16)] = make_uint4(w[0][i], w[1][i], w[2][i], w[3][i]);
