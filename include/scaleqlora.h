@@ -571,7 +571,8 @@ sq_status sq_dequantize(sq_handle h, const sq_rows *q, uint16_t *X, void *stream
 sq_status sq_quant_fwd(sq_handle h, const sq_weight *w, const sq_rows *x, uint16_t *Y, void *stream);
 
 /* sq_quant_fwd of every expert over its own rows. A graph can capture it: offsets is a
- * DEVICE int64 array [E + 1] (sq_sort_tokens'), read when the launch runs and kept within [0, x->R];
+ * DEVICE int64 array [E + 1] (sq_sort_tokens'), ascending, read when the launch runs and kept within [0, x->R]
+ * (where they descend, the rows that experts share have any one's products or none, and no others are written);
  * E <= 1024. ws2 DEVICE fp32 [E] for NVFP4, NULL for MXFP4 (w->ws2 is not read).
  * Y device bf16 [x->R, N]: rows of no expert are left as they are. */
 sq_status sq_grouped_quant_fwd(sq_handle h, const sq_grouped_weight *w, const float *ws2, const int64_t *offsets,

@@ -403,7 +403,7 @@ __device__ __forceinline__ void find_tile(const Fp4Args &p, TileSearch &f, int t
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
       const int v = __shfl_up_sync(0xFFFFFFFFu, upto, d);
-      if (lane >= d) upto += v;
+      if (lane >= d) upto = min(upto + v, (1 << 30) - 1);  // offsets that descend may give every expert all rows
     }
     if (tt >= upto - mine && tt < upto) {  // one lane, or none
       int left = tt - (upto - mine);
@@ -1013,6 +1013,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
     }
     __syncthreads();
     if (warp == 0) {
+      // never more tiles than the launch has room for, which only offsets that descend ask for
+      const int most = p.token_blocks >> 1;
       int before = 0;
       for (int e0 = 0; e0 < p.E; e0 += 32) {
         int v = e0 + lane < p.E ? ex.tiles[e0 + lane + 1] : 0;
@@ -1021,8 +1023,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
           const int u = __shfl_up_sync(0xFFFFFFFFu, v, d);
           if (lane >= d) v += u;
         }
-        if (e0 + lane < p.E) ex.tiles[e0 + lane + 1] = before + v;
-        before += __shfl_sync(0xFFFFFFFFu, v, 31);
+        if (e0 + lane < p.E) ex.tiles[e0 + lane + 1] = min(before + v, most);
+        before = min(before + __shfl_sync(0xFFFFFFFFu, v, 31), most);
       }
       if (lane == 0) ex.tiles[0] = 0;
     }

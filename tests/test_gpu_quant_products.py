@@ -183,3 +183,21 @@ def test_not_finite_rows_stay_alone(h, fmt, R):
     h.sq_sync()
     keep = torch.arange(R, device="cuda") != R // 2
     assert torch.equal(Y[keep], clean[keep]) and torch.isnan(Y[~keep].float()).all()
+
+
+@pytest.mark.parametrize("R, N, K", [(30, 136, 544), (6000, 2056, 544)])
+def test_offsets_that_descend_write_no_other_rows(h, R, N, K):
+    """Experts that claim the same rows, more of them than the launch has tiles for: rows outside every claim keep
+    what they held, and the call after it is right."""
+    g = torch.Generator(device="cuda").manual_seed(17)
+    E, lo, hi = 24, 5, R - 7
+    codes, scales = weight(g, pkg.NVFP4, (E, N), K)
+    q = rows(g, h, pkg.NVFP4, R, K)
+    w = pkg.GroupedWeight(pkg.NVFP4, E, N, K, codes, scales, torch.ones(E, device="cuda"))
+    buf = torch.full((R + 512, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    offsets = torch.tensor([hi if e % 2 else lo for e in range(E + 1)], dtype=torch.int64, device="cuda")
+    h.sq_grouped_quant_fwd(w, offsets, q, Y=buf[256:R + 256])
+    h.sq_sync()
+    assert (buf[:256 + lo] == 7).all() and (buf[256 + hi:] == 7).all()
+    assert torch.isfinite(buf.float()).all()
+    check_grouped(h, pkg.NVFP4, [R // 3, 0, R - R // 3], N, K, seed=18)
