@@ -738,28 +738,29 @@ class Handle:
             raise ValueError(f"out holds {out.R} rows of {out.K} in format {out.fmt} with"
                              f"{'' if out.row_ws2 is not None else 'out'} row_ws2; {R} of {K} in format {fmt} "
                              f"with{'' if own else 'out'} it are written")
-        out.ws2 = 1.0 if ws2 is None else float(ws2)
         x = _arg(X, "X", torch.bfloat16, (T, K))
         c = out._c(dev)
+        c.ws2 = 1.0 if ws2 is None else ws2
         self._check(self._L.sq_quantize(
             self._h, ctypes.byref(c), T, int(k), x,
             None if slot_of is None else _arg(slot_of, "slot_of", torch.int32, (R,), dev), _stream(stream)))
+        out.ws2 = 1.0 if ws2 is None else float(ws2)  # a refused call leaves out as it was
         return out
 
     def sq_dequantize(self, q: QuantRows, X: Optional[torch.Tensor] = None, stream=None):
         """4-bit rows back to bf16 [R, K]."""
+        c = q._c(None, stream, True)
         if X is None:
             X = _empty(stream, q.R, q.K, dtype=torch.bfloat16, device=q.codes.device)
-        c = q._c(None, stream, True)
         self._check(self._L.sq_dequantize(self._h, ctypes.byref(c), _arg(X, "X", torch.bfloat16, (q.R, q.K), q.codes.device),
                                           _stream(stream)))
         return X
 
     def sq_quant_fwd(self, w: QuantWeight, q: QuantRows, Y: Optional[torch.Tensor] = None, stream=None):
         """Y = X W^T with both operands in 4 bits (bf16 [R, N])."""
-        if Y is None:
-            Y = _empty(stream, q.R, w.N, dtype=torch.bfloat16, device=q.codes.device)
         c, dev = q._c(None, stream, True), q.codes.device
+        if Y is None:
+            Y = _empty(stream, q.R, w.N, dtype=torch.bfloat16, device=dev)
         wc = _SqWeight(w.fmt, w.N, w.K, _arg(w.codes, "w.codes", torch.uint8, (w.N, w.K // 2), dev),
                        _arg(w.scales, "w.scales", torch.uint8, (w.N, w.K // BLOCK[w.fmt]), dev), w.ws2)
         self._check(self._L.sq_quant_fwd(self._h, ctypes.byref(wc), ctypes.byref(c),
@@ -771,12 +772,11 @@ class Handle:
         """Y rows offsets[e]..offsets[e+1]-1 = X rows of expert e times W_e^T, both in 4 bits; the other rows of
         Y are left as they are (zeros of a new one). offsets int64 [E + 1] and, NVFP4, w.ws2 fp32 [E] are on the
         device: nothing comes back to the host, and a graph can capture the call."""
-        dev = q.codes.device
+        c, dev = q._c(None, stream, True), q.codes.device
         if Y is None:
             Y = _empty(stream, q.R, w.N, dtype=torch.bfloat16, device=dev)
             with torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream))):
                 Y.zero_()
-        c = q._c(None, stream, True)
         ws2 = None
         if w.fmt == NVFP4:
             if not isinstance(w.ws2, torch.Tensor):

@@ -92,3 +92,24 @@ def test_binding_checks_tensors(h):
         h.sq_dequantize(pkg.QuantRows(0, 4, 64, u8(4, 64), u8(4, 4)), X=X)
     with pytest.raises(ValueError, match="CUDA device"):
         h.sq_dequantize(q, X=X)
+
+
+def test_refused_rows_keep_their_scale(h):
+    """A refused quantisation into existing rows leaves their scale as it was: their codes are still under it."""
+    u8 = lambda *s: torch.zeros(*s, dtype=torch.uint8)  # noqa: E731
+    q = pkg.QuantRows(0, 4, 64, u8(4, 32), u8(4, 4), 0.25)
+    with pytest.raises(ValueError, match="X must be"):
+        h.sq_quantize(0, torch.zeros(4, 64), ws2=0.5, out=q)
+    assert q.ws2 == 0.25
+
+
+def test_products_refuse_rows_elsewhere_before_their_output_is_made(h):
+    u8 = lambda *s: torch.zeros(*s, dtype=torch.uint8)  # noqa: E731
+    q = pkg.QuantRows(1, 4, 64, u8(4, 32), u8(4, 2))
+    with pytest.raises(ValueError, match="CUDA device"):
+        h.sq_dequantize(q)
+    with pytest.raises(ValueError, match="CUDA device"):
+        h.sq_quant_fwd(pkg.QuantWeight(1, 16, 64, u8(16, 32), u8(16, 2), 1.0), q)
+    with pytest.raises(ValueError, match="CUDA device"):
+        h.sq_grouped_quant_fwd(pkg.GroupedWeight(1, 2, 16, 64, u8(2, 16, 32), u8(2, 16, 2), None),
+                               torch.zeros(3, dtype=torch.int64), q)
