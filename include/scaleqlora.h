@@ -44,7 +44,8 @@
  *    text is in sq_last_error(h). No exception or abort crosses the ABI.
  *  - A handle is not thread-safe; use one handle per host thread. The scratch a
  *    handle owns (a split scale gradient's partial planes; the adapter kernels'
- *    partial sums; the counts of a sort of more than 4096 slots; the scales of a large
+ *    partial sums; the counts of a sort of more than 4096 slots; the 4-bit rows of many tokens
+ *    that sq_quantize takes by slot; the scales of a large
  *    4-bit product, laid out for the tensor cores; the head loss's
  *    rows, sums, exponentials and planes) is one buffer per kind and device:
  *    calls of one handle that use the same kind must run on one stream or be
@@ -551,7 +552,9 @@ typedef struct {
  * and has no part in its row's own scale.
  * X device bf16 [T, K]. slot_of device int32 [R] or NULL: NULL, R == T and row r is X[r]; else row r
  * is X[slot_of[r] / k] (1 <= k <= 32, T * k < 2^31), the row that sq_dispatch would copy there, and a row whose slot
- * is outside [0, T * k) is a row of zeros. Results of a row do not depend on the rows beside it. */
+ * is outside [0, T * k) is a row of zeros. Where many rows are of few tokens, the tokens are quantised once,
+ * into scratch of the handle (T + 1 rows), and copied; a graph capture that finds no scratch quantises row by
+ * row. Results of a row do not depend on the rows beside it, nor on this. */
 sq_status sq_quantize(sq_handle h, const sq_rows *q, int64_t T, int32_t k, const uint16_t *X, const int32_t *slot_of,
                       void *stream);
 

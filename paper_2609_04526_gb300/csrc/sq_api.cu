@@ -53,6 +53,7 @@ struct DeviceState {
   int64_t *plane_acc;    // counter accumulators of the multi-plane calls (zero between calls)
   Scratch sort;          // per-CTA counts of the sort by expert
   Scratch head;          // packed rows, exponentials and partial planes of the head loss
+  Scratch tokens;        // 4-bit rows of the tokens that several rows are copied from
   Scratch scales;        // scale atoms of the 4-bit products
   sqi::Fp4Clusters clusters;  // of their few-token kernel, asked for by the first call
 };
@@ -949,6 +950,7 @@ sq_status sq_destroy(sq_handle h) {
       free_scratch(d.partial);
       free_scratch(d.sort);
       free_scratch(d.head);
+      free_scratch(d.tokens);
       free_scratch(d.scales);
       for (auto &t : d.tables) {
         if (t.done) {
@@ -1794,7 +1796,32 @@ sq_status sq_quantize(sq_handle h, const sq_rows *q, int64_t T, int32_t k, const
   a.k = slot_of ? k : 1;
   a.slots = T * a.k;
   a.wide = reinterpret_cast<uintptr_t>(X) % 32 == 0;
-  cudaError_t e = sqi::launch_quantize(q->fmt, a, dev->sm_count, static_cast<cudaStream_t>(stream));
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (slot_of && sqi::quantize_tokens_first(q->fmt, a.R, T, a.K)) {
+    // the tokens' 4-bit rows, a row of zeros behind them, then each row a copy of its token's
+    const int64_t rows = T + 1, G = a.K / block_of(q->fmt);
+    const int64_t codes = rows * (a.K / 2), scales = (rows * G + 15) / 16 * 16;
+    const size_t bytes = static_cast<size_t>(codes + scales + 4 * rows);
+    cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+    cudaError_t e = bytes <= dev->tokens.bytes ? cudaSuccess : cudaStreamIsCapturing(st, &cap);
+    if (e != cudaSuccess) return cuda_fail(h, e, "cudaStreamIsCapturing");
+    if (cap == cudaStreamCaptureStatusNone) {  // a capture that finds no scratch takes the other way to the same rows
+      SQ_TRY(ensure_scratch(h, dev->tokens, bytes, st, "a quantisation by slot"));
+      sqi::QuantArgs t = a;
+      t.R = rows;
+      t.codes = static_cast<uint8_t *>(dev->tokens.ptr);
+      t.scales = t.codes + codes;
+      t.row_ws2 = a.row_ws2 ? reinterpret_cast<float *>(t.scales + scales) : nullptr;
+      t.slot_of = nullptr;
+      t.k = 1;
+      t.slots = T;
+      e = sqi::launch_quantize(q->fmt, t, dev->sm_count, st);
+      if (e == cudaSuccess) e = sqi::launch_spread(q->fmt, a, t, st);
+      if (e != cudaSuccess) return cuda_fail(h, e, "quantisation launch");
+      return SQ_OK;
+    }
+  }
+  cudaError_t e = sqi::launch_quantize(q->fmt, a, dev->sm_count, st);
   if (e != cudaSuccess) return cuda_fail(h, e, "quantisation launch");
   return SQ_OK;
   SQ_GUARD_END

@@ -146,9 +146,9 @@ __global__ void __launch_bounds__(kRowsThreads) sq_quantize_kernel(const QuantAr
   dependency_start();
   const int t = threadIdx.x % TPR, chunks = a.K / 16;
   const int64_t r = static_cast<int64_t>(blockIdx.x) * (kRowsThreads / TPR) + threadIdx.x / TPR;
-  int64_t src = r < a.R ? r : -1;
-  if (a.slot_of && src >= 0) {
-    const int slot = a.slot_of[r];
+  int64_t src = r < a.R && r < a.slots ? r : -1;
+  if (a.slot_of) {
+    const int slot = r < a.R ? a.slot_of[r] : -1;
     src = slot >= 0 && slot < a.slots ? slot / a.k : -1;
   }
   const uint16_t *x = a.X + (src < 0 ? 0 : src) * a.K;
@@ -209,6 +209,44 @@ __global__ void __launch_bounds__(kRowsThreads) sq_quantize_kernel(const QuantAr
     if ((c0 += kSpan) >= chunks) break;
     load(c0);
   }
+}
+
+// Rows by slot from the 4-bit rows of the tokens (the last of those: zeros), a warp each: 16384 rows of 2048 values
+// NVFP4 (19 MB, from the L2) in 6 us. Codes move in 16-byte pieces;
+// scale bytes too, or, where a row is not whole pieces, in the units that divide it. All of a row's loads are
+// in flight before its first store.
+template <typename Unit>
+__global__ void __launch_bounds__(kRowsThreads) sq_spread_kernel(const QuantArgs a, const QuantArgs tokens, const int G) {
+  dependency_wait();
+  dependency_start();
+  const int lane = threadIdx.x % 32;
+  const int64_t r = static_cast<int64_t>(blockIdx.x) * (kRowsThreads / 32) + threadIdx.x / 32;
+  if (r >= a.R) return;
+  const int slot = a.slot_of[r];
+  const int64_t t = slot >= 0 && slot < a.slots ? slot / a.k : tokens.R - 1;
+  const int pieces = a.K / 32, units = G / static_cast<int>(sizeof(Unit));
+  const uint4 *codes = reinterpret_cast<const uint4 *>(tokens.codes + t * (a.K / 2));
+  uint4 *codes_to = reinterpret_cast<uint4 *>(a.codes + r * (a.K / 2));
+  const Unit *scales = reinterpret_cast<const Unit *>(tokens.scales + t * G);
+  Unit *scales_to = reinterpret_cast<Unit *>(a.scales + r * G);
+  const float row = a.row_ws2 ? tokens.row_ws2[t] : 0.f;
+  for (int c0 = lane; c0 < max(pieces, units); c0 += 32 * kRowsHold) {
+    uint4 v[kRowsHold];
+    Unit s[kRowsHold];
+#pragma unroll
+    for (int j = 0; j < kRowsHold; ++j) {
+      const int c = c0 + 32 * j;
+      if (c < pieces) v[j] = codes[c];
+      if (c < units) s[j] = scales[c];
+    }
+#pragma unroll
+    for (int j = 0; j < kRowsHold; ++j) {
+      const int c = c0 + 32 * j;
+      if (c < pieces) codes_to[c] = v[j];
+      if (c < units) scales_to[c] = s[j];
+    }
+  }
+  if (a.row_ws2 && lane == 0) a.row_ws2[r] = row;
 }
 
 // 16 values of a thread: code x block scale exactly in bf16, times the row's scale in fp32, rounded once.
@@ -287,6 +325,15 @@ cudaError_t launch_quantize(int fmt, const QuantArgs &a, int sm_count, cudaStrea
                                     : sq_quantize_kernel<0, false, kTpr>;
     return launch_after(kernel, row_ctas(a.R, kTpr), kRowsThreads, 0, stream, a);
   });
+}
+
+cudaError_t launch_spread(int fmt, const QuantArgs &a, const QuantArgs &tokens, cudaStream_t stream) {
+  const int G = a.K / (fmt == 0 ? 16 : 32);
+  const auto kernel = G % 16 == 0  ? sq_spread_kernel<uint4>
+                      : G % 4 == 0 ? sq_spread_kernel<uint32_t>
+                      : G % 2 == 0 ? sq_spread_kernel<uint16_t>
+                                   : sq_spread_kernel<uint8_t>;
+  return launch_after(kernel, row_ctas(a.R, 32), kRowsThreads, 0, stream, a, tokens, G);
 }
 
 cudaError_t launch_dequantize(int fmt, const QuantArgs &a, uint16_t *X, int sm_count, cudaStream_t stream) {

@@ -192,3 +192,77 @@ def test_a_step_that_keeps_its_rows_in_four_bits(h, fmt, R, N, K):  # noqa: F811
     assert abs(change - step * grad[n, b].double()) <= slack
     others = torch.arange(N, device="cuda") != n
     assert torch.equal(before[:, others], after[:, others])
+
+
+def by_slot(h, fmt, X, slots, k, ws2=None):
+    """The rows of `slots` out of X, zeros where there is none, quantised as rows of their own."""
+    on = (slots >= 0) & (slots < X.shape[0] * k)
+    rows_ = torch.zeros(slots.shape[0], X.shape[1], dtype=X.dtype, device=X.device)
+    rows_[on] = X[(slots[on] // k).long()]
+    return h.sq_quantize(fmt, rows_, ws2)
+
+
+def alike(a, b):
+    return (torch.equal(a.codes, b.codes) and torch.equal(a.scales, b.scales) and a.ws2 == b.ws2
+            and (a.row_ws2 is None) == (b.row_ws2 is None) and (a.row_ws2 is None or torch.equal(a.row_ws2, b.row_ws2)))
+
+
+@pytest.mark.parametrize("fmt, ws2", [(pkg.NVFP4, None), (pkg.NVFP4, 0.0031), (pkg.MXFP4, None)])
+@pytest.mark.parametrize("T, K, k", [(2000, 2048, 8), (2000, 2880, 8), (1500, 2912, 8), (4000, 1056, 8), (5001, 20512, 3), (300, 32, 1)])
+def test_many_rows_of_few_tokens(h, fmt, ws2, T, K, k):  # noqa: F811
+    g = torch.Generator(device="cuda").manual_seed(T + K)
+    X = torch.randn(T, K, generator=g, device="cuda").bfloat16()
+    X[3, 17], X[4, 20] = float("nan"), float("-inf")
+    slots = torch.randperm(T * k, generator=g, device="cuda").int()[:T * k - 5].clone()
+    slots[:4] = torch.tensor([-1, T * k, -(1 << 31), (1 << 31) - 1], dtype=torch.int32, device="cuda")
+    slots[50:60] = 3 * k  # a row of one token again and again, one that is not finite
+    slots[60:70] = T * k - 1
+    q = h.sq_quantize(fmt, X, ws2, slot_of=slots, k=k)
+    h.sq_sync()
+    assert alike(q, by_slot(h, fmt, X, slots, k, ws2))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_many_rows_of_no_token(h, fmt):  # noqa: F811
+    slots = torch.zeros(1000000, dtype=torch.int32, device="cuda")
+    X = torch.empty(0, 64, dtype=torch.bfloat16, device="cuda")
+    q = h.sq_quantize(fmt, X, slot_of=slots, k=4)
+    h.sq_sync()
+    assert alike(q, by_slot(h, fmt, X, torch.full_like(slots, -1), 4))
+
+
+def test_rows_by_slot_captured_with_scratch_and_without():
+    """A first call inside a capture, a captured one that has scratch, and one whose scratch grew since: the same rows,
+    of what the tokens and slots are when it runs."""
+    h2 = pkg.Handle()
+    g = torch.Generator(device="cuda").manual_seed(21)
+    T, K, k = 2000, 2880, 8
+    X = torch.randn(T, K, generator=g, device="cuda").bfloat16()
+    slots = torch.randperm(T * k, generator=g, device="cuda").int()
+    h2.sq_quantize(pkg.NVFP4, X[:1])  # the device is set up
+    graphs, outs = [], []
+    side = torch.cuda.Stream()
+    for i in range(2):
+        with torch.cuda.stream(side):
+            out = pkg.QuantRows(pkg.NVFP4, T * k, K, torch.zeros(T * k, K // 2, dtype=torch.uint8, device="cuda"),
+                                torch.zeros(T * k, K // 16, dtype=torch.uint8, device="cuda"), 1.0, torch.zeros(T * k, device="cuda"))
+            if i:
+                h2.sq_quantize(pkg.NVFP4, X, slot_of=slots, k=k)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            h2.sq_quantize(pkg.NVFP4, X, slot_of=slots, k=k, out=out)
+        graphs.append(graph)
+        outs.append(out)
+    big = torch.randn(2 * T, K, generator=g, device="cuda").bfloat16()
+    more = torch.randperm(2 * T * k, generator=g, device="cuda").int()
+    assert alike(h2.sq_quantize(pkg.NVFP4, big, slot_of=more, k=k), by_slot(h2, pkg.NVFP4, big, more, k))
+    for _ in range(2):
+        X.copy_(torch.randn(T, K, generator=g, device="cuda").bfloat16())
+        slots.copy_(torch.randperm(T * k, generator=g, device="cuda").int())
+        want = by_slot(h2, pkg.NVFP4, X, slots, k)
+        for graph, out in zip(graphs, outs):
+            graph.replay()
+            torch.cuda.synchronize()
+            assert alike(out, want)
+    h2.sq_sync()
