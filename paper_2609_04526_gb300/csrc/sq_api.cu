@@ -614,7 +614,7 @@ sq_status run_fp4(sq_handle h, int fmt, int E, int64_t N, int64_t K, const uint8
   sqi::fp4_plan(fmt, dev->sm_count, dev->clusters, p);
   if (p.pair) {
     // scratch: the atoms of both operands' scales, one word of each CTA that writes them
-    const int64_t cnt = (K + 255) / 256, block = cnt * sqi::fp4_atoms(fmt);
+    const int64_t block = int64_t(p.depth) * p.slices * sqi::fp4_atoms(fmt);
     const int64_t x_bytes = p.token_blocks * block, w_bytes = 2 * int64_t(E) * p.ftiles * block;
     SQ_TRY(ensure_scratch(h, dev->scales, static_cast<size_t>(x_bytes + w_bytes + 4 * int64_t(p.atom_ctas)), stream,
                           "a 4-bit product of this size"));
@@ -623,7 +623,7 @@ sq_status run_fp4(sq_handle h, int fmt, int E, int64_t N, int64_t K, const uint8
     p.w_atoms = reinterpret_cast<uint4 *>(base + x_bytes);
     p.negative = reinterpret_cast<int *>(base + x_bytes + w_bytes);
     sqi::Fp4PairMaps m;
-    const uint32_t atoms = sqi::fp4_atoms(fmt) / 512;
+    const uint32_t atoms = p.slices * sqi::fp4_atoms(fmt) / 512;
     SQ_TRY(make_experts_map(h, &m.w, codes, K / 2, N, E, 128, 128, CU_TENSOR_MAP_SWIZZLE_128B));
     for (int i = 0; i < sqi::kFp4PairBoxes; ++i)
       SQ_TRY(make_map(h, &m.x[i], x->codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, K / 2, x->R, 128,

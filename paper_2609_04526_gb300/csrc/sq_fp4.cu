@@ -19,7 +19,8 @@
 // zero) goes in as its magnitude, and the codes of its block, in shared memory by then, change their
 // signs.
 //
-// A stage is 256 deep: 128 bytes of codes and 16 (NVFP4) or 8 (MXFP4) scale bytes of each row.
+// A stage is a slice of the contraction 256 deep, 128 bytes of codes and 16 (NVFP4) or 8 (MXFP4) scale bytes of
+// each row, or, in dense products of the pair kernel, two slices.
 #include <type_traits>
 
 #include "sq_gemm_kernels.cuh"
@@ -28,7 +29,7 @@
 namespace sqi {
 namespace {
 
-constexpr int kDeep = 256;                 // contraction of a stage
+constexpr int kDeep = 256;                 // contraction of a slice
 constexpr int kAtom = 512;                 // bytes of a scale atom
 template <int FMT>
 struct Fp4 {
@@ -696,7 +697,7 @@ struct Fp4PairCfg {
   static constexpr int kThreads = 32 * (kMendWarp + 1);
   static constexpr int kA = 128 * 128, kB = kNT / 2 * 128;
   static constexpr int kMaxStages = 8;
-  static constexpr int kBox = 32 * 64;  // 32 tokens x 32 features of an epilogue warp
+  static constexpr int kBox = 16 * 64;  // 16 tokens x 32 features of an epilogue warp
 };
 static_assert(Fp4PairCfg::kNT <= 256 && Fp4PairCfg::kNT % 32 == 0 && 2 * Fp4PairCfg::kNT + 48 <= 512,
               "two accumulators and a stage's scales in tensor memory");
@@ -796,7 +797,7 @@ struct Fp4Tile {
   }
 };
 
-// Atoms of 128 rows and 8 (NVFP4) or 16 stages per CTA. The rows' bytes come in whole 16-byte pieces to shared memory
+// Atoms of 128 rows and 8 (NVFP4) or 16 slices (called stages here) per CTA; slices behind the end of K are zeros. The rows' bytes come in whole 16-byte pieces to shared memory
 // (lines apart by an odd number of pieces, free of bank conflicts) and are cut out from there.
 template <int FMT>
 struct AtomCfg {
@@ -812,7 +813,7 @@ __global__ void __launch_bounds__(AtomCfg<FMT>::kThreads) sq_fp4_atoms_kernel(co
   constexpr int W = Fp4<FMT>::kWords;
   __shared__ uint4 piece[128 * C::kPieces];
   static_assert(sizeof(TileSearch) <= sizeof(piece), "the search's memory");
-  const int cnt = (p.K + kDeep - 1) / kDeep, groups = (cnt + C::kStages - 1) / C::kStages;
+  const int cnt = p.depth * p.slices, groups = (cnt + C::kStages - 1) / C::kStages;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int block = static_cast<int>(blockIdx.x) / groups;
   const int kb0 = (static_cast<int>(blockIdx.x) - block * groups) * C::kStages;
@@ -949,14 +950,15 @@ __global__ void __launch_bounds__(AtomCfg<FMT>::kThreads) sq_fp4_atoms_kernel(co
   }
 }
 
-template <int FMT>
+// H: slices of a stage.
+template <int FMT, int H>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads, 1)
     sq_fp4_pair_kernel(const __grid_constant__ Fp4PairMaps maps, const Fp4Args p) {
   using C = Fp4PairCfg;
   constexpr int W = Fp4<FMT>::kWords;
   constexpr int kBlock = W * kAtom;  // the atoms of 128 rows and a stage
-  constexpr int kSf = C::kA + C::kB, kStage = fp4_pair_stage(FMT);
-  static_assert(kSf + 3 * kBlock <= kStage && kStage % 1024 == 0, "a stage");
+  constexpr int kBs = H * C::kA, kSf = kBs + H * C::kB, kXs = kSf + H * kBlock, kStage = fp4_pair_stage(FMT, H);
+  static_assert(kXs + 2 * H * kBlock <= kStage && kStage % 1024 == 0, "a stage");
   constexpr int kScaleCols = 12 * W, kScaleAt = 2 * C::kNT, kScaleBufs = (512 - kScaleAt) / kScaleCols >= 2 ? 2 : 1;
   extern __shared__ uint8_t fp4_smem_raw[];
   uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(fp4_smem_raw) + 1023) & ~uintptr_t(1023));
@@ -1034,7 +1036,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
   cluster_sync_all();
   tc_fence_after();
   const uint32_t tmem = tmem_slot, ring = smem_u32(smem);
-  const int cnt = (p.K + kDeep - 1) / kDeep;
+  const int cnt = p.depth;
   const int first = static_cast<int>(blockIdx.x >> 1), step = static_cast<int>(gridDim.x >> 1);
   const int tiles = p.offsets ? ex.tiles[p.E] * p.ftiles : static_cast<int>(p.units);
   const int pair_tiles = first < tiles ? (tiles - first + step - 1) / step : 0;  // of this pair
@@ -1060,12 +1062,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
       int box = 0;
       while (box + 1 < kFp4PairBoxes && (8 << box) < j.half) ++box;
       j.box = uniform(box);
-      j.bytes = C::kA + 3 * kBlock + (j.box + 1 < kFp4PairBoxes ? 8 << j.box : C::kNT / 2) * 128;
+      j.bytes = H * (C::kA + 3 * kBlock + (j.box + 1 < kFp4PairBoxes ? 8 << j.box : C::kNT / 2) * 128);
       j.row = uniform(t.row0) + j.half * static_cast<int>(rank);
       j.f = uniform(t.f0) + 128 * static_cast<int>(rank);
       j.e = uniform(t.e);
-      j.xa = uniform(t.token_tile) * cnt * 2 * W;
-      j.wa = (2 * uniform(t.feature_tile) + static_cast<int>(rank)) * cnt * W;
+      j.xa = uniform(t.token_tile) * cnt * H * 2 * W;
+      j.wa = (2 * uniform(t.feature_tile) + static_cast<int>(rank)) * cnt * H * W;
       return j;
     };
     Job j = {};
@@ -1083,10 +1085,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
         const uint32_t count = smem_u32(own ? &landed[s] : &full[s]);
         expect_tx_elect(counts ? go : 0, count, own ? j.bytes : 2 * j.bytes);
         const uint32_t bar = mapa_shared(count, own ? rank : 0);
-        tma_load_3d_pair_elect(go, at, &maps.w, bar, kb * (kDeep / 2), j.f, j.e);
-        tma_load_2d_pair_elect(go, at + C::kA, &maps.x[j.box], bar, kb * (kDeep / 2), j.row);
-        tma_load_2d_pair_elect(go, at + kSf, &maps.w_atoms, bar, 0, j.wa + kb * W);
-        tma_load_2d_pair_elect(go, at + kSf + kBlock, &maps.x_atoms, bar, 0, j.xa + kb * 2 * W);
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+          tma_load_3d_pair_elect(go, at + h * C::kA, &maps.w, bar, (kb * H + h) * (kDeep / 2), j.f, j.e);
+          tma_load_2d_pair_elect(go, at + kBs + h * C::kB, &maps.x[j.box], bar, (kb * H + h) * (kDeep / 2), j.row);
+        }
+        tma_load_2d_pair_elect(go, at + kSf, &maps.w_atoms, bar, 0, j.wa + kb * H * W);
+        tma_load_2d_pair_elect(go, at + kXs, &maps.x_atoms, bar, 0, j.xa + kb * H * 2 * W);
         if (++s == S) {
           s = 0;
           ph ^= 1u;
@@ -1101,7 +1106,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
   } else if (warp == C::kMmaWarp) {
     // ------------------------------------------------------ MMA issuer (leader; one elected lane)
     if (rank == 0) {
-      const uint64_t ad0 = smem_desc_sw128(ring, 16, 1024), bd0 = smem_desc_sw128(ring + C::kA, 16, 1024);
+      const uint64_t ad0 = smem_desc_sw128(ring, 16, 1024), bd0 = smem_desc_sw128(ring + kBs, 16, 1024);
       const uint64_t sd0 = atom_desc(ring + kSf);
       // Behind the MMA that they run the tensor cores hold about two more: between the last MMA of a stage and
       // the first of the next there are 250 cycles for the barriers, the commit and the atoms.
@@ -1122,19 +1127,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
           if (!there) warp_wait(&full[s], ph, abort_flag, p.err);
           tc_fence_after();
           const uint32_t so = static_cast<uint32_t>(s * kStage) >> 4;
-          const uint32_t sa = tmem + kScaleAt + (it & (kScaleBufs - 1)) * kScaleCols, sb = sa + 4 * W;
+          bool found = false;
 #pragma unroll
-          for (int i = 0; i < W; ++i) {
-            atom_to_tmem_pair_elect(sa + 4 * i, sd0 + so + i * (kAtom >> 4));
-            atom_to_tmem_pair_elect(sb + 8 * i, sd0 + so + ((kBlock + i * kAtom) >> 4));
-            atom_to_tmem_pair_elect(sb + 8 * i + 4, sd0 + so + ((2 * kBlock + i * kAtom) >> 4));
-          }
-          const bool found = mbar_test_wait(&full[s + 1 == S ? 0 : s + 1], s + 1 == S ? ph ^ 1u : ph);
+          for (int h = 0; h < H; ++h) {
+            const uint32_t sa = tmem + kScaleAt + ((it * H + h) & (kScaleBufs - 1)) * kScaleCols, sb = sa + 4 * W;
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk) {  // past the end of K: codes and scales are zeros
-            const int word = FMT == 0 ? kk : kk / 2;
-            umma_fp4_pair_elect<FMT>(d, ad0 + so + 2 * kk, bd0 + so + 2 * kk, kk & 1 ? desc1 : desc0, sa + 4 * word, sb + 8 * word,
-                                     (kb > 0 || kk > 0) ? 1u : 0u);
+            for (int i = 0; i < W; ++i) {
+              atom_to_tmem_pair_elect(sa + 4 * i, sd0 + so + ((h * kBlock + i * kAtom) >> 4));
+              atom_to_tmem_pair_elect(sb + 8 * i, sd0 + so + (((H + 2 * h) * kBlock + i * kAtom) >> 4));
+              atom_to_tmem_pair_elect(sb + 8 * i + 4, sd0 + so + (((H + 2 * h + 1) * kBlock + i * kAtom) >> 4));
+            }
+            if (h == H - 1) found = mbar_test_wait(&full[s + 1 == S ? 0 : s + 1], s + 1 == S ? ph ^ 1u : ph);
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {  // past the end of K: codes and scales are zeros
+              const int word = FMT == 0 ? kk : kk / 2;
+              umma_fp4_pair_elect<FMT>(d, ad0 + so + (h * C::kA >> 4) + 2 * kk, bd0 + so + (h * C::kB >> 4) + 2 * kk,
+                                       kk & 1 ? desc1 : desc0, sa + 4 * word, sb + 8 * word, (kb > 0 || h > 0 || kk > 0) ? 1u : 0u);
+            }
           }
           commit_pair_mc_elect(&empty[s]);
           if (++s == S) {
@@ -1159,16 +1168,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
           if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(&landed[s], ph, abort_flag, p.err)))) break;
           const uint32_t at = ring + s * kStage;
           const int half = ((t.rows + 15) & ~15) / 2;
-          for (int i = 0; i < 3 * W; ++i) {  // atom i % W of the features, the first 128 and the other tokens
-            const int of = i / W, word = i % W;
-            const int lift = of == 0 ? 0 : 128 * (of - 1) - half * static_cast<int>(rank), rows = of == 0 ? 128 : half;
-            const uint32_t line = at + kSf + i * kAtom + lane * 16;
+          for (int i = 0; i < 3 * W * H; ++i) {  // an atom of the features, then of the first 128 and the other tokens of a slice
+            const bool of_w = i < W * H;
+            const int j = of_w ? i : i - W * H, word = j % W, h = of_w ? j / W : j / (2 * W);
+            const int lift = of_w ? 0 : 128 * (j / W % 2) - half * static_cast<int>(rank), rows = of_w ? 128 : half;
+            const uint32_t line = at + kSf + i * kAtom + lane * 16, codes = at + (of_w ? h * C::kA : kBs + h * C::kB);
             const uint4 x = lds128(line);
             uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
               const int row = lane + 32 * r + lift;
-              if ((w[r] & 0x80808080u) && row >= 0 && row < rows) flip_codes(at + (of == 0 ? 0 : C::kA), row, word, w[r]);
+              if ((w[r] & 0x80808080u) && row >= 0 && row < rows) flip_codes(codes, row, word, w[r]);
             }
             st_shared_v4(line, w[0] & 0x7F7F7F7Fu, w[1] & 0x7F7F7F7Fu, w[2] & 0x7F7F7F7Fu, w[3] & 0x7F7F7F7Fu);
           }
@@ -1233,22 +1243,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
           o[i / 2 + 1] = *reinterpret_cast<const uint32_t *>(&b);
         }
         const bool odd = lane & 1;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {  // even lanes keep tokens 0-15, odd ones 16-31, of both features
-          const uint32_t other = __shfl_xor_sync(0xFFFFFFFFu, odd ? o[i] : o[i + 8], 1);
-          const uint32_t even_f = odd ? other : o[i], odd_f = odd ? o[i + 8] : other;
-          const uint32_t at = box + 2 * i * 128 + (odd ? 64 : 0) + (lane >> 1) * 4;
-          asm volatile("st.shared.b32 [%0], %1;" ::"r"(at), "r"(prmt(even_f, odd_f, 0x5410u)) : "memory");
-          asm volatile("st.shared.b32 [%0], %1;" ::"r"(at + 128), "r"(prmt(even_f, odd_f, 0x7632u)) : "memory");
-        }
-        __syncwarp();
         const int f = t.f0 + 128 * static_cast<int>(rank) + 32 * quad + 8 * (lane & 3);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int line = 4 * q + (lane >> 3), r = line + (lane & 4 ? 16 : 0);  // eight lanes a line
-          const uint4 y = lds128(box + line * 128 + (lane & 7) * 16);
-          if (r < left && f < p.N)
-            *reinterpret_cast<uint4 *>(p.out + (static_cast<int64_t>(t.row0) + 32 * g + r) * p.N + f) = y;
+        for (int part = 0; part < 2; ++part) {
+          if (part > 0) __syncwarp();  // the box is read
+#pragma unroll
+          for (int i = 4 * part; i < 4 * part + 4; ++i) {  // even lanes keep tokens 0-15, odd ones 16-31, of both features
+            const uint32_t other = __shfl_xor_sync(0xFFFFFFFFu, odd ? o[i] : o[i + 8], 1);
+            const uint32_t even_f = odd ? other : o[i], odd_f = odd ? o[i + 8] : other;
+            const uint32_t at = box + (2 * i - 8 * part) * 128 + (odd ? 64 : 0) + (lane >> 1) * 4;
+            asm volatile("st.shared.b32 [%0], %1;" ::"r"(at), "r"(prmt(even_f, odd_f, 0x5410u)) : "memory");
+            asm volatile("st.shared.b32 [%0], %1;" ::"r"(at + 128), "r"(prmt(even_f, odd_f, 0x7632u)) : "memory");
+          }
+          __syncwarp();
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            const int line = 4 * q + (lane >> 3), r = 8 * part + line + (lane & 4 ? 16 : 0);  // eight lanes a line
+            const uint4 y = lds128(box + line * 128 + (lane & 7) * 16);
+            if (r < left && f < p.N)
+              *reinterpret_cast<uint4 *>(p.out + (static_cast<int64_t>(t.row0) + 32 * g + r) * p.N + f) = y;
+          }
         }
       }
     }
@@ -1330,18 +1344,19 @@ cudaError_t launch_fp4_few(int fmt, const Fp4Maps &maps, const Fp4Args &p, cudaS
   return raw ? launch_few_fp4<1, true>(maps, p, stream) : launch_few_fp4<1, false>(maps, p, stream);
 }
 
-template <int FMT>
+template <int FMT, int H>
 static cudaError_t launch_pair(const Fp4PairMaps &maps, const Fp4Args &p, int sm_count, cudaStream_t stream) {
   static int done_mask = 0;
   const cudaError_t e = launch_after(sq_fp4_atoms_kernel<FMT>, static_cast<unsigned>(p.atom_ctas), AtomCfg<FMT>::kThreads, 0, stream, p);
   if (e != cudaSuccess) return e;
   const int clusters = static_cast<int>(std::min<int64_t>(p.units, sm_count / 2));
-  return launch_kernel<const Fp4PairMaps>(sq_fp4_pair_kernel<FMT>, done_mask, kFp4SmemMost, 2u * clusters, Fp4PairCfg::kThreads,
-                                          fp4_pair_smem(FMT, p.stages, p.offsets ? p.E : 0), 1, stream, maps, p);
+  return launch_kernel<const Fp4PairMaps>(sq_fp4_pair_kernel<FMT, H>, done_mask, kFp4SmemMost, 2u * clusters, Fp4PairCfg::kThreads,
+                                          fp4_pair_smem(FMT, H, p.stages, p.offsets ? p.E : 0), 1, stream, maps, p);
 }
 
 cudaError_t launch_fp4_pair(int fmt, const Fp4PairMaps &maps, const Fp4Args &p, int sm_count, cudaStream_t stream) {
-  return fmt == 0 ? launch_pair<0>(maps, p, sm_count, stream) : launch_pair<1>(maps, p, sm_count, stream);
+  if (fmt == 0) return p.slices == 1 ? launch_pair<0, 1>(maps, p, sm_count, stream) : launch_pair<0, 2>(maps, p, sm_count, stream);
+  return p.slices == 1 ? launch_pair<1, 1>(maps, p, sm_count, stream) : launch_pair<1, 2>(maps, p, sm_count, stream);
 }
 
 }  // namespace sqi

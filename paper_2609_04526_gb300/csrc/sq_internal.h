@@ -530,26 +530,30 @@ struct Fp4Args {
   int64_t units;             // tiles, at most
   int splits;                // few: parts of the contraction (CTAs of a cluster)
   int stages;                // of the ring
-  // pair: atoms of the scales, [token tile][stage][2] and [block of 128 features][stage], and per CTA that writes them
+  // pair: atoms of the scales, [token tile][slice][2] and [block of 128 features][slice], and per CTA that writes them
   // whether it met a negative one
   uint4 *x_atoms, *w_atoms;
   int *negative;
   int token_blocks, atom_ctas;
+  int slices;                // pair: of 256 of the contraction, in a stage: 1 or 2
+  int depth;                 // pair: stages of the contraction
   int whole;                 // pair, dense: whole token tiles
 };
-// A few-token stage: codes of 128 features and a tile's tokens, scales of 128 rows of both. A pair stage: codes of 128
-// features and half the tokens, atoms of those features and of 256 tokens; behind the ring eight 2 KiB boxes of the
-// epilogue and the experts' tiles and rows.
+// A few-token stage: codes of 128 features and a tile's tokens, scales of 128 rows of both. A slice
+// of a pair stage: codes of 128 features and half the tokens, atoms of those features and of 256 tokens; behind the
+// ring eight 1 KiB boxes of the epilogue and the experts' tiles and rows.
 constexpr int fp4_few_stage(int tile_tokens) { return 128 * 128 + tile_tokens * 128 + 2 * 2048; }
-__host__ __device__ constexpr int fp4_atoms(int fmt) { return fmt == 0 ? 2048 : 1024; }  // bytes of 128 rows and a stage
-__host__ __device__ constexpr int fp4_atom_stages(int fmt) { return fmt == 0 ? 8 : 16; }  // of a CTA that writes atoms
-__host__ __device__ constexpr int fp4_pair_stage(int fmt) { return 128 * 128 + kFp4PairTokens / 2 * 128 + 3 * fp4_atoms(fmt); }
-constexpr size_t fp4_pair_smem(int fmt, int stages, int E) {
-  return 1024 + static_cast<size_t>(stages) * fp4_pair_stage(fmt) + 8 * 2048 + (E > 0 ? 4 * (4 * E + 1) : 0);
+__host__ __device__ constexpr int fp4_atoms(int fmt) { return fmt == 0 ? 2048 : 1024; }  // bytes of 128 rows and a slice
+__host__ __device__ constexpr int fp4_atom_stages(int fmt) { return fmt == 0 ? 8 : 16; }  // slices of a CTA that writes atoms
+__host__ __device__ constexpr int fp4_pair_stage(int fmt, int slices) {
+  return slices * (128 * 128 + kFp4PairTokens / 2 * 128 + 3 * fp4_atoms(fmt));
+}
+constexpr size_t fp4_pair_smem(int fmt, int slices, int stages, int E) {
+  return 1024 + static_cast<size_t>(stages) * fp4_pair_stage(fmt, slices) + 8 * 1024 + (E > 0 ? 4 * (4 * E + 1) : 0);
 }
 // Tokens of a whole tile of a dense product. The launch lasts as long as its waves of tiles, 400 + 1.15 h
 // cycles a stage of a tile of h tokens (fitted; the MMAs alone take 2 h). 2048 tokens against 4096 x 14336 in tiles of 224
-// and a last one of 32: 73 us with their quantisation, 79 in ten of 208.
+// and a last one of 32: 70 us with their quantisation, 73 in ten of 208.
 inline int fp4_pair_tokens(int64_t R, int64_t ftiles, int clusters) {
   auto cost = [](int64_t h) { return h > 0 ? 400 + 1.15 * h : 0.0; };
   double best = 0;
@@ -573,11 +577,11 @@ cudaError_t fp4_clusters(Fp4Clusters &fit);
 // Kernel, tiles and parts of a product on sm_count SMs: fills the last fields of p.
 //
 // The kernel is chosen by estimates of both in microseconds, for each expert's rows where there are experts. Both
-// sides, few-token against pair kernel with the launches ahead, measured, in us: 4096 x 4096 9 against 13 with 32
-// rows, 22 against 24 with 1024; 4096 x 14336 14 against 23 with 32, 35 against 30 with 384; 14336 x 4096 12
-// against 14 with 32, 32 against 24 with 384; 128 experts of 768 x 2048 18 against 33 with a row each, 43 against 45 with
-// 16, 118 against 91 with 256; of 2880 x 2880 82 against 85 with a row, 167 against 121 with 16, 398 against
-// 210 with 256.
+// sides, few-token against pair kernel with the launches ahead, measured with NVFP4, in us: 4096 x 4096 8 against 11
+// with 32 rows, 21 against 22 with 1024; 4096 x 14336 13 against 20 with 32, 29 against 27 with 384; 14336 x 4096 11
+// against 13 with 32, 31 against 23 with 384; 128 experts of 768 x 2048 17 against 26 with a row each, 41 against 38 with
+// 16 (the estimates' worst miss), 104 against 75 with 256; of 2880 x 2880 (MXFP4) 79 against 84 with a row, 154
+// against 120 with 16, 380 against 193 with 256.
 inline void fp4_plan(int fmt, int sm_count, const Fp4Clusters &fit, Fp4Args &p) {
   auto up = [](double x, double n) { return static_cast<double>(static_cast<int64_t>((x + n - 1) / n)); };
   const int64_t groups = p.offsets ? std::min<int64_t>(p.E, p.R) : 1;
@@ -615,12 +619,18 @@ inline void fp4_plan(int fmt, int sm_count, const Fp4Clusters &fit, Fp4Args &p) 
     const int64_t token_tiles = (p.R + (pair_tokens - 1) * groups) / pair_tokens;
     p.units = token_tiles * p.ftiles;
     p.whole = static_cast<int>(p.R / pair_tokens);
+    // Two slices a stage halve the waits, commits and loads (one, two; us with the tokens' quantisation: 16384 x 14336
+    // x 4096 NVFP4 352, 340, 2048 x 4096 x 14336 74, 70, MXFP4 68, 63). Experts' narrow tiles wait for their loads and
+    // want the finer ring (8111 tokens to four of 128 of 2880 x 2880 200, 204). An odd slice behind K is computed as
+    // zeros: not where it would be more than a 17th of all.
+    p.slices = !p.offsets && (cnt % 2 == 0 || cnt > 16) ? 2 : 1;
+    p.depth = (cnt + p.slices - 1) / p.slices;
     p.token_blocks = static_cast<int>(2 * token_tiles);
     p.atom_ctas = static_cast<int>((p.token_blocks + 2 * int64_t(p.E) * p.ftiles) *
-                                   ((cnt + fp4_atom_stages(fmt) - 1) / fp4_atom_stages(fmt)));
+                                   ((p.depth * p.slices + fp4_atom_stages(fmt) - 1) / fp4_atom_stages(fmt)));
     p.splits = 1;
     p.stages = 8;
-    while (fp4_pair_smem(fmt, p.stages, p.offsets ? p.E : 0) > static_cast<size_t>(kFp4SmemMost)) --p.stages;
+    while (fp4_pair_smem(fmt, p.slices, p.stages, p.offsets ? p.E : 0) > static_cast<size_t>(kFp4SmemMost)) --p.stages;
     return;
   }
   p.ftiles = ftiles;
