@@ -570,7 +570,7 @@ sq_status sq_dequantize(sq_handle h, const sq_rows *q, uint16_t *X, void *stream
  * fp32's range are not kept apart (MXFP4: bytes whose sum is far from 254). w device weight as in sq_fwd;
  * Y device bf16 [x->R, N] (overwritten). The gradients are sq_bwd_dx and, of the scales, sq_scale_grad
  * with sq_dequantize's rows: the roundings of x pass them straight through. Large products use scratch of the
- * handle: the scale bytes of 256 rows for each tile of up to 224 (of an expert's) and for each 256 features. */
+ * handle: the scale bytes of 256 rows for each tile of 96 to 256 (of an expert's: up to 224) and for each 256 features. */
 sq_status sq_quant_fwd(sq_handle h, const sq_weight *w, const sq_rows *x, uint16_t *Y, void *stream);
 
 /* sq_quant_fwd of every expert over its own rows. A graph can capture it: offsets is a

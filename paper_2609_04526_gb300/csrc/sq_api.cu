@@ -627,7 +627,7 @@ sq_status run_fp4(sq_handle h, int fmt, int E, int64_t N, int64_t K, const uint8
     SQ_TRY(make_experts_map(h, &m.w, codes, K / 2, N, E, 128, 128, CU_TENSOR_MAP_SWIZZLE_128B));
     for (int i = 0; i < sqi::kFp4PairBoxes; ++i)
       SQ_TRY(make_map(h, &m.x[i], x->codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, K / 2, x->R, 128,
-                      i + 1 < sqi::kFp4PairBoxes ? 8u << i : sqi::kFp4PairTokens / 2u, CU_TENSOR_MAP_SWIZZLE_128B));
+                      static_cast<uint32_t>(sqi::fp4_pair_box(i)), CU_TENSOR_MAP_SWIZZLE_128B));
     SQ_TRY(make_map(h, &m.x_atoms, p.x_atoms, CU_TENSOR_MAP_DATA_TYPE_UINT32, 4, 128, x_bytes / 512, 128, 2 * atoms,
                     CU_TENSOR_MAP_SWIZZLE_NONE));
     SQ_TRY(make_map(h, &m.w_atoms, p.w_atoms, CU_TENSOR_MAP_DATA_TYPE_UINT32, 4, 128, w_bytes / 512, 128, atoms,

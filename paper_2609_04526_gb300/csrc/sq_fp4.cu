@@ -680,7 +680,7 @@ __global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
 
 // ---------------------------------------------------------------- many tokens
 //
-// A cluster of two CTAs per tile of 256 features and up to 224 tokens (tcgen05.mma.cta_group::2): each CTA
+// A cluster of two CTAs per tile of 256 features and up to 256 tokens, 224 of an expert (tcgen05.mma.cta_group::2): each CTA
 // holds the codes of 128 of the features and half of the tokens, the atoms of its features and those of
 // all the tokens. The tokens are the MMA's N, of any multiple of 16: an expert's rows, cut into equal
 // tiles, cost what they are. (With tokens as the 256 rows of a tile 32444 rows of 128 experts of 2880 x 2880
@@ -691,16 +691,20 @@ __global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
 // Only then the pair kernel has a warp that mends the codes of each stage before the MMAs may read it.
 
 struct Fp4PairCfg {
-  static constexpr int kNT = kFp4PairTokens;  // columns of an accumulator
   static constexpr int kEpiWarps = 8;  // 32 features w % 4, every other 32 tokens from w / 4 on
   static constexpr int kTmaWarp = kEpiWarps, kMmaWarp = kTmaWarp + 1, kMendWarp = kMmaWarp + 1;
   static constexpr int kThreads = 32 * (kMendWarp + 1);
-  static constexpr int kA = 128 * 128, kB = kNT / 2 * 128;
+  static constexpr int kA = 128 * 128;
   static constexpr int kMaxStages = 8;
   static constexpr int kBox = 16 * 64;  // 16 tokens x 32 features of an epilogue warp
 };
-static_assert(Fp4PairCfg::kNT <= 256 && Fp4PairCfg::kNT % 32 == 0 && 2 * Fp4PairCfg::kNT + 48 <= 512,
-              "two accumulators and a stage's scales in tensor memory");
+// Tensor memory: two accumulators and, behind them, 48 columns of a slice's scales. Those of wide tiles overlap, the
+// second begins at column 208: the epilogue reads the columns that both use before the others, and the MMAs of the
+// next tile wait for that much of it, some 2,500 cycles a tile.
+constexpr int kPairOver = 208, kPairScales = 464;
+static_assert(2 * kFp4PairApart <= kPairScales && kPairOver + kFp4PairTokens <= kPairScales && kPairScales + 48 <= 512 &&
+                  kFp4PairTokens - kPairOver <= 64 && kPairOver % 16 == 0,
+              "two accumulators and a slice's scales in tensor memory; two groups of 32 columns hold the shared ones");
 
 __device__ __forceinline__ void atom_to_tmem_pair_elect(uint32_t taddr, uint64_t desc) {
   asm volatile(
@@ -827,7 +831,7 @@ __global__ void __launch_bounds__(AtomCfg<FMT>::kThreads) sq_fp4_atoms_kernel(co
   if (tokens) {
     if (p.offsets) {
       int e, r0;
-      find_tile(p, *reinterpret_cast<TileSearch *>(piece), block >> 1, kFp4PairTokens, 16, e, r0, rows);
+      find_tile(p, *reinterpret_cast<TileSearch *>(piece), block >> 1, kFp4PairApart, 16, e, r0, rows);
       row0 = r0;
       __syncthreads();  // the search's memory is the pieces'
     } else {
@@ -950,16 +954,17 @@ __global__ void __launch_bounds__(AtomCfg<FMT>::kThreads) sq_fp4_atoms_kernel(co
   }
 }
 
-// H: slices of a stage.
-template <int FMT, int H>
+// H: slices of a stage. WIDE: a dense product in tiles of 240 or 256 tokens.
+template <int FMT, int H, bool WIDE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads, 1)
     sq_fp4_pair_kernel(const __grid_constant__ Fp4PairMaps maps, const Fp4Args p) {
   using C = Fp4PairCfg;
   constexpr int W = Fp4<FMT>::kWords;
   constexpr int kBlock = W * kAtom;  // the atoms of 128 rows and a stage
-  constexpr int kBs = H * C::kA, kSf = kBs + H * C::kB, kXs = kSf + H * kBlock, kStage = fp4_pair_stage(FMT, H);
+  constexpr int kB = (WIDE ? kFp4PairTokens : kFp4PairApart) / 2 * 128;  // codes of half the tokens
+  constexpr int kBs = H * C::kA, kSf = kBs + H * kB, kXs = kSf + H * kBlock, kStage = fp4_pair_stage(FMT, H, WIDE), kSecond = WIDE ? kPairOver : kFp4PairApart;
   static_assert(kXs + 2 * H * kBlock <= kStage && kStage % 1024 == 0, "a stage");
-  constexpr int kScaleCols = 12 * W, kScaleAt = 2 * C::kNT, kScaleBufs = (512 - kScaleAt) / kScaleCols >= 2 ? 2 : 1;
+  constexpr int kScaleCols = 12 * W, kScaleBufs = 48 / kScaleCols;
   extern __shared__ uint8_t fp4_smem_raw[];
   uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(fp4_smem_raw) + 1023) & ~uintptr_t(1023));
   __shared__ uint64_t bars[3 * C::kMaxStages + 5];
@@ -971,7 +976,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
   uint64_t *landed = full + C::kMaxStages;  // [S] with codes to mend: this CTA's copies have landed  (1 arrival + tx)
   uint64_t *empty = landed + C::kMaxStages;  // [S] the pair's MMAs have read the stage             (multicast commit)
   uint64_t *tfull = empty + C::kMaxStages;  // [2] accumulator complete                             (multicast commit)
-  uint64_t *tempty = tfull + 2;             // [2] leader: both epilogues have read it              (8 warps of each)
+  uint64_t *tempty = tfull + 2;             // [2] leader: both epilogues have read it              (8 warps of each; wide: and, of the tile behind, its shared columns)
   uint64_t *drain = tempty + 2;
   __shared__ __align__(16) float row_scale[C::kEpiWarps][32];
   __shared__ volatile uint32_t tile_n[C::kMaxStages];  // tokens of the tile that a stage belongs to, in whole 16
@@ -991,8 +996,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(&tfull[b], 1);
-      mbar_init(&tempty[b], 2 * C::kEpiWarps);
+      mbar_init(&tempty[b], (WIDE ? 4 : 2) * C::kEpiWarps);
     }
+    if (WIDE)  // no tile before the second one waits for its accumulator
+      for (int i = 0; i < 2 * C::kEpiWarps; ++i) mbar_arrive(&tempty[1]);
     mbar_init(drain, 1);
     abort_word = 0;
     fence_barrier_init();
@@ -1010,8 +1017,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
       expert_rows(p, e, lo, hi);
       ex.lo[e] = lo;
       ex.rows[e] = hi - lo;
-      ex.height[e] = tile_height(hi - lo, kFp4PairTokens, 16);
-      ex.tiles[e + 1] = tile_count(hi - lo, kFp4PairTokens);
+      ex.height[e] = tile_height(hi - lo, kFp4PairApart, 16);
+      ex.tiles[e + 1] = tile_count(hi - lo, kFp4PairApart);
     }
     __syncthreads();
     if (warp == 0) {
@@ -1060,9 +1067,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
       t.at(p, ex, first + tc * step);
       j.half = uniform(((t.rows + 15) & ~15) / 2);  // tokens of a CTA, in the smallest box that holds them
       int box = 0;
-      while (box + 1 < kFp4PairBoxes && (8 << box) < j.half) ++box;
+      while (box + 1 < kFp4PairBoxes && fp4_pair_box(box) < j.half) ++box;
       j.box = uniform(box);
-      j.bytes = H * (C::kA + 3 * kBlock + (j.box + 1 < kFp4PairBoxes ? 8 << j.box : C::kNT / 2) * 128);
+      j.bytes = H * (C::kA + 3 * kBlock + fp4_pair_box(j.box) * 128);
       j.row = uniform(t.row0) + j.half * static_cast<int>(rank);
       j.f = uniform(t.f0) + 128 * static_cast<int>(rank);
       j.e = uniform(t.e);
@@ -1088,7 +1095,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
 #pragma unroll
         for (int h = 0; h < H; ++h) {
           tma_load_3d_pair_elect(go, at + h * C::kA, &maps.w, bar, (kb * H + h) * (kDeep / 2), j.f, j.e);
-          tma_load_2d_pair_elect(go, at + kBs + h * C::kB, &maps.x[j.box], bar, (kb * H + h) * (kDeep / 2), j.row);
+          tma_load_2d_pair_elect(go, at + kBs + h * kB, &maps.x[j.box], bar, (kb * H + h) * (kDeep / 2), j.row);
         }
         tma_load_2d_pair_elect(go, at + kSf, &maps.w_atoms, bar, 0, j.wa + kb * H * W);
         tma_load_2d_pair_elect(go, at + kXs, &maps.x_atoms, bar, 0, j.xa + kb * H * 2 * W);
@@ -1116,12 +1123,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
       bool there = false;  // the stage was found complete while the one before was issued
       for (int tc = 0; tc < mine; ++tc) {
         const int ab = tc & 1;
-        if (tc >= 2) warp_wait(&tempty[ab], (static_cast<uint32_t>(tc >> 1) & 1u) ^ 1u, abort_flag, p.err);
+        if (tc >= (WIDE ? 1 : 2)) warp_wait(&tempty[ab], (static_cast<uint32_t>(tc >> 1) & 1u) ^ (WIDE && ab ? 0u : 1u), abort_flag, p.err);
         // the tile's N comes with its first stage: looked up here it would bring its branches into the loop
         if (!there) warp_wait(&full[s], ph, abort_flag, p.err);
         there = true;
         const uint32_t n16 = __reduce_max_sync(0xFFFFFFFFu, tile_n[s]);
-        const uint32_t d = tmem + ab * C::kNT;
+        const uint32_t d = tmem + ab * kSecond;
         const uint32_t desc0 = idesc_fp4<FMT>(2 * 128, 0, 0) | n16 << 14, desc1 = idesc_fp4<FMT>(2 * 128, 0, FMT == 0 ? 0 : 2) | n16 << 14;
         for (int kb = 0; kb < cnt; ++kb, ++it) {
           if (!there) warp_wait(&full[s], ph, abort_flag, p.err);
@@ -1130,7 +1137,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
           bool found = false;
 #pragma unroll
           for (int h = 0; h < H; ++h) {
-            const uint32_t sa = tmem + kScaleAt + ((it * H + h) & (kScaleBufs - 1)) * kScaleCols, sb = sa + 4 * W;
+            const uint32_t sa = tmem + kPairScales + ((it * H + h) & (kScaleBufs - 1)) * kScaleCols, sb = sa + 4 * W;
 #pragma unroll
             for (int i = 0; i < W; ++i) {
               atom_to_tmem_pair_elect(sa + 4 * i, sd0 + so + ((h * kBlock + i * kAtom) >> 4));
@@ -1141,7 +1148,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {  // past the end of K: codes and scales are zeros
               const int word = FMT == 0 ? kk : kk / 2;
-              umma_fp4_pair_elect<FMT>(d, ad0 + so + (h * C::kA >> 4) + 2 * kk, bd0 + so + (h * C::kB >> 4) + 2 * kk,
+              umma_fp4_pair_elect<FMT>(d, ad0 + so + (h * C::kA >> 4) + 2 * kk, bd0 + so + (h * kB >> 4) + 2 * kk,
                                        kk & 1 ? desc1 : desc0, sa + 4 * word, sb + 8 * word, (kb > 0 || h > 0 || kk > 0) ? 1u : 0u);
             }
           }
@@ -1172,7 +1179,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
             const bool of_w = i < W * H;
             const int j = of_w ? i : i - W * H, word = j % W, h = of_w ? j / W : j / (2 * W);
             const int lift = of_w ? 0 : 128 * (j / W % 2) - half * static_cast<int>(rank), rows = of_w ? 128 : half;
-            const uint32_t line = at + kSf + i * kAtom + lane * 16, codes = at + (of_w ? h * C::kA : kBs + h * C::kB);
+            const uint32_t line = at + kSf + i * kAtom + lane * 16, codes = at + (of_w ? h * C::kA : kBs + h * kB);
             const uint4 x = lds128(line);
             uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
@@ -1213,7 +1220,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
       const int ab = tc & 1;
       const int groups = (t.rows + 31) / 32;  // of 32 tokens
       const float ws2 = p.w_ws2 ? p.w_ws2[t.e] : p.ws2;
-      ok = __all_sync(0xFFFFFFFFu, mbar_wait(&tfull[ab], static_cast<uint32_t>(tc >> 1) & 1u, abort_flag, p.err));
+      ok = WIDE ? warp_wait(&tfull[ab], static_cast<uint32_t>(tc >> 1) & 1u, abort_flag, p.err)
+                : __all_sync(0xFFFFFFFFu, mbar_wait(&tfull[ab], static_cast<uint32_t>(tc >> 1) & 1u, abort_flag, p.err));
       if (!ok) break;
       tc_fence_after();
       auto release = [&] {  // the warp's part of the accumulator is read
@@ -1221,17 +1229,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
         __syncwarp();
         if (lane == 0) arrive_cluster(mapa_shared(smem_u32(&tempty[ab]), 0));
       };
-      if (share >= groups) release();
+      auto release_over = [&] {
+        if (!WIDE) return;
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive_cluster(mapa_shared(smem_u32(&tempty[ab ^ 1]), 0));
+      };
+      if (share >= groups) {
+        release_over();
+        release();
+      }
 #pragma unroll 1
-      for (int g = share; g < groups; g += 2) {
+      for (int n = share; n < groups; n += 2) {  // the first accumulator's shared columns are its last
+        const int g = WIDE && ab == 0 ? groups - 1 - n : n;
         const int left = t.rows - 32 * g;  // tokens of the group
         uint32_t v[32];
-        tmem_ld32(t_row + ab * C::kNT + 32 * g, v);
+        tmem_ld32(t_row + ab * kSecond + 32 * g, v);
+        if (WIDE && n == share) {  // the next tile's MMAs wait for this
+          tmem_ld_wait();
+          release_over();
+        }
         const float mine = lane < left ? (p.row_ws2 ? p.row_ws2[static_cast<int64_t>(t.row0) + 32 * g + lane] : p.x_ws2) : 0.f;
         __syncwarp();  // the box and the scales are read
         scales[lane] = mine;
         tmem_ld_wait();
-        if (g + 2 >= groups) release();
+        if (n + 2 >= groups) release();
         __syncwarp();
         uint32_t o[16];  // tokens 2 i and 2 i + 1
 #pragma unroll
@@ -1344,19 +1366,22 @@ cudaError_t launch_fp4_few(int fmt, const Fp4Maps &maps, const Fp4Args &p, cudaS
   return raw ? launch_few_fp4<1, true>(maps, p, stream) : launch_few_fp4<1, false>(maps, p, stream);
 }
 
-template <int FMT, int H>
+template <int FMT, int H, bool WIDE>
 static cudaError_t launch_pair(const Fp4PairMaps &maps, const Fp4Args &p, int sm_count, cudaStream_t stream) {
   static int done_mask = 0;
   const cudaError_t e = launch_after(sq_fp4_atoms_kernel<FMT>, static_cast<unsigned>(p.atom_ctas), AtomCfg<FMT>::kThreads, 0, stream, p);
   if (e != cudaSuccess) return e;
   const int clusters = static_cast<int>(std::min<int64_t>(p.units, sm_count / 2));
-  return launch_kernel<const Fp4PairMaps>(sq_fp4_pair_kernel<FMT, H>, done_mask, kFp4SmemMost, 2u * clusters, Fp4PairCfg::kThreads,
-                                          fp4_pair_smem(FMT, H, p.stages, p.offsets ? p.E : 0), 1, stream, maps, p);
+  return launch_kernel<const Fp4PairMaps>(sq_fp4_pair_kernel<FMT, H, WIDE>, done_mask, kFp4SmemMost, 2u * clusters, Fp4PairCfg::kThreads,
+                                          fp4_pair_smem(FMT, H, WIDE, p.stages, p.offsets ? p.E : 0), 1, stream, maps, p);
 }
 
 cudaError_t launch_fp4_pair(int fmt, const Fp4PairMaps &maps, const Fp4Args &p, int sm_count, cudaStream_t stream) {
-  if (fmt == 0) return p.slices == 1 ? launch_pair<0, 1>(maps, p, sm_count, stream) : launch_pair<0, 2>(maps, p, sm_count, stream);
-  return p.slices == 1 ? launch_pair<1, 1>(maps, p, sm_count, stream) : launch_pair<1, 2>(maps, p, sm_count, stream);
+  const bool wide = p.tile_tokens > kFp4PairApart;
+  if (fmt == 0 && wide) return launch_pair<0, 1, true>(maps, p, sm_count, stream);
+  if (fmt == 0) return p.slices == 1 ? launch_pair<0, 1, false>(maps, p, sm_count, stream) : launch_pair<0, 2, false>(maps, p, sm_count, stream);
+  if (wide) return p.slices == 1 ? launch_pair<1, 1, true>(maps, p, sm_count, stream) : launch_pair<1, 2, true>(maps, p, sm_count, stream);
+  return p.slices == 1 ? launch_pair<1, 1, false>(maps, p, sm_count, stream) : launch_pair<1, 2, false>(maps, p, sm_count, stream);
 }
 
 }  // namespace sqi

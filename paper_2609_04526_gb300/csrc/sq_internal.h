@@ -502,8 +502,10 @@ constexpr int kFp4FewBoxes = 5;              // boxes of 8 .. 128 token rows
 constexpr int kFp4SmemAlone = 224 * 1024;    // of a CTA alone on its SM
 constexpr int kFp4SmemShared = 112 * 1024;   // ... of two
 constexpr int kFp4SmemMost = 232448 - 1536;  // ... beside its static shared memory
-constexpr int kFp4PairTokens = 224, kFp4PairFeatures = 256;  // a tile of the pair kernel, at most
-constexpr int kFp4PairBoxes = 5;                             // boxes of 8 .. 64 and 112 token rows
+constexpr int kFp4PairTokens = 256, kFp4PairFeatures = 256;  // a tile of the pair kernel, at most
+constexpr int kFp4PairApart = 224;  // two accumulators of up to so many tokens lie beside each other; wider ones overlap
+constexpr int kFp4PairBoxes = 6;    // boxes of 8 .. 64, 112 and 128 token rows
+__host__ __device__ constexpr int fp4_pair_box(int i) { return i < 4 ? 8 << i : i == 4 ? kFp4PairApart / 2 : kFp4PairTokens / 2; }
 struct Fp4Maps {
   CUtensorMap w;                // codes [E][N][K / 2], boxes of 128 bytes x 128 rows
   CUtensorMap x[kFp4FewBoxes];  // codes [R][K / 2], boxes of 128 bytes x (8 << i) rows
@@ -545,20 +547,23 @@ struct Fp4Args {
 constexpr int fp4_few_stage(int tile_tokens) { return 128 * 128 + tile_tokens * 128 + 2 * 2048; }
 __host__ __device__ constexpr int fp4_atoms(int fmt) { return fmt == 0 ? 2048 : 1024; }  // bytes of 128 rows and a slice
 __host__ __device__ constexpr int fp4_atom_stages(int fmt) { return fmt == 0 ? 8 : 16; }  // slices of a CTA that writes atoms
-__host__ __device__ constexpr int fp4_pair_stage(int fmt, int slices) {
-  return slices * (128 * 128 + kFp4PairTokens / 2 * 128 + 3 * fp4_atoms(fmt));
+__host__ __device__ constexpr int fp4_pair_stage(int fmt, int slices, bool wide) {
+  return slices * (128 * 128 + (wide ? kFp4PairTokens : kFp4PairApart) / 2 * 128 + 3 * fp4_atoms(fmt));
 }
-constexpr size_t fp4_pair_smem(int fmt, int slices, int stages, int E) {
-  return 1024 + static_cast<size_t>(stages) * fp4_pair_stage(fmt, slices) + 8 * 1024 + (E > 0 ? 4 * (4 * E + 1) : 0);
+constexpr size_t fp4_pair_smem(int fmt, int slices, bool wide, int stages, int E) {
+  return 1024 + static_cast<size_t>(stages) * fp4_pair_stage(fmt, slices, wide) + 8 * 1024 + (E > 0 ? 4 * (4 * E + 1) : 0);
 }
 // Tokens of a whole tile of a dense product. The launch lasts as long as its waves of tiles, 400 + 1.15 h
-// cycles a stage of a tile of h tokens (fitted; the MMAs alone take 2 h). 2048 tokens against 4096 x 14336 in tiles of 224
-// and a last one of 32: 70 us with their quantisation, 73 in ten of 208.
-inline int fp4_pair_tokens(int64_t R, int64_t ftiles, int clusters) {
-  auto cost = [](int64_t h) { return h > 0 ? 400 + 1.15 * h : 0.0; };
+// cycles a slice of a tile of h tokens (fitted; the MMAs alone take 2 h) and 1.23 times that where accumulators overlap (of
+// 8 to 56 slices; of fewer the wait between tiles weighs more).
+// In us, with the tokens' quantisation: 2048 tokens against 4096 x 14336 NVFP4 in two waves of 240 65, in three of 224 and a
+// last one of 32 69, in ten tiles of 208 73; 1024 against 8192 x 8192 in 256 39, in 224 41; 4096 against 4096 x 4096, four
+// waves either way, in 256 46, in 224 40.
+inline int fp4_pair_tokens(int64_t R, int64_t ftiles, int clusters, int slices) {
+  auto cost = [](int64_t h) { return h > kFp4PairApart ? 1.23 * (400 + 1.15 * h) : h > 0 ? 400 + 1.15 * h : 0.0; };
   double best = 0;
-  int tokens = kFp4PairTokens;
-  for (int h = kFp4PairTokens; h >= 96; h -= 16) {
+  int tokens = kFp4PairApart;
+  for (int h = slices >= 8 ? kFp4PairTokens : kFp4PairApart; h >= 96; h -= 16) {
     const int64_t whole = R / h * ftiles, rest = R % h ? ftiles : 0, waves = (whole + clusters - 1) / clusters;
     const int64_t left = waves * clusters - whole;
     const double us = waves * cost(h) + (rest > left ? (rest - left + clusters - 1) / clusters * cost(R % h) : 0.0);
@@ -603,7 +608,7 @@ inline void fp4_plan(int fmt, int sm_count, const Fp4Clusters &fit, Fp4Args &p) 
   const bool alone = few_units <= fit.alone[splits];
   // What the launches take: rounds of CTAs (two on an SM), or waves of pair tiles and, at least, the weight's way
   // from memory. Tiles of ragged experts are half empty on average.
-  const int pair_tokens = p.offsets ? kFp4PairTokens : fp4_pair_tokens(p.R, pair_ftiles, clusters);
+  const int pair_tokens = p.offsets ? kFp4PairApart : fp4_pair_tokens(p.R, pair_ftiles, clusters, cnt);
   const double rows = static_cast<double>(p.R) / groups;
   const double few_tiles = p.offsets ? (p.R + 0.5 * few_tokens * groups) / few_tokens * ftiles : few_units;
   const double pair_tiles = (p.offsets ? (p.R + 0.5 * pair_tokens * groups) / pair_tokens : up(p.R, pair_tokens)) * pair_ftiles;
@@ -623,14 +628,14 @@ inline void fp4_plan(int fmt, int sm_count, const Fp4Clusters &fit, Fp4Args &p) 
     // x 4096 NVFP4 352, 340, 2048 x 4096 x 14336 74, 70, MXFP4 68, 63). Experts' narrow tiles wait for their loads and
     // want the finer ring (8111 tokens to four of 128 of 2880 x 2880 200, 204). An odd slice behind K is computed as
     // zeros: not where it would be more than a 17th of all.
-    p.slices = !p.offsets && (cnt % 2 == 0 || cnt > 16) ? 2 : 1;
+    p.slices = !p.offsets && (cnt % 2 == 0 || cnt > 16) && (fmt == 1 || pair_tokens <= kFp4PairApart) ? 2 : 1;
     p.depth = (cnt + p.slices - 1) / p.slices;
     p.token_blocks = static_cast<int>(2 * token_tiles);
     p.atom_ctas = static_cast<int>((p.token_blocks + 2 * int64_t(p.E) * p.ftiles) *
                                    ((p.depth * p.slices + fp4_atom_stages(fmt) - 1) / fp4_atom_stages(fmt)));
     p.splits = 1;
     p.stages = 8;
-    while (fp4_pair_smem(fmt, p.slices, p.stages, p.offsets ? p.E : 0) > static_cast<size_t>(kFp4SmemMost)) --p.stages;
+    while (fp4_pair_smem(fmt, p.slices, pair_tokens > kFp4PairApart, p.stages, p.offsets ? p.E : 0) > static_cast<size_t>(kFp4SmemMost)) --p.stages;
     return;
   }
   p.ftiles = ftiles;

@@ -266,3 +266,23 @@ def test_rows_by_slot_captured_with_scratch_and_without():
             torch.cuda.synchronize()
             assert alike(out, want)
     h2.sq_sync()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("R, N, K", [(2048, 4096, 2912), (2047, 4096, 2080), (1024, 8192, 2880), (1000, 8200, 4128), (1999, 4104, 2272),
+                                     (480, 19456, 2080)])
+def test_rows_in_tiles_of_more_than_224(h, fmt, R, N, K):  # noqa: F811
+    """Sizes at which tiles of 240 or 256 rows save a wave: their accumulators share columns."""
+    check_dense(h, fmt, R, N, K, seed=R + N + K)
+
+
+@pytest.mark.parametrize("R, N, K", [(2048, 4096, 2912), (1000, 8200, 2080), (2100, 2056, 8224)])
+def test_tall_tiles_and_deep_stages_with_negative_scales(h, R, N, K):  # noqa: F811
+    check_dense(h, pkg.NVFP4, R, N, K, seed=R + N + K, signs=True)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("R, N, K", [(3000, 4104, 544), (3000, 4104, 800), (2500, 4104, 4384), (2500, 4104, 4640)])
+def test_an_odd_number_of_slices(h, fmt, R, N, K):  # noqa: F811
+    """K whose last stage has one slice, none in stages of one, or a second one past its end."""
+    check_dense(h, fmt, R, N, K, seed=R + N + K)
