@@ -553,7 +553,7 @@ typedef struct {
  * X device bf16 [T, K]. slot_of device int32 [R] or NULL: NULL, R == T and row r is X[r]; else row r
  * is X[slot_of[r] / k] (1 <= k <= 32, T * k < 2^31), the row that sq_dispatch would copy there, and a row whose slot
  * is outside [0, T * k) is a row of zeros. Where many rows are of few tokens, the tokens are quantised once,
- * into scratch of the handle (T + 1 rows), and copied; a graph capture that finds no scratch quantises row by
+ * into scratch of the handle (T rows), and copied; a graph capture that finds no scratch quantises row by
  * row. Results of a row do not depend on the rows beside it, nor on this. */
 sq_status sq_quantize(sq_handle h, const sq_rows *q, int64_t T, int32_t k, const uint16_t *X, const int32_t *slot_of,
                       void *stream);

@@ -566,7 +566,7 @@ sq_status check_rows(sq_handle h, const sq_rows *q) {
 sqi::QuantArgs quant_args(const sq_rows *q) {
   sqi::QuantArgs a = {};
   a.R = q->R;
-  a.K = q->K;
+  a.K = a.last = q->K;
   a.codes = q->codes;
   a.scales = q->scales;
   a.row_ws2 = q->row_ws2;
@@ -1798,24 +1798,23 @@ sq_status sq_quantize(sq_handle h, const sq_rows *q, int64_t T, int32_t k, const
   a.wide = reinterpret_cast<uintptr_t>(X) % 32 == 0;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (slot_of && sqi::quantize_tokens_first(q->fmt, a.R, T, a.K)) {
-    // the tokens' 4-bit rows, a row of zeros behind them, then each row a copy of its token's
-    const int64_t rows = T + 1, G = a.K / block_of(q->fmt);
-    const int64_t codes = rows * (a.K / 2), scales = (rows * G + 15) / 16 * 16;
-    const size_t bytes = static_cast<size_t>(codes + scales + 4 * rows);
+    // the tokens' 4-bit rows, then each row a copy of its token's
+    const int64_t G = a.K / block_of(q->fmt), codes = T * (a.K / 2), scales = (T * G + 15) / 16 * 16;
+    const size_t bytes = static_cast<size_t>(codes + scales + 4 * T);
     cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
     cudaError_t e = bytes <= dev->tokens.bytes ? cudaSuccess : cudaStreamIsCapturing(st, &cap);
     if (e != cudaSuccess) return cuda_fail(h, e, "cudaStreamIsCapturing");
     if (cap == cudaStreamCaptureStatusNone) {  // a capture that finds no scratch takes the other way to the same rows
       SQ_TRY(ensure_scratch(h, dev->tokens, bytes, st, "a quantisation by slot"));
       sqi::QuantArgs t = a;
-      t.R = rows;
+      t.R = T;
       t.codes = static_cast<uint8_t *>(dev->tokens.ptr);
       t.scales = t.codes + codes;
       t.row_ws2 = a.row_ws2 ? reinterpret_cast<float *>(t.scales + scales) : nullptr;
       t.slot_of = nullptr;
       t.k = 1;
       t.slots = T;
-      e = sqi::launch_quantize(q->fmt, t, dev->sm_count, st);
+      e = T > 0 ? sqi::launch_quantize(q->fmt, t, dev->sm_count, st) : cudaSuccess;
       if (e == cudaSuccess) e = sqi::launch_spread(q->fmt, a, t, st);
       if (e != cudaSuccess) return cuda_fail(h, e, "quantisation launch");
       return SQ_OK;

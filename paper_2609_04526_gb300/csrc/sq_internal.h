@@ -472,7 +472,7 @@ cudaError_t launch_head_chunk(const HeadArgs &a, const HeadMaps &m, int first, i
 // Rows of FP4 (sq_rows.cu, sq_fp4.cu).
 struct QuantArgs {
   int64_t R;           // rows of codes
-  int K;
+  int K, last;         // values of a row, and of the last one (quantisation)
   uint8_t *codes, *scales;
   float *row_ws2;      // each row's own scale, or null: ws2 for all
   float ws2, inv;      // inv: fl32(1 / ws2)
@@ -480,7 +480,7 @@ struct QuantArgs {
   const uint16_t *X;
   const int32_t *slot_of;  // [R] slot of a row, its source row slot / k; null: row r is X[r]
   int k;
-  int64_t slots;           // T * k; without slot_of, rows from there on are zeros
+  int64_t slots;           // T * k
   bool wide;               // X starts on 32 bytes
 };
 cudaError_t launch_quantize(int fmt, const QuantArgs &a, int sm_count, cudaStream_t stream);

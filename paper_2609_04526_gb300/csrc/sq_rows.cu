@@ -144,9 +144,10 @@ __global__ void __launch_bounds__(kRowsThreads) sq_quantize_kernel(const QuantAr
   __shared__ uint32_t warp_top[kRowsThreads / 32];
   dependency_wait();
   dependency_start();
-  const int t = threadIdx.x % TPR, chunks = a.K / 16;
+  const int t = threadIdx.x % TPR;
   const int64_t r = static_cast<int64_t>(blockIdx.x) * (kRowsThreads / TPR) + threadIdx.x / TPR;
-  int64_t src = r < a.R && r < a.slots ? r : -1;
+  const int chunks = (!OWN && r == a.R - 1 ? a.last : a.K) / 16;
+  int64_t src = r < a.R ? r : -1;
   if (a.slot_of) {
     const int slot = r < a.R ? a.slot_of[r] : -1;
     src = slot >= 0 && slot < a.slots ? slot / a.k : -1;
@@ -211,24 +212,38 @@ __global__ void __launch_bounds__(kRowsThreads) sq_quantize_kernel(const QuantAr
   }
 }
 
-// Rows by slot from the 4-bit rows of the tokens (the last of those: zeros), a warp each: 16384 rows of 2048 values
-// NVFP4 (19 MB, from the L2) in 6 us. Codes move in 16-byte pieces;
+// Rows by slot from the 4-bit rows of the tokens, a warp each: 16384 rows of 2048 values
+// NVFP4 (19 MB, from the L2) in 6 us. A row of no token is what a row of zeros gives: the smallest scales. Codes move in 16-byte pieces;
 // scale bytes too, or, where a row is not whole pieces, in the units that divide it. All of a row's loads are
 // in flight before its first store.
+__device__ __forceinline__ void fill_bytes(uint4 &u, uint32_t word) { u = make_uint4(word, word, word, word); }
 template <typename Unit>
-__global__ void __launch_bounds__(kRowsThreads) sq_spread_kernel(const QuantArgs a, const QuantArgs tokens, const int G) {
+__device__ __forceinline__ void fill_bytes(Unit &u, uint32_t word) { u = static_cast<Unit>(word); }
+
+template <typename Unit>
+__global__ void __launch_bounds__(kRowsThreads) sq_spread_kernel(const QuantArgs a, const QuantArgs tokens, const int G,
+                                                                 const uint32_t least) {
   dependency_wait();
   dependency_start();
   const int lane = threadIdx.x % 32;
   const int64_t r = static_cast<int64_t>(blockIdx.x) * (kRowsThreads / 32) + threadIdx.x / 32;
   if (r >= a.R) return;
   const int slot = a.slot_of[r];
-  const int64_t t = slot >= 0 && slot < a.slots ? slot / a.k : tokens.R - 1;
+  const bool on = slot >= 0 && slot < a.slots;
+  const int64_t t = on ? slot / a.k : 0;
   const int pieces = a.K / 32, units = G / static_cast<int>(sizeof(Unit));
   const uint4 *codes = reinterpret_cast<const uint4 *>(tokens.codes + t * (a.K / 2));
   uint4 *codes_to = reinterpret_cast<uint4 *>(a.codes + r * (a.K / 2));
   const Unit *scales = reinterpret_cast<const Unit *>(tokens.scales + t * G);
   Unit *scales_to = reinterpret_cast<Unit *>(a.scales + r * G);
+  if (!on) {
+    for (int c = lane; c < pieces; c += 32) codes_to[c] = make_uint4(0, 0, 0, 0);
+    Unit s;
+    fill_bytes(s, least);
+    for (int c = lane; c < units; c += 32) scales_to[c] = s;
+    if (a.row_ws2 && lane == 0) a.row_ws2[r] = 0x1p-116f;
+    return;
+  }
   const float row = a.row_ws2 ? tokens.row_ws2[t] : 0.f;
   for (int c0 = lane; c0 < max(pieces, units); c0 += 32 * kRowsHold) {
     uint4 v[kRowsHold];
@@ -315,9 +330,23 @@ cudaError_t by_width(int64_t R, int K, int sm_count, F f) {
 }
 unsigned row_ctas(int64_t R, int tpr) { return static_cast<unsigned>((R + kRowsThreads / tpr - 1) / (kRowsThreads / tpr)); }
 
+// Without scales of the rows' own a block knows nothing of its row. Many are cut evenly, into rows of what 64 threads
+// hold (2048 x 14336 NVFP4, whose rows leave an eighth of 256 threads idle, 14.1 -> 12.8 us; 8111 x 2880 MXFP4 7.2 ->
+// 6.6). Read back, which waits for memory alone, they gain nothing.
+void even_rows(QuantArgs &a, int sm_count) {
+  constexpr int kEven = 64 * kRowsHold * 16;
+  const int64_t values = a.R * a.K;
+  if (a.row_ws2 || a.slot_of || values < int64_t(4) * sm_count * kRowsThreads * kRowsHold * 16) return;
+  a.R = (values + kEven - 1) / kEven;
+  a.K = kEven;
+  a.last = static_cast<int>(values - (a.R - 1) * kEven);
+}
+
 }  // namespace
 
-cudaError_t launch_quantize(int fmt, const QuantArgs &a, int sm_count, cudaStream_t stream) {
+cudaError_t launch_quantize(int fmt, const QuantArgs &rows, int sm_count, cudaStream_t stream) {
+  QuantArgs a = rows;
+  even_rows(a, sm_count);
   return by_width(a.R, a.K, sm_count, [&](auto tpr) {
     constexpr int kTpr = decltype(tpr)::value;
     const auto kernel = fmt == 1       ? sq_quantize_kernel<1, false, kTpr>
@@ -333,7 +362,7 @@ cudaError_t launch_spread(int fmt, const QuantArgs &a, const QuantArgs &tokens, 
                       : G % 4 == 0 ? sq_spread_kernel<uint32_t>
                       : G % 2 == 0 ? sq_spread_kernel<uint16_t>
                                    : sq_spread_kernel<uint8_t>;
-  return launch_after(kernel, row_ctas(a.R, 32), kRowsThreads, 0, stream, a, tokens, G);
+  return launch_after(kernel, row_ctas(a.R, 32), kRowsThreads, 0, stream, a, tokens, G, fmt == 0 ? 0x01010101u : 0u);
 }
 
 cudaError_t launch_dequantize(int fmt, const QuantArgs &a, uint16_t *X, int sm_count, cudaStream_t stream) {

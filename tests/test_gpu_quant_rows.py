@@ -142,3 +142,27 @@ def test_tensors_elsewhere_are_refused(h):
         h.sq_grouped_quant_fwd(gw, torch.zeros(3, dtype=torch.int64), q)
     with pytest.raises(pkg.SQError, match="format"):
         h.sq_quant_fwd(pkg.QuantWeight(pkg.MXFP4, 16, 64, gw.codes[0], torch.zeros(16, 2, dtype=torch.uint8, device="cuda"), 1.0), q)
+
+
+@pytest.mark.parametrize("fmt, ws2", [(pkg.NVFP4, None), (pkg.NVFP4, 0.00317), (pkg.MXFP4, None)])
+@pytest.mark.parametrize("T, K", [(2100, 5024), (1500, 14336), (330000, 32), (5, 4194400)])
+def test_many_values(h, fmt, ws2, T, K):
+    """So many that rows without scales of their own are cut evenly, with a last piece that is shorter; from 16 bytes
+    that are no boundary of 32 too. Infinite and empty blocks stay where they are."""
+    g = torch.Generator(device="cuda").manual_seed(T)
+    room = torch.randn(T * K + 8, generator=g, device="cuda").bfloat16()
+    for X in (room[8:].view(T, K), room[:T * K].view(T, K)):
+        X[T // 2, K - 1], X[T // 3, :32], X[T - 1, K - 32:] = float("inf"), 0, -0.0
+        q = h.sq_quantize(fmt, X, ws2)
+        few = [q]
+        for lo in (0, T // 3, T - 2):  # a few rows alone, cut by rows
+            part = h.sq_quantize(fmt, X[lo:lo + 2], ws2)
+            few.append(part)
+            assert torch.equal(q.codes[lo:lo + 2], part.codes) and torch.equal(q.scales[lo:lo + 2], part.scales)
+        back = h.sq_dequantize(q, X=torch.empty(T * K + 8, dtype=torch.bfloat16, device="cuda")[8:].view(T, K))
+        for lo, part in zip((0, T // 3, T - 2), few[1:]):
+            rows = h.sq_dequantize(part)
+            assert torch.equal(back[lo:lo + 2].nan_to_num(7), rows.nan_to_num(7)) and torch.equal(back[lo:lo + 2].isnan(), rows.isnan())
+        if T * K < 12e6:
+            check(h, fmt, X, ws2)
+    h.sq_sync()
