@@ -700,7 +700,7 @@ struct Fp4PairCfg {
 };
 // Tensor memory: two accumulators and, behind them, 48 columns of a slice's scales. Those of wide tiles overlap, the
 // second begins at column 208: the epilogue reads the columns that both use before the others, and the MMAs of the
-// next tile wait for that much of it, some 2,500 cycles a tile.
+// next tile wait for that much of it, some 2,500 cycles a tile (estimated from products of 16 and 32 slices).
 constexpr int kPairOver = 208, kPairScales = 464;
 static_assert(2 * kFp4PairApart <= kPairScales && kPairOver + kFp4PairTokens <= kPairScales && kPairScales + 48 <= 512 &&
                   kFp4PairTokens - kPairOver <= 64 && kPairOver % 16 == 0,
