@@ -91,13 +91,20 @@ __device__ __forceinline__ void umma_fp4_elect(uint32_t d, uint64_t a, uint64_t 
 // moves them to the uniform ones at every use: an instruction then takes 30 cycles to issue, not 8. The
 // MMA warps for that reason go on after a wait that ran out: they issue what is left (on whatever the
 // shared memory holds), every later wait returns at once, and the error word is set.
+// CLUSTER: for a barrier that threads of the peer CTA arrive on or signal. They release at cluster scope, and
+// only an acquire at that scope, in whichever CTA, orders what follows behind what they did.
+template <bool CLUSTER = false>
+__device__ __forceinline__ bool warp_test(uint64_t *bar, uint32_t parity) {
+  return CLUSTER ? mbar_test_wait_cluster(bar, parity) : mbar_test_wait(bar, parity);
+}
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag, int *err) {
-  if (__all_sync(0xFFFFFFFFu, mbar_test_wait(bar, parity))) return true;
+  if (__all_sync(0xFFFFFFFFu, warp_test<CLUSTER>(bar, parity))) return true;
   const unsigned long long t0 = globaltimer();
   while (true) {
 #pragma unroll 1
     for (int i = 0; i < 64; ++i)
-      if (__all_sync(0xFFFFFFFFu, mbar_test_wait(bar, parity))) return true;
+      if (__all_sync(0xFFFFFFFFu, warp_test<CLUSTER>(bar, parity))) return true;
     const bool late = globaltimer() - t0 > kWaitLimitNs;
     if (__any_sync(0xFFFFFFFFu, late || *abort_flag)) {
       if (__any_sync(0xFFFFFFFFu, late)) {
@@ -1117,50 +1124,58 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Fp4PairCfg::kThreads
       const uint64_t sd0 = atom_desc(ring + kSf);
       // Behind the MMA that they run the tensor cores hold about two more: between the last MMA of a stage and
       // the first of the next there are 250 cycles for the barriers, the commit and the atoms.
+      // The loop is there twice: a stage whose codes the peer has mended is waited for at cluster scope.
       const int mine = __reduce_max_sync(0xFFFFFFFFu, pair_tiles);
-      int s = 0, it = 0;
-      uint32_t ph = 0;
-      bool there = false;  // the stage was found complete while the one before was issued
-      for (int tc = 0; tc < mine; ++tc) {
-        const int ab = tc & 1;
-        if (tc >= (WIDE ? 1 : 2)) warp_wait(&tempty[ab], (static_cast<uint32_t>(tc >> 1) & 1u) ^ (WIDE && ab ? 0u : 1u), abort_flag, p.err);
-        // the tile's N comes with its first stage: looked up here it would bring its branches into the loop
-        if (!there) warp_wait(&full[s], ph, abort_flag, p.err);
-        there = true;
-        const uint32_t n16 = __reduce_max_sync(0xFFFFFFFFu, tile_n[s]);
-        const uint32_t d = tmem + ab * kSecond;
-        const uint32_t desc0 = idesc_fp4<FMT>(2 * 128, 0, 0) | n16 << 14, desc1 = idesc_fp4<FMT>(2 * 128, 0, FMT == 0 ? 0 : 2) | n16 << 14;
-        for (int kb = 0; kb < cnt; ++kb, ++it) {
-          if (!there) warp_wait(&full[s], ph, abort_flag, p.err);
-          tc_fence_after();
-          const uint32_t so = static_cast<uint32_t>(s * kStage) >> 4;
-          bool found = false;
+      auto issue = [&](auto mended) {
+        constexpr bool kMended = decltype(mended)::value;
+        int s = 0, it = 0;
+        uint32_t ph = 0;
+        bool there = false;  // the stage was found complete while the one before was issued
+        for (int tc = 0; tc < mine; ++tc) {
+          const int ab = tc & 1;
+          if (tc >= (WIDE ? 1 : 2)) warp_wait<true>(&tempty[ab], (static_cast<uint32_t>(tc >> 1) & 1u) ^ (WIDE && ab ? 0u : 1u), abort_flag, p.err);
+          // the tile's N comes with its first stage: looked up here it would bring its branches into the loop
+          if (!there) warp_wait<kMended>(&full[s], ph, abort_flag, p.err);
+          there = true;
+          const uint32_t n16 = __reduce_max_sync(0xFFFFFFFFu, tile_n[s]);
+          const uint32_t d = tmem + ab * kSecond;
+          const uint32_t desc0 = idesc_fp4<FMT>(2 * 128, 0, 0) | n16 << 14, desc1 = idesc_fp4<FMT>(2 * 128, 0, FMT == 0 ? 0 : 2) | n16 << 14;
+          for (int kb = 0; kb < cnt; ++kb, ++it) {
+            if (!there) warp_wait<kMended>(&full[s], ph, abort_flag, p.err);
+            tc_fence_after();
+            const uint32_t so = static_cast<uint32_t>(s * kStage) >> 4;
+            bool found = false;
 #pragma unroll
-          for (int h = 0; h < H; ++h) {
-            const uint32_t sa = tmem + kPairScales + ((it * H + h) & (kScaleBufs - 1)) * kScaleCols, sb = sa + 4 * W;
+            for (int h = 0; h < H; ++h) {
+              const uint32_t sa = tmem + kPairScales + ((it * H + h) & (kScaleBufs - 1)) * kScaleCols, sb = sa + 4 * W;
 #pragma unroll
-            for (int i = 0; i < W; ++i) {
-              atom_to_tmem_pair_elect(sa + 4 * i, sd0 + so + ((h * kBlock + i * kAtom) >> 4));
-              atom_to_tmem_pair_elect(sb + 8 * i, sd0 + so + (((H + 2 * h) * kBlock + i * kAtom) >> 4));
-              atom_to_tmem_pair_elect(sb + 8 * i + 4, sd0 + so + (((H + 2 * h + 1) * kBlock + i * kAtom) >> 4));
+              for (int i = 0; i < W; ++i) {
+                atom_to_tmem_pair_elect(sa + 4 * i, sd0 + so + ((h * kBlock + i * kAtom) >> 4));
+                atom_to_tmem_pair_elect(sb + 8 * i, sd0 + so + (((H + 2 * h) * kBlock + i * kAtom) >> 4));
+                atom_to_tmem_pair_elect(sb + 8 * i + 4, sd0 + so + (((H + 2 * h + 1) * kBlock + i * kAtom) >> 4));
+              }
+              if (h == H - 1) found = warp_test<kMended>(&full[s + 1 == S ? 0 : s + 1], s + 1 == S ? ph ^ 1u : ph);
+#pragma unroll
+              for (int kk = 0; kk < 4; ++kk) {  // past the end of K: codes and scales are zeros
+                const int word = FMT == 0 ? kk : kk / 2;
+                umma_fp4_pair_elect<FMT>(d, ad0 + so + (h * C::kA >> 4) + 2 * kk, bd0 + so + (h * kB >> 4) + 2 * kk,
+                                         kk & 1 ? desc1 : desc0, sa + 4 * word, sb + 8 * word, (kb > 0 || h > 0 || kk > 0) ? 1u : 0u);
+              }
             }
-            if (h == H - 1) found = mbar_test_wait(&full[s + 1 == S ? 0 : s + 1], s + 1 == S ? ph ^ 1u : ph);
-#pragma unroll
-            for (int kk = 0; kk < 4; ++kk) {  // past the end of K: codes and scales are zeros
-              const int word = FMT == 0 ? kk : kk / 2;
-              umma_fp4_pair_elect<FMT>(d, ad0 + so + (h * C::kA >> 4) + 2 * kk, bd0 + so + (h * kB >> 4) + 2 * kk,
-                                       kk & 1 ? desc1 : desc0, sa + 4 * word, sb + 8 * word, (kb > 0 || h > 0 || kk > 0) ? 1u : 0u);
+            commit_pair_mc_elect(&empty[s]);
+            if (++s == S) {
+              s = 0;
+              ph ^= 1u;
             }
+            there = __all_sync(0xFFFFFFFFu, found);
           }
-          commit_pair_mc_elect(&empty[s]);
-          if (++s == S) {
-            s = 0;
-            ph ^= 1u;
-          }
-          there = __all_sync(0xFFFFFFFFu, found);
+          commit_pair_mc_elect(&tfull[ab]);
         }
-        commit_pair_mc_elect(&tfull[ab]);
-      }
+      };
+      if (FMT == 0 && __any_sync(0xFFFFFFFFu, mend))
+        issue(std::true_type());
+      else
+        issue(std::false_type());
       commit_pair_elect(drain);
       mbar_drain(drain, 0);
     }
