@@ -9,7 +9,7 @@ from __future__ import annotations
 import ctypes
 import dataclasses
 import os
-from typing import Optional
+from typing import Optional, Union
 
 import torch
 
@@ -158,18 +158,18 @@ class QuantWeight:
 @dataclasses.dataclass
 class GroupedWeight:
     """The E experts of one MoE linear, each [N, K]: codes [E, N, K/2] u8, scales
-    [E, N, K/B] u8 (device), ws2 one tensor scale per expert (host floats; for
-    sq_grouped_quant_fwd a device fp32 tensor [E], MXFP4 any)."""
+    [E, N, K/B] u8 (device), ws2 one tensor scale per expert: host floats or, for
+    sq_grouped_quant_fwd, a device fp32 tensor [E]; MXFP4 None, or ones."""
     fmt: int
     E: int
     N: int
     K: int
     codes: torch.Tensor
     scales: Optional[torch.Tensor]
-    ws2: list
+    ws2: Union[list, torch.Tensor, None]
 
     def _c(self):
-        ws = (ctypes.c_float * self.E)(*[float(x) for x in self.ws2])
+        ws = None if self.ws2 is None else (ctypes.c_float * self.E)(*[float(x) for x in self.ws2])
         c = _SqGroupedWeight(self.fmt, self.E, self.N, self.K, _ptr(self.codes), _ptr(self.scales),
                              ctypes.cast(ws, ctypes.POINTER(ctypes.c_float)))
         return c, ws  # keep the array alive for the call
@@ -177,7 +177,8 @@ class GroupedWeight:
     def expert(self, e: int) -> QuantWeight:
         """Expert e as a dense weight (views into the grouped planes)."""
         return QuantWeight(self.fmt, self.N, self.K, self.codes[e],
-                           None if self.scales is None else self.scales[e], float(self.ws2[e]))
+                           None if self.scales is None else self.scales[e],
+                           1.0 if self.ws2 is None and self.fmt == MXFP4 else float(self.ws2[e]))
 
 
 @dataclasses.dataclass
