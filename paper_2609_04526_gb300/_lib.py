@@ -159,7 +159,8 @@ class QuantWeight:
 class GroupedWeight:
     """The E experts of one MoE linear, each [N, K]: codes [E, N, K/2] u8, scales
     [E, N, K/B] u8 (device), ws2 one tensor scale per expert: host floats or, for
-    sq_grouped_quant_fwd, a device fp32 tensor [E]; MXFP4 None, or ones."""
+    sq_grouped_quant_fwd, a device fp32 tensor [E], which the other calls wait for and
+    copy to the host; MXFP4 None, or ones."""
     fmt: int
     E: int
     N: int
@@ -169,7 +170,7 @@ class GroupedWeight:
     ws2: Union[list, torch.Tensor, None]
 
     def _c(self):
-        ws = None if self.ws2 is None else (ctypes.c_float * self.E)(*[float(x) for x in self.ws2])
+        ws = None if self.ws2 is None else (ctypes.c_float * self.E)(*[float(x) for x in _on_host(self.ws2)])
         c = _SqGroupedWeight(self.fmt, self.E, self.N, self.K, _ptr(self.codes), _ptr(self.scales),
                              ctypes.cast(ws, ctypes.POINTER(ctypes.c_float)))
         return c, ws  # keep the array alive for the call
@@ -209,8 +210,13 @@ class QuantRows:
         return c
 
 
+def _on_host(values):
+    """The values of a sequence or tensor: of a device tensor one copy and wait, not one for each of them."""
+    return values.tolist() if isinstance(values, torch.Tensor) and values.dim() == 1 else values
+
+
 def _offsets(offsets, E: int):
-    vals = [int(x) for x in offsets]
+    vals = [int(x) for x in _on_host(offsets)]
     if len(vals) != E + 1:  # the library reads exactly E + 1 values
         raise ValueError(f"offsets has {len(vals)} values; a grouped call over {E} experts needs {E + 1}")
     return (ctypes.c_int64 * len(vals))(*vals), vals

@@ -43,3 +43,22 @@ def test_nvfp4_tensor_scales(ws2):
     c, keep = w._c()
     assert [c.ws2[e] for e in range(E)] == [0.5, 0.25, 2.0] and len(keep) == E
     assert w.expert(2).ws2 == 2.0
+
+
+class Reads(torch.utils._python_dispatch.TorchDispatchMode):
+    """Counts single elements read from tensors: each is a copy and a wait where the tensor is on a device."""
+    count = 0
+
+    def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+        self.count += func is torch.ops.aten._local_scalar_dense.default
+        return func(*args, **(kwargs or {}))
+
+
+def test_tensors_are_read_at_once():
+    """Tensor scales and offsets that are tensors come to the host as a whole, not value by value."""
+    w = weight(pkg.NVFP4, torch.tensor([0.5, 0.25, 2.0]))
+    with Reads() as reads:
+        c, _ = w._c()
+        _, vals = pkg._lib._offsets(torch.tensor([0, 4, 4, 9]), E)
+    assert reads.count == 0
+    assert [c.ws2[e] for e in range(E)] == [0.5, 0.25, 2.0] and vals == [0, 4, 4, 9]
