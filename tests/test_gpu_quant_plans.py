@@ -1,0 +1,70 @@
+"""4-bit products at the sizes of tests/quant_shapes.py: rings of an odd number of slots that are gone through again,
+experts on the pair kernel captured and replayed."""
+import pytest
+import torch
+
+import quant_ref as ref
+import quant_shapes as shapes
+from test_gpu_quant_products import check_dense, check_grouped, close, decoded, h, weight  # noqa: F401
+
+pkg = pytest.importorskip("paper_2609_04526_gb300")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("case", shapes.THREE_SLOTS + shapes.FIVE_SLOTS, ids=lambda c: f"{c[0]}-{len(c[1])}-{c[2]}-{c[3]}")
+def test_experts_in_odd_rings(h, case):  # noqa: F811
+    fmt, counts, N, K = case
+    check_grouped(h, fmt, counts, N, K, seed=K + len(counts))
+    if fmt == pkg.NVFP4:
+        check_grouped(h, fmt, counts, N, K, seed=K + 1, signs=True)
+
+
+@pytest.mark.parametrize("case", shapes.THREE_SLOTS_DENSE)
+def test_dense_products_in_odd_rings(h, case):  # noqa: F811
+    check_dense(h, *case, seed=sum(case))
+    if case[0] == pkg.NVFP4:
+        check_dense(h, *case, seed=sum(case) + 1, signs=True)
+
+
+@pytest.mark.parametrize("case", shapes.PAIR_EXPERTS)
+def test_pair_experts_captured_and_replayed_with_other_offsets(h, case):  # noqa: F811
+    """A captured product by expert follows the rows and offsets that a replay finds: unequal ones, all rows one
+    expert's, none of some, rows of no expert behind the last."""
+    fmt, counts, N, K = case
+    g = torch.Generator(device="cuda").manual_seed(23)
+    E, R = len(counts), sum(counts)
+    codes, scales = weight(g, fmt, (E, N), K)
+    w = pkg.GroupedWeight(fmt, E, N, K, codes, scales, None if fmt == pkg.MXFP4 else torch.rand(E, generator=g, device="cuda") + 0.5)
+    X = torch.randn(R, K, generator=g, device="cuda").bfloat16()
+    offsets = torch.tensor([0, *torch.tensor(counts).cumsum(0).tolist()], device="cuda")
+    Y = torch.zeros(R, N, dtype=torch.bfloat16, device="cuda")
+    side = torch.cuda.Stream()
+
+    def step():
+        h.sq_grouped_quant_fwd(w, offsets, h.sq_quantize(fmt, X), Y=Y)
+
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for ends in (counts, [0, R, 0, 0], [1, 223, 225, R - 449], [R - 1000, 0, 0, 300], [0, 0, 0, 0]):
+        X.copy_(torch.randn(R, K, generator=g, device="cuda"))
+        offsets.copy_(torch.tensor([0, *torch.tensor(ends).cumsum(0).tolist()]))
+        Y.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = Y.clone()
+        Y.fill_(7.0)
+        step()
+        h.sq_sync()
+        assert torch.equal(got, Y) and (got[sum(ends):] == 7.0).all()
+        x = decoded(h.sq_quantize(fmt, X))
+        first = 0
+        for e, n in enumerate(ends):
+            if n:
+                v = ref.values(fmt, codes[e].cpu(), scales[e].cpu()) * (1.0 if w.ws2 is None else float(w.ws2[e]))
+                close(got[first:first + n], x[first:first + n], v, f"{ends} expert {e}")
+            first += n
