@@ -17,3 +17,7 @@ THREE_SLOTS_DENSE = [(fmt, 1900, 2056, 2048) for fmt in FORMATS] + [(fmt, 400, 9
 FIVE_SLOTS = [(fmt, [1 + e % 2 for e in range(60)], 520, K) for fmt in FORMATS for K in (4096, 4128)]
 # pair kernel by expert: several tiles of a CTA pair
 PAIR_EXPERTS = [(fmt, [2000, 0, 2500, 1500], 2056, 544) for fmt in FORMATS]
+# pair kernel, tiles of 240 or 256 rows, three and more of them for some CTA pairs; one or (MXFP4) two slices a stage
+TALL = [(fmt, R, N, K) for fmt in FORMATS for R, N, K in ((704, 15616, 2080), (720, 15616, 4128), (461, 38216, 2080))]
+# ... with a last tile of 32 rows or fewer, two tiles of a CTA pair
+TALL_AND_SHORT = [(NVFP4, 3361, 2552, 2880), (MXFP4, 4638, 1824, 8224)]

@@ -1,5 +1,5 @@
 """4-bit products at the sizes of tests/quant_shapes.py: rings of an odd number of slots that are gone through again,
-experts on the pair kernel captured and replayed."""
+tall tiles whose accumulators are used again, experts on the pair kernel captured and replayed."""
 import pytest
 import torch
 
@@ -24,6 +24,17 @@ def test_dense_products_in_odd_rings(h, case):  # noqa: F811
     check_dense(h, *case, seed=sum(case))
     if case[0] == pkg.NVFP4:
         check_dense(h, *case, seed=sum(case) + 1, signs=True)
+
+
+@pytest.mark.parametrize("case", shapes.TALL + shapes.TALL_AND_SHORT)
+def test_tall_tiles_use_their_accumulators_again(h, case):  # noqa: F811
+    """The third tile of a CTA pair, whose accumulator shares columns with the two before it, and later ones."""
+    check_dense(h, *case, seed=sum(case))
+
+
+@pytest.mark.parametrize("case", [c for c in shapes.TALL + shapes.TALL_AND_SHORT if c[0] == pkg.NVFP4])
+def test_tall_tiles_with_negative_scales(h, case):  # noqa: F811
+    check_dense(h, *case, seed=sum(case) + 1, signs=True)
 
 
 @pytest.mark.parametrize("case", shapes.PAIR_EXPERTS)

@@ -35,3 +35,17 @@ def test_experts_of_the_pair_kernel():
     for c in shapes.PAIR_EXPERTS:
         p = experts(c, 0)
         assert p.pair and p.units > 2 * fp4_plan.SMS // 2, p
+
+
+def test_tall_tiles_three_and_more_of_a_pair():
+    plans = [dense(c) for c in shapes.TALL]
+    assert all(p.pair and p.tile_tokens > 224 and p.units > 2 * (fp4_plan.SMS // 2) for p in plans), plans
+    assert any(p.units > 3 * (fp4_plan.SMS // 2) for p in plans)
+    assert {(c[0], p.slices) for c, p in zip(shapes.TALL, plans)} == {(0, 1), (1, 1), (1, 2)}
+    assert {p.tile_tokens for p in plans} == {240, 256}
+
+
+def test_tall_tiles_before_a_short_one():
+    for c in shapes.TALL_AND_SHORT:
+        p = dense(c)
+        assert p.pair and p.tile_tokens > 224 and p.units > fp4_plan.SMS // 2 and 0 < c[1] % p.tile_tokens <= 32, p
