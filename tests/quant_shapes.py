@@ -21,3 +21,5 @@ PAIR_EXPERTS = [(fmt, [2000, 0, 2500, 1500], 2056, 544) for fmt in FORMATS]
 TALL = [(fmt, R, N, K) for fmt in FORMATS for R, N, K in ((704, 15616, 2080), (720, 15616, 4128), (461, 38216, 2080))]
 # ... with a last tile of 32 rows or fewer, two tiles of a CTA pair
 TALL_AND_SHORT = [(NVFP4, 3361, 2552, 2880), (MXFP4, 4638, 1824, 8224)]
+# one part of the contraction, thousands of steps long
+LONG = [(NVFP4, 1500, 2600, 1 << 18), (MXFP4, 1500, 2600, 1 << 18)]

@@ -1,5 +1,5 @@
 """4-bit products at the sizes of tests/quant_shapes.py: rings of an odd number of slots that are gone through again,
-tall tiles whose accumulators are used again, experts on the pair kernel captured and replayed."""
+tall tiles whose accumulators are used again, experts on the pair kernel captured and replayed, long sums."""
 import pytest
 import torch
 
@@ -79,3 +79,18 @@ def test_pair_experts_captured_and_replayed_with_other_offsets(h, case):  # noqa
                 v = ref.values(fmt, codes[e].cpu(), scales[e].cpu()) * (1.0 if w.ws2 is None else float(w.ws2[e]))
                 close(got[first:first + n], x[first:first + n], v, f"{ends} expert {e}")
             first += n
+
+
+@pytest.mark.parametrize("fmt, R, N, K", shapes.LONG)
+def test_long_sums(h, fmt, R, N, K):  # noqa: F811
+    """Sums of 2^18 products, all of one sign: a few rows and features over and over, the same bits wherever they lie."""
+    g = torch.Generator(device="cuda").manual_seed(24)
+    few, some = 20, 26
+    codes, scales = weight(g, fmt, (some,), K)
+    x_codes, x_scales = weight(g, fmt, (few,), K)
+    codes, x_codes = codes & 0x77, x_codes & 0x77
+    q = pkg.QuantRows(fmt, R, K, x_codes.repeat(R // few, 1), x_scales.repeat(R // few, 1))
+    Y = h.sq_quant_fwd(pkg.QuantWeight(fmt, N, K, codes.repeat(N // some, 1), scales.repeat(N // some, 1), 1.0), q)
+    h.sq_sync()
+    assert torch.equal(Y, Y[:few, :some].repeat(R // few, N // some))
+    close(Y[:few, :some], ref.values(fmt, x_codes.cpu(), x_scales.cpu()), ref.values(fmt, codes.cpu(), scales.cpu()))

@@ -49,3 +49,9 @@ def test_tall_tiles_before_a_short_one():
     for c in shapes.TALL_AND_SHORT:
         p = dense(c)
         assert p.pair and p.tile_tokens > 224 and p.units > fp4_plan.SMS // 2 and 0 < c[1] % p.tile_tokens <= 32, p
+
+
+def test_long_sums_in_one_part():
+    for c in shapes.LONG:
+        p = dense(c)
+        assert p.splits == 1, p
