@@ -550,7 +550,7 @@ typedef struct {
  *   E2M1(x / s), saturating at 6.
  * A block that holds an infinity or NaN gets scale byte 0x7F (NVFP4) or 0xFF, NaN, whatever its codes,
  * and has no part in its row's own scale.
- * X device bf16 [T, K]. slot_of device int32 [R] or NULL: NULL, R == T and row r is X[r]; else row r
+ * X device bf16 [T, K]. slot_of device int32 [R] or NULL: NULL, R == T (or 0) and row r is X[r]; else row r
  * is X[slot_of[r] / k] (1 <= k <= 32, T * k < 2^31), the row that sq_dispatch would copy there, and a row whose slot
  * is outside [0, T * k) is a row of zeros. Where many rows are of few tokens, the tokens are quantised once,
  * into scratch of the handle (T rows), and copied; a graph capture that finds no scratch quantises row by

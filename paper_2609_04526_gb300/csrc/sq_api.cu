@@ -1781,7 +1781,7 @@ sq_status sq_quantize(sq_handle h, const sq_rows *q, int64_t T, int32_t k, const
     if (k < 1 || k > sqi::kRouteMaxK) return fail(h, SQ_ERR_INVALID_ARG, "k=%d must be in [1, 32]", k);
     if (T > kMaxTokens / k) return fail(h, SQ_ERR_INVALID_ARG, "T=%lld: T * k must be in [0, 2^31)", (long long)T);
     SQ_TRY(check_elements(h, slot_of, "slot_of"));
-  } else if (q->R != T) {
+  } else if (q->R != T && q->R > 0) {  // no slots have no address
     return fail(h, SQ_ERR_INVALID_ARG, "R=%lld rows of T=%lld tokens without slot_of", (long long)q->R, (long long)T);
   }
   if (!q->row_ws2 && !(q->ws2 >= 0x1p-126f && q->ws2 <= 0x1p126f))
