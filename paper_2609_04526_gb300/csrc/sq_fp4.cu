@@ -9,18 +9,17 @@
 // of rows l, l + 32, l + 64 and l + 96 side by side in line l. For many tokens a launch ahead lays both
 // planes out as atoms, which TMA then brings like the codes; for few, TMA brings 16 bytes of each row
 // and a warp turns them into atoms, in place, or, where rows are not whole 16-byte pieces (K / 16 or K /
-// 32 not a multiple of 16) and have no TMA descriptor, loads them itself. (Turned in the pair kernel
-// too, a stage took 750 cycles whatever its MMAs: 390 ns with tiles of 128, 160, 192 and 224 features
-// alike. Loaded by warps 1,600: such loads take 37 wavefronts each, the lanes' rows being different
-// lines, and the proxy fence behind the atoms waits for the loads that run ahead. So where warps load
-// it is the reader that executes the fence, behind the barrier.)
+// 32 not a multiple of 16) and have no TMA descriptor, loads them itself. (A stage of many tokens takes 550
+// to 650 cycles with atoms; turned by a warp 750, whatever its MMAs; loaded by warps 1,600: such loads take 37
+// wavefronts each, the lanes' rows being different lines, and the proxy fence behind the atoms waits for the
+// loads that run ahead. So where warps load it is the reader that executes the fence, behind the barrier.)
 //
 // The tensor cores take E4M3 scales without a sign. A negative scale byte (training may drive one below
 // zero) goes in as its magnitude, and the codes of its block, in shared memory by then, change their
 // signs.
 //
 // A stage is a slice of the contraction 256 deep, 128 bytes of codes and 16 (NVFP4) or 8 (MXFP4) scale bytes of
-// each row, or, in dense products of the pair kernel, two slices.
+// each row, or, in most dense products of the pair kernel, two slices (fp4_plan).
 #include <type_traits>
 
 #include "sq_gemm_kernels.cuh"
@@ -690,12 +689,14 @@ __global__ void __launch_bounds__(Fp4FewCfg::kThreads, 2)
 // A cluster of two CTAs per tile of 256 features and up to 256 tokens, 224 of an expert (tcgen05.mma.cta_group::2): each CTA
 // holds the codes of 128 of the features and half of the tokens, the atoms of its features and those of
 // all the tokens. The tokens are the MMA's N, of any multiple of 16: an expert's rows, cut into equal
-// tiles, cost what they are. (With tokens as the 256 rows of a tile 32444 rows of 128 experts of 2880 x 2880
-// took 171 us, 157 so.) Persistent, with two accumulators, so a tile's epilogue runs under the next one's MMAs.
+// tiles, cost what they are (32444 rows of 128 experts of 2880 x 2880: 157 us, and 171 with the tokens as the 256 rows of
+// a tile). Persistent, with two accumulators, so a tile's epilogue runs under the next one's MMAs.
 //
 // A launch ahead (sq_fp4_atoms_kernel) writes the atoms: of each token tile two blocks of 128 rows (the second
 // of fewer), of each feature tile two, for every stage, and whether it met a negative scale.
-// Only then the pair kernel has a warp that mends the codes of each stage before the MMAs may read it.
+// Only then the pair kernel has a warp that mends the codes of each stage before the MMAs may read it: every stage of
+// the launch, for one negative byte anywhere. That warp is slower than the MMAs (16384 x 14336 x 4096 309 us, 1765 with
+// one such byte, 4684 with half of them).
 
 struct Fp4PairCfg {
   static constexpr int kEpiWarps = 8;  // 32 features w % 4, every other 32 tokens from w / 4 on
@@ -707,7 +708,8 @@ struct Fp4PairCfg {
 };
 // Tensor memory: two accumulators and, behind them, 48 columns of a slice's scales. Those of wide tiles overlap, the
 // second begins at column 208: the epilogue reads the columns that both use before the others, and the MMAs of the
-// next tile wait for that much of it, some 2,500 cycles a tile (estimated from products of 16 and 32 slices).
+// next tile wait for that much of it, some 2,500 cycles a tile (estimated from products of 16 and 32 slices;
+// fp4_pair_tokens charges 1.23 times the tile's own time).
 constexpr int kPairOver = 208, kPairScales = 464;
 static_assert(2 * kFp4PairApart <= kPairScales && kPairOver + kFp4PairTokens <= kPairScales && kPairScales + 48 <= 512 &&
                   kFp4PairTokens - kPairOver <= 64 && kPairOver % 16 == 0,

@@ -486,8 +486,8 @@ struct QuantArgs {
 cudaError_t launch_quantize(int fmt, const QuantArgs &a, int sm_count, cudaStream_t stream);
 cudaError_t launch_spread(int fmt, const QuantArgs &a, const QuantArgs &tokens, cudaStream_t stream);
 // R rows by slot of T tokens: whether to quantise each token once and copy its row. Quantising is bound by its
-// arithmetic where rows come from the L2, 2.3 (NVFP4) or 3.6 values in a picosecond; a copied value costs a third of that, and
-// the second launch about 2 us. Measured, one launch against two, in us: NVFP4, 2048 values a row, 512 tokens of 8 rows
+// arithmetic where rows come from the L2, 2.3 (NVFP4) or 3.6 values in a picosecond; a copied value costs a third (NVFP4) or
+// a half of that, and the second launch about 2 us. Measured, one launch against two, in us: NVFP4, 2048 values a row, 512 tokens of 8 rows
 // each 5.3 against 5.5, 2048 of 2 5.3 and 7.3, 2048 of 8 15.0 and 9.4, 8192 of 2 15.0 and 13.2; MXFP4, 2880 values, 2048
 // tokens of 4 8.1 and 6.7, 8192 of 4 30.7 and 21.8, 2048 of 8 14.7 and 8.6.
 inline bool quantize_tokens_first(int fmt, int64_t R, int64_t T, int K) {
@@ -555,10 +555,14 @@ constexpr size_t fp4_pair_smem(int fmt, int slices, bool wide, int stages, int E
 }
 // Tokens of a whole tile of a dense product. The launch lasts as long as its waves of tiles, 400 + 1.15 h
 // cycles a slice of a tile of h tokens (fitted; the MMAs alone take 2 h) and 1.23 times that where accumulators overlap (of
-// 8 to 56 slices; of fewer the wait between tiles weighs more).
-// In us, with the tokens' quantisation: 2048 tokens against 4096 x 14336 NVFP4 in two waves of 240 65, in three of 224 and a
-// last one of 32 69, in ten tiles of 208 73; 1024 against 8192 x 8192 in 256 39, in 224 41; 4096 against 4096 x 4096, four
-// waves either way, in 256 46, in 224 40.
+// 8 slices on; of fewer the wait between tiles weighs more). The factor is that wait in a tile of about 16 slices, charged
+// by the slice: a deeper tile waits no longer, so it keeps some tall tiles from products that they would suit.
+// The product alone in us, in tiles of 224 or fewer against 240 or 256, the taken side first. NVFP4: 1024 tokens against 8192
+// x 2048 in 256 18.5, in 160 19.7; 2048 against 4096 x 2048 in 240 18.4, in 224 19.4; 1024 against 8192 x 8192 in 256 33.6, in
+// 224 36.5; 2048 against 4096 x 14336 in 240 48.3, in 224 51.3; 4096 against 4096 x 4096 in 224 31.5, in 256 35.5. It
+// misses 1000 against 8192 x 14336 in 144 59.0, in 256 51.7, 2048 against 14336 x 14336 in 224 174, in 256 156, and of MXFP4,
+// whose shallow tiles of up to 224 have two slices a stage, 1024 against 8192 x 2048 in 256 18.0, in 160 17.2 and 2048
+// against 4096 x 2048 in 240 17.9, in 224 16.7.
 inline int fp4_pair_tokens(int64_t R, int64_t ftiles, int clusters, int slices) {
   auto cost = [](int64_t h) { return h > kFp4PairApart ? 1.23 * (400 + 1.15 * h) : h > 0 ? 400 + 1.15 * h : 0.0; };
   double best = 0;
@@ -566,15 +570,17 @@ inline int fp4_pair_tokens(int64_t R, int64_t ftiles, int clusters, int slices) 
   for (int h = slices >= 8 ? kFp4PairTokens : kFp4PairApart; h >= 96; h -= 16) {
     const int64_t whole = R / h * ftiles, rest = R % h ? ftiles : 0, waves = (whole + clusters - 1) / clusters;
     const int64_t left = waves * clusters - whole;
-    const double us = waves * cost(h) + (rest > left ? (rest - left + clusters - 1) / clusters * cost(R % h) : 0.0);
-    if (best == 0 || us < best) {
-      best = us;
+    const double cycles = waves * cost(h) + (rest > left ? (rest - left + clusters - 1) / clusters * cost(R % h) : 0.0);
+    if (best == 0 || cycles < best) {
+      best = cycles;
       tokens = h;
     }
   }
   return tokens;
 }
-// Clusters of 1 .. 8 CTAs of the few-token kernel that a device runs at once, a CTA alone on its SM or two on one.
+// Clusters of 1 .. 8 CTAs of the few-token kernel that a device runs at once, a CTA alone on its SM or two on one. (Driver
+// 580 counts one CTA of this kernel to an SM, whatever its shared memory, though two do run there: both counts are 152, 76,
+// 46, 36, 28, 23, 15 and 15 clusters, and a cut product is one CTA to an SM.)
 struct Fp4Clusters {
   int alone[9], shared[9];  // alone[0] == 0: not asked yet
 };
@@ -625,9 +631,9 @@ inline void fp4_plan(int fmt, int sm_count, const Fp4Clusters &fit, Fp4Args &p) 
     p.units = token_tiles * p.ftiles;
     p.whole = static_cast<int>(p.R / pair_tokens);
     // Two slices a stage halve the waits, commits and loads (one, two; us with the tokens' quantisation: 16384 x 14336
-    // x 4096 NVFP4 352, 340, 2048 x 4096 x 14336 74, 70, MXFP4 68, 63). Experts' narrow tiles wait for their loads and
+    // x 4096 NVFP4 352, 340, 2048 x 4096 x 14336 MXFP4 68, 63). Experts' narrow tiles wait for their loads and
     // want the finer ring (8111 tokens to four of 128 of 2880 x 2880 200, 204). An odd slice behind K is computed as
-    // zeros: not where it would be more than a 17th of all.
+    // zeros: not where it would be more than a 17th of all. Of tall NVFP4 tiles only two such stages would fit.
     p.slices = !p.offsets && (cnt % 2 == 0 || cnt > 16) && (fmt == 1 || pair_tokens <= kFp4PairApart) ? 2 : 1;
     p.depth = (cnt + p.slices - 1) / p.slices;
     p.token_blocks = static_cast<int>(2 * token_tiles);
