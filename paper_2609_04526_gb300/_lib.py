@@ -777,8 +777,8 @@ class Handle:
     def sq_grouped_quant_fwd(self, w: GroupedWeight, offsets: torch.Tensor, q: QuantRows, Y: Optional[torch.Tensor] = None,
                            stream=None):
         """Y rows offsets[e]..offsets[e+1]-1 = X rows of expert e times W_e^T, both in 4 bits; the other rows of
-        Y are left as they are (zeros of a new one). offsets int64 [E + 1] and, NVFP4, w.ws2 fp32 [E] are on the
-        device: nothing comes back to the host, and a graph can capture the call."""
+        Y are left as they are (zeros of a new one, which is zeroed whole first). offsets int64 [E + 1] and, NVFP4,
+        w.ws2 fp32 [E] are on the device: nothing comes back to the host, and a graph can capture the call."""
         c, dev = q._c(None, stream, True), q.codes.device
         if Y is None:
             Y = _empty(stream, q.R, w.N, dtype=torch.bfloat16, device=dev)

@@ -578,9 +578,9 @@ inline int fp4_pair_tokens(int64_t R, int64_t ftiles, int clusters, int slices) 
   }
   return tokens;
 }
-// Clusters of 1 .. 8 CTAs of the few-token kernel that a device runs at once, a CTA alone on its SM or two on one. (Driver
-// 580 counts one CTA of this kernel to an SM, whatever its shared memory, though two do run there: both counts are 152, 76,
-// 46, 36, 28, 23, 15 and 15 clusters, and a cut product is one CTA to an SM.)
+// Clusters of 1 .. 8 CTAs of the few-token kernel that a device runs at once, a CTA alone on its SM or two on one. (CUDA
+// 13.0 counts one CTA of this kernel to an SM, whatever its shared memory, though two do run there: both counts are 152,
+// 76, 46, 36, 28, 23, 15 and 15 clusters, and a cut product is one CTA to an SM.)
 struct Fp4Clusters {
   int alone[9], shared[9];  // alone[0] == 0: not asked yet
 };
